@@ -307,6 +307,119 @@ int pb_mlp_run_static(const int32_t* sizes, int n_sizes, float lr, float momentu
                       float* dev_w, float* dev_v, const float* dev_xs, const int32_t* dev_labels,
                       int n_ticks, float* dev_losses, void* stream);
 
+/* ---- Token operators: the two ends of a model over tokens, and the optimizer such
+ * models are trained with.  They work on the caller's device memory, keep nothing
+ * between calls, allocate nothing, do not synchronise and can be captured into a CUDA
+ * graph.  All pointers belong to the device that is current at the call, on which
+ * `stream` lives; pointers need the alignment of one element.  Errors: status code,
+ * text via pb_last_error(NULL) on the same thread.  Sizes are checked before anything is
+ * launched.
+ *
+ * Token ids are int32 or int64 (`id_bytes` 4 or 8).  The id -1 stands for "no token"
+ * (padding).  Any other id outside [0, vocab) is treated like -1 and, where dev_status is
+ * not NULL, *dev_status is set to 1 (the caller clears it). */
+typedef enum { PB_F32 = 0, PB_BF16 = 1, PB_F16 = 2 } pb_dtype;
+
+/* out[t, :] = scale * table[id_t, :], rounded once; a zero row where there is no token.
+ * table: [vocab, dim] with row stride ld_table, out: [n_tokens, dim] with row stride
+ * ld_out, both of `dtype`; columns between dim and the stride are left alone.  n_tokens
+ * == 0 is a no-op.  PB_E_ARG if out overlaps the table. */
+int pb_embed_forward(const void* dev_table, int dtype, int64_t vocab, int64_t dim, int64_t ld_table,
+                     const void* dev_ids, int id_bytes, int64_t n_tokens, float scale,
+                     void* dev_out, int64_t ld_out, int32_t* dev_status, void* stream);
+
+/* Its gradient: with S_v = sum of dout[t, :] over the t with id_t = v (float32, in an order
+ * that depends on the ids alone), dtable[v, :] = scale * S_v, rounded once.  accumulate = 0
+ * writes every row (zeros where no token points); accumulate = 1 adds to what is there (a
+ * gradient over several batches; the gradient of a table that is also the output head) and
+ * leaves rows without tokens untouched.  padding_idx: a row that gets no gradient, or -1.
+ * dtable is float32 or of dout's type.  dev_scratch: pb_embed_scratch_bytes(...) bytes,
+ * 256-byte aligned, not used by another call that may run at the same time (two captured
+ * graphs included). */
+size_t pb_embed_scratch_bytes(int64_t n_tokens, int64_t vocab, int64_t dim);
+int pb_embed_backward(const void* dev_dout, int dtype, int64_t ld_dout, const void* dev_ids, int id_bytes,
+                      int64_t n_tokens, int64_t vocab, int64_t dim, float scale, int64_t padding_idx,
+                      void* dev_dtable, int dtable_dtype, int64_t ld_dtable, int accumulate,
+                      void* dev_scratch, size_t scratch_bytes, int32_t* dev_status, void* stream);
+
+/* Log probabilities of one given token per row, with the row's entropy and its most probable
+ * alternatives.  logits: [rows, vocab], row stride ld.  With p = softmax(inv_temperature *
+ * logits[r, :]):
+ *   logp[r] = log p[token_r] (0 where there is no token), entropy[r] = -sum p log p,
+ *   lse[r] = log sum exp(inv_temperature * logits[r, :]),
+ *   top_ids / top_logp [rows, top_k]: the top_k largest logits in descending order, the
+ *   lower index first among equal ones, and their log probabilities (top_k <= 32).
+ * dev_logp and dev_tokens are given together or not at all; entropy and lse may be NULL.
+ * Logits of -inf are tokens that cannot occur.  Places of the alternatives beyond the last
+ * finite logit hold -1 and -inf.  A row whose logits are all -inf has lse and logp -inf,
+ * entropy 0 and no alternatives.  A row with a NaN or +inf has NaN everywhere and ids -1. */
+int pb_logprob_forward(const void* dev_logits, int dtype, int64_t rows, int64_t vocab, int64_t ld,
+                       const void* dev_tokens, int token_bytes, double inv_temperature,
+                       float* dev_logp, float* dev_entropy, float* dev_lse,
+                       int top_k, float* dev_top_logp, int32_t* dev_top_ids, int32_t* dev_status, void* stream);
+
+/* Gradient with respect to the logits, from lse (and entropy, where its gradient is given) of
+ * the forward call and the gradients of the three row values ([rows] float32, any may be
+ * NULL):  dlogits[r, i] = inv_temperature * ( g_logp (1[i = token] - p_i)
+ *                          - g_entropy p_i (log p_i + entropy) + g_lse p_i ).
+ * dlogits: [rows, vocab] of the logits' type, row stride ld_d; the logits' own buffer (same
+ * pointer and stride) is allowed, any other overlap is PB_E_ARG.  Rows without a finite logit
+ * have gradient zero.  Like softmax_ce at the end of a stage list, but over rows of the
+ * caller's memory. */
+int pb_logprob_backward(const void* dev_logits, int dtype, int64_t rows, int64_t vocab, int64_t ld,
+                        const void* dev_tokens, int token_bytes, double inv_temperature,
+                        const float* dev_lse, const float* dev_entropy,
+                        const float* dev_g_logp, const float* dev_g_entropy, const float* dev_g_lse,
+                        void* dev_dlogits, int64_t ld_d, int32_t* dev_status, void* stream);
+
+/* One AdamW step over n_tensors tensors:
+ *   g = grad * *dev_grad_scale,  m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2,
+ *   u = (m / (1 - beta1^step)) / (sqrt(v / (1 - beta2^step)) + eps),
+ *   w = w (1 - lr weight_decay) - lr u,   w_forward = w - lr horizon u (if not NULL).
+ * Weights are float32; gradients are of grad_dtype, w_forward of forward_dtype: the copy of
+ * the weights that the forward computes with, predicted `horizon` steps ahead as linear
+ * weight prediction does (horizon 0: a plain copy; a stage of delay D uses D).
+ * state_bits 32: m and v are float32.  state_bits 8: m and v are one byte per element and
+ * m_scale / v_scale one float32 per 256 elements of the tensor (ceil(n / 256)); zero bytes and
+ * scales are a fresh state.  m is held as e4m3, sqrt(v) as an unsigned float of 4 exponent and 4
+ * mantissa bits, rounded at random by `seed`, the step number, the tensor's place in the list
+ * and the element: the same call gives the same result.  A block of 256 with a moment that is
+ * not finite reads back as NaN.
+ * *dev_grad_scale (device, NULL: 1) is the product of whatever clipping and loss scaling leave;
+ * if it is not finite the step changes nothing.  dev_lr and dev_step (device, may be NULL) take
+ * the place of lr and step, so that a captured graph can be replayed with other values.  Tensors
+ * of a call must not overlap (not checked here). */
+typedef struct {
+    float* w;
+    void* m;
+    void* v;
+    float* m_scale;
+    float* v_scale;
+    void* w_forward;
+    int64_t n;
+    float weight_decay;
+    float horizon;
+} pb_adamw_tensor;
+
+typedef struct {
+    double lr, beta1, beta2, eps;
+    int64_t step;              /* 1 for the first step                                   */
+    uint64_t seed;
+    const float* dev_grad_scale;
+    const float* dev_lr;
+    const int64_t* dev_step;
+    int32_t grad_dtype;
+    int32_t forward_dtype;
+    int32_t state_bits;
+} pb_adamw_args;
+
+int pb_adamw_step(const pb_adamw_tensor* tensors, const void* const* dev_grads, int n_tensors,
+                  const pb_adamw_args* args, void* stream);
+
+/* The float32 moments that an 8-bit state of n elements stands for (either output may be NULL). */
+int pb_adamw_moments(const void* dev_m, const float* dev_m_scale, const void* dev_v, const float* dev_v_scale,
+                     int64_t n, float* dev_m_out, float* dev_v_out, void* stream);
+
 const char* pb_last_error(const pb_handle* h);
 void pb_destroy(pb_handle* h);
 

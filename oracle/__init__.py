@@ -18,6 +18,6 @@ per-sample replay of every gradient from logged weight versions.
 """
 from .optimizer import StageOptimizer, sc_coefficients
 from .pipeline import PBOracle
-from . import layers
+from . import layers, tokens
 
-__all__ = ["StageOptimizer", "sc_coefficients", "PBOracle", "layers"]
+__all__ = ["StageOptimizer", "sc_coefficients", "PBOracle", "layers", "tokens"]

@@ -22,6 +22,8 @@ EXPORTS = [
     "pb_profile_ms", "pb_last_error", "pb_destroy", "pb_mlp_run_static", "pb_set_mitigation",
     "pb_set_update_size", "pb_kernel_min_bytes", "pb_bench_l2_bandwidth", "pb_bench_fp32_fma",
     "pb_split_plan", "pb_create_split", "pb_split_range", "pb_split_ports", "pb_split_connect",
+    "pb_embed_forward", "pb_embed_scratch_bytes", "pb_embed_backward", "pb_logprob_forward",
+    "pb_logprob_backward", "pb_adamw_step", "pb_adamw_moments",
 ]
 
 
@@ -32,6 +34,18 @@ class pb_layer(C.Structure):
 
 class pb_split_port(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("act", "act_stamp", "grad", "grad_stamp")]
+
+
+class pb_adamw_tensor(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("w", "m", "v", "m_scale", "v_scale", "w_forward")] + \
+               [("n", C.c_int64), ("weight_decay", C.c_float), ("horizon", C.c_float)]
+
+
+class pb_adamw_args(C.Structure):
+    _fields_ = [(n, C.c_double) for n in ("lr", "beta1", "beta2", "eps")] + \
+               [("step", C.c_int64), ("seed", C.c_uint64)] + \
+               [(n, C.c_void_p) for n in ("dev_grad_scale", "dev_lr", "dev_step")] + \
+               [(n, C.c_int32) for n in ("grad_dtype", "forward_dtype", "state_bits")]
 
 
 class PBError(RuntimeError):
@@ -93,6 +107,15 @@ def load_library():
     lib.pb_split_ports.argtypes = [vp, C.POINTER(pb_split_port)]
     lib.pb_split_connect.argtypes = [vp, C.POINTER(pb_split_port), C.POINTER(pb_split_port)]
     lib.pb_mlp_run_static.argtypes = [C.POINTER(C.c_int32), i32, f32, f32, C.c_uint, vp, vp, vp, vp, i32, vp, vp]
+    i64 = C.c_int64
+    lib.pb_embed_forward.argtypes = [vp, i32, i64, i64, i64, vp, i32, i64, f32, vp, i64, vp, vp]
+    lib.pb_embed_scratch_bytes.argtypes = [i64, i64, i64]
+    lib.pb_embed_scratch_bytes.restype = C.c_size_t
+    lib.pb_embed_backward.argtypes = [vp, i32, i64, vp, i32, i64, i64, i64, f32, i64, vp, i32, i64, i32, vp, C.c_size_t, vp, vp]
+    lib.pb_logprob_forward.argtypes = [vp, i32, i64, i64, i64, vp, i32, C.c_double, vp, vp, vp, i32, vp, vp, vp, vp]
+    lib.pb_logprob_backward.argtypes = [vp, i32, i64, i64, i64, vp, i32, C.c_double, vp, vp, vp, vp, vp, vp, i64, vp, vp]
+    lib.pb_adamw_step.argtypes = [C.POINTER(pb_adamw_tensor), C.POINTER(vp), i32, C.POINTER(pb_adamw_args), vp]
+    lib.pb_adamw_moments.argtypes = [vp, vp, vp, vp, i64, vp, vp, vp]
     _lib = lib
     return lib
 

@@ -16,7 +16,7 @@ using namespace pb;
 
 namespace {
 
-std::string g_create_error;
+thread_local std::string g_create_error;
 
 int fail(pb_handle* h, int code, const std::string& msg) {
     if (h) h->err = msg; else g_create_error = msg;
@@ -29,6 +29,23 @@ int fail(pb_handle* h, int code, const std::string& msg) {
         if (e_ != cudaSuccess)                                                        \
             return fail(h, PB_E_CUDA, std::string(#call) + ": " + cudaGetErrorString(e_)); \
     } while (0)
+
+}  // namespace
+
+namespace pb {
+
+// Errors of the entry points that have no handle (tok_api.cu).
+int fail_text(int code, const char* text) {
+    try {
+        g_create_error = text;
+    } catch (...) {
+    }
+    return code;
+}
+
+}  // namespace pb
+
+namespace {
 
 size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 

@@ -1,0 +1,258 @@
+// C entry points of the token operators and the AdamW step: argument checks and launches.
+// Nothing here allocates, and no state is kept between calls.
+#include <cmath>
+#include <cstdio>
+#include <cstring>
+
+#include "../../include/pb.h"
+#include "adamw.cuh"
+#include "tok_embed.cuh"
+#include "tok_logprob.cuh"
+
+namespace pb {
+int fail_text(int code, const char* text);      // pb_api.cu: what pb_last_error(NULL) returns
+}
+
+using namespace pb;
+
+namespace {
+
+int launched(const char* who) {
+    const cudaError_t e = cudaGetLastError();
+    if (e == cudaSuccess) return PB_OK;
+    char text[256];
+    snprintf(text, sizeof text, "%s: launch failed: %s", who, cudaGetErrorString(e));
+    return fail_text(PB_E_CUDA, text);
+}
+
+size_t dtype_bytes(int dtype) { return dtype == PB_F32 ? 4 : 2; }
+bool dtype_ok(int dtype) { return dtype == PB_F32 || dtype == PB_BF16 || dtype == PB_F16; }
+bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+
+constexpr int64_t kMaxCount = 0x7fffffff;       // rows, tokens, vocabulary, dimension
+
+// Bytes from the first element of a [rows, cols] matrix with row stride ld to behind its last.
+size_t extent(int64_t rows, int64_t cols, int64_t ld, size_t elem) {
+    return rows > 0 && cols > 0 ? ((size_t)(rows - 1) * (size_t)ld + (size_t)cols) * elem : 0;
+}
+bool overlap(const void* a, size_t na, const void* b, size_t nb) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return na && nb && x < y + nb && y < x + na;
+}
+
+}  // namespace
+
+#define PB_REFUSE(cond, text) \
+    do { if (cond) return fail_text(PB_E_ARG, text); } while (0)
+
+extern "C" {
+
+int pb_embed_forward(const void* dev_table, int dtype, int64_t vocab, int64_t dim, int64_t ld_table, const void* dev_ids,
+                     int id_bytes, int64_t n_tokens, float scale, void* dev_out, int64_t ld_out, int32_t* dev_status,
+                     void* stream) {
+    PB_REFUSE(!dtype_ok(dtype), "pb_embed_forward: unknown element type");
+    PB_REFUSE(id_bytes != 4 && id_bytes != 8, "pb_embed_forward: token ids have 4 or 8 bytes");
+    PB_REFUSE(n_tokens < 0 || n_tokens > kMaxCount, "pb_embed_forward: n_tokens out of range");
+    PB_REFUSE(vocab < 1 || vocab > kMaxCount || dim < 1 || dim > kMaxCount, "pb_embed_forward: vocab and dim must be between 1 and 2^31 - 1");
+    PB_REFUSE(ld_table < dim || ld_out < dim, "pb_embed_forward: a row stride is smaller than dim");
+    if (n_tokens == 0) return PB_OK;
+    PB_REFUSE(!dev_table || !dev_ids || !dev_out, "pb_embed_forward: NULL pointer");
+    const size_t es = dtype_bytes(dtype);
+    PB_REFUSE(!aligned(dev_table, es) || !aligned(dev_out, es) || !aligned(dev_ids, id_bytes) || !aligned(dev_status, 4),
+              "pb_embed_forward: a pointer is not aligned to its element");
+    PB_REFUSE(overlap(dev_out, extent(n_tokens, dim, ld_out, es), dev_table, extent(vocab, dim, ld_table, es)),
+              "pb_embed_forward: the output overlaps the table");
+    const cudaStream_t s = (cudaStream_t)stream;
+    auto go = [&](auto t, auto i) {
+        using T = decltype(t);
+        using I = decltype(i);
+        embed_fwd_kernel<T, I><<<(unsigned)n_tokens, 256, 0, s>>>((const T*)dev_table, vocab, dim, ld_table, (const I*)dev_ids, scale,
+                                                                  (T*)dev_out, ld_out, dev_status);
+    };
+    auto by_id = [&](auto t) { if (id_bytes == 4) go(t, int32_t()); else go(t, int64_t()); };
+    if (dtype == PB_F32) by_id(float()); else if (dtype == PB_BF16) by_id(__nv_bfloat16()); else by_id(__half());
+    return launched("pb_embed_forward");
+}
+
+size_t pb_embed_scratch_bytes(int64_t n_tokens, int64_t vocab, int64_t dim) {
+    if (n_tokens < 0 || n_tokens > kMaxCount || vocab < 1 || vocab > kMaxCount || dim < 1 || dim > kMaxCount) return 0;
+    return 256;
+}
+
+int pb_embed_backward(const void* dev_dout, int dtype, int64_t ld_dout, const void* dev_ids, int id_bytes, int64_t n_tokens,
+                      int64_t vocab, int64_t dim, float scale, int64_t padding_idx, void* dev_dtable, int dtable_dtype,
+                      int64_t ld_dtable, int accumulate, void* dev_scratch, size_t scratch_bytes, int32_t* dev_status,
+                      void* stream) {
+    PB_REFUSE(!dtype_ok(dtype) || !dtype_ok(dtable_dtype), "pb_embed_backward: unknown element type");
+    PB_REFUSE(dtable_dtype != PB_F32 && dtable_dtype != dtype, "pb_embed_backward: the table's gradient is float32 or of dout's type");
+    PB_REFUSE(id_bytes != 4 && id_bytes != 8, "pb_embed_backward: token ids have 4 or 8 bytes");
+    PB_REFUSE(n_tokens < 0 || n_tokens > kMaxCount, "pb_embed_backward: n_tokens out of range");
+    PB_REFUSE(vocab < 1 || vocab > kMaxCount || dim < 1 || dim > kMaxCount, "pb_embed_backward: vocab and dim must be between 1 and 2^31 - 1");
+    PB_REFUSE(ld_dtable < dim || ld_dout < dim, "pb_embed_backward: a row stride is smaller than dim");
+    PB_REFUSE(padding_idx < -1 || padding_idx >= vocab, "pb_embed_backward: padding_idx must be -1 or a row of the table");
+    PB_REFUSE(accumulate != 0 && accumulate != 1, "pb_embed_backward: accumulate must be 0 or 1");
+    if (n_tokens == 0 && accumulate) return PB_OK;
+    PB_REFUSE(!dev_dtable, "pb_embed_backward: NULL pointer");
+    PB_REFUSE(n_tokens > 0 && (!dev_dout || !dev_ids || !dev_scratch), "pb_embed_backward: NULL pointer");
+    PB_REFUSE(n_tokens > 0 && scratch_bytes < pb_embed_scratch_bytes(n_tokens, vocab, dim), "pb_embed_backward: scratch is smaller than pb_embed_scratch_bytes");
+    const size_t es = dtype_bytes(dtype), gs = dtype_bytes(dtable_dtype);
+    PB_REFUSE(!aligned(dev_dtable, gs) || !aligned(dev_dout, es) || !aligned(dev_ids, id_bytes) || !aligned(dev_status, 4),
+              "pb_embed_backward: a pointer is not aligned to its element");
+    PB_REFUSE(n_tokens > 0 && !aligned(dev_scratch, 256), "pb_embed_backward: scratch must be 256-byte aligned");
+    const size_t n_dt = extent(vocab, dim, ld_dtable, gs), n_do = extent(n_tokens, dim, ld_dout, es);
+    PB_REFUSE(overlap(dev_dtable, n_dt, dev_dout, n_do) || overlap(dev_scratch, scratch_bytes, dev_dtable, n_dt) ||
+              overlap(dev_scratch, scratch_bytes, dev_dout, n_do), "pb_embed_backward: buffers overlap");
+    const cudaStream_t s = (cudaStream_t)stream;
+    auto go = [&](auto t, auto g, auto i) {
+        using T = decltype(t);
+        using G = decltype(g);
+        using I = decltype(i);
+        if (!accumulate) embed_zero_kernel<G><<<(unsigned)vocab, 256, 0, s>>>((G*)dev_dtable, dim, ld_dtable);
+        if (n_tokens)
+            embed_bwd_kernel<T, G, I><<<(unsigned)n_tokens, 256, 0, s>>>((const T*)dev_dout, ld_dout, (const I*)dev_ids, n_tokens, vocab,
+                                                                         dim, scale, padding_idx, (G*)dev_dtable, ld_dtable, accumulate, dev_status);
+    };
+    auto by_id = [&](auto t, auto g) { if (id_bytes == 4) go(t, g, int32_t()); else go(t, g, int64_t()); };
+    auto by_g = [&](auto t) { if (dtable_dtype == PB_F32) by_id(t, float()); else by_id(t, t); };
+    if (dtype == PB_F32) by_id(float(), float()); else if (dtype == PB_BF16) by_g(__nv_bfloat16()); else by_g(__half());
+    return launched("pb_embed_backward");
+}
+
+int pb_logprob_forward(const void* dev_logits, int dtype, int64_t rows, int64_t vocab, int64_t ld, const void* dev_tokens,
+                       int token_bytes, double inv_temperature, float* dev_logp, float* dev_entropy, float* dev_lse, int top_k,
+                       float* dev_top_logp, int32_t* dev_top_ids, int32_t* dev_status, void* stream) {
+    PB_REFUSE(!dtype_ok(dtype), "pb_logprob_forward: unknown element type");
+    PB_REFUSE(rows < 0 || rows > kMaxCount, "pb_logprob_forward: rows out of range");
+    PB_REFUSE(vocab < 1 || vocab > kMaxCount, "pb_logprob_forward: vocab must be between 1 and 2^31 - 1");
+    PB_REFUSE(ld < vocab, "pb_logprob_forward: the row stride is smaller than vocab");
+    PB_REFUSE(!(inv_temperature > 0.0) || !std::isfinite((float)inv_temperature) || (float)inv_temperature == 0.f, "pb_logprob_forward: inv_temperature must be positive and finite");
+    PB_REFUSE(top_k < 0 || top_k > kMaxTop, "pb_logprob_forward: top_k must be between 0 and 32");
+    PB_REFUSE(top_k > vocab, "pb_logprob_forward: top_k is larger than vocab");
+    PB_REFUSE((dev_logp != nullptr) != (dev_tokens != nullptr) && rows > 0, "pb_logprob_forward: logp and tokens go together");
+    PB_REFUSE(dev_tokens && token_bytes != 4 && token_bytes != 8, "pb_logprob_forward: tokens have 4 or 8 bytes");
+    if (rows == 0) return PB_OK;
+    PB_REFUSE(!dev_logits || (top_k > 0 && (!dev_top_logp || !dev_top_ids)), "pb_logprob_forward: NULL pointer");
+    PB_REFUSE(!aligned(dev_logits, dtype_bytes(dtype)) || (dev_tokens && !aligned(dev_tokens, token_bytes)) || !aligned(dev_logp, 4) ||
+              !aligned(dev_entropy, 4) || !aligned(dev_lse, 4) || !aligned(dev_top_logp, 4) || !aligned(dev_top_ids, 4) ||
+              !aligned(dev_status, 4), "pb_logprob_forward: a pointer is not aligned to its element");
+    const cudaStream_t s = (cudaStream_t)stream;
+    auto go = [&](auto t, auto i) {
+        using T = decltype(t);
+        using I = decltype(i);
+        logprob_fwd_kernel<T, I><<<(unsigned)rows, 512, 0, s>>>((const T*)dev_logits, vocab, ld, (const I*)dev_tokens, inv_temperature, dev_logp,
+                                                                dev_entropy, dev_lse, top_k, dev_top_logp, dev_top_ids, dev_status);
+    };
+    auto by_id = [&](auto t) { if (token_bytes == 8) go(t, int64_t()); else go(t, int32_t()); };
+    if (dtype == PB_F32) by_id(float()); else if (dtype == PB_BF16) by_id(__nv_bfloat16()); else by_id(__half());
+    return launched("pb_logprob_forward");
+}
+
+int pb_logprob_backward(const void* dev_logits, int dtype, int64_t rows, int64_t vocab, int64_t ld, const void* dev_tokens,
+                        int token_bytes, double inv_temperature, const float* dev_lse, const float* dev_entropy,
+                        const float* dev_g_logp, const float* dev_g_entropy, const float* dev_g_lse, void* dev_dlogits,
+                        int64_t ld_d, int32_t* dev_status, void* stream) {
+    PB_REFUSE(!dtype_ok(dtype), "pb_logprob_backward: unknown element type");
+    PB_REFUSE(rows < 0 || rows > kMaxCount, "pb_logprob_backward: rows out of range");
+    PB_REFUSE(vocab < 1 || vocab > kMaxCount, "pb_logprob_backward: vocab must be between 1 and 2^31 - 1");
+    PB_REFUSE(ld < vocab || ld_d < vocab, "pb_logprob_backward: a row stride is smaller than vocab");
+    PB_REFUSE(!(inv_temperature > 0.0) || !std::isfinite((float)inv_temperature) || (float)inv_temperature == 0.f, "pb_logprob_backward: inv_temperature must be positive and finite");
+    if (rows == 0) return PB_OK;
+    PB_REFUSE(!dev_logits || !dev_dlogits || !dev_lse, "pb_logprob_backward: NULL pointer");
+    PB_REFUSE(dev_g_logp && !dev_tokens, "pb_logprob_backward: a gradient of logp needs the tokens");
+    PB_REFUSE(dev_g_entropy && !dev_entropy, "pb_logprob_backward: a gradient of the entropy needs the entropy");
+    PB_REFUSE(dev_tokens && token_bytes != 4 && token_bytes != 8, "pb_logprob_backward: tokens have 4 or 8 bytes");
+    const size_t es = dtype_bytes(dtype);
+    PB_REFUSE(!aligned(dev_logits, es) || !aligned(dev_dlogits, es) || (dev_tokens && !aligned(dev_tokens, token_bytes)) || !aligned(dev_lse, 4) ||
+              !aligned(dev_entropy, 4) || !aligned(dev_g_logp, 4) || !aligned(dev_g_entropy, 4) || !aligned(dev_g_lse, 4) || !aligned(dev_status, 4),
+              "pb_logprob_backward: a pointer is not aligned to its element");
+    PB_REFUSE(!(dev_logits == dev_dlogits && ld == ld_d) &&
+              overlap(dev_logits, extent(rows, vocab, ld, es), dev_dlogits, extent(rows, vocab, ld_d, es)),
+              "pb_logprob_backward: dlogits overlaps logits (the very same buffer and stride is allowed)");
+    const cudaStream_t s = (cudaStream_t)stream;
+    const int64_t per_launch = 65535;                       // rows are the grid's second dimension
+    for (int64_t r0 = 0; r0 < rows; r0 += per_launch) {
+        const unsigned nr = (unsigned)(rows - r0 < per_launch ? rows - r0 : per_launch);
+        auto go = [&](auto t, auto i) {
+            using T = decltype(t);
+            using I = decltype(i);
+            auto at = [&](const float* p) { return p ? p + r0 : nullptr; };
+            const unsigned gx = (unsigned)((vocab + 8191) / 8192);
+            logprob_bwd_kernel<T, I><<<dim3(gx, nr), 256, 0, s>>>((const T*)dev_logits + r0 * ld, vocab, ld, dev_tokens ? (const I*)dev_tokens + r0 : nullptr,
+                                                                  inv_temperature, at(dev_lse), at(dev_entropy), at(dev_g_logp), at(dev_g_entropy), at(dev_g_lse),
+                                                                  (T*)dev_dlogits + r0 * ld_d, ld_d, dev_status);
+        };
+        auto by_id = [&](auto t) { if (token_bytes == 8) go(t, int64_t()); else go(t, int32_t()); };
+        if (dtype == PB_F32) by_id(float()); else if (dtype == PB_BF16) by_id(__nv_bfloat16()); else by_id(__half());
+        const int rc = launched("pb_logprob_backward");
+        if (rc != PB_OK) return rc;
+    }
+    return PB_OK;
+}
+
+int pb_adamw_step(const pb_adamw_tensor* tensors, const void* const* dev_grads, int n_tensors, const pb_adamw_args* args, void* stream) {
+    PB_REFUSE(n_tensors < 0, "pb_adamw_step: negative tensor count");
+    PB_REFUSE(!args, "pb_adamw_step: NULL pointer");
+    PB_REFUSE(args->state_bits != 32 && args->state_bits != 8, "pb_adamw_step: states have 32 or 8 bits");
+    PB_REFUSE(!dtype_ok(args->grad_dtype) || !dtype_ok(args->forward_dtype), "pb_adamw_step: unknown element type");
+    PB_REFUSE(!(args->beta1 >= 0.0 && args->beta1 < 1.0) || !(args->beta2 >= 0.0 && args->beta2 < 1.0), "pb_adamw_step: need 0 <= beta1, beta2 < 1");
+    PB_REFUSE(!(args->lr >= 0.0) || !std::isfinite(args->lr) || !(args->eps >= 0.0) || !std::isfinite(args->eps), "pb_adamw_step: lr and eps must not be negative");
+    PB_REFUSE(args->step < 1 && !args->dev_step, "pb_adamw_step: the first step has number 1");
+    PB_REFUSE(!aligned(args->dev_grad_scale, 4) || !aligned(args->dev_lr, 4) || !aligned(args->dev_step, 8), "pb_adamw_step: a pointer is not aligned to its element");
+    if (n_tensors == 0) return PB_OK;
+    PB_REFUSE(!tensors || !dev_grads, "pb_adamw_step: NULL pointer");
+    const size_t gb = dtype_bytes(args->grad_dtype), fb = dtype_bytes(args->forward_dtype), sb = args->state_bits == 8 ? 1 : 4;
+    for (int k = 0; k < n_tensors; ++k) {
+        const pb_adamw_tensor& t = tensors[k];
+        PB_REFUSE(t.n < 0, "pb_adamw_step: negative tensor size");
+        PB_REFUSE(t.n > (int64_t)kMaxCount * kAdamChunk / 2, "pb_adamw_step: a tensor is too large");
+        PB_REFUSE(!(t.weight_decay >= 0.f) || !std::isfinite(t.weight_decay) || !std::isfinite(t.horizon), "pb_adamw_step: weight_decay must not be negative, horizon must be finite");
+        if (t.n == 0) continue;
+        PB_REFUSE(!t.w || !t.m || !t.v || !dev_grads[k], "pb_adamw_step: NULL pointer");
+        PB_REFUSE(args->state_bits == 8 && (!t.m_scale || !t.v_scale), "pb_adamw_step: an 8-bit state needs its scales");
+        PB_REFUSE(!aligned(t.w, 4) || !aligned(dev_grads[k], gb) || !aligned(t.m, sb) || !aligned(t.v, sb) || !aligned(t.m_scale, 4) ||
+                  !aligned(t.v_scale, 4) || !aligned(t.w_forward, fb), "pb_adamw_step: a pointer is not aligned to its element");
+    }
+    static_assert(sizeof(AdamTable) <= 32764, "kernel parameters");
+    AdamTable a;
+    a.lr = args->lr; a.beta1 = args->beta1; a.beta2 = args->beta2; a.eps = args->eps;
+    a.step = args->step; a.seed = args->seed;
+    a.grad_scale = args->dev_grad_scale; a.dev_lr = args->dev_lr; a.dev_step = (const long long*)args->dev_step;
+    a.grad_dtype = args->grad_dtype; a.fwd_dtype = args->forward_dtype; a.bits = args->state_bits;
+    int k = 0;
+    while (k < n_tensors) {
+        a.n = 0;
+        int64_t chunks = 0;
+        for (; k < n_tensors && a.n < kAdamMaxTensors; ++k) {
+            const pb_adamw_tensor& t = tensors[k];
+            if (t.n == 0) continue;
+            const int64_t c = (t.n + kAdamChunk - 1) / kAdamChunk;
+            if (chunks + c > kMaxCount) break;
+            AdamTensor& d = a.t[a.n++];
+            d.w = t.w; d.g = dev_grads[k]; d.m = t.m; d.v = t.v; d.m_scale = t.m_scale; d.v_scale = t.v_scale; d.fwd = t.w_forward;
+            d.n = t.n; d.decay = t.weight_decay; d.horizon = t.horizon;
+            d.rnd = (unsigned long long)k * 0xA0761D6478BD642Full;
+            d.first_chunk = (unsigned)chunks;
+            chunks += c;
+        }
+        if (a.n == 0) break;
+        adamw_kernel<<<(unsigned)chunks, 256, 0, (cudaStream_t)stream>>>(a);
+        const int rc = launched("pb_adamw_step");
+        if (rc != PB_OK) return rc;
+    }
+    return PB_OK;
+}
+
+int pb_adamw_moments(const void* dev_m, const float* dev_m_scale, const void* dev_v, const float* dev_v_scale, int64_t n,
+                     float* dev_m_out, float* dev_v_out, void* stream) {
+    PB_REFUSE(n < 0 || n > (int64_t)kMaxCount * 256, "pb_adamw_moments: size out of range");
+    if (n == 0) return PB_OK;
+    PB_REFUSE(!dev_m_out && !dev_v_out, "pb_adamw_moments: NULL pointer");
+    PB_REFUSE((dev_m_out && (!dev_m || !dev_m_scale)) || (dev_v_out && (!dev_v || !dev_v_scale)), "pb_adamw_moments: NULL pointer");
+    PB_REFUSE(!aligned(dev_m_scale, 4) || !aligned(dev_v_scale, 4) || !aligned(dev_m_out, 4) || !aligned(dev_v_out, 4),
+              "pb_adamw_moments: a pointer is not aligned to its element");
+    adamw_moments_kernel<<<(unsigned)((n + 255) / 256), 256, 0, (cudaStream_t)stream>>>(
+        (const unsigned char*)dev_m, dev_m_scale, (const unsigned char*)dev_v, dev_v_scale, n, dev_m_out, dev_v_out);
+    return launched("pb_adamw_moments");
+}
+
+}  // extern "C"

@@ -1,0 +1,247 @@
+"""Token operators and the AdamW step on torch tensors: argument marshalling only.
+
+Each function has the name and meaning of the C entry point it calls (include/pb.h) and
+works on CUDA tensors that the caller owns, on the current device.  Outputs are written in
+place; nothing is allocated, computed or synchronised here.  `stream` is a cudaStream_t as
+an integer (0: the default stream), like everywhere in this package.  Arguments that do not
+fit raise PBError with code -1 before anything is launched.
+"""
+import ctypes as C
+
+import torch
+
+from .binding import PBError, load_library, pb_adamw_args, pb_adamw_tensor
+
+_DTYPE = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+_ARG = -1
+
+
+def _refuse(who, text):
+    raise PBError(_ARG, "%s: %s" % (who, text))
+
+
+def _check(rc):
+    if rc != 0:
+        raise PBError(rc, load_library().pb_last_error(None).decode())
+
+
+def _on_device(who, device, *tensors):
+    """Every tensor given lives on `device`, the current one."""
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            _refuse(who, "every tensor must be a CUDA tensor on the current device")
+
+
+def _device(who, t):
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        _refuse(who, "every tensor must be a CUDA tensor on the current device")
+    d = t.get_device()
+    if d != torch.cuda.current_device():
+        _refuse(who, "every tensor must be a CUDA tensor on the current device")
+    return d
+
+
+def _rows(who, name, t, dtypes=_DTYPE):
+    """(rows, columns, row stride) of a matrix whose rows are dense."""
+    if t.dim() != 2 or t.dtype not in dtypes:
+        _refuse(who, "%s must be a matrix of float32, bfloat16 or float16" % name)
+    rows, cols = t.shape
+    if cols > 1 and t.stride(1) != 1:
+        _refuse(who, "%s must have dense rows" % name)
+    return rows, cols, t.stride(0) if rows > 1 else cols
+
+
+def _vector(who, name, t, n, dtype=torch.float32):
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.numel() != n or not t.is_contiguous():
+        _refuse(who, "%s must be a dense %s tensor of %d elements" % (name, dtype, n))
+    return t.data_ptr()
+
+
+def _ids(who, name, t):
+    if t.dtype is torch.int64:
+        size = 8
+    elif t.dtype is torch.int32:
+        size = 4
+    else:
+        _refuse(who, "%s must be int32 or int64" % name)
+    if not t.is_contiguous():
+        _refuse(who, "%s must be dense" % name)
+    return t.data_ptr(), size
+
+
+def _status(who, t):
+    return _vector(who, "status", t, 1, torch.int32)
+
+
+def embed_forward(table, ids, out, scale=1.0, status=None, stream=0):
+    """pb_embed_forward: out[t] = scale * table[ids[t]].  out: [n_tokens, dim], rows may be strided."""
+    who = "embed_forward"
+    d = _device(who, table)
+    _on_device(who, d, ids, out, status)
+    vocab, dim, ld = _rows(who, "table", table)
+    p, size = _ids(who, "ids", ids)
+    rows, cols, ld_out = _rows(who, "out", out)
+    if rows != ids.numel() or cols != dim or out.dtype is not table.dtype:
+        _refuse(who, "out must be [number of ids, dim] of the table's type")
+    _check(load_library().pb_embed_forward(table.data_ptr(), _DTYPE[table.dtype], vocab, dim, ld, p, size, rows, scale,
+                                           out.data_ptr(), ld_out, _status(who, status), stream))
+
+
+def embed_scratch_bytes(n_tokens, vocab, dim):
+    """pb_embed_scratch_bytes: bytes of scratch that embed_backward needs for these sizes."""
+    n = load_library().pb_embed_scratch_bytes(int(n_tokens), int(vocab), int(dim))
+    if n == 0:
+        _refuse("embed_scratch_bytes", "sizes out of range")
+    return n
+
+
+def embed_backward(dout, ids, dtable, scratch, scale=1.0, padding_idx=-1, accumulate=False, status=None, stream=0):
+    """pb_embed_backward: dtable[v] (+)= scale * sum of dout[t] over ids[t] == v.  scratch: uint8 tensor of
+    embed_scratch_bytes(...) bytes."""
+    who = "embed_backward"
+    d = _device(who, dtable)
+    _on_device(who, d, dout, ids, scratch, status)
+    vocab, dim, ld = _rows(who, "dtable", dtable)
+    rows, cols, ld_dout = _rows(who, "dout", dout)
+    p, size = _ids(who, "ids", ids)
+    if rows != ids.numel() or cols != dim:
+        _refuse(who, "dout must be [number of ids, dim]")
+    if scratch.dtype is not torch.uint8 or not scratch.is_contiguous():
+        _refuse(who, "scratch must be a dense uint8 tensor")
+    _check(load_library().pb_embed_backward(dout.data_ptr(), _DTYPE[dout.dtype], ld_dout, p, size, rows, vocab, dim, scale,
+                                            padding_idx, dtable.data_ptr(), _DTYPE[dtable.dtype], ld, 1 if accumulate else 0,
+                                            scratch.data_ptr(), scratch.numel(), _status(who, status), stream))
+
+
+def logprob_forward(logits, tokens=None, logp=None, entropy=None, lse=None, top_logp=None, top_ids=None, inv_temperature=1.0,
+                    status=None, stream=0):
+    """pb_logprob_forward: log probabilities of `tokens`, entropies, logsumexps and top alternatives of rows of logits."""
+    who = "logprob_forward"
+    d = _device(who, logits)
+    _on_device(who, d, tokens, logp, entropy, lse, top_logp, top_ids, status)
+    rows, vocab, ld = _rows(who, "logits", logits)
+    p, size = None, 4
+    if tokens is not None:
+        p, size = _ids(who, "tokens", tokens)
+        if tokens.numel() != rows:
+            _refuse(who, "tokens must hold one id per row")
+    if (tokens is None) != (logp is None):
+        _refuse(who, "logp and tokens go together")
+    k = 0
+    if (top_logp is None) != (top_ids is None):
+        _refuse(who, "top_logp and top_ids go together")
+    if top_ids is not None:
+        if top_ids.dim() != 2 or top_ids.shape[0] != rows:
+            _refuse(who, "top_ids must be [rows, top_k]")
+        k = top_ids.shape[1]
+    _check(load_library().pb_logprob_forward(
+        logits.data_ptr(), _DTYPE[logits.dtype], rows, vocab, ld, p, size, inv_temperature, _vector(who, "logp", logp, rows),
+        _vector(who, "entropy", entropy, rows), _vector(who, "lse", lse, rows), k, _vector(who, "top_logp", top_logp, rows * k),
+        _vector(who, "top_ids", top_ids, rows * k, torch.int32), _status(who, status), stream))
+
+
+def logprob_backward(logits, tokens, lse, dlogits, g_logp=None, g_entropy=None, entropy=None, g_lse=None, inv_temperature=1.0,
+                     status=None, stream=0):
+    """pb_logprob_backward: gradient with respect to the logits (dlogits may be the logits themselves)."""
+    who = "logprob_backward"
+    d = _device(who, logits)
+    _on_device(who, d, tokens, lse, dlogits, g_logp, g_entropy, entropy, g_lse, status)
+    rows, vocab, ld = _rows(who, "logits", logits)
+    drows, dcols, ld_d = _rows(who, "dlogits", dlogits)
+    if (drows, dcols) != (rows, vocab) or dlogits.dtype is not logits.dtype:
+        _refuse(who, "dlogits must have the logits' shape and type")
+    p, size = None, 4
+    if tokens is not None:
+        p, size = _ids(who, "tokens", tokens)
+        if tokens.numel() != rows:
+            _refuse(who, "tokens must hold one id per row")
+    _check(load_library().pb_logprob_backward(
+        logits.data_ptr(), _DTYPE[logits.dtype], rows, vocab, ld, p, size, inv_temperature, _vector(who, "lse", lse, rows),
+        _vector(who, "entropy", entropy, rows), _vector(who, "g_logp", g_logp, rows), _vector(who, "g_entropy", g_entropy, rows),
+        _vector(who, "g_lse", g_lse, rows), dlogits.data_ptr(), ld_d, _status(who, status), stream))
+
+
+def adamw_moments(m, m_scale, v, v_scale, m_out=None, v_out=None, stream=0):
+    """pb_adamw_moments: the float32 moments that an 8-bit state stands for."""
+    who = "adamw_moments"
+    d = _device(who, m)
+    _on_device(who, d, m_scale, v, v_scale, m_out, v_out)
+    n = m.numel()
+    blocks = -(-n // 256)
+    _check(load_library().pb_adamw_moments(
+        _vector(who, "m", m, n, torch.uint8), _vector(who, "m_scale", m_scale, blocks), _vector(who, "v", v, n, torch.uint8),
+        _vector(who, "v_scale", v_scale, blocks), n, _vector(who, "m_out", m_out, n), _vector(who, "v_out", v_out, n), stream))
+
+
+class AdamW:
+    """pb_adamw_step over a fixed list of tensors: holds the tensors and the table of their addresses.
+
+    w: float32 weights.  m, v: float32 states, or uint8 ones with m_scale / v_scale (float32, one per 256 elements).
+    w_forward: copies of the weights in the forward's type, predicted `horizon` steps ahead, or None.  weight_decay and
+    horizon are numbers or one number per tensor.  All tensors are dense, of the caller's, and must not overlap.
+    """
+
+    def __init__(self, w, m, v, m_scale=None, v_scale=None, w_forward=None, weight_decay=0.0, horizon=0.0):
+        who = "AdamW"
+        n = len(w)
+        lists = [list(x) if x is not None else [None] * n for x in (w, m, v, m_scale, v_scale, w_forward)]
+        if any(len(x) != n for x in lists):
+            _refuse(who, "the lists must have the same length")
+        decay = list(weight_decay) if hasattr(weight_decay, "__len__") else [weight_decay] * n
+        ahead = list(horizon) if hasattr(horizon, "__len__") else [horizon] * n
+        if len(decay) != n or len(ahead) != n:
+            _refuse(who, "weight_decay and horizon are numbers, or one number per tensor")
+        self._keep = lists
+        self._bits = 8 if n and lists[1][0].dtype is torch.uint8 else 32
+        self._forward = _DTYPE.get(lists[5][0].dtype, -1) if n and lists[5][0] is not None else 0
+        self._device = _device(who, lists[0][0]) if n else None
+        self._n = [t.numel() for t in lists[0]]
+        self._table = (pb_adamw_tensor * n)()
+        self._grads = (C.c_void_p * n)()
+        state = torch.uint8 if self._bits == 8 else torch.float32
+        spans = []
+        for k in range(n):
+            tw, tm, tv, ms, vs, tf = (x[k] for x in lists)
+            _on_device(who, self._device, tw, tm, tv, ms, vs, tf)
+            size = self._n[k]
+            if (ms is None) != (self._bits == 32) or (vs is None) != (self._bits == 32):
+                _refuse(who, "8-bit states, and only those, come with scales")
+            if (tf is None) != (lists[5][0] is None):
+                _refuse(who, "w_forward is given for every tensor or for none")
+            blocks = -(-size // 256)
+            p = [_vector(who, "w", tw, size), _vector(who, "m", tm, size, state), _vector(who, "v", tv, size, state),
+                 _vector(who, "m_scale", ms, blocks), _vector(who, "v_scale", vs, blocks),
+                 _vector(who, "w_forward", tf, size, lists[5][0].dtype) if tf is not None else None]
+            self._table[k] = pb_adamw_tensor(*p, size, float(decay[k]), float(ahead[k]))
+            spans += [(a, a + t.numel() * t.element_size()) for a, t in zip(p, (tw, tm, tv, ms, vs, tf)) if a and t.numel()]
+        if self._forward < 0:
+            _refuse(who, "w_forward must be float32, bfloat16 or float16")
+        spans.sort()
+        if any(a[1] > b[0] for a, b in zip(spans[:-1], spans[1:])):
+            _refuse(who, "two of the tensors overlap")
+
+    def step(self, grads, lr, step, beta1=0.9, beta2=0.999, eps=1e-8, seed=0, grad_scale=None, dev_lr=None, dev_step=None, stream=0):
+        """One step with `grads`, one tensor per weight, all of one type.  `step` counts from 1."""
+        who = "AdamW.step"
+        n = len(self._n)
+        if len(grads) != n:
+            _refuse(who, "one gradient per tensor is needed")
+        if n == 0:
+            return
+        if self._device != torch.cuda.current_device():
+            _refuse(who, "every tensor must be a CUDA tensor on the current device")
+        dtype, device, ptr = grads[0].dtype, self._device, []
+        for g, size in zip(grads, self._n):
+            if g.dtype is not dtype or g.numel() != size or g.get_device() != device or not g.is_contiguous():
+                _refuse(who, "gradients must be dense CUDA tensors of the weights' sizes and of one type")
+            ptr.append(g.data_ptr())
+        if dtype not in _DTYPE:
+            _refuse(who, "gradients must be float32, bfloat16 or float16")
+        _on_device(who, device, grad_scale, dev_lr, dev_step)
+        self._grads[:] = ptr
+        args = pb_adamw_args(lr, beta1, beta2, eps, step, seed & 0xFFFFFFFFFFFFFFFF, _vector(who, "grad_scale", grad_scale, 1),
+                             _vector(who, "dev_lr", dev_lr, 1), _vector(who, "dev_step", dev_step, 1, torch.int64), _DTYPE[dtype],
+                             self._forward, self._bits)
+        _check(load_library().pb_adamw_step(self._table, self._grads, n, C.byref(args), stream))

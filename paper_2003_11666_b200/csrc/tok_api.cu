@@ -40,6 +40,59 @@ bool overlap(const void* a, size_t na, const void* b, size_t nb) {
     return na && nb && x < y + nb && y < x + na;
 }
 
+// Sizes and scratch layout of the embedding gradient.
+constexpr int64_t kMaxEmbedDim = 1 << 26;
+
+struct EmbedPlan {
+    SortPlan sort;
+    RedPlan red;
+    int slabs;
+    size_t bytes;
+};
+
+EmbedPlan embed_plan(int64_t n, int64_t vocab, int64_t dim, char* scratch) {
+    EmbedPlan e{};
+    int len = 1;
+    while (vocab >> len) ++len;                              // bits of the largest key, vocab itself
+    SortPlan& s = e.sort;
+    s.n = n;
+    s.passes = (len + kSortMaxBits - 1) / kSortMaxBits;
+    s.bits = (len + s.passes - 1) / s.passes;
+    const int64_t sub = (n + kSortSub - 1) / kSortSub;       // sub-tiles, spread over at most kSortMaxTiles blocks
+    const int64_t each = (sub + kSortMaxTiles - 1) / kSortMaxTiles;
+    s.tile = (each > 0 ? each : 1) * kSortSub;
+    s.tiles = (int)((n + s.tile - 1) / s.tile);
+    RedPlan& r = e.red;
+    r.n = n; r.vocab = vocab; r.dim = dim;
+    r.lanes = 1;
+    while (r.lanes < kRedThreads && (int64_t)r.lanes * kRedCols < dim) r.lanes *= 2;
+    e.slabs = (int)((dim + (int64_t)r.lanes * kRedCols - 1) / ((int64_t)r.lanes * kRedCols));
+    // stretches of 16 to 128 entries: six blocks per SM if the list is long enough
+    const int per_block = kRedThreads / r.lanes;
+    int64_t want = n * e.slabs / ((int64_t)148 * 6 * per_block);
+    r.len = (int)(want < 16 ? 16 : want > 128 ? 128 : (want + 3) / 4 * 4);
+    r.stretches = (int)((n + r.len - 1) / r.len);
+    r.red_blocks = (r.stretches + per_block - 1) / per_block;
+    size_t at = 0;
+    auto take = [&](size_t bytes) {
+        char* p = scratch ? scratch + at : nullptr;
+        at += (bytes + 255) / 256 * 256;
+        return p;
+    };
+    for (int k = 0; k < 2; ++k) {
+        s.key[k] = (unsigned*)take((size_t)n * 4);
+        s.pos[k] = (unsigned*)take((size_t)n * 4);
+    }
+    s.hist = (int*)take(s.tiles > 1 ? ((size_t)s.passes * s.tiles << s.bits) * 4 : 0);
+    s.n_zero = (int64_t)e.slabs * r.stretches * 3;
+    s.zero = r.arrived = (unsigned*)take((size_t)s.n_zero * 4);
+    r.part = (float*)take((size_t)r.stretches * 2 * dim * 4);
+    r.key = s.key[(s.passes - 1) & 1];
+    r.pos = s.pos[(s.passes - 1) & 1];
+    e.bytes = at > 256 ? at : 256;
+    return e;
+}
+
 }  // namespace
 
 #define PB_REFUSE(cond, text) \
@@ -75,8 +128,8 @@ int pb_embed_forward(const void* dev_table, int dtype, int64_t vocab, int64_t di
 }
 
 size_t pb_embed_scratch_bytes(int64_t n_tokens, int64_t vocab, int64_t dim) {
-    if (n_tokens < 0 || n_tokens > kMaxCount || vocab < 1 || vocab > kMaxCount || dim < 1 || dim > kMaxCount) return 0;
-    return 256;
+    if (n_tokens < 0 || n_tokens > kMaxCount || vocab < 1 || vocab > kMaxCount || dim < 1 || dim > kMaxEmbedDim) return 0;
+    return embed_plan(n_tokens, vocab, dim, nullptr).bytes;
 }
 
 int pb_embed_backward(const void* dev_dout, int dtype, int64_t ld_dout, const void* dev_ids, int id_bytes, int64_t n_tokens,
@@ -87,7 +140,8 @@ int pb_embed_backward(const void* dev_dout, int dtype, int64_t ld_dout, const vo
     PB_REFUSE(dtable_dtype != PB_F32 && dtable_dtype != dtype, "pb_embed_backward: the table's gradient is float32 or of dout's type");
     PB_REFUSE(id_bytes != 4 && id_bytes != 8, "pb_embed_backward: token ids have 4 or 8 bytes");
     PB_REFUSE(n_tokens < 0 || n_tokens > kMaxCount, "pb_embed_backward: n_tokens out of range");
-    PB_REFUSE(vocab < 1 || vocab > kMaxCount || dim < 1 || dim > kMaxCount, "pb_embed_backward: vocab and dim must be between 1 and 2^31 - 1");
+    PB_REFUSE(vocab < 1 || vocab > kMaxCount, "pb_embed_backward: vocab must be between 1 and 2^31 - 1");
+    PB_REFUSE(dim < 1 || dim > kMaxEmbedDim, "pb_embed_backward: dim must be between 1 and 2^26");
     PB_REFUSE(ld_dtable < dim || ld_dout < dim, "pb_embed_backward: a row stride is smaller than dim");
     PB_REFUSE(padding_idx < -1 || padding_idx >= vocab, "pb_embed_backward: padding_idx must be -1 or a row of the table");
     PB_REFUSE(accumulate != 0 && accumulate != 1, "pb_embed_backward: accumulate must be 0 or 1");
@@ -103,14 +157,22 @@ int pb_embed_backward(const void* dev_dout, int dtype, int64_t ld_dout, const vo
     PB_REFUSE(overlap(dev_dtable, n_dt, dev_dout, n_do) || overlap(dev_scratch, scratch_bytes, dev_dtable, n_dt) ||
               overlap(dev_scratch, scratch_bytes, dev_dout, n_do), "pb_embed_backward: buffers overlap");
     const cudaStream_t s = (cudaStream_t)stream;
+    EmbedPlan e = embed_plan(n_tokens, vocab, dim, (char*)dev_scratch);
+    e.red.ld_dout = ld_dout; e.red.ld = ld_dtable; e.red.scale = scale; e.red.accumulate = accumulate;
+    // eight columns per thread move as 16-byte pieces where every row starts on 16 bytes
+    const bool vec = dim % kRedCols == 0 && aligned(dev_dout, 16) && aligned(dev_dtable, 16) && (size_t)ld_dout * es % 16 == 0 &&
+                     (size_t)ld_dtable * gs % 16 == 0;
     auto go = [&](auto t, auto g, auto i) {
         using T = decltype(t);
         using G = decltype(g);
         using I = decltype(i);
-        if (!accumulate) embed_zero_kernel<G><<<(unsigned)vocab, 256, 0, s>>>((G*)dev_dtable, dim, ld_dtable);
-        if (n_tokens)
-            embed_bwd_kernel<T, G, I><<<(unsigned)n_tokens, 256, 0, s>>>((const T*)dev_dout, ld_dout, (const I*)dev_ids, n_tokens, vocab,
-                                                                         dim, scale, padding_idx, (G*)dev_dtable, ld_dtable, accumulate, dev_status);
+        const SortIds<I> in{(const I*)dev_ids, vocab, padding_idx, dev_status};
+        if (n_tokens) embed_sort_kernel<I><<<e.sort.tiles, kSortThreads, 0, s>>>(e.sort, in);
+        for (int p = 0; e.sort.tiles > 1 && p < e.sort.passes; ++p) embed_scatter_kernel<I><<<e.sort.tiles, kSortThreads, 0, s>>>(e.sort, in, p);
+        const int64_t blocks = e.red.red_blocks + (accumulate ? 0 : (vocab + kZeroRows - 1) / kZeroRows);
+        const dim3 grid((unsigned)blocks, (unsigned)e.slabs);
+        if (vec) embed_reduce_kernel<true, T, G><<<grid, kRedThreads, 0, s>>>(e.red, (const T*)dev_dout, (G*)dev_dtable);
+        else embed_reduce_kernel<false, T, G><<<grid, kRedThreads, 0, s>>>(e.red, (const T*)dev_dout, (G*)dev_dtable);
     };
     auto by_id = [&](auto t, auto g) { if (id_bytes == 4) go(t, g, int32_t()); else go(t, g, int64_t()); };
     auto by_g = [&](auto t) { if (dtable_dtype == PB_F32) by_id(t, float()); else by_id(t, t); };

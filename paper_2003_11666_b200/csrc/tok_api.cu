@@ -40,8 +40,27 @@ bool overlap(const void* a, size_t na, const void* b, size_t nb) {
     return na && nb && x < y + nb && y < x + na;
 }
 
+// Launch that may begin while the launch before it in the stream ends; the kernel waits for that
+// launch's results itself (cudaGridDependencySynchronize).
+template <typename... P, typename... A>
+cudaError_t launch_after(void (*kernel)(P...), dim3 grid, int threads, cudaStream_t stream, A... args) {
+    cudaLaunchConfig_t c{};
+    c.gridDim = grid;
+    c.blockDim = dim3((unsigned)threads);
+    c.stream = stream;
+    cudaLaunchAttribute attr{};
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    c.attrs = &attr;
+    c.numAttrs = 1;
+    return cudaLaunchKernelEx(&c, kernel, P(args)...);
+}
+
 // Sizes and scratch layout of the embedding gradient.
 constexpr int64_t kMaxEmbedDim = 1 << 26;
+// Blocks per SM that the reduction's stretches are cut for; four are resident.  More and shorter
+// stretches even out the tail: 65536 tokens of 2048 columns take 230 us at 4, 192 at 8, 189 at 16.
+constexpr int kRedWave = 16;
 
 struct EmbedPlan {
     SortPlan sort;
@@ -55,22 +74,22 @@ EmbedPlan embed_plan(int64_t n, int64_t vocab, int64_t dim, char* scratch) {
     int len = 1;
     while (vocab >> len) ++len;                              // bits of the largest key, vocab itself
     SortPlan& s = e.sort;
-    s.n = n;
+    s.n = (int)n;
     s.passes = (len + kSortMaxBits - 1) / kSortMaxBits;
     s.bits = (len + s.passes - 1) / s.passes;
-    const int64_t sub = (n + kSortSub - 1) / kSortSub;       // sub-tiles, spread over at most kSortMaxTiles blocks
-    const int64_t each = (sub + kSortMaxTiles - 1) / kSortMaxTiles;
-    s.tile = (each > 0 ? each : 1) * kSortSub;
-    s.tiles = (int)((n + s.tile - 1) / s.tile);
+    s.tile_shift = 11;                                       // kSortSub tokens a block; longer lists: several sub-tiles
+    while (((n - 1) >> s.tile_shift) >= kSortMaxTiles) ++s.tile_shift;
+    s.tiles = n ? (int)(((n - 1) >> s.tile_shift) + 1) : 0;
     RedPlan& r = e.red;
     r.n = n; r.vocab = vocab; r.dim = dim;
     r.lanes = 1;
     while (r.lanes < kRedThreads && (int64_t)r.lanes * kRedCols < dim) r.lanes *= 2;
     e.slabs = (int)((dim + (int64_t)r.lanes * kRedCols - 1) / ((int64_t)r.lanes * kRedCols));
-    // stretches of 16 to 128 entries: six blocks per SM if the list is long enough
+    // stretches of 8 to 128 entries: about kRedWave blocks per SM if the list is long enough
     const int per_block = kRedThreads / r.lanes;
-    int64_t want = n * e.slabs / ((int64_t)148 * 6 * per_block);
-    r.len = (int)(want < 16 ? 16 : want > 128 ? 128 : (want + 3) / 4 * 4);
+    const int64_t want = (n * e.slabs / ((int64_t)148 * kRedWave * per_block) + 7) / 8 * 8;
+    const int most = kRedEntries / per_block < 128 ? kRedEntries / per_block : 128;
+    r.len = (int)(want < 8 ? 8 : want > most ? most : want);
     r.stretches = (int)((n + r.len - 1) / r.len);
     r.red_blocks = (r.stretches + per_block - 1) / per_block;
     size_t at = 0;
@@ -84,7 +103,7 @@ EmbedPlan embed_plan(int64_t n, int64_t vocab, int64_t dim, char* scratch) {
         s.pos[k] = (unsigned*)take((size_t)n * 4);
     }
     s.hist = (int*)take(s.tiles > 1 ? ((size_t)s.passes * s.tiles << s.bits) * 4 : 0);
-    s.n_zero = (int64_t)e.slabs * r.stretches * 3;
+    s.n_zero = (int)((int64_t)e.slabs * r.stretches * 3);
     s.zero = r.arrived = (unsigned*)take((size_t)s.n_zero * 4);
     r.part = (float*)take((size_t)r.stretches * 2 * dim * 4);
     r.key = s.key[(s.passes - 1) & 1];
@@ -159,20 +178,39 @@ int pb_embed_backward(const void* dev_dout, int dtype, int64_t ld_dout, const vo
     const cudaStream_t s = (cudaStream_t)stream;
     EmbedPlan e = embed_plan(n_tokens, vocab, dim, (char*)dev_scratch);
     e.red.ld_dout = ld_dout; e.red.ld = ld_dtable; e.red.scale = scale; e.red.accumulate = accumulate;
-    // eight columns per thread move as 16-byte pieces where every row starts on 16 bytes
-    const bool vec = dim % kRedCols == 0 && aligned(dev_dout, 16) && aligned(dev_dtable, 16) && (size_t)ld_dout * es % 16 == 0 &&
-                     (size_t)ld_dtable * gs % 16 == 0;
+    // columns move in pieces of four where every row starts on a piece
+    const bool vec = dim % 4 == 0 && aligned(dev_dout, 4 * es) && aligned(dev_dtable, 4 * gs) && ld_dout % 4 == 0 && ld_dtable % 4 == 0;
     auto go = [&](auto t, auto g, auto i) {
         using T = decltype(t);
         using G = decltype(g);
         using I = decltype(i);
         const SortIds<I> in{(const I*)dev_ids, vocab, padding_idx, dev_status};
-        if (n_tokens) embed_sort_kernel<I><<<e.sort.tiles, kSortThreads, 0, s>>>(e.sort, in);
-        for (int p = 0; e.sort.tiles > 1 && p < e.sort.passes; ++p) embed_scatter_kernel<I><<<e.sort.tiles, kSortThreads, 0, s>>>(e.sort, in, p);
-        const int64_t blocks = e.red.red_blocks + (accumulate ? 0 : (vocab + kZeroRows - 1) / kZeroRows);
+        // A list that one block sorts leaves the GPU idle meanwhile: all rows are cleared then, and those
+        // with tokens written again.  Longer lists clear only the rows without tokens, in the last launch.
+        const bool clear_now = !accumulate && e.sort.tiles == 1;
+        int clear_blocks = 0;
+        if (clear_now) {
+            e.sort.clear = (char*)dev_dtable;
+            e.sort.clear_rows = vocab;
+            e.sort.clear_bytes = dim * (int64_t)gs;
+            e.sort.clear_stride = ld_dtable * (int64_t)gs;
+            const size_t any = reinterpret_cast<size_t>(dev_dtable) | (size_t)e.sort.clear_bytes | (size_t)e.sort.clear_stride;
+            e.sort.clear_unit = any % 16 == 0 ? 16 : any % 4 == 0 ? 4 : 2;
+            const int64_t by_rows = (vocab + kSortWarps - 1) / kSortWarps;
+            clear_blocks = (int)(by_rows < 148 * 3 ? by_rows : 148 * 3);
+        }
+        cudaError_t err = cudaSuccess;
+        if (n_tokens) {
+            embed_sort_kernel<I><<<e.sort.tiles + clear_blocks, kSortThreads, 0, s>>>(e.sort, in);
+            for (int p = 0; e.sort.tiles > 1 && p < e.sort.passes && err == cudaSuccess; ++p)
+                err = launch_after(embed_scatter_kernel<I>, dim3(e.sort.tiles), kSortThreads, s, e.sort, in, p);
+        }
+        const int64_t blocks = e.red.red_blocks + (accumulate || clear_now ? 0 : (vocab + kZeroRows - 1) / kZeroRows);
         const dim3 grid((unsigned)blocks, (unsigned)e.slabs);
-        if (vec) embed_reduce_kernel<true, T, G><<<grid, kRedThreads, 0, s>>>(e.red, (const T*)dev_dout, (G*)dev_dtable);
-        else embed_reduce_kernel<false, T, G><<<grid, kRedThreads, 0, s>>>(e.red, (const T*)dev_dout, (G*)dev_dtable);
+        const T* x = (const T*)dev_dout;
+        G* d = (G*)dev_dtable;
+        if (err == cudaSuccess) err = vec ? launch_after(embed_reduce_kernel<true, T, G>, grid, kRedThreads, s, e.red, x, d)
+                                          : launch_after(embed_reduce_kernel<false, T, G>, grid, kRedThreads, s, e.red, x, d);
     };
     auto by_id = [&](auto t, auto g) { if (id_bytes == 4) go(t, g, int32_t()); else go(t, g, int64_t()); };
     auto by_g = [&](auto t) { if (dtable_dtype == PB_F32) by_id(t, float()); else by_id(t, t); };

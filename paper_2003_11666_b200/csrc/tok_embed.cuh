@@ -12,6 +12,8 @@
 // sums depend on the ids alone, no addition to memory is atomic, and a row shared by
 // thousands of tokens is still the work of many groups.
 #pragma once
+#include <type_traits>
+
 #include "tok_common.cuh"
 
 namespace pb {
@@ -33,12 +35,16 @@ constexpr int kSortMaxBits = 9;            // digit bits of a pass: one bin per 
 constexpr int kSortMaxTiles = 256;         // blocks; longer lists give each block several sub-tiles
 
 struct SortPlan {
-    int passes, bits, tiles;
-    long long n, tile;                     // tokens, tokens per block (a multiple of kSortSub)
+    int passes, bits, tiles, n;
+    int tile_shift;                        // tokens per block: kSortSub times a power of two
     unsigned *key[2], *pos[2];             // ping-pong
     int* hist;                             // [passes][tiles][1 << bits]
     unsigned* zero;                        // words to clear for the reduction's counters
-    long long n_zero;
+    int n_zero;
+    // rows to clear beside the sort (a list that fits one block leaves the other SMs idle)
+    char* clear;
+    long long clear_rows, clear_bytes, clear_stride;
+    int clear_unit;
 };
 
 struct SortShared {
@@ -79,19 +85,140 @@ struct SortIds {
     }
 };
 
-// One stable pass over the tokens [lo, hi) of a block whose first free place of digit b is sh.base[b].
+// Place of each of the 4 x 512 tokens among those of its digit.  Warp w holds 128 consecutive
+// tokens, 32 at a time; `digit` is -1 where there is none.  Leaves each warp's counts in sh.warp.
+__device__ __forceinline__ void rank_digits(const int (&digit)[4], int (&rank)[4], int bins, SortShared& sh) {
+    const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
+    for (int b = lane; b < bins; b += 32) sh.warp[w][b] = 0;
+    __syncwarp();
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const unsigned peers = __match_any_sync(0xffffffffu, digit[q]);
+        const int before = __popc(peers & ((1u << lane) - 1));
+        int had = 0;
+        if (digit[q] >= 0) had = sh.warp[w][digit[q]];
+        __syncwarp();
+        rank[q] = had + before;
+        if (digit[q] >= 0 && before == 0) sh.warp[w][digit[q]] = had + __popc(peers);
+        __syncwarp();
+    }
+    __syncthreads();
+}
+
+// Counts of the warps -> first places of each warp's tokens of a digit; returns the digit's total.
+__device__ __forceinline__ int place_warps(int bin, int at, SortShared& sh) {
+    const int first = at;
+#pragma unroll
+    for (int q = 0; q < kSortWarps; ++q) {
+        const int c = sh.warp[q][bin];
+        sh.warp[q][bin] = at;
+        at += c;
+    }
+    return at - first;
+}
+
+// A list of at most kSortSub tokens: all passes in one block, the list in shared memory.
 template <typename I>
-__device__ __forceinline__ void sort_scatter(const SortPlan& a, const SortIds<I>& in, int p, long long lo, long long hi, SortShared& sh) {
+__device__ __forceinline__ void sort_small(const SortPlan& a, const SortIds<I>& in, SortShared& sh, unsigned* sh_key, unsigned short* sh_pos) {
+    const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5, bins = 1 << a.bits;
+    unsigned key[4], pos[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const int t = w * 128 + q * 32 + lane;
+        key[q] = t < a.n ? in.key(t) : 0u;
+        pos[q] = t;
+    }
+    for (int p = 0; p < a.passes; ++p) {
+        int digit[4], rank[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int t = w * 128 + q * 32 + lane;
+            if (p > 0 && t < a.n) { key[q] = sh_key[t]; pos[q] = sh_pos[t]; }
+            digit[q] = t < a.n ? (int)((key[q] >> (p * a.bits)) & (bins - 1)) : -1;
+        }
+        rank_digits(digit, rank, bins, sh);
+        if (tid < bins) sh.base[tid] = place_warps(tid, 0, sh);
+        __syncthreads();
+        scan_bins(sh, bins);
+        const bool last = p + 1 == a.passes;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            if (digit[q] < 0) continue;
+            const int d = sh.base[digit[q]] + sh.warp[w][digit[q]] + rank[q];
+            if (last) { a.key[p & 1][d] = key[q]; a.pos[p & 1][d] = pos[q]; }
+            else { sh_key[d] = key[q]; sh_pos[d] = (unsigned short)pos[q]; }
+        }
+        __syncthreads();
+    }
+}
+
+// First launch: the digit counts of the first pass, and the memory that later launches count in.
+// A list that fits one block is sorted here, while the other blocks clear the table's gradient.
+template <typename I>
+__global__ void __launch_bounds__(kSortThreads)
+embed_sort_kernel(const __grid_constant__ SortPlan a, const SortIds<I> in) {
+    __shared__ SortShared sh;
+    __shared__ unsigned sh_key[kSortSub];
+    __shared__ unsigned short sh_pos[kSortSub];
+    cudaTriggerProgrammaticLaunchCompletion();
+    const int tid = threadIdx.x, bins = 1 << a.bits;
+    if ((int)blockIdx.x >= a.tiles) {
+        const int nz = gridDim.x - a.tiles, warp = tid >> 5, lane = tid & 31;
+        for (long long r = (long long)(blockIdx.x - a.tiles) * kSortWarps + warp; r < a.clear_rows; r += (long long)nz * kSortWarps) {
+            char* row = a.clear + r * a.clear_stride;
+            if (a.clear_unit == 16) for (long long c = lane * 16; c < a.clear_bytes; c += 512) *reinterpret_cast<uint4*>(row + c) = make_uint4(0, 0, 0, 0);
+            else if (a.clear_unit == 4) for (long long c = lane * 4; c < a.clear_bytes; c += 128) *reinterpret_cast<unsigned*>(row + c) = 0;
+            else for (long long c = lane * 2; c < a.clear_bytes; c += 64) *reinterpret_cast<unsigned short*>(row + c) = 0;
+        }
+        return;
+    }
+    for (int k = blockIdx.x * kSortThreads + tid; k < a.n_zero; k += a.tiles * kSortThreads) a.zero[k] = 0;
+    if (a.tiles == 1 && a.n <= kSortSub) {
+        sort_small(a, in, sh, sh_key, sh_pos);
+        return;
+    }
+    const long long lo = (long long)blockIdx.x << a.tile_shift, hi = min((long long)a.n, lo + (1ll << a.tile_shift));
+    if (tid < bins) sh.base[tid] = 0;
+    __syncthreads();
+    for (long long t = lo + tid; t < hi; t += kSortThreads) atomicAdd(&sh.base[in.key(t) & (bins - 1)], 1);
+    __syncthreads();
+    if (tid < bins) {
+        a.hist[(size_t)blockIdx.x * bins + tid] = sh.base[tid];
+        for (int q = 1; q < a.passes; ++q) a.hist[((size_t)q * a.tiles + blockIdx.x) * bins + tid] = 0;
+    }
+}
+
+// One stable pass: every block places its stretch of tokens by the digit of this pass and counts
+// the next pass's digits where the tokens land.
+template <typename I>
+__global__ void __launch_bounds__(kSortThreads)
+embed_scatter_kernel(const __grid_constant__ SortPlan a, const SortIds<I> in, int p) {
+    __shared__ SortShared sh;
+    cudaTriggerProgrammaticLaunchCompletion();
+    cudaGridDependencySynchronize();
     const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
     const int bins = 1 << a.bits, shift = p * a.bits;
+    const int* hist = a.hist + (size_t)p * a.tiles * bins;
+    int before = 0, total = 0;                             // earlier blocks' count of this thread's digit, and all blocks'
+    if (tid < bins) {
+#pragma unroll 16
+        for (int t = 0; t < a.tiles; ++t) {
+            const int c = hist[(size_t)t * bins + tid];
+            if (t < (int)blockIdx.x) before += c;
+            total += c;
+        }
+        sh.base[tid] = total;
+    }
+    __syncthreads();
+    scan_bins(sh, bins);
+    int place = tid < bins ? sh.base[tid] + before : 0;    // first free place of this thread's digit
     const unsigned* ik = a.key[(p + 1) & 1];
     const unsigned* ip = a.pos[(p + 1) & 1];
     unsigned* ok = a.key[p & 1];
     unsigned* op = a.pos[p & 1];
-    int* next = p + 1 < a.passes && a.tiles > 1 ? a.hist + (size_t)(p + 1) * a.tiles * bins : nullptr;
+    int* next = p + 1 < a.passes ? a.hist + (size_t)(p + 1) * a.tiles * bins : nullptr;
+    const long long lo = (long long)blockIdx.x << a.tile_shift, hi = min((long long)a.n, lo + (1ll << a.tile_shift));
     for (long long s0 = lo; s0 < hi; s0 += kSortSub) {
-        for (int b = tid; b < bins * kSortWarps; b += kSortThreads) sh.warp[b >> a.bits][b & (bins - 1)] = 0;
-        __syncthreads();
         unsigned key[4], pos[4];
         int digit[4], rank[4];
 #pragma unroll
@@ -102,39 +229,19 @@ __device__ __forceinline__ void sort_scatter(const SortPlan& a, const SortIds<I>
             pos[q] = !live ? 0u : p == 0 ? (unsigned)t : ip[t];
             digit[q] = live ? (int)((key[q] >> shift) & (bins - 1)) : -1;
         }
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {                      // rank among the warp's earlier tokens of the digit
-            const unsigned peers = __match_any_sync(0xffffffffu, digit[q]);
-            const int before = __popc(peers & ((1u << lane) - 1));
-            int had = 0;
-            if (digit[q] >= 0) had = sh.warp[w][digit[q]];
-            __syncwarp();
-            rank[q] = had + before;
-            if (digit[q] >= 0 && before == 0) sh.warp[w][digit[q]] = had + __popc(peers);
-            __syncwarp();
-        }
-        __syncthreads();
-        for (int b = tid; b < bins; b += kSortThreads) {   // counts of the warps -> first places
-            int at = sh.base[b];
-#pragma unroll
-            for (int q = 0; q < kSortWarps; ++q) {
-                const int c = sh.warp[q][b];
-                sh.warp[q][b] = at;
-                at += c;
-            }
-            sh.base[b] = at;
-        }
+        rank_digits(digit, rank, bins, sh);
+        if (tid < bins) place += place_warps(tid, place, sh);
         __syncthreads();
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             int bin = -1;
             if (digit[q] >= 0) {
-                const long long d = sh.warp[w][digit[q]] + rank[q];
+                const int d = sh.warp[w][digit[q]] + rank[q];
                 ok[d] = key[q];
                 op[d] = pos[q];
-                if (next) bin = (int)(d / a.tile) * bins + (int)((key[q] >> (shift + a.bits)) & (bins - 1));
+                if (next) bin = (d >> a.tile_shift) * bins + (int)((key[q] >> (shift + a.bits)) & (bins - 1));
             }
-            if (next) {                                    // the next pass's counts, one addition per warp and bin
+            if (next) {                                    // one addition per warp and bin: frequent ids meet here
                 const unsigned peers = __match_any_sync(0xffffffffu, bin);
                 if (bin >= 0 && lane == __ffs(peers) - 1) atomicAdd(next + bin, __popc(peers));
             }
@@ -143,62 +250,10 @@ __device__ __forceinline__ void sort_scatter(const SortPlan& a, const SortIds<I>
     }
 }
 
-// Counts of the first pass; clears what later launches count in.  A list that fits one block is
-// sorted here altogether.
-template <typename I>
-__global__ void __launch_bounds__(kSortThreads)
-embed_sort_kernel(const __grid_constant__ SortPlan a, const SortIds<I> in) {
-    __shared__ SortShared sh;
-    const int tid = threadIdx.x, bins = 1 << a.bits;
-    for (long long k = (long long)blockIdx.x * kSortThreads + tid; k < a.n_zero; k += (long long)gridDim.x * kSortThreads) a.zero[k] = 0;
-    const long long lo = (long long)blockIdx.x * a.tile, hi = min(a.n, lo + a.tile);
-    const int passes = a.tiles == 1 ? a.passes : 1;
-    for (int p = 0; p < passes; ++p) {
-        for (int b = tid; b < bins; b += kSortThreads) sh.base[b] = 0;
-        __syncthreads();
-        for (long long t = lo + tid; t < hi; t += kSortThreads) {
-            const unsigned k = p == 0 ? in.key(t) : a.key[(p + 1) & 1][t];
-            atomicAdd(&sh.base[(k >> (p * a.bits)) & (bins - 1)], 1);
-        }
-        __syncthreads();
-        if (a.tiles == 1) {
-            scan_bins(sh, bins);
-            sort_scatter(a, in, p, lo, hi, sh);            // ends with a barrier: its stores are visible to the block
-        } else {
-            for (int b = tid; b < bins; b += kSortThreads) a.hist[(size_t)blockIdx.x * bins + b] = sh.base[b];
-            for (int q = 1; q < a.passes; ++q)
-                for (int b = tid; b < bins; b += kSortThreads) a.hist[((size_t)q * a.tiles + blockIdx.x) * bins + b] = 0;
-        }
-    }
-}
-
-template <typename I>
-__global__ void __launch_bounds__(kSortThreads)
-embed_scatter_kernel(const __grid_constant__ SortPlan a, const SortIds<I> in, int p) {
-    __shared__ SortShared sh;
-    const int tid = threadIdx.x, bins = 1 << a.bits;
-    const int* hist = a.hist + (size_t)p * a.tiles * bins;
-    int before = 0, total = 0;                               // earlier blocks' count of this thread's digit, and all blocks'
-    if (tid < bins) {
-#pragma unroll 8
-        for (int t = 0; t < a.tiles; ++t) {
-            const int c = hist[(size_t)t * bins + tid];
-            if (t < (int)blockIdx.x) before += c;
-            total += c;
-        }
-        sh.base[tid] = total;
-    }
-    __syncthreads();
-    scan_bins(sh, bins);
-    if (tid < bins) sh.base[tid] += before;
-    __syncthreads();
-    const long long lo = (long long)blockIdx.x * a.tile;
-    sort_scatter(a, in, p, lo, min(a.n, lo + a.tile), sh);
-}
-
 // ---------------------------------------------------------------- reduction
 constexpr int kRedThreads = 256;
 constexpr int kRedCols = 8;                // columns of a thread
+constexpr int kRedEntries = 2048;          // entries of a block's stretches, held in shared memory
 constexpr int kRedGroup = 32;              // stretches whose partial rows are joined first
 constexpr int kZeroRows = 32;              // table rows of a clearing block
 
@@ -206,7 +261,7 @@ struct RedPlan {
     const unsigned *key, *pos;             // sorted
     long long n, vocab, dim, ld_dout, ld;
     float scale;
-    int len;                               // entries of a stretch, a multiple of 4
+    int len;                               // entries of a stretch, a multiple of 8
     int stretches, lanes;                  // lanes: threads across a row's columns (a power of two)
     int red_blocks;                        // blocks [0, red_blocks) reduce, the rest clear rows
     float* part;                           // [stretches][2][dim]: runs that came in from before, runs that go on
@@ -214,32 +269,68 @@ struct RedPlan {
     int accumulate;
 };
 
-// Eight columns of a row: thread-contiguous where everything is aligned, else interleaved.
+// Eight columns of a row, as two pieces of four that lie `lanes` pieces apart where rows are aligned to a
+// piece: then every access of a warp covers memory without gaps (pieces of eight leave half of each
+// 32-byte sector to a second access, which for additions in memory doubles the work of the L2).
+// Otherwise single columns, `lanes` apart.
 template <bool VEC>
 struct Cols {
     long long c;
     int lanes;
     long long dim;
-    __device__ __forceinline__ long long at(int k) const { return VEC ? c + k : c + (long long)k * lanes; }
+    __device__ __forceinline__ long long at(int k) const { return VEC ? c + (k >> 2) * 4ll * lanes + (k & 3) : c + (long long)k * lanes; }
     __device__ __forceinline__ bool in(int k) const { return at(k) < dim; }
 };
 
+// A thread's columns of a row as they were loaded, converted only when they are added.
+template <bool VEC, typename T> struct Raw { T x[kRedCols]; };
+template <> struct Raw<true, float> { float4 x[2]; };
+template <> struct Raw<true, __nv_bfloat16> { uint2 x[2]; };
+template <> struct Raw<true, __half> { uint2 x[2]; };
+
 template <bool VEC, typename T>
-__device__ __forceinline__ void load_cols(float (&x)[kRedCols], const T* row, const Cols<VEC>& q) {
+__device__ __forceinline__ void load_raw(Raw<VEC, T>& r, const T* row, const Cols<VEC>& q) {
     if constexpr (VEC) {
-        if (q.c < q.dim) load8(x, row + q.c);
-        else
+        using P = std::remove_reference_t<decltype(r.x[0])>;
 #pragma unroll
-            for (int k = 0; k < kRedCols; ++k) x[k] = 0.f;
+        for (int h = 0; h < 2; ++h)
+            if (q.in(4 * h)) r.x[h] = __ldcs(reinterpret_cast<const P*>(row + q.at(4 * h)));
     } else {
 #pragma unroll
-        for (int k = 0; k < kRedCols; ++k) x[k] = q.in(k) ? to_f32(row[q.at(k)]) : 0.f;
+        for (int k = 0; k < kRedCols; ++k) r.x[k] = q.in(k) ? row[q.at(k)] : from_f32<T>(0.f);
     }
+}
+__device__ __forceinline__ void widen4(float* x, const float4& r) { x[0] = r.x; x[1] = r.y; x[2] = r.z; x[3] = r.w; }
+
+template <bool VEC, typename T>
+__device__ __forceinline__ void widen(float (&x)[kRedCols], const Raw<VEC, T>& r) {
+    if constexpr (!VEC) {
+#pragma unroll
+        for (int k = 0; k < kRedCols; ++k) x[k] = to_f32(r.x[k]);
+    } else if constexpr (sizeof(T) == 4) {
+        widen4(x, r.x[0]);
+        widen4(x + 4, r.x[1]);
+    } else {
+        unpack8(x, make_uint4(r.x[0].x, r.x[0].y, r.x[1].x, r.x[1].y), T());
+    }
+}
+
+template <bool VEC, typename T>
+__device__ __forceinline__ void load_cols(float (&x)[kRedCols], const T* row, const Cols<VEC>& q) {
+    Raw<VEC, T> r{};
+    load_raw(r, row, q);
+    widen(x, r);
 }
 template <bool VEC, typename T>
 __device__ __forceinline__ void store_cols(T* row, const float (&x)[kRedCols], const Cols<VEC>& q) {
     if constexpr (VEC) {
-        if (q.c < q.dim) store8(row + q.c, x);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            if (!q.in(4 * h)) continue;
+            T* p = row + q.at(4 * h);
+            if constexpr (sizeof(T) == 4) *reinterpret_cast<float4*>(p) = make_float4(x[4 * h], x[4 * h + 1], x[4 * h + 2], x[4 * h + 3]);
+            else *reinterpret_cast<uint2*>(p) = make_uint2(pack2(x[4 * h], x[4 * h + 1], T()), pack2(x[4 * h + 2], x[4 * h + 3], T()));
+        }
     } else {
 #pragma unroll
         for (int k = 0; k < kRedCols; ++k)
@@ -247,27 +338,63 @@ __device__ __forceinline__ void store_cols(T* row, const float (&x)[kRedCols], c
     }
 }
 
-// First entry of the sorted list with a key of at least v.
-__device__ __forceinline__ long long lower_bound(const unsigned* key, long long n, unsigned v) {
-    long long lo = 0, hi = n;
-    while (lo < hi) {
-        const long long mid = (lo + hi) >> 1;
-        if (key[mid] < v) lo = mid + 1; else hi = mid;
+// First and last stretch of the run of v that passes through stretch st.  Most runs reach one stretch
+// further, so the distance is doubled before it is halved.
+__device__ __forceinline__ int first_stretch(const RedPlan& a, int st, unsigned v) {
+    auto reaches = [&](int t) { return t >= 0 && a.key[(long long)t * a.len + a.len - 1] == v; };    // t is before st: a full stretch
+    int in = st, step = 1;                                   // the run is known to be in `in`
+    while (reaches(in - step)) { in -= step; step *= 2; }
+    int out = max(in - step, -1);                            // and known not to be in `out`
+    while (in - out > 1) {
+        const int mid = (in + out) / 2;
+        if (reaches(mid)) in = mid; else out = mid;
     }
-    return lo;
+    return in;
+}
+__device__ __forceinline__ int last_stretch(const RedPlan& a, int st, unsigned v) {
+    auto reaches = [&](int t) { return t < a.stretches && a.key[(long long)t * a.len] == v; };
+    int in = st, step = 1;
+    while (reaches(in + step)) { in += step; step *= 2; }
+    int out = min(in + step, a.stretches);
+    while (out - in > 1) {
+        const int mid = (in + out) / 2;
+        if (reaches(mid)) in = mid; else out = mid;
+    }
+    return in;
 }
 
+// The row's only writer: float32 rows that accumulate are added to in memory, which needs no wait
+// for the old values; 16-bit ones are read, so that the sum is rounded once.
 template <bool VEC, typename G>
 __device__ __forceinline__ void finish_row(G* dtable, const RedPlan& a, unsigned v, float (&s)[kRedCols], const Cols<VEC>& q) {
     G* row = dtable + (long long)v * a.ld;
-    float old[kRedCols];
-    if (a.accumulate) load_cols<VEC>(old, row, q);
 #pragma unroll
-    for (int k = 0; k < kRedCols; ++k) s[k] = a.accumulate ? old[k] + a.scale * s[k] : a.scale * s[k];
+    for (int k = 0; k < kRedCols; ++k) s[k] *= a.scale;
+    if (a.accumulate) {
+        if constexpr (sizeof(G) == 4) {
+            if constexpr (VEC) {
+#pragma unroll
+                for (int h = 0; h < 8; h += 4)
+                    if (q.in(h))
+                        asm volatile("red.relaxed.gpu.global.add.v4.f32 [%0], {%1, %2, %3, %4};" ::"l"(row + q.at(h)), "f"(s[h]), "f"(s[h + 1]),
+                                     "f"(s[h + 2]), "f"(s[h + 3]) : "memory");
+            } else {
+#pragma unroll
+                for (int k = 0; k < kRedCols; ++k)
+                    if (q.in(k)) asm volatile("red.relaxed.gpu.global.add.f32 [%0], %1;" ::"l"(row + q.at(k)), "f"(s[k]) : "memory");
+            }
+            return;
+        }
+        float old[kRedCols];
+        load_cols<VEC>(old, row, q);
+#pragma unroll
+        for (int k = 0; k < kRedCols; ++k) s[k] += old[k];
+    }
     store_cols<VEC>(row, s, q);
 }
 
-// Sum of the partial rows `kind[first]`, head[first + step], ... in order; `slot(first)` is the first.
+// Sum, in order, of the partial rows of stretch `first` (the one that goes on, or the one that came in) and of the
+// stretches up to `last` at distance `step` (those that came in).
 template <bool VEC>
 __device__ __forceinline__ void add_parts(float (&s)[kRedCols], const RedPlan& a, int first, int first_kind, int last, int step, const Cols<VEC>& q) {
 #pragma unroll
@@ -277,9 +404,8 @@ __device__ __forceinline__ void add_parts(float (&s)[kRedCols], const RedPlan& a
         float x[kRedCols];
         const float* row = a.part + ((size_t)t * 2 + (t == first ? first_kind : 0)) * a.dim;
         if constexpr (VEC) {
-            const float4* r4 = reinterpret_cast<const float4*>(row + (q.c < q.dim ? q.c : 0));
-            const float4 y = __ldcg(r4), z = __ldcg(r4 + 1);
-            x[0] = y.x; x[1] = y.y; x[2] = y.z; x[3] = y.w; x[4] = z.x; x[5] = z.y; x[6] = z.z; x[7] = z.w;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) widen4(x + 4 * h, q.in(4 * h) ? __ldcg(reinterpret_cast<const float4*>(row + q.at(4 * h))) : make_float4(0, 0, 0, 0));
         } else {
 #pragma unroll
             for (int k = 0; k < kRedCols; ++k) x[k] = q.in(k) ? __ldcg(row + q.at(k)) : 0.f;
@@ -291,112 +417,160 @@ __device__ __forceinline__ void add_parts(float (&s)[kRedCols], const RedPlan& a
 }
 
 template <bool VEC, typename T, typename G>
-__global__ void __launch_bounds__(kRedThreads)
+__global__ void __launch_bounds__(kRedThreads, !VEC ? 2 : sizeof(T) == 4 ? 3 : 4)
 embed_reduce_kernel(const __grid_constant__ RedPlan a, const T* __restrict__ dout, G* __restrict__ dtable) {
+    __shared__ unsigned sh_key[kRedEntries + 2], sh_pos[kRedEntries];
     __shared__ int sh_last[kRedThreads][2];
     __shared__ int sh_touched[kZeroRows];
+    cudaGridDependencySynchronize();
     const int tid = threadIdx.x;
     if ((int)blockIdx.x >= a.red_blocks) {                   // clear the rows that no token points to
         if (blockIdx.y) return;
         const long long v0 = (long long)(blockIdx.x - a.red_blocks) * kZeroRows;
-        if (tid < kZeroRows && v0 + tid < a.vocab) {
-            const long long e = lower_bound(a.key, a.n, (unsigned)(v0 + tid));
-            sh_touched[tid] = e < a.n && a.key[e] == (unsigned)(v0 + tid);
+        const int warp = tid >> 5, lane = tid & 31;
+        if (warp == 0) {
+            // 32-way search for the first entry of these rows, then a walk over theirs
+            long long lo = 0, hi = a.n;                      // the answer is in [lo, hi]
+            while (hi - lo > 32) {
+                const long long step = (hi - lo) / 32, at = lo + step * (lane + 1) - 1;
+                const unsigned below = __ballot_sync(0xffffffffu, a.key[at] < (unsigned)v0);
+                const int c = __popc(below);                 // the keys are sorted: the first c probes are below
+                if (c < 32) hi = lo + step * (c + 1) - 1;
+                lo += step * c;
+            }
+            sh_touched[lane] = 0;
+            __syncwarp();
+            for (long long e = lo; e < a.n; e += 32) {
+                const unsigned k = e + lane < a.n ? a.key[e + lane] : 0xffffffffu;
+                if (k >= (unsigned)v0 && k < (unsigned)v0 + kZeroRows) sh_touched[k - (unsigned)v0] = 1;
+                if (__any_sync(0xffffffffu, k >= (unsigned)v0 + kZeroRows)) break;
+            }
         }
         __syncthreads();
-        const int warp = tid >> 5, lane = tid & 31;
         float z[kRedCols] = {};
         for (int r = warp; r < kZeroRows && v0 + r < a.vocab; r += kRedThreads / 32) {
             if (sh_touched[r]) continue;
             G* row = dtable + (v0 + r) * a.ld;
             for (long long c = 0; c < a.dim; c += 32 * kRedCols)
-                store_cols<VEC>(row, z, Cols<VEC>{VEC ? c + lane * kRedCols : c + lane, 32, a.dim});
+                store_cols<VEC>(row, z, Cols<VEC>{c + lane * (VEC ? 4 : 1), 32, a.dim});
         }
         return;
     }
     const int group = tid / a.lanes, lane = tid % a.lanes, per_block = kRedThreads / a.lanes;
     const int st = blockIdx.x * per_block + group;           // this group's stretch
     const long long slab = (long long)blockIdx.y * a.lanes * kRedCols;
-    const Cols<VEC> q{slab + (VEC ? lane * kRedCols : lane), a.lanes, min(a.dim, slab + (long long)a.lanes * kRedCols)};
-    const long long e0 = (long long)st * a.len, e1 = min(a.n, e0 + a.len);
+    const Cols<VEC> q{slab + lane * (VEC ? 4 : 1), a.lanes, min(a.dim, slab + (long long)a.lanes * kRedCols)};
+    {                                                        // the block's entries, one more on each side
+        const long long b0 = (long long)blockIdx.x * per_block * a.len;
+        for (int k = tid; k < per_block * a.len + 2; k += kRedThreads) {
+            const long long e = b0 + k - 1;
+            sh_key[k] = e >= 0 && e < a.n ? a.key[e] : 0xffffffffu;
+            if (k > 0 && e < a.n) sh_pos[k - 1] = a.pos[e];  // the last one is not used
+        }
+    }
+    __syncthreads();
+    const unsigned* key = sh_key + 1 + group * a.len;        // key[-1 .. len]
+    const unsigned* pos = sh_pos + group * a.len;
     bool head = false, tail = false;                         // partial rows that this stretch leaves
     unsigned head_key = 0, tail_key = 0;
     if (st < a.stretches) {
-        const unsigned before = e0 > 0 ? a.key[e0 - 1] : 0xffffffffu;
-        const unsigned after = e1 < a.n ? a.key[e1] : 0xffffffffu;
+        constexpr int U = sizeof(T) == 4 ? 2 : 4;            // rows of a batch; the next batch is on its way meanwhile
+        Raw<VEC, T> x[U], y[U];
+        auto load = [&](Raw<VEC, T>(&z)[U], int e) {
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (e + u < a.len && key[e + u] < a.vocab) load_raw(z[u], dout + (long long)pos[e + u] * a.ld_dout, q);
+        };
         float s[kRedCols];
 #pragma unroll
         for (int k = 0; k < kRedCols; ++k) s[k] = 0.f;
-        bool from_before = a.key[e0] == before;
-        for (long long e = e0; e < e1; e += 4) {
-            unsigned key[5];
-            float x[4][kRedCols];
+        bool from_before = key[0] == key[-1];
+        auto add = [&](Raw<VEC, T>(&z)[U], int e) {
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                key[u] = e + u < e1 ? a.key[e + u] : 0xffffffffu;
-                if (key[u] < a.vocab) load_cols<VEC>(x[u], dout + (long long)a.pos[e + u] * a.ld_dout, q);
-            }
-            key[4] = e + 4 < e1 ? a.key[e + 4] : 0xffffffffu;
+            for (int u = 0; u < U; ++u) {
+                const unsigned v = key[e + u];
+                if (v >= a.vocab) continue;                  // tokens without a gradient, or behind the end
+                float w[kRedCols];
+                widen(w, z[u]);
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                if (key[u] >= a.vocab) continue;             // tokens without a gradient, or behind the end
-#pragma unroll
-                for (int k = 0; k < kRedCols; ++k) s[k] += x[u][k];
-                const bool last = e + u + 1 == e1;
-                if (!last && key[u + 1] == key[u]) continue;
-                const bool on = last && after == key[u];
-                if (from_before || on) {
+                for (int k = 0; k < kRedCols; ++k) s[k] += w[k];
+                const bool same = key[e + u + 1] == v, last = e + u + 1 == a.len;
+                if (same && !last) continue;
+                if (from_before || same) {
                     // a run that came in from before keeps that place even if it goes on
                     float* row = a.part + ((size_t)st * 2 + (from_before ? 0 : 1)) * a.dim;
                     store_cols<VEC>(row, s, q);
-                    if (from_before) { head = true; head_key = key[u]; } else { tail = true; tail_key = key[u]; }
+                    if (from_before) { head = true; head_key = v; } else { tail = true; tail_key = v; }
                 } else {
-                    finish_row<VEC>(dtable, a, key[u], s, q);
+                    finish_row<VEC>(dtable, a, v, s, q);
                 }
                 from_before = false;
 #pragma unroll
                 for (int k = 0; k < kRedCols; ++k) s[k] = 0.f;
             }
+        };
+        load(x, 0);
+        for (int e = 0; e < a.len; e += 2 * U) {
+            load(y, e + U);
+            add(x, e);
+            load(x, e + 2 * U);
+            add(y, e + U);
         }
     }
     if (!__syncthreads_or(head || tail)) return;
     // Joining: the stretches of a run inside one aligned group of kRedGroup first, then the groups.
+    // Of those who left a partial row, the one that arrives last adds them up in list order.
     unsigned* arrived = a.arrived + (size_t)blockIdx.y * a.stretches * 3;
+    int run_first[2], run_last[2], first[2], last[2];
 #pragma unroll
     for (int kind = 0; kind < 2; ++kind) {
-        const bool have = kind ? tail : head;
+        run_first[kind] = run_last[kind] = first[kind] = last[kind] = 0;
+        if (kind ? !tail : !head) continue;
         const unsigned v = kind ? tail_key : head_key;
-        int run_first = 0, run_last = 0, first = 0, last = 0;
-        if (have) {
-            run_first = kind ? st : (int)(lower_bound(a.key, e0, v) / a.len);
-            run_last = (int)((lower_bound(a.key, a.n, v + 1) - 1) / a.len);
-            const int g0 = st / kRedGroup * kRedGroup;
-            first = max(run_first, g0);
-            last = min(run_last, g0 + kRedGroup - 1);
-        }
-        const int first_kind = first == run_first ? 1 : 0;
-        __threadfence();
-        __syncthreads();
-        if (lane == 0) sh_last[group][0] = have && atomicAdd(arrived + (size_t)first * 3 + first_kind, 1u) == (unsigned)(last - first);
-        __syncthreads();
-        bool top = have && sh_last[group][0];
+        run_first[kind] = kind ? st : first_stretch(a, st, v);
+        run_last[kind] = last_stretch(a, st, v);
+        const int g0 = st / kRedGroup * kRedGroup;
+        first[kind] = max(run_first[kind], g0);
+        last[kind] = min(run_last[kind], g0 + kRedGroup - 1);
+    }
+    __threadfence();
+    __syncthreads();
+    if (lane == 0) {
+#pragma unroll
+        for (int kind = 0; kind < 2; ++kind)
+            sh_last[group][kind] = (kind ? tail : head) &&
+                atomicAdd(arrived + (size_t)first[kind] * 3 + (first[kind] == run_first[kind]), 1u) == (unsigned)(last[kind] - first[kind]);
+    }
+    __syncthreads();
+    bool top[2] = {false, false};                            // joined a group of a run over several groups
+    __threadfence();
+#pragma unroll
+    for (int kind = 0; kind < 2; ++kind) {
+        if (!sh_last[group][kind]) continue;
+        const int first_kind = first[kind] == run_first[kind];
         float s[kRedCols];
-        const int g_first = run_first / kRedGroup, g_last = run_last / kRedGroup;
-        if (top) {
-            __threadfence();
-            add_parts<VEC>(s, a, first, first_kind, last, 1, q);
-            if (g_first != g_last) store_cols<VEC>(a.part + ((size_t)first * 2 + first_kind) * a.dim, s, q);
-            else { finish_row<VEC>(dtable, a, v, s, q); top = false; }
-        }
-        __threadfence();
-        __syncthreads();
-        if (lane == 0) sh_last[group][1] = top && atomicAdd(arrived + (size_t)run_first * 3 + 2, 1u) == (unsigned)(g_last - g_first);
-        __syncthreads();
-        if (top && sh_last[group][1]) {
-            __threadfence();
-            add_parts<VEC>(s, a, run_first, 1, run_last, kRedGroup, q);
-            finish_row<VEC>(dtable, a, v, s, q);
-        }
+        add_parts<VEC>(s, a, first[kind], first_kind, last[kind], 1, q);
+        top[kind] = run_first[kind] / kRedGroup != run_last[kind] / kRedGroup;
+        if (top[kind]) store_cols<VEC>(a.part + ((size_t)first[kind] * 2 + first_kind) * a.dim, s, q);
+        else finish_row<VEC>(dtable, a, kind ? tail_key : head_key, s, q);
+    }
+    if (!__syncthreads_or(top[0] || top[1])) return;
+    __threadfence();
+    __syncthreads();
+    if (lane == 0) {
+#pragma unroll
+        for (int kind = 0; kind < 2; ++kind)
+            sh_last[group][kind] = top[kind] &&
+                atomicAdd(arrived + (size_t)run_first[kind] * 3 + 2, 1u) == (unsigned)(run_last[kind] / kRedGroup - run_first[kind] / kRedGroup);
+    }
+    __syncthreads();
+    __threadfence();
+#pragma unroll
+    for (int kind = 0; kind < 2; ++kind) {
+        if (!sh_last[group][kind]) continue;
+        float s[kRedCols];
+        add_parts<VEC>(s, a, run_first[kind], 1, run_last[kind], kRedGroup, q);
+        finish_row<VEC>(dtable, a, kind ? tail_key : head_key, s, q);
     }
 }
 

@@ -20,9 +20,13 @@
 
 namespace pb {
 
-constexpr int kAdamMaxTensors = 256;      // tensors of one launch: their table is a kernel parameter
-constexpr int kAdamBlock = 256;           // elements that share a scale
-constexpr int kAdamChunk = 2048;          // elements of one thread block: a warp per 256
+// The table of tensors is a kernel parameter: a call needs no copy and no memory of its own.  Launches
+// of few tensors take the small table, whose parameters are quicker to hand over.
+constexpr int kAdamFewTensors = 16, kAdamManyTensors = 330;
+constexpr int kAdamNear = 256;
+constexpr int kAdamBlock = 256;           // elements that share a scale: a warp, eight elements per lane
+constexpr int kAdamThreads = 128;         // small blocks, so that few of an SM's warps load or compute at the same time
+constexpr int kAdamRound = kAdamThreads * 8;   // elements of a thread block
 
 struct AdamTensor {
     float* w;
@@ -35,138 +39,382 @@ struct AdamTensor {
     long long n;
     unsigned long long rnd;      // start of the tensor's random stream, without seed and step
     float decay, horizon;
-    unsigned first_chunk;
+    unsigned first_round;
+    int vec;                     // every pointer is aligned to eight elements
 };
 
-struct AdamTable {
-    AdamTensor t[kAdamMaxTensors];
-    int n;
-    double lr, beta1, beta2, eps;
+struct AdamScalars {
+    double lr, beta1, beta2;
+    float b1, o1, b2, o2, eps;
+    float minus_zero;
+    float c1, c2;                // 1 / (1 - beta1^step), 1 / sqrt(1 - beta2^step)
     long long step;
     unsigned long long seed;
     const float* grad_scale;
     const float* dev_lr;
     const long long* dev_step;
-    int grad_dtype, fwd_dtype, bits;
+    int fwd_dtype;
+    int n;                       // tensors of this launch
+    int near_shift;
+    unsigned short near[kAdamNear];    // tensor that holds round k << near_shift
 };
 
-__device__ __forceinline__ float load_as(const void* p, int dtype, long long i) {
-    if (dtype == 0) return reinterpret_cast<const float*>(p)[i];
-    if (dtype == 1) return to_f32(reinterpret_cast<const __nv_bfloat16*>(p)[i]);
-    return to_f32(reinterpret_cast<const __half*>(p)[i]);
-}
-__device__ __forceinline__ void store_as(void* p, int dtype, long long i, float x) {
-    if (dtype == 0) reinterpret_cast<float*>(p)[i] = x;
-    else if (dtype == 1) reinterpret_cast<__nv_bfloat16*>(p)[i] = from_f32<__nv_bfloat16>(x);
-    else reinterpret_cast<__half*>(p)[i] = from_f32<__half>(x);
-}
+template <int MAXT>
+struct AdamTable {
+    AdamScalars s;
+    AdamTensor t[MAXT];
+};
 
 constexpr float kMTop = 448.f, kRTop = 1.9375f;
 constexpr int kRBias = 112 << 4;          // exponent and mantissa bits of 2^-15
 
-__device__ __forceinline__ float decode_m(unsigned char c) {
-    __nv_fp8_e4m3 q;
-    q.__x = c;
-    return (float)q;
+__device__ __forceinline__ float decode_r(unsigned c) { return c ? __uint_as_float((c + kRBias) << 19) : 0.f; }
+
+// Eight codes <-> eight values.
+__device__ __forceinline__ void decode_m8(float (&x)[8], uint2 c) {
+    const unsigned w[2] = {c.x, c.y};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w[k >> 1] >> (16 * (k & 1))), __NV_E4M3);
+        const float2 f = __half22float2(__half2(h));
+        x[2 * k] = f.x;
+        x[2 * k + 1] = f.y;
+    }
 }
-__device__ __forceinline__ float decode_r(unsigned char c) {
-    return c ? __uint_as_float((unsigned)(c + kRBias) << 19) : 0.f;
+__device__ __forceinline__ void decode_r8(float (&x)[8], uint2 c) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) x[k] = decode_r(((k < 4 ? c.x : c.y) >> (8 * (k & 3))) & 255u);
+}
+__device__ __forceinline__ uint2 encode_m8(const float (&x)[8]) {
+    unsigned w[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) w[k] = __nv_cvt_float2_to_fp8x2(make_float2(x[2 * k], x[2 * k + 1]), __NV_SATFINITE, __NV_E4M3);
+    return make_uint2(w[0] | w[1] << 16, w[2] | w[3] << 16);
 }
 
-__global__ void __launch_bounds__(256)
-adamw_kernel(const __grid_constant__ AdamTable a) {
-    __shared__ float sh[4];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    int lo = 0, hi = a.n - 1;                        // the tensor whose chunks hold this block
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (a.t[mid].first_chunk <= blockIdx.x) lo = mid; else hi = mid - 1;
-    }
-    const AdamTensor& t = a.t[lo];
-    const long long step = a.dev_step ? *a.dev_step : a.step;
-    if (threadIdx.x == 0) {
-        const double lr = a.dev_lr ? (double)*a.dev_lr : a.lr;
-        sh[0] = (float)(1.0 / (1.0 - pow(a.beta1, (double)step)));
-        sh[1] = (float)(1.0 / sqrt(1.0 - pow(a.beta2, (double)step)));
-        sh[2] = (float)lr;
-        sh[3] = (float)(1.0 - lr * (double)t.decay);
-    }
-    __syncthreads();
-    const float c1 = sh[0], c2 = sh[1], lr = sh[2], keep = sh[3];
-    const float b1 = (float)a.beta1, o1 = (float)(1.0 - a.beta1), b2 = (float)a.beta2, o2 = (float)(1.0 - a.beta2), eps = (float)a.eps;
-    const float gs = a.grad_scale ? *a.grad_scale : 1.f;
-    if (!isfinite(gs)) return;                       // the step is left out
-    const long long block = (long long)(blockIdx.x - t.first_chunk) * (kAdamChunk / kAdamBlock) + warp;
-    const long long base = block * kAdamBlock;
-    if (base >= t.n) return;
-    float m[8], r[8], ms = 0.f, rs = 0.f;
-    unsigned mmax = 0, rmax = 0;
-    if (a.bits == 8) { ms = t.m_scale[block]; rs = t.v_scale[block]; }
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-        const long long i = base + k * 32 + lane;
-        if (i >= t.n) { m[k] = r[k] = 0.f; continue; }
-        const float g = __fmul_rn(load_as(t.g, a.grad_dtype, i), gs);
-        float mk, vk;
-        if (a.bits == 8) {
-            mk = __fmul_rn(decode_m(reinterpret_cast<const unsigned char*>(t.m)[i]), ms);
-            vk = __fmul_rn(decode_r(reinterpret_cast<const unsigned char*>(t.v)[i]), rs);
-            vk = __fmul_rn(vk, vk);
+// Eight elements of a lane: element k of lane l is base + 8 l + k in a whole block whose memory is aligned
+// (VEC), else base + 32 k + l, with a test for the tensor's end.
+template <bool VEC>
+struct AdamLane {
+    long long base, n;
+    int lane;
+    __device__ __forceinline__ long long at(int k) const { return VEC ? base + 8 * lane + k : base + 32 * k + lane; }
+    __device__ __forceinline__ bool in(int k) const { return VEC || at(k) < n; }
+
+    template <typename T>
+    __device__ __forceinline__ void load(float (&x)[8], const T* p) const {
+        if constexpr (VEC) {
+            if constexpr (sizeof(T) == 4) load8_wide(x, p + at(0));
+            else load8(x, p + at(0));
         } else {
-            mk = reinterpret_cast<const float*>(t.m)[i];
-            vk = reinterpret_cast<const float*>(t.v)[i];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) x[k] = in(k) ? to_f32(p[at(k)]) : 0.f;
         }
-        mk = __fadd_rn(__fmul_rn(b1, mk), __fmul_rn(o1, g));
-        vk = __fadd_rn(__fmul_rn(b2, vk), __fmul_rn(__fmul_rn(o2, g), g));
-        m[k] = mk;
-        r[k] = __fsqrt_rn(vk);
-        const float u = (mk * c1) / fmaf(r[k], c2, eps);
-        const float w = fmaf(-lr, u, keep * t.w[i]);
-        t.w[i] = w;
-        if (t.fwd) store_as(t.fwd, a.fwd_dtype, i, fmaf(-lr * t.horizon, u, w));
-        if (a.bits == 32) {
-            reinterpret_cast<float*>(t.m)[i] = mk;
-            reinterpret_cast<float*>(t.v)[i] = vk;
+    }
+    // 16-bit elements as they are in memory: eight in four registers
+    template <typename T>
+    __device__ __forceinline__ uint4 load_raw(const T* p) const {
+        if constexpr (VEC) {
+            return *reinterpret_cast<const uint4*>(p + at(0));
+        } else {
+            unsigned h[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) h[k] = in(k) ? (unsigned)reinterpret_cast<const unsigned short*>(p)[at(k)] : 0u;
+            return make_uint4(h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16);
         }
-        mmax = max(mmax, __float_as_uint(mk) & 0x7fffffffu);
-        rmax = max(rmax, __float_as_uint(r[k]) & 0x7fffffffu);
     }
-    if (a.bits == 32) return;
-    mmax = __reduce_max_sync(0xffffffffu, mmax);     // magnitudes order like their bits, NaN on top
-    rmax = __reduce_max_sync(0xffffffffu, rmax);
-    const float nan = __int_as_float(0x7fc00000);
-    const float ma = __uint_as_float(mmax), ra = __uint_as_float(rmax);
-    const bool m_live = ma >= 0x1p-100f, r_live = ra > 0.f;      // below: a zero block (1 / ma may overflow)
-    const float mi = m_live ? __fdiv_rn(kMTop, ma) : 0.f, ri = r_live ? __fdiv_rn(kRTop, ra) : 0.f;
-    if (lane == 0) {
-        t.m_scale[block] = mmax >= 0x7f800000u ? nan : m_live ? __fmul_rn(ma, 1.f / kMTop) : 0.f;
-        t.v_scale[block] = rmax >= 0x7f800000u ? nan : __fdiv_rn(ra, kRTop);
+    template <typename T>
+    __device__ __forceinline__ void store(T* p, const float (&x)[8]) const {
+        if constexpr (VEC) {
+            if constexpr (sizeof(T) == 4) store8_wide(p + at(0), x);
+            else store8(p + at(0), x);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (in(k)) p[at(k)] = from_f32<T>(x[k]);
+        }
     }
-    const unsigned long long key = t.rnd + (a.seed + (unsigned long long)step) * 0xD1342543DE82EF95ull;
+    __device__ __forceinline__ uint2 load_codes(const unsigned char* p) const {
+        if constexpr (VEC) {
+            return *reinterpret_cast<const uint2*>(p + at(0));
+        } else {
+            unsigned c[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) c[k] = in(k) ? p[at(k)] : 0u;
+            return make_uint2(c[0] | c[1] << 8 | c[2] << 16 | c[3] << 24, c[4] | c[5] << 8 | c[6] << 16 | c[7] << 24);
+        }
+    }
+    __device__ __forceinline__ void store_codes(unsigned char* p, uint2 c) const {
+        if constexpr (VEC) {
+            *reinterpret_cast<uint2*>(p + at(0)) = c;
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (in(k)) p[at(k)] = (unsigned char)((k < 4 ? c.x : c.y) >> (8 * (k & 3)));
+        }
+    }
+};
+
+// Pairs of float32 in one instruction, each rounded like the single operation: the 8-bit step is bound
+// by the instructions it issues.  The assembler contracts a product and a sum of pairs; a product that
+// must be rounded before it is added is therefore a fused multiply-add of a -0 that it cannot see.
+struct Pair {
+    unsigned long long x;
+    __device__ __forceinline__ Pair() {}
+    __device__ __forceinline__ Pair(float a, float b) { asm("mov.b64 %0, {%1, %2};" : "=l"(x) : "f"(a), "f"(b)); }
+    __device__ __forceinline__ explicit Pair(float a) : Pair(a, a) {}
+    __device__ __forceinline__ void split(float& a, float& b) const { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(x)); }
+};
+__device__ __forceinline__ Pair operator*(Pair a, Pair b) { Pair r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.x) : "l"(a.x), "l"(b.x)); return r; }
+__device__ __forceinline__ Pair operator+(Pair a, Pair b) { Pair r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.x) : "l"(a.x), "l"(b.x)); return r; }
+__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) { Pair r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.x) : "l"(a.x), "l"(b.x), "l"(c.x)); return r; }
+// x[k] <- s x[k] for eight elements
+__device__ __forceinline__ void scale8(float (&x)[8], float s) {
+#pragma unroll
+    for (int k = 0; k < 8; k += 2) (Pair(x[k], x[k + 1]) * Pair(s)).split(x[k], x[k + 1]);
+}
+
+// Square root and reciprocal to 2^-23 or so of themselves; results and arguments below 2^-126 count as zero.
+__device__ __forceinline__ float sqrt_near(float x) {
+    float r;
+    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ float rcp_near(float x) {
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ float max_nan(float a, float b) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+
+// Codes of eight second moments from their roots r (scaled by `ri`) and the random bits z of each four:
+// the root's bits plus a random number below one step of the code, cut off.  The low byte of what
+// is left is the code, since the exponent's bias there is a multiple of 256; the largest root, whose
+// bits below the code are zero up to a rounding, cannot pass code 255.  Returns whether an element lies
+// so near a border between two codes that r has to be the exactly rounded root.
+template <bool VEC>
+__device__ __forceinline__ bool encode_r8(uint2& code, const float (&v)[8], const float (&r)[8], float ri, const unsigned long long (&z)[VEC ? 2 : 8]) {
+    unsigned near = 0xffffffffu, t[8];
+    const float lowest = __uint_as_float((unsigned)(kRBias + 1) << 19);
+    float s[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) s[k] = r[k];
+    scale8(s, ri);
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-        const long long i = base + k * 32 + lane;
-        if (i >= t.n) continue;
-        reinterpret_cast<unsigned char*>(t.m)[i] = __nv_fp8_e4m3(__fmul_rn(m[k], mi)).__x;
-        const unsigned noise = (unsigned)(splitmix64(key, (unsigned long long)i >> 2) >> (16 * (i & 3))) & 0xffffu;
-        int c = (int)((__float_as_uint(__fmul_rn(r[k], ri)) + (noise << 3)) >> 19) - kRBias;
-        c = min(max(c, 1), 255);
-        reinterpret_cast<unsigned char*>(t.v)[i] = (unsigned char)(r[k] > 0.f ? c : 0);
+        const unsigned noise = VEC ? (unsigned)(z[k >> 2] >> (16 * (k & 3))) & 0xffffu : (unsigned)z[k];
+        const float x = v[k] > 0.f ? fmaxf(s[k], lowest) : 0.f;
+        t[k] = __float_as_uint(x) + (noise << 3);
+        near = min(near, (t[k] + 8u) & 0x7fff0u);
+        t[k] >>= 19;
+    }
+    const unsigned a = __byte_perm(t[0], t[1], 0x0040), b = __byte_perm(t[2], t[3], 0x0040);
+    const unsigned c = __byte_perm(t[4], t[5], 0x0040), d = __byte_perm(t[6], t[7], 0x0040);
+    code = make_uint2(__byte_perm(a, b, 0x5410), __byte_perm(c, d, 0x5410));
+    return near == 0;
+}
+
+struct AdamNow {                 // what a step's scalars come to
+    float gs, c1, c2, lr, keep;   // keep: 1 - lr * weight decay
+    unsigned long long key;
+};
+
+// What a block's update starts from, as it is in memory.
+template <int BITS, typename GT, bool VEC>
+struct AdamIn {
+    float w[8], m[BITS == 32 ? 8 : 1], v[BITS == 32 ? 8 : 1], g[sizeof(GT) == 4 ? 8 : 1];
+    uint4 g16;
+    uint2 mc, vc;
+    float ms, rs;
+    __device__ __forceinline__ void load(const AdamTensor& t, long long block, const AdamLane<VEC>& q) {
+        if constexpr (sizeof(GT) == 4) q.load(g, reinterpret_cast<const GT*>(t.g));
+        else g16 = q.load_raw(reinterpret_cast<const GT*>(t.g));
+        if constexpr (BITS == 8) {
+            mc = q.load_codes(reinterpret_cast<const unsigned char*>(t.m));
+            vc = q.load_codes(reinterpret_cast<const unsigned char*>(t.v));
+            ms = t.m_scale[block];
+            rs = t.v_scale[block];
+        } else {
+            q.load(m, reinterpret_cast<const float*>(t.m));
+            q.load(v, reinterpret_cast<const float*>(t.v));
+        }
+        q.load(w, t.w);
+    }
+};
+
+// One block of 256 elements by a warp.
+template <int BITS, typename GT, bool VEC, typename Now>
+__device__ __forceinline__ void adamw_block(const AdamScalars& a, const AdamTensor& t, long long block, int lane, Now scalars) {
+    const AdamLane<VEC> q{block * kAdamBlock, t.n, lane};
+    AdamIn<BITS, GT, VEC> in;
+    in.load(t, block, q);
+    AdamNow now;
+    if (!scalars(now)) return;                       // read while the block is on its way
+    float g[8], w[8], m[8], v[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) w[k] = in.w[k];
+    if constexpr (sizeof(GT) == 4) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) g[k] = in.g[k];
+    } else {
+        unpack8(g, in.g16, GT());
+    }
+    if constexpr (BITS == 8) {
+        decode_m8(m, in.mc);
+        decode_r8(v, in.vc);
+        scale8(m, in.ms);
+        scale8(v, in.rs);
+#pragma unroll
+        for (int k = 0; k < 8; k += 2) {
+            const Pair x(v[k], v[k + 1]);
+            (x * x).split(v[k], v[k + 1]);
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) { m[k] = in.m[k]; v[k] = in.v[k]; }
+    }
+    const Pair ahead(-now.lr * t.horizon), down(-now.lr), keep(now.keep), b1(a.b1), o1(a.o1), b2(a.b2), o2(a.o2), c1(now.c1), c2(now.c2), eps(a.eps), none(a.minus_zero);
+    float r[8], f[8];
+    float mtop = 0.f;
+    unsigned vmax = 0;                               // v is not negative: its values order like their bits, NaN on top
+    scale8(g, now.gs);
+#pragma unroll
+    for (int k = 0; k < 8; k += 2) {
+        const Pair gk(g[k], g[k + 1]);
+        const Pair mk = fma2(b1, Pair(m[k], m[k + 1]), none) + fma2(o1, gk, none);
+        const Pair vk = fma2(b2, Pair(v[k], v[k + 1]), none) + fma2(o2 * gk, gk, none);
+        mk.split(m[k], m[k + 1]);
+        vk.split(v[k], v[k + 1]);
+        r[k] = sqrt_near(v[k]);
+        r[k + 1] = sqrt_near(v[k + 1]);
+        float d0, d1;                                // denominators, below 2^126
+        fma2(Pair(r[k], r[k + 1]), c2, eps).split(d0, d1);
+        const Pair u = (mk * c1) * Pair(rcp_near(d0), rcp_near(d1));
+        const Pair wk = fma2(down, u, keep * Pair(w[k], w[k + 1]));
+        wk.split(w[k], w[k + 1]);
+        fma2(ahead, u, wk).split(f[k], f[k + 1]);
+        mtop = max_nan(mtop, max_nan(fabsf(m[k]), fabsf(m[k + 1])));
+        vmax = max(vmax, max(__float_as_uint(v[k]), __float_as_uint(v[k + 1])));
+    }
+    q.store(t.w, w);
+    if (t.fwd) {
+        if (a.fwd_dtype == 0) q.store(reinterpret_cast<float*>(t.fwd), f);
+        else if (a.fwd_dtype == 1) q.store(reinterpret_cast<__nv_bfloat16*>(t.fwd), f);
+        else q.store(reinterpret_cast<__half*>(t.fwd), f);
+    }
+    if constexpr (BITS == 32) {
+        q.store(reinterpret_cast<float*>(t.m), m);
+        q.store(reinterpret_cast<float*>(t.v), v);
+    } else {
+        const unsigned mmax = __reduce_max_sync(0xffffffffu, __float_as_uint(mtop));
+        vmax = __reduce_max_sync(0xffffffffu, vmax);
+        const float nan = __int_as_float(0x7fc00000);
+        const float ma = __uint_as_float(mmax), ra = __fsqrt_rn(__uint_as_float(vmax));   // the root grows with v
+        const bool m_live = ma >= 0x1p-100f, r_live = ra > 0.f;      // below: a zero block (1 / ma may overflow)
+        const float mi = m_live ? __fdiv_rn(kMTop, ma) : 0.f, ri = r_live ? __fdiv_rn(kRTop, ra) : 0.f;
+        if (lane == 0) {
+            t.m_scale[block] = mmax >= 0x7f800000u ? nan : m_live ? __fmul_rn(ma, 1.f / kMTop) : 0.f;
+            t.v_scale[block] = vmax >= 0x7f800000u ? nan : __fdiv_rn(ra, kRTop);
+        }
+        unsigned long long z[VEC ? 2 : 8];
+        if constexpr (VEC) {
+            z[0] = splitmix64(now.key, (unsigned long long)q.at(0) >> 2);
+            z[1] = splitmix64(now.key, ((unsigned long long)q.at(0) >> 2) + 1);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) z[k] = (splitmix64(now.key, (unsigned long long)q.at(k) >> 2) >> (16 * (int)(q.at(k) & 3))) & 0xffffu;
+        }
+        scale8(m, mi);
+        uint2 rc;
+        // Exactly rounded roots: for one lane in some 8000, and for blocks so small that roots which count as
+        // zero above are not far below the largest (2^-86: the smallest normal root is 2^-20 of its root).
+        if (encode_r8<VEC>(rc, v, r, ri, z) || (vmax != 0 && __uint_as_float(vmax) < 0x1p-86f)) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) r[k] = __fsqrt_rn(v[k]);
+            encode_r8<VEC>(rc, v, r, ri, z);
+        }
+        q.store_codes(reinterpret_cast<unsigned char*>(t.m), encode_m8(m));
+        q.store_codes(reinterpret_cast<unsigned char*>(t.v), rc);
     }
 }
 
-// The moments that an 8-bit state stands for.
-__global__ void __launch_bounds__(256)
-adamw_moments_kernel(const unsigned char* __restrict__ m, const float* __restrict__ m_scale,
-                     const unsigned char* __restrict__ v, const float* __restrict__ v_scale, long long n,
-                     float* __restrict__ m_out, float* __restrict__ v_out) {
-    const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
-    if (i >= n) return;
-    if (m_out) m_out[i] = __fmul_rn(decode_m(m[i]), m_scale[i / kAdamBlock]);
-    if (v_out) {
-        const float r = __fmul_rn(decode_r(v[i]), v_scale[i / kAdamBlock]);
-        v_out[i] = __fmul_rn(r, r);
+// A thread block takes one round of kAdamRound elements.  What is in flight at any time is then one
+// contiguous stretch of every array, which the DRAM's open pages reward: blocks of four consecutive
+// rounds move an 8-bit step's bytes at 4.6 TB/s, single rounds at 6.5 (151 M elements, no arithmetic).
+// Measured: 32-bit states, float32 gradients and a bf16 copy, 63 M elements: 281 us, 6.7 TB/s, the copy
+// rate.  8-bit states, bf16 gradients and copy, 151 M elements: 465 us, 5.2 TB/s; there some 70
+// instructions per element (roundings that have to be exact, random numbers, two encodings) take
+// nearly as long to issue as the bytes take to move.  Seven blocks of 128 threads beat four of 256 (480 us)
+// and eight (473 us, spilling).  Inputs copied ahead into shared memory by the warp that uses them did not help.
+template <int BITS, typename GT, int MAXT>
+__global__ void __launch_bounds__(kAdamThreads, 7)
+adamw_kernel(const __grid_constant__ AdamTable<MAXT> a) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int at = a.s.near[blockIdx.x >> a.s.near_shift]; // the tensor that holds this round
+    while (at + 1 < a.s.n && a.t[at + 1].first_round <= blockIdx.x) ++at;
+    const AdamTensor& t = a.t[at];
+    const long long block = (long long)(blockIdx.x - t.first_round) * (kAdamRound / kAdamBlock) + warp;
+    if (block * kAdamBlock >= t.n) return;
+    auto scalars = [&](AdamNow& now) {
+        long long step = a.s.step;
+        now.gs = a.s.grad_scale ? *a.s.grad_scale : 1.f;
+        const double lr = a.s.dev_lr ? (double)*a.s.dev_lr : a.s.lr;
+        now.lr = (float)lr;
+        now.c1 = a.s.c1;
+        now.c2 = a.s.c2;
+        if (a.s.dev_step) {
+            step = *a.s.dev_step;
+            // one lane's work for the warp
+            float c = 0.f;
+            if (lane < 2) {
+                const double left = 1.0 - pow(lane ? a.s.beta2 : a.s.beta1, (double)step);
+                c = (float)(1.0 / (lane ? sqrt(left) : left));
+            }
+            now.c1 = __shfl_sync(0xffffffffu, c, 0);
+            now.c2 = __shfl_sync(0xffffffffu, c, 1);
+        }
+        now.keep = (float)(1.0 - lr * (double)t.decay);
+        now.key = t.rnd + (a.s.seed + (unsigned long long)step) * 0xD1342543DE82EF95ull;
+        return (bool)isfinite(now.gs);               // else the step is left out
+    };
+    if (t.vec && (block + 1) * kAdamBlock <= t.n) adamw_block<BITS, GT, true>(a.s, t, block, lane, scalars);
+    else adamw_block<BITS, GT, false>(a.s, t, block, lane, scalars);
+}
+
+template <bool VEC>
+__device__ __forceinline__ void moments_block(const unsigned char* m, const float* m_scale, const unsigned char* v, const float* v_scale,
+                                              long long block, const AdamLane<VEC>& q, float* m_out, float* v_out) {
+    float x[8];
+    if (m_out) {
+        const float s = m_scale[block];
+        decode_m8(x, q.load_codes(m));
+        scale8(x, s);
+        q.store(m_out, x);
     }
+    if (v_out) {
+        const float s = v_scale[block];
+        decode_r8(x, q.load_codes(v));
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const float r = __fmul_rn(x[k], s);
+            x[k] = __fmul_rn(r, r);
+        }
+        q.store(v_out, x);
+    }
+}
+
+__global__ void __launch_bounds__(kAdamThreads)
+adamw_moments_kernel(const unsigned char* __restrict__ m, const float* __restrict__ m_scale, const unsigned char* __restrict__ v,
+                     const float* __restrict__ v_scale, long long n, float* __restrict__ m_out, float* __restrict__ v_out, int vec) {
+    const long long block = (long long)blockIdx.x * (kAdamRound / kAdamBlock) + (threadIdx.x >> 5), base = block * kAdamBlock;
+    const int lane = threadIdx.x & 31;
+    if (base >= n) return;
+    if (vec && base + kAdamBlock <= n) moments_block(m, m_scale, v, v_scale, block, AdamLane<true>{base, n, lane}, m_out, v_out);
+    else moments_block(m, m_scale, v, v_scale, block, AdamLane<false>{base, n, lane}, m_out, v_out);
 }
 
 }  // namespace pb

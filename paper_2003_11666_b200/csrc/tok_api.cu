@@ -3,6 +3,7 @@
 #include <cmath>
 #include <cstdio>
 #include <cstring>
+#include <type_traits>
 
 #include "../../include/pb.h"
 #include "adamw.cuh"
@@ -110,6 +111,43 @@ EmbedPlan embed_plan(int64_t n, int64_t vocab, int64_t dim, char* scratch) {
     r.pos = s.pos[(s.passes - 1) & 1];
     e.bytes = at > 256 ? at : 256;
     return e;
+}
+
+// One launch over as many tensors from `k` on as the table takes; moves k behind them.
+template <int MAXT>
+int adamw_launch(const pb_adamw_tensor* tensors, const void* const* grads, int n_tensors, int& k, const AdamScalars& q,
+                 const pb_adamw_args& args, cudaStream_t stream) {
+    static_assert(sizeof(AdamTable<MAXT>) <= 32764, "kernel parameters");
+    AdamTable<MAXT> a;
+    a.s = q;
+    a.s.n = 0;
+    const size_t gb = dtype_bytes(args.grad_dtype), fb = dtype_bytes(args.forward_dtype), sb = args.state_bits == 8 ? 1 : 4;
+    int64_t rounds = 0;
+    for (; k < n_tensors && a.s.n < MAXT; ++k) {
+        const pb_adamw_tensor& t = tensors[k];
+        if (t.n == 0) continue;
+        const int64_t c = (t.n + kAdamRound - 1) / kAdamRound;
+        if (rounds + c > kMaxCount) break;
+        AdamTensor& d = a.t[a.s.n++];
+        d.w = t.w; d.g = grads[k]; d.m = t.m; d.v = t.v; d.m_scale = t.m_scale; d.v_scale = t.v_scale; d.fwd = t.w_forward;
+        d.n = t.n; d.decay = t.weight_decay; d.horizon = t.horizon;
+        d.rnd = (unsigned long long)k * 0xA0761D6478BD642Full;
+        d.first_round = (unsigned)rounds;
+        d.vec = aligned(t.w, 32) && aligned(grads[k], 8 * gb) && aligned(t.m, 8 * sb) && aligned(t.v, 8 * sb) && aligned(t.w_forward, 8 * fb);
+        rounds += c;
+    }
+    if (a.s.n == 0) return PB_OK;
+    while (((rounds - 1) >> a.s.near_shift) >= kAdamNear) ++a.s.near_shift;
+    for (int64_t j = 0, at = 0; j <= (rounds - 1) >> a.s.near_shift; ++j) {
+        while (at + 1 < a.s.n && (int64_t)a.t[at + 1].first_round <= j << a.s.near_shift) ++at;
+        a.s.near[j] = (unsigned short)at;
+    }
+    auto go = [&](auto bits, auto g) { adamw_kernel<decltype(bits)::value, decltype(g), MAXT><<<(unsigned)rounds, kAdamThreads, 0, stream>>>(a); };
+    auto by_bits = [&](auto g) {
+        if (args.state_bits == 8) go(std::integral_constant<int, 8>(), g); else go(std::integral_constant<int, 32>(), g);
+    };
+    if (args.grad_dtype == PB_F32) by_bits(float()); else if (args.grad_dtype == PB_BF16) by_bits(__nv_bfloat16()); else by_bits(__half());
+    return launched("pb_adamw_step");
 }
 
 }  // namespace
@@ -304,7 +342,7 @@ int pb_adamw_step(const pb_adamw_tensor* tensors, const void* const* dev_grads, 
     for (int k = 0; k < n_tensors; ++k) {
         const pb_adamw_tensor& t = tensors[k];
         PB_REFUSE(t.n < 0, "pb_adamw_step: negative tensor size");
-        PB_REFUSE(t.n > (int64_t)kMaxCount * kAdamChunk / 2, "pb_adamw_step: a tensor is too large");
+        PB_REFUSE(t.n > (int64_t)kMaxCount * kAdamRound / 2, "pb_adamw_step: a tensor is too large");
         PB_REFUSE(!(t.weight_decay >= 0.f) || !std::isfinite(t.weight_decay) || !std::isfinite(t.horizon), "pb_adamw_step: weight_decay must not be negative, horizon must be finite");
         if (t.n == 0) continue;
         PB_REFUSE(!t.w || !t.m || !t.v || !dev_grads[k], "pb_adamw_step: NULL pointer");
@@ -312,34 +350,24 @@ int pb_adamw_step(const pb_adamw_tensor* tensors, const void* const* dev_grads, 
         PB_REFUSE(!aligned(t.w, 4) || !aligned(dev_grads[k], gb) || !aligned(t.m, sb) || !aligned(t.v, sb) || !aligned(t.m_scale, 4) ||
                   !aligned(t.v_scale, 4) || !aligned(t.w_forward, fb), "pb_adamw_step: a pointer is not aligned to its element");
     }
-    static_assert(sizeof(AdamTable) <= 32764, "kernel parameters");
-    AdamTable a;
-    a.lr = args->lr; a.beta1 = args->beta1; a.beta2 = args->beta2; a.eps = args->eps;
-    a.step = args->step; a.seed = args->seed;
-    a.grad_scale = args->dev_grad_scale; a.dev_lr = args->dev_lr; a.dev_step = (const long long*)args->dev_step;
-    a.grad_dtype = args->grad_dtype; a.fwd_dtype = args->forward_dtype; a.bits = args->state_bits;
-    int k = 0;
-    while (k < n_tensors) {
-        a.n = 0;
-        int64_t chunks = 0;
-        for (; k < n_tensors && a.n < kAdamMaxTensors; ++k) {
-            const pb_adamw_tensor& t = tensors[k];
-            if (t.n == 0) continue;
-            const int64_t c = (t.n + kAdamChunk - 1) / kAdamChunk;
-            if (chunks + c > kMaxCount) break;
-            AdamTensor& d = a.t[a.n++];
-            d.w = t.w; d.g = dev_grads[k]; d.m = t.m; d.v = t.v; d.m_scale = t.m_scale; d.v_scale = t.v_scale; d.fwd = t.w_forward;
-            d.n = t.n; d.decay = t.weight_decay; d.horizon = t.horizon;
-            d.rnd = (unsigned long long)k * 0xA0761D6478BD642Full;
-            d.first_chunk = (unsigned)chunks;
-            chunks += c;
+    AdamScalars q{};
+    q.lr = args->lr; q.beta1 = args->beta1; q.beta2 = args->beta2;
+    q.b1 = (float)args->beta1; q.o1 = (float)(1.0 - args->beta1); q.b2 = (float)args->beta2; q.o2 = (float)(1.0 - args->beta2);
+    q.eps = (float)args->eps;
+    q.minus_zero = -0.f;
+    q.c1 = (float)(1.0 / (1.0 - std::pow(args->beta1, (double)args->step)));
+    q.c2 = (float)(1.0 / std::sqrt(1.0 - std::pow(args->beta2, (double)args->step)));
+    q.step = args->step; q.seed = args->seed;
+    q.grad_scale = args->dev_grad_scale; q.dev_lr = args->dev_lr; q.dev_step = (const long long*)args->dev_step;
+    q.fwd_dtype = args->forward_dtype;
+    auto by_size = [&](auto few) {
+        for (int k = 0; k < n_tensors;) {
+            const int rc = adamw_launch<decltype(few)::value>(tensors, dev_grads, n_tensors, k, q, *args, (cudaStream_t)stream);
+            if (rc != PB_OK) return rc;
         }
-        if (a.n == 0) break;
-        adamw_kernel<<<(unsigned)chunks, 256, 0, (cudaStream_t)stream>>>(a);
-        const int rc = launched("pb_adamw_step");
-        if (rc != PB_OK) return rc;
-    }
-    return PB_OK;
+        return (int)PB_OK;
+    };
+    return n_tensors <= kAdamFewTensors ? by_size(std::integral_constant<int, kAdamFewTensors>()) : by_size(std::integral_constant<int, kAdamManyTensors>());
 }
 
 int pb_adamw_moments(const void* dev_m, const float* dev_m_scale, const void* dev_v, const float* dev_v_scale, int64_t n,
@@ -350,8 +378,9 @@ int pb_adamw_moments(const void* dev_m, const float* dev_m_scale, const void* de
     PB_REFUSE((dev_m_out && (!dev_m || !dev_m_scale)) || (dev_v_out && (!dev_v || !dev_v_scale)), "pb_adamw_moments: NULL pointer");
     PB_REFUSE(!aligned(dev_m_scale, 4) || !aligned(dev_v_scale, 4) || !aligned(dev_m_out, 4) || !aligned(dev_v_out, 4),
               "pb_adamw_moments: a pointer is not aligned to its element");
-    adamw_moments_kernel<<<(unsigned)((n + 255) / 256), 256, 0, (cudaStream_t)stream>>>(
-        (const unsigned char*)dev_m, dev_m_scale, (const unsigned char*)dev_v, dev_v_scale, n, dev_m_out, dev_v_out);
+    const bool vec = aligned(dev_m, 8) && aligned(dev_v, 8) && aligned(dev_m_out, 32) && aligned(dev_v_out, 32);
+    adamw_moments_kernel<<<(unsigned)((n + kAdamRound - 1) / kAdamRound), kAdamThreads, 0, (cudaStream_t)stream>>>(
+        (const unsigned char*)dev_m, dev_m_scale, (const unsigned char*)dev_v, dev_v_scale, n, dev_m_out, dev_v_out, vec);
     return launched("pb_adamw_moments");
 }
 

@@ -17,7 +17,7 @@ template <> __device__ __forceinline__ float from_f32<float>(float x) { return x
 template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
 template <> __device__ __forceinline__ __half from_f32<__half>(float x) { return __float2half_rn(x); }
 
-// Eight consecutive elements, 16-byte aligned (float: 32-byte aligned rows move as two such loads).
+// Eight consecutive elements, 16-byte aligned.
 __device__ __forceinline__ void unpack8(float (&x)[8], const uint4& q, __nv_bfloat16) {
     const unsigned w[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
@@ -56,6 +56,16 @@ __device__ __forceinline__ void store8(float* p, const float (&x)[8]) {
 }
 template <typename T> __device__ __forceinline__ void store8(T* p, const float (&x)[8]) {
     *reinterpret_cast<uint4*>(p) = make_uint4(pack2(x[0], x[1], T()), pack2(x[2], x[3], T()), pack2(x[4], x[5], T()), pack2(x[6], x[7], T()));
+}
+
+// The same from 32-byte aligned memory in one access.
+__device__ __forceinline__ void load8_wide(float (&x)[8], const float* p) {
+    asm volatile("ld.global.v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=f"(x[0]), "=f"(x[1]), "=f"(x[2]), "=f"(x[3]), "=f"(x[4]), "=f"(x[5]), "=f"(x[6]), "=f"(x[7]) : "l"(p));
+}
+__device__ __forceinline__ void store8_wide(float* p, const float (&x)[8]) {
+    asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                 ::"l"(p), "f"(x[0]), "f"(x[1]), "f"(x[2]), "f"(x[3]), "f"(x[4]), "f"(x[5]), "f"(x[6]), "f"(x[7]) : "memory");
 }
 
 // Index of a token, or -1 where there is none.  A value outside [0, n) other than -1 is

@@ -173,11 +173,24 @@ int pb_embed_forward(const void* dev_table, int dtype, int64_t vocab, int64_t di
     PB_REFUSE(overlap(dev_out, extent(n_tokens, dim, ld_out, es), dev_table, extent(vocab, dim, ld_table, es)),
               "pb_embed_forward: the output overlaps the table");
     const cudaStream_t s = (cudaStream_t)stream;
+    const int64_t piece = 16 / (int64_t)es;
+    const bool vec = dim % piece == 0 && ld_table % piece == 0 && ld_out % piece == 0 && aligned(dev_table, 16) && aligned(dev_out, 16);
+    const int64_t pieces = vec ? dim / piece : dim;
+    int lanes = 1;
+    while (lanes < 256 && lanes < pieces) lanes *= 2;
+    // Four tokens per group once that still gives every SM eight blocks; a few long rows are spread over blocks.
+    const int64_t groups = 256 / lanes;
+    const bool many = n_tokens >= (int64_t)148 * 8 * 4 * groups;
+    const int64_t blocks = (n_tokens + (many ? 4 : 1) * groups - 1) / ((many ? 4 : 1) * groups);
+    const int64_t walks = (pieces + lanes - 1) / lanes;
+    const int64_t spread = many ? 1 : walks < 16 ? walks : 16;
     auto go = [&](auto t, auto i) {
         using T = decltype(t);
         using I = decltype(i);
-        embed_fwd_kernel<T, I><<<(unsigned)n_tokens, 256, 0, s>>>((const T*)dev_table, vocab, dim, ld_table, (const I*)dev_ids, scale,
-                                                                  (T*)dev_out, ld_out, dev_status);
+        auto kernel = vec ? (many ? embed_fwd_kernel<T, I, true, 4> : embed_fwd_kernel<T, I, true, 1>)
+                          : (many ? embed_fwd_kernel<T, I, false, 4> : embed_fwd_kernel<T, I, false, 1>);
+        kernel<<<dim3((unsigned)blocks, (unsigned)spread), 256, 0, s>>>((const T*)dev_table, vocab, dim, ld_table, (const I*)dev_ids, n_tokens, scale,
+                                                                        (T*)dev_out, ld_out, lanes, dev_status);
     };
     auto by_id = [&](auto t) { if (id_bytes == 4) go(t, int32_t()); else go(t, int64_t()); };
     if (dtype == PB_F32) by_id(float()); else if (dtype == PB_BF16) by_id(__nv_bfloat16()); else by_id(__half());
@@ -314,10 +327,10 @@ int pb_logprob_backward(const void* dev_logits, int dtype, int64_t rows, int64_t
             using T = decltype(t);
             using I = decltype(i);
             auto at = [&](const float* p) { return p ? p + r0 : nullptr; };
-            const unsigned gx = (unsigned)((vocab + 8191) / 8192);
-            logprob_bwd_kernel<T, I><<<dim3(gx, nr), 256, 0, s>>>((const T*)dev_logits + r0 * ld, vocab, ld, dev_tokens ? (const I*)dev_tokens + r0 : nullptr,
-                                                                  inv_temperature, at(dev_lse), at(dev_entropy), at(dev_g_logp), at(dev_g_entropy), at(dev_g_lse),
-                                                                  (T*)dev_dlogits + r0 * ld_d, ld_d, dev_status);
+            const unsigned gx = (unsigned)((vocab + kBwdTile - 1) / kBwdTile);
+            logprob_bwd_kernel<T, I><<<dim3(gx, nr), kBwdThreads, 0, s>>>((const T*)dev_logits + r0 * ld, vocab, ld, dev_tokens ? (const I*)dev_tokens + r0 : nullptr,
+                                                                          inv_temperature, at(dev_lse), at(dev_entropy), at(dev_g_logp), at(dev_g_entropy),
+                                                                          at(dev_g_lse), (T*)dev_dlogits + r0 * ld_d, ld_d, dev_status);
         };
         auto by_id = [&](auto t) { if (token_bytes == 8) go(t, int64_t()); else go(t, int32_t()); };
         if (dtype == PB_F32) by_id(float()); else if (dtype == PB_BF16) by_id(__nv_bfloat16()); else by_id(__half());

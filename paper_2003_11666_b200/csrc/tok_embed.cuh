@@ -18,14 +18,50 @@
 
 namespace pb {
 
-template <typename T, typename I>
+// `lanes` threads walk a row in pieces (16 bytes where rows are aligned to them, else one element);
+// a group of them takes `ROWS` tokens, whose pieces are all on their way before the first is scaled.
+template <typename T, typename I, bool VEC, int ROWS>
 __global__ void __launch_bounds__(256)
 embed_fwd_kernel(const T* __restrict__ table, long long vocab, long long dim, long long ld_table,
-                 const I* __restrict__ ids, float scale, T* __restrict__ out, long long ld_out, int* status) {
-    const long long t = blockIdx.x;
-    const long long id = token_id(ids, t, vocab, status);
-    for (long long c = threadIdx.x; c < dim; c += blockDim.x)
-        out[t * ld_out + c] = from_f32<T>(id >= 0 ? scale * to_f32(table[id * ld_table + c]) : 0.f);
+                 const I* __restrict__ ids, long long n, float scale, T* __restrict__ out, long long ld_out, int lanes, int* status) {
+    constexpr int PIECE = VEC ? 16 / (int)sizeof(T) : 1;
+    const int group = threadIdx.x / lanes, lane = threadIdx.x % lanes;
+    const long long t0 = ((long long)blockIdx.x * (256 / lanes) + group) * ROWS;
+    if (t0 >= n) return;
+    long long id[ROWS];
+#pragma unroll
+    for (int k = 0; k < ROWS; ++k) id[k] = t0 + k < n ? token_id(ids, t0 + k, vocab, lane == 0 && blockIdx.y == 0 ? status : nullptr) : -2;
+    for (long long c = ((long long)blockIdx.y * lanes + lane) * PIECE; c < dim; c += (long long)gridDim.y * lanes * PIECE) {
+        if constexpr (VEC) {
+            uint4 x[ROWS];
+#pragma unroll
+            for (int k = 0; k < ROWS; ++k)
+                x[k] = id[k] >= 0 ? *reinterpret_cast<const uint4*>(table + id[k] * ld_table + c) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+            for (int k = 0; k < ROWS; ++k) {
+                if (id[k] == -2) continue;
+                uint4 y;
+                if constexpr (sizeof(T) == 4) {
+                    y = make_uint4(__float_as_uint(scale * __uint_as_float(x[k].x)), __float_as_uint(scale * __uint_as_float(x[k].y)),
+                                   __float_as_uint(scale * __uint_as_float(x[k].z)), __float_as_uint(scale * __uint_as_float(x[k].w)));
+                } else {
+                    float f[8];
+                    unpack8(f, x[k], T());
+                    y = make_uint4(pack2(scale * f[0], scale * f[1], T()), pack2(scale * f[2], scale * f[3], T()),
+                                   pack2(scale * f[4], scale * f[5], T()), pack2(scale * f[6], scale * f[7], T()));
+                }
+                if (id[k] < 0) y = make_uint4(0, 0, 0, 0);          // even if the scale is not finite
+                *reinterpret_cast<uint4*>(out + (t0 + k) * ld_out + c) = y;
+            }
+        } else {
+            float x[ROWS];
+#pragma unroll
+            for (int k = 0; k < ROWS; ++k) x[k] = id[k] >= 0 ? to_f32(table[id[k] * ld_table + c]) : 0.f;
+#pragma unroll
+            for (int k = 0; k < ROWS; ++k)
+                if (id[k] != -2) out[(t0 + k) * ld_out + c] = from_f32<T>(id[k] < 0 ? 0.f : scale * x[k]);
+        }
+    }
 }
 
 // ---------------------------------------------------------------- sort

@@ -105,31 +105,102 @@ logprob_fwd_kernel(const T* __restrict__ logits, long long vocab, long long ld, 
 
 // d x_i = it * ( g_logp (1[i = token] - p_i) - g_entropy p_i (log p_i + H) + g_lse p_i )
 // with log p_i = it * x_i - lse.  At the token 1 - p is -expm1(log p).  A row without any
-// finite logit has no gradient.
+// finite logit has no gradient.  One read and one write per logit: bound by memory traffic.
+constexpr int kBwdThreads = 256, kBwdVecs = 4, kBwdTile = kBwdThreads * kBwdVecs * 8;
+
+struct BwdRow {
+    float it, z, h, all, gh;        // all: gradient factor common to the row, g_lse - g_logp
+    // NaN stays NaN; a logit of -inf has p = 0 and a finite factor
+    __device__ __forceinline__ float gradient(float x) const {
+        float lp = fmaf(x, it, -z);
+        asm("max.NaN.f32 %0, %0, %1;" : "+f"(lp) : "f"(-1e30f));
+        return it * (__expf(lp) * fmaf(-gh, lp + h, all));
+    }
+};
+
 template <typename T, typename I>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(kBwdThreads)
 logprob_bwd_kernel(const T* logits, long long vocab, long long ld, const I* __restrict__ tokens, double inv_temp,
                    const float* __restrict__ lse, const float* __restrict__ entropy, const float* __restrict__ g_logp,
                    const float* __restrict__ g_entropy, const float* __restrict__ g_lse, T* dlogits, long long ld_d,
                    int* status) {
     const long long r = blockIdx.y;
-    const float z = lse[r], it = (float)inv_temp;
+    const T* x = logits + r * ld;
+    T* d = dlogits + r * ld_d;
+    const int tid = threadIdx.x;
+    // Pieces of eight start where the logits' row reaches their alignment, if the gradient's row does there too.
+    constexpr int ALIGN = 8 * (int)sizeof(T);
+    const long long head = min(vocab, (long long)((-(long long)reinterpret_cast<uintptr_t>(x)) & (ALIGN - 1)) / (int)sizeof(T));
+    const bool vec = ((reinterpret_cast<uintptr_t>(d + head)) & (ALIGN - 1)) == 0;
+    const long long pieces = vec ? (vocab - head) / 8 : 0;
+    const long long first = (long long)blockIdx.x * kBwdThreads * kBwdVecs + tid;
+    uint4 raw[kBwdVecs][sizeof(T) / 2];
+#pragma unroll
+    for (int k = 0; k < kBwdVecs; ++k)
+        if (first + k * kBwdThreads < pieces)
+#pragma unroll
+            for (int j = 0; j < (int)sizeof(T) / 2; ++j)
+                raw[k][j] = *reinterpret_cast<const uint4*>(x + head + (first + k * kBwdThreads) * 8 + j * 4);
+    BwdRow q;
+    q.z = lse[r];
+    q.it = (float)inv_temp;
     long long id = -1;
-    float gl = 0.f, gh = 0.f, gz = 0.f, h = 0.f;
-    if (g_logp) { id = token_id(tokens, r, vocab, status); gl = id >= 0 ? g_logp[r] : 0.f; }
-    if (g_entropy) { gh = g_entropy[r]; h = entropy[r]; }
+    float gl = 0.f, gz = 0.f;
+    q.gh = q.h = 0.f;
+    if (g_logp) { id = token_id(tokens, r, vocab, tid == 0 && blockIdx.x == 0 ? status : nullptr); gl = id >= 0 ? g_logp[r] : 0.f; }
+    if (g_entropy) { q.gh = g_entropy[r]; q.h = entropy[r]; }
     if (g_lse) gz = g_lse[r];
-    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < vocab; i += (long long)gridDim.x * 256) {
-        const float x = to_f32(logits[r * ld + i]);
-        float g = 0.f;
-        if (z != -INFINITY) {
-            const float lp = i == id ? (float)((double)x * inv_temp - z) : fmaf(x, it, -z);
-            const float p = expf(lp);
-            g = (gz - gl) * p;
-            if (i == id) g = gz * p - gl * expm1f(lp);
-            if (p > 0.f) g -= gh * p * (lp + h);
+    q.all = gz - gl;
+    const bool empty = q.z == -INFINITY;
+    // the token's own gradient replaces what the row's formula gives there
+    auto at_token = [&](float xv) {
+        const float lp = (float)((double)xv * inv_temp - q.z);
+        const float p = expf(lp);
+        const float g = gz * p - gl * expm1f(lp) - (p > 0.f ? q.gh * p * (lp + q.h) : 0.f);
+        return empty ? 0.f : q.it * g;
+    };
+#pragma unroll
+    for (int k = 0; k < kBwdVecs; ++k) {
+        const long long piece = first + k * kBwdThreads;
+        if (piece >= pieces) continue;
+        float f[8];
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                f[4 * j] = __uint_as_float(raw[k][j].x); f[4 * j + 1] = __uint_as_float(raw[k][j].y);
+                f[4 * j + 2] = __uint_as_float(raw[k][j].z); f[4 * j + 3] = __uint_as_float(raw[k][j].w);
+            }
+        } else {
+            unpack8(f, raw[k][0], T());
         }
-        dlogits[r * ld_d + i] = from_f32<T>(it * g);
+        const long long i = head + piece * 8;
+        const bool mine = id >= i && id < i + 8;
+        float xt = 0.f;
+        if (mine)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) xt = id == i + j ? f[j] : xt;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f[j] = empty ? 0.f : q.gradient(f[j]);
+        if (mine) {
+            const float g = at_token(xt);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) f[j] = id == i + j ? g : f[j];
+        }
+        if constexpr (sizeof(T) == 4) store8_wide(d + i, f);
+        else store8(d + i, f);
+    }
+    // what the pieces leave: the row's ends, or the whole tile
+    auto one = [&](long long i) {
+        const float xv = to_f32(x[i]);
+        d[i] = from_f32<T>(i == id ? at_token(xv) : empty ? 0.f : q.gradient(xv));
+    };
+    if (vec) {
+        const long long tail = head + pieces * 8;
+        if (blockIdx.x == 0 && tid < head) one(tid);
+        if (blockIdx.x == 0 && tid >= 32 && tail + tid - 32 < vocab) one(tail + tid - 32);
+    } else {
+        const long long i0 = (long long)blockIdx.x * kBwdTile, i1 = min(vocab, i0 + kBwdTile);
+        for (long long i = i0 + tid; i < i1; i += kBwdThreads) one(i);
     }
 }
 

@@ -155,19 +155,7 @@ struct AdamLane {
     }
 };
 
-// Pairs of float32 in one instruction, each rounded like the single operation: the 8-bit step is bound
-// by the instructions it issues.  The assembler contracts a product and a sum of pairs; a product that
-// must be rounded before it is added is therefore a fused multiply-add of a -0 that it cannot see.
-struct Pair {
-    unsigned long long x;
-    __device__ __forceinline__ Pair() {}
-    __device__ __forceinline__ Pair(float a, float b) { asm("mov.b64 %0, {%1, %2};" : "=l"(x) : "f"(a), "f"(b)); }
-    __device__ __forceinline__ explicit Pair(float a) : Pair(a, a) {}
-    __device__ __forceinline__ void split(float& a, float& b) const { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(x)); }
-};
-__device__ __forceinline__ Pair operator*(Pair a, Pair b) { Pair r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.x) : "l"(a.x), "l"(b.x)); return r; }
-__device__ __forceinline__ Pair operator+(Pair a, Pair b) { Pair r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.x) : "l"(a.x), "l"(b.x)); return r; }
-__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) { Pair r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.x) : "l"(a.x), "l"(b.x), "l"(c.x)); return r; }
+// The step uses pairs (tok_common.cuh) because with 8-bit states it is bound by the instructions it issues.
 // x[k] <- s x[k] for eight elements
 __device__ __forceinline__ void scale8(float (&x)[8], float s) {
 #pragma unroll
@@ -185,12 +173,6 @@ __device__ __forceinline__ float rcp_near(float x) {
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
 }
-__device__ __forceinline__ float max_nan(float a, float b) {
-    float r;
-    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
-    return r;
-}
-
 // Codes of eight second moments from their roots r (scaled by `ri`) and the random bits z of each four:
 // the root's bits plus a random number below one step of the code, cut off.  The low byte of what
 // is left is the code, since the exponent's bias there is a multiple of 256; the largest root, whose

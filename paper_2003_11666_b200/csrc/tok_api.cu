@@ -327,7 +327,7 @@ int pb_logprob_backward(const void* dev_logits, int dtype, int64_t rows, int64_t
             using T = decltype(t);
             using I = decltype(i);
             auto at = [&](const float* p) { return p ? p + r0 : nullptr; };
-            const unsigned gx = (unsigned)((vocab + kBwdTile - 1) / kBwdTile);
+            const unsigned gx = (unsigned)((vocab + kBwdTile<T> - 1) / kBwdTile<T>);
             logprob_bwd_kernel<T, I><<<dim3(gx, nr), kBwdThreads, 0, s>>>((const T*)dev_logits + r0 * ld, vocab, ld, dev_tokens ? (const I*)dev_tokens + r0 : nullptr,
                                                                           inv_temperature, at(dev_lse), at(dev_entropy), at(dev_g_logp), at(dev_g_entropy),
                                                                           at(dev_g_lse), (T*)dev_dlogits + r0 * ld_d, ld_d, dev_status);

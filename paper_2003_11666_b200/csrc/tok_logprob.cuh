@@ -106,15 +106,34 @@ logprob_fwd_kernel(const T* __restrict__ logits, long long vocab, long long ld, 
 // d x_i = it * ( g_logp (1[i = token] - p_i) - g_entropy p_i (log p_i + H) + g_lse p_i )
 // with log p_i = it * x_i - lse.  At the token 1 - p is -expm1(log p).  A row without any
 // finite logit has no gradient.  One read and one write per logit: bound by memory traffic.
-constexpr int kBwdThreads = 256, kBwdVecs = 4, kBwdTile = kBwdThreads * kBwdVecs * 8;
+constexpr int kBwdThreads = 128;
+template <typename T> constexpr int kBwdVecs = 16 / (int)sizeof(T);          // pieces of eight per thread
+template <typename T> constexpr int kBwdTile = kBwdThreads * kBwdVecs<T> * 8;
+
+constexpr float kLog2e = 1.4426950408889634f;
 
 struct BwdRow {
-    float it, z, h, all, gh;        // all: gradient factor common to the row, g_lse - g_logp
-    // NaN stays NaN; a logit of -inf has p = 0 and a finite factor
+    float it, z, h, all, gh;        // with the factor it: all = g_lse - g_logp, gh = g_entropy
+    bool entropy;
+    __device__ __forceinline__ void gradient(float (&x)[8]) const {
+        const Pair t(it), mz(-z), log2e(kLog2e), f(all), mh(-gh), hh(h);
+#pragma unroll
+        for (int k = 0; k < 8; k += 2) {
+            float a, b;
+            Pair lp = fma2(Pair(x[k], x[k + 1]), t, mz), factor = f;
+            if (entropy) {
+                lp.split(a, b);     // NaN stays NaN; a logit of -inf has p = 0, and a finite factor through this
+                lp = Pair(max_nan(a, -1e30f), max_nan(b, -1e30f));
+                factor = fma2(mh, lp + hh, f);
+            }
+            (lp * log2e).split(a, b);
+            (Pair(exp2_near(a), exp2_near(b)) * factor).split(x[k], x[k + 1]);
+        }
+    }
     __device__ __forceinline__ float gradient(float x) const {
-        float lp = fmaf(x, it, -z);
-        asm("max.NaN.f32 %0, %0, %1;" : "+f"(lp) : "f"(-1e30f));
-        return it * (__expf(lp) * fmaf(-gh, lp + h, all));
+        float e[8] = {x, x, x, x, x, x, x, x};
+        gradient(e);
+        return e[0];
     }
 };
 
@@ -133,10 +152,10 @@ logprob_bwd_kernel(const T* logits, long long vocab, long long ld, const I* __re
     const long long head = min(vocab, (long long)((-(long long)reinterpret_cast<uintptr_t>(x)) & (ALIGN - 1)) / (int)sizeof(T));
     const bool vec = ((reinterpret_cast<uintptr_t>(d + head)) & (ALIGN - 1)) == 0;
     const long long pieces = vec ? (vocab - head) / 8 : 0;
-    const long long first = (long long)blockIdx.x * kBwdThreads * kBwdVecs + tid;
-    uint4 raw[kBwdVecs][sizeof(T) / 2];
+    const long long first = (long long)blockIdx.x * kBwdThreads * kBwdVecs<T> + tid;
+    uint4 raw[kBwdVecs<T>][sizeof(T) / 2];
 #pragma unroll
-    for (int k = 0; k < kBwdVecs; ++k)
+    for (int k = 0; k < kBwdVecs<T>; ++k)
         if (first + k * kBwdThreads < pieces)
 #pragma unroll
             for (int j = 0; j < (int)sizeof(T) / 2; ++j)
@@ -146,21 +165,24 @@ logprob_bwd_kernel(const T* logits, long long vocab, long long ld, const I* __re
     q.it = (float)inv_temp;
     long long id = -1;
     float gl = 0.f, gz = 0.f;
-    q.gh = q.h = 0.f;
+    q.h = 0.f;
     if (g_logp) { id = token_id(tokens, r, vocab, tid == 0 && blockIdx.x == 0 ? status : nullptr); gl = id >= 0 ? g_logp[r] : 0.f; }
-    if (g_entropy) { q.gh = g_entropy[r]; q.h = entropy[r]; }
+    float gh = 0.f;
+    if (g_entropy) { gh = g_entropy[r]; q.h = entropy[r]; }
     if (g_lse) gz = g_lse[r];
-    q.all = gz - gl;
+    q.all = q.it * (gz - gl);
+    q.gh = q.it * gh;
+    q.entropy = g_entropy != nullptr;
     const bool empty = q.z == -INFINITY;
     // the token's own gradient replaces what the row's formula gives there
     auto at_token = [&](float xv) {
         const float lp = (float)((double)xv * inv_temp - q.z);
         const float p = expf(lp);
-        const float g = gz * p - gl * expm1f(lp) - (p > 0.f ? q.gh * p * (lp + q.h) : 0.f);
+        const float g = gz * p - gl * expm1f(lp) - (p > 0.f ? gh * p * (lp + q.h) : 0.f);
         return empty ? 0.f : q.it * g;
     };
 #pragma unroll
-    for (int k = 0; k < kBwdVecs; ++k) {
+    for (int k = 0; k < kBwdVecs<T>; ++k) {
         const long long piece = first + k * kBwdThreads;
         if (piece >= pieces) continue;
         float f[8];
@@ -179,8 +201,10 @@ logprob_bwd_kernel(const T* logits, long long vocab, long long ld, const I* __re
         if (mine)
 #pragma unroll
             for (int j = 0; j < 8; ++j) xt = id == i + j ? f[j] : xt;
+        q.gradient(f);
+        if (empty)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) f[j] = empty ? 0.f : q.gradient(f[j]);
+            for (int j = 0; j < 8; ++j) f[j] = 0.f;
         if (mine) {
             const float g = at_token(xt);
 #pragma unroll
@@ -199,7 +223,7 @@ logprob_bwd_kernel(const T* logits, long long vocab, long long ld, const I* __re
         if (blockIdx.x == 0 && tid < head) one(tid);
         if (blockIdx.x == 0 && tid >= 32 && tail + tid - 32 < vocab) one(tail + tid - 32);
     } else {
-        const long long i0 = (long long)blockIdx.x * kBwdTile, i1 = min(vocab, i0 + kBwdTile);
+        const long long i0 = (long long)blockIdx.x * kBwdTile<T>, i1 = min(vocab, i0 + kBwdTile<T>);
         for (long long i = i0 + tid; i < i1; i += kBwdThreads) one(i);
     }
 }

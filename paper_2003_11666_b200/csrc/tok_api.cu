@@ -58,7 +58,7 @@ cudaError_t launch_after(void (*kernel)(P...), dim3 grid, int threads, cudaStrea
 }
 
 // Sizes and scratch layout of the embedding gradient.
-constexpr int64_t kMaxEmbedDim = 1 << 26;
+constexpr int64_t kMaxEmbedDim = 1 << 26, kMaxLogprobVocab = 1 << 30;
 // Blocks per SM that the reduction's stretches are cut for; four are resident.  More and shorter
 // stretches even out the tail: 65536 tokens of 2048 columns take 230 us at 4, 192 at 8, 189 at 16.
 constexpr int kRedWave = 16;
@@ -274,7 +274,7 @@ int pb_logprob_forward(const void* dev_logits, int dtype, int64_t rows, int64_t 
                        float* dev_top_logp, int32_t* dev_top_ids, int32_t* dev_status, void* stream) {
     PB_REFUSE(!dtype_ok(dtype), "pb_logprob_forward: unknown element type");
     PB_REFUSE(rows < 0 || rows > kMaxCount, "pb_logprob_forward: rows out of range");
-    PB_REFUSE(vocab < 1 || vocab > kMaxCount, "pb_logprob_forward: vocab must be between 1 and 2^31 - 1");
+    PB_REFUSE(vocab < 1 || vocab > kMaxLogprobVocab, "pb_logprob_forward: vocab must be between 1 and 2^30");
     PB_REFUSE(ld < vocab, "pb_logprob_forward: the row stride is smaller than vocab");
     PB_REFUSE(!(inv_temperature > 0.0) || !std::isfinite((float)inv_temperature) || (float)inv_temperature == 0.f, "pb_logprob_forward: inv_temperature must be positive and finite");
     PB_REFUSE(top_k < 0 || top_k > kMaxTop, "pb_logprob_forward: top_k must be between 0 and 32");
@@ -287,15 +287,43 @@ int pb_logprob_forward(const void* dev_logits, int dtype, int64_t rows, int64_t 
               !aligned(dev_entropy, 4) || !aligned(dev_lse, 4) || !aligned(dev_top_logp, 4) || !aligned(dev_top_ids, 4) ||
               !aligned(dev_status, 4), "pb_logprob_forward: a pointer is not aligned to its element");
     const cudaStream_t s = (cudaStream_t)stream;
+    // A few rows are split over clusters as long as all blocks are resident at once (four per SM) and every warp
+    // of a block still has a piece.
+    const int64_t pieces = (vocab + kPiece - 1) / kPiece;
+    int parts = 1;
+    while (parts < kMaxCluster && rows * parts * 2 <= 148 * 4 && pieces >= (int64_t)parts * 2 * kFwdWarps) parts *= 2;
+    int per_segment = 1;
+    while ((pieces + 1) / per_segment / parts + 2 > kMaxSegments) per_segment *= 2;
     auto go = [&](auto t, auto i) {
         using T = decltype(t);
         using I = decltype(i);
-        logprob_fwd_kernel<T, I><<<(unsigned)rows, 512, 0, s>>>((const T*)dev_logits, vocab, ld, (const I*)dev_tokens, inv_temperature, dev_logp,
-                                                                dev_entropy, dev_lse, top_k, dev_top_logp, dev_top_ids, dev_status);
+        const T* x = (const T*)dev_logits;
+        const I* tok = (const I*)dev_tokens;
+        if (parts == 1) {
+            logprob_fwd_kernel<T, I, false><<<(unsigned)rows, kFwdThreads, 0, s>>>(x, (int)vocab, ld, tok, inv_temperature, dev_logp, dev_entropy, dev_lse, top_k,
+                                                                                 dev_top_logp, dev_top_ids, per_segment, dev_status);
+            return launched("pb_logprob_forward");
+        }
+        auto kernel = logprob_fwd_kernel<T, I, true>;
+        cudaError_t e = parts > 8 ? cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) : cudaSuccess;
+        cudaLaunchConfig_t cfg{};
+        cfg.gridDim = dim3((unsigned)(rows * parts));
+        cfg.blockDim = dim3(kFwdThreads);
+        cfg.stream = s;
+        cudaLaunchAttribute attr{};
+        attr.id = cudaLaunchAttributeClusterDimension;
+        attr.val.clusterDim.x = (unsigned)parts;
+        attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+        cfg.attrs = &attr;
+        cfg.numAttrs = 1;
+        if (e == cudaSuccess)
+            e = cudaLaunchKernelEx(&cfg, kernel, x, (int)vocab, (long long)ld, tok, inv_temperature, dev_logp, dev_entropy, dev_lse, top_k, dev_top_logp,
+                                   (int*)dev_top_ids, per_segment, (int*)dev_status);
+        const int rc = launched("pb_logprob_forward");
+        return rc != PB_OK || e == cudaSuccess ? rc : fail_text(PB_E_CUDA, cudaGetErrorString(e));
     };
-    auto by_id = [&](auto t) { if (token_bytes == 8) go(t, int64_t()); else go(t, int32_t()); };
-    if (dtype == PB_F32) by_id(float()); else if (dtype == PB_BF16) by_id(__nv_bfloat16()); else by_id(__half());
-    return launched("pb_logprob_forward");
+    auto by_id = [&](auto t) { return token_bytes == 8 ? go(t, int64_t()) : go(t, int32_t()); };
+    return dtype == PB_F32 ? by_id(float()) : dtype == PB_BF16 ? by_id(__nv_bfloat16()) : by_id(__half());
 }
 
 int pb_logprob_backward(const void* dev_logits, int dtype, int64_t rows, int64_t vocab, int64_t ld, const void* dev_tokens,
@@ -304,7 +332,7 @@ int pb_logprob_backward(const void* dev_logits, int dtype, int64_t rows, int64_t
                         int64_t ld_d, int32_t* dev_status, void* stream) {
     PB_REFUSE(!dtype_ok(dtype), "pb_logprob_backward: unknown element type");
     PB_REFUSE(rows < 0 || rows > kMaxCount, "pb_logprob_backward: rows out of range");
-    PB_REFUSE(vocab < 1 || vocab > kMaxCount, "pb_logprob_backward: vocab must be between 1 and 2^31 - 1");
+    PB_REFUSE(vocab < 1 || vocab > kMaxLogprobVocab, "pb_logprob_backward: vocab must be between 1 and 2^30");
     PB_REFUSE(ld < vocab || ld_d < vocab, "pb_logprob_backward: a row stride is smaller than vocab");
     PB_REFUSE(!(inv_temperature > 0.0) || !std::isfinite((float)inv_temperature) || (float)inv_temperature == 0.f, "pb_logprob_backward: inv_temperature must be positive and finite");
     if (rows == 0) return PB_OK;

@@ -7,102 +7,362 @@
 // The elements equal to the maximum are counted apart from the rest of the sum,
 // Z = count + rest, so that a confident row's log Z = log1p(rest) keeps its digits.
 #pragma once
+#include <cooperative_groups.h>
+
 #include "tok_common.cuh"
 
 namespace pb {
 
+namespace cg = cooperative_groups;
+
 constexpr int kMaxTop = 32;
 
-// Order of the alternatives: larger logit first, lower index among equal ones.  NaN sorts above
-// everything (such a row's results are NaN anyway).
-__device__ __forceinline__ unsigned long long top_key(float x, long long i) {
-    unsigned b = __float_as_uint(x + 0.f);                    // -0 counts as 0
-    b = (b & 0x80000000u) ? ~b : (b | 0x80000000u);
-    return ((unsigned long long)b << 32) | (0xffffffffu - (unsigned)i);
+// ---------------------------------------------------------------- forward
+// One pass over the row.  A warp takes pieces of 256 consecutive logits, finds a piece's maximum with one
+// warp reduction, and moves its running maximum (the same for all lanes) only when a piece exceeds it; the
+// sums e and e d stay in registers.  The maxima of the pieces (of runs of them, for very long rows)
+// stay in shared memory, and give the alternatives without a second pass: the k best elements, by value and
+// then by index, lie in the k best segments by the same order, for each better segment holds a better
+// element.  So at most 32 segments are read again, from L2.
+// A few rows are split over a cluster of blocks, joined through distributed shared memory.
+constexpr int kFwdThreads = 256, kFwdWarps = kFwdThreads / 32;
+constexpr int kPiece = 256;                 // logits of a warp's step: eight per lane
+constexpr int kMaxSegments = 2048;          // segments of a block
+constexpr int kMaxCluster = 16;
+constexpr int kFwdUnroll = 4;               // pieces on their way
+
+struct FwdStats {                           // of a warp, a block or a row, relative to the maximum `mx`
+    double count, rest, moment;             // elements at the maximum; sum of the others' e; sum of e d
+    float mx;
+    int bad;
+};
+
+struct FwdShared {
+    float seg[kMaxSegments];
+    unsigned long long keys[kMaxCluster * kMaxTop > kFwdWarps * kMaxTop ? kMaxCluster * kMaxTop : kFwdWarps * kMaxTop];
+    unsigned long long best[kMaxTop];
+    FwdStats stats[kMaxCluster > kFwdWarps ? kMaxCluster : kFwdWarps];
+    int picked[kMaxTop];
+    float threshold;
+    int n_picked, n_keys;
+    double log_z;
+};
+
+template <typename T>
+struct FwdRow {
+    const T* x;
+    int vocab, head;                        // head: logits before the first aligned one, a segment of their own
+    __device__ __forceinline__ bool full(int piece) const { return head + (piece + 1) * kPiece <= vocab; }
+    // Lane's eight logits of a piece; -inf beyond the end.  Piece -1: the head.
+    __device__ __forceinline__ int first(int piece, int lane) const { return piece < 0 ? lane * 8 : head + piece * kPiece + lane * 8; }
+    __device__ __forceinline__ void load_any(float (&f)[8], int piece, int lane) const {
+        const int i = first(piece, lane), end = piece < 0 ? head : vocab;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) f[k] = i + k < end ? to_f32(x[i + k]) : -INFINITY;
+    }
+    __device__ __forceinline__ void load(float (&f)[8], int piece, int lane) const {
+        if (piece >= 0 && full(piece)) {
+            if constexpr (sizeof(T) == 4) load8_wide(f, x + first(piece, lane));
+            else load8(f, x + first(piece, lane));
+        } else {
+            load_any(f, piece, lane);
+        }
+    }
+};
+
+__device__ __forceinline__ float warp_max_nan(float x) {
+    float r;
+    asm("redux.sync.max.NaN.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(x));
+    return r;
 }
-__device__ __forceinline__ float top_value(unsigned long long key) {
-    unsigned b = (unsigned)(key >> 32);
-    b = (b & 0x80000000u) ? (b & 0x7fffffffu) : ~b;
-    return __uint_as_float(b);
+__device__ __forceinline__ float max8(const float (&f)[8]) {
+    return max_nan(max_nan(max_nan(f[0], f[1]), max_nan(f[2], f[3])), max_nan(max_nan(f[4], f[5]), max_nan(f[6], f[7])));
 }
 
-template <typename T, typename I>
-__global__ void __launch_bounds__(512)
-logprob_fwd_kernel(const T* __restrict__ logits, long long vocab, long long ld, const I* __restrict__ tokens,
-                   double inv_temp, float* __restrict__ logp, float* __restrict__ entropy, float* __restrict__ lse,
-                   int top, float* __restrict__ top_logp, int* __restrict__ top_ids, int* status) {
-    __shared__ float sh_f[16];
-    __shared__ double sh_d[3][16];
-    __shared__ unsigned long long sh_k[16];
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const long long r = blockIdx.x;
-    const T* x = logits + r * ld;
-    const float it = (float)inv_temp;
+// A warp's running sums.
+struct FwdAcc {
     float mx = -INFINITY;
-    bool bad = false;
-    for (long long i = tid; i < vocab; i += 512) {
-        const float v = to_f32(x[i]);
-        bad |= v != v;
-        mx = fmaxf(mx, v);
+    int count = 0;
+    Pair rest{0.f, 0.f}, moment{0.f, 0.f};
+    // c: log2(e) times the inverse temperature
+    __device__ __forceinline__ void add(const float (&f)[8], float top, float c) {
+        if (top > mx) {                      // the same for the whole warp
+            if (mx > -INFINITY) {
+                const float shift = mx - top, s = exp2_near(shift * c);
+                float r0, r1;
+                rest.split(r0, r1);
+                r0 += (float)count;
+                moment = (moment + Pair(r0, r1) * Pair(shift)) * Pair(s);
+                rest = Pair(r0, r1) * Pair(s);
+                count = 0;
+            }
+            mx = top;
+        }
+        if (mx == -INFINITY) return;         // nothing finite so far
+        const Pair m(-mx), cc(c);
+        const bool has_top = top == mx;
+#pragma unroll
+        for (int k = 0; k < 8; k += 2) {
+            float a, b;
+            (Pair(f[k], f[k + 1]) + m).split(a, b);
+            if (has_top) {                   // the maximum itself is counted, not added
+                const bool ta = a == 0.f, tb = b == 0.f;
+                count += (int)ta + (int)tb;
+                a = ta ? -INFINITY : a;
+                b = tb ? -INFINITY : b;
+            }
+            a = max_nan(a, -1e30f);          // e d is 0, not 0 times infinity, where e is 0
+            b = max_nan(b, -1e30f);
+            const Pair d(a, b);
+            (d * cc).split(a, b);
+            const Pair e(exp2_near(a), exp2_near(b));
+            rest = rest + e;
+            moment = fma2(e, d, moment);
+        }
     }
-    mx = warp_max_f(mx);
-    if (lane == 0) sh_f[warp] = mx;
-    bad = __syncthreads_or(bad);
-    for (int w = 0; w < 16; ++w) mx = fmaxf(mx, sh_f[w]);
-    bad |= mx == INFINITY;
-    const bool empty = mx == -INFINITY && !bad;
-    double count = 0, rest = 0, moment = 0;
-    for (long long i = tid; i < vocab; i += 512) {
-        const float d = it * (to_f32(x[i]) - mx);
-        if (d == 0.f) { count += 1; continue; }
-        const float e = expf(d);
-        if (e > 0.f) { rest += e; moment += (double)e * d; }
+};
+
+__device__ __forceinline__ FwdStats join(const FwdStats* p, int n, float c) {
+    FwdStats t{0, 0, 0, -INFINITY, 0};
+    for (int k = 0; k < n; ++k) { t.mx = fmaxf(t.mx, p[k].mx); t.bad |= p[k].bad; }
+    if (t.mx == -INFINITY) return t;
+    for (int k = 0; k < n; ++k) {
+        if (p[k].mx == -INFINITY) continue;
+        if (p[k].mx == t.mx) {
+            t.count += p[k].count;
+            t.rest += p[k].rest;
+            t.moment += p[k].moment;
+        } else {
+            const float shift = p[k].mx - t.mx;
+            const double s = exp2_near(shift * c), all = p[k].rest + p[k].count;
+            t.rest += s * all;
+            t.moment += s * (p[k].moment + all * shift);
+        }
     }
-    for (int o = 16; o > 0; o >>= 1) {
-        count += __shfl_xor_sync(0xffffffffu, count, o);
-        rest += __shfl_xor_sync(0xffffffffu, rest, o);
-        moment += __shfl_xor_sync(0xffffffffu, moment, o);
+    return t;
+}
+
+__device__ __forceinline__ int total_at_least(const float* v, int n, float t, int lane) {
+    int c = 0;
+    for (int j = lane; j < n; j += 32) c += v[j] >= t;
+    return __reduce_add_sync(0xffffffffu, c);
+}
+// Floats in the order of their values as unsigned numbers, and back.
+__device__ __forceinline__ unsigned ordered(float x) {
+    const unsigned b = __float_as_uint(x + 0.f);              // -0 counts as 0
+    return (b & 0x80000000u) ? ~b : (b | 0x80000000u);
+}
+__device__ __forceinline__ float from_ordered(unsigned b) {
+    return __uint_as_float((b & 0x80000000u) ? (b & 0x7fffffffu) : ~b);
+}
+
+// The k best of n segments (by maximum, then by index) into sh.picked; one warp.
+__device__ __forceinline__ void pick_segments(FwdShared& sh, int n, int k, int lane) {
+    float t = -INFINITY;
+    if (n > k) {
+        // largest t with at least k maxima of at least t, by bisection of its bits
+        unsigned lo = ordered(-INFINITY), hi = ordered(INFINITY);
+        while (lo < hi) {
+            const unsigned mid = lo + (hi - lo + 1) / 2;
+            const int c = total_at_least(sh.seg, n, from_ordered(mid), lane);
+            if (c >= k) lo = mid; else hi = mid - 1;
+            if (c == k) break;
+        }
+        t = from_ordered(lo);
     }
-    if (lane == 0) { sh_d[0][warp] = count; sh_d[1][warp] = rest; sh_d[2][warp] = moment; }
+    int above = 0;                           // segments above t; those equal to t fill up in order
+    for (int j = lane; j < n; j += 32) above += sh.seg[j] > t;
+    above = __reduce_add_sync(0xffffffffu, above);
+    const int equal = min(k, n) - above;
+    int at = 0, taken = 0;
+    for (int j0 = 0; j0 < n; j0 += 32) {
+        const float v = j0 + lane < n ? sh.seg[j0 + lane] : 0.f;
+        const bool more = j0 + lane < n && v > t, same = j0 + lane < n && v == t;
+        const unsigned below = (1u << lane) - 1, ms = __ballot_sync(0xffffffffu, same);
+        const bool take = more || (same && taken + __popc(ms & below) < equal);
+        const unsigned mt = __ballot_sync(0xffffffffu, take);
+        if (take) sh.picked[at + __popc(mt & below)] = j0 + lane;
+        at += __popc(mt);
+        taken += __popc(ms);
+    }
+    if (lane == 0) { sh.n_picked = at; sh.threshold = t; }
+}
+
+// A warp's best k keys, the j-th in lane j.
+struct BestList {
+    unsigned long long mine = 0, least = 0;
+    __device__ __forceinline__ void offer(unsigned long long key, int k, int lane) {
+        unsigned who = __ballot_sync(0xffffffffu, key > least);
+        while (who) {
+            const unsigned long long x = __shfl_sync(0xffffffffu, key, __ffs(who) - 1);
+            const int at = __popc(__ballot_sync(0xffffffffu, mine > x));
+            const unsigned long long up = __shfl_up_sync(0xffffffffu, mine, 1);
+            mine = lane < at ? mine : lane == at ? x : up;
+            least = __shfl_sync(0xffffffffu, mine, k - 1);
+            who &= who - 1;
+            who &= __ballot_sync(0xffffffffu, key > least);
+        }
+    }
+};
+
+// best[0..k) <- the k largest of n keys, in order; zero where there are fewer.  By all threads.
+__device__ __forceinline__ void rank_keys(unsigned long long* best, const unsigned long long* keys, int n, int k) {
+    if ((int)threadIdx.x < k) best[threadIdx.x] = 0;
     __syncthreads();
-    count = rest = moment = 0;
-    for (int w = 0; w < 16; ++w) { count += sh_d[0][w]; rest += sh_d[1][w]; moment += sh_d[2][w]; }
-    double log_z = count > 0 ? log(count) + log1p(rest / count) : 0.0;
-    const double nan = __longlong_as_double(0x7ff8000000000000ll);
-    if (bad) log_z = nan;
-    if (tid == 0) {
-        if (logp) {
-            const long long id = token_id(tokens, r, vocab, status);
-            logp[r] = id < 0 ? 0.f : empty ? -INFINITY : (float)(((double)to_f32(x[id]) - mx) * inv_temp - log_z);
-        }
-        if (entropy) entropy[r] = empty ? 0.f : (float)(log_z - moment / (count + rest));
-        if (lse) lse[r] = empty ? -INFINITY : (float)((double)mx * inv_temp + log_z);
+    for (int i = threadIdx.x; i < n; i += kFwdThreads) {
+        const unsigned long long x = keys[i];
+        int above = 0;
+        for (int j = 0; j < n; ++j) above += keys[j] > x;     // keys differ: each holds its index; zeros are none
+        if (x != 0 && above < k) best[above] = x;
     }
-    unsigned long long last = ~0ull;
-    for (int k = 0; k < top; ++k) {
-        unsigned long long best = 0;
-        for (long long i = tid; i < vocab; i += 512) {
-            const unsigned long long key = top_key(to_f32(x[i]), i);
-            if (key < last && key > best) best = key;
+    __syncthreads();
+}
+
+template <typename T, typename I, bool CLUSTER>
+__global__ void __launch_bounds__(kFwdThreads, 4)
+logprob_fwd_kernel(const T* __restrict__ logits, int vocab, long long ld, const I* __restrict__ tokens, double inv_temp,
+                   float* __restrict__ logp, float* __restrict__ entropy, float* __restrict__ lse, int top,
+                   float* __restrict__ top_logp, int* __restrict__ top_ids, int per_segment, int* status) {
+    __shared__ FwdShared sh;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int parts = CLUSTER ? (int)cg::this_cluster().num_blocks() : 1, part = CLUSTER ? (int)cg::this_cluster().block_rank() : 0;
+    const long long r = blockIdx.x / parts;
+    if constexpr (CLUSTER) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");     // this block runs
+    FwdRow<T> row;
+    row.x = logits + r * ld;
+    row.vocab = vocab;
+    constexpr int ALIGN = 8 * (int)sizeof(T);
+    row.head = min(vocab, (int)((-(long long)reinterpret_cast<uintptr_t>(row.x)) & (ALIGN - 1)) / (int)sizeof(T));
+    const int pieces = (vocab - row.head + kPiece - 1) / kPiece;
+    // segments: [the head if there is one,] then runs of `per_segment` pieces; blocks take equal stretches of them
+    const int heads = row.head > 0, segments = heads + (pieces + per_segment - 1) / per_segment;
+    const int each = (segments + parts - 1) / parts, s_lo = min(segments, part * each), s_hi = min(segments, s_lo + each), n = s_hi - s_lo;
+    const float c = (float)(1.4426950408889634 * inv_temp);
+    long long id = -1;
+    float x_token = 0.f;
+    if (part == 0 && tid == 0 && logp) {
+        id = token_id(tokens, r, vocab, status);
+        if (id >= 0) x_token = to_f32(row.x[id]);
+    }
+
+    FwdAcc acc;
+    bool bad = false;
+    if (per_segment == 1) {
+        // A warp's next pieces are on their way while it adds these.
+        for (int s0 = s_lo + warp; s0 < s_hi; s0 += kFwdWarps * kFwdUnroll) {
+            float f[kFwdUnroll][8];
+#pragma unroll
+            for (int u = 0; u < kFwdUnroll; ++u) {
+                const int s = s0 + u * kFwdWarps;
+                if (s < s_hi) row.load(f[u], s - heads, lane);
+            }
+#pragma unroll
+            for (int u = 0; u < kFwdUnroll; ++u) {
+                const int s = s0 + u * kFwdWarps;
+                if (s >= s_hi) break;
+                const float m = warp_max_nan(max8(f[u]));
+                bad |= m != m;
+                if (lane == 0) sh.seg[s - s_lo] = m;
+                acc.add(f[u], m, c);
+            }
         }
+    } else {
+        for (int s = s_lo + warp; s < s_hi; s += kFwdWarps) {
+            const int p0 = s < heads ? -1 : (s - heads) * per_segment, p1 = s < heads ? 0 : min(pieces, p0 + per_segment);
+            float best = -INFINITY;
+            for (int p = p0; p < p1; ++p) {
+                float f[8];
+                row.load(f, p, lane);
+                const float m = warp_max_nan(max8(f));
+                best = max_nan(best, m);
+                acc.add(f, m, c);
+            }
+            bad |= best != best;
+            if (lane == 0) sh.seg[s - s_lo] = best;
+        }
+    }
+    {
+        float a, b, p, q;
+        acc.rest.split(a, b);
+        acc.moment.split(p, q);
+        a += b;
+        p += q;
+#pragma unroll
         for (int o = 16; o > 0; o >>= 1) {
-            const unsigned long long other = __shfl_xor_sync(0xffffffffu, best, o);
-            best = other > best ? other : best;
+            a += __shfl_xor_sync(0xffffffffu, a, o);
+            p += __shfl_xor_sync(0xffffffffu, p, o);
         }
+        const int count = __reduce_add_sync(0xffffffffu, acc.count);
+        if (lane == 0) sh.stats[warp] = FwdStats{(double)count, (double)a, (double)p, acc.mx, bad || acc.mx == INFINITY};
+    }
+    __syncthreads();
+    if (top > 0) {
+        if (warp == 0) pick_segments(sh, n, top, lane);
+        if (tid == 32) sh.n_keys = 0;
         __syncthreads();
-        if (lane == 0) sh_k[warp] = best;
+        const float t = sh.threshold;
+        BestList list;
+        const int picked = sh.n_picked;
+        for (int j = warp; j < picked; j += kFwdWarps) {
+            const int s = s_lo + sh.picked[j];
+            const int p0 = s < heads ? -1 : (s - heads) * per_segment, p1 = s < heads ? 0 : min(pieces, p0 + per_segment);
+            for (int p = p0; p < p1; ++p) {
+                float f[8];
+                row.load(f, p, lane);
+                const int i = row.first(p, lane);
+                if (!__any_sync(0xffffffffu, max8(f) >= t)) continue;
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    list.offer(f[k] >= t && f[k] > -INFINITY ? (unsigned long long)ordered(f[k]) << 32 | (0xffffffffu - (unsigned)(i + k)) : 0ull, top, lane);
+            }
+        }
+        const unsigned have = __ballot_sync(0xffffffffu, lane < top && list.mine != 0);
+        int at = 0;
+        if (lane == 0 && have) at = atomicAdd(&sh.n_keys, __popc(have));
+        at = __shfl_sync(0xffffffffu, at, 0);
+        if ((have >> lane) & 1) sh.keys[at + lane] = list.mine;                // valid keys are the first lanes
         __syncthreads();
-        for (int w = 0; w < 16; ++w) best = sh_k[w] > best ? sh_k[w] : best;
-        last = best;
-        if (tid == 0) {
-            const float v = top_value(best);
-            const bool none = best == 0 || v == -INFINITY || bad;
-            top_ids[r * top + k] = none ? -1 : (int)(0xffffffffu - (unsigned)best);
-            top_logp[r * top + k] = bad ? __int_as_float(0x7fc00000) : none ? -INFINITY : (float)(((double)v - mx) * inv_temp - log_z);
+        rank_keys(sh.best, sh.keys, sh.n_keys, top);
+    }
+    FwdStats all{};
+    if constexpr (CLUSTER) {
+        cg::cluster_group cluster = cg::this_cluster();
+        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");                    // every block runs
+        if (tid == 0) all = join(sh.stats, kFwdWarps, c);
+        __syncthreads();
+        cluster.sync();                                       // the first block is done with its own use of what others write
+        FwdShared* first = cluster.map_shared_rank(&sh, 0);
+        if (tid == 0) first->stats[part] = all;
+        if (tid < top) first->keys[part * top + tid] = sh.best[tid];
+        cluster.sync();
+        if (part != 0) return;
+        if (top > 0) rank_keys(sh.best, sh.keys, parts * top, top);
+        if (tid == 0) all = join(sh.stats, parts, c);
+    } else {
+        if (tid == 0) all = join(sh.stats, kFwdWarps, c);
+    }
+    if (tid == 0) {
+        const bool empty = all.mx == -INFINITY && !all.bad;
+        double log_z = all.bad ? __longlong_as_double(0x7ff8000000000000ll) : empty ? 0.0 : log(all.count) + log1p(all.rest / all.count);
+        if (logp) logp[r] = id < 0 ? 0.f : empty ? -INFINITY : (float)(((double)x_token - all.mx) * inv_temp - log_z);
+        if (entropy) entropy[r] = empty ? 0.f : (float)(log_z - inv_temp * all.moment / (all.count + all.rest));
+        if (lse) lse[r] = empty ? -INFINITY : (float)((double)all.mx * inv_temp + log_z);
+        sh.log_z = log_z;
+        sh.stats[0] = all;
+    }
+    if (top > 0) {
+        __syncthreads();
+        if (tid < top) {
+            const unsigned long long key = sh.best[tid];
+            const bool broken = sh.stats[0].bad, none = key == 0 || broken;
+            top_ids[r * top + tid] = none ? -1 : (int)(0xffffffffu - (unsigned)key);
+            top_logp[r * top + tid] = broken ? __int_as_float(0x7fc00000) : none ? -INFINITY
+                : (float)(((double)from_ordered((unsigned)(key >> 32)) - sh.stats[0].mx) * inv_temp - sh.log_z);
         }
     }
 }
 
+// ---------------------------------------------------------------- gradient
 // d x_i = it * ( g_logp (1[i = token] - p_i) - g_entropy p_i (log p_i + H) + g_lse p_i )
 // with log p_i = it * x_i - lse.  At the token 1 - p is -expm1(log p).  A row without any
 // finite logit has no gradient.  One read and one write per logit: bound by memory traffic.

@@ -293,7 +293,7 @@ int pb_logprob_forward(const void* dev_logits, int dtype, int64_t rows, int64_t 
     int parts = 1;
     while (parts < kMaxCluster && rows * parts * 2 <= 148 * 4 && pieces >= (int64_t)parts * 2 * kFwdWarps) parts *= 2;
     int per_segment = 1;
-    while ((pieces + 1) / per_segment / parts + 2 > kMaxSegments) per_segment *= 2;
+    while ((pieces + 1) / per_segment + 2 > kMaxSegments) per_segment *= 2;
     auto go = [&](auto t, auto i) {
         using T = decltype(t);
         using I = decltype(i);

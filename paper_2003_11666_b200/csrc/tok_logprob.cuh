@@ -9,6 +9,8 @@
 #pragma once
 #include <cooperative_groups.h>
 
+#include <type_traits>
+
 #include "tok_common.cuh"
 
 namespace pb {
@@ -27,9 +29,10 @@ constexpr int kMaxTop = 32;
 // A few rows are split over a cluster of blocks, joined through distributed shared memory.
 constexpr int kFwdThreads = 256, kFwdWarps = kFwdThreads / 32;
 constexpr int kPiece = 256;                 // logits of a warp's step: eight per lane
-constexpr int kMaxSegments = 2048;          // segments of a block
+constexpr int kMaxSegments = 2048;          // segments of a row
+constexpr int kPickRegs = 16;               // maxima per lane that the pick keeps in registers
 constexpr int kMaxCluster = 16;
-constexpr int kFwdUnroll = 4;               // pieces on their way
+template <typename T> constexpr int kFwdUnroll = 8 / (int)sizeof(T);       // pieces on their way while as many are added
 
 struct FwdStats {                           // of a warp, a block or a row, relative to the maximum `mx`
     double count, rest, moment;             // elements at the maximum; sum of the others' e; sum of e d
@@ -38,13 +41,12 @@ struct FwdStats {                           // of a warp, a block or a row, rela
 };
 
 struct FwdShared {
-    float seg[kMaxSegments];
-    unsigned long long keys[kMaxCluster * kMaxTop > kFwdWarps * kMaxTop ? kMaxCluster * kMaxTop : kFwdWarps * kMaxTop];
-    unsigned long long best[kMaxTop];
-    FwdStats stats[kMaxCluster > kFwdWarps ? kMaxCluster : kFwdWarps];
+    float seg[kMaxSegments];                // of the whole row; a block of a cluster fills its stretch and copies the others'
+    unsigned long long keys[kFwdWarps * kMaxTop], gathered[kMaxCluster * kMaxTop], best[kMaxTop];
+    FwdStats warp_stats[kFwdWarps], block, row;
     int picked[kMaxTop];
     float threshold;
-    int n_picked, n_keys;
+    int n_picked, n_keys, n_gathered;
     double log_z;
 };
 
@@ -59,6 +61,22 @@ struct FwdRow {
         const int i = first(piece, lane), end = piece < 0 ? head : vocab;
 #pragma unroll
         for (int k = 0; k < 8; ++k) f[k] = i + k < end ? to_f32(x[i + k]) : -INFINITY;
+    }
+    // a full piece as it is in memory
+    __device__ __forceinline__ void load_raw(uint4 (&q)[sizeof(T) / 2], int piece, int lane) const {
+#pragma unroll
+        for (int k = 0; k < (int)sizeof(T) / 2; ++k) q[k] = *reinterpret_cast<const uint4*>(x + first(piece, lane) + 4 * k);
+    }
+    __device__ __forceinline__ void widen(float (&f)[8], const uint4 (&q)[sizeof(T) / 2]) const {
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                f[4 * k] = __uint_as_float(q[k].x); f[4 * k + 1] = __uint_as_float(q[k].y);
+                f[4 * k + 2] = __uint_as_float(q[k].z); f[4 * k + 3] = __uint_as_float(q[k].w);
+            }
+        } else {
+            unpack8(f, q[0], T());
+        }
     }
     __device__ __forceinline__ void load(float (&f)[8], int piece, int lane) const {
         if (piece >= 0 && full(piece)) {
@@ -75,8 +93,13 @@ __device__ __forceinline__ float warp_max_nan(float x) {
     asm("redux.sync.max.NaN.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(x));
     return r;
 }
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
 __device__ __forceinline__ float max8(const float (&f)[8]) {
-    return max_nan(max_nan(max_nan(f[0], f[1]), max_nan(f[2], f[3])), max_nan(max_nan(f[4], f[5]), max_nan(f[6], f[7])));
+    return max_nan(max3(max3(f[0], f[1], f[2]), f[3], f[4]), max3(f[5], f[6], f[7]));
 }
 
 // A warp's running sums.
@@ -98,27 +121,35 @@ struct FwdAcc {
             }
             mx = top;
         }
-        if (mx == -INFINITY) return;         // nothing finite so far
+        if (top == mx) {
+            if (mx > -INFINITY) add_at_top(f, c);
+        } else {
+            add_below(f, c);
+        }
+    }
+    // every logit is below the maximum (or NaN)
+    __device__ __forceinline__ void add_below(const float (&f)[8], float c) {
         const Pair m(-mx), cc(c);
-        const bool has_top = top == mx;
 #pragma unroll
         for (int k = 0; k < 8; k += 2) {
             float a, b;
             (Pair(f[k], f[k + 1]) + m).split(a, b);
-            if (has_top) {                   // the maximum itself is counted, not added
-                const bool ta = a == 0.f, tb = b == 0.f;
-                count += (int)ta + (int)tb;
-                a = ta ? -INFINITY : a;
-                b = tb ? -INFINITY : b;
-            }
-            a = max_nan(a, -1e30f);          // e d is 0, not 0 times infinity, where e is 0
-            b = max_nan(b, -1e30f);
-            const Pair d(a, b);
+            const Pair d(max_nan(a, -1e30f), max_nan(b, -1e30f));      // e d is 0, not 0 times infinity, where e is 0
             (d * cc).split(a, b);
             const Pair e(exp2_near(a), exp2_near(b));
             rest = rest + e;
             moment = fma2(e, d, moment);
         }
+    }
+    // the maximum itself is counted, not added
+    __device__ __forceinline__ void add_at_top(const float (&f)[8], float c) {
+        float g[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            count += f[k] == mx;
+            g[k] = f[k] == mx ? -INFINITY : f[k];
+        }
+        add_below(g, c);
     }
 };
 
@@ -142,11 +173,6 @@ __device__ __forceinline__ FwdStats join(const FwdStats* p, int n, float c) {
     return t;
 }
 
-__device__ __forceinline__ int total_at_least(const float* v, int n, float t, int lane) {
-    int c = 0;
-    for (int j = lane; j < n; j += 32) c += v[j] >= t;
-    return __reduce_add_sync(0xffffffffu, c);
-}
 // Floats in the order of their values as unsigned numbers, and back.
 __device__ __forceinline__ unsigned ordered(float x) {
     const unsigned b = __float_as_uint(x + 0.f);              // -0 counts as 0
@@ -156,19 +182,55 @@ __device__ __forceinline__ float from_ordered(unsigned b) {
     return __uint_as_float((b & 0x80000000u) ? (b & 0x7fffffffu) : ~b);
 }
 
-// The k best of n segments (by maximum, then by index) into sh.picked; one warp.
+// The value whose ordered bits, without GRAIN low bits that are zero in the value itself, are `k`.
+template <int GRAIN>
+__device__ __forceinline__ float from_grain(unsigned k) {
+    const unsigned b = k << GRAIN;
+    return from_ordered((b & 0x80000000u) ? b : b | ((1u << GRAIN) - 1));
+}
+
+// The k best of n segments (by maximum, then by index) into sh.picked, and a value that the k-th best
+// maximum reaches into sh.threshold; one warp.  Maxima are values of T: GRAIN low bits of them are zero.
+template <int GRAIN>
 __device__ __forceinline__ void pick_segments(FwdShared& sh, int n, int k, int lane) {
     float t = -INFINITY;
     if (n > k) {
         // largest t with at least k maxima of at least t, by bisection of its bits
-        unsigned lo = ordered(-INFINITY), hi = ordered(INFINITY);
+        float v[kPickRegs];
+        const bool in_regs = n <= 32 * kPickRegs;
+        float top = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < kPickRegs; ++j) {
+            v[j] = in_regs && lane + 32 * j < n ? sh.seg[lane + 32 * j] : -INFINITY;
+            top = fmaxf(top, v[j]);
+        }
+        unsigned lo = ordered(-INFINITY) >> GRAIN, hi = ordered(INFINITY) >> GRAIN;
+        if (in_regs) {
+            // the k-th largest of the lanes' maxima is reached k times: the answer is there or above
+            int above = 0;
+            for (int j = 0; j < 32; ++j) {
+                const float o = __shfl_sync(0xffffffffu, top, j);
+                above += o > top || (o == top && j < lane);
+            }
+            const unsigned who = __ballot_sync(0xffffffffu, above == min(k, 32) - 1);
+            if (who) lo = max(lo, ordered(__shfl_sync(0xffffffffu, top, __ffs(who) - 1)) >> GRAIN);
+            hi = max(lo, __reduce_max_sync(0xffffffffu, ordered(top) >> GRAIN));
+        }
         while (lo < hi) {
             const unsigned mid = lo + (hi - lo + 1) / 2;
-            const int c = total_at_least(sh.seg, n, from_ordered(mid), lane);
+            const float at = from_grain<GRAIN>(mid);
+            int c = 0;
+            if (in_regs) {
+#pragma unroll
+                for (int j = 0; j < kPickRegs; ++j) c += v[j] >= at;
+            } else {
+                for (int j = lane; j < n; j += 32) c += sh.seg[j] >= at;
+            }
+            c = __reduce_add_sync(0xffffffffu, c);
             if (c >= k) lo = mid; else hi = mid - 1;
             if (c == k) break;
         }
-        t = from_ordered(lo);
+        t = from_grain<GRAIN>(lo);
     }
     int above = 0;                           // segments above t; those equal to t fill up in order
     for (int j = lane; j < n; j += 32) above += sh.seg[j] > t;
@@ -227,7 +289,6 @@ logprob_fwd_kernel(const T* __restrict__ logits, int vocab, long long ld, const 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int parts = CLUSTER ? (int)cg::this_cluster().num_blocks() : 1, part = CLUSTER ? (int)cg::this_cluster().block_rank() : 0;
     const long long r = blockIdx.x / parts;
-    if constexpr (CLUSTER) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");     // this block runs
     FwdRow<T> row;
     row.x = logits + r * ld;
     row.vocab = vocab;
@@ -236,36 +297,55 @@ logprob_fwd_kernel(const T* __restrict__ logits, int vocab, long long ld, const 
     const int pieces = (vocab - row.head + kPiece - 1) / kPiece;
     // segments: [the head if there is one,] then runs of `per_segment` pieces; blocks take equal stretches of them
     const int heads = row.head > 0, segments = heads + (pieces + per_segment - 1) / per_segment;
-    const int each = (segments + parts - 1) / parts, s_lo = min(segments, part * each), s_hi = min(segments, s_lo + each), n = s_hi - s_lo;
+    const int each = (segments + parts - 1) / parts, s_lo = min(segments, part * each), s_hi = min(segments, s_lo + each);
     const float c = (float)(1.4426950408889634 * inv_temp);
     long long id = -1;
     float x_token = 0.f;
-    if (part == 0 && tid == 0 && logp) {
+    if (part == 0 && tid == 32 && logp) {
         id = token_id(tokens, r, vocab, status);
         if (id >= 0) x_token = to_f32(row.x[id]);
     }
+    if (tid == 0) sh.n_keys = sh.n_gathered = 0;
 
     FwdAcc acc;
     bool bad = false;
     if (per_segment == 1) {
-        // A warp's next pieces are on their way while it adds these.
-        for (int s0 = s_lo + warp; s0 < s_hi; s0 += kFwdWarps * kFwdUnroll) {
-            float f[kFwdUnroll][8];
+        constexpr int U = kFwdUnroll<T>;
+        uint4 x[U][sizeof(T) / 2], y[U][sizeof(T) / 2];
+        const int full = heads + (vocab - row.head) / kPiece;            // segments [heads, full) are full pieces
+        const int lo = max(s_lo, heads), hi = min(s_hi, full);
+        auto load = [&](uint4(&q)[U][sizeof(T) / 2], int s0) {
 #pragma unroll
-            for (int u = 0; u < kFwdUnroll; ++u) {
-                const int s = s0 + u * kFwdWarps;
-                if (s < s_hi) row.load(f[u], s - heads, lane);
-            }
+            for (int u = 0; u < U; ++u)
+                if (s0 + u * kFwdWarps < hi) row.load_raw(q[u], s0 + u * kFwdWarps - heads, lane);
+        };
+        auto one = [&](const float (&f)[8], int s) {
+            const float m = warp_max_nan(max8(f));
+            bad |= m != m;
+            if (lane == 0) sh.seg[s] = m;
+            acc.add(f, m, c);
+        };
+        auto add = [&](uint4(&q)[U][sizeof(T) / 2], int s0) {
 #pragma unroll
-            for (int u = 0; u < kFwdUnroll; ++u) {
+            for (int u = 0; u < U; ++u) {
                 const int s = s0 + u * kFwdWarps;
-                if (s >= s_hi) break;
-                const float m = warp_max_nan(max8(f[u]));
-                bad |= m != m;
-                if (lane == 0) sh.seg[s - s_lo] = m;
-                acc.add(f[u], m, c);
+                if (s >= hi) break;
+                float f[8];
+                row.widen(f, q[u]);
+                one(f, s);
             }
+        };
+        load(x, lo + warp);
+        for (int s0 = lo + warp; s0 < hi; s0 += 2 * U * kFwdWarps) {
+            load(y, s0 + U * kFwdWarps);
+            add(x, s0);
+            load(x, s0 + 2 * U * kFwdWarps);
+            add(y, s0 + U * kFwdWarps);
         }
+        // the row's ends
+        float f[8];
+        if (warp == kFwdWarps - 1 && s_lo < heads && s_hi > 0) { row.load_any(f, -1, lane); one(f, 0); }
+        if (warp == kFwdWarps - 2 && full < segments && s_lo <= full && full < s_hi) { row.load_any(f, full - heads, lane); one(f, full); }
     } else {
         for (int s = s_lo + warp; s < s_hi; s += kFwdWarps) {
             const int p0 = s < heads ? -1 : (s - heads) * per_segment, p1 = s < heads ? 0 : min(pieces, p0 + per_segment);
@@ -278,7 +358,7 @@ logprob_fwd_kernel(const T* __restrict__ logits, int vocab, long long ld, const 
                 acc.add(f, m, c);
             }
             bad |= best != best;
-            if (lane == 0) sh.seg[s - s_lo] = best;
+            if (lane == 0) sh.seg[s] = best;
         }
     }
     {
@@ -293,18 +373,50 @@ logprob_fwd_kernel(const T* __restrict__ logits, int vocab, long long ld, const 
             p += __shfl_xor_sync(0xffffffffu, p, o);
         }
         const int count = __reduce_add_sync(0xffffffffu, acc.count);
-        if (lane == 0) sh.stats[warp] = FwdStats{(double)count, (double)a, (double)p, acc.mx, bad || acc.mx == INFINITY};
+        if (lane == 0) sh.warp_stats[warp] = FwdStats{(double)count, (double)a, (double)p, acc.mx, bad || acc.mx == INFINITY};
     }
     __syncthreads();
+    FwdShared* first = &sh;
+    if constexpr (CLUSTER) {
+        cg::cluster_group cluster = cg::this_cluster();
+        if (tid == 0) sh.block = join(sh.warp_stats, kFwdWarps, c);
+        cluster.sync();
+        first = cluster.map_shared_rank(&sh, 0);
+        if (top > 0) {                                        // every block picks from the whole row's segments
+            for (int s = tid; s < segments; s += kFwdThreads) {
+                const int owner = s / each;
+                if (owner != part) sh.seg[s] = cluster.map_shared_rank(&sh, owner)->seg[s];
+            }
+            __syncthreads();
+        }
+    }
+    if (part == 0 && tid == 32) {                             // the row's values, beside the pick
+        FwdStats all;
+        if constexpr (CLUSTER) {
+            FwdStats of[kMaxCluster];
+            for (int k = 0; k < parts; ++k) of[k] = cg::this_cluster().map_shared_rank(&sh, k)->block;
+            all = join(of, parts, c);
+        } else {
+            all = join(sh.warp_stats, kFwdWarps, c);
+        }
+        const bool empty = all.mx == -INFINITY && !all.bad;
+        const double log_z = all.bad ? __longlong_as_double(0x7ff8000000000000ll) : empty ? 0.0 : log(all.count) + log1p(all.rest / all.count);
+        if (logp) logp[r] = id < 0 ? 0.f : empty ? -INFINITY : (float)(((double)x_token - all.mx) * inv_temp - log_z);
+        if (entropy) entropy[r] = empty ? 0.f : (float)(log_z - inv_temp * all.moment / (all.count + all.rest));
+        if (lse) lse[r] = empty ? -INFINITY : (float)((double)all.mx * inv_temp + log_z);
+        sh.log_z = log_z;
+        sh.row = all;
+    }
     if (top > 0) {
-        if (warp == 0) pick_segments(sh, n, top, lane);
-        if (tid == 32) sh.n_keys = 0;
+        constexpr int GRAIN = sizeof(T) == 4 ? 0 : std::is_same_v<T, __half> ? 13 : 16;
+        if (warp == 0) pick_segments<GRAIN>(sh, segments, top, lane);
         __syncthreads();
         const float t = sh.threshold;
         BestList list;
         const int picked = sh.n_picked;
         for (int j = warp; j < picked; j += kFwdWarps) {
-            const int s = s_lo + sh.picked[j];
+            const int s = sh.picked[j];
+            if (s < s_lo || s >= s_hi) continue;
             const int p0 = s < heads ? -1 : (s - heads) * per_segment, p1 = s < heads ? 0 : min(pieces, p0 + per_segment);
             for (int p = p0; p < p1; ++p) {
                 float f[8];
@@ -322,43 +434,28 @@ logprob_fwd_kernel(const T* __restrict__ logits, int vocab, long long ld, const 
         at = __shfl_sync(0xffffffffu, at, 0);
         if ((have >> lane) & 1) sh.keys[at + lane] = list.mine;                // valid keys are the first lanes
         __syncthreads();
-        rank_keys(sh.best, sh.keys, sh.n_keys, top);
-    }
-    FwdStats all{};
-    if constexpr (CLUSTER) {
-        cg::cluster_group cluster = cg::this_cluster();
-        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");                    // every block runs
-        if (tid == 0) all = join(sh.stats, kFwdWarps, c);
-        __syncthreads();
-        cluster.sync();                                       // the first block is done with its own use of what others write
-        FwdShared* first = cluster.map_shared_rank(&sh, 0);
-        if (tid == 0) first->stats[part] = all;
-        if (tid < top) first->keys[part * top + tid] = sh.best[tid];
-        cluster.sync();
-        if (part != 0) return;
-        if (top > 0) rank_keys(sh.best, sh.keys, parts * top, top);
-        if (tid == 0) all = join(sh.stats, parts, c);
-    } else {
-        if (tid == 0) all = join(sh.stats, kFwdWarps, c);
-    }
-    if (tid == 0) {
-        const bool empty = all.mx == -INFINITY && !all.bad;
-        double log_z = all.bad ? __longlong_as_double(0x7ff8000000000000ll) : empty ? 0.0 : log(all.count) + log1p(all.rest / all.count);
-        if (logp) logp[r] = id < 0 ? 0.f : empty ? -INFINITY : (float)(((double)x_token - all.mx) * inv_temp - log_z);
-        if (entropy) entropy[r] = empty ? 0.f : (float)(log_z - inv_temp * all.moment / (all.count + all.rest));
-        if (lse) lse[r] = empty ? -INFINITY : (float)((double)all.mx * inv_temp + log_z);
-        sh.log_z = log_z;
-        sh.stats[0] = all;
-    }
-    if (top > 0) {
-        __syncthreads();
+        int n = sh.n_keys;
+        rank_keys(sh.best, sh.keys, n, top);
+        if constexpr (CLUSTER) {
+            n = min(n, top);
+            if (warp == 0) {
+                if (lane == 0 && n) at = atomicAdd(&first->n_gathered, n);
+                at = __shfl_sync(0xffffffffu, at, 0);
+                if (lane < n) first->gathered[at + lane] = sh.best[lane];
+            }
+            cg::this_cluster().sync();
+            if (part != 0) return;
+            rank_keys(sh.best, sh.gathered, sh.n_gathered, top);
+        }
         if (tid < top) {
             const unsigned long long key = sh.best[tid];
-            const bool broken = sh.stats[0].bad, none = key == 0 || broken;
+            const bool broken = sh.row.bad, none = key == 0 || broken;
             top_ids[r * top + tid] = none ? -1 : (int)(0xffffffffu - (unsigned)key);
             top_logp[r * top + tid] = broken ? __int_as_float(0x7fc00000) : none ? -INFINITY
-                : (float)(((double)from_ordered((unsigned)(key >> 32)) - sh.stats[0].mx) * inv_temp - sh.log_z);
+                : (float)(((double)from_ordered((unsigned)(key >> 32)) - sh.row.mx) * inv_temp - sh.log_z);
         }
+    } else if constexpr (CLUSTER) {
+        cg::this_cluster().sync();                            // the first block has read the others' sums
     }
 }
 

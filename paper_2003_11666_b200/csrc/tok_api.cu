@@ -292,6 +292,7 @@ int pb_logprob_forward(const void* dev_logits, int dtype, int64_t rows, int64_t 
     const int64_t pieces = (vocab + kPiece - 1) / kPiece;
     int parts = 1;
     while (parts < kMaxCluster && rows * parts * 2 <= 148 * 4 && pieces >= (int64_t)parts * 2 * kFwdWarps) parts *= 2;
+    const bool few = parts == 1 && pieces + 1 < kMaxFewSegments && rows > 148 * 4;       // short rows: two warps each
     int per_segment = 1;
     while ((pieces + 1) / per_segment + 2 > kMaxSegments) per_segment *= 2;
     auto go = [&](auto t, auto i) {
@@ -300,15 +301,16 @@ int pb_logprob_forward(const void* dev_logits, int dtype, int64_t rows, int64_t 
         const T* x = (const T*)dev_logits;
         const I* tok = (const I*)dev_tokens;
         if (parts == 1) {
-            logprob_fwd_kernel<T, I, false><<<(unsigned)rows, kFwdThreads, 0, s>>>(x, (int)vocab, ld, tok, inv_temperature, dev_logp, dev_entropy, dev_lse, top_k,
-                                                                                 dev_top_logp, dev_top_ids, per_segment, dev_status);
+            auto kernel = few ? logprob_fwd_kernel<T, I, kFwdFewWarps, false> : logprob_fwd_kernel<T, I, kFwdWarps, false>;
+            kernel<<<(unsigned)rows, (few ? kFwdFewWarps : kFwdWarps) * 32, 0, s>>>(x, (int)vocab, ld, tok, inv_temperature, dev_logp, dev_entropy, dev_lse,
+                                                                                  top_k, dev_top_logp, dev_top_ids, per_segment, dev_status);
             return launched("pb_logprob_forward");
         }
-        auto kernel = logprob_fwd_kernel<T, I, true>;
+        auto kernel = logprob_fwd_kernel<T, I, kFwdWarps, true>;
         cudaError_t e = parts > 8 ? cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) : cudaSuccess;
         cudaLaunchConfig_t cfg{};
         cfg.gridDim = dim3((unsigned)(rows * parts));
-        cfg.blockDim = dim3(kFwdThreads);
+        cfg.blockDim = dim3(kFwdWarps * 32);
         cfg.stream = s;
         cudaLaunchAttribute attr{};
         attr.id = cudaLaunchAttributeClusterDimension;

@@ -1,3 +1,6 @@
+#ifndef FLB
+#define FLB 4
+#endif
 // Log probabilities of given tokens, entropy and top alternatives of rows of logits, and the
 // gradient of the three row values.
 //
@@ -20,72 +23,35 @@ namespace cg = cooperative_groups;
 constexpr int kMaxTop = 32;
 
 // ---------------------------------------------------------------- forward
-// One pass over the row.  A warp takes pieces of 256 consecutive logits, finds a piece's maximum with one
+// One pass over the row.  A warp takes pieces of 512 consecutive logits, finds a piece's maximum with one
 // warp reduction, and moves its running maximum (the same for all lanes) only when a piece exceeds it; the
 // sums e and e d stay in registers.  The maxima of the pieces (of runs of them, for very long rows)
 // stay in shared memory, and give the alternatives without a second pass: the k best elements, by value and
 // then by index, lie in the k best segments by the same order, for each better segment holds a better
 // element.  So at most 32 segments are read again, from L2.
 // A few rows are split over a cluster of blocks, joined through distributed shared memory.
-constexpr int kFwdThreads = 256, kFwdWarps = kFwdThreads / 32;
-constexpr int kPiece = 256;                 // logits of a warp's step: eight per lane
-constexpr int kMaxSegments = 2048;          // segments of a row
+constexpr int kFwdWarps = 8, kFwdFewWarps = 2;   // warps of a block; few for rows of a few pieces
+constexpr int kPiece = 512, kHalf = 256;    // logits of a warp's step: twice eight per lane
+constexpr int kMaxSegments = 1024, kMaxFewSegments = 32;    // segments of a row
 constexpr int kPickRegs = 16;               // maxima per lane that the pick keeps in registers
 constexpr int kMaxCluster = 16;
-template <typename T> constexpr int kFwdUnroll = 8 / (int)sizeof(T);       // pieces on their way while as many are added
+template <typename T> constexpr int kFwdStages = 8 / (int)sizeof(T);       // pieces of a warp in shared memory, all but one on their way
 
 struct FwdStats {                           // of a warp, a block or a row, relative to the maximum `mx`
-    double count, rest, moment;             // elements at the maximum; sum of the others' e; sum of e d
+    double count, rest, moment;             // elements at the maximum; sum of the others' e; sum of e log2(e)
     float mx;
     int bad;
 };
 
+template <int WARPS>
 struct FwdShared {
-    float seg[kMaxSegments];                // of the whole row; a block of a cluster fills its stretch and copies the others'
-    unsigned long long keys[kFwdWarps * kMaxTop], gathered[kMaxCluster * kMaxTop], best[kMaxTop];
-    FwdStats warp_stats[kFwdWarps], block, row;
+    float seg[WARPS == kFwdWarps ? kMaxSegments : kMaxFewSegments];                // of the whole row; a block of a cluster fills its stretch and copies the others'
+    unsigned long long keys[WARPS * kMaxTop], gathered[WARPS == kFwdWarps ? kMaxCluster * kMaxTop : 1], best[kMaxTop];
+    FwdStats warp_stats[WARPS], block, row;
     int picked[kMaxTop];
     float threshold;
     int n_picked, n_keys, n_gathered;
     double log_z;
-};
-
-template <typename T>
-struct FwdRow {
-    const T* x;
-    int vocab, head;                        // head: logits before the first aligned one, a segment of their own
-    __device__ __forceinline__ bool full(int piece) const { return head + (piece + 1) * kPiece <= vocab; }
-    // Lane's eight logits of a piece; -inf beyond the end.  Piece -1: the head.
-    __device__ __forceinline__ int first(int piece, int lane) const { return piece < 0 ? lane * 8 : head + piece * kPiece + lane * 8; }
-    __device__ __forceinline__ void load_any(float (&f)[8], int piece, int lane) const {
-        const int i = first(piece, lane), end = piece < 0 ? head : vocab;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) f[k] = i + k < end ? to_f32(x[i + k]) : -INFINITY;
-    }
-    // a full piece as it is in memory
-    __device__ __forceinline__ void load_raw(uint4 (&q)[sizeof(T) / 2], int piece, int lane) const {
-#pragma unroll
-        for (int k = 0; k < (int)sizeof(T) / 2; ++k) q[k] = *reinterpret_cast<const uint4*>(x + first(piece, lane) + 4 * k);
-    }
-    __device__ __forceinline__ void widen(float (&f)[8], const uint4 (&q)[sizeof(T) / 2]) const {
-        if constexpr (sizeof(T) == 4) {
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                f[4 * k] = __uint_as_float(q[k].x); f[4 * k + 1] = __uint_as_float(q[k].y);
-                f[4 * k + 2] = __uint_as_float(q[k].z); f[4 * k + 3] = __uint_as_float(q[k].w);
-            }
-        } else {
-            unpack8(f, q[0], T());
-        }
-    }
-    __device__ __forceinline__ void load(float (&f)[8], int piece, int lane) const {
-        if (piece >= 0 && full(piece)) {
-            if constexpr (sizeof(T) == 4) load8_wide(f, x + first(piece, lane));
-            else load8(f, x + first(piece, lane));
-        } else {
-            load_any(f, piece, lane);
-        }
-    }
 };
 
 __device__ __forceinline__ float warp_max_nan(float x) {
@@ -102,54 +68,188 @@ __device__ __forceinline__ float max8(const float (&f)[8]) {
     return max_nan(max3(max3(f[0], f[1], f[2]), f[3], f[4]), max3(f[5], f[6], f[7]));
 }
 
-// A warp's running sums.
+// A lane's sixteen logits of a piece, as they are in memory.
+template <typename T>
+struct FwdPiece {
+    uint4 q[2][sizeof(T) / 2];
+    __device__ __forceinline__ void widen(float (&f)[8], int half) const {
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                f[4 * k] = __uint_as_float(q[half][k].x); f[4 * k + 1] = __uint_as_float(q[half][k].y);
+                f[4 * k + 2] = __uint_as_float(q[half][k].z); f[4 * k + 3] = __uint_as_float(q[half][k].w);
+            }
+        } else {
+            unpack8(f, q[half][0], T());
+        }
+    }
+    // 16-bit logits raised to at least `lowest`, two at a time
+    __device__ __forceinline__ void widen_raised(float (&f)[8], int half) const {
+        const T low = from_f32<T>(lowest<T>());
+        unsigned w[4] = {q[half][0].x, q[half][0].y, q[half][0].z, q[half][0].w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) w[k] = max2<T>(w[k], low);
+        unpack8(f, make_uint4(w[0], w[1], w[2], w[3]), T());
+    }
+    // far below any maximum for which it is used, and finite times c
+    template <typename V> static __device__ __forceinline__ float lowest() { return std::is_same_v<V, __half> ? -65504.f : -0x1p100f; }
+    template <typename V> static __device__ __forceinline__ unsigned max2(unsigned a, unsigned b) {
+        unsigned r;
+        if constexpr (std::is_same_v<V, __half>) asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+        else asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+        return r;
+    }
+    template <typename V> static __device__ __forceinline__ unsigned max2(unsigned a, V low) {
+        const unsigned l = *reinterpret_cast<const unsigned short*>(&low);
+        return max2<V>(a, l | l << 16);
+    }
+    __device__ __forceinline__ float top() const {
+        if constexpr (sizeof(T) == 4) {
+            float f[8], g[8];
+            widen(f, 0);
+            widen(g, 1);
+            return max_nan(max8(f), max8(g));
+        } else {
+            const uint4 a = q[0][0], b = q[1][0];
+            const unsigned m = max2<T>(max2<T>(max2<T>(a.x, a.y), max2<T>(a.z, a.w)), max2<T>(max2<T>(b.x, b.y), max2<T>(b.z, b.w)));
+            float f[8];
+            unpack8(f, make_uint4(m, m, m, m), T());
+            return max_nan(f[0], f[1]);
+        }
+    }
+};
+
+template <typename T> constexpr int kPieceQuads = (int)sizeof(T);      // 16-byte quads of a lane
+
+template <typename T>
+struct FwdRow {
+    const T* x;
+    int vocab, head;                        // head: logits before the first aligned one, a segment of their own
+    // a lane's first logit of half a piece
+    __device__ __forceinline__ int first(int piece, int half, int lane) const {
+        return piece < 0 ? (half ? vocab : lane * 8) : head + piece * kPiece + half * kHalf + lane * 8;
+    }
+    // -inf beyond the end; piece -1: the head
+    __device__ __forceinline__ void load_any(float (&f)[8], int piece, int half, int lane) const {
+        const int i = first(piece, half, lane), end = piece < 0 ? head : vocab;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) f[k] = i + k < end ? to_f32(x[i + k]) : -INFINITY;
+    }
+    // A lane copies its own sixteen logits and reads them itself, so nothing but the copy is waited for.
+    __device__ __forceinline__ void copy(uint4* slot, int piece, int lane) const {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int k = 0; k < (int)sizeof(T) / 2; ++k)
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;"
+                             ::"r"((unsigned)__cvta_generic_to_shared(slot + (h * (int)sizeof(T) / 2 + k) * 32 + lane)),
+                               "l"(x + first(piece, h, lane) + 4 * k) : "memory");
+    }
+    __device__ __forceinline__ void read(FwdPiece<T>& p, const uint4* slot, int lane) const {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int k = 0; k < (int)sizeof(T) / 2; ++k) p.q[h][k] = slot[(h * (int)sizeof(T) / 2 + k) * 32 + lane];
+    }
+    __device__ __forceinline__ bool full(int piece) const { return piece >= 0 && head + (piece + 1) * kPiece <= vocab; }
+};
+
+// A warp's running sums, in units of log2: with c = log2(e) inverse_temperature and the rounded R = c max,
+// y = fma(x, c, -R) takes one instruction for two logits, and the rounding of R, known exactly as
+// delta = c max - R, is put right when the sums are used.  Sums: rest of 2^y, moment of 2^y y, over the logits
+// below the maximum; those equal to it are counted.
 struct FwdAcc {
-    float mx = -INFINITY;
+    float mx = -INFINITY, ref = 0.f, delta = 0.f;
+    bool wide = false;                      // c max near float32's range: y = (x - max) c
+    bool raise = false;                     // logits may be raised to FwdPiece::lowest: 2^y is zero there as well
     int count = 0;
     Pair rest{0.f, 0.f}, moment{0.f, 0.f};
-    // c: log2(e) times the inverse temperature
-    __device__ __forceinline__ void add(const float (&f)[8], float top, float c) {
-        if (top > mx) {                      // the same for the whole warp
-            if (mx > -INFINITY) {
-                const float shift = mx - top, s = exp2_near(shift * c);
-                float r0, r1;
-                rest.split(r0, r1);
-                r0 += (float)count;
-                moment = (moment + Pair(r0, r1) * Pair(shift)) * Pair(s);
-                rest = Pair(r0, r1) * Pair(s);
-                count = 0;
-            }
-            mx = top;
+
+    __device__ __forceinline__ void move(float top, float c, float lowest) {
+        const bool w = !(fabsf(top) < 1e36f && fabsf(top * c) < 1e36f);
+        const float r = w ? 0.f : top * c, d = w ? 0.f : fmaf(top, c, -r);
+        if (mx > -INFINITY) {
+            const float shift = fmaxf((mx - top) * c, -1e30f) - delta + d, s = exp2_near(shift), own = (float)count * exp2_near(delta);
+            float r0, r1, m0, m1;
+            rest.split(r0, r1);
+            moment.split(m0, m1);
+            r0 += own;
+            m0 = fmaf(own, delta, m0);
+            moment = Pair(fmaf(r0, shift, m0) * s, fmaf(r1, shift, m1) * s);
+            rest = Pair(r0 * s, r1 * s);
+            count = 0;
         }
-        if (top == mx) {
-            if (mx > -INFINITY) add_at_top(f, c);
-        } else {
-            add_below(f, c);
-        }
+        mx = top;
+        ref = r;
+        delta = d;
+        wide = w;
+        raise = !w && c < 1e8f && (top - lowest) * c > 200.f;
     }
-    // every logit is below the maximum (or NaN)
+    // LOW: -inf may be among the logits
+    template <bool LOW, bool WIDE>
     __device__ __forceinline__ void add_below(const float (&f)[8], float c) {
-        const Pair m(-mx), cc(c);
+        const Pair m(WIDE ? -mx : -ref), cc(c);
 #pragma unroll
         for (int k = 0; k < 8; k += 2) {
+            const Pair x(f[k], f[k + 1]);
+            Pair y = WIDE ? (x + m) * cc : fma2(x, cc, m);
             float a, b;
-            (Pair(f[k], f[k + 1]) + m).split(a, b);
-            const Pair d(max_nan(a, -1e30f), max_nan(b, -1e30f));      // e d is 0, not 0 times infinity, where e is 0
-            (d * cc).split(a, b);
+            y.split(a, b);
+            if (LOW) {                       // 2^y y is 0, not 0 times infinity, where 2^y is 0
+                a = max_nan(a, -1e30f);
+                b = max_nan(b, -1e30f);
+                y = Pair(a, b);
+            }
             const Pair e(exp2_near(a), exp2_near(b));
             rest = rest + e;
-            moment = fma2(e, d, moment);
+            moment = fma2(e, y, moment);
         }
     }
-    // the maximum itself is counted, not added
-    __device__ __forceinline__ void add_at_top(const float (&f)[8], float c) {
-        float g[8];
+    // counts the logits at the maximum and leaves `instead` in their place
+    __device__ __forceinline__ void take_top(float (&f)[8], float instead) {
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
             count += f[k] == mx;
-            g[k] = f[k] == mx ? -INFINITY : f[k];
+            f[k] = f[k] == mx ? instead : f[k];
         }
-        add_below(g, c);
+    }
+    // eight logits per lane whose warp-wide maximum is `top`
+    __device__ __forceinline__ void add(float (&f)[8], float top, float c, float lowest) {
+        if (top > mx) move(top, c, lowest);
+        if (mx == -INFINITY) return;         // nothing finite so far
+        take_top(f, -INFINITY);
+        if (wide) add_below<true, true>(f, c); else add_below<true, false>(f, c);
+    }
+    // a full piece; `again` gives half of it a second time
+    template <typename T, typename Again>
+    __device__ __forceinline__ void add(const FwdPiece<T>& p, float top, float c, float lowest, Again again) {
+        if (top > mx) move(top, c, lowest);
+        if (sizeof(T) == 2 ? raise : !wide && mx > -INFINITY) {
+            const bool at_top = top == mx;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                float f[8];
+                if constexpr (sizeof(T) == 2) p.widen_raised(f, h); else p.widen(f, h);
+                if (at_top) take_top(f, sizeof(T) == 2 ? lowest : -INFINITY);
+                add_below<sizeof(T) == 4, false>(f, c);
+            }
+        } else {
+#pragma unroll 1
+            for (int h = 0; h < 2; ++h) {
+                float f[8];
+                again(f, h);
+                add(f, top, c, lowest);
+            }
+        }
+    }
+    // sums relative to the maximum itself, in natural units over the inverse temperature's: c d = y - delta
+    __device__ __forceinline__ void finish(float (&out)[2]) const {
+        float r0, r1, m0, m1;
+        rest.split(r0, r1);
+        moment.split(m0, m1);
+        const float s = exp2_near(-delta);
+        out[0] = (r0 + r1) * s;
+        out[1] = fmaf(-delta, r0 + r1, m0 + m1) * s;
     }
 };
 
@@ -164,8 +264,8 @@ __device__ __forceinline__ FwdStats join(const FwdStats* p, int n, float c) {
             t.rest += p[k].rest;
             t.moment += p[k].moment;
         } else {
-            const float shift = p[k].mx - t.mx;
-            const double s = exp2_near(shift * c), all = p[k].rest + p[k].count;
+            const float shift = fmaxf((p[k].mx - t.mx) * c, -1e30f);         // finite: times a sum that it makes zero
+            const double s = exp2_near(shift), all = p[k].rest + p[k].count;
             t.rest += s * all;
             t.moment += s * (p[k].moment + all * shift);
         }
@@ -191,8 +291,8 @@ __device__ __forceinline__ float from_grain(unsigned k) {
 
 // The k best of n segments (by maximum, then by index) into sh.picked, and a value that the k-th best
 // maximum reaches into sh.threshold; one warp.  Maxima are values of T: GRAIN low bits of them are zero.
-template <int GRAIN>
-__device__ __forceinline__ void pick_segments(FwdShared& sh, int n, int k, int lane) {
+template <int GRAIN, int WARPS>
+__device__ __forceinline__ void pick_segments(FwdShared<WARPS>& sh, int n, int k, int lane) {
     float t = -INFINITY;
     if (n > k) {
         // largest t with at least k maxima of at least t, by bisection of its bits
@@ -268,10 +368,11 @@ struct BestList {
 };
 
 // best[0..k) <- the k largest of n keys, in order; zero where there are fewer.  By all threads.
+template <int WARPS>
 __device__ __forceinline__ void rank_keys(unsigned long long* best, const unsigned long long* keys, int n, int k) {
     if ((int)threadIdx.x < k) best[threadIdx.x] = 0;
     __syncthreads();
-    for (int i = threadIdx.x; i < n; i += kFwdThreads) {
+    for (int i = threadIdx.x; i < n; i += WARPS * 32) {
         const unsigned long long x = keys[i];
         int above = 0;
         for (int j = 0; j < n; ++j) above += keys[j] > x;     // keys differ: each holds its index; zeros are none
@@ -280,12 +381,13 @@ __device__ __forceinline__ void rank_keys(unsigned long long* best, const unsign
     __syncthreads();
 }
 
-template <typename T, typename I, bool CLUSTER>
-__global__ void __launch_bounds__(kFwdThreads, 4)
+template <typename T, typename I, int WARPS, bool CLUSTER>
+__global__ void __launch_bounds__(WARPS * 32, WARPS == kFwdWarps ? FLB : 4 * FLB)
 logprob_fwd_kernel(const T* __restrict__ logits, int vocab, long long ld, const I* __restrict__ tokens, double inv_temp,
                    float* __restrict__ logp, float* __restrict__ entropy, float* __restrict__ lse, int top,
                    float* __restrict__ top_logp, int* __restrict__ top_ids, int per_segment, int* status) {
-    __shared__ FwdShared sh;
+    __shared__ FwdShared<WARPS> sh;
+    __shared__ uint4 sh_ring[WARPS * kFwdStages<T> * kPieceQuads<T> * 32];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int parts = CLUSTER ? (int)cg::this_cluster().num_blocks() : 1, part = CLUSTER ? (int)cg::this_cluster().block_rank() : 0;
     const long long r = blockIdx.x / parts;
@@ -309,64 +411,66 @@ logprob_fwd_kernel(const T* __restrict__ logits, int vocab, long long ld, const 
 
     FwdAcc acc;
     bool bad = false;
-    if (per_segment == 1) {
-        constexpr int U = kFwdUnroll<T>;
-        uint4 x[U][sizeof(T) / 2], y[U][sizeof(T) / 2];
-        const int full = heads + (vocab - row.head) / kPiece;            // segments [heads, full) are full pieces
-        const int lo = max(s_lo, heads), hi = min(s_hi, full);
-        auto load = [&](uint4(&q)[U][sizeof(T) / 2], int s0) {
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-                if (s0 + u * kFwdWarps < hi) row.load_raw(q[u], s0 + u * kFwdWarps - heads, lane);
+    const float lowest = FwdPiece<T>::template lowest<T>();
+    {
+        // The warp's full pieces: those of its segments, WARPS apart.
+        constexpr int S = kFwdStages<T>;
+        uint4* ring = sh_ring + warp * S * kPieceQuads<T> * 32;
+        const int full = (vocab - row.head) / kPiece;                    // pieces [0, full) are full
+        const int lo = max(s_lo, heads), mine = max(0, (s_hi - lo - warp + WARPS - 1) / WARPS);
+        const int shift = __ffs(per_segment) - 1;
+        int count = 0;
+        if (mine > 0) count = ((mine - 1) << shift) + min(per_segment, max(0, full - ((lo + warp + (mine - 1) * WARPS - heads) << shift)));
+        auto segment = [&](int j) { return lo + warp + (j >> shift) * WARPS; };
+        auto piece = [&](int j) { return ((segment(j) - heads) << shift) + (j & (per_segment - 1)); };
+        auto ahead = [&](int j) {
+            if (j < count) row.copy(ring + (j % S) * kPieceQuads<T> * 32, piece(j), lane);
+            asm volatile("cp.async.commit_group;" ::: "memory");
         };
-        auto one = [&](const float (&f)[8], int s) {
-            const float m = warp_max_nan(max8(f));
-            bad |= m != m;
-            if (lane == 0) sh.seg[s] = m;
-            acc.add(f, m, c);
-        };
-        auto add = [&](uint4(&q)[U][sizeof(T) / 2], int s0) {
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int s = s0 + u * kFwdWarps;
-                if (s >= hi) break;
-                float f[8];
-                row.widen(f, q[u]);
-                one(f, s);
+        for (int j = 0; j < S - 1; ++j) ahead(j);
+        float best = -INFINITY;
+#pragma unroll 1
+        for (int j = 0; j < count; ++j) {
+            ahead(j + S - 1);
+            asm volatile("cp.async.wait_group %0;" ::"n"(S - 1) : "memory");
+            FwdPiece<T> p;
+            row.read(p, ring + (j % S) * kPieceQuads<T> * 32, lane);
+            const float m = warp_max_nan(p.top());
+            best = max_nan(best, m);
+            if (((j + 1) & (per_segment - 1)) == 0 || j + 1 == count) {
+                bad |= best != best;
+                if (lane == 0) sh.seg[segment(j)] = best;
+                best = -INFINITY;
             }
-        };
-        load(x, lo + warp);
-        for (int s0 = lo + warp; s0 < hi; s0 += 2 * U * kFwdWarps) {
-            load(y, s0 + U * kFwdWarps);
-            add(x, s0);
-            load(x, s0 + 2 * U * kFwdWarps);
-            add(y, s0 + U * kFwdWarps);
+            acc.add(p, m, c, lowest, [&](float(&f)[8], int h) { row.load_any(f, piece(j), h, lane); });
         }
-        // the row's ends
-        float f[8];
-        if (warp == kFwdWarps - 1 && s_lo < heads && s_hi > 0) { row.load_any(f, -1, lane); one(f, 0); }
-        if (warp == kFwdWarps - 2 && full < segments && s_lo <= full && full < s_hi) { row.load_any(f, full - heads, lane); one(f, full); }
-    } else {
-        for (int s = s_lo + warp; s < s_hi; s += kFwdWarps) {
-            const int p0 = s < heads ? -1 : (s - heads) * per_segment, p1 = s < heads ? 0 : min(pieces, p0 + per_segment);
-            float best = -INFINITY;
-            for (int p = p0; p < p1; ++p) {
+        // The row's ends: the logits before the first piece are a segment of the first block, those behind the
+        // last full piece join its segment or are one.
+        const int last = heads + (full >> shift);
+        const bool behind = row.head + full * kPiece < vocab && last >= lo && last < s_hi && (last - lo) % WARPS == warp;
+        const bool before = heads && s_lo == 0 && s_hi > 0 && warp == WARPS - 1;
+#pragma unroll 1
+        for (int e = 0; e < 2; ++e) {
+            if (!(e ? behind : before)) continue;
+            float top = -INFINITY;
+#pragma unroll 1
+            for (int h = 0; h < 2; ++h) {
                 float f[8];
-                row.load(f, p, lane);
+                row.load_any(f, e ? full : -1, h, lane);
                 const float m = warp_max_nan(max8(f));
-                best = max_nan(best, m);
-                acc.add(f, m, c);
+                top = max_nan(top, m);
+                acc.add(f, m, c, lowest);
             }
-            bad |= best != best;
-            if (lane == 0) sh.seg[s] = best;
+            bad |= top != top;
+            __syncwarp();
+            if (lane == 0) sh.seg[e ? last : 0] = e && (full & (per_segment - 1)) ? max_nan(sh.seg[last], top) : top;
         }
     }
     {
-        float a, b, p, q;
-        acc.rest.split(a, b);
-        acc.moment.split(p, q);
-        a += b;
-        p += q;
+        float sums[2];
+        acc.finish(sums);
+        float a = sums[0], p = sums[1];
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) {
             a += __shfl_xor_sync(0xffffffffu, a, o);
@@ -376,14 +480,14 @@ logprob_fwd_kernel(const T* __restrict__ logits, int vocab, long long ld, const 
         if (lane == 0) sh.warp_stats[warp] = FwdStats{(double)count, (double)a, (double)p, acc.mx, bad || acc.mx == INFINITY};
     }
     __syncthreads();
-    FwdShared* first = &sh;
+    FwdShared<WARPS>* first = &sh;
     if constexpr (CLUSTER) {
         cg::cluster_group cluster = cg::this_cluster();
-        if (tid == 0) sh.block = join(sh.warp_stats, kFwdWarps, c);
+        if (tid == 0) sh.block = join(sh.warp_stats, WARPS, c);
         cluster.sync();
         first = cluster.map_shared_rank(&sh, 0);
         if (top > 0) {                                        // every block picks from the whole row's segments
-            for (int s = tid; s < segments; s += kFwdThreads) {
+            for (int s = tid; s < segments; s += WARPS * 32) {
                 const int owner = s / each;
                 if (owner != part) sh.seg[s] = cluster.map_shared_rank(&sh, owner)->seg[s];
             }
@@ -397,31 +501,38 @@ logprob_fwd_kernel(const T* __restrict__ logits, int vocab, long long ld, const 
             for (int k = 0; k < parts; ++k) of[k] = cg::this_cluster().map_shared_rank(&sh, k)->block;
             all = join(of, parts, c);
         } else {
-            all = join(sh.warp_stats, kFwdWarps, c);
+            all = join(sh.warp_stats, WARPS, c);
         }
         const bool empty = all.mx == -INFINITY && !all.bad;
         const double log_z = all.bad ? __longlong_as_double(0x7ff8000000000000ll) : empty ? 0.0 : log(all.count) + log1p(all.rest / all.count);
         if (logp) logp[r] = id < 0 ? 0.f : empty ? -INFINITY : (float)(((double)x_token - all.mx) * inv_temp - log_z);
-        if (entropy) entropy[r] = empty ? 0.f : (float)(log_z - inv_temp * all.moment / (all.count + all.rest));
+        if (entropy) entropy[r] = empty ? 0.f : (float)(log_z - 0.6931471805599453 * all.moment / (all.count + all.rest));
         if (lse) lse[r] = empty ? -INFINITY : (float)((double)all.mx * inv_temp + log_z);
         sh.log_z = log_z;
         sh.row = all;
     }
     if (top > 0) {
         constexpr int GRAIN = sizeof(T) == 4 ? 0 : std::is_same_v<T, __half> ? 13 : 16;
-        if (warp == 0) pick_segments<GRAIN>(sh, segments, top, lane);
+        if (warp == 0) pick_segments<GRAIN, WARPS>(sh, segments, top, lane);
         __syncthreads();
         const float t = sh.threshold;
         BestList list;
         const int picked = sh.n_picked;
-        for (int j = warp; j < picked; j += kFwdWarps) {
+        for (int j = warp; j < picked; j += WARPS) {
             const int s = sh.picked[j];
             if (s < s_lo || s >= s_hi) continue;
             const int p0 = s < heads ? -1 : (s - heads) * per_segment, p1 = s < heads ? 0 : min(pieces, p0 + per_segment);
-            for (int p = p0; p < p1; ++p) {
+#pragma unroll 1
+            for (int ph = 2 * p0; ph < 2 * p1; ++ph) {        // halves of pieces
+                const int p = ph >> 1, h = ph & 1;
                 float f[8];
-                row.load(f, p, lane);
-                const int i = row.first(p, lane);
+                const int i = row.first(p, h, lane);
+                if (row.full(p)) {
+                    if constexpr (sizeof(T) == 4) load8_wide(f, row.x + i);
+                    else load8(f, row.x + i);
+                } else {
+                    row.load_any(f, p, h, lane);
+                }
                 if (!__any_sync(0xffffffffu, max8(f) >= t)) continue;
 #pragma unroll
                 for (int k = 0; k < 8; ++k)
@@ -435,7 +546,7 @@ logprob_fwd_kernel(const T* __restrict__ logits, int vocab, long long ld, const 
         if ((have >> lane) & 1) sh.keys[at + lane] = list.mine;                // valid keys are the first lanes
         __syncthreads();
         int n = sh.n_keys;
-        rank_keys(sh.best, sh.keys, n, top);
+        rank_keys<WARPS>(sh.best, sh.keys, n, top);
         if constexpr (CLUSTER) {
             n = min(n, top);
             if (warp == 0) {
@@ -445,7 +556,7 @@ logprob_fwd_kernel(const T* __restrict__ logits, int vocab, long long ld, const 
             }
             cg::this_cluster().sync();
             if (part != 0) return;
-            rank_keys(sh.best, sh.gathered, sh.n_gathered, top);
+            rank_keys<WARPS>(sh.best, sh.gathered, sh.n_gathered, top);
         }
         if (tid < top) {
             const unsigned long long key = sh.best[tid];

@@ -289,12 +289,12 @@ int pb_logprob_forward(const void* dev_logits, int dtype, int64_t rows, int64_t 
     const cudaStream_t s = (cudaStream_t)stream;
     // A few rows are split over clusters as long as all blocks are resident at once (four per SM) and every warp
     // of a block still has a piece.
-    const int64_t pieces = (vocab + kPiece - 1) / kPiece;
+    const int64_t pieces = vocab / (2048 / (int64_t)dtype_bytes(dtype));
     int parts = 1;
-    while (parts < kMaxCluster && rows * parts * 2 <= 148 * 4 && pieces >= (int64_t)parts * 2 * kFwdWarps) parts *= 2;
-    const bool few = parts == 1 && pieces + 1 < kMaxFewSegments && rows > 148 * 4;       // short rows: two warps each
+    while (parts < kMaxCluster && rows * parts * 2 <= 148 * 4 && pieces >= (int64_t)parts * kFwdWarps) parts *= 2;
+    const bool few = parts == 1 && pieces < kMaxFewSegments && rows > 148 * 4;       // short rows: two warps each
     int per_segment = 1;
-    while ((pieces + 1) / per_segment + 2 > kMaxSegments) per_segment *= 2;
+    while (pieces / per_segment + 1 > kMaxSegments) per_segment *= 2;
     auto go = [&](auto t, auto i) {
         using T = decltype(t);
         using I = decltype(i);

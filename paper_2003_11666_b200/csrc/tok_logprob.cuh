@@ -23,7 +23,7 @@ namespace cg = cooperative_groups;
 constexpr int kMaxTop = 32;
 
 // ---------------------------------------------------------------- forward
-// One pass over the row.  A warp takes pieces of 512 consecutive logits, finds a piece's maximum with one
+// One pass over the row.  A warp takes pieces of 2 KB of consecutive logits, finds a piece's maximum with one
 // warp reduction, and moves its running maximum (the same for all lanes) only when a piece exceeds it; the
 // sums e and e d stay in registers.  The maxima of the pieces (of runs of them, for very long rows)
 // stay in shared memory, and give the alternatives without a second pass: the k best elements, by value and
@@ -31,11 +31,14 @@ constexpr int kMaxTop = 32;
 // element.  So at most 32 segments are read again, from L2.
 // A few rows are split over a cluster of blocks, joined through distributed shared memory.
 constexpr int kFwdWarps = 8, kFwdFewWarps = 2;   // warps of a block; few for rows of a few pieces
-constexpr int kPiece = 512, kHalf = 256;    // logits of a warp's step: twice eight per lane
+constexpr int kEight = 256;                 // logits of a warp, eight per lane
+constexpr int kQuads = 4;                   // 16-byte quads of a lane in a piece
+template <typename T> constexpr int kEights = 8 / (int)sizeof(T);          // times eight logits of a lane in a piece
+template <typename T> constexpr int kPiece = kEight * kEights<T>;          // logits of a warp's step
 constexpr int kMaxSegments = 1024, kMaxFewSegments = 32;    // segments of a row
 constexpr int kPickRegs = 16;               // maxima per lane that the pick keeps in registers
 constexpr int kMaxCluster = 16;
-template <typename T> constexpr int kFwdStages = 8 / (int)sizeof(T);       // pieces of a warp in shared memory, all but one on their way
+constexpr int kFwdStages = 2;               // pieces of a warp on their way through shared memory
 
 struct FwdStats {                           // of a warp, a block or a row, relative to the maximum `mx`
     double count, rest, moment;             // elements at the maximum; sum of the others' e; sum of e log2(e)
@@ -45,11 +48,11 @@ struct FwdStats {                           // of a warp, a block or a row, rela
 
 template <int WARPS>
 struct FwdShared {
-    float seg[WARPS == kFwdWarps ? kMaxSegments : kMaxFewSegments];                // of the whole row; a block of a cluster fills its stretch and copies the others'
+    unsigned seg[WARPS == kFwdWarps ? kMaxSegments : kMaxFewSegments];   // maxima in order as ordered(); a block of a cluster fills its stretch
     unsigned long long keys[WARPS * kMaxTop], gathered[WARPS == kFwdWarps ? kMaxCluster * kMaxTop : 1], best[kMaxTop];
     FwdStats warp_stats[WARPS], block, row;
     int picked[kMaxTop];
-    float threshold;
+    unsigned threshold;
     int n_picked, n_keys, n_gathered;
     double log_z;
 };
@@ -68,40 +71,34 @@ __device__ __forceinline__ float max8(const float (&f)[8]) {
     return max_nan(max3(max3(f[0], f[1], f[2]), f[3], f[4]), max3(f[5], f[6], f[7]));
 }
 
-// A lane's sixteen logits of a piece, as they are in memory.
+// A lane's logits of a piece, as they are in memory.
 template <typename T>
 struct FwdPiece {
-    uint4 q[2][sizeof(T) / 2];
-    __device__ __forceinline__ void widen(float (&f)[8], int half) const {
+    uint4 q[kQuads];
+    __device__ __forceinline__ void widen(float (&f)[8], int e) const {
         if constexpr (sizeof(T) == 4) {
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
-                f[4 * k] = __uint_as_float(q[half][k].x); f[4 * k + 1] = __uint_as_float(q[half][k].y);
-                f[4 * k + 2] = __uint_as_float(q[half][k].z); f[4 * k + 3] = __uint_as_float(q[half][k].w);
+                f[4 * k] = __uint_as_float(q[2 * e + k].x); f[4 * k + 1] = __uint_as_float(q[2 * e + k].y);
+                f[4 * k + 2] = __uint_as_float(q[2 * e + k].z); f[4 * k + 3] = __uint_as_float(q[2 * e + k].w);
             }
         } else {
-            unpack8(f, q[half][0], T());
+            unpack8(f, q[e], T());
         }
     }
-    // 16-bit logits raised to at least `lowest`, two at a time
-    __device__ __forceinline__ void widen_raised(float (&f)[8], int half) const {
-        const T low = from_f32<T>(lowest<T>());
-        unsigned w[4] = {q[half][0].x, q[half][0].y, q[half][0].z, q[half][0].w};
-#pragma unroll
-        for (int k = 0; k < 4; ++k) w[k] = max2<T>(w[k], low);
-        unpack8(f, make_uint4(w[0], w[1], w[2], w[3]), T());
+    // 16-bit logits raised to at least lowest(), two at a time
+    __device__ __forceinline__ void widen_raised(float (&f)[8], int e) const {
+        const T low = from_f32<T>(lowest());
+        const unsigned l = (unsigned)*reinterpret_cast<const unsigned short*>(&low) * 0x10001u;
+        unpack8(f, make_uint4(max2(q[e].x, l), max2(q[e].y, l), max2(q[e].z, l), max2(q[e].w, l)), T());
     }
     // far below any maximum for which it is used, and finite times c
-    template <typename V> static __device__ __forceinline__ float lowest() { return std::is_same_v<V, __half> ? -65504.f : -0x1p100f; }
-    template <typename V> static __device__ __forceinline__ unsigned max2(unsigned a, unsigned b) {
+    static __device__ __forceinline__ float lowest() { return std::is_same_v<T, __half> ? -65504.f : -0x1p100f; }
+    static __device__ __forceinline__ unsigned max2(unsigned a, unsigned b) {
         unsigned r;
-        if constexpr (std::is_same_v<V, __half>) asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+        if constexpr (std::is_same_v<T, __half>) asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
         else asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
         return r;
-    }
-    template <typename V> static __device__ __forceinline__ unsigned max2(unsigned a, V low) {
-        const unsigned l = *reinterpret_cast<const unsigned short*>(&low);
-        return max2<V>(a, l | l << 16);
     }
     __device__ __forceinline__ float top() const {
         if constexpr (sizeof(T) == 4) {
@@ -110,48 +107,32 @@ struct FwdPiece {
             widen(g, 1);
             return max_nan(max8(f), max8(g));
         } else {
-            const uint4 a = q[0][0], b = q[1][0];
-            const unsigned m = max2<T>(max2<T>(max2<T>(a.x, a.y), max2<T>(a.z, a.w)), max2<T>(max2<T>(b.x, b.y), max2<T>(b.z, b.w)));
+            unsigned m[kQuads];
+#pragma unroll
+            for (int k = 0; k < kQuads; ++k) m[k] = max2(max2(q[k].x, q[k].y), max2(q[k].z, q[k].w));
+            const unsigned t = max2(max2(m[0], m[1]), max2(m[2], m[3]));
             float f[8];
-            unpack8(f, make_uint4(m, m, m, m), T());
+            unpack8(f, make_uint4(t, t, t, t), T());
             return max_nan(f[0], f[1]);
         }
     }
 };
 
-template <typename T> constexpr int kPieceQuads = (int)sizeof(T);      // 16-byte quads of a lane
-
 template <typename T>
 struct FwdRow {
     const T* x;
-    int vocab, head;                        // head: logits before the first aligned one, a segment of their own
-    // a lane's first logit of half a piece
-    __device__ __forceinline__ int first(int piece, int half, int lane) const {
-        return piece < 0 ? (half ? vocab : lane * 8) : head + piece * kPiece + half * kHalf + lane * 8;
+    int vocab, head;                        // head: logits before the first aligned one
+    // eight logits of a lane from logit `at` + 8 lane on; -inf from `end` on
+    __device__ __forceinline__ void load(float (&f)[8], int at, int end, int lane) const {
+        const int i = at + 8 * lane;
+        if (at >= head && at + kEight <= end) {
+            if constexpr (sizeof(T) == 4) load8_wide(f, x + i);
+            else load8(f, x + i);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) f[k] = i + k < end ? to_f32(x[i + k]) : -INFINITY;
+        }
     }
-    // -inf beyond the end; piece -1: the head
-    __device__ __forceinline__ void load_any(float (&f)[8], int piece, int half, int lane) const {
-        const int i = first(piece, half, lane), end = piece < 0 ? head : vocab;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) f[k] = i + k < end ? to_f32(x[i + k]) : -INFINITY;
-    }
-    // A lane copies its own sixteen logits and reads them itself, so nothing but the copy is waited for.
-    __device__ __forceinline__ void copy(uint4* slot, int piece, int lane) const {
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int k = 0; k < (int)sizeof(T) / 2; ++k)
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;"
-                             ::"r"((unsigned)__cvta_generic_to_shared(slot + (h * (int)sizeof(T) / 2 + k) * 32 + lane)),
-                               "l"(x + first(piece, h, lane) + 4 * k) : "memory");
-    }
-    __device__ __forceinline__ void read(FwdPiece<T>& p, const uint4* slot, int lane) const {
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int k = 0; k < (int)sizeof(T) / 2; ++k) p.q[h][k] = slot[(h * (int)sizeof(T) / 2 + k) * 32 + lane];
-    }
-    __device__ __forceinline__ bool full(int piece) const { return piece >= 0 && head + (piece + 1) * kPiece <= vocab; }
 };
 
 // A warp's running sums, in units of log2: with c = log2(e) inverse_temperature and the rounded R = c max,
@@ -220,24 +201,25 @@ struct FwdAcc {
         take_top(f, -INFINITY);
         if (wide) add_below<true, true>(f, c); else add_below<true, false>(f, c);
     }
-    // a full piece; `again` gives half of it a second time
+    // a full piece; `again` gives eight of its logits a second time
     template <typename T, typename Again>
-    __device__ __forceinline__ void add(const FwdPiece<T>& p, float top, float c, float lowest, Again again) {
+    __device__ __forceinline__ void add(const FwdPiece<T>& p, float top, float c, Again again) {
+        const float lowest = FwdPiece<T>::lowest();
         if (top > mx) move(top, c, lowest);
         if (sizeof(T) == 2 ? raise : !wide && mx > -INFINITY) {
             const bool at_top = top == mx;
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
+            for (int e = 0; e < kEights<T>; ++e) {
                 float f[8];
-                if constexpr (sizeof(T) == 2) p.widen_raised(f, h); else p.widen(f, h);
+                if constexpr (sizeof(T) == 2) p.widen_raised(f, e); else p.widen(f, e);
                 if (at_top) take_top(f, sizeof(T) == 2 ? lowest : -INFINITY);
                 add_below<sizeof(T) == 4, false>(f, c);
             }
         } else {
 #pragma unroll 1
-            for (int h = 0; h < 2; ++h) {
+            for (int e = 0; e < kEights<T>; ++e) {
                 float f[8];
-                again(f, h);
+                again(f, e);
                 add(f, top, c, lowest);
             }
         }
@@ -282,43 +264,36 @@ __device__ __forceinline__ float from_ordered(unsigned b) {
     return __uint_as_float((b & 0x80000000u) ? (b & 0x7fffffffu) : ~b);
 }
 
-// The value whose ordered bits, without GRAIN low bits that are zero in the value itself, are `k`.
-template <int GRAIN>
-__device__ __forceinline__ float from_grain(unsigned k) {
-    const unsigned b = k << GRAIN;
-    return from_ordered((b & 0x80000000u) ? b : b | ((1u << GRAIN) - 1));
-}
-
-// The k best of n segments (by maximum, then by index) into sh.picked, and a value that the k-th best
-// maximum reaches into sh.threshold; one warp.  Maxima are values of T: GRAIN low bits of them are zero.
+// The k best of n segments (by maximum, then by index) into sh.picked, and a key that the k-th best
+// maximum reaches into sh.threshold; one warp.  Maxima are values of T, in whose ordered() bits
+// the low GRAIN are all alike.
 template <int GRAIN, int WARPS>
 __device__ __forceinline__ void pick_segments(FwdShared<WARPS>& sh, int n, int k, int lane) {
-    float t = -INFINITY;
+    unsigned t = 0;
     if (n > k) {
         // largest t with at least k maxima of at least t, by bisection of its bits
-        float v[kPickRegs];
+        unsigned v[kPickRegs];
         const bool in_regs = n <= 32 * kPickRegs;
-        float top = -INFINITY;
+        unsigned top = 0;
 #pragma unroll
         for (int j = 0; j < kPickRegs; ++j) {
-            v[j] = in_regs && lane + 32 * j < n ? sh.seg[lane + 32 * j] : -INFINITY;
-            top = fmaxf(top, v[j]);
+            v[j] = in_regs && lane + 32 * j < n ? sh.seg[lane + 32 * j] : 0;
+            top = max(top, v[j]);
         }
-        unsigned lo = ordered(-INFINITY) >> GRAIN, hi = ordered(INFINITY) >> GRAIN;
+        unsigned lo = 0, hi = 0xffffffffu >> GRAIN;
         if (in_regs) {
             // the k-th largest of the lanes' maxima is reached k times: the answer is there or above
             int above = 0;
             for (int j = 0; j < 32; ++j) {
-                const float o = __shfl_sync(0xffffffffu, top, j);
+                const unsigned o = __shfl_sync(0xffffffffu, top, j);
                 above += o > top || (o == top && j < lane);
             }
-            const unsigned who = __ballot_sync(0xffffffffu, above == min(k, 32) - 1);
-            if (who) lo = max(lo, ordered(__shfl_sync(0xffffffffu, top, __ffs(who) - 1)) >> GRAIN);
-            hi = max(lo, __reduce_max_sync(0xffffffffu, ordered(top) >> GRAIN));
+            const unsigned who = __ballot_sync(0xffffffffu, above == k - 1);
+            lo = __shfl_sync(0xffffffffu, top, __ffs(who) - 1) >> GRAIN;
+            hi = max(lo, __reduce_max_sync(0xffffffffu, top) >> GRAIN);
         }
         while (lo < hi) {
-            const unsigned mid = lo + (hi - lo + 1) / 2;
-            const float at = from_grain<GRAIN>(mid);
+            const unsigned mid = lo + (hi - lo + 1) / 2, at = mid << GRAIN;
             int c = 0;
             if (in_regs) {
 #pragma unroll
@@ -330,15 +305,16 @@ __device__ __forceinline__ void pick_segments(FwdShared<WARPS>& sh, int n, int k
             if (c >= k) lo = mid; else hi = mid - 1;
             if (c == k) break;
         }
-        t = from_grain<GRAIN>(lo);
+        t = lo;
     }
-    int above = 0;                           // segments above t; those equal to t fill up in order
-    for (int j = lane; j < n; j += 32) above += sh.seg[j] > t;
+    // segments above t; those equal to t (without the low bits) fill up in order
+    int above = 0;
+    for (int j = lane; j < n; j += 32) above += (sh.seg[j] >> GRAIN) > t;
     above = __reduce_add_sync(0xffffffffu, above);
     const int equal = min(k, n) - above;
     int at = 0, taken = 0;
     for (int j0 = 0; j0 < n; j0 += 32) {
-        const float v = j0 + lane < n ? sh.seg[j0 + lane] : 0.f;
+        const unsigned v = j0 + lane < n ? sh.seg[j0 + lane] >> GRAIN : 0;
         const bool more = j0 + lane < n && v > t, same = j0 + lane < n && v == t;
         const unsigned below = (1u << lane) - 1, ms = __ballot_sync(0xffffffffu, same);
         const bool take = more || (same && taken + __popc(ms & below) < equal);
@@ -347,7 +323,7 @@ __device__ __forceinline__ void pick_segments(FwdShared<WARPS>& sh, int n, int k
         at += __popc(mt);
         taken += __popc(ms);
     }
-    if (lane == 0) { sh.n_picked = at; sh.threshold = t; }
+    if (lane == 0) { sh.n_picked = at; sh.threshold = t << GRAIN; }
 }
 
 // A warp's best k keys, the j-th in lane j.
@@ -387,7 +363,7 @@ logprob_fwd_kernel(const T* __restrict__ logits, int vocab, long long ld, const 
                    float* __restrict__ logp, float* __restrict__ entropy, float* __restrict__ lse, int top,
                    float* __restrict__ top_logp, int* __restrict__ top_ids, int per_segment, int* status) {
     __shared__ FwdShared<WARPS> sh;
-    __shared__ uint4 sh_ring[WARPS * kFwdStages<T> * kPieceQuads<T> * 32];
+    __shared__ uint4 sh_ring[WARPS * kFwdStages * kQuads * 32];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int parts = CLUSTER ? (int)cg::this_cluster().num_blocks() : 1, part = CLUSTER ? (int)cg::this_cluster().block_rank() : 0;
     const long long r = blockIdx.x / parts;
@@ -396,9 +372,10 @@ logprob_fwd_kernel(const T* __restrict__ logits, int vocab, long long ld, const 
     row.vocab = vocab;
     constexpr int ALIGN = 8 * (int)sizeof(T);
     row.head = min(vocab, (int)((-(long long)reinterpret_cast<uintptr_t>(row.x)) & (ALIGN - 1)) / (int)sizeof(T));
-    const int pieces = (vocab - row.head + kPiece - 1) / kPiece;
-    // segments: [the head if there is one,] then runs of `per_segment` pieces; blocks take equal stretches of them
-    const int heads = row.head > 0, segments = heads + (pieces + per_segment - 1) / per_segment;
+    // Segments: the pieces, `per_segment` at a time, the logits before the first and behind the last full piece
+    // included in the first and last segment; blocks take equal stretches of them.
+    const int full = (vocab - row.head) / kPiece<T>;                      // full pieces
+    const int shift = __ffs(per_segment) - 1, segments = max(1, (full + per_segment - 1) >> shift);
     const int each = (segments + parts - 1) / parts, s_lo = min(segments, part * each), s_hi = min(segments, s_lo + each);
     const float c = (float)(1.4426950408889634 * inv_temp);
     long long id = -1;
@@ -411,60 +388,60 @@ logprob_fwd_kernel(const T* __restrict__ logits, int vocab, long long ld, const 
 
     FwdAcc acc;
     bool bad = false;
-    const float lowest = FwdPiece<T>::template lowest<T>();
+    for (int s = s_lo + tid; s < s_hi; s += WARPS * 32) sh.seg[s] = 0;
+    __syncthreads();
     {
-        // The warp's full pieces: those of its segments, WARPS apart.
-        constexpr int S = kFwdStages<T>;
-        uint4* ring = sh_ring + warp * S * kPieceQuads<T> * 32;
-        const int full = (vocab - row.head) / kPiece;                    // pieces [0, full) are full
-        const int lo = max(s_lo, heads), mine = max(0, (s_hi - lo - warp + WARPS - 1) / WARPS);
-        const int shift = __ffs(per_segment) - 1;
-        int count = 0;
-        if (mine > 0) count = ((mine - 1) << shift) + min(per_segment, max(0, full - ((lo + warp + (mine - 1) * WARPS - heads) << shift)));
-        auto segment = [&](int j) { return lo + warp + (j >> shift) * WARPS; };
-        auto piece = [&](int j) { return ((segment(j) - heads) << shift) + (j & (per_segment - 1)); };
+        // This warp's full pieces, WARPS apart: it copies each to shared memory, kFwdStages ahead, and a lane
+        // copies what it reads itself, so nothing but the copy is waited for.
+        uint4* ring = sh_ring + warp * kFwdStages * kQuads * 32 + lane;
+        const unsigned ring_at = (unsigned)__cvta_generic_to_shared(ring);
+        const int p_lo = (s_lo << shift) + warp, p_hi = min(full, s_hi << shift), count = max(0, (p_hi - p_lo + WARPS - 1) / WARPS);
+        constexpr int STEP = WARPS * kPiece<T>;
+        const T* from = row.x + row.head + (long long)p_lo * kPiece<T> + 8 * lane;
         auto ahead = [&](int j) {
-            if (j < count) row.copy(ring + (j % S) * kPieceQuads<T> * 32, piece(j), lane);
+            if (j < count) {
+                const unsigned to = ring_at + (j & (kFwdStages - 1)) * (kQuads * 512);
+#pragma unroll
+                for (int k = 0; k < kQuads; ++k)
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;"
+                                 ::"r"(to + k * 512), "l"(from + (sizeof(T) == 4 ? (k >> 1) * kEight + (k & 1) * 4 : k * kEight)) : "memory");
+            }
             asm volatile("cp.async.commit_group;" ::: "memory");
+            from += STEP;
         };
 #pragma unroll
-        for (int j = 0; j < S - 1; ++j) ahead(j);
-        float best = -INFINITY;
+        for (int j = 0; j < kFwdStages; ++j) ahead(j);
 #pragma unroll 1
         for (int j = 0; j < count; ++j) {
-            ahead(j + S - 1);
-            asm volatile("cp.async.wait_group %0;" ::"n"(S - 1) : "memory");
+            asm volatile("cp.async.wait_group %0;" ::"n"(kFwdStages - 1) : "memory");
             FwdPiece<T> p;
-            row.read(p, ring + (j % S) * kPieceQuads<T> * 32, lane);
+#pragma unroll
+            for (int k = 0; k < kQuads; ++k) p.q[k] = ring[(j & (kFwdStages - 1)) * kQuads * 32 + k * 32];
             const float m = warp_max_nan(p.top());
-            best = max_nan(best, m);
-            if (((j + 1) & (per_segment - 1)) == 0 || j + 1 == count) {
-                bad |= best != best;
-                if (lane == 0) sh.seg[segment(j)] = best;
-                best = -INFINITY;
+            ahead(j + kFwdStages);                            // the quads are in registers: their place is free
+            bad |= m != m;
+            const int piece = p_lo + j * WARPS;
+            if (lane == 0) {
+                if (shift == 0) sh.seg[piece] = ordered(m);
+                else atomicMax(&sh.seg[piece >> shift], ordered(m));
             }
-            acc.add(p, m, c, lowest, [&](float(&f)[8], int h) { row.load_any(f, piece(j), h, lane); });
+            acc.add(p, m, c, [&](float(&f)[8], int e) { row.load(f, row.head + piece * kPiece<T> + e * kEight, vocab, lane); });
         }
-        // The row's ends: the logits before the first piece are a segment of the first block, those behind the
-        // last full piece join its segment or are one.
-        const int last = heads + (full >> shift);
-        const bool behind = row.head + full * kPiece < vocab && last >= lo && last < s_hi && (last - lo) % WARPS == warp;
-        const bool before = heads && s_lo == 0 && s_hi > 0 && warp == WARPS - 1;
+    }
+    __syncthreads();
+    {
+        // The row's ends, 256 logits per warp: before the first full piece (first block) and behind the last (last block).
+        const int behind = row.head + full * kPiece<T>, ends = 1 + (vocab - behind + kEight - 1) / kEight;
 #pragma unroll 1
-        for (int e = 0; e < 2; ++e) {
-            if (!(e ? behind : before)) continue;
-            float top = -INFINITY;
-#pragma unroll 1
-            for (int h = 0; h < 2; ++h) {
-                float f[8];
-                row.load_any(f, e ? full : -1, h, lane);
-                const float m = warp_max_nan(max8(f));
-                top = max_nan(top, m);
-                acc.add(f, m, c, lowest);
-            }
-            bad |= top != top;
-            __syncwarp();
-            if (lane == 0) sh.seg[e ? last : 0] = e && (full & (per_segment - 1)) ? max_nan(sh.seg[last], top) : top;
+        for (int e = warp; e < ends; e += WARPS) {
+            const int s = e == 0 ? 0 : segments - 1;
+            if (s < s_lo || s >= s_hi || (e == 0 && row.head == 0)) continue;
+            float f[8];
+            row.load(f, e == 0 ? 0 : behind + (e - 1) * kEight, e == 0 ? row.head : vocab, lane);
+            const float m = warp_max_nan(max8(f));
+            bad |= m != m;
+            if (lane == 0) atomicMax(&sh.seg[s], ordered(m));
+            acc.add(f, m, c, FwdPiece<T>::lowest());
         }
     }
     {
@@ -515,28 +492,26 @@ logprob_fwd_kernel(const T* __restrict__ logits, int vocab, long long ld, const 
         constexpr int GRAIN = sizeof(T) == 4 ? 0 : std::is_same_v<T, __half> ? 13 : 16;
         if (warp == 0) pick_segments<GRAIN, WARPS>(sh, segments, top, lane);
         __syncthreads();
-        const float t = sh.threshold;
+        const unsigned t = max(sh.threshold, ordered(-INFINITY) + 1);
         BestList list;
         const int picked = sh.n_picked;
         for (int j = warp; j < picked; j += WARPS) {
             const int s = sh.picked[j];
             if (s < s_lo || s >= s_hi) continue;
-            const int p0 = s < heads ? -1 : (s - heads) * per_segment, p1 = s < heads ? 0 : min(pieces, p0 + per_segment);
+            const int from = s == 0 ? -1 : 0, end = s == segments - 1 ? vocab : row.head + ((s + 1) << shift) * kPiece<T>;
+            const int base = row.head + (s << shift) * kPiece<T>;
 #pragma unroll 1
-            for (int ph = 2 * p0; ph < 2 * p1; ++ph) {        // halves of pieces
-                const int p = ph >> 1, h = ph & 1;
+            for (int e = from; e < 0 || base + e * kEight < end; ++e) {
                 float f[8];
-                const int i = row.first(p, h, lane);
-                if (row.full(p)) {
-                    if constexpr (sizeof(T) == 4) load8_wide(f, row.x + i);
-                    else load8(f, row.x + i);
-                } else {
-                    row.load_any(f, p, h, lane);
-                }
-                if (!__any_sync(0xffffffffu, max8(f) >= t)) continue;
+                const int at = e < 0 ? 0 : base + e * kEight;
+                row.load(f, at, e < 0 ? row.head : end, lane);
+                unsigned key[8], best = 0;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) best = max(best, key[k] = ordered(f[k]));
+                if (!__any_sync(0xffffffffu, best >= t)) continue;
 #pragma unroll
                 for (int k = 0; k < 8; ++k)
-                    list.offer(f[k] >= t && f[k] > -INFINITY ? (unsigned long long)ordered(f[k]) << 32 | (0xffffffffu - (unsigned)(i + k)) : 0ull, top, lane);
+                    list.offer(key[k] >= t ? (unsigned long long)key[k] << 32 | (0xffffffffu - (unsigned)(at + 8 * lane + k)) : 0ull, top, lane);
             }
         }
         const unsigned have = __ballot_sync(0xffffffffu, lane < top && list.mine != 0);

@@ -236,27 +236,21 @@ int pb_embed_backward(const void* dev_dout, int dtype, int64_t ld_dout, const vo
         using G = decltype(g);
         using I = decltype(i);
         const SortIds<I> in{(const I*)dev_ids, vocab, padding_idx, dev_status};
-        // A list that one block sorts leaves the GPU idle meanwhile: all rows are cleared then, and those
-        // with tokens written again.  Longer lists clear only the rows without tokens, in the last launch.
-        const bool clear_now = !accumulate && e.sort.tiles == 1;
-        int clear_blocks = 0;
-        if (clear_now) {
-            e.sort.clear = (char*)dev_dtable;
-            e.sort.clear_rows = vocab;
-            e.sort.clear_bytes = dim * (int64_t)gs;
-            e.sort.clear_stride = ld_dtable * (int64_t)gs;
-            const size_t any = reinterpret_cast<size_t>(dev_dtable) | (size_t)e.sort.clear_bytes | (size_t)e.sort.clear_stride;
-            e.sort.clear_unit = any % 16 == 0 ? 16 : any % 4 == 0 ? 4 : 2;
-            const int64_t by_rows = (vocab + kSortWarps - 1) / kSortWarps;
-            clear_blocks = (int)(by_rows < 148 * 3 ? by_rows : 148 * 3);
-        }
         cudaError_t err = cudaSuccess;
         if (n_tokens) {
-            embed_sort_kernel<I><<<e.sort.tiles + clear_blocks, kSortThreads, 0, s>>>(e.sort, in);
+            embed_sort_kernel<I><<<e.sort.tiles, kSortThreads, 0, s>>>(e.sort, in);
             for (int p = 0; e.sort.tiles > 1 && p < e.sort.passes && err == cudaSuccess; ++p)
                 err = launch_after(embed_scatter_kernel<I>, dim3(e.sort.tiles), kSortThreads, s, e.sort, in, p);
         }
-        const int64_t blocks = e.red.red_blocks + (accumulate || clear_now ? 0 : (vocab + kZeroRows - 1) / kZeroRows);
+        // A list that one block sorts leaves the GPU to the clearing, which goes by the ids then.
+        if (e.sort.tiles == 1) {
+            e.red.ids = dev_ids;
+            e.red.id_bytes = id_bytes;
+            e.red.padding = padding_idx < 0 ? -2 : padding_idx;
+        }
+        const int64_t rows = (int64_t)131072 / ((int64_t)gs * dim);          // some 128 KB of the table per block
+        e.red.clear_rows = (int)(rows < 32 ? 32 : rows > kZeroRows ? kZeroRows : rows);
+        const int64_t blocks = e.red.red_blocks + (accumulate ? 0 : (vocab + e.red.clear_rows - 1) / e.red.clear_rows);
         const dim3 grid((unsigned)blocks, (unsigned)e.slabs);
         const T* x = (const T*)dev_dout;
         G* d = (G*)dev_dtable;

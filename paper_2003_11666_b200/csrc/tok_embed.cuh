@@ -77,10 +77,6 @@ struct SortPlan {
     int* hist;                             // [passes][tiles][1 << bits]
     unsigned* zero;                        // words to clear for the reduction's counters
     int n_zero;
-    // rows to clear beside the sort (a list that fits one block leaves the other SMs idle)
-    char* clear;
-    long long clear_rows, clear_bytes, clear_stride;
-    int clear_unit;
 };
 
 struct SortShared {
@@ -189,7 +185,7 @@ __device__ __forceinline__ void sort_small(const SortPlan& a, const SortIds<I>& 
 }
 
 // First launch: the digit counts of the first pass, and the memory that later launches count in.
-// A list that fits one block is sorted here, while the other blocks clear the table's gradient.
+// A list that fits one block is sorted here altogether.
 template <typename I>
 __global__ void __launch_bounds__(kSortThreads)
 embed_sort_kernel(const __grid_constant__ SortPlan a, const SortIds<I> in) {
@@ -198,16 +194,6 @@ embed_sort_kernel(const __grid_constant__ SortPlan a, const SortIds<I> in) {
     __shared__ unsigned short sh_pos[kSortSub];
     cudaTriggerProgrammaticLaunchCompletion();
     const int tid = threadIdx.x, bins = 1 << a.bits;
-    if ((int)blockIdx.x >= a.tiles) {
-        const int nz = gridDim.x - a.tiles, warp = tid >> 5, lane = tid & 31;
-        for (long long r = (long long)(blockIdx.x - a.tiles) * kSortWarps + warp; r < a.clear_rows; r += (long long)nz * kSortWarps) {
-            char* row = a.clear + r * a.clear_stride;
-            if (a.clear_unit == 16) for (long long c = lane * 16; c < a.clear_bytes; c += 512) *reinterpret_cast<uint4*>(row + c) = make_uint4(0, 0, 0, 0);
-            else if (a.clear_unit == 4) for (long long c = lane * 4; c < a.clear_bytes; c += 128) *reinterpret_cast<unsigned*>(row + c) = 0;
-            else for (long long c = lane * 2; c < a.clear_bytes; c += 64) *reinterpret_cast<unsigned short*>(row + c) = 0;
-        }
-        return;
-    }
     for (int k = blockIdx.x * kSortThreads + tid; k < a.n_zero; k += a.tiles * kSortThreads) a.zero[k] = 0;
     if (a.tiles == 1 && a.n <= kSortSub) {
         sort_small(a, in, sh, sh_key, sh_pos);
@@ -291,7 +277,7 @@ constexpr int kRedThreads = 256;
 constexpr int kRedCols = 8;                // columns of a thread
 constexpr int kRedEntries = 2048;          // entries of a block's stretches, held in shared memory
 constexpr int kRedGroup = 32;              // stretches whose partial rows are joined first
-constexpr int kZeroRows = 32;              // table rows of a clearing block
+constexpr int kZeroRows = 1024;            // most table rows of a clearing block
 
 struct RedPlan {
     const unsigned *key, *pos;             // sorted
@@ -299,7 +285,13 @@ struct RedPlan {
     float scale;
     int len;                               // entries of a stretch, a multiple of 8
     int stretches, lanes;                  // lanes: threads across a row's columns (a power of two)
-    int red_blocks;                        // blocks [0, red_blocks) reduce, the rest clear rows
+    int red_blocks;                        // blocks [0, red_blocks) reduce, the rest clear `clear_rows` rows each
+    int clear_rows;
+    // Short lists: the ids themselves.  Clearing blocks look through them for their rows' tokens and so need not
+    // wait for the sort, which one block does meanwhile.
+    const void* ids;
+    int id_bytes;
+    long long padding;
     float* part;                           // [stretches][2][dim]: runs that came in from before, runs that go on
     unsigned* arrived;                     // [slabs][stretches][3]
     int accumulate;
@@ -457,14 +449,24 @@ __global__ void __launch_bounds__(kRedThreads, !VEC ? 2 : sizeof(T) == 4 ? 3 : 4
 embed_reduce_kernel(const __grid_constant__ RedPlan a, const T* __restrict__ dout, G* __restrict__ dtable) {
     __shared__ unsigned sh_key[kRedEntries + 2], sh_pos[kRedEntries];
     __shared__ int sh_last[kRedThreads][2];
-    __shared__ int sh_touched[kZeroRows];
-    cudaGridDependencySynchronize();
+    __shared__ unsigned sh_touched[kZeroRows / 32];
     const int tid = threadIdx.x;
     if ((int)blockIdx.x >= a.red_blocks) {                   // clear the rows that no token points to
         if (blockIdx.y) return;
-        const long long v0 = (long long)(blockIdx.x - a.red_blocks) * kZeroRows;
+        const long long v0 = (long long)(blockIdx.x - a.red_blocks) * a.clear_rows, v1 = min(a.vocab, v0 + a.clear_rows);
         const int warp = tid >> 5, lane = tid & 31;
-        if (warp == 0) {
+        for (int k = tid; k < kZeroRows / 32; k += kRedThreads) sh_touched[k] = 0;
+        __syncthreads();
+        auto touch = [&](long long v) {
+            if (v >= v0 && v < v1) atomicOr(&sh_touched[(v - v0) >> 5], 1u << ((v - v0) & 31));
+        };
+        if (a.ids) {
+            for (long long t = tid; t < a.n; t += kRedThreads) {
+                const long long id = a.id_bytes == 4 ? (long long)reinterpret_cast<const int*>(a.ids)[t] : reinterpret_cast<const long long*>(a.ids)[t];
+                if (id != a.padding) touch(id);
+            }
+        } else {
+            cudaGridDependencySynchronize();
             // 32-way search for the first entry of these rows, then a walk over theirs
             long long lo = 0, hi = a.n;                      // the answer is in [lo, hi]
             while (hi - lo > 32) {
@@ -474,24 +476,23 @@ embed_reduce_kernel(const __grid_constant__ RedPlan a, const T* __restrict__ dou
                 if (c < 32) hi = lo + step * (c + 1) - 1;
                 lo += step * c;
             }
-            sh_touched[lane] = 0;
-            __syncwarp();
-            for (long long e = lo; e < a.n; e += 32) {
+            for (long long e = lo + warp * 32; e < a.n; e += kRedThreads) {
                 const unsigned k = e + lane < a.n ? a.key[e + lane] : 0xffffffffu;
-                if (k >= (unsigned)v0 && k < (unsigned)v0 + kZeroRows) sh_touched[k - (unsigned)v0] = 1;
-                if (__any_sync(0xffffffffu, k >= (unsigned)v0 + kZeroRows)) break;
+                if (k < a.vocab) touch(k);
+                if (__any_sync(0xffffffffu, (long long)k >= v1)) break;
             }
         }
         __syncthreads();
         float z[kRedCols] = {};
-        for (int r = warp; r < kZeroRows && v0 + r < a.vocab; r += kRedThreads / 32) {
-            if (sh_touched[r]) continue;
-            G* row = dtable + (v0 + r) * a.ld;
+        for (long long v = v0 + warp; v < v1; v += kRedThreads / 32) {
+            if (sh_touched[(v - v0) >> 5] >> ((v - v0) & 31) & 1) continue;
+            G* row = dtable + v * a.ld;
             for (long long c = 0; c < a.dim; c += 32 * kRedCols)
                 store_cols<VEC>(row, z, Cols<VEC>{c + lane * (VEC ? 4 : 1), 32, a.dim});
         }
         return;
     }
+    cudaGridDependencySynchronize();
     const int group = tid / a.lanes, lane = tid % a.lanes, per_block = kRedThreads / a.lanes;
     const int st = blockIdx.x * per_block + group;           // this group's stretch
     const long long slab = (long long)blockIdx.y * a.lanes * kRedCols;

@@ -1,6 +1,3 @@
-#ifndef FLB
-#define FLB 4
-#endif
 // Log probabilities of given tokens, entropy and top alternatives of rows of logits, and the
 // gradient of the three row values.
 //
@@ -235,26 +232,6 @@ struct FwdAcc {
     }
 };
 
-__device__ __forceinline__ FwdStats join(const FwdStats* p, int n, float c) {
-    FwdStats t{0, 0, 0, -INFINITY, 0};
-    for (int k = 0; k < n; ++k) { t.mx = fmaxf(t.mx, p[k].mx); t.bad |= p[k].bad; }
-    if (t.mx == -INFINITY) return t;
-    for (int k = 0; k < n; ++k) {
-        if (p[k].mx == -INFINITY) continue;
-        if (p[k].mx == t.mx) {
-            t.count += p[k].count;
-            t.rest += p[k].rest;
-            t.moment += p[k].moment;
-        } else {
-            const float shift = fmaxf((p[k].mx - t.mx) * c, -1e30f);         // finite: times a sum that it makes zero
-            const double s = exp2_near(shift), all = p[k].rest + p[k].count;
-            t.rest += s * all;
-            t.moment += s * (p[k].moment + all * shift);
-        }
-    }
-    return t;
-}
-
 // Floats in the order of their values as unsigned numbers, and back.
 __device__ __forceinline__ unsigned ordered(float x) {
     const unsigned b = __float_as_uint(x + 0.f);              // -0 counts as 0
@@ -262,6 +239,29 @@ __device__ __forceinline__ unsigned ordered(float x) {
 }
 __device__ __forceinline__ float from_ordered(unsigned b) {
     return __uint_as_float((b & 0x80000000u) ? (b & 0x7fffffffu) : ~b);
+}
+
+__device__ __forceinline__ double warp_total(double x) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+    return x;
+}
+// Sums of the lanes' parts, relative to the largest maximum; the same in every lane.
+__device__ __forceinline__ FwdStats join(FwdStats p, float c) {
+    FwdStats t;
+    t.bad = __any_sync(0xffffffffu, p.bad);
+    t.mx = from_ordered(__reduce_max_sync(0xffffffffu, ordered(p.mx)));
+    if (p.mx != t.mx || p.mx == -INFINITY) {
+        const float shift = fmaxf((p.mx - t.mx) * c, -1e30f);         // finite: times a sum that it makes zero
+        const double s = p.mx == -INFINITY ? 0.0 : exp2_near(shift), all = p.rest + p.count;
+        p.rest = s * all;
+        p.moment = s == 0.0 ? 0.0 : s * (p.moment + all * shift);
+        p.count = 0;
+    }
+    t.count = warp_total(p.count);
+    t.rest = warp_total(p.rest);
+    t.moment = warp_total(p.moment);
+    return t;
 }
 
 // The k best of n segments (by maximum, then by index) into sh.picked, and a key that the k-th best
@@ -295,7 +295,10 @@ __device__ __forceinline__ void pick_segments(FwdShared<WARPS>& sh, int n, int k
         while (lo < hi) {
             const unsigned mid = lo + (hi - lo + 1) / 2, at = mid << GRAIN;
             int c = 0;
-            if (in_regs) {
+            if (n <= 128) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) c += v[j] >= at;
+            } else if (in_regs) {
 #pragma unroll
                 for (int j = 0; j < kPickRegs; ++j) c += v[j] >= at;
             } else {
@@ -358,7 +361,7 @@ __device__ __forceinline__ void rank_keys(unsigned long long* best, const unsign
 }
 
 template <typename T, typename I, int WARPS, bool CLUSTER>
-__global__ void __launch_bounds__(WARPS * 32, WARPS == kFwdWarps ? FLB : 4 * FLB)
+__global__ void __launch_bounds__(WARPS * 32, WARPS == kFwdWarps ? 4 : 16)
 logprob_fwd_kernel(const T* __restrict__ logits, int vocab, long long ld, const I* __restrict__ tokens, double inv_temp,
                    float* __restrict__ logp, float* __restrict__ entropy, float* __restrict__ lse, int top,
                    float* __restrict__ top_logp, int* __restrict__ top_ids, int per_segment, int* status) {
@@ -378,12 +381,6 @@ logprob_fwd_kernel(const T* __restrict__ logits, int vocab, long long ld, const 
     const int shift = __ffs(per_segment) - 1, segments = max(1, (full + per_segment - 1) >> shift);
     const int each = (segments + parts - 1) / parts, s_lo = min(segments, part * each), s_hi = min(segments, s_lo + each);
     const float c = (float)(1.4426950408889634 * inv_temp);
-    long long id = -1;
-    float x_token = 0.f;
-    if (part == 0 && tid == 32 && logp) {
-        id = token_id(tokens, r, vocab, status);
-        if (id >= 0) x_token = to_f32(row.x[id]);
-    }
     if (tid == 0) sh.n_keys = sh.n_gathered = 0;
 
     FwdAcc acc;
@@ -460,7 +457,10 @@ logprob_fwd_kernel(const T* __restrict__ logits, int vocab, long long ld, const 
     FwdShared<WARPS>* first = &sh;
     if constexpr (CLUSTER) {
         cg::cluster_group cluster = cg::this_cluster();
-        if (tid == 0) sh.block = join(sh.warp_stats, WARPS, c);
+        if (warp == 0) {
+            const FwdStats all = join(lane < WARPS ? sh.warp_stats[lane] : FwdStats{0, 0, 0, -INFINITY, 0}, c);
+            if (lane == 0) sh.block = all;
+        }
         cluster.sync();
         first = cluster.map_shared_rank(&sh, 0);
         if (top > 0) {                                        // every block picks from the whole row's segments
@@ -471,22 +471,26 @@ logprob_fwd_kernel(const T* __restrict__ logits, int vocab, long long ld, const 
             __syncthreads();
         }
     }
-    if (part == 0 && tid == 32) {                             // the row's values, beside the pick
-        FwdStats all;
+    if (part == 0 && warp == 1) {                             // the row's values, beside the pick
+        FwdStats mine{0, 0, 0, -INFINITY, 0};
         if constexpr (CLUSTER) {
-            FwdStats of[kMaxCluster];
-            for (int k = 0; k < parts; ++k) of[k] = cg::this_cluster().map_shared_rank(&sh, k)->block;
-            all = join(of, parts, c);
+            if (lane < parts) mine = cg::this_cluster().map_shared_rank(&sh, lane)->block;
         } else {
-            all = join(sh.warp_stats, WARPS, c);
+            if (lane < WARPS) mine = sh.warp_stats[lane];
         }
+        const FwdStats all = join(mine, c);
         const bool empty = all.mx == -INFINITY && !all.bad;
         const double log_z = all.bad ? __longlong_as_double(0x7ff8000000000000ll) : empty ? 0.0 : log(all.count) + log1p(all.rest / all.count);
-        if (logp) logp[r] = id < 0 ? 0.f : empty ? -INFINITY : (float)(((double)x_token - all.mx) * inv_temp - log_z);
-        if (entropy) entropy[r] = empty ? 0.f : (float)(log_z - 0.6931471805599453 * all.moment / (all.count + all.rest));
-        if (lse) lse[r] = empty ? -INFINITY : (float)((double)all.mx * inv_temp + log_z);
-        sh.log_z = log_z;
-        sh.row = all;
+        if (lane == 0) {
+            // the token's logit, in L2 by now
+            const long long id = logp ? token_id(tokens, r, vocab, status) : -1;
+            const float x_token = id >= 0 ? to_f32(row.x[id]) : 0.f;
+            if (logp) logp[r] = id < 0 ? 0.f : empty ? -INFINITY : (float)(((double)x_token - all.mx) * inv_temp - log_z);
+            if (entropy) entropy[r] = empty ? 0.f : (float)(log_z - 0.6931471805599453 * all.moment / (all.count + all.rest));
+            if (lse) lse[r] = empty ? -INFINITY : (float)((double)all.mx * inv_temp + log_z);
+            sh.log_z = log_z;
+            sh.row = all;
+        }
     }
     if (top > 0) {
         constexpr int GRAIN = sizeof(T) == 4 ? 0 : std::is_same_v<T, __half> ? 13 : 16;
@@ -501,17 +505,29 @@ logprob_fwd_kernel(const T* __restrict__ logits, int vocab, long long ld, const 
             const int from = s == 0 ? -1 : 0, end = s == segments - 1 ? vocab : row.head + ((s + 1) << shift) * kPiece<T>;
             const int base = row.head + (s << shift) * kPiece<T>;
 #pragma unroll 1
-            for (int e = from; e < 0 || base + e * kEight < end; ++e) {
-                float f[8];
-                const int at = e < 0 ? 0 : base + e * kEight;
-                row.load(f, at, e < 0 ? row.head : end, lane);
-                unsigned key[8], best = 0;
+            for (int e0 = from; e0 < 0 || base + e0 * kEight < end; e0 += kEights<T>) {
+                // loads that do not wait for each other find where there are candidates at all ...
+                unsigned hits = 0;
+                float f[kEights<T>][8];
 #pragma unroll
-                for (int k = 0; k < 8; ++k) best = max(best, key[k] = ordered(f[k]));
-                if (!__any_sync(0xffffffffu, best >= t)) continue;
+                for (int u = 0; u < kEights<T>; ++u) {
+                    const int e = e0 + u, at = e < 0 ? 0 : base + e * kEight;
+                    row.load(f[u], at, e < 0 ? row.head : end, lane);
+                }
 #pragma unroll
-                for (int k = 0; k < 8; ++k)
-                    list.offer(key[k] >= t ? (unsigned long long)key[k] << 32 | (0xffffffffu - (unsigned)(at + 8 * lane + k)) : 0ull, top, lane);
+                for (int u = 0; u < kEights<T>; ++u) hits |= (unsigned)__any_sync(0xffffffffu, ordered(max8(f[u])) >= t) << u;
+                // ... and those, by now near, are read once more
+                while (hits) {
+                    const int e = e0 + __ffs(hits) - 1, at = e < 0 ? 0 : base + e * kEight;
+                    hits &= hits - 1;
+                    float g[8];
+                    row.load(g, at, e < 0 ? row.head : end, lane);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        const unsigned key = ordered(g[k]);
+                        list.offer(key >= t ? (unsigned long long)key << 32 | (0xffffffffu - (unsigned)(at + 8 * lane + k)) : 0ull, top, lane);
+                    }
+                }
             }
         }
         const unsigned have = __ballot_sync(0xffffffffu, lane < top && list.mine != 0);

@@ -13,6 +13,7 @@ import torch
 from .binding import PBError, load_library, pb_adamw_args, pb_adamw_tensor
 
 _DTYPE = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+_ID_BYTES = {torch.int64: 8, torch.int32: 4}
 _ARG = -1
 
 
@@ -20,35 +21,41 @@ def _refuse(who, text):
     raise PBError(_ARG, "%s: %s" % (who, text))
 
 
+_lib = load_library()
+
+
 def _check(rc):
     if rc != 0:
-        raise PBError(rc, load_library().pb_last_error(None).decode())
+        raise PBError(rc, _lib.pb_last_error(None).decode())
+
+
+_OFF_DEVICE = "every tensor must be a CUDA tensor on the current device"
 
 
 def _on_device(who, device, *tensors):
     """Every tensor given lives on `device`, the current one."""
     for t in tensors:
         if t is not None and t.get_device() != device:
-            _refuse(who, "every tensor must be a CUDA tensor on the current device")
+            _refuse(who, _OFF_DEVICE)
 
 
 def _device(who, t):
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
-        _refuse(who, "every tensor must be a CUDA tensor on the current device")
-    d = t.get_device()
-    if d != torch.cuda.current_device():
-        _refuse(who, "every tensor must be a CUDA tensor on the current device")
+    d = t.get_device() if isinstance(t, torch.Tensor) else -1
+    if d < 0 or d != torch.cuda.current_device():
+        _refuse(who, _OFF_DEVICE)
     return d
 
 
-def _rows(who, name, t, dtypes=_DTYPE):
+def _rows(who, name, t):
     """(rows, columns, row stride) of a matrix whose rows are dense."""
-    if t.dim() != 2 or t.dtype not in dtypes:
+    shape = t.shape
+    if len(shape) != 2 or t.dtype not in _DTYPE:
         _refuse(who, "%s must be a matrix of float32, bfloat16 or float16" % name)
-    rows, cols = t.shape
-    if cols > 1 and t.stride(1) != 1:
+    rows, cols = shape
+    stride, step = t.stride()
+    if step != 1 and cols > 1:
         _refuse(who, "%s must have dense rows" % name)
-    return rows, cols, t.stride(0) if rows > 1 else cols
+    return rows, cols, stride if rows > 1 else cols
 
 
 def _vector(who, name, t, n, dtype=torch.float32):
@@ -60,19 +67,14 @@ def _vector(who, name, t, n, dtype=torch.float32):
 
 
 def _ids(who, name, t):
-    if t.dtype is torch.int64:
-        size = 8
-    elif t.dtype is torch.int32:
-        size = 4
-    else:
-        _refuse(who, "%s must be int32 or int64" % name)
-    if not t.is_contiguous():
-        _refuse(who, "%s must be dense" % name)
+    size = _ID_BYTES.get(t.dtype)
+    if size is None or not t.is_contiguous():
+        _refuse(who, "%s must be a dense int32 or int64 tensor" % name)
     return t.data_ptr(), size
 
 
 def _status(who, t):
-    return _vector(who, "status", t, 1, torch.int32)
+    return None if t is None else _vector(who, "status", t, 1, torch.int32)
 
 
 def embed_forward(table, ids, out, scale=1.0, status=None, stream=0):
@@ -85,13 +87,13 @@ def embed_forward(table, ids, out, scale=1.0, status=None, stream=0):
     rows, cols, ld_out = _rows(who, "out", out)
     if rows != ids.numel() or cols != dim or out.dtype is not table.dtype:
         _refuse(who, "out must be [number of ids, dim] of the table's type")
-    _check(load_library().pb_embed_forward(table.data_ptr(), _DTYPE[table.dtype], vocab, dim, ld, p, size, rows, scale,
+    _check(_lib.pb_embed_forward(table.data_ptr(), _DTYPE[table.dtype], vocab, dim, ld, p, size, rows, scale,
                                            out.data_ptr(), ld_out, _status(who, status), stream))
 
 
 def embed_scratch_bytes(n_tokens, vocab, dim):
     """pb_embed_scratch_bytes: bytes of scratch that embed_backward needs for these sizes."""
-    n = load_library().pb_embed_scratch_bytes(int(n_tokens), int(vocab), int(dim))
+    n = _lib.pb_embed_scratch_bytes(int(n_tokens), int(vocab), int(dim))
     if n == 0:
         _refuse("embed_scratch_bytes", "sizes out of range")
     return n
@@ -110,7 +112,7 @@ def embed_backward(dout, ids, dtable, scratch, scale=1.0, padding_idx=-1, accumu
         _refuse(who, "dout must be [number of ids, dim]")
     if scratch.dtype is not torch.uint8 or not scratch.is_contiguous():
         _refuse(who, "scratch must be a dense uint8 tensor")
-    _check(load_library().pb_embed_backward(dout.data_ptr(), _DTYPE[dout.dtype], ld_dout, p, size, rows, vocab, dim, scale,
+    _check(_lib.pb_embed_backward(dout.data_ptr(), _DTYPE[dout.dtype], ld_dout, p, size, rows, vocab, dim, scale,
                                             padding_idx, dtable.data_ptr(), _DTYPE[dtable.dtype], ld, 1 if accumulate else 0,
                                             scratch.data_ptr(), scratch.numel(), _status(who, status), stream))
 
@@ -136,7 +138,7 @@ def logprob_forward(logits, tokens=None, logp=None, entropy=None, lse=None, top_
         if top_ids.dim() != 2 or top_ids.shape[0] != rows:
             _refuse(who, "top_ids must be [rows, top_k]")
         k = top_ids.shape[1]
-    _check(load_library().pb_logprob_forward(
+    _check(_lib.pb_logprob_forward(
         logits.data_ptr(), _DTYPE[logits.dtype], rows, vocab, ld, p, size, inv_temperature, _vector(who, "logp", logp, rows),
         _vector(who, "entropy", entropy, rows), _vector(who, "lse", lse, rows), k, _vector(who, "top_logp", top_logp, rows * k),
         _vector(who, "top_ids", top_ids, rows * k, torch.int32), _status(who, status), stream))
@@ -157,7 +159,7 @@ def logprob_backward(logits, tokens, lse, dlogits, g_logp=None, g_entropy=None, 
         p, size = _ids(who, "tokens", tokens)
         if tokens.numel() != rows:
             _refuse(who, "tokens must hold one id per row")
-    _check(load_library().pb_logprob_backward(
+    _check(_lib.pb_logprob_backward(
         logits.data_ptr(), _DTYPE[logits.dtype], rows, vocab, ld, p, size, inv_temperature, _vector(who, "lse", lse, rows),
         _vector(who, "entropy", entropy, rows), _vector(who, "g_logp", g_logp, rows), _vector(who, "g_entropy", g_entropy, rows),
         _vector(who, "g_lse", g_lse, rows), dlogits.data_ptr(), ld_d, _status(who, status), stream))
@@ -170,7 +172,7 @@ def adamw_moments(m, m_scale, v, v_scale, m_out=None, v_out=None, stream=0):
     _on_device(who, d, m_scale, v, v_scale, m_out, v_out)
     n = m.numel()
     blocks = -(-n // 256)
-    _check(load_library().pb_adamw_moments(
+    _check(_lib.pb_adamw_moments(
         _vector(who, "m", m, n, torch.uint8), _vector(who, "m_scale", m_scale, blocks), _vector(who, "v", v, n, torch.uint8),
         _vector(who, "v_scale", v_scale, blocks), n, _vector(who, "m_out", m_out, n), _vector(who, "v_out", v_out, n), stream))
 
@@ -244,4 +246,4 @@ class AdamW:
         args = pb_adamw_args(lr, beta1, beta2, eps, step, seed & 0xFFFFFFFFFFFFFFFF, _vector(who, "grad_scale", grad_scale, 1),
                              _vector(who, "dev_lr", dev_lr, 1), _vector(who, "dev_step", dev_step, 1, torch.int64), _DTYPE[dtype],
                              self._forward, self._bits)
-        _check(load_library().pb_adamw_step(self._table, self._grads, n, C.byref(args), stream))
+        _check(_lib.pb_adamw_step(self._table, self._grads, n, C.byref(args), stream))

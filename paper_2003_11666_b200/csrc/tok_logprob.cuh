@@ -49,7 +49,8 @@ struct FwdShared {
     unsigned long long keys[WARPS * kMaxTop], gathered[WARPS == kFwdWarps ? kMaxCluster * kMaxTop : 1], best[kMaxTop];
     FwdStats warp_stats[WARPS], block, row;
     int picked[kMaxTop];
-    unsigned threshold;
+    unsigned lane_top[WARPS * 32];          // every thread's own largest logit
+    unsigned threshold, lane_threshold;
     int n_picked, n_keys, n_gathered;
     double log_z;
 };
@@ -264,52 +265,57 @@ __device__ __forceinline__ FwdStats join(FwdStats p, float c) {
     return t;
 }
 
+// Largest t such that at least k of n > k keys, without their low GRAIN bits, reach it; one warp.  By bisection,
+// from the k-th largest of the lanes' largest keys up, if every lane has REGS keys at most.
+template <int GRAIN, int REGS>
+__device__ __forceinline__ unsigned kth_largest(const unsigned* key, int n, int k, int lane) {
+    unsigned v[REGS];
+    const bool in_regs = n <= 32 * REGS;
+    unsigned top = 0;
+#pragma unroll
+    for (int j = 0; j < REGS; ++j) {
+        v[j] = in_regs && lane + 32 * j < n ? key[lane + 32 * j] : 0;
+        top = max(top, v[j]);
+    }
+    unsigned lo = 0, hi = 0xffffffffu >> GRAIN;
+    if (in_regs) {
+        int above = 0;
+#pragma unroll 8
+        for (int j = 0; j < 32; ++j) {
+            const unsigned o = __shfl_sync(0xffffffffu, top, j);
+            above += o > top || (o == top && j < lane);
+        }
+        const unsigned who = __ballot_sync(0xffffffffu, above == k - 1);
+        lo = __shfl_sync(0xffffffffu, top, __ffs(who) - 1) >> GRAIN;
+        hi = max(lo, __reduce_max_sync(0xffffffffu, top) >> GRAIN);
+    }
+    while (lo < hi) {
+        const unsigned mid = lo + (hi - lo + 1) / 2, at = mid << GRAIN;
+        int c = 0;
+        if (in_regs) {
+#pragma unroll
+            for (int j = 0; j < REGS; ++j) c += v[j] >= at;
+        } else {
+            for (int j = lane; j < n; j += 32) c += key[j] >= at;
+        }
+        c = __reduce_add_sync(0xffffffffu, c);
+        if (c >= k) lo = mid; else hi = mid - 1;
+        if (c == k) break;
+    }
+    return lo;
+}
+
 // The k best of n segments (by maximum, then by index) into sh.picked, and a key that the k-th best
 // maximum reaches into sh.threshold; one warp.  Maxima are values of T, in whose ordered() bits
 // the low GRAIN are all alike.
 template <int GRAIN, int WARPS>
 __device__ __forceinline__ void pick_segments(FwdShared<WARPS>& sh, int n, int k, int lane) {
-    unsigned t = 0;
-    if (n > k) {
-        // largest t with at least k maxima of at least t, by bisection of its bits
-        unsigned v[kPickRegs];
-        const bool in_regs = n <= 32 * kPickRegs;
-        unsigned top = 0;
-#pragma unroll
-        for (int j = 0; j < kPickRegs; ++j) {
-            v[j] = in_regs && lane + 32 * j < n ? sh.seg[lane + 32 * j] : 0;
-            top = max(top, v[j]);
-        }
-        unsigned lo = 0, hi = 0xffffffffu >> GRAIN;
-        if (in_regs) {
-            // the k-th largest of the lanes' maxima is reached k times: the answer is there or above
-            int above = 0;
-            for (int j = 0; j < 32; ++j) {
-                const unsigned o = __shfl_sync(0xffffffffu, top, j);
-                above += o > top || (o == top && j < lane);
-            }
-            const unsigned who = __ballot_sync(0xffffffffu, above == k - 1);
-            lo = __shfl_sync(0xffffffffu, top, __ffs(who) - 1) >> GRAIN;
-            hi = max(lo, __reduce_max_sync(0xffffffffu, top) >> GRAIN);
-        }
-        while (lo < hi) {
-            const unsigned mid = lo + (hi - lo + 1) / 2, at = mid << GRAIN;
-            int c = 0;
-            if (n <= 128) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) c += v[j] >= at;
-            } else if (in_regs) {
-#pragma unroll
-                for (int j = 0; j < kPickRegs; ++j) c += v[j] >= at;
-            } else {
-                for (int j = lane; j < n; j += 32) c += sh.seg[j] >= at;
-            }
-            c = __reduce_add_sync(0xffffffffu, c);
-            if (c >= k) lo = mid; else hi = mid - 1;
-            if (c == k) break;
-        }
-        t = lo;
+    if (n <= k) {
+        if (lane < n) sh.picked[lane] = lane;
+        if (lane == 0) { sh.n_picked = n; sh.threshold = 0; }
+        return;
     }
+    const unsigned t = n <= 128 ? kth_largest<GRAIN, 4>(sh.seg, n, k, lane) : kth_largest<GRAIN, kPickRegs>(sh.seg, n, k, lane);
     // segments above t; those equal to t (without the low bits) fill up in order
     int above = 0;
     for (int j = lane; j < n; j += 32) above += (sh.seg[j] >> GRAIN) > t;
@@ -384,6 +390,7 @@ logprob_fwd_kernel(const T* __restrict__ logits, int vocab, long long ld, const 
     if (tid == 0) sh.n_keys = sh.n_gathered = 0;
 
     FwdAcc acc;
+    float lane_top = -INFINITY;
     bool bad = false;
     for (int s = s_lo + tid; s < s_hi; s += WARPS * 32) sh.seg[s] = 0;
     __syncthreads();
@@ -394,14 +401,15 @@ logprob_fwd_kernel(const T* __restrict__ logits, int vocab, long long ld, const 
         const unsigned ring_at = (unsigned)__cvta_generic_to_shared(ring);
         const int p_lo = (s_lo << shift) + warp, p_hi = min(full, s_hi << shift), count = max(0, (p_hi - p_lo + WARPS - 1) / WARPS);
         constexpr int STEP = WARPS * kPiece<T>;
-        const T* from = row.x + row.head + (long long)p_lo * kPiece<T> + 8 * lane;
+        constexpr int QUAD = 16 / (int)sizeof(T);             // a warp's quads lie side by side
+        const T* from = row.x + row.head + (long long)p_lo * kPiece<T> + QUAD * lane;
         auto ahead = [&](int j) {
             if (j < count) {
                 const unsigned to = ring_at + (j & (kFwdStages - 1)) * (kQuads * 512);
 #pragma unroll
                 for (int k = 0; k < kQuads; ++k)
                     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;"
-                                 ::"r"(to + k * 512), "l"(from + (sizeof(T) == 4 ? (k >> 1) * kEight + (k & 1) * 4 : k * kEight)) : "memory");
+                                 ::"r"(to + k * 512), "l"(from + k * 32 * QUAD) : "memory");
             }
             asm volatile("cp.async.commit_group;" ::: "memory");
             from += STEP;
@@ -414,7 +422,8 @@ logprob_fwd_kernel(const T* __restrict__ logits, int vocab, long long ld, const 
             FwdPiece<T> p;
 #pragma unroll
             for (int k = 0; k < kQuads; ++k) p.q[k] = ring[(j & (kFwdStages - 1)) * kQuads * 32 + k * 32];
-            const float m = warp_max_nan(p.top());
+            const float own = p.top(), m = warp_max_nan(own);
+            lane_top = max_nan(lane_top, own);
             ahead(j + kFwdStages);                            // the quads are in registers: their place is free
             bad |= m != m;
             const int piece = p_lo + j * WARPS;
@@ -435,12 +444,14 @@ logprob_fwd_kernel(const T* __restrict__ logits, int vocab, long long ld, const 
             if (s < s_lo || s >= s_hi || (e == 0 && row.head == 0)) continue;
             float f[8];
             row.load(f, e == 0 ? 0 : behind + (e - 1) * kEight, e == 0 ? row.head : vocab, lane);
-            const float m = warp_max_nan(max8(f));
+            const float own = max8(f), m = warp_max_nan(own);
+            lane_top = max_nan(lane_top, own);
             bad |= m != m;
             if (lane == 0) atomicMax(&sh.seg[s], ordered(m));
             acc.add(f, m, c, FwdPiece<T>::lowest());
         }
     }
+    sh.lane_top[tid] = ordered(lane_top);
     {
         float sums[2];
         acc.finish(sums);
@@ -495,48 +506,72 @@ logprob_fwd_kernel(const T* __restrict__ logits, int vocab, long long ld, const 
     if (top > 0) {
         constexpr int GRAIN = sizeof(T) == 4 ? 0 : std::is_same_v<T, __half> ? 13 : 16;
         if (warp == 0) pick_segments<GRAIN, WARPS>(sh, segments, top, lane);
+        if (warp == WARPS - 1) {                              // k threads of this block have seen a logit of at least this
+            const unsigned t = kth_largest<GRAIN, WARPS>(sh.lane_top, WARPS * 32, top, lane) << GRAIN;
+            if (lane == 0) sh.lane_threshold = t;
+        }
         __syncthreads();
-        const unsigned t = max(sh.threshold, ordered(-INFINITY) + 1);
-        BestList list;
+        const unsigned t = max(max(sh.threshold, sh.lane_threshold), ordered(-INFINITY) + 1);
         const int picked = sh.n_picked;
-        for (int j = warp; j < picked; j += WARPS) {
-            const int s = sh.picked[j];
-            if (s < s_lo || s >= s_hi) continue;
-            const int from = s == 0 ? -1 : 0, end = s == segments - 1 ? vocab : row.head + ((s + 1) << shift) * kPiece<T>;
-            const int base = row.head + (s << shift) * kPiece<T>;
-#pragma unroll 1
-            for (int e0 = from; e0 < 0 || base + e0 * kEight < end; e0 += kEights<T>) {
+        // The candidates of the picked segments, a piece (or one of the row's ends) per warp at a time.
+        auto visit = [&](auto see) {
+            for (int u = warp; u < picked * (per_segment + 2); u += WARPS) {
+                const int s = sh.picked[u / (per_segment + 2)], j = u % (per_segment + 2), piece = (s << shift) + j;
+                if (s < s_lo || s >= s_hi) continue;
+                int from = row.head + piece * kPiece<T>, end = from + kPiece<T>;
+                if (j < per_segment) {
+                    if (piece >= full) continue;
+                } else if (j == per_segment) {
+                    if (s != segments - 1) continue;
+                    from = row.head + full * kPiece<T>;
+                    end = vocab;
+                } else {
+                    if (s != 0) continue;
+                    from = 0;
+                    end = row.head;
+                }
                 // loads that do not wait for each other find where there are candidates at all ...
                 unsigned hits = 0;
                 float f[kEights<T>][8];
 #pragma unroll
-                for (int u = 0; u < kEights<T>; ++u) {
-                    const int e = e0 + u, at = e < 0 ? 0 : base + e * kEight;
-                    row.load(f[u], at, e < 0 ? row.head : end, lane);
-                }
+                for (int e = 0; e < kEights<T>; ++e) row.load(f[e], from + e * kEight, end, lane);
 #pragma unroll
-                for (int u = 0; u < kEights<T>; ++u) hits |= (unsigned)__any_sync(0xffffffffu, ordered(max8(f[u])) >= t) << u;
+                for (int e = 0; e < kEights<T>; ++e) hits |= (unsigned)__any_sync(0xffffffffu, ordered(max8(f[e])) >= t) << e;
                 // ... and those, by now near, are read once more
                 while (hits) {
-                    const int e = e0 + __ffs(hits) - 1, at = e < 0 ? 0 : base + e * kEight;
+                    const int at = from + (__ffs(hits) - 1) * kEight;
                     hits &= hits - 1;
                     float g[8];
-                    row.load(g, at, e < 0 ? row.head : end, lane);
+                    row.load(g, at, end, lane);
 #pragma unroll
                     for (int k = 0; k < 8; ++k) {
                         const unsigned key = ordered(g[k]);
-                        list.offer(key >= t ? (unsigned long long)key << 32 | (0xffffffffu - (unsigned)(at + 8 * lane + k)) : 0ull, top, lane);
+                        see(key >= t ? (unsigned long long)key << 32 | (0xffffffffu - (unsigned)(at + 8 * lane + k)) : 0ull);
                     }
                 }
             }
-        }
-        const unsigned have = __ballot_sync(0xffffffffu, lane < top && list.mine != 0);
-        int at = 0;
-        if (lane == 0 && have) at = atomicAdd(&sh.n_keys, __popc(have));
-        at = __shfl_sync(0xffffffffu, at, 0);
-        if ((have >> lane) & 1) sh.keys[at + lane] = list.mine;                // valid keys are the first lanes
+        };
+        constexpr int ROOM = WARPS * kMaxTop;
+        visit([&](unsigned long long key) {
+            if (key == 0) return;
+            const int at = atomicAdd(&sh.n_keys, 1);
+            if (at < ROOM) sh.keys[at] = key;
+        });
         __syncthreads();
-        int n = sh.n_keys;
+        int n = sh.n_keys, at = 0;
+        if (n > ROOM) {                                       // many equal logits: each warp keeps its best only
+            __syncthreads();
+            if (tid == 0) sh.n_keys = 0;
+            __syncthreads();
+            BestList list;
+            visit([&](unsigned long long key) { list.offer(key, top, lane); });
+            const unsigned have = __ballot_sync(0xffffffffu, lane < top && list.mine != 0);
+            if (lane == 0 && have) at = atomicAdd(&sh.n_keys, __popc(have));
+            at = __shfl_sync(0xffffffffu, at, 0);
+            if ((have >> lane) & 1) sh.keys[at + lane] = list.mine;            // valid keys are the first lanes
+            __syncthreads();
+            n = sh.n_keys;
+        }
         rank_keys<WARPS>(sh.best, sh.keys, n, top);
         if constexpr (CLUSTER) {
             n = min(n, top);

@@ -155,6 +155,23 @@ def test_embed_backward_of_many_tokens(n, vocab, dim, kind):
     _embed_backward(torch, p, n, vocab, dim, "float32", "float32", "int32", kind, True, pad=vocab - 1)
 
 
+@pytest.mark.parametrize("n", [50, 2048, 2049, 7000])
+@pytest.mark.parametrize("dim,ld", [(64, 64), (64, 67), (33, 40)])
+def test_embed_backward_clears_the_padding_row(n, dim, ld):
+    torch, p = _torch()
+    for kind, pad in (("frequent", 299), ("same", 150), ("uniform", 0)):
+        _embed_backward(torch, p, n, 300, dim, "bfloat16", "bfloat16", "int64", kind, False, pad=pad, ld=ld)
+
+
+@pytest.mark.parametrize("dtype,gtype", [("bfloat16", "float32"), ("float32", "float32"), ("float16", "float16")])
+def test_embed_backward_of_wide_rows_and_long_runs(dtype, gtype):
+    # runs over many stretches, in several slabs of columns
+    torch, p = _torch()
+    for kind in ("frequent", "same", "uniform"):
+        _embed_backward(torch, p, 5000, 6, 4104, dtype, gtype, "int32", kind, kind == "uniform")
+    _embed_backward(torch, p, 4500, 3, 2051, dtype, gtype, "int32", "frequent", True)
+
+
 def test_embed_backward_of_no_tokens_clears_the_table():
     torch, p = _torch()
     d = torch.ones(10, 12, device="cuda")
@@ -320,6 +337,41 @@ def test_logprob_row_counts(rows, vocab, dtype):
     for k in (0, 20):
         x, dev_tok, tok, *_ = _logprob_case(rows, vocab, dtype, "ties", 1.0, k, seed=k)
     _logprob_gradient(torch, p, x, dev_tok, tok, 1.0, dtype, False)
+
+
+def test_logprob_of_more_rows_than_a_grid_has_in_one_direction():
+    torch, p = _torch()
+    x, dev_tok, tok, *_ = _logprob_case(66000, 5, "bfloat16", "normal", 1.0, 2)
+    _logprob_gradient(torch, p, x, dev_tok, tok, 1.0, "bfloat16", False)
+
+
+@pytest.mark.parametrize("rows,vocab,dtype", [(1, 131075, "bfloat16"), (3, 40000, "float32"), (20, 50001, "float16")])
+def test_logprob_captured_and_replayed(rows, vocab, dtype):
+    # rows split over clusters, on logits that change between the replays
+    torch, p = _torch()
+    k, stream = 20, torch.cuda.Stream()
+    x = torch.randn(rows, vocab, device="cuda").to(getattr(torch, dtype))
+    tok = torch.randint(0, vocab, (rows,), device="cuda")
+    f = lambda *n: torch.empty(*n, device="cuda")                 # noqa: E731
+    out = [f(rows), f(rows), f(rows), f(rows, k), torch.empty(rows, k, dtype=torch.int32, device="cuda")]
+
+    def call(s):
+        p.logprob_forward(x, tok, out[0], entropy=out[1], lse=out[2], top_logp=out[3], top_ids=out[4], stream=s)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        call(stream.cuda_stream)
+    for _ in range(3):
+        x.copy_(torch.randn(rows, vocab, device="cuda"))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in out]
+        call(0)
+        for a, b in zip(got, out):
+            assert torch.equal(a, b)
+        order = torch.sort(x.float(), dim=1, descending=True, stable=True).indices[:, :k]
+        assert torch.equal(got[4].long(), order)
 
 
 @pytest.mark.parametrize("dtype", DTYPES)

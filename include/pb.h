@@ -333,7 +333,8 @@ int pb_embed_forward(const void* dev_table, int dtype, int64_t vocab, int64_t di
  * writes every row (zeros where no token points); accumulate = 1 adds to what is there (a
  * gradient over several batches; the gradient of a table that is also the output head) and
  * leaves rows without tokens untouched.  padding_idx: a row that gets no gradient, or -1.
- * dtable is float32 or of dout's type.  dev_scratch: pb_embed_scratch_bytes(...) bytes,
+ * dtable is float32 or of dout's type; dim is at most 2^26.  The tokens are sorted by id on
+ * the device; nothing is known of them on the host.  dev_scratch: pb_embed_scratch_bytes(...) bytes,
  * 256-byte aligned, not used by another call that may run at the same time (two captured
  * graphs included). */
 size_t pb_embed_scratch_bytes(int64_t n_tokens, int64_t vocab, int64_t dim);
@@ -349,6 +350,7 @@ int pb_embed_backward(const void* dev_dout, int dtype, int64_t ld_dout, const vo
  *   lse[r] = log sum exp(inv_temperature * logits[r, :]),
  *   top_ids / top_logp [rows, top_k]: the top_k largest logits in descending order, the
  *   lower index first among equal ones, and their log probabilities (top_k <= 32).
+ * vocab is at most 2^30.
  * dev_logp and dev_tokens are given together or not at all; entropy and lse may be NULL.
  * Logits of -inf are tokens that cannot occur.  Places of the alternatives beyond the last
  * finite logit hold -1 and -inf.  A row whose logits are all -inf has lse and logp -inf,
@@ -384,10 +386,12 @@ int pb_logprob_backward(const void* dev_logits, int dtype, int64_t rows, int64_t
  * scales are a fresh state.  m is held as e4m3, sqrt(v) as an unsigned float of 4 exponent and 4
  * mantissa bits, rounded at random by `seed`, the step number, the tensor's place in the list
  * and the element: the same call gives the same result.  A block of 256 with a moment that is
- * not finite reads back as NaN.
+ * not finite reads back as NaN.  A block of m whose largest magnitude is below 2^-100 is
+ * held as zeros.  In u, a v below 2^-126 counts as zero.
  * *dev_grad_scale (device, NULL: 1) is the product of whatever clipping and loss scaling leave;
  * if it is not finite the step changes nothing.  dev_lr and dev_step (device, may be NULL) take
- * the place of lr and step, so that a captured graph can be replayed with other values.  Tensors
+ * the place of lr and step (*dev_step at least 1), so that a captured graph can be replayed
+ * with other values.  grads[k] is tensor k's gradient, read where it lies at the call.  Tensors
  * of a call must not overlap (not checked here). */
 typedef struct {
     float* w;

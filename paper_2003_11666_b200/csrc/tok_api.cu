@@ -57,6 +57,26 @@ cudaError_t launch_after(void (*kernel)(P...), dim3 grid, int threads, cudaStrea
     return cudaLaunchKernelEx(&c, kernel, P(args)...);
 }
 
+// Launch of `blocks` blocks in clusters of `size`.
+template <typename... P, typename... A>
+cudaError_t launch_cluster(void (*kernel)(P...), int size, int64_t blocks, int threads, cudaStream_t stream, A... args) {
+    if (size > 8) {                                         // more than the portable size: has to be asked for
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+        if (e != cudaSuccess) return e;
+    }
+    cudaLaunchConfig_t c{};
+    c.gridDim = dim3((unsigned)blocks);
+    c.blockDim = dim3((unsigned)threads);
+    c.stream = stream;
+    cudaLaunchAttribute attr{};
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = (unsigned)size;
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    c.attrs = &attr;
+    c.numAttrs = 1;
+    return cudaLaunchKernelEx(&c, kernel, P(args)...);
+}
+
 // Sizes and scratch layout of the embedding gradient.
 constexpr int64_t kMaxEmbedDim = 1 << 26, kMaxLogprobVocab = 1 << 30;
 // Blocks per SM that the reduction's stretches are cut for; four are resident.  More and shorter
@@ -238,6 +258,8 @@ int pb_embed_backward(const void* dev_dout, int dtype, int64_t ld_dout, const vo
         const SortIds<I> in{(const I*)dev_ids, vocab, padding_idx, dev_status};
         cudaError_t err = cudaSuccess;
         if (n_tokens) {
+            // One block up to 2048 tokens; else a launch for the first counts and one for each digit (65536 tokens: some
+            // 28 us of launches of 32 blocks; a single launch of a 16-block cluster took 40).
             embed_sort_kernel<I><<<e.sort.tiles, kSortThreads, 0, s>>>(e.sort, in);
             for (int p = 0; e.sort.tiles > 1 && p < e.sort.passes && err == cudaSuccess; ++p)
                 err = launch_after(embed_scatter_kernel<I>, dim3(e.sort.tiles), kSortThreads, s, e.sort, in, p);
@@ -300,21 +322,8 @@ int pb_logprob_forward(const void* dev_logits, int dtype, int64_t rows, int64_t 
                                                                                   top_k, dev_top_logp, dev_top_ids, per_segment, dev_status);
             return launched("pb_logprob_forward");
         }
-        auto kernel = logprob_fwd_kernel<T, I, kFwdWarps, true>;
-        cudaError_t e = parts > 8 ? cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) : cudaSuccess;
-        cudaLaunchConfig_t cfg{};
-        cfg.gridDim = dim3((unsigned)(rows * parts));
-        cfg.blockDim = dim3(kFwdWarps * 32);
-        cfg.stream = s;
-        cudaLaunchAttribute attr{};
-        attr.id = cudaLaunchAttributeClusterDimension;
-        attr.val.clusterDim.x = (unsigned)parts;
-        attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-        cfg.attrs = &attr;
-        cfg.numAttrs = 1;
-        if (e == cudaSuccess)
-            e = cudaLaunchKernelEx(&cfg, kernel, x, (int)vocab, (long long)ld, tok, inv_temperature, dev_logp, dev_entropy, dev_lse, top_k, dev_top_logp,
-                                   (int*)dev_top_ids, per_segment, (int*)dev_status);
+        const cudaError_t e = launch_cluster(logprob_fwd_kernel<T, I, kFwdWarps, true>, parts, rows * parts, kFwdWarps * 32, s, x, (int)vocab, (long long)ld, tok,
+                                             inv_temperature, dev_logp, dev_entropy, dev_lse, top_k, dev_top_logp, dev_top_ids, per_segment, dev_status);
         const int rc = launched("pb_logprob_forward");
         return rc != PB_OK || e == cudaSuccess ? rc : fail_text(PB_E_CUDA, cudaGetErrorString(e));
     };

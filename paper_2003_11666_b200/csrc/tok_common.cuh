@@ -17,7 +17,7 @@ template <> __device__ __forceinline__ float from_f32<float>(float x) { return x
 template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
 template <> __device__ __forceinline__ __half from_f32<__half>(float x) { return __float2half_rn(x); }
 
-// Eight consecutive elements, 16-byte aligned.
+// Eight consecutive 16-bit elements, 16-byte aligned.
 __device__ __forceinline__ void unpack8(float (&x)[8], const uint4& q, __nv_bfloat16) {
     const unsigned w[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
@@ -35,10 +35,6 @@ __device__ __forceinline__ void unpack8(float (&x)[8], const uint4& q, __half) {
         x[2 * k + 1] = f.y;
     }
 }
-__device__ __forceinline__ void load8(float (&x)[8], const float* p) {
-    const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
-    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
-}
 template <typename T> __device__ __forceinline__ void load8(float (&x)[8], const T* p) {
     unpack8(x, *reinterpret_cast<const uint4*>(p), T());
 }
@@ -50,15 +46,11 @@ __device__ __forceinline__ unsigned pack2(float a, float b, __half) {
     const __half2 h = __floats2half2_rn(a, b);
     return *reinterpret_cast<const unsigned*>(&h);
 }
-__device__ __forceinline__ void store8(float* p, const float (&x)[8]) {
-    reinterpret_cast<float4*>(p)[0] = make_float4(x[0], x[1], x[2], x[3]);
-    reinterpret_cast<float4*>(p)[1] = make_float4(x[4], x[5], x[6], x[7]);
-}
 template <typename T> __device__ __forceinline__ void store8(T* p, const float (&x)[8]) {
     *reinterpret_cast<uint4*>(p) = make_uint4(pack2(x[0], x[1], T()), pack2(x[2], x[3], T()), pack2(x[4], x[5], T()), pack2(x[6], x[7], T()));
 }
 
-// The same from 32-byte aligned memory in one access.
+// Eight consecutive floats, 32-byte aligned, in one access.
 __device__ __forceinline__ void load8_wide(float (&x)[8], const float* p) {
     asm volatile("ld.global.v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
                  : "=f"(x[0]), "=f"(x[1]), "=f"(x[2]), "=f"(x[3]), "=f"(x[4]), "=f"(x[5]), "=f"(x[6]), "=f"(x[7]) : "l"(p));
@@ -101,12 +93,6 @@ struct Pair {
 __device__ __forceinline__ Pair operator*(Pair a, Pair b) { Pair r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.x) : "l"(a.x), "l"(b.x)); return r; }
 __device__ __forceinline__ Pair operator+(Pair a, Pair b) { Pair r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.x) : "l"(a.x), "l"(b.x)); return r; }
 __device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) { Pair r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.x) : "l"(a.x), "l"(b.x), "l"(c.x)); return r; }
-__device__ __forceinline__ float warp_max_f(float x) {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, o));
-    return x;
-}
-
 // SplitMix64 finaliser (Steele, Lea & Flood 2014) of a counter on a stream that starts at `base`.
 __host__ __device__ __forceinline__ unsigned long long splitmix64(unsigned long long base, unsigned long long counter) {
     unsigned long long z = base + (counter + 1ull) * 0x9E3779B97F4A7C15ull;

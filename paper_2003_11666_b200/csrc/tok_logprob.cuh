@@ -27,6 +27,11 @@ constexpr int kMaxTop = 32;
 // then by index, lie in the k best segments by the same order, for each better segment holds a better
 // element.  So at most 32 segments are read again, from L2.
 // A few rows are split over a cluster of blocks, joined through distributed shared memory.
+//
+// Bound by memory traffic for long rows: 4096 x 100003 bf16 take 139 us without alternatives (5.9 TB/s of 6.6)
+// and 171 us with 8; per logit it issues some 9 instructions and one exponential, which four blocks per SM
+// overlap with the copies (register double-buffering instead of copies to shared memory: 200 us).  Short
+// batches are bound by latency: one row of 131072 takes 4.8 us, 9.1 us with 20 alternatives.
 constexpr int kFwdWarps = 8, kFwdFewWarps = 2;   // warps of a block; few for rows of a few pieces
 constexpr int kEight = 256;                 // logits of a warp, eight per lane
 constexpr int kQuads = 4;                   // 16-byte quads of a lane in a piece
@@ -57,7 +62,7 @@ struct FwdShared {
 
 __device__ __forceinline__ float warp_max_nan(float x) {
     float r;
-    asm("redux.sync.max.NaN.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(x));
+    asm volatile("redux.sync.max.NaN.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(x));
     return r;
 }
 __device__ __forceinline__ float max3(float a, float b, float c) {

@@ -182,7 +182,8 @@ class AdamW:
 
     w: float32 weights.  m, v: float32 states, or uint8 ones with m_scale / v_scale (float32, one per 256 elements).
     w_forward: copies of the weights in the forward's type, predicted `horizon` steps ahead, or None.  weight_decay and
-    horizon are numbers or one number per tensor.  All tensors are dense, of the caller's, and must not overlap.
+    horizon are numbers or one number per tensor.  All tensors are dense, of the caller's, and must not overlap.  One
+    thread at a time steps an object.
     """
 
     def __init__(self, w, m, v, m_scale=None, v_scale=None, w_forward=None, weight_decay=0.0, horizon=0.0):
@@ -202,6 +203,8 @@ class AdamW:
         self._n = [t.numel() for t in lists[0]]
         self._table = (pb_adamw_tensor * n)()
         self._grads = (C.c_void_p * n)()
+        self._args = pb_adamw_args(forward_dtype=self._forward, state_bits=self._bits)
+        self._args_ref = C.byref(self._args)
         state = torch.uint8 if self._bits == 8 else torch.float32
         spans = []
         for k in range(n):
@@ -243,7 +246,9 @@ class AdamW:
             _refuse(who, "gradients must be float32, bfloat16 or float16")
         _on_device(who, device, grad_scale, dev_lr, dev_step)
         self._grads[:] = ptr
-        args = pb_adamw_args(lr, beta1, beta2, eps, step, seed & 0xFFFFFFFFFFFFFFFF, _vector(who, "grad_scale", grad_scale, 1),
-                             _vector(who, "dev_lr", dev_lr, 1), _vector(who, "dev_step", dev_step, 1, torch.int64), _DTYPE[dtype],
-                             self._forward, self._bits)
-        _check(_lib.pb_adamw_step(self._table, self._grads, n, C.byref(args), stream))
+        a = self._args
+        a.lr, a.beta1, a.beta2, a.eps, a.step, a.seed, a.grad_dtype = lr, beta1, beta2, eps, step, seed & 0xFFFFFFFFFFFFFFFF, _DTYPE[dtype]
+        a.dev_grad_scale = None if grad_scale is None else _vector(who, "grad_scale", grad_scale, 1)
+        a.dev_lr = None if dev_lr is None else _vector(who, "dev_lr", dev_lr, 1)
+        a.dev_step = None if dev_step is None else _vector(who, "dev_step", dev_step, 1, torch.int64)
+        _check(_lib.pb_adamw_step(self._table, self._grads, n, self._args_ref, stream))

@@ -1,4 +1,4 @@
-"""Token operators for the CPU checker (test infrastructure; float64): embedding lookup and
+"""Token operators for the CPU oracle (test infrastructure; float64): embedding lookup and
 its gradient, log probabilities of given tokens with entropy and alternatives and their
 gradient, and the AdamW step.
 

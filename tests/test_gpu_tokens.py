@@ -1,4 +1,4 @@
-"""Token operators and the AdamW step on the GPU against the float64 checker.
+"""Token operators and the AdamW step on the GPU against the float64 oracle.
 
 Tolerances: a value rounded to a type is off by at most half a step, eps_t / 2 of itself
 (2^-24 float32, 2^-8 bfloat16, 2^-11 float16; float16 also half of its smallest step, 2^-25);

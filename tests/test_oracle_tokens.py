@@ -1,4 +1,4 @@
-"""The checker's token operators against torch CPU autograd, torch's AdamW and central differences."""
+"""The oracle's token operators against torch CPU autograd, torch's AdamW and central differences."""
 import numpy as np
 import pytest
 import torch

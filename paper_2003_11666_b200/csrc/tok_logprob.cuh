@@ -28,10 +28,10 @@ constexpr int kMaxTop = 32;
 // element.  So at most 32 segments are read again, from L2.
 // A few rows are split over a cluster of blocks, joined through distributed shared memory.
 //
-// Bound by memory traffic for long rows: 4096 x 100003 bf16 take 139 us without alternatives (5.9 TB/s of 6.6)
-// and 171 us with 8; per logit it issues some 9 instructions and one exponential, which four blocks per SM
+// Bound by memory traffic for long rows: 4096 x 100003 bf16 take 137 us without alternatives (6.0 TB/s of 6.6)
+// and 166 us with 8; per logit it issues some 9 instructions and one exponential, which four blocks per SM
 // overlap with the copies (register double-buffering instead of copies to shared memory: 200 us).  Short
-// batches are bound by latency: one row of 131072 takes 4.8 us, 9.1 us with 20 alternatives.
+// batches are bound by latency: one row of 131072 takes 4.6 us, 8.8 us with 20 alternatives.
 constexpr int kFwdWarps = 8, kFwdFewWarps = 2;   // warps of a block; few for rows of a few pieces
 constexpr int kEight = 256;                 // logits of a warp, eight per lane
 constexpr int kQuads = 4;                   // 16-byte quads of a lane in a piece
@@ -421,27 +421,8 @@ logprob_fwd_kernel(const T* __restrict__ logits, int vocab, long long ld, const 
         };
 #pragma unroll
         for (int j = 0; j < kFwdStages; ++j) ahead(j);
-#pragma unroll 1
-        for (int j = 0; j < count; ++j) {
-            asm volatile("cp.async.wait_group %0;" ::"n"(kFwdStages - 1) : "memory");
-            FwdPiece<T> p;
-#pragma unroll
-            for (int k = 0; k < kQuads; ++k) p.q[k] = ring[(j & (kFwdStages - 1)) * kQuads * 32 + k * 32];
-            const float own = p.top(), m = warp_max_nan(own);
-            lane_top = max_nan(lane_top, own);
-            ahead(j + kFwdStages);                            // the quads are in registers: their place is free
-            bad |= m != m;
-            const int piece = p_lo + j * WARPS;
-            if (lane == 0) {
-                if (shift == 0) sh.seg[piece] = ordered(m);
-                else atomicMax(&sh.seg[piece >> shift], ordered(m));
-            }
-            acc.add(p, m, c, [&](float(&f)[8], int e) { row.load(f, row.head + piece * kPiece<T> + e * kEight, vocab, lane); });
-        }
-    }
-    __syncthreads();
-    {
-        // The row's ends, 256 logits per warp: before the first full piece (first block) and behind the last (last block).
+        // The row's ends, 256 logits per warp, while the first pieces are on their way: before the first full piece (first
+        // block) and behind the last (last block).
         const int behind = row.head + full * kPiece<T>, ends = 1 + (vocab - behind + kEight - 1) / kEight;
 #pragma unroll 1
         for (int e = warp; e < ends; e += WARPS) {
@@ -454,6 +435,20 @@ logprob_fwd_kernel(const T* __restrict__ logits, int vocab, long long ld, const 
             bad |= m != m;
             if (lane == 0) atomicMax(&sh.seg[s], ordered(m));
             acc.add(f, m, c, FwdPiece<T>::lowest());
+        }
+#pragma unroll 1
+        for (int j = 0; j < count; ++j) {
+            asm volatile("cp.async.wait_group %0;" ::"n"(kFwdStages - 1) : "memory");
+            FwdPiece<T> p;
+#pragma unroll
+            for (int k = 0; k < kQuads; ++k) p.q[k] = ring[(j & (kFwdStages - 1)) * kQuads * 32 + k * 32];
+            const float own = p.top(), m = warp_max_nan(own);
+            lane_top = max_nan(lane_top, own);
+            ahead(j + kFwdStages);                            // the quads are in registers: their place is free
+            bad |= m != m;
+            const int piece = p_lo + j * WARPS;
+            if (lane == 0) atomicMax(&sh.seg[piece >> shift], ordered(m));
+            acc.add(p, m, c, [&](float(&f)[8], int e) { row.load(f, row.head + piece * kPiece<T> + e * kEight, vocab, lane); });
         }
     }
     sh.lane_top[tid] = ordered(lane_top);
@@ -511,7 +506,7 @@ logprob_fwd_kernel(const T* __restrict__ logits, int vocab, long long ld, const 
     if (top > 0) {
         constexpr int GRAIN = sizeof(T) == 4 ? 0 : std::is_same_v<T, __half> ? 13 : 16;
         if (warp == 0) pick_segments<GRAIN, WARPS>(sh, segments, top, lane);
-        if (warp == WARPS - 1) {                              // k threads of this block have seen a logit of at least this
+        if (warp == (WARPS > 2 ? WARPS - 1 : 0)) {            // k threads of this block have seen a logit of at least this
             const unsigned t = kth_largest<GRAIN, WARPS>(sh.lane_top, WARPS * 32, top, lane) << GRAIN;
             if (lane == 0) sh.lane_threshold = t;
         }

@@ -98,9 +98,10 @@ EmbedPlan embed_plan(int64_t n, int64_t vocab, int64_t dim, char* scratch) {
     s.n = (int)n;
     s.passes = (len + kSortMaxBits - 1) / kSortMaxBits;
     s.bits = (len + s.passes - 1) / s.passes;
-    s.tile_shift = 11;                                       // kSortSub tokens a block; longer lists: several sub-tiles
+    s.tile_shift = 10;                                       // kSortSub tokens a block; longer lists: several sub-tiles
+    static_assert(kSortSub == 1 << 10, "tokens of a block");
     while (((n - 1) >> s.tile_shift) >= kSortMaxTiles) ++s.tile_shift;
-    s.tiles = n ? (int)(((n - 1) >> s.tile_shift) + 1) : 0;
+    s.tiles = n <= kSortSmall ? n > 0 : (int)(((n - 1) >> s.tile_shift) + 1);
     RedPlan& r = e.red;
     r.n = n; r.vocab = vocab; r.dim = dim;
     r.lanes = 1;
@@ -119,16 +120,12 @@ EmbedPlan embed_plan(int64_t n, int64_t vocab, int64_t dim, char* scratch) {
         at += (bytes + 255) / 256 * 256;
         return p;
     };
-    for (int k = 0; k < 2; ++k) {
-        s.key[k] = (unsigned*)take((size_t)n * 4);
-        s.pos[k] = (unsigned*)take((size_t)n * 4);
-    }
+    for (int k = 0; k < 2; ++k) s.list[k] = (uint2*)take((size_t)n * 8);
     s.hist = (int*)take(s.tiles > 1 ? ((size_t)s.passes * s.tiles << s.bits) * 4 : 0);
     s.n_zero = (int)((int64_t)e.slabs * r.stretches * 3);
     s.zero = r.arrived = (unsigned*)take((size_t)s.n_zero * 4);
     r.part = (float*)take((size_t)r.stretches * 2 * dim * 4);
-    r.key = s.key[(s.passes - 1) & 1];
-    r.pos = s.pos[(s.passes - 1) & 1];
+    r.list = s.list[(s.passes - 1) & 1];
     e.bytes = at > 256 ? at : 256;
     return e;
 }
@@ -259,7 +256,7 @@ int pb_embed_backward(const void* dev_dout, int dtype, int64_t ld_dout, const vo
         cudaError_t err = cudaSuccess;
         if (n_tokens) {
             // One block up to 2048 tokens; else a launch for the first counts and one for each digit (65536 tokens: some
-            // 28 us of launches of 32 blocks; a single launch of a 16-block cluster took 40).
+            // 28 us, with 64 blocks of 1024 tokens as with 32 of 2048; a single launch of a 16-block cluster took 40).
             embed_sort_kernel<I><<<e.sort.tiles, kSortThreads, 0, s>>>(e.sort, in);
             for (int p = 0; e.sort.tiles > 1 && p < e.sort.passes && err == cudaSuccess; ++p)
                 err = launch_after(embed_scatter_kernel<I>, dim3(e.sort.tiles), kSortThreads, s, e.sort, in, p);

@@ -66,14 +66,15 @@ embed_fwd_kernel(const T* __restrict__ table, long long vocab, long long dim, lo
 
 // ---------------------------------------------------------------- sort
 constexpr int kSortThreads = 512, kSortWarps = kSortThreads / 32;
-constexpr int kSortSub = 2048;             // tokens a block ranks at a time: 128 consecutive ones per warp
+constexpr int kSortSmall = 4 * kSortThreads;       // tokens that one block sorts altogether
+constexpr int kSortSub = 2 * kSortThreads;         // tokens that a block of many places at a time
 constexpr int kSortMaxBits = 9;            // digit bits of a pass: one bin per thread
 constexpr int kSortMaxTiles = 256;         // blocks; longer lists give each block several sub-tiles
 
 struct SortPlan {
     int passes, bits, tiles, n;
     int tile_shift;                        // tokens per block: kSortSub times a power of two
-    unsigned *key[2], *pos[2];             // ping-pong
+    uint2* list[2];                        // (key, position), ping-pong
     int* hist;                             // [passes][tiles][1 << bits]
     unsigned* zero;                        // words to clear for the reduction's counters
     int n_zero;
@@ -117,14 +118,15 @@ struct SortIds {
     }
 };
 
-// Place of each of the 4 x 512 tokens among those of its digit.  Warp w holds 128 consecutive
+// Place of each of the N x 512 tokens among those of its digit.  Warp w holds 32 N consecutive
 // tokens, 32 at a time; `digit` is -1 where there is none.  Leaves each warp's counts in sh.warp.
-__device__ __forceinline__ void rank_digits(const int (&digit)[4], int (&rank)[4], int bins, SortShared& sh) {
+template <int N>
+__device__ __forceinline__ void rank_digits(const int (&digit)[N], int (&rank)[N], int bins, SortShared& sh) {
     const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
     for (int b = lane; b < bins; b += 32) sh.warp[w][b] = 0;
     __syncwarp();
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
+    for (int q = 0; q < N; ++q) {
         const unsigned peers = __match_any_sync(0xffffffffu, digit[q]);
         const int before = __popc(peers & ((1u << lane) - 1));
         int had = 0;
@@ -149,7 +151,7 @@ __device__ __forceinline__ int place_warps(int bin, int at, SortShared& sh) {
     return at - first;
 }
 
-// A list of at most kSortSub tokens: all passes in one block, the list in shared memory.
+// A list of at most kSortSmall tokens: all passes in one block, the list in shared memory.
 template <typename I>
 __device__ __forceinline__ void sort_small(const SortPlan& a, const SortIds<I>& in, SortShared& sh, unsigned* sh_key, unsigned short* sh_pos) {
     const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5, bins = 1 << a.bits;
@@ -177,7 +179,7 @@ __device__ __forceinline__ void sort_small(const SortPlan& a, const SortIds<I>& 
         for (int q = 0; q < 4; ++q) {
             if (digit[q] < 0) continue;
             const int d = sh.base[digit[q]] + sh.warp[w][digit[q]] + rank[q];
-            if (last) { a.key[p & 1][d] = key[q]; a.pos[p & 1][d] = pos[q]; }
+            if (last) a.list[p & 1][d] = make_uint2(key[q], pos[q]);
             else { sh_key[d] = key[q]; sh_pos[d] = (unsigned short)pos[q]; }
         }
         __syncthreads();
@@ -190,12 +192,12 @@ template <typename I>
 __global__ void __launch_bounds__(kSortThreads)
 embed_sort_kernel(const __grid_constant__ SortPlan a, const SortIds<I> in) {
     __shared__ SortShared sh;
-    __shared__ unsigned sh_key[kSortSub];
-    __shared__ unsigned short sh_pos[kSortSub];
+    __shared__ unsigned sh_key[kSortSmall];
+    __shared__ unsigned short sh_pos[kSortSmall];
     cudaTriggerProgrammaticLaunchCompletion();
     const int tid = threadIdx.x, bins = 1 << a.bits;
     for (int k = blockIdx.x * kSortThreads + tid; k < a.n_zero; k += a.tiles * kSortThreads) a.zero[k] = 0;
-    if (a.tiles == 1 && a.n <= kSortSub) {
+    if (a.tiles == 1) {
         sort_small(a, in, sh, sh_key, sh_pos);
         return;
     }
@@ -234,34 +236,31 @@ embed_scatter_kernel(const __grid_constant__ SortPlan a, const SortIds<I> in, in
     __syncthreads();
     scan_bins(sh, bins);
     int place = tid < bins ? sh.base[tid] + before : 0;    // first free place of this thread's digit
-    const unsigned* ik = a.key[(p + 1) & 1];
-    const unsigned* ip = a.pos[(p + 1) & 1];
-    unsigned* ok = a.key[p & 1];
-    unsigned* op = a.pos[p & 1];
+    const uint2* from = a.list[(p + 1) & 1];
+    uint2* to = a.list[p & 1];
+    constexpr int N = kSortSub / kSortThreads;
     int* next = p + 1 < a.passes ? a.hist + (size_t)(p + 1) * a.tiles * bins : nullptr;
     const long long lo = (long long)blockIdx.x << a.tile_shift, hi = min((long long)a.n, lo + (1ll << a.tile_shift));
     for (long long s0 = lo; s0 < hi; s0 += kSortSub) {
-        unsigned key[4], pos[4];
-        int digit[4], rank[4];
+        uint2 token[N];
+        int digit[N], rank[N];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const long long t = s0 + w * 128 + q * 32 + lane;
+        for (int q = 0; q < N; ++q) {
+            const long long t = s0 + w * (32 * N) + q * 32 + lane;
             const bool live = t < hi;
-            key[q] = !live ? 0u : p == 0 ? in.key(t) : ik[t];
-            pos[q] = !live ? 0u : p == 0 ? (unsigned)t : ip[t];
-            digit[q] = live ? (int)((key[q] >> shift) & (bins - 1)) : -1;
+            token[q] = !live ? make_uint2(0, 0) : p == 0 ? make_uint2(in.key(t), (unsigned)t) : from[t];
+            digit[q] = live ? (int)((token[q].x >> shift) & (bins - 1)) : -1;
         }
         rank_digits(digit, rank, bins, sh);
         if (tid < bins) place += place_warps(tid, place, sh);
         __syncthreads();
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
+        for (int q = 0; q < N; ++q) {
             int bin = -1;
             if (digit[q] >= 0) {
                 const int d = sh.warp[w][digit[q]] + rank[q];
-                ok[d] = key[q];
-                op[d] = pos[q];
-                if (next) bin = (d >> a.tile_shift) * bins + (int)((key[q] >> (shift + a.bits)) & (bins - 1));
+                to[d] = token[q];
+                if (next) bin = (d >> a.tile_shift) * bins + (int)((token[q].x >> (shift + a.bits)) & (bins - 1));
             }
             if (next) {                                    // one addition per warp and bin: frequent ids meet here
                 const unsigned peers = __match_any_sync(0xffffffffu, bin);
@@ -280,7 +279,7 @@ constexpr int kRedGroup = 32;              // stretches whose partial rows are j
 constexpr int kZeroRows = 1024;            // most table rows of a clearing block
 
 struct RedPlan {
-    const unsigned *key, *pos;             // sorted
+    const uint2* list;                     // sorted (key, position)
     long long n, vocab, dim, ld_dout, ld;
     float scale;
     int len;                               // entries of a stretch, a multiple of 8
@@ -369,7 +368,7 @@ __device__ __forceinline__ void store_cols(T* row, const float (&x)[kRedCols], c
 // First and last stretch of the run of v that passes through stretch st.  Most runs reach one stretch
 // further, so the distance is doubled before it is halved.
 __device__ __forceinline__ int first_stretch(const RedPlan& a, int st, unsigned v) {
-    auto reaches = [&](int t) { return t >= 0 && a.key[(long long)t * a.len + a.len - 1] == v; };    // t is before st: a full stretch
+    auto reaches = [&](int t) { return t >= 0 && a.list[(long long)t * a.len + a.len - 1].x == v; };    // t is before st: a full stretch
     int in = st, step = 1;                                   // the run is known to be in `in`
     while (reaches(in - step)) { in -= step; step *= 2; }
     int out = max(in - step, -1);                            // and known not to be in `out`
@@ -380,7 +379,7 @@ __device__ __forceinline__ int first_stretch(const RedPlan& a, int st, unsigned 
     return in;
 }
 __device__ __forceinline__ int last_stretch(const RedPlan& a, int st, unsigned v) {
-    auto reaches = [&](int t) { return t < a.stretches && a.key[(long long)t * a.len] == v; };
+    auto reaches = [&](int t) { return t < a.stretches && a.list[(long long)t * a.len].x == v; };
     int in = st, step = 1;
     while (reaches(in + step)) { in += step; step *= 2; }
     int out = min(in + step, a.stretches);
@@ -471,13 +470,13 @@ embed_reduce_kernel(const __grid_constant__ RedPlan a, const T* __restrict__ dou
             long long lo = 0, hi = a.n;                      // the answer is in [lo, hi]
             while (hi - lo > 32) {
                 const long long step = (hi - lo) / 32, at = lo + step * (lane + 1) - 1;
-                const unsigned below = __ballot_sync(0xffffffffu, a.key[at] < (unsigned)v0);
+                const unsigned below = __ballot_sync(0xffffffffu, a.list[at].x < (unsigned)v0);
                 const int c = __popc(below);                 // the keys are sorted: the first c probes are below
                 if (c < 32) hi = lo + step * (c + 1) - 1;
                 lo += step * c;
             }
             for (long long e = lo + warp * 32; e < a.n; e += kRedThreads) {
-                const unsigned k = e + lane < a.n ? a.key[e + lane] : 0xffffffffu;
+                const unsigned k = e + lane < a.n ? a.list[e + lane].x : 0xffffffffu;
                 if (k < a.vocab) touch(k);
                 if (__any_sync(0xffffffffu, (long long)k >= v1)) break;
             }
@@ -501,8 +500,9 @@ embed_reduce_kernel(const __grid_constant__ RedPlan a, const T* __restrict__ dou
         const long long b0 = (long long)blockIdx.x * per_block * a.len;
         for (int k = tid; k < per_block * a.len + 2; k += kRedThreads) {
             const long long e = b0 + k - 1;
-            sh_key[k] = e >= 0 && e < a.n ? a.key[e] : 0xffffffffu;
-            if (k > 0 && e < a.n) sh_pos[k - 1] = a.pos[e];  // the last one is not used
+            const uint2 token = e >= 0 && e < a.n ? a.list[e] : make_uint2(0xffffffffu, 0);
+            sh_key[k] = token.x;
+            if (k > 0 && k <= per_block * a.len) sh_pos[k - 1] = token.y;
         }
     }
     __syncthreads();

@@ -12,6 +12,7 @@
 #include <type_traits>
 
 #include "tok_common.cuh"
+#include "tok_select.h"
 
 namespace pb {
 
@@ -294,8 +295,8 @@ __device__ __forceinline__ unsigned kth_largest(const unsigned* key, int n, int 
         lo = __shfl_sync(0xffffffffu, top, __ffs(who) - 1) >> GRAIN;
         hi = max(lo, __reduce_max_sync(0xffffffffu, top) >> GRAIN);
     }
-    while (lo < hi) {
-        const unsigned mid = lo + (hi - lo + 1) / 2, at = mid << GRAIN;
+    return highest_reached(lo, hi, k, [&](unsigned t) {
+        const unsigned at = t << GRAIN;
         int c = 0;
         if (in_regs) {
 #pragma unroll
@@ -303,11 +304,8 @@ __device__ __forceinline__ unsigned kth_largest(const unsigned* key, int n, int 
         } else {
             for (int j = lane; j < n; j += 32) c += key[j] >= at;
         }
-        c = __reduce_add_sync(0xffffffffu, c);
-        if (c >= k) lo = mid; else hi = mid - 1;
-        if (c == k) break;
-    }
-    return lo;
+        return (int)__reduce_add_sync(0xffffffffu, c);
+    });
 }
 
 // The k best of n segments (by maximum, then by index) into sh.picked, and a key that the k-th best

@@ -142,16 +142,20 @@ struct FwdRow {
 // A warp's running sums, in units of log2: with c = log2(e) inverse_temperature and the rounded R = c max,
 // y = fma(x, c, -R) takes one instruction for two logits, and the rounding of R, known exactly as
 // delta = c max - R, is put right when the sums are used.  Sums: rest of 2^y, moment of 2^y y, over the logits
-// below the maximum; those equal to it are counted.
+// below the maximum; those equal to it are counted.  delta is half a step of R at most, and 2^delta a factor of
+// the sums: beyond |R| = kFarRef (masks of -1e10, a very low temperature) y = (x - max) c takes its place, which
+// has no delta and rounds twice.
+constexpr float kFarRef = 0x1p20f;          // delta is 2^-5 at most below it; past 2^31 2^delta would overflow
+
 struct FwdAcc {
     float mx = -INFINITY, ref = 0.f, delta = 0.f;
-    bool wide = false;                      // c max near float32's range: y = (x - max) c
+    bool wide = false;                      // c max beyond kFarRef: y = (x - max) c
     bool raise = false;                     // logits may be raised to FwdPiece::lowest: 2^y is zero there as well
     int count = 0;
     Pair rest{0.f, 0.f}, moment{0.f, 0.f};
 
     __device__ __forceinline__ void move(float top, float c, float lowest) {
-        const bool w = !(fabsf(top) < 1e36f && fabsf(top * c) < 1e36f);
+        const bool w = !(fabsf(top) < 1e36f && fabsf(top * c) < kFarRef);
         const float r = w ? 0.f : top * c, d = w ? 0.f : fmaf(top, c, -r);
         if (mx > -INFINITY) {
             const float shift = fmaxf((mx - top) * c, -1e30f) - delta + d, s = exp2_near(shift), own = (float)count * exp2_near(delta);

@@ -3,7 +3,8 @@ float64 oracle, with the tolerances that tests/test_gpu_tokens.py derives."""
 import numpy as np
 import pytest
 
-from tests.test_gpu_tokens import _logprob_case, _torch
+from oracle import tokens as O
+from tests.test_gpu_tokens import U, _close, _logprob_case, _logprob_tolerance, _matrix, _np, _torch
 
 pytestmark = pytest.mark.gpu
 
@@ -40,3 +41,72 @@ def test_alternatives_of_a_long_float32_row_that_is_not_finite():
     assert top[[0, 3]].isnan().all() and (top[1] == -float("inf")).all() and lse[[0, 3]].isnan().all()
     # equal logits: each has the logarithm of 1 / vocab, rounded once
     assert np.abs(top[2].double().cpu().numpy() + np.log(vocab)).max() <= np.log(vocab) * 2.0 ** -22
+
+
+def _masked_rows(rng, vocab, mask, dtype):
+    """Rows whose finite mask lies where a warp or a row meets it first, last, or alone."""
+    x = rng.normal(size=(9, vocab)) * 2.5
+    at = np.arange(vocab)
+    x[0, :vocab * 3 // 5] = mask                                  # whole leading pieces
+    x[1, vocab * 2 // 5:] = mask                                  # whole trailing pieces
+    x[2] = mask
+    x[2, vocab // 2] = 0.25                                       # one token left
+    x[3] = mask                                                   # none left
+    x[4, :5] = mask                                               # the logits before a row's first aligned one
+    x[5, (at >> 10) % 2 == 1] = mask                              # every other piece
+    x[6, rng.random(vocab) < 0.5] = mask
+    x[7, at % 2 == 0] = mask                                      # two masks, and nothing else
+    x[7, at % 2 == 1] = mask * 1.5 if abs(mask) < 1e37 and dtype != "float16" else mask
+    x[8] += -mask if abs(mask) < 1e36 and dtype != "float16" else 0.0     # far above zero
+    return x
+
+
+def _check_values(x, dtype, it, k, offset=0):
+    torch, p = _torch()
+    rows, vocab = x.shape
+    flat, dev = _matrix(torch, x, dtype, None, offset)
+    xs = _np(dev)
+    tok = np.arange(rows) * 7919 % vocab
+    f = lambda *n: torch.full(n, 9.0, device="cuda")              # noqa: E731
+    logp, entropy, lse, top, ids = f(rows), f(rows), f(rows), f(rows, k), torch.full((rows, k), 9, dtype=torch.int32, device="cuda")
+    p.logprob_forward(dev, torch.tensor(tok, device="cuda"), logp, entropy=entropy, lse=lse, top_logp=top, top_ids=ids, inv_temperature=it)
+    rl, re, rz, rt, ri = O.logprob_forward(xs, tok, it, k)
+    tz, te = _logprob_tolerance(xs, it, rows)
+    big = float(np.finfo(np.float32).max)                         # what float32 cannot hold is infinite
+    for got, ref, tol in ((lse, rz, tz), (logp, rl, tz), (entropy, re, te), (top, rt, tz[:, None])):
+        ref = np.where(np.abs(ref) > big * (1 + U), np.sign(ref) * np.inf, ref)
+        with np.errstate(invalid="ignore"):
+            _close(_np(got), ref, tol + np.where(np.isfinite(ref), 2 * U * np.abs(ref), 0.0))
+    np.testing.assert_array_equal(ids.cpu().numpy(), ri)
+    return dev, tok, rl, re, rz
+
+
+MASKS = [-1e5, -1e9, -4.5e9, -1e10, -1e12, -1e15, -1e20, -1e30, -1e32, -7e35, -2e36, -1e38]
+
+
+@pytest.mark.parametrize("mask", MASKS)
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("vocab,offset", [(300, 0), (300, 3), (40000, 0), (40001, 5), (131075, 1)])
+def test_values_of_rows_with_finite_masks(vocab, offset, dtype, mask):
+    rng = np.random.default_rng(vocab)
+    x = _masked_rows(rng, vocab, mask, dtype)
+    for it in (1.0, 0.7, 1.3):
+        _check_values(x, dtype, it, 4, offset)
+
+
+@pytest.mark.parametrize("it", [1e-38, 1e-6, 1e-3, 1e3, 1e6, 1e9, 1e12, 1e20, 1e30, 3e38])
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16", "float16"])
+@pytest.mark.parametrize("vocab", [300, 40001, 131075])
+def test_values_at_temperatures_far_from_one(vocab, dtype, it):
+    rng = np.random.default_rng(vocab)
+    x = np.concatenate([_masked_rows(rng, vocab, float(np.finfo(np.float16).min), dtype), 20.0 * rng.normal(size=(20, vocab))])
+    x[-1] = 0.0
+    _check_values(x, dtype, it, 4, 1)
+
+
+def test_values_of_many_short_rows_with_finite_masks():
+    # more rows than blocks are resident: two warps each
+    rng = np.random.default_rng(5)
+    for dtype in ("float32", "bfloat16"):
+        x = np.tile(_masked_rows(rng, 3001, -1e10, dtype), (90, 1))
+        _check_values(x, dtype, 0.7, 4)

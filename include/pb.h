@@ -366,7 +366,9 @@ int pb_logprob_forward(const void* dev_logits, int dtype, int64_t rows, int64_t 
  *                          - g_entropy p_i (log p_i + entropy) + g_lse p_i ).
  * dlogits: [rows, vocab] of the logits' type, row stride ld_d; the logits' own buffer (same
  * pointer and stride) is allowed, any other overlap is PB_E_ARG.  Rows without a finite logit
- * have gradient zero.  Like softmax_ce at the end of a stage list, but over rows of the
+ * have gradient zero.  p is exp(inv_temperature * x - lse) with the float32 lse given, so it is off by
+ * up to |lse| 2^-23 of itself; where |lse| passes 2^23 (rows of nothing but a finite mask of -1e10, say)
+ * it is some number between 0 and 1.  Like softmax_ce at the end of a stage list, but over rows of the
  * caller's memory. */
 int pb_logprob_backward(const void* dev_logits, int dtype, int64_t rows, int64_t vocab, int64_t ld,
                         const void* dev_tokens, int token_bytes, double inv_temperature,

@@ -4,7 +4,7 @@ import numpy as np
 import pytest
 
 from oracle import tokens as O
-from tests.test_gpu_tokens import U, _close, _logprob_case, _logprob_tolerance, _matrix, _np, _torch
+from tests.test_gpu_tokens import U, _close, _logprob_case, _logprob_gradient, _logprob_tolerance, _matrix, _np, _torch
 
 pytestmark = pytest.mark.gpu
 
@@ -110,3 +110,49 @@ def test_values_of_many_short_rows_with_finite_masks():
     for dtype in ("float32", "bfloat16"):
         x = np.tile(_masked_rows(rng, 3001, -1e10, dtype), (90, 1))
         _check_values(x, dtype, 0.7, 4)
+
+
+FULL_MASKS = [-1e6, -1e9, -1e10, -1e12, -1e30, -3e38, 1e10]
+
+
+@pytest.mark.parametrize("it", [1.0, 0.7, 1.3, 1e-3])
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("vocab,offset", [(300, 0), (5001, 3)])
+def test_gradient_of_rows_whose_logsumexp_is_large(vocab, offset, dtype, it):
+    # A float32 lse of 1e10 is a multiple of 1024, so exp(it x - lse) of such a row could be anything.  It is a
+    # probability all the same: rows that get no gradient pass none on, others none beyond their factor.
+    torch, p = _torch()
+    rows = len(FULL_MASKS)
+    _, dev = _matrix(torch, np.repeat(np.array(FULL_MASKS)[:, None], vocab, 1), dtype, None, offset)
+    _, d = _matrix(torch, np.zeros((rows, vocab)), dtype, None, offset)
+    tok = torch.full((rows,), vocab // 2, device="cuda")
+    logp, lse, entropy = (torch.empty(rows, device="cuda") for _ in range(3))
+    p.logprob_forward(dev, tok, logp, lse=lse, entropy=entropy, inv_temperature=it)
+    # 3e38 times 1.3 is beyond float32: that row's lse is -inf, and it has no gradient
+    assert torch.equal(torch.isfinite(lse), (dev[:, 0].double() * it).abs() < 3.4e38) and torch.isfinite(entropy).all()
+    full = lambda v: torch.full((rows,), v, device="cuda")        # noqa: E731
+    for where in (d, dev.clone()):                                # apart, and over the logits themselves
+        same = where is not d
+        src = where if same else dev
+        p.logprob_backward(src, tok, lse, where, g_logp=full(0.0), g_entropy=full(0.0), entropy=entropy, g_lse=full(0.0), inv_temperature=it)
+        assert (where == 0).all()
+    p.logprob_backward(dev, None, lse, d, g_lse=full(0.0), inv_temperature=it)
+    assert (d == 0).all()
+    p.logprob_backward(dev, tok, lse, d, g_logp=full(-2.0), g_lse=full(0.5), inv_temperature=it)
+    got = _np(d)
+    # 0 <= p <= 1; the store's rounding and those of the products
+    assert np.isfinite(got).all() and (np.abs(got) <= 2.5 * it * (1 + 2.0 ** -7)).all()
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("shift", [3e4, 4e4, -1e5, 1e5])
+@pytest.mark.parametrize("vocab,offset", [(300, 0), (5001, 3)])
+def test_gradient_of_rows_far_from_zero(vocab, offset, shift, dtype):
+    torch, p = _torch()
+    rng = np.random.default_rng(3)
+    x = rng.normal(size=(5, vocab)) * 2.5 + shift
+    x[1, vocab // 3] += 9.0
+    for it in (1.0, 0.7):
+        _, dev = _matrix(torch, x, dtype, None, offset)
+        tok = rng.integers(0, vocab, 5)
+        _logprob_gradient(torch, p, dev, torch.tensor(tok, device="cuda"), tok, it, dtype, False, None, offset)

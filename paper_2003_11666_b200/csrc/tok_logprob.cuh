@@ -630,8 +630,9 @@ struct BwdRow {
             float a, b;
             Pair lp = fma2(Pair(x[k], x[k + 1]), t, mz), factor = f;
             if (entropy) {
-                lp.split(a, b);     // NaN stays NaN; a logit of -inf has p = 0, and a finite factor through this
-                lp = Pair(max_nan(a, -1e30f), max_nan(b, -1e30f));
+                // NaN stays NaN.  2^-288 is zero, so a masked logit has p = 0; the clamp keeps the factor beside it finite.
+                lp.split(a, b);
+                lp = Pair(max_nan(a, -200.f), max_nan(b, -200.f));
                 factor = fma2(mh, lp + hh, f);
             }
             (lp * log2e).split(a, b);

@@ -156,3 +156,31 @@ def test_gradient_of_rows_far_from_zero(vocab, offset, shift, dtype):
         _, dev = _matrix(torch, x, dtype, None, offset)
         tok = rng.integers(0, vocab, 5)
         _logprob_gradient(torch, p, dev, torch.tensor(tok, device="cuda"), tok, it, dtype, False, None, offset)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("vocab,offset", [(300, 0), (40001, 5)])
+def test_entropy_gradient_of_masked_logits_is_zero_at_any_scale(vocab, offset, dtype):
+    # a masked logit has p = 0: its gradient is 0, however large the factor beside p is
+    torch, p = _torch()
+    rng = np.random.default_rng(1)
+    x = rng.normal(size=(6, vocab))
+    mask = np.array([-np.inf, -np.inf, -1e9, -1e30, -3e38, -1e5])
+    hit = rng.random((6, vocab)) < 0.4
+    hit[:, 1] = False
+    x = np.where(hit, mask[:, None], x)
+    _, dev = _matrix(torch, x, dtype, None, offset)
+    lse, entropy, d = torch.empty(6, device="cuda"), torch.empty(6, device="cuda"), torch.empty_like(dev)
+    xs = _np(dev)
+    for it, scale in ((1.0, 1.0), (1.0, 1e9), (1.0, 1e30), (1e6, 1e3), (1e9, 1.0)):
+        p.logprob_forward(dev, lse=lse, entropy=entropy, inv_temperature=it)
+        p.logprob_backward(dev, None, lse, d, g_entropy=torch.full((6,), scale, device="cuda"), entropy=entropy, inv_temperature=it)
+        got = _np(d)
+        assert np.isfinite(got).all() and (got[hit] == 0).all(), (it, scale)
+        if it == 1.0:
+            z, h = _np(lse)[:, None], _np(entropy)[:, None]
+            lp = xs - z
+            ref = -scale * np.exp(lp) * (np.where(hit, 0.0, lp) + h)
+            # p: 2^-20 of itself; the bracket: a few roundings of |log p| + H; the stores's rounding
+            tol = scale * np.exp(lp) * (np.where(hit, 0.0, np.abs(lp)) + h) * 2.0 ** -19 + (2.0 ** -8 if dtype == "bfloat16" else U) * np.abs(ref)
+            _close(got, ref, tol)

@@ -9,8 +9,8 @@
 // sort of (id, position) pairs; then groups of threads walk stretches of the sorted list, add the
 // rows of a run of equal ids in registers and write each table row once.  Runs that cross
 // stretches leave partial rows, which the group that arrives last adds up in list order; so
-// sums depend on the ids alone, no addition to memory is atomic, and a row shared by
-// thousands of tokens is still the work of many groups.
+// sums depend on the ids alone, every table row has one writer, which adds to it once, and a row
+// shared by thousands of tokens is still the work of many groups.
 #pragma once
 #include <type_traits>
 
@@ -390,8 +390,13 @@ __device__ __forceinline__ int last_stretch(const RedPlan& a, int st, unsigned v
     return in;
 }
 
-// The row's only writer: float32 rows that accumulate are added to in memory, which needs no wait
-// for the old values; 16-bit ones are read, so that the sum is rounded once.
+// A row's only writer: float32 rows that accumulate are added to in memory, which needs no wait for the old
+// values (65536 tokens of 2048 columns: 191 us; reading them first 255).  Such an addition flushes what is below
+// 2^-126 to zero, which changes nothing if the addend is kRedLeast at least: an old value that is flushed is less
+// than half a step of the sum (2^-126 to a step of 2^-124; to 2^-125 below a power of two), and a sum that
+// cancels is a multiple of 2^-125, the step of both numbers.  Smaller addends, and zeros, are added to the value
+// read, like those of 16-bit rows, whose sum is rounded once.
+constexpr float kRedLeast = 0x1p-100f;
 template <bool VEC, typename G>
 __device__ __forceinline__ void finish_row(G* dtable, const RedPlan& a, unsigned v, float (&s)[kRedCols], const Cols<VEC>& q) {
     G* row = dtable + (long long)v * a.ld;
@@ -401,14 +406,25 @@ __device__ __forceinline__ void finish_row(G* dtable, const RedPlan& a, unsigned
         if constexpr (sizeof(G) == 4) {
             if constexpr (VEC) {
 #pragma unroll
-                for (int h = 0; h < 8; h += 4)
-                    if (q.in(h))
-                        asm volatile("red.relaxed.gpu.global.add.v4.f32 [%0], {%1, %2, %3, %4};" ::"l"(row + q.at(h)), "f"(s[h]), "f"(s[h + 1]),
-                                     "f"(s[h + 2]), "f"(s[h + 3]) : "memory");
+                for (int h = 0; h < 8; h += 4) {
+                    if (!q.in(h)) continue;
+                    float* p = row + q.at(h);
+                    if (fminf(fminf(fabsf(s[h]), fabsf(s[h + 1])), fminf(fabsf(s[h + 2]), fabsf(s[h + 3]))) >= kRedLeast) {
+                        asm volatile("red.relaxed.gpu.global.add.v4.f32 [%0], {%1, %2, %3, %4};" ::"l"(p), "f"(s[h]), "f"(s[h + 1]), "f"(s[h + 2]),
+                                     "f"(s[h + 3]) : "memory");
+                    } else {
+                        const float4 old = *reinterpret_cast<const float4*>(p);
+                        *reinterpret_cast<float4*>(p) = make_float4(s[h] + old.x, s[h + 1] + old.y, s[h + 2] + old.z, s[h + 3] + old.w);
+                    }
+                }
             } else {
 #pragma unroll
-                for (int k = 0; k < kRedCols; ++k)
-                    if (q.in(k)) asm volatile("red.relaxed.gpu.global.add.f32 [%0], %1;" ::"l"(row + q.at(k)), "f"(s[k]) : "memory");
+                for (int k = 0; k < kRedCols; ++k) {
+                    if (!q.in(k)) continue;
+                    float* p = row + q.at(k);
+                    if (fabsf(s[k]) >= kRedLeast) asm volatile("red.relaxed.gpu.global.add.f32 [%0], %1;" ::"l"(p), "f"(s[k]) : "memory");
+                    else *p += s[k];
+                }
             }
             return;
         }

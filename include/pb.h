@@ -389,7 +389,7 @@ int pb_logprob_backward(const void* dev_logits, int dtype, int64_t rows, int64_t
  * mantissa bits, rounded at random by `seed`, the step number, the tensor's place in the list
  * and the element: the same call gives the same result.  A block of 256 with a moment that is
  * not finite reads back as NaN.  A block of m whose largest magnitude is below 2^-100 is
- * held as zeros.  In u, a v below 2^-126 counts as zero.
+ * held as zeros.  In u, a v below 2^-126 counts as zero where that is less than 2^-25 of eps.
  * *dev_grad_scale (device, NULL: 1) is the product of whatever clipping and loss scaling leave;
  * if it is not finite the step changes nothing.  dev_lr and dev_step (device, may be NULL) take
  * the place of lr and step (*dev_step at least 1), so that a captured graph can be replayed

@@ -54,6 +54,7 @@ struct AdamScalars {
     const float* dev_lr;
     const long long* dev_step;
     int fwd_dtype;
+    int subnormal;               // eps is so small that roots of numbers below 2^-126 count beside it
     int n;                       // tensors of this launch
     int near_shift;
     unsigned short near[kAdamNear];    // tensor that holds round k << near_shift
@@ -162,10 +163,13 @@ __device__ __forceinline__ void scale8(float (&x)[8], float s) {
     for (int k = 0; k < 8; k += 2) (Pair(x[k], x[k + 1]) * Pair(s)).split(x[k], x[k + 1]);
 }
 
-// Square root and reciprocal to 2^-23 or so of themselves; results and arguments below 2^-126 count as zero.
+// Square root and reciprocal to 2^-23 or so of themselves; results, and arguments unless SUB, below 2^-126 count as
+// zero.
+template <bool SUB>
 __device__ __forceinline__ float sqrt_near(float x) {
     float r;
-    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    if (SUB) asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
+    else asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
 }
 __device__ __forceinline__ float rcp_near(float x) {
@@ -229,7 +233,7 @@ struct AdamIn {
 };
 
 // One block of 256 elements by a warp.
-template <int BITS, typename GT, bool VEC, typename Now>
+template <int BITS, typename GT, bool VEC, bool SUB, typename Now>
 __device__ __forceinline__ void adamw_block(const AdamScalars& a, const AdamTensor& t, long long block, int lane, Now scalars) {
     const AdamLane<VEC> q{block * kAdamBlock, t.n, lane};
     AdamIn<BITS, GT, VEC> in;
@@ -271,8 +275,8 @@ __device__ __forceinline__ void adamw_block(const AdamScalars& a, const AdamTens
         const Pair vk = fma2(b2, Pair(v[k], v[k + 1]), none) + fma2(o2 * gk, gk, none);
         mk.split(m[k], m[k + 1]);
         vk.split(v[k], v[k + 1]);
-        r[k] = sqrt_near(v[k]);
-        r[k + 1] = sqrt_near(v[k + 1]);
+        r[k] = sqrt_near<SUB>(v[k]);
+        r[k + 1] = sqrt_near<SUB>(v[k + 1]);
         float d0, d1;                                // denominators, below 2^126
         fma2(Pair(r[k], r[k + 1]), c2, eps).split(d0, d1);
         const Pair u = (mk * c1) * Pair(rcp_near(d0), rcp_near(d1));
@@ -363,8 +367,14 @@ adamw_kernel(const __grid_constant__ AdamTable<MAXT> a) {
         now.key = t.rnd + (a.s.seed + (unsigned long long)step) * 0xD1342543DE82EF95ull;
         return (bool)isfinite(now.gs);               // else the step is left out
     };
-    if (t.vec && (block + 1) * kAdamBlock <= t.n) adamw_block<BITS, GT, true>(a.s, t, block, lane, scalars);
-    else adamw_block<BITS, GT, false>(a.s, t, block, lane, scalars);
+    const bool whole = t.vec && (block + 1) * kAdamBlock <= t.n;
+    if (a.s.subnormal) {
+        if (whole) adamw_block<BITS, GT, true, true>(a.s, t, block, lane, scalars);
+        else adamw_block<BITS, GT, false, true>(a.s, t, block, lane, scalars);
+    } else {
+        if (whole) adamw_block<BITS, GT, true, false>(a.s, t, block, lane, scalars);
+        else adamw_block<BITS, GT, false, false>(a.s, t, block, lane, scalars);
+    }
 }
 
 template <bool VEC>

@@ -408,6 +408,8 @@ int pb_adamw_step(const pb_adamw_tensor* tensors, const void* const* dev_grads, 
     q.step = args->step; q.seed = args->seed;
     q.grad_scale = args->dev_grad_scale; q.dev_lr = args->dev_lr; q.dev_step = (const long long*)args->dev_step;
     q.fwd_dtype = args->forward_dtype;
+    // Roots below 2^-63, corrected by 1 / sqrt(1 - beta2) at most, are less than 2^-25 of an eps from here on.
+    q.subnormal = args->eps < 0x1p-38 / std::sqrt(1.0 - args->beta2);
     auto by_size = [&](auto few) {
         for (int k = 0; k < n_tensors;) {
             const int rc = adamw_launch<decltype(few)::value>(tensors, dev_grads, n_tensors, k, q, *args, (cudaStream_t)stream);

@@ -2,9 +2,10 @@
 
 Each function has the name and meaning of the C entry point it calls (include/pb.h) and
 works on CUDA tensors that the caller owns, on the current device.  Outputs are written in
-place; nothing is allocated, computed or synchronised here.  `stream` is a cudaStream_t as
-an integer (0: the default stream), like everywhere in this package.  Arguments that do not
-fit raise PBError with code -1 before anything is launched.
+place; nothing is allocated, computed or synchronised here.  Calls run on torch's current
+stream, like the torch operations that make and use their tensors; `stream`, a cudaStream_t as
+an integer (0: the legacy default stream), names another one.  Arguments that do not fit raise
+PBError with code -1 before anything is launched.
 """
 import ctypes as C
 
@@ -28,6 +29,9 @@ def _check(rc):
     if rc != 0:
         raise PBError(rc, _lib.pb_last_error(None).decode())
 
+
+# The current stream of a device as an integer, without the object that torch.cuda.current_stream() makes.
+_current = torch._C._cuda_getCurrentRawStream
 
 _OFF_DEVICE = "every tensor must be a CUDA tensor on the current device"
 
@@ -77,7 +81,7 @@ def _status(who, t):
     return None if t is None else _vector(who, "status", t, 1, torch.int32)
 
 
-def embed_forward(table, ids, out, scale=1.0, status=None, stream=0):
+def embed_forward(table, ids, out, scale=1.0, status=None, stream=None):
     """pb_embed_forward: out[t] = scale * table[ids[t]].  out: [n_tokens, dim], rows may be strided."""
     who = "embed_forward"
     d = _device(who, table)
@@ -88,7 +92,7 @@ def embed_forward(table, ids, out, scale=1.0, status=None, stream=0):
     if rows != ids.numel() or cols != dim or out.dtype is not table.dtype:
         _refuse(who, "out must be [number of ids, dim] of the table's type")
     _check(_lib.pb_embed_forward(table.data_ptr(), _DTYPE[table.dtype], vocab, dim, ld, p, size, rows, scale,
-                                           out.data_ptr(), ld_out, _status(who, status), stream))
+                                           out.data_ptr(), ld_out, _status(who, status), _current(d) if stream is None else stream))
 
 
 def embed_scratch_bytes(n_tokens, vocab, dim):
@@ -99,7 +103,7 @@ def embed_scratch_bytes(n_tokens, vocab, dim):
     return n
 
 
-def embed_backward(dout, ids, dtable, scratch, scale=1.0, padding_idx=-1, accumulate=False, status=None, stream=0):
+def embed_backward(dout, ids, dtable, scratch, scale=1.0, padding_idx=-1, accumulate=False, status=None, stream=None):
     """pb_embed_backward: dtable[v] (+)= scale * sum of dout[t] over ids[t] == v.  scratch: uint8 tensor of
     embed_scratch_bytes(...) bytes."""
     who = "embed_backward"
@@ -114,11 +118,11 @@ def embed_backward(dout, ids, dtable, scratch, scale=1.0, padding_idx=-1, accumu
         _refuse(who, "scratch must be a dense uint8 tensor")
     _check(_lib.pb_embed_backward(dout.data_ptr(), _DTYPE[dout.dtype], ld_dout, p, size, rows, vocab, dim, scale,
                                             padding_idx, dtable.data_ptr(), _DTYPE[dtable.dtype], ld, 1 if accumulate else 0,
-                                            scratch.data_ptr(), scratch.numel(), _status(who, status), stream))
+                                            scratch.data_ptr(), scratch.numel(), _status(who, status), _current(d) if stream is None else stream))
 
 
 def logprob_forward(logits, tokens=None, logp=None, entropy=None, lse=None, top_logp=None, top_ids=None, inv_temperature=1.0,
-                    status=None, stream=0):
+                    status=None, stream=None):
     """pb_logprob_forward: log probabilities of `tokens`, entropies, logsumexps and top alternatives of rows of logits."""
     who = "logprob_forward"
     d = _device(who, logits)
@@ -141,11 +145,11 @@ def logprob_forward(logits, tokens=None, logp=None, entropy=None, lse=None, top_
     _check(_lib.pb_logprob_forward(
         logits.data_ptr(), _DTYPE[logits.dtype], rows, vocab, ld, p, size, inv_temperature, _vector(who, "logp", logp, rows),
         _vector(who, "entropy", entropy, rows), _vector(who, "lse", lse, rows), k, _vector(who, "top_logp", top_logp, rows * k),
-        _vector(who, "top_ids", top_ids, rows * k, torch.int32), _status(who, status), stream))
+        _vector(who, "top_ids", top_ids, rows * k, torch.int32), _status(who, status), _current(d) if stream is None else stream))
 
 
 def logprob_backward(logits, tokens, lse, dlogits, g_logp=None, g_entropy=None, entropy=None, g_lse=None, inv_temperature=1.0,
-                     status=None, stream=0):
+                     status=None, stream=None):
     """pb_logprob_backward: gradient with respect to the logits (dlogits may be the logits themselves)."""
     who = "logprob_backward"
     d = _device(who, logits)
@@ -162,10 +166,10 @@ def logprob_backward(logits, tokens, lse, dlogits, g_logp=None, g_entropy=None, 
     _check(_lib.pb_logprob_backward(
         logits.data_ptr(), _DTYPE[logits.dtype], rows, vocab, ld, p, size, inv_temperature, _vector(who, "lse", lse, rows),
         _vector(who, "entropy", entropy, rows), _vector(who, "g_logp", g_logp, rows), _vector(who, "g_entropy", g_entropy, rows),
-        _vector(who, "g_lse", g_lse, rows), dlogits.data_ptr(), ld_d, _status(who, status), stream))
+        _vector(who, "g_lse", g_lse, rows), dlogits.data_ptr(), ld_d, _status(who, status), _current(d) if stream is None else stream))
 
 
-def adamw_moments(m, m_scale, v, v_scale, m_out=None, v_out=None, stream=0):
+def adamw_moments(m, m_scale, v, v_scale, m_out=None, v_out=None, stream=None):
     """pb_adamw_moments: the float32 moments that an 8-bit state stands for."""
     who = "adamw_moments"
     d = _device(who, m)
@@ -174,7 +178,8 @@ def adamw_moments(m, m_scale, v, v_scale, m_out=None, v_out=None, stream=0):
     blocks = -(-n // 256)
     _check(_lib.pb_adamw_moments(
         _vector(who, "m", m, n, torch.uint8), _vector(who, "m_scale", m_scale, blocks), _vector(who, "v", v, n, torch.uint8),
-        _vector(who, "v_scale", v_scale, blocks), n, _vector(who, "m_out", m_out, n), _vector(who, "v_out", v_out, n), stream))
+        _vector(who, "v_scale", v_scale, blocks), n, _vector(who, "m_out", m_out, n), _vector(who, "v_out", v_out, n),
+        _current(d) if stream is None else stream))
 
 
 class AdamW:
@@ -227,7 +232,7 @@ class AdamW:
         if any(a[1] > b[0] for a, b in zip(spans[:-1], spans[1:])):
             _refuse(who, "two of the tensors overlap")
 
-    def step(self, grads, lr, step, beta1=0.9, beta2=0.999, eps=1e-8, seed=0, grad_scale=None, dev_lr=None, dev_step=None, stream=0):
+    def step(self, grads, lr, step, beta1=0.9, beta2=0.999, eps=1e-8, seed=0, grad_scale=None, dev_lr=None, dev_step=None, stream=None):
         """One step with `grads`, one tensor per weight, all of one type.  `step` counts from 1."""
         who = "AdamW.step"
         n = len(self._n)
@@ -251,4 +256,4 @@ class AdamW:
         a.dev_grad_scale = None if grad_scale is None else _vector(who, "grad_scale", grad_scale, 1)
         a.dev_lr = None if dev_lr is None else _vector(who, "dev_lr", dev_lr, 1)
         a.dev_step = None if dev_step is None else _vector(who, "dev_step", dev_step, 1, torch.int64)
-        _check(_lib.pb_adamw_step(self._table, self._grads, n, self._args_ref, stream))
+        _check(_lib.pb_adamw_step(self._table, self._grads, n, self._args_ref, _current(device) if stream is None else stream))

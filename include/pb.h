@@ -426,6 +426,9 @@ int pb_adamw_step(const pb_adamw_tensor* tensors, const void* const* dev_grads, 
 int pb_adamw_moments(const void* dev_m, const float* dev_m_scale, const void* dev_v, const float* dev_v_scale,
                      int64_t n, float* dev_m_out, float* dev_v_out, void* stream);
 
+/* Text of the handle's latest failure; of NULL: of the latest failure without a handle.  That is this thread's, if its
+ * latest is a token operator's, else the engine's latest on any thread.  The text of NULL holds until the thread's
+ * next call of this function or of a token operator. */
 const char* pb_last_error(const pb_handle* h);
 void pb_destroy(pb_handle* h);
 

@@ -4,6 +4,7 @@
 #include <cmath>
 #include <cstdio>
 #include <cstring>
+#include <mutex>
 #include <new>
 
 #include "conv_gemm.cuh"
@@ -16,10 +17,21 @@ using namespace pb;
 
 namespace {
 
-thread_local std::string g_create_error;
+// Texts of failures without a handle.  The engine's entry points leave theirs for every thread (one thread may create
+// and another report); the token operators, which may run on several threads at a time, for their own.
+std::mutex g_error_lock;
+std::string g_create_error;                  // the engine's latest, under the lock
+thread_local std::string t_error;            // what pb_last_error(NULL) has returned on this thread, or its token operator's text
+thread_local bool t_token_failed = false;    // this thread's latest failure is a token operator's
 
 int fail(pb_handle* h, int code, const std::string& msg) {
-    if (h) h->err = msg; else g_create_error = msg;
+    if (h) {
+        h->err = msg;
+    } else {
+        std::lock_guard<std::mutex> hold(g_error_lock);
+        g_create_error = msg;
+        t_token_failed = false;
+    }
     return code;
 }
 
@@ -37,7 +49,8 @@ namespace pb {
 // Errors of the entry points that have no handle (tok_api.cu).
 int fail_text(int code, const char* text) {
     try {
-        g_create_error = text;
+        t_error = text;
+        t_token_failed = true;
     } catch (...) {
     }
     return code;
@@ -1690,7 +1703,18 @@ double pb_profile_ms(pb_handle* h, int which, long long* launches) {
     return h->prof[which].ms;
 }
 
-const char* pb_last_error(const pb_handle* h) { return h ? h->err.c_str() : g_create_error.c_str(); }
+const char* pb_last_error(const pb_handle* h) {
+    if (h) return h->err.c_str();
+    if (!t_token_failed) {
+        try {
+            std::lock_guard<std::mutex> hold(g_error_lock);
+            t_error = g_create_error;
+        } catch (...) {
+            return "";
+        }
+    }
+    return t_error.c_str();
+}
 
 void pb_destroy(pb_handle* h) {
     if (!h) return;

@@ -30,8 +30,11 @@ def _check(rc):
         raise PBError(rc, _lib.pb_last_error(None).decode())
 
 
-# The current stream of a device as an integer, without the object that torch.cuda.current_stream() makes.
-_current = torch._C._cuda_getCurrentRawStream
+# The current device, and its current stream as an integer: what torch.cuda.current_device() and current_stream() ask,
+# without their other work (a CUDA tensor is at hand, so CUDA is up).
+_current_device, _current = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+
+_address, _numel, _get_device, _is_contiguous = torch.Tensor.data_ptr, torch.Tensor.numel, torch.Tensor.get_device, torch.Tensor.is_contiguous
 
 _OFF_DEVICE = "every tensor must be a CUDA tensor on the current device"
 
@@ -45,7 +48,7 @@ def _on_device(who, device, *tensors):
 
 def _device(who, t):
     d = t.get_device() if isinstance(t, torch.Tensor) else -1
-    if d < 0 or d != torch.cuda.current_device():
+    if d < 0 or d != _current_device():
         _refuse(who, _OFF_DEVICE)
     return d
 
@@ -183,7 +186,9 @@ def adamw_moments(m, m_scale, v, v_scale, m_out=None, v_out=None, stream=None):
 
 
 class AdamW:
-    """pb_adamw_step over a fixed list of tensors: holds the tensors and the table of their addresses.
+    """pb_adamw_step over a fixed list of tensors: holds the tensors and the table of their addresses.  Weights and
+    w_forward may be moved between steps (`w.data = ...`): the table is laid out anew.  The states' memory is held as it
+    was given.
 
     w: float32 weights.  m, v: float32 states, or uint8 ones with m_scale / v_scale (float32, one per 256 elements).
     w_forward: copies of the weights in the forward's type, predicted `horizon` steps ahead, or None.  weight_decay and
@@ -201,22 +206,32 @@ class AdamW:
         ahead = list(horizon) if hasattr(horizon, "__len__") else [horizon] * n
         if len(decay) != n or len(ahead) != n:
             _refuse(who, "weight_decay and horizon are numbers, or one number per tensor")
-        self._keep = lists
-        self._bits = 8 if n and lists[1][0].dtype is torch.uint8 else 32
-        self._forward = _DTYPE.get(lists[5][0].dtype, -1) if n and lists[5][0] is not None else 0
-        self._device = _device(who, lists[0][0]) if n else None
-        self._n = [t.numel() for t in lists[0]]
+        for x in lists[1:5]:                                 # names of their own for the states' memory
+            x[:] = [t.detach() if isinstance(t, torch.Tensor) else t for t in x]
+        self._lists, self._decay, self._ahead = lists, decay, ahead
+        self._may_move = [t for t in lists[0] + lists[5] if t is not None]
         self._table = (pb_adamw_tensor * n)()
         self._grads = (C.c_void_p * n)()
-        self._args = pb_adamw_args(forward_dtype=self._forward, state_bits=self._bits)
+        self._args = pb_adamw_args()
         self._args_ref = C.byref(self._args)
-        state = torch.uint8 if self._bits == 8 else torch.float32
+        self._lay_out(who)
+
+    def _lay_out(self, who):
+        """The table of addresses, and what has to hold of the tensors."""
+        lists, n = self._lists, len(self._table)
+        self._at = None                                      # until they have been looked at
+        bits = 8 if n and lists[1][0].dtype is torch.uint8 else 32
+        forward = _DTYPE.get(lists[5][0].dtype, -1) if n and lists[5][0] is not None else 0
+        self._args.state_bits, self._args.forward_dtype = bits, forward
+        self._device = _device(who, lists[0][0]) if n else None
+        self._n = [t.numel() for t in lists[0]]
+        state = torch.uint8 if bits == 8 else torch.float32
         spans = []
         for k in range(n):
             tw, tm, tv, ms, vs, tf = (x[k] for x in lists)
             _on_device(who, self._device, tw, tm, tv, ms, vs, tf)
             size = self._n[k]
-            if (ms is None) != (self._bits == 32) or (vs is None) != (self._bits == 32):
+            if (ms is None) != (bits == 32) or (vs is None) != (bits == 32):
                 _refuse(who, "8-bit states, and only those, come with scales")
             if (tf is None) != (lists[5][0] is None):
                 _refuse(who, "w_forward is given for every tensor or for none")
@@ -224,13 +239,14 @@ class AdamW:
             p = [_vector(who, "w", tw, size), _vector(who, "m", tm, size, state), _vector(who, "v", tv, size, state),
                  _vector(who, "m_scale", ms, blocks), _vector(who, "v_scale", vs, blocks),
                  _vector(who, "w_forward", tf, size, lists[5][0].dtype) if tf is not None else None]
-            self._table[k] = pb_adamw_tensor(*p, size, float(decay[k]), float(ahead[k]))
+            self._table[k] = pb_adamw_tensor(*p, size, float(self._decay[k]), float(self._ahead[k]))
             spans += [(a, a + t.numel() * t.element_size()) for a, t in zip(p, (tw, tm, tv, ms, vs, tf)) if a and t.numel()]
-        if self._forward < 0:
+        if forward < 0:
             _refuse(who, "w_forward must be float32, bfloat16 or float16")
         spans.sort()
         if any(a[1] > b[0] for a, b in zip(spans[:-1], spans[1:])):
             _refuse(who, "two of the tensors overlap")
+        self._at = list(map(_address, self._may_move))
 
     def step(self, grads, lr, step, beta1=0.9, beta2=0.999, eps=1e-8, seed=0, grad_scale=None, dev_lr=None, dev_step=None, stream=None):
         """One step with `grads`, one tensor per weight, all of one type.  `step` counts from 1."""
@@ -240,17 +256,20 @@ class AdamW:
             _refuse(who, "one gradient per tensor is needed")
         if n == 0:
             return
-        if self._device != torch.cuda.current_device():
-            _refuse(who, "every tensor must be a CUDA tensor on the current device")
-        dtype, device, ptr = grads[0].dtype, self._device, []
-        for g, size in zip(grads, self._n):
-            if g.dtype is not dtype or g.numel() != size or g.get_device() != device or not g.is_contiguous():
-                _refuse(who, "gradients must be dense CUDA tensors of the weights' sizes and of one type")
-            ptr.append(g.data_ptr())
+        if list(map(_address, self._may_move)) != self._at:
+            self._lay_out(who)
+        device = self._device
+        if device != _current_device():
+            _refuse(who, _OFF_DEVICE)
+        dtype = grads[0].dtype
+        # a list per property: of many tensors their calls are the time of a step
+        if list(map(_numel, grads)) != self._n or list(map(_get_device, grads)) != [device] * n or \
+           not all(map(_is_contiguous, grads)) or any([g.dtype is not dtype for g in grads]):
+            _refuse(who, "gradients must be dense CUDA tensors of the weights' sizes and of one type")
         if dtype not in _DTYPE:
             _refuse(who, "gradients must be float32, bfloat16 or float16")
         _on_device(who, device, grad_scale, dev_lr, dev_step)
-        self._grads[:] = ptr
+        self._grads[:] = list(map(_address, grads))
         a = self._args
         a.lr, a.beta1, a.beta2, a.eps, a.step, a.seed, a.grad_dtype = lr, beta1, beta2, eps, step, seed & 0xFFFFFFFFFFFFFFFF, _DTYPE[dtype]
         a.dev_grad_scale = None if grad_scale is None else _vector(who, "grad_scale", grad_scale, 1)

@@ -33,9 +33,11 @@ def _token_call_fails(lib):
 
 def test_a_failed_engine_call_can_be_read_from_another_thread(lib):
     # a worker creates, the thread that waits for it reports
-    text = _in_thread(lambda: _create_fails(lib))
-    assert b"pb_mlp_run_static" in text
-    assert lib.pb_last_error(None) == text
+    def wait_and_report():                                         # a thread that has no failure of its own
+        text = _in_thread(lambda: _create_fails(lib))
+        return text, lib.pb_last_error(None)
+    text, reported = _in_thread(wait_and_report)
+    assert b"pb_mlp_run_static" in text and reported == text
     assert _in_thread(lambda: lib.pb_last_error(None)) == text
 
 

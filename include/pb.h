@@ -323,7 +323,7 @@ typedef enum { PB_F32 = 0, PB_BF16 = 1, PB_F16 = 2 } pb_dtype;
 /* out[t, :] = scale * table[id_t, :], rounded once; a zero row where there is no token.
  * table: [vocab, dim] with row stride ld_table, out: [n_tokens, dim] with row stride
  * ld_out, both of `dtype`; columns between dim and the stride are left alone.  n_tokens
- * == 0 is a no-op.  PB_E_ARG if out overlaps the table. */
+ * == 0 is a no-op.  PB_E_ARG if out overlaps the table or the ids. */
 int pb_embed_forward(const void* dev_table, int dtype, int64_t vocab, int64_t dim, int64_t ld_table,
                      const void* dev_ids, int id_bytes, int64_t n_tokens, float scale,
                      void* dev_out, int64_t ld_out, int32_t* dev_status, void* stream);
@@ -336,7 +336,8 @@ int pb_embed_forward(const void* dev_table, int dtype, int64_t vocab, int64_t di
  * dtable is float32 or of dout's type; dim is at most 2^26.  The tokens are sorted by id on
  * the device; nothing is known of them on the host.  dev_scratch: pb_embed_scratch_bytes(...) bytes,
  * 256-byte aligned, not used by another call that may run at the same time (two captured
- * graphs included). */
+ * graphs included).  The ids must not change while the call runs.  PB_E_ARG if dtable, dout and scratch overlap, the
+ * ids one that is written, or the status word the scratch or the ids. */
 size_t pb_embed_scratch_bytes(int64_t n_tokens, int64_t vocab, int64_t dim);
 int pb_embed_backward(const void* dev_dout, int dtype, int64_t ld_dout, const void* dev_ids, int id_bytes,
                       int64_t n_tokens, int64_t vocab, int64_t dim, float scale, int64_t padding_idx,

@@ -192,6 +192,8 @@ int pb_embed_forward(const void* dev_table, int dtype, int64_t vocab, int64_t di
               "pb_embed_forward: a pointer is not aligned to its element");
     PB_REFUSE(overlap(dev_out, extent(n_tokens, dim, ld_out, es), dev_table, extent(vocab, dim, ld_table, es)),
               "pb_embed_forward: the output overlaps the table");
+    PB_REFUSE(overlap(dev_out, extent(n_tokens, dim, ld_out, es), dev_ids, (size_t)n_tokens * id_bytes),
+              "pb_embed_forward: the output overlaps the ids");
     const cudaStream_t s = (cudaStream_t)stream;
     const int64_t piece = 16 / (int64_t)es;
     const bool vec = dim % piece == 0 && ld_table % piece == 0 && ld_out % piece == 0 && aligned(dev_table, 16) && aligned(dev_out, 16);
@@ -244,8 +246,12 @@ int pb_embed_backward(const void* dev_dout, int dtype, int64_t ld_dout, const vo
               "pb_embed_backward: a pointer is not aligned to its element");
     PB_REFUSE(n_tokens > 0 && !aligned(dev_scratch, 256), "pb_embed_backward: scratch must be 256-byte aligned");
     const size_t n_dt = extent(vocab, dim, ld_dtable, gs), n_do = extent(n_tokens, dim, ld_dout, es);
+    // The ids are read several times and have to be the same each time: their places in the sorted list follow from them.
+    const size_t n_id = (size_t)n_tokens * id_bytes, n_st = dev_status ? sizeof(int32_t) : 0;
     PB_REFUSE(overlap(dev_dtable, n_dt, dev_dout, n_do) || overlap(dev_scratch, scratch_bytes, dev_dtable, n_dt) ||
-              overlap(dev_scratch, scratch_bytes, dev_dout, n_do), "pb_embed_backward: buffers overlap");
+              overlap(dev_scratch, scratch_bytes, dev_dout, n_do) || overlap(dev_ids, n_id, dev_scratch, scratch_bytes) ||
+              overlap(dev_ids, n_id, dev_dtable, n_dt) || overlap(dev_status, n_st, dev_scratch, scratch_bytes) ||
+              overlap(dev_status, n_st, dev_ids, n_id), "pb_embed_backward: buffers overlap");
     const cudaStream_t s = (cudaStream_t)stream;
     EmbedPlan e = embed_plan(n_tokens, vocab, dim, (char*)dev_scratch);
     e.red.ld_dout = ld_dout; e.red.ld = ld_dtable; e.red.scale = scale; e.red.accumulate = accumulate;

@@ -41,9 +41,12 @@ _OFF_DEVICE = "every tensor must be a CUDA tensor on the current device"
 
 def _on_device(who, device, *tensors):
     """Every tensor given lives on `device`, the current one."""
-    for t in tensors:
-        if t is not None and t.get_device() != device:
-            _refuse(who, _OFF_DEVICE)
+    try:
+        for t in tensors:
+            if t is not None and t.get_device() != device:
+                _refuse(who, _OFF_DEVICE)
+    except AttributeError:
+        _refuse(who, _OFF_DEVICE)
 
 
 def _device(who, t):
@@ -55,6 +58,8 @@ def _device(who, t):
 
 def _rows(who, name, t):
     """(rows, columns, row stride) of a matrix whose rows are dense."""
+    if t is None:
+        _refuse(who, "%s is needed" % name)
     shape = t.shape
     if len(shape) != 2 or t.dtype not in _DTYPE:
         _refuse(who, "%s must be a matrix of float32, bfloat16 or float16" % name)
@@ -74,6 +79,8 @@ def _vector(who, name, t, n, dtype=torch.float32):
 
 
 def _ids(who, name, t):
+    if t is None:
+        _refuse(who, "%s is needed" % name)
     size = _ID_BYTES.get(t.dtype)
     if size is None or not t.is_contiguous():
         _refuse(who, "%s must be a dense int32 or int64 tensor" % name)
@@ -117,7 +124,7 @@ def embed_backward(dout, ids, dtable, scratch, scale=1.0, padding_idx=-1, accumu
     p, size = _ids(who, "ids", ids)
     if rows != ids.numel() or cols != dim:
         _refuse(who, "dout must be [number of ids, dim]")
-    if scratch.dtype is not torch.uint8 or not scratch.is_contiguous():
+    if scratch is None or scratch.dtype is not torch.uint8 or not scratch.is_contiguous():
         _refuse(who, "scratch must be a dense uint8 tensor")
     _check(_lib.pb_embed_backward(dout.data_ptr(), _DTYPE[dout.dtype], ld_dout, p, size, rows, vocab, dim, scale,
                                             padding_idx, dtable.data_ptr(), _DTYPE[dtable.dtype], ld, 1 if accumulate else 0,
@@ -209,27 +216,31 @@ class AdamW:
         for x in lists[1:5]:                                 # names of their own for the states' memory
             x[:] = [t.detach() if isinstance(t, torch.Tensor) else t for t in x]
         self._lists, self._decay, self._ahead = lists, decay, ahead
-        self._may_move = [t for t in lists[0] + lists[5] if t is not None]
         self._table = (pb_adamw_tensor * n)()
         self._grads = (C.c_void_p * n)()
         self._args = pb_adamw_args()
         self._args_ref = C.byref(self._args)
+        self._may_move = [t for t in lists[0] + lists[5] if t is not None]
         self._lay_out(who)
 
     def _lay_out(self, who):
         """The table of addresses, and what has to hold of the tensors."""
         lists, n = self._lists, len(self._table)
         self._at = None                                      # until they have been looked at
+        for name, x in zip(("w", "m", "v"), lists):
+            if any(t is None for t in x):
+                _refuse(who, "%s is needed for every tensor" % name)
+        self._device = _device(who, lists[0][0]) if n else None
+        for x in lists:
+            _on_device(who, self._device, *x)
         bits = 8 if n and lists[1][0].dtype is torch.uint8 else 32
         forward = _DTYPE.get(lists[5][0].dtype, -1) if n and lists[5][0] is not None else 0
         self._args.state_bits, self._args.forward_dtype = bits, forward
-        self._device = _device(who, lists[0][0]) if n else None
         self._n = [t.numel() for t in lists[0]]
         state = torch.uint8 if bits == 8 else torch.float32
         spans = []
         for k in range(n):
             tw, tm, tv, ms, vs, tf = (x[k] for x in lists)
-            _on_device(who, self._device, tw, tm, tv, ms, vs, tf)
             size = self._n[k]
             if (ms is None) != (bits == 32) or (vs is None) != (bits == 32):
                 _refuse(who, "8-bit states, and only those, come with scales")
@@ -261,10 +272,13 @@ class AdamW:
         device = self._device
         if device != _current_device():
             _refuse(who, _OFF_DEVICE)
-        dtype = grads[0].dtype
-        # a list per property: of many tensors their calls are the time of a step
-        if list(map(_numel, grads)) != self._n or list(map(_get_device, grads)) != [device] * n or \
-           not all(map(_is_contiguous, grads)) or any([g.dtype is not dtype for g in grads]):
+        try:                                                 # a list per property: of many tensors their calls are the time of a step
+            dtype = grads[0].dtype
+            fits = list(map(_numel, grads)) == self._n and list(map(_get_device, grads)) == [device] * n and \
+                all(map(_is_contiguous, grads)) and not any([g.dtype is not dtype for g in grads])
+        except (AttributeError, TypeError):                  # None among them, or no tensors
+            fits = False
+        if not fits:
             _refuse(who, "gradients must be dense CUDA tensors of the weights' sizes and of one type")
         if dtype not in _DTYPE:
             _refuse(who, "gradients must be float32, bfloat16 or float16")

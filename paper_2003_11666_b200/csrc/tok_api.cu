@@ -18,9 +18,11 @@ using namespace pb;
 
 namespace {
 
-int launched(const char* who) {
-    const cudaError_t e = cudaGetLastError();
+// The status of a call from its launches' own: cudaGetLastError() may still hold what an earlier call of this library
+// has failed with and reported.
+int launched(const char* who, cudaError_t e) {
     if (e == cudaSuccess) return PB_OK;
+    cudaGetLastError();                                      // reported here, so not again
     char text[256];
     snprintf(text, sizeof text, "%s: launch failed: %s", who, cudaGetErrorString(e));
     return fail_text(PB_E_CUDA, text);
@@ -41,20 +43,29 @@ bool overlap(const void* a, size_t na, const void* b, size_t nb) {
     return na && nb && x < y + nb && y < x + na;
 }
 
-// Launch that may begin while the launch before it in the stream ends; the kernel waits for that
-// launch's results itself (cudaGridDependencySynchronize).
 template <typename... P, typename... A>
-cudaError_t launch_after(void (*kernel)(P...), dim3 grid, int threads, cudaStream_t stream, A... args) {
+cudaError_t launch(const cudaLaunchAttribute* attr, void (*kernel)(P...), dim3 grid, int threads, cudaStream_t stream, A... args) {
     cudaLaunchConfig_t c{};
     c.gridDim = grid;
     c.blockDim = dim3((unsigned)threads);
     c.stream = stream;
+    c.attrs = const_cast<cudaLaunchAttribute*>(attr);
+    c.numAttrs = attr != nullptr;
+    return cudaLaunchKernelEx(&c, kernel, P(args)...);
+}
+template <typename... P, typename... A>
+cudaError_t launch(void (*kernel)(P...), dim3 grid, int threads, cudaStream_t stream, A... args) {
+    return launch(nullptr, kernel, grid, threads, stream, args...);
+}
+
+// Launch that may begin while the launch before it in the stream ends; the kernel waits for that
+// launch's results itself (cudaGridDependencySynchronize).
+template <typename... P, typename... A>
+cudaError_t launch_after(void (*kernel)(P...), dim3 grid, int threads, cudaStream_t stream, A... args) {
     cudaLaunchAttribute attr{};
     attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr.val.programmaticStreamSerializationAllowed = 1;
-    c.attrs = &attr;
-    c.numAttrs = 1;
-    return cudaLaunchKernelEx(&c, kernel, P(args)...);
+    return launch(&attr, kernel, grid, threads, stream, args...);
 }
 
 // Launch of `blocks` blocks in clusters of `size`.
@@ -64,17 +75,11 @@ cudaError_t launch_cluster(void (*kernel)(P...), int size, int64_t blocks, int t
         const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
         if (e != cudaSuccess) return e;
     }
-    cudaLaunchConfig_t c{};
-    c.gridDim = dim3((unsigned)blocks);
-    c.blockDim = dim3((unsigned)threads);
-    c.stream = stream;
     cudaLaunchAttribute attr{};
     attr.id = cudaLaunchAttributeClusterDimension;
     attr.val.clusterDim.x = (unsigned)size;
     attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-    c.attrs = &attr;
-    c.numAttrs = 1;
-    return cudaLaunchKernelEx(&c, kernel, P(args)...);
+    return launch(&attr, kernel, dim3((unsigned)blocks), threads, stream, args...);
 }
 
 // Sizes and scratch layout of the embedding gradient.
@@ -162,12 +167,16 @@ int adamw_launch(const pb_adamw_tensor* tensors, const void* const* grads, int n
         while (at + 1 < a.s.n && (int64_t)a.t[at + 1].first_round <= j << a.s.near_shift) ++at;
         a.s.near[j] = (unsigned short)at;
     }
-    auto go = [&](auto bits, auto g) { adamw_kernel<decltype(bits)::value, decltype(g), MAXT><<<(unsigned)rounds, kAdamThreads, 0, stream>>>(a); };
-    auto by_bits = [&](auto g) {
-        if (args.state_bits == 8) go(std::integral_constant<int, 8>(), g); else go(std::integral_constant<int, 32>(), g);
+    auto go = [&](auto bits, auto g) {
+        cudaLaunchConfig_t c{};
+        c.gridDim = dim3((unsigned)rounds);
+        c.blockDim = dim3(kAdamThreads);
+        c.stream = stream;
+        void* table[] = {&a};                                // as it is: a launch by values would copy it on the way
+        return cudaLaunchKernelExC(&c, (const void*)adamw_kernel<decltype(bits)::value, decltype(g), MAXT>, table);
     };
-    if (args.grad_dtype == PB_F32) by_bits(float()); else if (args.grad_dtype == PB_BF16) by_bits(__nv_bfloat16()); else by_bits(__half());
-    return launched("pb_adamw_step");
+    auto by_bits = [&](auto g) { return args.state_bits == 8 ? go(std::integral_constant<int, 8>(), g) : go(std::integral_constant<int, 32>(), g); };
+    return launched("pb_adamw_step", args.grad_dtype == PB_F32 ? by_bits(float()) : args.grad_dtype == PB_BF16 ? by_bits(__nv_bfloat16()) : by_bits(__half()));
 }
 
 }  // namespace
@@ -211,12 +220,11 @@ int pb_embed_forward(const void* dev_table, int dtype, int64_t vocab, int64_t di
         using I = decltype(i);
         auto kernel = vec ? (many ? embed_fwd_kernel<T, I, true, 4> : embed_fwd_kernel<T, I, true, 1>)
                           : (many ? embed_fwd_kernel<T, I, false, 4> : embed_fwd_kernel<T, I, false, 1>);
-        kernel<<<dim3((unsigned)blocks, (unsigned)spread), 256, 0, s>>>((const T*)dev_table, vocab, dim, ld_table, (const I*)dev_ids, n_tokens, scale,
-                                                                        (T*)dev_out, ld_out, lanes, dev_status);
+        return launch(kernel, dim3((unsigned)blocks, (unsigned)spread), 256, s, (const T*)dev_table, vocab, dim, ld_table, (const I*)dev_ids, n_tokens,
+                      scale, (T*)dev_out, ld_out, lanes, dev_status);
     };
-    auto by_id = [&](auto t) { if (id_bytes == 4) go(t, int32_t()); else go(t, int64_t()); };
-    if (dtype == PB_F32) by_id(float()); else if (dtype == PB_BF16) by_id(__nv_bfloat16()); else by_id(__half());
-    return launched("pb_embed_forward");
+    auto by_id = [&](auto t) { return id_bytes == 4 ? go(t, int32_t()) : go(t, int64_t()); };
+    return launched("pb_embed_forward", dtype == PB_F32 ? by_id(float()) : dtype == PB_BF16 ? by_id(__nv_bfloat16()) : by_id(__half()));
 }
 
 size_t pb_embed_scratch_bytes(int64_t n_tokens, int64_t vocab, int64_t dim) {
@@ -266,7 +274,7 @@ int pb_embed_backward(const void* dev_dout, int dtype, int64_t ld_dout, const vo
         if (n_tokens) {
             // One block up to 2048 tokens; else a launch for the first counts and one for each digit (65536 tokens: some
             // 28 us, with 64 blocks of 1024 tokens as with 32 of 2048; a single launch of a 16-block cluster took 40).
-            embed_sort_kernel<I><<<e.sort.tiles, kSortThreads, 0, s>>>(e.sort, in);
+            err = launch(embed_sort_kernel<I>, dim3(e.sort.tiles), kSortThreads, s, e.sort, in);
             for (int p = 0; e.sort.tiles > 1 && p < e.sort.passes && err == cudaSuccess; ++p)
                 err = launch_after(embed_scatter_kernel<I>, dim3(e.sort.tiles), kSortThreads, s, e.sort, in, p);
         }
@@ -286,11 +294,11 @@ int pb_embed_backward(const void* dev_dout, int dtype, int64_t ld_dout, const vo
         G* d = (G*)dev_dtable;
         if (err == cudaSuccess) err = vec ? launch_after(embed_reduce_kernel<true, T, G>, grid, kRedThreads, s, e.red, x, d)
                                           : launch_after(embed_reduce_kernel<false, T, G>, grid, kRedThreads, s, e.red, x, d);
+        return err;
     };
-    auto by_id = [&](auto t, auto g) { if (id_bytes == 4) go(t, g, int32_t()); else go(t, g, int64_t()); };
-    auto by_g = [&](auto t) { if (dtable_dtype == PB_F32) by_id(t, float()); else by_id(t, t); };
-    if (dtype == PB_F32) by_id(float(), float()); else if (dtype == PB_BF16) by_g(__nv_bfloat16()); else by_g(__half());
-    return launched("pb_embed_backward");
+    auto by_id = [&](auto t, auto g) { return id_bytes == 4 ? go(t, g, int32_t()) : go(t, g, int64_t()); };
+    auto by_g = [&](auto t) { return dtable_dtype == PB_F32 ? by_id(t, float()) : by_id(t, t); };
+    return launched("pb_embed_backward", dtype == PB_F32 ? by_id(float(), float()) : dtype == PB_BF16 ? by_g(__nv_bfloat16()) : by_g(__half()));
 }
 
 int pb_logprob_forward(const void* dev_logits, int dtype, int64_t rows, int64_t vocab, int64_t ld, const void* dev_tokens,
@@ -324,19 +332,15 @@ int pb_logprob_forward(const void* dev_logits, int dtype, int64_t rows, int64_t 
         using I = decltype(i);
         const T* x = (const T*)dev_logits;
         const I* tok = (const I*)dev_tokens;
-        if (parts == 1) {
-            auto kernel = few ? logprob_fwd_kernel<T, I, kFwdFewWarps, false> : logprob_fwd_kernel<T, I, kFwdWarps, false>;
-            kernel<<<(unsigned)rows, (few ? kFwdFewWarps : kFwdWarps) * 32, 0, s>>>(x, (int)vocab, ld, tok, inv_temperature, dev_logp, dev_entropy, dev_lse,
-                                                                                  top_k, dev_top_logp, dev_top_ids, per_segment, dev_status);
-            return launched("pb_logprob_forward");
-        }
-        const cudaError_t e = launch_cluster(logprob_fwd_kernel<T, I, kFwdWarps, true>, parts, rows * parts, kFwdWarps * 32, s, x, (int)vocab, (long long)ld, tok,
-                                             inv_temperature, dev_logp, dev_entropy, dev_lse, top_k, dev_top_logp, dev_top_ids, per_segment, dev_status);
-        const int rc = launched("pb_logprob_forward");
-        return rc != PB_OK || e == cudaSuccess ? rc : fail_text(PB_E_CUDA, cudaGetErrorString(e));
+        if (parts > 1)
+            return launch_cluster(logprob_fwd_kernel<T, I, kFwdWarps, true>, parts, rows * parts, kFwdWarps * 32, s, x, (int)vocab, (long long)ld, tok,
+                                  inv_temperature, dev_logp, dev_entropy, dev_lse, top_k, dev_top_logp, dev_top_ids, per_segment, dev_status);
+        auto kernel = few ? logprob_fwd_kernel<T, I, kFwdFewWarps, false> : logprob_fwd_kernel<T, I, kFwdWarps, false>;
+        return launch(kernel, dim3((unsigned)rows), (few ? kFwdFewWarps : kFwdWarps) * 32, s, x, (int)vocab, (long long)ld, tok, inv_temperature, dev_logp,
+                      dev_entropy, dev_lse, top_k, dev_top_logp, dev_top_ids, per_segment, dev_status);
     };
     auto by_id = [&](auto t) { return token_bytes == 8 ? go(t, int64_t()) : go(t, int32_t()); };
-    return dtype == PB_F32 ? by_id(float()) : dtype == PB_BF16 ? by_id(__nv_bfloat16()) : by_id(__half());
+    return launched("pb_logprob_forward", dtype == PB_F32 ? by_id(float()) : dtype == PB_BF16 ? by_id(__nv_bfloat16()) : by_id(__half()));
 }
 
 int pb_logprob_backward(const void* dev_logits, int dtype, int64_t rows, int64_t vocab, int64_t ld, const void* dev_tokens,
@@ -369,13 +373,12 @@ int pb_logprob_backward(const void* dev_logits, int dtype, int64_t rows, int64_t
             using I = decltype(i);
             auto at = [&](const float* p) { return p ? p + r0 : nullptr; };
             const unsigned gx = (unsigned)((vocab + kBwdTile<T> - 1) / kBwdTile<T>);
-            logprob_bwd_kernel<T, I><<<dim3(gx, nr), kBwdThreads, 0, s>>>((const T*)dev_logits + r0 * ld, vocab, ld, dev_tokens ? (const I*)dev_tokens + r0 : nullptr,
-                                                                          inv_temperature, at(dev_lse), at(dev_entropy), at(dev_g_logp), at(dev_g_entropy),
-                                                                          at(dev_g_lse), (T*)dev_dlogits + r0 * ld_d, ld_d, dev_status);
+            return launch(logprob_bwd_kernel<T, I>, dim3(gx, nr), kBwdThreads, s, (const T*)dev_logits + r0 * ld, vocab, ld,
+                          dev_tokens ? (const I*)dev_tokens + r0 : nullptr, inv_temperature, at(dev_lse), at(dev_entropy), at(dev_g_logp), at(dev_g_entropy),
+                          at(dev_g_lse), (T*)dev_dlogits + r0 * ld_d, ld_d, dev_status);
         };
-        auto by_id = [&](auto t) { if (token_bytes == 8) go(t, int64_t()); else go(t, int32_t()); };
-        if (dtype == PB_F32) by_id(float()); else if (dtype == PB_BF16) by_id(__nv_bfloat16()); else by_id(__half());
-        const int rc = launched("pb_logprob_backward");
+        auto by_id = [&](auto t) { return token_bytes == 8 ? go(t, int64_t()) : go(t, int32_t()); };
+        const int rc = launched("pb_logprob_backward", dtype == PB_F32 ? by_id(float()) : dtype == PB_BF16 ? by_id(__nv_bfloat16()) : by_id(__half()));
         if (rc != PB_OK) return rc;
     }
     return PB_OK;
@@ -435,9 +438,8 @@ int pb_adamw_moments(const void* dev_m, const float* dev_m_scale, const void* de
     PB_REFUSE(!aligned(dev_m_scale, 4) || !aligned(dev_v_scale, 4) || !aligned(dev_m_out, 4) || !aligned(dev_v_out, 4),
               "pb_adamw_moments: a pointer is not aligned to its element");
     const bool vec = aligned(dev_m, 8) && aligned(dev_v, 8) && aligned(dev_m_out, 32) && aligned(dev_v_out, 32);
-    adamw_moments_kernel<<<(unsigned)((n + kAdamRound - 1) / kAdamRound), kAdamThreads, 0, (cudaStream_t)stream>>>(
-        (const unsigned char*)dev_m, dev_m_scale, (const unsigned char*)dev_v, dev_v_scale, n, dev_m_out, dev_v_out, vec);
-    return launched("pb_adamw_moments");
+    return launched("pb_adamw_moments", launch(adamw_moments_kernel, dim3((unsigned)((n + kAdamRound - 1) / kAdamRound)), kAdamThreads, (cudaStream_t)stream,
+                                               (const unsigned char*)dev_m, dev_m_scale, (const unsigned char*)dev_v, dev_v_scale, n, dev_m_out, dev_v_out, vec));
 }
 
 }  // extern "C"

@@ -33,6 +33,7 @@ bool dtype_ok(int dtype) { return dtype == PB_F32 || dtype == PB_BF16 || dtype =
 bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
 constexpr int64_t kMaxCount = 0x7fffffff;       // rows, tokens, vocabulary, dimension
+constexpr int kSms = 148;                       // of a B200: what splits and waves are cut for; any number is right
 
 // Bytes from the first element of a [rows, cols] matrix with row stride ld to behind its last.
 size_t extent(int64_t rows, int64_t cols, int64_t ld, size_t elem) {
@@ -84,8 +85,9 @@ cudaError_t launch_cluster(void (*kernel)(P...), int size, int64_t blocks, int t
 
 // Sizes and scratch layout of the embedding gradient.
 constexpr int64_t kMaxEmbedDim = 1 << 26, kMaxLogprobVocab = 1 << 30;
-// Blocks per SM that the reduction's stretches are cut for; four are resident.  More and shorter
-// stretches even out the tail: 65536 tokens of 2048 columns take 230 us at 4, 192 at 8, 189 at 16.
+// Blocks per SM that the reduction's stretches are cut for.  Four are resident for 16-bit rows in pieces of four columns,
+// three for float32 ones, two for rows that move column by column.  More and shorter stretches even out the tail:
+// 65536 tokens of 2048 columns take 230 us at 4, 192 at 8, 189 at 16.
 constexpr int kRedWave = 16;
 
 struct EmbedPlan {
@@ -116,7 +118,7 @@ EmbedPlan embed_plan(int64_t n, int64_t vocab, int64_t dim, char* scratch) {
     // column keep to 16 at least, since a stretch's end costs them more (17892 tokens of 754 columns: 57 us with 16, 67
     // with 8; 2047 of 1000 columns in pieces: 24 and 21).
     const int per_block = kRedThreads / r.lanes;
-    const int64_t want = (n * e.slabs / ((int64_t)148 * kRedWave * per_block) + 7) / 8 * 8;
+    const int64_t want = (n * e.slabs / ((int64_t)kSms * kRedWave * per_block) + 7) / 8 * 8;
     const int most = kRedEntries / per_block < 128 ? kRedEntries / per_block : 128;
     const int least = dim % 4 && most >= 16 ? 16 : 8;
     r.len = (int)(want < least ? least : want > most ? most : want);
@@ -211,7 +213,7 @@ int pb_embed_forward(const void* dev_table, int dtype, int64_t vocab, int64_t di
     while (lanes < 256 && lanes < pieces) lanes *= 2;
     // Four tokens per group once that still gives every SM eight blocks; a few long rows are spread over blocks.
     const int64_t groups = 256 / lanes;
-    const bool many = n_tokens >= (int64_t)148 * 8 * 4 * groups;
+    const bool many = n_tokens >= (int64_t)kSms * 8 * 4 * groups;
     const int64_t blocks = (n_tokens + (many ? 4 : 1) * groups - 1) / ((many ? 4 : 1) * groups);
     const int64_t walks = (pieces + lanes - 1) / lanes;
     const int64_t spread = many ? 1 : walks < 16 ? walks : 16;
@@ -323,8 +325,8 @@ int pb_logprob_forward(const void* dev_logits, int dtype, int64_t rows, int64_t 
     // of a block still has a piece.
     const int64_t pieces = vocab / (2048 / (int64_t)dtype_bytes(dtype));
     int parts = 1;
-    while (parts < kMaxCluster && rows * parts * 2 <= 148 * 4 && pieces >= (int64_t)parts * kFwdWarps) parts *= 2;
-    const bool few = parts == 1 && pieces < kMaxFewSegments && rows > 148 * 4;       // short rows: two warps each
+    while (parts < kMaxCluster && rows * parts * 2 <= kSms * 4 && pieces >= (int64_t)parts * kFwdWarps) parts *= 2;
+    const bool few = parts == 1 && pieces < kMaxFewSegments && rows > kSms * 4;       // short rows: two warps each
     int per_segment = 1;
     while (pieces / per_segment + 1 > kMaxSegments) per_segment *= 2;
     auto go = [&](auto t, auto i) {

@@ -29,10 +29,11 @@ constexpr int kMaxTop = 32;
 // element.  So at most 32 segments are read again, from L2.
 // A few rows are split over a cluster of blocks, joined through distributed shared memory.
 //
-// Bound by memory traffic for long rows: 4096 x 100003 bf16 take 137 us without alternatives (6.0 TB/s of 6.6)
-// and 166 us with 8; per logit it issues some 9 instructions and one exponential, which four blocks per SM
-// overlap with the copies (register double-buffering instead of copies to shared memory: 200 us).  Short
-// batches are bound by latency: one row of 131072 takes 4.6 us, 8.8 us with 20 alternatives.
+// Bound by memory traffic for long rows: among 50 to 500 calls in a row, 4096 x 100003 bf16 take 143 to 149 us
+// without alternatives (5.6 TB/s of 6.6) and 169 to 175 with 8; the first calls after an idle time take some 25 us
+// more.  Per logit it issues some 9 instructions and one exponential, which four blocks per SM overlap with the
+// copies (register double-buffering instead of copies to shared memory: 40 us more).  Short batches are bound by
+// latency: one row of 131072 takes 4.4 us on the device, 8.5 with 20 alternatives.
 constexpr int kFwdWarps = 8, kFwdFewWarps = 2;   // warps of a block; few for rows of a few pieces
 constexpr int kEight = 256;                 // logits of a warp, eight per lane
 constexpr int kQuads = 4;                   // 16-byte quads of a lane in a piece
@@ -125,7 +126,7 @@ struct FwdPiece {
 template <typename T>
 struct FwdRow {
     const T* x;
-    int vocab, head;                        // head: logits before the first aligned one
+    int head;                               // logits before the first aligned one
     // eight logits of a lane from logit `at` + 8 lane on; -inf from `end` on
     __device__ __forceinline__ void load(float (&f)[8], int at, int end, int lane) const {
         const int i = at + 8 * lane;
@@ -385,7 +386,6 @@ logprob_fwd_kernel(const T* __restrict__ logits, int vocab, long long ld, const 
     const long long r = blockIdx.x / parts;
     FwdRow<T> row;
     row.x = logits + r * ld;
-    row.vocab = vocab;
     constexpr int ALIGN = 8 * (int)sizeof(T);
     row.head = min(vocab, (int)((-(long long)reinterpret_cast<uintptr_t>(row.x)) & (ALIGN - 1)) / (int)sizeof(T));
     // Segments: the pieces, `per_segment` at a time, the logits before the first and behind the last full piece

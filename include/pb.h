@@ -329,7 +329,7 @@ int pb_embed_forward(const void* dev_table, int dtype, int64_t vocab, int64_t di
                      void* dev_out, int64_t ld_out, int32_t* dev_status, void* stream);
 
 /* Its gradient: with S_v = sum of dout[t, :] over the t with id_t = v (float32, in an order
- * that depends on the ids alone), dtable[v, :] = scale * S_v, rounded once.  accumulate = 0
+ * that depends on the ids alone), dtable[v, :] = scale * S_v, a float32 product rounded to dtable's type.  accumulate = 0
  * writes every row (zeros where no token points); accumulate = 1 adds to what is there (a
  * gradient over several batches; the gradient of a table that is also the output head) and
  * leaves rows without tokens untouched.  padding_idx: a row that gets no gradient, or -1.
@@ -387,8 +387,9 @@ int pb_logprob_backward(const void* dev_logits, int dtype, int64_t rows, int64_t
  * state_bits 32: m and v are float32.  state_bits 8: m and v are one byte per element and
  * m_scale / v_scale one float32 per 256 elements of the tensor (ceil(n / 256)); zero bytes and
  * scales are a fresh state.  m is held as e4m3, sqrt(v) as an unsigned float of 4 exponent and 4
- * mantissa bits, rounded at random by `seed`, the step number, the tensor's place in the list
- * and the element: the same call gives the same result.  A block of 256 with a moment that is
+ * mantissa bits, rounded at random by seed + step number, the tensor's place in the list
+ * and the element: the same call gives the same result.  (Only that sum counts: step t + 1 of one seed rounds
+ * like step t of the next, so runs that are to be independent take seeds further apart than their steps.)  A block of 256 with a moment that is
  * not finite reads back as NaN.  A block of m whose largest magnitude is below 2^-100 is
  * held as zeros.  In u, a v below 2^-126 counts as zero where that is less than 2^-25 of eps.
  * *dev_grad_scale (device, NULL: 1) is the product of whatever clipping and loss scaling leave;

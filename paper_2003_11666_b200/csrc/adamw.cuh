@@ -331,11 +331,12 @@ __device__ __forceinline__ void adamw_block(const AdamScalars& a, const AdamTens
 // A thread block takes one round of kAdamRound elements.  What is in flight at any time is then one
 // contiguous stretch of every array, which the DRAM's open pages reward: blocks of four consecutive
 // rounds move an 8-bit step's bytes at 4.6 TB/s, single rounds at 6.5 (151 M elements, no arithmetic).
-// Measured: 32-bit states, float32 gradients and a bf16 copy, 63 M elements: 281 us, 6.7 TB/s, the copy
-// rate.  8-bit states, bf16 gradients and copy, 151 M elements: 465 us, 5.2 TB/s; there some 70
+// Measured: 32-bit states, float32 gradients and a bf16 copy, 63 M elements: 277 us, 6.8 TB/s, the copy
+// rate.  8-bit states, bf16 gradients and copy, 151 M elements: 443 us, 5.5 TB/s; there some 70
 // instructions per element (roundings that have to be exact, random numbers, two encodings) take
-// nearly as long to issue as the bytes take to move.  Seven blocks of 128 threads beat four of 256 (480 us)
-// and eight (473 us, spilling).  Inputs copied ahead into shared memory by the warp that uses them did not help.
+// nearly as long to issue as the bytes take to move.  Seven blocks of 128 threads, 72 registers and a few spilled
+// ones, beat four of 256 and eight of 128 by 2 to 3 %.  Inputs copied ahead into shared memory by the warp that
+// uses them did not help.
 template <int BITS, typename GT, int MAXT>
 __global__ void __launch_bounds__(kAdamThreads, 7)
 adamw_kernel(const __grid_constant__ AdamTable<MAXT> a) {

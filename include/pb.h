@@ -311,7 +311,8 @@ int pb_mlp_run_static(const int32_t* sizes, int n_sizes, float lr, float momentu
  * models are trained with.  They work on the caller's device memory, keep nothing
  * between calls, allocate nothing, do not synchronise and can be captured into a CUDA
  * graph.  All pointers belong to the device that is current at the call, on which
- * `stream` lives; pointers need the alignment of one element.  Errors: status code,
+ * `stream` lives; pointers need the alignment of one element.  What a call writes must not
+ * overlap anything else of that call, except where this says so.  Errors: status code,
  * text via pb_last_error(NULL) on the same thread.  Sizes are checked before anything is
  * launched.
  *

@@ -74,7 +74,7 @@ def _check_values(x, dtype, it, k, offset=0):
     tz, te = _logprob_tolerance(xs, it, rows)
     big = float(np.finfo(np.float32).max)                         # what float32 cannot hold is infinite
     for got, ref, tol in ((lse, rz, tz), (logp, rl, tz), (entropy, re, te), (top, rt, tz[:, None])):
-        ref = np.where(np.abs(ref) > big * (1 + U), np.sign(ref) * np.inf, ref)
+        ref = np.where(np.abs(ref) > big * (1 + U), np.copysign(np.inf, ref), ref)
         with np.errstate(invalid="ignore"):
             _close(_np(got), ref, tol + np.where(np.isfinite(ref), 2 * U * np.abs(ref), 0.0))
     np.testing.assert_array_equal(ids.cpu().numpy(), ri)

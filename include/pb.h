@@ -378,6 +378,38 @@ int pb_logprob_backward(const void* dev_logits, int dtype, int64_t rows, int64_t
                         const float* dev_g_logp, const float* dev_g_entropy, const float* dev_g_lse,
                         void* dev_dlogits, int64_t ld_d, int32_t* dev_status, void* stream);
 
+/* The same log probabilities straight from hidden states and the output head, without a matrix
+ * of logits: logits[r, v] = hidden[r, :] . weight[v, :], hidden: [rows, dim] with row stride
+ * ld_hidden, weight: [vocab, dim] (an embedding table will do) with row stride ld_weight, both of
+ * `dtype`.  logp, entropy, lse are those of pb_logprob_forward (the cross entropy is -logp); each
+ * may be NULL, logp and tokens are given together.  Products are summed in float32; float32
+ * operands are multiplied to 2^-23 of their products.  A row that meets a value that is not finite has NaN, or for
+ * infinite logits what pb_logprob_forward says.  rows and vocab are at most 2^24, dim 2^20.
+ * dev_scratch: pb_head_scratch_bytes(...) bytes, 256-byte aligned, not used by another call that may run
+ * at the same time (two captured graphs included); aligned_rows says that every row of a 16-bit hidden and
+ * weight starts on 16 bytes (rows that do not are copied through the scratch).  Should a kernel give up
+ * waiting for its own copies, *dev_status is 2 and values that depend on them are NaN. */
+size_t pb_head_scratch_bytes(int dtype, int64_t rows, int64_t vocab, int64_t dim, int aligned_rows, int backward);
+int pb_head_logprob_forward(const void* dev_hidden, const void* dev_weight, int dtype, int64_t rows, int64_t vocab, int64_t dim,
+                            int64_t ld_hidden, int64_t ld_weight, const void* dev_tokens, int token_bytes, double inv_temperature,
+                            float* dev_logp, float* dev_entropy, float* dev_lse, void* dev_scratch, size_t scratch_bytes,
+                            int32_t* dev_status, void* stream);
+
+/* Gradients with respect to the hidden states and the head, from lse (and entropy, where its gradient is
+ * given) of the forward call: with d[r, v] the gradient with respect to the logits as in
+ * pb_logprob_backward, dhidden = d weight (of `dtype`, row stride ld_dhidden) and
+ * dweight = d^T hidden (float32 or of `dtype`, row stride ld_dweight).  accumulate = 1 adds to the dweight that is
+ * there (several batches; a table that is also the embedding, see pb_embed_backward).  Either
+ * gradient may be NULL, not both.  d is formed for a piece of the vocabulary at a time and held in
+ * the operands' type, scaled by a power of two so that it does not underflow: 16-bit operands give gradients whose terms are
+ * off by up to 2^-9 (bfloat16) or 2^-12 (float16) of themselves, whatever the type of dweight.  rows == 0 clears dweight,
+ * or leaves it if accumulate.  PB_E_ARG if a buffer that is written overlaps another. */
+int pb_head_logprob_backward(const void* dev_hidden, const void* dev_weight, int dtype, int64_t rows, int64_t vocab, int64_t dim,
+                             int64_t ld_hidden, int64_t ld_weight, const void* dev_tokens, int token_bytes, double inv_temperature,
+                             const float* dev_lse, const float* dev_entropy, const float* dev_g_logp, const float* dev_g_entropy,
+                             const float* dev_g_lse, void* dev_dhidden, int64_t ld_dhidden, void* dev_dweight, int dweight_dtype,
+                             int64_t ld_dweight, int accumulate, void* dev_scratch, size_t scratch_bytes, int32_t* dev_status, void* stream);
+
 /* One AdamW step over n_tensors tensors:
  *   g = grad * *dev_grad_scale,  m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2,
  *   u = (m / (1 - beta1^step)) / (sqrt(v / (1 - beta2^step)) + eps),

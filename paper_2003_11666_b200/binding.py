@@ -23,7 +23,8 @@ EXPORTS = [
     "pb_set_update_size", "pb_kernel_min_bytes", "pb_bench_l2_bandwidth", "pb_bench_fp32_fma",
     "pb_split_plan", "pb_create_split", "pb_split_range", "pb_split_ports", "pb_split_connect",
     "pb_embed_forward", "pb_embed_scratch_bytes", "pb_embed_backward", "pb_logprob_forward",
-    "pb_logprob_backward", "pb_adamw_step", "pb_adamw_moments",
+    "pb_logprob_backward", "pb_adamw_step", "pb_adamw_moments", "pb_head_scratch_bytes",
+    "pb_head_logprob_forward", "pb_head_logprob_backward",
 ]
 
 
@@ -116,6 +117,11 @@ def load_library():
     lib.pb_logprob_backward.argtypes = [vp, i32, i64, i64, i64, vp, i32, C.c_double, vp, vp, vp, vp, vp, vp, i64, vp, vp]
     lib.pb_adamw_step.argtypes = [C.POINTER(pb_adamw_tensor), C.POINTER(vp), i32, C.POINTER(pb_adamw_args), vp]
     lib.pb_adamw_moments.argtypes = [vp, vp, vp, vp, i64, vp, vp, vp]
+    lib.pb_head_scratch_bytes.argtypes = [i32, i64, i64, i64, i32, i32]
+    lib.pb_head_scratch_bytes.restype = C.c_size_t
+    lib.pb_head_logprob_forward.argtypes = [vp, vp, i32, i64, i64, i64, i64, i64, vp, i32, C.c_double, vp, vp, vp, vp, C.c_size_t, vp, vp]
+    lib.pb_head_logprob_backward.argtypes = [vp, vp, i32, i64, i64, i64, i64, i64, vp, i32, C.c_double, vp, vp, vp, vp, vp, vp, i64, vp, i32, i64, i32,
+                                             vp, C.c_size_t, vp, vp]
     _lib = lib
     return lib
 

@@ -1,0 +1,379 @@
+// C entry points of the log probabilities of hidden states under an output head: argument checks, plan, launches.
+// Nothing here allocates, and no state is kept between calls.
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+#include <type_traits>
+
+#include "tok_head.cuh"
+#include "tok_host.h"
+
+namespace pb {
+// pb_api.cu: map of a matrix of 16-bit elements, innermost dimension first, strides in bytes.
+bool tensor_map(CUtensorMap* map, const void* base, int rank, const unsigned long long* dims, const unsigned long long* strides, const unsigned* box);
+}
+
+using namespace pb;
+
+namespace {
+
+constexpr int64_t kMaxHeadRows = 1 << 24, kMaxHeadVocab = 1 << 24, kMaxHeadDim = 1 << 20;
+constexpr int64_t kHeadFewRows = 128;           // rows that one block's tile holds; more run in pairs of blocks
+constexpr int64_t kHeadPieceBytes = 256 << 20;  // of d, or of packed weights, held at a time
+constexpr int64_t kHeadPieceMin = 8192;         // tokens of a piece at least: dhidden's partial sums are read and written once for each
+constexpr int64_t kHeadStatRows = 8192;         // rows whose statistics are held at a time
+constexpr int kHeadPromote = 4;                 // chunks of K that the tensor core adds up by itself where that is to be exact
+constexpr int kHeadNever = 1 << 28;
+
+int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
+
+struct HeadPlan {
+    int cg, planes, terms;
+    bool packed;
+    int64_t dp;                  // row stride of packed operands
+    int64_t piece;               // tokens of a piece of the vocabulary
+    int64_t stat_rows, parts;
+    int64_t ldd, ldp;
+    int splits;
+    int64_t split_chunks;
+    // scratch
+    unsigned short *hidden, *weight, *d;
+    float *part, *ztok, *plane, *unscale;
+    HeadRow* coef;
+    int* row_token;
+    size_t bytes;
+};
+
+HeadPlan head_plan(int dtype, int64_t rows, int64_t vocab, int64_t dim, bool direct, bool backward, char* scratch) {
+    HeadPlan e{};
+    e.cg = rows <= kHeadFewRows ? 1 : 2;
+    e.planes = dtype == PB_F32 ? kHeadPlanes : 1;
+    e.terms = dtype == PB_F32 ? 6 : 1;
+    e.packed = dtype == PB_F32 || !direct;
+    e.dp = up(dim, 8);
+    const int64_t tile = 128 * e.cg;
+    int64_t most = vocab;
+    if (e.packed) most = std::min(most, kHeadPieceBytes / (e.planes * e.dp * 2));
+    if (backward) most = std::min(most, kHeadPieceBytes / (e.planes * rows * 2));
+    e.piece = most >= vocab ? vocab : std::min(vocab, up(std::max(most, kHeadPieceMin), 256));
+    const int64_t pieces = (vocab + e.piece - 1) / e.piece;
+    if (pieces > 1) e.piece = up((vocab + pieces - 1) / pieces, 256);          // of one size, but for the last
+    size_t at = 0;
+    auto take = [&](int64_t bytes) {
+        char* p = scratch ? scratch + at : nullptr;
+        at += (size_t)up(bytes, 256);
+        return p;
+    };
+    if (e.packed) {
+        e.hidden = (unsigned short*)take(e.planes * rows * e.dp * 2);
+        e.weight = (unsigned short*)take(e.planes * e.piece * e.dp * 2);
+    }
+    if (!backward) {
+        e.stat_rows = std::min(rows, kHeadStatRows);
+        for (int64_t v = 0; v < vocab; v += e.piece) e.parts += 2 * ((std::min(e.piece, vocab - v) + tile - 1) / tile);
+        e.part = (float*)take(3 * e.parts * e.stat_rows * 4);
+        e.ztok = (float*)take(e.stat_rows * 4);
+    } else {
+        e.ldd = up(e.piece, 64);
+        e.ldp = up(dim, 8);
+        e.d = (unsigned short*)take(e.planes * rows * e.ldd * 2);
+        // Enough splits of K for every block where dhidden has few tiles, but no shorter than 16 chunks.
+        const int64_t tiles = ((rows + tile - 1) / tile) * ((dim + tile - 1) / tile), chunks = (e.piece + kHeadChunk - 1) / kHeadChunk;
+        const int64_t splits = std::max<int64_t>(1, std::min((kSms / e.cg) / tiles, chunks / 16));
+        e.split_chunks = (chunks + splits - 1) / splits;
+        e.splits = (int)((chunks + e.split_chunks - 1) / e.split_chunks);
+        e.plane = (float*)take(e.splits * rows * e.ldp * 4);
+        e.coef = (HeadRow*)take(rows * (int64_t)sizeof(HeadRow));
+        e.row_token = (int*)take(rows * 4);
+        e.unscale = (float*)take(4);
+    }
+    e.bytes = at;
+    return e;
+}
+
+// A matrix that a product reads: 16-bit elements, planes of [rows, cols] with row stride ld.
+struct HeadMatrix {
+    const void* p;
+    int64_t rows, cols, ld, plane;
+    int planes;
+};
+
+bool map_of(CUtensorMap* map, const HeadMatrix& m, bool mn, int box_rows) {
+    const unsigned long long dims[3] = {(unsigned long long)m.cols, (unsigned long long)m.rows, (unsigned long long)m.planes};
+    const int64_t ld = m.rows > 1 ? m.ld : up(m.cols, 8);    // of a single row any will do
+    const unsigned long long strides[2] = {(unsigned long long)ld * 2, (unsigned long long)std::max(m.plane, ld) * 2};
+    const unsigned box[3] = {64u, mn ? 64u : (unsigned)box_rows, 1u};
+    return tensor_map(map, m.p, 3, dims, strides, box);
+}
+
+// D[m, n] = sum over k of a[m, k] b[n, k]; an MN-major operand lies as [k, m] or [k, n].
+bool job_of(HeadJob& j, int kind, int cg, const HeadMatrix& a, bool a_mn, const HeadMatrix& b, bool b_mn, int64_t chunks_per_split = 0) {
+    const int64_t tile = 128 * cg, m = a_mn ? a.cols : a.rows, n = b_mn ? b.cols : b.rows, k = a_mn ? a.rows : a.cols;
+    const int box = a_mn || m >= 128 ? 128 : (int)up(m, 8);
+    if (!map_of(&j.a, a, a_mn, box) || !map_of(&j.b, b, b_mn, 128)) return false;
+    j.kind = kind;
+    j.a_mn = a_mn; j.b_mn = b_mn;
+    j.a_bytes = a_mn ? kHeadOperand : box * 128;
+    j.tiles_m = (int)((m + tile - 1) / tile);
+    j.tiles_n = (int)((n + tile - 1) / tile);
+    // Row tiles of a group stay in L2 (4096 rows) while the columns go by.
+    j.group_m = kind == kHeadWeight ? 1 : std::min(j.tiles_m, 16);
+    j.chunks = (int)((k + kHeadChunk - 1) / kHeadChunk);
+    j.chunks_per_split = chunks_per_split ? (int)chunks_per_split : j.chunks;
+    j.splits = (j.chunks + j.chunks_per_split - 1) / j.chunks_per_split;
+    j.rows = (int)m;
+    j.cols = (int)n;
+    j.tiles = j.tiles_m * j.tiles_n * j.splits;
+    return true;
+}
+
+template <int CG, int KIND, bool PROMOTE>
+cudaError_t head_launch(const HeadArgs& g, cudaStream_t s) {
+    auto kernel = head_kernel<CG, KIND, PROMOTE>;
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kHeadSmem);
+    if (e != cudaSuccess) return e;
+    int64_t tiles = 0;
+    for (int j = 0; j < g.jobs; ++j) tiles += g.job[j].tiles;
+    cudaLaunchAttribute attr{};
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = CG;
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cudaLaunchConfig_t c{};
+    c.gridDim = dim3((unsigned)(std::min<int64_t>(tiles, kSms / CG) * CG));
+    c.blockDim = dim3(kHeadThreads);
+    c.dynamicSmemBytes = kHeadSmem;
+    c.stream = s;
+    c.attrs = &attr;
+    c.numAttrs = 1;
+    void* args[] = {const_cast<HeadArgs*>(&g)};
+    return cudaLaunchKernelExC(&c, (const void*)kernel, args);
+}
+template <int KIND>
+cudaError_t head_launch(const HeadArgs& g, int cg, bool promote, cudaStream_t s) {
+    if (cg == 2) return promote ? head_launch<2, KIND, true>(g, s) : head_launch<2, KIND, false>(g, s);
+    return promote ? head_launch<1, KIND, true>(g, s) : head_launch<1, KIND, false>(g, s);
+}
+
+cudaError_t pack(int dtype, const void* x, int64_t rows, int64_t dim, int64_t ld, unsigned short* out, int64_t ldp, cudaStream_t s) {
+    const int64_t pairs = rows * (ldp / 2);
+    const dim3 grid((unsigned)std::min<int64_t>((pairs + 255) / 256, kSms * 16));
+    if (dtype == PB_F32) return launch(head_pack_kernel<float>, grid, 256, s, (const float*)x, rows, (int)dim, ld, out, (int)ldp, rows * ldp);
+    return launch(head_pack_kernel<__half>, grid, 256, s, (const __half*)x, rows, (int)dim, ld, out, (int)ldp, rows * ldp);
+}
+
+// Rows that a bulk copy can start on.
+bool direct_rows(const void* p, int64_t rows, int64_t ld) { return aligned(p, 16) && (ld % 8 == 0 || rows == 1); }
+
+int no_map(const char* who) {
+    char text[128];
+    snprintf(text, sizeof text, "%s: no tensor map for an operand", who);
+    return fail_text(PB_E_CUDA, text);
+}
+
+const char* bad_sizes(int dtype, int64_t rows, int64_t vocab, int64_t dim, int64_t ld_hidden, int64_t ld_weight) {
+    if (!dtype_ok(dtype)) return "unknown element type";
+    if (rows < 0 || rows > kMaxHeadRows) return "rows must be between 0 and 2^24";
+    if (vocab < 1 || vocab > kMaxHeadVocab) return "vocab must be between 1 and 2^24";
+    if (dim < 1 || dim > kMaxHeadDim) return "dim must be between 1 and 2^20";
+    if (ld_hidden < dim || ld_weight < dim) return "a row stride is smaller than dim";
+    if (ld_hidden > (int64_t(1) << 36) || ld_weight > (int64_t(1) << 36)) return "a row stride is above 2^36";
+    return nullptr;
+}
+int refuse(const char* who, const char* what) {
+    char text[256];
+    snprintf(text, sizeof text, "%s: %s", who, what);
+    return fail_text(PB_E_ARG, text);
+}
+bool bad_temperature(double it) { return !(it > 0.0) || !std::isfinite((float)(it * 1.5)) || (float)it == 0.f; }
+
+}  // namespace
+
+extern "C" {
+
+size_t pb_head_scratch_bytes(int dtype, int64_t rows, int64_t vocab, int64_t dim, int aligned_rows, int backward) {
+    if (bad_sizes(dtype, rows, vocab, dim, dim, dim)) return 0;
+    return std::max<size_t>(256, head_plan(dtype, std::max<int64_t>(rows, 1), vocab, dim, aligned_rows != 0, backward != 0, nullptr).bytes);
+}
+
+int pb_head_logprob_forward(const void* dev_hidden, const void* dev_weight, int dtype, int64_t rows, int64_t vocab, int64_t dim, int64_t ld_hidden,
+                            int64_t ld_weight, const void* dev_tokens, int token_bytes, double inv_temperature, float* dev_logp, float* dev_entropy,
+                            float* dev_lse, void* dev_scratch, size_t scratch_bytes, int32_t* dev_status, void* stream) {
+    const char* who = "pb_head_logprob_forward";
+    if (const char* bad = bad_sizes(dtype, rows, vocab, dim, ld_hidden, ld_weight)) return refuse(who, bad);
+    if (bad_temperature(inv_temperature)) return refuse(who, "inv_temperature must be positive and finite");
+    if (rows == 0) return PB_OK;
+    if ((dev_logp != nullptr) != (dev_tokens != nullptr)) return refuse(who, "logp and tokens go together");
+    if (dev_tokens && token_bytes != 4 && token_bytes != 8) return refuse(who, "tokens have 4 or 8 bytes");
+    if (!dev_hidden || !dev_weight || !dev_scratch) return refuse(who, "NULL pointer");
+    const size_t es = dtype_bytes(dtype);
+    if (!aligned(dev_hidden, es) || !aligned(dev_weight, es) || (dev_tokens && !aligned(dev_tokens, token_bytes)) || !aligned(dev_logp, 4) ||
+        !aligned(dev_entropy, 4) || !aligned(dev_lse, 4) || !aligned(dev_status, 4)) return refuse(who, "a pointer is not aligned to its element");
+    if (!aligned(dev_scratch, 256)) return refuse(who, "scratch must be 256-byte aligned");
+    const bool direct = direct_rows(dev_hidden, rows, ld_hidden) && direct_rows(dev_weight, vocab, ld_weight);
+    const HeadPlan e = head_plan(dtype, rows, vocab, dim, direct, false, (char*)dev_scratch);
+    if (scratch_bytes < e.bytes) return refuse(who, "scratch is smaller than pb_head_scratch_bytes");
+    const size_t n_h = extent(rows, dim, ld_hidden, es), n_w = extent(vocab, dim, ld_weight, es), n_t = dev_tokens ? (size_t)rows * token_bytes : 0,
+                 n_st = dev_status ? 4 : 0;
+    auto in_scratch = [&](const void* p, size_t n) { return overlap(p, p ? n : 0, dev_scratch, scratch_bytes); };
+    if (in_scratch(dev_hidden, n_h) || in_scratch(dev_weight, n_w) || in_scratch(dev_tokens, n_t) || in_scratch(dev_status, n_st) ||
+        in_scratch(dev_logp, rows * 4) || in_scratch(dev_entropy, rows * 4) || in_scratch(dev_lse, rows * 4)) return refuse(who, "buffers overlap");
+    const cudaStream_t s = (cudaStream_t)stream;
+    const bool half = dtype == PB_F16;
+    const HeadMatrix hidden = e.packed ? HeadMatrix{e.hidden, rows, dim, e.dp, rows * e.dp, e.planes}
+                                       : HeadMatrix{dev_hidden, rows, dim, ld_hidden, 0, 1};
+    cudaError_t err = cudaSuccess;
+    if (e.packed) err = pack(dtype, dev_hidden, rows, dim, ld_hidden, e.hidden, e.dp, s);
+    for (int64_t r0 = 0; r0 < rows && err == cudaSuccess; r0 += e.stat_rows) {
+        const int64_t nr = std::min(e.stat_rows, rows - r0);
+        HeadMatrix a = hidden;
+        a.p = (const unsigned short*)hidden.p + r0 * hidden.ld;
+        a.rows = nr;
+        HeadArgs g{};
+        g.jobs = 1;
+        g.half = half;
+        g.terms = e.terms;
+        g.promote = kHeadPromote;
+        g.c = (float)(inv_temperature * 1.4426950408889634074);
+        g.status = dev_status;
+        g.part = e.part;
+        g.parts = (int)e.parts;
+        g.ztok = e.ztok;
+        g.tokens = dev_tokens ? (const char*)dev_tokens + r0 * token_bytes : nullptr;
+        g.token_bytes = token_bytes;
+        g.vocab = vocab;
+        for (int64_t v0 = 0; v0 < vocab && err == cudaSuccess; v0 += e.piece) {
+            const int64_t nv = std::min(e.piece, vocab - v0);
+            const char* w0 = (const char*)dev_weight + v0 * ld_weight * (int64_t)es;
+            HeadMatrix b{w0, nv, dim, ld_weight, 0, 1};
+            if (e.packed) {
+                if (r0 == 0 || e.piece < vocab) err = pack(dtype, w0, nv, dim, ld_weight, e.weight, e.dp, s);
+                b = HeadMatrix{e.weight, nv, dim, e.dp, nv * e.dp, e.planes};
+            }
+            if (!job_of(g.job[0], kHeadStats, e.cg, a, false, b, false)) return no_map(who);
+            g.col0 = (int)v0;
+            if (err == cudaSuccess) err = head_launch<kHeadStats>(g, e.cg, true, s);
+            g.part0 += 2 * g.job[0].tiles_n;
+        }
+        int width = 1;
+        while (width < 32 && width < nr) width *= 2;
+        auto at = [&](float* p) { return p ? p + r0 : nullptr; };
+        if (err == cudaSuccess)
+            err = launch(head_rows_kernel, dim3((unsigned)((nr + width - 1) / width)), kHeadRowThreads, s, e.part, (int)e.parts, (int)nr, width, e.ztok, g.tokens,
+                         token_bytes, (long long)vocab, g.c, at(dev_logp), at(dev_entropy), at(dev_lse), dev_status);
+    }
+    return launched(who, err);
+}
+
+int pb_head_logprob_backward(const void* dev_hidden, const void* dev_weight, int dtype, int64_t rows, int64_t vocab, int64_t dim, int64_t ld_hidden,
+                             int64_t ld_weight, const void* dev_tokens, int token_bytes, double inv_temperature, const float* dev_lse,
+                             const float* dev_entropy, const float* dev_g_logp, const float* dev_g_entropy, const float* dev_g_lse, void* dev_dhidden,
+                             int64_t ld_dhidden, void* dev_dweight, int dweight_dtype, int64_t ld_dweight, int accumulate, void* dev_scratch,
+                             size_t scratch_bytes, int32_t* dev_status, void* stream) {
+    const char* who = "pb_head_logprob_backward";
+    if (const char* bad = bad_sizes(dtype, rows, vocab, dim, ld_hidden, ld_weight)) return refuse(who, bad);
+    if (bad_temperature(inv_temperature)) return refuse(who, "inv_temperature must be positive and finite");
+    if (accumulate != 0 && accumulate != 1) return refuse(who, "accumulate must be 0 or 1");
+    if (dev_dhidden && ld_dhidden < dim) return refuse(who, "a row stride is smaller than dim");
+    if (dev_dweight) {
+        if (!dtype_ok(dweight_dtype) || (dweight_dtype != PB_F32 && dweight_dtype != dtype)) return refuse(who, "dweight is float32 or of the weight's type");
+        if (ld_dweight < dim) return refuse(who, "a row stride is smaller than dim");
+    }
+    const size_t es = dtype_bytes(dtype), gs = dtype_bytes(dweight_dtype);
+    const cudaStream_t s = (cudaStream_t)stream;
+    if (!dev_dhidden && !dev_dweight) return rows == 0 ? PB_OK : refuse(who, "neither gradient is asked for");
+    if (rows == 0) {
+        if (!dev_dweight || accumulate) return PB_OK;
+        if (!aligned(dev_dweight, gs)) return refuse(who, "a pointer is not aligned to its element");
+        return launched(who, cudaMemset2DAsync(dev_dweight, (size_t)ld_dweight * gs, 0, (size_t)dim * gs, (size_t)vocab, s));
+    }
+    if (!dev_hidden || !dev_weight || !dev_lse || !dev_scratch) return refuse(who, "NULL pointer");
+    if (dev_g_logp && !dev_tokens) return refuse(who, "a gradient of logp needs the tokens");
+    if (dev_g_entropy && !dev_entropy) return refuse(who, "a gradient of the entropy needs the entropy");
+    if (dev_tokens && token_bytes != 4 && token_bytes != 8) return refuse(who, "tokens have 4 or 8 bytes");
+    if (!aligned(dev_hidden, es) || !aligned(dev_weight, es) || (dev_tokens && !aligned(dev_tokens, token_bytes)) || !aligned(dev_lse, 4) ||
+        !aligned(dev_entropy, 4) || !aligned(dev_g_logp, 4) || !aligned(dev_g_entropy, 4) || !aligned(dev_g_lse, 4) || !aligned(dev_dhidden, es) ||
+        !aligned(dev_dweight, gs) || !aligned(dev_status, 4)) return refuse(who, "a pointer is not aligned to its element");
+    if (!aligned(dev_scratch, 256)) return refuse(who, "scratch must be 256-byte aligned");
+    const bool direct = direct_rows(dev_hidden, rows, ld_hidden) && direct_rows(dev_weight, vocab, ld_weight);
+    const HeadPlan e = head_plan(dtype, rows, vocab, dim, direct, true, (char*)dev_scratch);
+    if (scratch_bytes < e.bytes) return refuse(who, "scratch is smaller than pb_head_scratch_bytes");
+    struct Span { const void* p; size_t n; };
+    const size_t nr4 = (size_t)rows * 4;
+    const Span read[] = {{dev_hidden, extent(rows, dim, ld_hidden, es)}, {dev_weight, extent(vocab, dim, ld_weight, es)},
+                         {dev_tokens, dev_tokens ? (size_t)rows * token_bytes : 0}, {dev_lse, nr4}, {dev_entropy, nr4}, {dev_g_logp, nr4},
+                         {dev_g_entropy, nr4}, {dev_g_lse, nr4}};
+    const Span written[] = {{dev_scratch, scratch_bytes}, {dev_dhidden, extent(rows, dim, ld_dhidden, es)},
+                            {dev_dweight, extent(vocab, dim, ld_dweight, gs)}, {dev_status, 4}};
+    for (int k = 0; k < 4; ++k) {
+        if (!written[k].p) continue;
+        for (const Span& r : read)
+            if (r.p && overlap(written[k].p, written[k].n, r.p, r.n)) return refuse(who, "buffers overlap");
+        for (int l = 0; l < k; ++l)
+            if (written[l].p && overlap(written[k].p, written[k].n, written[l].p, written[l].n)) return refuse(who, "buffers overlap");
+    }
+    const bool half = dtype == PB_F16, promote = dtype == PB_F32;
+    cudaError_t err = launch(head_coef_kernel, dim3(1), 1024, s, (int)rows, (long long)vocab, dev_tokens, token_bytes, inv_temperature, dev_lse, dev_entropy,
+                             dev_g_logp, dev_g_entropy, dev_g_lse, half ? 16384.f : 1.f, e.coef, e.row_token, e.unscale, dev_status);
+    if (e.packed && err == cudaSuccess) err = pack(dtype, dev_hidden, rows, dim, ld_hidden, e.hidden, e.dp, s);
+    const HeadMatrix hidden = e.packed ? HeadMatrix{e.hidden, rows, dim, e.dp, rows * e.dp, e.planes}
+                                       : HeadMatrix{dev_hidden, rows, dim, ld_hidden, 0, 1};
+    HeadArgs g{};
+    g.half = half;
+    g.terms = e.terms;
+    g.promote = promote ? kHeadPromote : kHeadNever;
+    g.c = (float)(inv_temperature * 1.4426950408889634074);
+    g.status = dev_status;
+    g.coef = e.coef;
+    g.row_token = e.row_token;
+    g.d = e.d;
+    g.ldd = (int)e.ldd;
+    g.d_plane = rows * e.ldd;
+    g.plane = e.plane;
+    g.plane_size = rows * e.ldp;
+    g.ldp = (int)e.ldp;
+    g.unscale = e.unscale;
+    g.out_type = dweight_dtype;
+    g.ldo = ld_dweight;
+    g.accumulate = accumulate;
+    g.wide = dev_dweight && aligned(dev_dweight, 32) && ld_dweight * (int64_t)gs % 32 == 0;
+    int planes = 0;
+    for (int64_t v0 = 0; v0 < vocab && err == cudaSuccess; v0 += e.piece) {
+        const int64_t nv = std::min(e.piece, vocab - v0);
+        const char* w0 = (const char*)dev_weight + v0 * ld_weight * (int64_t)es;
+        HeadMatrix w{w0, nv, dim, ld_weight, 0, 1};
+        if (e.packed) {
+            err = pack(dtype, w0, nv, dim, ld_weight, e.weight, e.dp, s);
+            w = HeadMatrix{e.weight, nv, dim, e.dp, nv * e.dp, e.planes};
+        }
+        const HeadMatrix d{e.d, rows, nv, e.ldd, g.d_plane, e.planes};
+        g.col0 = (int)v0;
+        g.jobs = 1;
+        if (!job_of(g.job[0], kHeadGrad, e.cg, hidden, false, w, false)) return no_map(who);
+        if (err == cudaSuccess) err = head_launch<kHeadGrad>(g, e.cg, promote, s);
+        g.jobs = 0;
+        g.add = v0 > 0;
+        if (dev_dhidden) {
+            // as many chunks in each split of every piece, so that the first piece has the most splits
+            HeadJob& j = g.job[g.jobs++];
+            if (!job_of(j, kHeadHidden, e.cg, d, false, w, true, e.split_chunks)) return no_map(who);
+            planes = std::max(planes, j.splits);
+        }
+        if (dev_dweight) {
+            g.out = (char*)dev_dweight + v0 * ld_dweight * (int64_t)gs;
+            if (!job_of(g.job[g.jobs++], kHeadWeight, e.cg, d, true, hidden, true)) return no_map(who);
+        }
+        if (err == cudaSuccess) err = head_launch<kHeadHidden>(g, e.cg, promote, s);
+    }
+    if (dev_dhidden && err == cudaSuccess) {
+        const int64_t n = rows * (e.ldp / 8);
+        const dim3 grid((unsigned)std::min<int64_t>((n + 255) / 256, kSms * 16));
+        auto go = [&](auto t) {
+            using T = decltype(t);
+            return launch(head_sum_kernel<T>, grid, 256, s, e.plane, g.plane_size, planes, g.ldp, (int)rows, (int)dim, e.unscale, (T*)dev_dhidden, (long long)ld_dhidden);
+        };
+        err = dtype == PB_F32 ? go(float()) : dtype == PB_BF16 ? go(__nv_bfloat16()) : go(__half());
+    }
+    return launched(who, err);
+}
+
+}  // extern "C"

@@ -56,6 +56,25 @@ int fail_text(int code, const char* text) {
     return code;
 }
 
+// Map of a matrix of 16-bit elements for bulk tensor copies: up to three dimensions, innermost first, strides in bytes,
+// 128-byte swizzle, zero fill outside the matrix.
+bool tensor_map(CUtensorMap* map, const void* base, int rank, const unsigned long long* dims, const unsigned long long* strides, const unsigned* box) {
+    typedef CUresult (*Encode)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
+                               CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+    static const Encode encode = [] {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult qr;
+        const bool found = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &qr) == cudaSuccess && qr == cudaDriverEntryPointSuccess;
+        return found ? reinterpret_cast<Encode>(p) : nullptr;
+    }();
+    cuuint64_t gd[3] = {1, 1, 1}, gs[2] = {0, 0};
+    cuuint32_t bx[3] = {1, 1, 1}, es[3] = {1, 1, 1};
+    for (int q = 0; q < rank; ++q) { gd[q] = dims[q]; bx[q] = box[q]; }
+    for (int q = 0; q + 1 < rank; ++q) gs[q] = strides[q];
+    return encode && encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)rank, const_cast<void*>(base), gd, gs, bx, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 }  // namespace pb
 
 namespace {
@@ -418,42 +437,14 @@ void add_tiles(std::vector<GemmTile>& tiles, int gemm, int M, int N, int nsplit,
 // dimensions, innermost first; strides in bytes for dimensions 1.., 128-byte swizzle, zero
 // fill outside the matrix.  With a null base (the sizing pass before the arena exists) an
 // empty placeholder is filed so that table sizes do not change between the passes.
-typedef CUresult (*TensorMapEncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
-                                      const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                      CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-TensorMapEncodeFn tensor_map_encoder() {
-    static TensorMapEncodeFn fn = nullptr;
-    static bool tried = false;
-    if (!tried) {
-        tried = true;
-        void* p = nullptr;
-        cudaDriverEntryPointQueryResult qr;
-        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &qr) == cudaSuccess && qr == cudaDriverEntryPointSuccess)
-            fn = reinterpret_cast<TensorMapEncodeFn>(p);
-    }
-    return fn;
-}
-
 int add_tensor_map(pb_handle* h, const void* base, int rank, const unsigned long long* dims, const unsigned long long* strides_bytes,
                    const unsigned* box, bool* all_ok) {
-    bool this_ok = true;
-    bool* ok = &this_ok;
-    struct Note { bool* all; bool* one; ~Note() { if (!*one) *all = false; } } note{all_ok, &this_ok};
     CUtensorMap tm;
     std::memset(&tm, 0, sizeof(tm));
-    if (base) {
-        TensorMapEncodeFn enc = tensor_map_encoder();
-        cuuint64_t gd[3] = {1, 1, 1}, gs[2] = {0, 0};
-        cuuint32_t bx[3] = {1, 1, 1}, es[3] = {1, 1, 1};
-        for (int q = 0; q < rank; ++q) { gd[q] = dims[q]; bx[q] = box[q]; }
-        for (int q = 0; q + 1 < rank; ++q) gs[q] = strides_bytes[q];
-        if (!enc || enc(&tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)rank, const_cast<void*>(base), gd, gs, bx, es,
-                        CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
-                        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
-            *ok = false;
-    }
+    const bool ok = !base || tensor_map(&tm, base, rank, dims, strides_bytes, box);
+    if (!ok) *all_ok = false;
     h->h_tmaps.push_back(tm);
-    return *ok ? (int)h->h_tmaps.size() - 1 : -1;       // an operand without a map is gathered instead
+    return ok ? (int)h->h_tmaps.size() - 1 : -1;        // an operand without a map is gathered instead
 }
 
 // Tiles of one grouped tensor-core launch handed to persistent blocks: longest first, each

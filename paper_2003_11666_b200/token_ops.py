@@ -179,6 +179,85 @@ def logprob_backward(logits, tokens, lse, dlogits, g_logp=None, g_entropy=None, 
         _vector(who, "g_lse", g_lse, rows), dlogits.data_ptr(), ld_d, _status(who, status), _current(d) if stream is None else stream))
 
 
+def _head(who, hidden, weight):
+    """Sizes and row strides of the two operands: (rows, vocab, dim, ld_hidden, ld_weight, dtype)."""
+    rows, dim, ldh = _rows(who, "hidden", hidden)
+    vocab, wdim, ldw = _rows(who, "weight", weight)
+    if wdim != dim or weight.dtype is not hidden.dtype:
+        _refuse(who, "weight must be [vocab, dim] of the hidden states' type")
+    return rows, vocab, dim, ldh, ldw, _DTYPE[hidden.dtype]
+
+
+def _scratch(who, t):
+    if t is None or t.dtype is not torch.uint8 or not t.is_contiguous():
+        _refuse(who, "scratch must be a dense uint8 tensor")
+    return t.data_ptr(), t.numel()
+
+
+def head_scratch_bytes(hidden, weight, backward=False):
+    """pb_head_scratch_bytes: bytes of scratch that head_logprob_forward (or _backward) needs for these tensors."""
+    who = "head_scratch_bytes"
+    if not isinstance(hidden, torch.Tensor) or not isinstance(weight, torch.Tensor):
+        _refuse(who, "hidden and weight must be tensors")
+    rows, vocab, dim, ldh, ldw, dtype = _head(who, hidden, weight)
+    whole = all(t.data_ptr() % 16 == 0 and (n <= 1 or ld % 8 == 0) for t, n, ld in ((hidden, rows, ldh), (weight, vocab, ldw)))
+    n = _lib.pb_head_scratch_bytes(dtype, rows, vocab, dim, int(whole), int(bool(backward)))
+    if n == 0:
+        _refuse(who, "sizes out of range")
+    return n
+
+
+def head_logprob_forward(hidden, weight, scratch, tokens=None, logp=None, entropy=None, lse=None, inv_temperature=1.0, status=None, stream=None):
+    """pb_head_logprob_forward: log probabilities of `tokens`, entropies and logsumexps of the rows of hidden @ weight.T, whose
+    logits are not stored.  scratch: uint8 tensor of head_scratch_bytes(hidden, weight) bytes."""
+    who = "head_logprob_forward"
+    d = _device(who, hidden)
+    _on_device(who, d, weight, scratch, tokens, logp, entropy, lse, status)
+    rows, vocab, dim, ldh, ldw, dtype = _head(who, hidden, weight)
+    p, size = None, 4
+    if tokens is not None:
+        p, size = _ids(who, "tokens", tokens)
+        if tokens.numel() != rows:
+            _refuse(who, "tokens must hold one id per row")
+    if (tokens is None) != (logp is None):
+        _refuse(who, "logp and tokens go together")
+    _check(_lib.pb_head_logprob_forward(
+        hidden.data_ptr(), weight.data_ptr(), dtype, rows, vocab, dim, ldh, ldw, p, size, inv_temperature, _vector(who, "logp", logp, rows),
+        _vector(who, "entropy", entropy, rows), _vector(who, "lse", lse, rows), *_scratch(who, scratch), _status(who, status),
+        _current(d) if stream is None else stream))
+
+
+def head_logprob_backward(hidden, weight, scratch, tokens, lse, dhidden=None, dweight=None, g_logp=None, g_entropy=None, entropy=None, g_lse=None,
+                          inv_temperature=1.0, accumulate=False, status=None, stream=None):
+    """pb_head_logprob_backward: gradients with respect to the hidden states and the head.  scratch: uint8 tensor of
+    head_scratch_bytes(hidden, weight, backward=True) bytes."""
+    who = "head_logprob_backward"
+    d = _device(who, hidden)
+    _on_device(who, d, weight, scratch, tokens, lse, dhidden, dweight, g_logp, g_entropy, entropy, g_lse, status)
+    rows, vocab, dim, ldh, ldw, dtype = _head(who, hidden, weight)
+    p, size = None, 4
+    if tokens is not None:
+        p, size = _ids(who, "tokens", tokens)
+        if tokens.numel() != rows:
+            _refuse(who, "tokens must hold one id per row")
+    ld_dh = ld_dw = dim
+    dw_type = dtype
+    if dhidden is not None:
+        r, c, ld_dh = _rows(who, "dhidden", dhidden)
+        if (r, c) != (rows, dim) or dhidden.dtype is not hidden.dtype:
+            _refuse(who, "dhidden must have the hidden states' shape and type")
+    if dweight is not None:
+        r, c, ld_dw = _rows(who, "dweight", dweight)
+        if (r, c) != (vocab, dim):
+            _refuse(who, "dweight must have the weight's shape")
+        dw_type = _DTYPE[dweight.dtype]
+    _check(_lib.pb_head_logprob_backward(
+        hidden.data_ptr(), weight.data_ptr(), dtype, rows, vocab, dim, ldh, ldw, p, size, inv_temperature, _vector(who, "lse", lse, rows),
+        _vector(who, "entropy", entropy, rows), _vector(who, "g_logp", g_logp, rows), _vector(who, "g_entropy", g_entropy, rows),
+        _vector(who, "g_lse", g_lse, rows), None if dhidden is None else dhidden.data_ptr(), ld_dh, None if dweight is None else dweight.data_ptr(), dw_type,
+        ld_dw, 1 if accumulate else 0, *_scratch(who, scratch), _status(who, status), _current(d) if stream is None else stream))
+
+
 def adamw_moments(m, m_scale, v, v_scale, m_out=None, v_out=None, stream=None):
     """pb_adamw_moments: the float32 moments that an 8-bit state stands for."""
     who = "adamw_moments"

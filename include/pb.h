@@ -410,6 +410,67 @@ int pb_head_logprob_backward(const void* dev_hidden, const void* dev_weight, int
                              const float* dev_g_lse, void* dev_dhidden, int64_t ld_dhidden, void* dev_dweight, int dweight_dtype,
                              int64_t ld_dweight, int accumulate, void* dev_scratch, size_t scratch_bytes, int32_t* dev_status, void* stream);
 
+/* Dropout: out[r, c] = x[r, c] / (1 - q) where the element is kept, 0 where it is dropped, with q = p
+ * rounded to a multiple of 2^-16.  Which elements are kept is a function of seed, offset and the
+ * element's place i = r * dim + c alone (16 bits of SplitMix64 of the counter i / 4 on the stream that
+ * SplitMix64 of `offset` on the stream `seed` names), so that no mask is stored: the gradient is the same call
+ * on the gradient of out.  Steps and layers take an offset (or a seed) each; dev_offset (device, may be NULL) takes
+ * its place, so that a captured graph can be replayed with other values.  x: [rows, dim] with row
+ * stride ld_x, out with ld_out, both of `dtype`; the very same buffer and stride is allowed. */
+int pb_dropout(const void* dev_x, int dtype, int64_t rows, int64_t dim, int64_t ld_x, double p, uint64_t seed, int64_t offset,
+               const int64_t* dev_offset, void* dev_out, int64_t ld_out, void* stream);
+
+/* The join of a block's output u to the residual stream x, with the norm behind the block, a gate, dropout
+ * and the norm before the next block, in one pass:
+ *   b = u * rstd_post * post_weight     rstd_post = (mean(u^2) + eps)^-1/2 per row   (b = u if post_weight is NULL)
+ *   y = residual_scale * x + drop(gate * b)          (no gate if NULL; drop: as pb_dropout, by the place in [rows, dim])
+ *   h = y * rstd_pre * pre_weight       rstd_pre = (mean(y^2) + eps)^-1/2 per row    (h and pre_weight go together)
+ * y and x are the stream, of stream_dtype (float32, or dtype); u, h and gate are of dtype; the norms' weights
+ * are float32 or of dtype.  Row r takes row r / rows_per_gate of the gate: 1 is a gate per row, a sequence's length one
+ * per sequence, rows one for all.  Sums are float32, y enters the norm before it is rounded.  The rstds
+ * (float32, [rows], may be NULL) are for the backward.  y may be the very buffer of x, h that of u.  dim is at most 16384. */
+typedef struct {
+    int64_t rows, dim;
+    int32_t dtype, stream_dtype, weight_dtype;
+    float residual_scale, eps;
+    double p;                        /* dropout: see pb_dropout */
+    uint64_t seed;
+    int64_t offset;
+    const int64_t* dev_offset;
+    const void* x; int64_t ld_x;
+    const void* u; int64_t ld_u;
+    const void* gate; int64_t ld_gate, rows_per_gate;
+    const void* post_weight;
+    const void* pre_weight;
+    void* y; int64_t ld_y;
+    void* h; int64_t ld_h;
+    float* rstd_post;
+    float* rstd_pre;
+} pb_join_args;
+
+int pb_join_forward(const pb_join_args* args, void* stream);
+
+/* Its gradient, from y, u and the rstds of the forward call (x and h are not read): of dy (gradient of y, may be
+ * NULL) and dh (of h, may be NULL; with it y, pre_weight and rstd_pre are read) to dx (may be NULL), du, and what else
+ * is given of dgate (one row per row of the gate; float32 or dtype), dpost_weight and dpre_weight (float32 or dtype).
+ * They are written, not added to.  Sums over rows are float32, in an order that depends on the sizes alone.  dx may
+ * be the very buffer of dy, du that of dh.  dev_scratch: pb_join_scratch_bytes(rows, dim, rows_per_gate, or 0 without a
+ * gate) bytes, 256-byte aligned, not used by another call that may run at the same time (two captured
+ * graphs included).  Buffers that overlap otherwise are PB_E_ARG. */
+typedef struct {
+    const void* dy; int64_t ld_dy;
+    const void* dh; int64_t ld_dh;
+    void* dx; int64_t ld_dx;
+    void* du; int64_t ld_du;
+    void* dgate; int64_t ld_dgate;
+    void* dpost_weight;
+    void* dpre_weight;
+    int32_t dgate_dtype, dweight_dtype;
+} pb_join_grads;
+
+size_t pb_join_scratch_bytes(int64_t rows, int64_t dim, int64_t rows_per_gate);
+int pb_join_backward(const pb_join_args* args, const pb_join_grads* grads, void* dev_scratch, size_t scratch_bytes, void* stream);
+
 /* One AdamW step over n_tensors tensors:
  *   g = grad * *dev_grad_scale,  m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2,
  *   u = (m / (1 - beta1^step)) / (sqrt(v / (1 - beta2^step)) + eps),

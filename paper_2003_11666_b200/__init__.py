@@ -7,8 +7,8 @@ binding raises.
 from .binding import PB, PBError, mlp_run_static, split_plan, bench_l2_bandwidth, bench_fp32_fma, PB_SC, PB_LWP, PB_LWP_WFORM, PB_CONV_BF16, PB_WEIGHT_STASH, load_library, LIB_PATH, EXPORTS
 
 # The token operators take torch tensors; torch is imported when one of them is first used.
-_TOKEN_OPS = ("AdamW", "adamw_moments", "embed_backward", "embed_forward", "embed_scratch_bytes", "head_logprob_backward", "head_logprob_forward",
-              "head_scratch_bytes", "logprob_backward", "logprob_forward")
+_TOKEN_OPS = ("AdamW", "adamw_moments", "dropout", "embed_backward", "embed_forward", "embed_scratch_bytes", "head_logprob_backward", "head_logprob_forward",
+              "head_scratch_bytes", "join_backward", "join_forward", "join_scratch_bytes", "logprob_backward", "logprob_forward")
 
 
 def __getattr__(name):

@@ -24,7 +24,8 @@ EXPORTS = [
     "pb_split_plan", "pb_create_split", "pb_split_range", "pb_split_ports", "pb_split_connect",
     "pb_embed_forward", "pb_embed_scratch_bytes", "pb_embed_backward", "pb_logprob_forward",
     "pb_logprob_backward", "pb_adamw_step", "pb_adamw_moments", "pb_head_scratch_bytes",
-    "pb_head_logprob_forward", "pb_head_logprob_backward",
+    "pb_head_logprob_forward", "pb_head_logprob_backward", "pb_dropout", "pb_join_forward",
+    "pb_join_scratch_bytes", "pb_join_backward",
 ]
 
 
@@ -47,6 +48,20 @@ class pb_adamw_args(C.Structure):
                [("step", C.c_int64), ("seed", C.c_uint64)] + \
                [(n, C.c_void_p) for n in ("dev_grad_scale", "dev_lr", "dev_step")] + \
                [(n, C.c_int32) for n in ("grad_dtype", "forward_dtype", "state_bits")]
+
+
+class pb_join_args(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("dim", C.c_int64)] + [(n, C.c_int32) for n in ("dtype", "stream_dtype", "weight_dtype")] + \
+               [("residual_scale", C.c_float), ("eps", C.c_float), ("p", C.c_double), ("seed", C.c_uint64), ("offset", C.c_int64),
+                ("dev_offset", C.c_void_p), ("x", C.c_void_p), ("ld_x", C.c_int64), ("u", C.c_void_p), ("ld_u", C.c_int64),
+                ("gate", C.c_void_p), ("ld_gate", C.c_int64), ("rows_per_gate", C.c_int64), ("post_weight", C.c_void_p),
+                ("pre_weight", C.c_void_p), ("y", C.c_void_p), ("ld_y", C.c_int64), ("h", C.c_void_p), ("ld_h", C.c_int64),
+                ("rstd_post", C.c_void_p), ("rstd_pre", C.c_void_p)]
+
+
+class pb_join_grads(C.Structure):
+    _fields_ = [(n, t) for name in ("dy", "dh", "dx", "du", "dgate") for n, t in ((name, C.c_void_p), ("ld_" + name, C.c_int64))] + \
+               [("dpost_weight", C.c_void_p), ("dpre_weight", C.c_void_p), ("dgate_dtype", C.c_int32), ("dweight_dtype", C.c_int32)]
 
 
 class PBError(RuntimeError):
@@ -122,6 +137,11 @@ def load_library():
     lib.pb_head_logprob_forward.argtypes = [vp, vp, i32, i64, i64, i64, i64, i64, vp, i32, C.c_double, vp, vp, vp, vp, C.c_size_t, vp, vp]
     lib.pb_head_logprob_backward.argtypes = [vp, vp, i32, i64, i64, i64, i64, i64, vp, i32, C.c_double, vp, vp, vp, vp, vp, vp, i64, vp, i32, i64, i32,
                                              vp, C.c_size_t, vp, vp]
+    lib.pb_dropout.argtypes = [vp, i32, i64, i64, i64, C.c_double, C.c_uint64, i64, vp, vp, i64, vp]
+    lib.pb_join_forward.argtypes = [C.POINTER(pb_join_args), vp]
+    lib.pb_join_scratch_bytes.argtypes = [i64, i64, i64]
+    lib.pb_join_scratch_bytes.restype = C.c_size_t
+    lib.pb_join_backward.argtypes = [C.POINTER(pb_join_args), C.POINTER(pb_join_grads), vp, C.c_size_t, vp]
     _lib = lib
     return lib
 

@@ -7,7 +7,7 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libpb_b200.so")
-SOURCES = ["pb_api.cu", "tok_api.cu", "head_api.cu"]
+SOURCES = ["pb_api.cu", "tok_api.cu", "head_api.cu", "join_api.cu"]
 
 
 def _nvcc():

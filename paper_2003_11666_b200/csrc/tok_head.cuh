@@ -423,7 +423,7 @@ struct HeadEpilogue {
         if (g.wide && c0 + 32 <= q.cols) {
 #pragma unroll
             for (int u = 0; u < 32; u += kEach) {
-                if (sizeof(T) == 4) {
+                if constexpr (sizeof(T) == 4) {
                     float v[8];
 #pragma unroll
                     for (int k = 0; k < 8; ++k) v[k] = z[u + k] * unscale;
@@ -442,11 +442,11 @@ struct HeadEpilogue {
                         for (int k = 0; k < 8; ++k) v[k] = z[u + h + k] * unscale;
                         if (g.accumulate) {
                             float old[8];
-                            read8(old, to + u + h);
+                            load8(old, to + u + h);
 #pragma unroll
                             for (int k = 0; k < 8; ++k) v[k] += old[k];
                         }
-                        write8(to + u + h, v);
+                        store8(to + u + h, v);
                     }
                 }
             }
@@ -456,11 +456,6 @@ struct HeadEpilogue {
         for (int u = 0; u < 32; ++u)
             if (c0 + u < q.cols) to[u] = from_f32<T>(g.accumulate ? fmaf(z[u], unscale, to_f32(to[u])) : z[u] * unscale);
     }
-    static __device__ __forceinline__ void read8(float (&x)[8], const float*) {}
-    static __device__ __forceinline__ void write8(float*, const float (&)[8]) {}
-    template <typename T> static __device__ __forceinline__ void read8(float (&x)[8], const T* p) { load8(x, p); }
-    template <typename T> static __device__ __forceinline__ void write8(T* p, const float (&x)[8]) { store8(p, x); }
-
     __device__ __forceinline__ void weight(float (&z)[32], int c0) {
         if (row >= q.rows || c0 >= q.cols) return;
         if (g.out_type == 0) weight_as<float>(z, c0);
@@ -603,7 +598,7 @@ __global__ void __launch_bounds__(256) head_pack_kernel(const T* x, long long ro
         const int c = (int)(i - r * pairs) * 2;
         const T* p = x + r * ld + c;
         unsigned* to = (unsigned*)(out + r * ldp + c);
-        if (sizeof(T) == 2) {
+        if constexpr (sizeof(T) == 2) {
             const unsigned short* q = (const unsigned short*)p;
             *to = (c < dim ? (unsigned)q[0] : 0u) | (c + 1 < dim ? (unsigned)q[1] << 16 : 0u);
         } else {

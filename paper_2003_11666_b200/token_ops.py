@@ -11,7 +11,7 @@ import ctypes as C
 
 import torch
 
-from .binding import PBError, load_library, pb_adamw_args, pb_adamw_tensor
+from .binding import PBError, load_library, pb_adamw_args, pb_adamw_tensor, pb_join_args, pb_join_grads
 
 _DTYPE = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 _ID_BYTES = {torch.int64: 8, torch.int32: 4}
@@ -256,6 +256,110 @@ def head_logprob_backward(hidden, weight, scratch, tokens, lse, dhidden=None, dw
         _vector(who, "entropy", entropy, rows), _vector(who, "g_logp", g_logp, rows), _vector(who, "g_entropy", g_entropy, rows),
         _vector(who, "g_lse", g_lse, rows), None if dhidden is None else dhidden.data_ptr(), ld_dh, None if dweight is None else dweight.data_ptr(), dw_type,
         ld_dw, 1 if accumulate else 0, *_scratch(who, scratch), _status(who, status), _current(d) if stream is None else stream))
+
+
+def dropout(x, out, p, seed, offset=0, dev_offset=None, stream=None):
+    """pb_dropout: out = x / (1 - p) where kept, else 0; of matrices [rows, dim].  The gradient is the same call on out's gradient."""
+    who = "dropout"
+    d = _device(who, x)
+    _on_device(who, d, out, dev_offset)
+    rows, dim, ld = _rows(who, "x", x)
+    orows, odim, ld_out = _rows(who, "out", out)
+    if (orows, odim) != (rows, dim) or out.dtype is not x.dtype:
+        _refuse(who, "out must have x's shape and type")
+    _check(_lib.pb_dropout(x.data_ptr(), _DTYPE[x.dtype], rows, dim, ld, p, seed & 0xFFFFFFFFFFFFFFFF, offset, _vector(who, "dev_offset", dev_offset, 1, torch.int64),
+                           out.data_ptr(), ld_out, _current(d) if stream is None else stream))
+
+
+def _join_weights(who, dim, post_weight, pre_weight):
+    """Type of the norms' weights, which have one."""
+    given = [w for w in (post_weight, pre_weight) if w is not None]
+    if not given:
+        return torch.float32
+    if any(w.dtype not in _DTYPE or w.dtype is not given[0].dtype for w in given):
+        _refuse(who, "the norms' weights must be of one type")
+    return given[0].dtype
+
+
+def _join_like(who, name, t, rows, dim, dtype):
+    """Address and row stride of a [rows, dim] matrix that may be absent."""
+    if t is None:
+        return None, dim
+    r, c, ld = _rows(who, name, t)
+    if (r, c) != (rows, dim) or t.dtype is not dtype:
+        _refuse(who, "%s must be [rows, dim] of type %s" % (name, dtype))
+    return t.data_ptr(), ld
+
+
+def _join_args(who, u, stream_dtype, gate, rows_per_gate, post_weight, pre_weight, rstd_post, rstd_pre, residual_scale, eps, p, seed, offset, dev_offset):
+    rows, dim, ld = _rows(who, "u", u)
+    a = pb_join_args()
+    a.rows, a.dim, a.u, a.ld_u = rows, dim, u.data_ptr(), ld
+    weights = _join_weights(who, dim, post_weight, pre_weight)
+    a.dtype, a.stream_dtype, a.weight_dtype = _DTYPE[u.dtype], _DTYPE[stream_dtype], _DTYPE[weights]
+    a.residual_scale, a.eps, a.p, a.seed, a.offset = residual_scale, eps, p, seed & 0xFFFFFFFFFFFFFFFF, offset
+    a.dev_offset = _vector(who, "dev_offset", dev_offset, 1, torch.int64)
+    if gate is not None:
+        per = rows if rows_per_gate is None else rows_per_gate
+        if rows and per < 1:
+            _refuse(who, "rows_per_gate must be at least 1")
+        a.gate, a.ld_gate = _join_like(who, "gate", gate, -(-rows // max(per, 1)), dim, u.dtype)
+        a.rows_per_gate = max(per, 1)
+    a.post_weight, a.pre_weight = _vector(who, "post_weight", post_weight, dim, weights), _vector(who, "pre_weight", pre_weight, dim, weights)
+    a.rstd_post, a.rstd_pre = _vector(who, "rstd_post", rstd_post, rows), _vector(who, "rstd_pre", rstd_pre, rows)
+    return a
+
+
+def join_forward(x, u, y, h=None, pre_weight=None, post_weight=None, gate=None, rows_per_gate=None, rstd_pre=None, rstd_post=None, residual_scale=1.0,
+                 eps=1e-6, p=0.0, seed=0, offset=0, dev_offset=None, stream=None):
+    """pb_join_forward: y = residual_scale * x + dropout(gate * norm(u)), h = norm(y).  A norm is there if its weight is; gate:
+    [ceil(rows / rows_per_gate), dim] (rows_per_gate None: one row for all)."""
+    who = "join_forward"
+    d = _device(who, x)
+    _on_device(who, d, u, y, h, pre_weight, post_weight, gate, rstd_pre, rstd_post, dev_offset)
+    if u is None or y is None or x.dtype not in _DTYPE:
+        _refuse(who, "x, u and y are needed, of float32, bfloat16 or float16")
+    a = _join_args(who, u, x.dtype, gate, rows_per_gate, post_weight, pre_weight, rstd_post, rstd_pre, residual_scale, eps, p, seed, offset, dev_offset)
+    a.x, a.ld_x = _join_like(who, "x", x, a.rows, a.dim, x.dtype)
+    a.y, a.ld_y = _join_like(who, "y", y, a.rows, a.dim, x.dtype)
+    a.h, a.ld_h = _join_like(who, "h", h, a.rows, a.dim, u.dtype)
+    _check(_lib.pb_join_forward(C.byref(a), _current(d) if stream is None else stream))
+
+
+def join_scratch_bytes(rows, dim, rows_per_gate=0):
+    """pb_join_scratch_bytes: bytes of scratch that join_backward needs for these sizes (rows_per_gate 0: no gate)."""
+    n = _lib.pb_join_scratch_bytes(int(rows), int(dim), int(rows_per_gate))
+    if n == 0:
+        _refuse("join_scratch_bytes", "sizes out of range")
+    return n
+
+
+def join_backward(y, u, dx, du, scratch, dy=None, dh=None, pre_weight=None, post_weight=None, gate=None, rows_per_gate=None, rstd_pre=None, rstd_post=None,
+                  dpre_weight=None, dpost_weight=None, dgate=None, residual_scale=1.0, p=0.0, seed=0, offset=0, dev_offset=None, stream=None):
+    """pb_join_backward: gradients of a join_forward call with the same settings, from its y, u and rstds.  scratch: uint8 tensor of
+    join_scratch_bytes(...) bytes; y may be None without dh, dx if it is not wanted."""
+    who = "join_backward"
+    d = _device(who, u)
+    _on_device(who, d, y, dx, du, scratch, dy, dh, pre_weight, post_weight, gate, rstd_pre, rstd_post, dpre_weight, dpost_weight, dgate, dev_offset)
+    stream_dtype = next((t.dtype for t in (y, dy, dx) if t is not None), u.dtype)
+    if du is None or stream_dtype not in _DTYPE:
+        _refuse(who, "du is needed, and the stream of float32, bfloat16 or float16")
+    a = _join_args(who, u, stream_dtype, gate, rows_per_gate, post_weight, pre_weight, rstd_post, rstd_pre, residual_scale, 0.0, p, seed, offset, dev_offset)
+    g = pb_join_grads()
+    a.y, a.ld_y = _join_like(who, "y", y, a.rows, a.dim, stream_dtype)
+    g.dy, g.ld_dy = _join_like(who, "dy", dy, a.rows, a.dim, stream_dtype)
+    g.dh, g.ld_dh = _join_like(who, "dh", dh, a.rows, a.dim, u.dtype)
+    g.dx, g.ld_dx = _join_like(who, "dx", dx, a.rows, a.dim, stream_dtype)
+    g.du, g.ld_du = _join_like(who, "du", du, a.rows, a.dim, u.dtype)
+    if dgate is not None:
+        if gate is None or dgate.dtype not in _DTYPE:
+            _refuse(who, "dgate goes with a gate, and is of float32 or of its type")
+        g.dgate, g.ld_dgate = _join_like(who, "dgate", dgate, gate.shape[0], a.dim, dgate.dtype)
+        g.dgate_dtype = _DTYPE[dgate.dtype]
+    weights = _join_weights(who, a.dim, dpost_weight, dpre_weight)
+    g.dweight_dtype = _DTYPE[weights]
+    g.dpost_weight, g.dpre_weight = _vector(who, "dpost_weight", dpost_weight, a.dim, weights), _vector(who, "dpre_weight", dpre_weight, a.dim, weights)
+    _check(_lib.pb_join_backward(C.byref(a), C.byref(g), *_scratch(who, scratch), _current(d) if stream is None else stream))
 
 
 def adamw_moments(m, m_scale, v, v_scale, m_out=None, v_out=None, stream=None):

@@ -9,8 +9,9 @@
 #include "tok_host.h"
 
 namespace pb {
-// pb_api.cu: map of a matrix of 16-bit elements, innermost dimension first, strides in bytes.
-bool tensor_map(CUtensorMap* map, const void* base, int rank, const unsigned long long* dims, const unsigned long long* strides, const unsigned* box);
+// pb_api.cu: map of a matrix of 16-bit (or float32) elements, innermost dimension first, strides in bytes.
+bool tensor_map(CUtensorMap* map, const void* base, int rank, const unsigned long long* dims, const unsigned long long* strides, const unsigned* box,
+                bool ahead, bool f32);
 }
 
 using namespace pb;
@@ -22,8 +23,13 @@ constexpr int64_t kHeadFewRows = 128;           // rows that one block's tile ho
 constexpr int64_t kHeadPieceBytes = 256 << 20;  // of d, or of packed weights, held at a time
 constexpr int64_t kHeadPieceMin = 8192;         // tokens of a piece at least: dhidden's partial sums are read and written once for each
 constexpr int64_t kHeadStatRows = 8192;         // rows whose statistics are held at a time
-constexpr int kHeadPromote = 4;                 // chunks of K that the tensor core adds up by itself where that is to be exact
+// Chunks of K that the tensor core adds up by itself.  It does not round to nearest, so its sums drift towards zero: log probabilities
+// of normal logits are off by 2e-7 of themselves after 1024 columns, 8e-7 after 4096, 1.7e-6 after 8192.
+constexpr int kHeadPromote = 4;                 // float32 operands: 6e-8
+constexpr int kHeadPromoteLong = 32;            // 16-bit ones of more than kHeadLong chunks in the forward: 4096 x 131072 x 4096 takes 3.40 ms
+constexpr int kHeadLong = 64;                   // without, 3.51 with 16 chunks, 4.10 with 4
 constexpr int kHeadNever = 1 << 28;
+constexpr int kHeadTileCost = 2;                // what a tile costs beside its chunks, in chunks
 
 int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 
@@ -70,7 +76,7 @@ HeadPlan head_plan(int dtype, int64_t rows, int64_t vocab, int64_t dim, bool dir
     }
     if (!backward) {
         e.stat_rows = std::min(rows, kHeadStatRows);
-        for (int64_t v = 0; v < vocab; v += e.piece) e.parts += 2 * ((std::min(e.piece, vocab - v) + tile - 1) / tile);
+        for (int64_t v = 0; v < vocab; v += e.piece) e.parts += (std::min(e.piece, vocab - v) + tile - 1) / tile;
         e.part = (float*)take(3 * e.parts * e.stat_rows * 4);
         e.ztok = (float*)take(e.stat_rows * 4);
     } else {
@@ -103,7 +109,23 @@ bool map_of(CUtensorMap* map, const HeadMatrix& m, bool mn, int box_rows) {
     const int64_t ld = m.rows > 1 ? m.ld : up(m.cols, 8);    // of a single row any will do
     const unsigned long long strides[2] = {(unsigned long long)ld * 2, (unsigned long long)std::max(m.plane, ld) * 2};
     const unsigned box[3] = {64u, mn ? 64u : (unsigned)box_rows, 1u};
-    return tensor_map(map, m.p, 3, dims, strides, box);
+    return tensor_map(map, m.p, 3, dims, strides, box, true, false);
+}
+
+
+// Map of what a product stores: planes of [rows, cols] with row stride ld, in boxes of 128 bytes by 32 rows.
+bool map_of_out(CUtensorMap* map, const void* p, int64_t rows, int64_t cols, int64_t ld, int64_t plane, int planes, int elem) {
+    if (rows == 1) ld = up(cols, 8);
+    const unsigned long long dims[3] = {(unsigned long long)cols, (unsigned long long)rows, (unsigned long long)planes};
+    const unsigned long long strides[2] = {(unsigned long long)(ld * elem), (unsigned long long)(std::max(plane, ld) * elem)};
+    const unsigned box[3] = {128u / elem, 32u, 1u};
+    return tensor_map(map, p, 3, dims, strides, box, false, elem == 4);
+}
+
+HeadDiv div_by(int64_t d) {
+    int l = 0;
+    while (((int64_t)1 << l) < d) ++l;
+    return HeadDiv{(unsigned)(((uint64_t)1 << (31 + l)) / (uint64_t)d + 1), 31 + l};
 }
 
 // D[m, n] = sum over k of a[m, k] b[n, k]; an MN-major operand lies as [k, m] or [k, n].
@@ -124,32 +146,54 @@ bool job_of(HeadJob& j, int kind, int cg, const HeadMatrix& a, bool a_mn, const 
     j.rows = (int)m;
     j.cols = (int)n;
     j.tiles = j.tiles_m * j.tiles_n * j.splits;
+    j.groups = (j.tiles_m + j.group_m - 1) / j.group_m;
+    j.by_split = div_by((int64_t)j.tiles_m * j.tiles_n);
+    j.by_group = div_by((int64_t)j.group_m * j.tiles_n);
+    j.by_height = div_by(j.group_m);
+    j.by_last = div_by(j.tiles_m - (j.groups - 1) * j.group_m);
     return true;
 }
 
 template <int CG, int KIND, bool PROMOTE>
-cudaError_t head_launch(const HeadArgs& g, cudaStream_t s) {
+cudaError_t head_launch(HeadArgs& g, cudaStream_t s) {
     auto kernel = head_kernel<CG, KIND, PROMOTE>;
     const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kHeadSmem);
     if (e != cudaSuccess) return e;
     int64_t tiles = 0;
-    for (int j = 0; j < g.jobs; ++j) tiles += g.job[j].tiles;
-    cudaLaunchAttribute attr{};
-    attr.id = cudaLaunchAttributeClusterDimension;
-    attr.val.clusterDim.x = CG;
-    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    g.a_slot = 1024;
+    for (int j = 0; j < g.jobs; ++j) {
+        tiles += g.job[j].tiles;
+        g.a_slot = std::max(g.a_slot, g.job[j].a_bytes);
+    }
+    const int clusters = (int)std::min<int64_t>(tiles, kSms / CG);
+    g.late = g.job[0].tiles % clusters;
+    g.rounds = g.job[0].tiles / clusters;
+    g.extra = 0;
+    if (g.jobs == 2) {
+        const int64_t early = clusters - g.late;
+        const int64_t ratio = (g.job[0].chunks_per_split + kHeadTileCost) / (g.job[1].chunks_per_split + kHeadTileCost);
+        if (g.late) g.extra = (int)std::min(ratio, g.job[1].tiles / early);
+    }
+    // A whole A tile is read from the last slot too.
+    g.stages = std::min(kHeadMaxStages, (kHeadRing + g.a_slot - kHeadOperand) / (kHeadOperand + g.a_slot));
+    cudaLaunchAttribute attr[2] = {};
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;      // barriers and tensor memory are set up while the launch before ends
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = CG;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cudaLaunchConfig_t c{};
-    c.gridDim = dim3((unsigned)(std::min<int64_t>(tiles, kSms / CG) * CG));
+    c.gridDim = dim3((unsigned)(clusters * CG));
     c.blockDim = dim3(kHeadThreads);
     c.dynamicSmemBytes = kHeadSmem;
     c.stream = s;
-    c.attrs = &attr;
-    c.numAttrs = 1;
-    void* args[] = {const_cast<HeadArgs*>(&g)};
+    c.attrs = attr;
+    c.numAttrs = 2;
+    void* args[] = {&g};
     return cudaLaunchKernelExC(&c, (const void*)kernel, args);
 }
 template <int KIND>
-cudaError_t head_launch(const HeadArgs& g, int cg, bool promote, cudaStream_t s) {
+cudaError_t head_launch(HeadArgs& g, int cg, bool promote, cudaStream_t s) {
     if (cg == 2) return promote ? head_launch<2, KIND, true>(g, s) : head_launch<2, KIND, false>(g, s);
     return promote ? head_launch<1, KIND, true>(g, s) : head_launch<1, KIND, false>(g, s);
 }
@@ -157,8 +201,8 @@ cudaError_t head_launch(const HeadArgs& g, int cg, bool promote, cudaStream_t s)
 cudaError_t pack(int dtype, const void* x, int64_t rows, int64_t dim, int64_t ld, unsigned short* out, int64_t ldp, cudaStream_t s) {
     const int64_t pairs = rows * (ldp / 2);
     const dim3 grid((unsigned)std::min<int64_t>((pairs + 255) / 256, kSms * 16));
-    if (dtype == PB_F32) return launch(head_pack_kernel<float>, grid, 256, s, (const float*)x, rows, (int)dim, ld, out, (int)ldp, rows * ldp);
-    return launch(head_pack_kernel<__half>, grid, 256, s, (const __half*)x, rows, (int)dim, ld, out, (int)ldp, rows * ldp);
+    if (dtype == PB_F32) return launch_after(head_pack_kernel<float>, grid, 256, s, (const float*)x, rows, (int)dim, ld, out, (int)ldp, rows * ldp);
+    return launch_after(head_pack_kernel<__half>, grid, 256, s, (const __half*)x, rows, (int)dim, ld, out, (int)ldp, rows * ldp);
 }
 
 // Rows that a bulk copy can start on.
@@ -232,12 +276,14 @@ int pb_head_logprob_forward(const void* dev_hidden, const void* dev_weight, int 
         g.jobs = 1;
         g.half = half;
         g.terms = e.terms;
-        g.promote = kHeadPromote;
+        const bool promote = dtype == PB_F32 || dim > kHeadLong * kHeadChunk;
+        g.promote = dtype == PB_F32 ? kHeadPromote : promote ? kHeadPromoteLong : kHeadNever;
         g.c = (float)(inv_temperature * 1.4426950408889634074);
         g.status = dev_status;
         g.part = e.part;
         g.parts = (int)e.parts;
         g.ztok = e.ztok;
+        g.entropy = dev_entropy != nullptr;
         g.tokens = dev_tokens ? (const char*)dev_tokens + r0 * token_bytes : nullptr;
         g.token_bytes = token_bytes;
         g.vocab = vocab;
@@ -251,15 +297,15 @@ int pb_head_logprob_forward(const void* dev_hidden, const void* dev_weight, int 
             }
             if (!job_of(g.job[0], kHeadStats, e.cg, a, false, b, false)) return no_map(who);
             g.col0 = (int)v0;
-            if (err == cudaSuccess) err = head_launch<kHeadStats>(g, e.cg, true, s);
-            g.part0 += 2 * g.job[0].tiles_n;
+            if (err == cudaSuccess) err = head_launch<kHeadStats>(g, e.cg, promote, s);
+            g.part0 += g.job[0].tiles_n;
         }
         int width = 1;
-        while (width < 32 && width < nr) width *= 2;
+        while (width < 16 && width < nr) width *= 2;
         auto at = [&](float* p) { return p ? p + r0 : nullptr; };
         if (err == cudaSuccess)
-            err = launch(head_rows_kernel, dim3((unsigned)((nr + width - 1) / width)), kHeadRowThreads, s, e.part, (int)e.parts, (int)nr, width, e.ztok, g.tokens,
-                         token_bytes, (long long)vocab, g.c, at(dev_logp), at(dev_entropy), at(dev_lse), dev_status);
+            err = launch_after(head_rows_kernel, dim3((unsigned)((nr + width - 1) / width)), kHeadRowThreads, s, e.part, (int)e.parts, (int)nr, width, e.ztok, g.tokens,
+                         token_bytes, (long long)vocab, g.c, g.entropy, at(dev_logp), at(dev_entropy), at(dev_lse), dev_status);
     }
     return launched(who, err);
 }
@@ -312,7 +358,7 @@ int pb_head_logprob_backward(const void* dev_hidden, const void* dev_weight, int
             if (written[l].p && overlap(written[k].p, written[k].n, written[l].p, written[l].n)) return refuse(who, "buffers overlap");
     }
     const bool half = dtype == PB_F16, promote = dtype == PB_F32;
-    cudaError_t err = launch(head_coef_kernel, dim3(1), 1024, s, (int)rows, (long long)vocab, dev_tokens, token_bytes, inv_temperature, dev_lse, dev_entropy,
+    cudaError_t err = launch_after(head_coef_kernel, dim3(1), 1024, s, (int)rows, (long long)vocab, dev_tokens, token_bytes, inv_temperature, dev_lse, dev_entropy,
                              dev_g_logp, dev_g_entropy, dev_g_lse, half ? 16384.f : 1.f, e.coef, e.row_token, e.unscale, dev_status);
     if (e.packed && err == cudaSuccess) err = pack(dtype, dev_hidden, rows, dim, ld_hidden, e.hidden, e.dp, s);
     const HeadMatrix hidden = e.packed ? HeadMatrix{e.hidden, rows, dim, e.dp, rows * e.dp, e.planes}
@@ -325,17 +371,15 @@ int pb_head_logprob_backward(const void* dev_hidden, const void* dev_weight, int
     g.status = dev_status;
     g.coef = e.coef;
     g.row_token = e.row_token;
-    g.d = e.d;
-    g.ldd = (int)e.ldd;
-    g.d_plane = rows * e.ldd;
-    g.plane = e.plane;
-    g.plane_size = rows * e.ldp;
-    g.ldp = (int)e.ldp;
+    g.entropy = dev_g_entropy != nullptr;
+    const int64_t d_plane = rows * e.ldd, plane_size = rows * e.ldp;
     g.unscale = e.unscale;
     g.out_type = dweight_dtype;
     g.ldo = ld_dweight;
     g.accumulate = accumulate;
-    g.wide = dev_dweight && aligned(dev_dweight, 32) && ld_dweight * (int64_t)gs % 32 == 0;
+    // Sums that are rounded to 16 bits once more are formed in registers.  A bulk store writes whole pieces of 16 bytes, so rows have to end on one.
+    g.bulk = dev_dweight && aligned(dev_dweight, 16) && (ld_dweight * (int64_t)gs % 16 == 0 || vocab == 1) && dim * (int64_t)gs % 16 == 0 &&
+             (dweight_dtype == PB_F32 || !accumulate);
     int planes = 0;
     for (int64_t v0 = 0; v0 < vocab && err == cudaSuccess; v0 += e.piece) {
         const int64_t nv = std::min(e.piece, vocab - v0);
@@ -345,23 +389,28 @@ int pb_head_logprob_backward(const void* dev_hidden, const void* dev_weight, int
             err = pack(dtype, w0, nv, dim, ld_weight, e.weight, e.dp, s);
             w = HeadMatrix{e.weight, nv, dim, e.dp, nv * e.dp, e.planes};
         }
-        const HeadMatrix d{e.d, rows, nv, e.ldd, g.d_plane, e.planes};
+        const HeadMatrix d{e.d, rows, nv, e.ldd, d_plane, e.planes};
         g.col0 = (int)v0;
         g.jobs = 1;
-        if (!job_of(g.job[0], kHeadGrad, e.cg, hidden, false, w, false)) return no_map(who);
+        if (!job_of(g.job[0], kHeadGrad, e.cg, hidden, false, w, false) || !map_of_out(&g.job[0].out, e.d, rows, nv, e.ldd, d_plane, e.planes, 2))
+            return no_map(who);
         if (err == cudaSuccess) err = head_launch<kHeadGrad>(g, e.cg, promote, s);
         g.jobs = 0;
         g.add = v0 > 0;
         if (dev_dhidden) {
             // as many chunks in each split of every piece, so that the first piece has the most splits
             HeadJob& j = g.job[g.jobs++];
-            if (!job_of(j, kHeadHidden, e.cg, d, false, w, true, e.split_chunks)) return no_map(who);
+            if (!job_of(j, kHeadHidden, e.cg, d, false, w, true, e.split_chunks) || !map_of_out(&j.out, e.plane, rows, dim, e.ldp, plane_size, e.splits, 4))
+                return no_map(who);
             planes = std::max(planes, j.splits);
         }
         if (dev_dweight) {
             g.out = (char*)dev_dweight + v0 * ld_dweight * (int64_t)gs;
-            if (!job_of(g.job[g.jobs++], kHeadWeight, e.cg, d, true, hidden, true)) return no_map(who);
+            HeadJob& j = g.job[g.jobs++];
+            if (!job_of(j, kHeadWeight, e.cg, d, true, hidden, true) || (g.bulk && !map_of_out(&j.out, g.out, nv, dim, ld_dweight, 0, 1, (int)gs))) return no_map(who);
         }
+        // the longer product's tiles first
+        if (g.jobs == 2 && g.job[1].chunks_per_split > g.job[0].chunks_per_split) std::swap(g.job[0], g.job[1]);
         if (err == cudaSuccess) err = head_launch<kHeadHidden>(g, e.cg, promote, s);
     }
     if (dev_dhidden && err == cudaSuccess) {
@@ -369,7 +418,7 @@ int pb_head_logprob_backward(const void* dev_hidden, const void* dev_weight, int
         const dim3 grid((unsigned)std::min<int64_t>((n + 255) / 256, kSms * 16));
         auto go = [&](auto t) {
             using T = decltype(t);
-            return launch(head_sum_kernel<T>, grid, 256, s, e.plane, g.plane_size, planes, g.ldp, (int)rows, (int)dim, e.unscale, (T*)dev_dhidden, (long long)ld_dhidden);
+            return launch_after(head_sum_kernel<T>, grid, 256, s, e.plane, plane_size, planes, (int)e.ldp, (int)rows, (int)dim, e.unscale, (T*)dev_dhidden, (long long)ld_dhidden);
         };
         err = dtype == PB_F32 ? go(float()) : dtype == PB_BF16 ? go(__nv_bfloat16()) : go(__half());
     }

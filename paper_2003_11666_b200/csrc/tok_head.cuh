@@ -10,11 +10,12 @@
 // operands' type, and both products of a piece read it from L2 or memory once.
 //
 // All four products are tiles of one kernel: 256 x 256 of D per pair of blocks (cta_group::2, each
-// block holds 128 rows of A, 128 rows of B and 128 x 256 of D), K in chunks of 64 through a ring of six
+// block holds 128 rows of A, 128 rows of B and 128 x 256 of D), K in chunks of 64 through a ring of
 // stages filled by bulk tensor copies, two accumulators of 256 columns in tensor memory, so that eight
 // warps work on the last tile while the next one is multiplied.  Up to 128 rows of hidden states run in
 // single blocks of 128 x 128, since a pair would leave half of its rows empty: these calls are bound by
-// reading the weights.
+// reading the weights, and the fewer rows there are, the more stages fit (A's rows that do not exist are not
+// copied; what the tensor core finds in their place goes to rows of D that nobody reads).
 //   logits   A = hidden (K-major)        B = weight (K-major)      the row statistics, or d, are computed from the tile
 //   hidden   A = d (K-major)             B = weight (MN-major)     float32 partial sums, one plane per split of K
 //   weight   A = d, read transposed (MN-major)  B = hidden (MN-major)
@@ -32,17 +33,27 @@ namespace pb {
 
 constexpr int kHeadChunk = 64;                // K elements per stage: one 128-byte swizzled row
 constexpr int kHeadOperand = 128 * 128;       // bytes of an operand's 128 x 64 tile
-constexpr int kHeadStages = 6;
-constexpr int kHeadSmem = kHeadStages * 2 * kHeadOperand + 1024;
+constexpr int kHeadMaxStages = 12;
 constexpr int kHeadEpiWarps = 8;              // quarter w % 4 of the tensor-memory lanes, half w / 4 of the columns
+constexpr int kHeadBuf = 32 * 128;            // bytes of an epilogue warp's buffer: 128 of each of its rows
+constexpr int kHeadRing = 196608;             // bytes for the stages: six of 32 KB, or twelve with A tiles of up to eight rows
+constexpr int kHeadSmem = 1024 + kHeadRing + kHeadEpiWarps * kHeadBuf;
 constexpr int kHeadThreads = 32 * (kHeadEpiWarps + 2);
 constexpr int kHeadPlanes = 3;                // bfloat16 planes of a float32 operand
 
 enum HeadKind { kHeadStats = 0, kHeadGrad = 1, kHeadHidden = 2, kHeadWeight = 3 };
 
+// Quotient of a number below 2^31 by d >= 1: n m >> s with m = floor(2^s / d) + 1, s = 31 + ceil(log2 d).
+struct HeadDiv {
+    unsigned m;
+    int s;
+    __device__ __forceinline__ int operator()(int n) const { return (int)((unsigned long long)(unsigned)n * m >> s); }
+};
+
 // One product: tiles_m x tiles_n tiles, K split `splits` ways.
 struct alignas(64) HeadJob {
     CUtensorMap a, b;            // K-major: (k, row, plane); MN-major: (row, k, plane)
+    CUtensorMap out;             // (column, row, plane) of what is stored by bulk copies: boxes of 128 bytes by 32 rows
     int kind;
     int a_mn, b_mn;              // operand is MN-major
     int tiles_m, tiles_n, splits;
@@ -50,6 +61,8 @@ struct alignas(64) HeadJob {
     int chunks, chunks_per_split;
     int rows, cols;              // of D
     int tiles;                   // tiles_m * tiles_n * splits
+    HeadDiv by_split, by_group, by_height, by_last;      // tiles of a split, of a group; row tiles of a group, of the last one
+    int groups;
     int a_bytes;                 // bytes of A that a stage receives per block
 };
 
@@ -63,6 +76,8 @@ struct HeadRow {
 struct alignas(64) HeadArgs {
     HeadJob job[2];
     int jobs, half;              // half: operands are float16
+    int extra, late, rounds;     // see head_tile
+    int stages, a_slot;          // of the ring; bytes between two stages' A tiles, which lie behind the B tiles
     int terms;                   // 1, or 6 products of planes
     int promote;                 // chunks of K that the tensor core adds up by itself
     float c;                     // inv_temperature * log2(e)
@@ -70,7 +85,7 @@ struct alignas(64) HeadArgs {
     int* status;
     // row statistics
     float* part;                 // [3][parts][rows]: reference (log2), sum, sum of e log2 e
-    int part0, parts;
+    int part0, parts, entropy;   // entropy: its sum is wanted, or its gradient given
     float* ztok;                 // the token's logit of each row
     const void* tokens;
     int token_bytes;
@@ -78,16 +93,11 @@ struct alignas(64) HeadArgs {
     // d
     const HeadRow* coef;
     const int* row_token;        // index of the token, or -1
-    unsigned short* d;           // [planes][rows][ldd]
-    long long d_plane;
-    int ldd;
     // products
-    float* plane;                // [splits][rows][ldp]
-    long long plane_size;
-    int ldp, add;                // add: an earlier piece is there
+    int add;                     // partial sums of dhidden: those of an earlier piece are there
     void* out;                   // of this piece of dweight
     long long ldo;
-    int out_type, accumulate, wide;      // pb_dtype; wide: rows start on 32 bytes
+    int out_type, accumulate, bulk;      // pb_dtype; bulk: rows that bulk copies can store
     const float* unscale;
 };
 
@@ -141,8 +151,8 @@ __device__ __forceinline__ void tma_3d_pair(uint32_t dst, const CUtensorMap* tm,
 }
 
 struct HeadShared {
-    uint64_t full[kHeadStages];   // a stage's operands have landed (at the leader: both blocks')
-    uint64_t empty[kHeadStages];  // the products that read a stage are done
+    uint64_t full[kHeadMaxStages];   // a stage's operands have landed (at the leader: both blocks')
+    uint64_t empty[kHeadMaxStages];  // the products that read a stage are done
     uint64_t acc_full[2], acc_empty[2];
     uint32_t tmem_base;
     int fail;
@@ -152,20 +162,32 @@ struct HeadTile {
     int m, n, split, chunk0, chunk1;
 };
 
-// The job that tile `t` of the launch belongs to, and its place there; false behind the last.
-__device__ __forceinline__ bool head_tile(const HeadArgs& g, int t, int& j, HeadTile& x) {
+// The i-th tile of this block (or pair): its job, and its place there; false behind the last.  The first job's tiles go round the blocks, `late` of
+// which get rounds + 1 and the others `rounds`.  The second job's are shorter: those others take `extra` of them before all take
+// turns, so that all end together (4096 rows, 2048 columns, 25088 tokens: 128 long tiles for 74 pairs).
+__device__ __forceinline__ bool head_tile(const HeadArgs& g, int i, int& j, HeadTile& x) {
+    const int n = (int)cluster_count(), id = (int)cluster_id();
+    int t = id + i * n;
     j = 0;
-    while (j < g.jobs && t >= g.job[j].tiles) t -= g.job[j++].tiles;
-    if (j == g.jobs) return false;
+    if (t >= g.job[0].tiles) {
+        if (g.jobs == 1) return false;
+        j = 1;
+        const bool is_late = id < g.late;
+        const int early = n - g.late, ahead = early * g.extra;
+        i -= g.rounds + is_late;                              // tiles of the second job that this block has had
+        if (is_late) t = ahead + id + i * n;
+        else if (i < g.extra) t = id - g.late + i * early;
+        else t = ahead + id + (i - g.extra) * n;
+        if (t >= g.job[1].tiles) return false;
+    }
     const HeadJob& q = g.job[j];
-    const int per_split = q.tiles_m * q.tiles_n;
-    x.split = t / per_split;
-    t -= x.split * per_split;
-    const int per_group = q.group_m * q.tiles_n, group = t / per_group;
-    const int m0 = group * q.group_m, height = min(q.group_m, q.tiles_m - m0);
-    t -= group * per_group;
-    x.n = t / height;
-    x.m = m0 + t - x.n * height;
+    x.split = q.by_split(t);
+    t -= x.split * q.tiles_m * q.tiles_n;
+    const int group = q.by_group(t), m0 = group * q.group_m;
+    t -= group * q.group_m * q.tiles_n;
+    const bool last = group == q.groups - 1;
+    x.n = last ? q.by_last(t) : q.by_height(t);
+    x.m = m0 + t - x.n * (last ? q.tiles_m - m0 : q.group_m);
     x.chunk0 = x.split * q.chunks_per_split;
     x.chunk1 = min(q.chunks, x.chunk0 + q.chunks_per_split);
     return true;
@@ -181,10 +203,12 @@ __device__ __forceinline__ void head_term(int terms, int k, int& pa, int& pb) {
 // ------------------------------------------------------------------ copies (one thread of each block)
 template <int CG>
 __device__ void head_copies(const HeadArgs& g, unsigned char* smem, HeadShared& sh, int rank) {
-    int it = 0, j;
+    int stg = 0, j;
+    uint32_t phase = 1;                                       // every stage is free at first
     HeadTile x;
     constexpr int kRows = 128 * CG;
-    for (int t = cluster_id(); head_tile(g, t, j, x); t += cluster_count()) {
+    const uint32_t b_tiles = smem_u32(smem), a_tiles = b_tiles + g.stages * kHeadOperand;
+    for (int i = 0; head_tile(g, i, j, x); ++i) {
         const HeadJob& q = g.job[j];
         const int m0 = x.m * kRows + rank * 128, n0 = x.n * kRows + rank * 128;
         const uint32_t bytes = (uint32_t)(q.a_bytes + kHeadOperand) * CG;
@@ -193,11 +217,10 @@ __device__ void head_copies(const HeadArgs& g, unsigned char* smem, HeadShared& 
             for (int term = 0; term < g.terms; ++term) {
                 int pa, pb;
                 head_term(g.terms, term, pa, pb);
-                for (int c = c0; c < c1; ++c, ++it) {
-                    const int stg = it % kHeadStages;
-                    const uint32_t empty = smem_u32(&sh.empty[stg]), parity = (uint32_t)(((it / kHeadStages) & 1) ^ 1);
-                    if (it >= kHeadStages && !(CG == 2 ? mbar_wait_pair(empty, parity, &sh.fail) : mbar_wait(empty, parity, &sh.fail))) { sh.fail = 1; return; }
-                    const uint32_t sa = smem_u32(smem + stg * 2 * kHeadOperand), sb = sa + kHeadOperand;
+                for (int c = c0; c < c1; ++c) {
+                    const uint32_t empty = smem_u32(&sh.empty[stg]);
+                    if (!(CG == 2 ? mbar_wait_pair(empty, phase, &sh.fail) : mbar_wait(empty, phase, &sh.fail))) { sh.fail = 1; return; }
+                    const uint32_t sa = a_tiles + stg * g.a_slot, sb = b_tiles + stg * kHeadOperand;
                     const uint32_t own = smem_u32(&sh.full[stg]), full = CG == 2 ? of_leader(own) : own;
                     if (rank == 0) mbar_arrive_tx(own, bytes);
                     auto copy = [&](uint32_t dst, const CUtensorMap* tm, int u, int v, int w) {
@@ -216,6 +239,7 @@ __device__ void head_copies(const HeadArgs& g, unsigned char* smem, HeadShared& 
                     } else {
                         copy(sb, &q.b, k, n0, pb);
                     }
+                    if (++stg == g.stages) { stg = 0; phase ^= 1; }
                 }
             }
         }
@@ -225,10 +249,12 @@ __device__ void head_copies(const HeadArgs& g, unsigned char* smem, HeadShared& 
 // ------------------------------------------------------------------ products (one thread of a block or pair)
 template <int CG>
 __device__ void head_products(const HeadArgs& g, unsigned char* smem, HeadShared& sh) {
-    int it = 0, at = 0, j;
+    int stg = 0, at = 0, j;
+    uint32_t phase = 0;
     HeadTile x;
     constexpr int kCols = 128 * CG;
-    for (int t = cluster_id(); head_tile(g, t, j, x); t += cluster_count()) {
+    const uint32_t b_tiles = smem_u32(smem), a_tiles = b_tiles + g.stages * kHeadOperand;
+    for (int i = 0; head_tile(g, i, j, x); ++i) {
         const HeadJob& q = g.job[j];
         const uint32_t type = g.half ? 0u : (1u << 7) | (1u << 10);
         const uint32_t idesc = (1u << 4) | type | ((uint32_t)q.a_mn << 15) | ((uint32_t)q.b_mn << 16) | ((uint32_t)(kCols >> 3) << 17) |
@@ -243,12 +269,11 @@ __device__ void head_products(const HeadArgs& g, unsigned char* smem, HeadShared
             }
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             const uint32_t dcol = sh.tmem_base + (uint32_t)(buf * kCols);
-            for (int k = 0; k < n; ++k, ++it) {
-                const int stg = it % kHeadStages;
-                const uint32_t full = smem_u32(&sh.full[stg]), parity = (uint32_t)((it / kHeadStages) & 1);
-                if (!(CG == 2 ? mbar_wait_pair(full, parity, &sh.fail) : mbar_wait(full, parity, &sh.fail))) { sh.fail = 1; return; }
+            for (int k = 0; k < n; ++k) {
+                const uint32_t full = smem_u32(&sh.full[stg]);
+                if (!(CG == 2 ? mbar_wait_pair(full, phase, &sh.fail) : mbar_wait(full, phase, &sh.fail))) { sh.fail = 1; return; }
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                const uint32_t sa = smem_u32(smem + stg * 2 * kHeadOperand), sb = sa + kHeadOperand;
+                const uint32_t sa = a_tiles + stg * g.a_slot, sb = b_tiles + stg * kHeadOperand;
 #pragma unroll
                 for (int u = 0; u < kHeadChunk / 16; ++u) {
                     const uint64_t da = tc_desc(sa + u * step_a, lead_a, 1024), db = tc_desc(sb + u * step_b, lead_b, 1024);
@@ -269,269 +294,308 @@ __device__ void head_products(const HeadArgs& g, unsigned char* smem, HeadShared
                 };
                 commit(&sh.empty[stg]);
                 if (k == n - 1) commit(&sh.acc_full[buf]);
+                if (++stg == g.stages) { stg = 0; phase ^= 1; }
             }
         }
     }
 }
 
 // ------------------------------------------------------------------ what becomes of a tile (eight warps of each block)
-// Running statistics of one row's logits, in units of log 2 around a reference.
+// A thread holds a row, 32 threads of a warp 32 rows: stored as they are, an instruction would send 32 sectors of 32 rows one by one (2 us for
+// a tile of 128 x 128, whatever its K).  Instead 128 bytes of each row go to a buffer of the warp, 16-byte piece k of row r at k ^ (r mod 8) as the
+// 128-byte swizzle of the bulk copy that stores them.
+__device__ __forceinline__ void buf_free(int lane) {           // the copy before has read the buffer
+    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+    __syncwarp();
+}
+__device__ __forceinline__ void buf_put(unsigned char* buf, int lane, const unsigned* w) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+        *reinterpret_cast<uint4*>(buf + lane * 128 + ((k ^ (lane & 7)) << 4)) = make_uint4(w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]);
+}
+template <bool kAdd>
+__device__ __forceinline__ void buf_store(unsigned char* buf, int lane, const CUtensorMap* map, int c, int r, int plane) {
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncwarp();
+    if (lane == 0) {
+        if (kAdd) asm volatile("cp.reduce.async.bulk.tensor.3d.global.shared::cta.add.tile.bulk_group [%0, {%1, %2, %3}], [%4];"
+                               ::"l"(map), "r"(c), "r"(r), "r"(plane), "r"(smem_u32(buf)) : "memory");
+        else asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%1, %2, %3}], [%4];"
+                          ::"l"(map), "r"(c), "r"(r), "r"(plane), "r"(smem_u32(buf)) : "memory");
+        asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+    }
+}
+// 64 columns of float32 rows.
+__device__ __forceinline__ void buf_floats(const HeadJob& q, unsigned char* buf, int lane, const float (&z)[64], int c0, int r, int plane, bool add) {
+#pragma unroll
+    for (int h = 0; h < 64; h += 32) {
+        if (c0 + h >= q.cols) break;
+        unsigned w[32];
+#pragma unroll
+        for (int k = 0; k < 32; ++k) w[k] = __float_as_uint(z[h + k]);
+        buf_free(lane);
+        buf_put(buf, lane, w);
+        if (add) buf_store<true>(buf, lane, &q.out, c0 + h, r, plane); else buf_store<false>(buf, lane, &q.out, c0 + h, r, plane);
+    }
+}
+
+// Exponents from here down give zero; a finite one, so that zero times it is zero too.  A NaN stays.
+__device__ __forceinline__ float head_floor(float t) { return max_nan(t, -1000.f); }
+
+// Statistics of one row's logits, in units of log 2 around a reference.
 struct HeadStat {
     float ref, sum, elog;
     __device__ __forceinline__ void start() { ref = -INFINITY; sum = elog = 0.f; }
-    __device__ __forceinline__ void add(float (&z)[32], float c) {
-        float top = z[0];
+    template <bool kEntropy> __device__ __forceinline__ void add(const float (&z)[64], float c) {
+        float m0 = fmaxf(z[0], z[1]), m1 = fmaxf(z[2], z[3]);
 #pragma unroll
-        for (int u = 1; u < 32; ++u) top = fmaxf(top, z[u]);
-        const float now = fmaxf(ref, top * c);               // c > 0
+        for (int u = 4; u < 64; u += 4) {
+            m0 = fmaxf(m0, fmaxf(z[u], z[u + 1]));
+            m1 = fmaxf(m1, fmaxf(z[u + 2], z[u + 3]));
+        }
+        const float now = fmaxf(ref, fmaxf(m0, m1) * c);     // c > 0
         const float base = now == -INFINITY ? 0.f : now;
         if (now > ref && ref != -INFINITY) {
             const float shift = ref - now, f = exp2_near(shift);
-            elog = f * fmaf(shift, sum, elog);
+            if (kEntropy) elog = f * fmaf(shift, sum, elog);
             sum *= f;
         }
         ref = now;
-        float s0 = 0.f, s1 = 0.f, l0 = 0.f, l1 = 0.f;
+        const Pair scale(c), from(-base);
+        Pair s[2] = {Pair(0.f), Pair(0.f)}, l[2] = {Pair(0.f), Pair(0.f)};
 #pragma unroll
-        for (int u = 0; u < 32; u += 2) {
-            const float t0 = fmaf(z[u], c, -base), t1 = fmaf(z[u + 1], c, -base);
-            const float e0 = exp2_near(t0), e1 = exp2_near(t1);
-            s0 += e0; s1 += e1;
-            // what cannot occur has no entropy, though its logarithm is infinite
-            l0 = e0 != 0.f ? fmaf(e0, t0, l0) : l0;
-            l1 = e1 != 0.f ? fmaf(e1, t1, l1) : l1;
+        for (int u = 0; u < 64; u += 2) {
+            float a, b;
+            fma2(Pair(z[u], z[u + 1]), scale, from).split(a, b);
+            if (kEntropy) { a = head_floor(a); b = head_floor(b); }
+            const Pair e(exp2_near(a), exp2_near(b));
+            s[u / 2 & 1] = s[u / 2 & 1] + e;
+            if (kEntropy) l[u / 2 & 1] = fma2(e, Pair(a, b), l[u / 2 & 1]);
         }
-        sum += s0 + s1;
-        elog += l0 + l1;
+        float a, b;
+        (s[0] + s[1]).split(a, b);
+        sum += a + b;
+        if (kEntropy) {
+            (l[0] + l[1]).split(a, b);
+            elog += a + b;
+        }
     }
+    __device__ __forceinline__ void join(float m, float s, float e) {
+        const float now = fmaxf(ref, m), base = now == -INFINITY ? 0.f : now;
+        const float d0 = fmaxf(ref - base, -1000.f), d1 = fmaxf(m - base, -1000.f), f = exp2_near(d0), h = exp2_near(d1);
+        elog = f * fmaf(d0, sum, elog) + h * fmaf(d1, s, e);
+        sum = fmaf(f, sum, h * s);
+        ref = now;
+    }
+};
+
+// A tile as one thread sees it: a row, and what is read for that row before the tile is ready.
+struct HeadView {
+    HeadTile x;
+    int j, row;
+    bool live;
+    HeadRow hr;
+    int tok;                      // column of the row's token in the piece, or out of it
 };
 
 template <int CG, int KIND>
-struct HeadEpilogue {
-    const HeadArgs& g;
-    const HeadJob& q;
-    const HeadTile& x;
-    int row, col;                 // this thread's row of D, first column of its half
-    HeadStat st;
-    HeadRow hr;
-    int tok;                      // column of the row's token, in the piece
-    float unscale;
-
-    __device__ __forceinline__ HeadEpilogue(const HeadArgs& g_, const HeadJob& q_, const HeadTile& x_, int rank, int warp, int lane)
-        : g(g_), q(q_), x(x_) {
-        row = x.m * 128 * CG + rank * 128 + (warp & 3) * 32 + lane;
-        col = x.n * 128 * CG + (warp >> 2) * 64 * CG;
-        if (KIND == kHeadStats) {
-            st.start();
-            tok = -1;
-            if (row < q.rows && g.tokens) {
-                const long long id = g.token_bytes == 8 ? ((const long long*)g.tokens)[row] : (long long)((const int*)g.tokens)[row];
-                if (id >= g.col0 && id < (long long)g.col0 + q.cols) tok = (int)(id - g.col0);
-            }
-        }
-        if (KIND == kHeadGrad && row < q.rows) {
-            hr = g.coef[row];
-            tok = g.row_token[row] - g.col0;
-        }
-        if (KIND == kHeadHidden) unscale = g.unscale ? *g.unscale : 1.f;
+__device__ __forceinline__ HeadView head_view(const HeadArgs& g, int i, int rank, int warp, int lane) {
+    HeadView v;
+    v.live = head_tile(g, i, v.j, v.x);
+    if (!v.live) return v;
+    const HeadJob& q = g.job[v.j];
+    v.row = v.x.m * 128 * CG + rank * 128 + (warp & 3) * 32 + lane;
+    v.tok = -1;
+    if (KIND == kHeadStats && v.row < q.rows && g.tokens) {
+        const long long id = g.token_bytes == 8 ? ((const long long*)g.tokens)[v.row] : (long long)((const int*)g.tokens)[v.row];
+        if (id >= g.col0 && id < (long long)g.col0 + q.cols) v.tok = (int)(id - g.col0);
     }
-
-    // 32 columns from `c0` on.
-    __device__ __forceinline__ void take(float (&z)[32], int c0) {
-        if (KIND == kHeadStats) {
-            if (c0 + 32 > q.cols) {
-#pragma unroll
-                for (int u = 0; u < 32; ++u) z[u] = c0 + u < q.cols ? z[u] : -INFINITY;
-            }
-            if (tok >= c0 && tok < c0 + 32) {
-                float v = 0.f;
-#pragma unroll
-                for (int u = 0; u < 32; ++u) v = tok == c0 + u ? z[u] : v;
-                g.ztok[row] = v;
-            }
-            st.add(z, g.c);
-        } else if (KIND == kHeadGrad) {
-            if (row < q.rows && c0 < g.ldd) gradient(z, c0);
-        } else if (q.kind == kHeadHidden) {
-            hidden(z, c0);
-        } else {
-            weight(z, c0);
-        }
+    if (KIND == kHeadGrad && v.row < q.rows) {
+        const float4 c = *reinterpret_cast<const float4*>(g.coef + v.row);
+        v.hr = HeadRow{c.x, c.y, c.z, c.w};
+        v.tok = g.row_token[v.row] - g.col0;
     }
+    return v;
+}
 
-    __device__ __forceinline__ void gradient(float (&z)[32], int c0) {
-        const bool token = tok >= c0 && tok < c0 + 32;
-        float own = 0.f;
-        if (token) {                                         // c0 has -a: the token's 1 - p without the cancellation
+// d of 64 columns, to its planes.
+template <bool kEntropy, bool kF32>
+__device__ __forceinline__ void head_gradient(const HeadArgs& g, const HeadJob& q, const HeadView& v, float (&z)[64], int c0, unsigned char* buf, int lane) {
+    const bool token = v.tok >= c0 && v.tok < c0 + 64;
+    float own = 0.f;
+    if (token) {                                             // c0 has -a: the token's 1 - p without the cancellation
 #pragma unroll
-            for (int u = 0; u < 32; ++u) own = tok == c0 + u ? z[u] : own;
-            const float t = fmaf(own, g.c, -hr.lse2), p = exp2_near(t);
-            own = (p == 0.f ? 0.f : p * fmaf(hr.c1, t, hr.c0 + hr.a)) - hr.a * expm1f(t * 0.69314718055994531f);
-        }
-#pragma unroll
-        for (int u = 0; u < 32; ++u) {
-            const float t = fmaf(z[u], g.c, -hr.lse2), p = exp2_near(t);
-            z[u] = p == 0.f ? 0.f : p * fmaf(hr.c1, t, hr.c0);
-        }
-        if (token) {
-#pragma unroll
-            for (int u = 0; u < 32; ++u) z[u] = tok == c0 + u ? own : z[u];
-        }
-        unsigned short* to = g.d + (long long)row * g.ldd + c0;
-        for (int plane = 0;; ++plane) {
-            unsigned w[16];
-#pragma unroll
-            for (int u = 0; u < 16; ++u)
-                w[u] = g.half ? pack2(z[2 * u], z[2 * u + 1], __half()) : pack2(z[2 * u], z[2 * u + 1], __nv_bfloat16());
-#pragma unroll
-            for (int u = 0; u < 2; ++u)
-                asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to + 16 * u), "r"(w[8 * u]), "r"(w[8 * u + 1]), "r"(w[8 * u + 2]),
-                             "r"(w[8 * u + 3]), "r"(w[8 * u + 4]), "r"(w[8 * u + 5]), "r"(w[8 * u + 6]), "r"(w[8 * u + 7]) : "memory");
-            if (g.terms == 1 || plane == kHeadPlanes - 1) break;
-#pragma unroll
-            for (int u = 0; u < 16; ++u) {                   // what the plane has left over; exact
-                z[2 * u] -= __uint_as_float(w[u] << 16);
-                z[2 * u + 1] -= __uint_as_float(w[u] & 0xffff0000u);
-            }
-            to += g.d_plane;
-        }
+        for (int u = 0; u < 64; ++u) own = v.tok == c0 + u ? z[u] : own;
+        const float t = head_floor(fmaf(own, g.c, -v.hr.lse2)), p = exp2_near(t);
+        own = p * fmaf(v.hr.c1, t, v.hr.c0 + v.hr.a) - v.hr.a * expm1f(t * 0.69314718055994531f);
     }
-
-    __device__ __forceinline__ void hidden(float (&z)[32], int c0) {
-        if (row >= q.rows || c0 >= g.ldp) return;
-        float* to = g.plane + x.split * g.plane_size + (long long)row * g.ldp + c0;
+    const Pair scale(g.c), from(-v.hr.lse2), k0(v.hr.c0), k1(v.hr.c1);
 #pragma unroll
-        for (int u = 0; u < 32; u += 8) {
-            if (c0 + u >= g.ldp) break;                      // ldp is a multiple of 8
-            float v[8];
-#pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] = z[u + k];
-            if (g.add) {
-                float old[8];
-                load8_wide(old, to + u);
-#pragma unroll
-                for (int k = 0; k < 8; ++k) v[k] += old[k];
-            }
-            store8_wide(to + u, v);
-        }
+    for (int u = 0; u < 64; u += 2) {
+        float a, b;
+        fma2(Pair(z[u], z[u + 1]), scale, from).split(a, b);
+        if (kEntropy) { a = head_floor(a); b = head_floor(b); }
+        const Pair p(exp2_near(a), exp2_near(b));
+        (p * (kEntropy ? fma2(k1, Pair(a, b), k0) : k0)).split(z[u], z[u + 1]);
     }
-
-    template <typename T>
-    __device__ __forceinline__ void weight_as(float (&z)[32], int c0) {
-        T* to = (T*)g.out + (long long)row * g.ldo + c0;
-        constexpr int kEach = 32 / (int)sizeof(T);           // 32 bytes
-        if (g.wide && c0 + 32 <= q.cols) {
+    if (token) {
 #pragma unroll
-            for (int u = 0; u < 32; u += kEach) {
-                if constexpr (sizeof(T) == 4) {
-                    float v[8];
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) v[k] = z[u + k] * unscale;
-                    if (g.accumulate) {
-                        float old[8];
-                        load8_wide(old, (const float*)to + u);
-#pragma unroll
-                        for (int k = 0; k < 8; ++k) v[k] += old[k];
-                    }
-                    store8_wide((float*)to + u, v);
-                } else {
-#pragma unroll
-                    for (int h = 0; h < kEach; h += 8) {
-                        float v[8];
-#pragma unroll
-                        for (int k = 0; k < 8; ++k) v[k] = z[u + h + k] * unscale;
-                        if (g.accumulate) {
-                            float old[8];
-                            load8(old, to + u + h);
-#pragma unroll
-                            for (int k = 0; k < 8; ++k) v[k] += old[k];
-                        }
-                        store8(to + u + h, v);
-                    }
-                }
-            }
-            return;
-        }
+        for (int u = 0; u < 64; ++u) z[u] = v.tok == c0 + u ? own : z[u];
+    }
+    for (int plane = 0;; ++plane) {
+        unsigned w[32];
 #pragma unroll
         for (int u = 0; u < 32; ++u)
-            if (c0 + u < q.cols) to[u] = from_f32<T>(g.accumulate ? fmaf(z[u], unscale, to_f32(to[u])) : z[u] * unscale);
-    }
-    __device__ __forceinline__ void weight(float (&z)[32], int c0) {
-        if (row >= q.rows || c0 >= q.cols) return;
-        if (g.out_type == 0) weight_as<float>(z, c0);
-        else if (g.out_type == 1) weight_as<__nv_bfloat16>(z, c0);
-        else weight_as<__half>(z, c0);
-    }
-
-    __device__ __forceinline__ void finish(int half) {
-        if (KIND == kHeadStats && row < q.rows) {
-            float* p = g.part + (long long)(g.part0 + 2 * x.n + half) * q.rows + row;
-            const long long plane = (long long)g.parts * q.rows;
-            p[0] = st.ref;
-            p[plane] = st.sum;
-            p[2 * plane] = st.elog;
+            w[u] = !kF32 && g.half ? pack2(z[2 * u], z[2 * u + 1], __half()) : pack2(z[2 * u], z[2 * u + 1], __nv_bfloat16());
+        buf_free(lane);
+        buf_put(buf, lane, w);
+        buf_store<false>(buf, lane, &q.out, c0, v.row - lane, plane);
+        if (!kF32 || plane == kHeadPlanes - 1) break;
+#pragma unroll
+        for (int u = 0; u < 32; ++u) {                       // what the plane has left over; exact
+            z[2 * u] -= __uint_as_float(w[u] << 16);
+            z[2 * u + 1] -= __uint_as_float(w[u] & 0xffff0000u);
         }
     }
-};
+}
+
+// 64 columns of dweight.
+template <typename T>
+__device__ __forceinline__ void head_weight(const HeadArgs& g, const HeadJob& q, const HeadView& v, float (&z)[64], int c0, unsigned char* buf, int lane) {
+    if (g.bulk) {
+        if constexpr (sizeof(T) == 4) {
+            buf_floats(q, buf, lane, z, c0, v.row - lane, 0, g.accumulate);
+        } else {
+            unsigned w[32];
+#pragma unroll
+            for (int k = 0; k < 32; ++k) w[k] = pack2(z[2 * k], z[2 * k + 1], T());
+            buf_free(lane);
+            buf_put(buf, lane, w);
+            buf_store<false>(buf, lane, &q.out, c0, v.row - lane, 0);
+        }
+        return;
+    }
+    // Rows at any alignment, and 16-bit ones that are added to before they are rounded: 32 columns at a time by way of the buffer, from which the warp
+    // writes one row after the other.  Column u of row r lies at u ^ r of its row there, so that neither way meets a bank twice.
+    const int rows = min(32, q.rows - (v.row - lane));
+    T* to = (T*)g.out + (long long)(v.row - lane) * g.ldo + c0 + lane;
+    float* f = (float*)buf;
+#pragma unroll
+    for (int h = 0; h < 64; h += 32) {
+        buf_free(lane);
+#pragma unroll
+        for (int u = 0; u < 32; ++u) f[lane * 32 + (u ^ lane)] = z[h + u];
+        __syncwarp();
+        if (c0 + h + lane < q.cols) {
+            T* p = to + h;
+#pragma unroll 8
+            for (int r = 0; r < rows; ++r, p += g.ldo) {
+                const float s = f[r * 32 + (lane ^ r)];
+                *p = from_f32<T>(g.accumulate ? s + to_f32(*p) : s);
+            }
+        }
+    }
+}
+
+// 64 columns of a tile from c0 on; the whole warp calls this.  kF32: the operands are float32 (the statistics do not ask).
+template <int KIND, bool kF32>
+__device__ __forceinline__ void head_take(const HeadArgs& g, const HeadJob& q, const HeadView& v, HeadStat& st, float (&z)[64], int c0, float unscale,
+                                          unsigned char* buf, int lane) {
+    if (c0 >= q.cols || v.row - lane >= q.rows) return;       // the same for all
+    if (KIND == kHeadStats) {
+        if (c0 + 64 > q.cols) {
+#pragma unroll
+            for (int k = 0; k < 64; ++k) z[k] = c0 + k < q.cols ? z[k] : -INFINITY;
+        }
+        if (v.tok >= c0 && v.tok < c0 + 64) {
+            float own = 0.f;
+#pragma unroll
+            for (int k = 0; k < 64; ++k) own = v.tok == c0 + k ? z[k] : own;
+            g.ztok[v.row] = own;
+        }
+        if (g.entropy) st.add<true>(z, g.c); else st.add<false>(z, g.c);
+    } else if (KIND == kHeadGrad) {
+        if (g.entropy) head_gradient<true, kF32>(g, q, v, z, c0, buf, lane); else head_gradient<false, kF32>(g, q, v, z, c0, buf, lane);
+    } else if (q.kind == kHeadHidden) {
+        buf_floats(q, buf, lane, z, c0, v.row - lane, v.x.split, g.add);
+    } else {
+#pragma unroll
+        for (int k = 0; k < 64; ++k) z[k] *= unscale;
+        if (kF32 || g.out_type == 0) head_weight<float>(g, q, v, z, c0, buf, lane);
+        else if (g.out_type == 1) head_weight<__nv_bfloat16>(g, q, v, z, c0, buf, lane);
+        else head_weight<__half>(g, q, v, z, c0, buf, lane);
+    }
+}
 
 template <int CG, int KIND, bool PROMOTE>
-__device__ void head_epilogue(const HeadArgs& g, HeadShared& sh, int rank, int warp, int lane) {
-    constexpr int kHalf = 64 * CG;                            // columns of a thread
-    int at = 0, j;
+__device__ void head_epilogue(const HeadArgs& g, HeadShared& sh, unsigned char* area, int rank, int warp, int lane) {
+    constexpr int kCols = 64 * CG;                            // columns of a thread
+    const int right = warp >> 2;
+    const float unscale = KIND == kHeadHidden && g.unscale ? *g.unscale : 1.f;
+    unsigned char* buf = area + warp * kHeadBuf;
+    int at = 0;
     bool ok = true;
-    HeadTile x;
-    for (int t = cluster_id(); head_tile(g, t, j, x); t += cluster_count()) {
-        const HeadJob& q = g.job[j];
-        HeadEpilogue<CG, KIND> e(g, q, x, rank, warp, lane);
-        float sum[PROMOTE ? kHalf : 1];
-        for (int c0 = x.chunk0; c0 < x.chunk1; c0 += g.promote, ++at) {
-            const int buf = at & 1;
-            const uint32_t bar = smem_u32(&sh.acc_full[buf]), parity = (uint32_t)((at >> 1) & 1);
+    HeadView v = head_view<CG, KIND>(g, 0, rank, warp, lane);
+    for (int i = 1; v.live; ++i) {
+        const HeadView next = head_view<CG, KIND>(g, i, rank, warp, lane);        // its reads are under way meanwhile
+        const HeadJob& q = g.job[v.j];
+        const int col = v.x.n * 128 * CG + right * kCols;
+        HeadStat st;
+        st.start();
+        float sum[PROMOTE ? CG : 1][64];                      // 64 columns of the tile each, where the parts of K are added up here
+        for (int c0 = v.x.chunk0; c0 < v.x.chunk1; c0 += g.promote, ++at) {
+            const int half = at & 1;
+            const uint32_t bar = smem_u32(&sh.acc_full[half]), parity = (uint32_t)((at >> 1) & 1);
             if (ok) ok = __all_sync(0xffffffffu, CG == 2 ? mbar_wait_pair(bar, parity, &sh.fail) : mbar_wait(bar, parity, &sh.fail));
             if (!ok) sh.fail = 1;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            const uint32_t from = sh.tmem_base + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)(buf * 128 * CG + (warp >> 2) * kHalf);
+            const uint32_t from = sh.tmem_base + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)(half * 128 * CG + right * kCols);
 #pragma unroll
-            for (int u = 0; u < kHalf; u += 32) {
-                uint32_t r[32];
-                tmem_ld32(from + u, r);
+            for (int u = 0; u < CG; ++u) {
+                float (&z)[64] = sum[PROMOTE ? u : 0];
+#pragma unroll
+                for (int h = 0; h < 64; h += 32) {
+                    uint32_t r[32];
+                    tmem_ld32(from + u * 64 + h, r);
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) z[h + k] = PROMOTE && c0 > v.x.chunk0 ? z[h + k] + __uint_as_float(r[k]) : __uint_as_float(r[k]);
+                }
+                if (u + 1 == CG) {                            // all of it is in registers: the next product may have the accumulator
+                    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) {
+                        const uint32_t done = smem_u32(&sh.acc_empty[half]);
+                        if (CG == 2) arrive_cluster(of_leader(done)); else mbar_arrive(done);
+                    }
+                }
                 if (!ok) {
 #pragma unroll
-                    for (int k = 0; k < 32; ++k) r[k] = 0x7fffffffu;
+                    for (int k = 0; k < 64; ++k) z[k] = __int_as_float(0x7fffffff);
                 }
-                if (PROMOTE) {
-                    if (c0 == x.chunk0) {
-#pragma unroll
-                        for (int k = 0; k < 32; ++k) sum[u + k] = __uint_as_float(r[k]);
-                    } else {
-#pragma unroll
-                        for (int k = 0; k < 32; ++k) sum[u + k] += __uint_as_float(r[k]);
-                    }
-                } else {
-                    float z[32];
-#pragma unroll
-                    for (int k = 0; k < 32; ++k) z[k] = __uint_as_float(r[k]);
-                    e.take(z, e.col + u);
-                }
-            }
-            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-            __syncwarp();
-            if (lane == 0) {
-                const uint32_t done = smem_u32(&sh.acc_empty[buf]);
-                if (CG == 2) arrive_cluster(of_leader(done)); else mbar_arrive(done);
+                if (!PROMOTE) head_take<KIND, PROMOTE>(g, q, v, st, z, col + u * 64, unscale, buf, lane);
             }
         }
         if (PROMOTE) {
 #pragma unroll
-            for (int u = 0; u < kHalf; u += 32) {
-                float z[32];
-#pragma unroll
-                for (int k = 0; k < 32; ++k) z[k] = sum[u + k];
-                e.take(z, e.col + u);
+            for (int u = 0; u < CG; ++u) head_take<KIND, PROMOTE>(g, q, v, st, sum[u], col + u * 64, unscale, buf, lane);
+        }
+        if (KIND == kHeadStats) {
+            // the two halves of the columns meet in shared memory, in one of two places by turns
+            float* meet = (float*)area + (i & 1) * 384 + (warp & 3) * 32 + lane;
+            if (right) { meet[0] = st.ref; meet[128] = st.sum; meet[256] = st.elog; }
+            asm volatile("bar.sync 1, %0;" ::"n"(32 * kHeadEpiWarps) : "memory");
+            if (!right && v.row < q.rows) {
+                st.join(meet[0], meet[128], meet[256]);
+                float* p = g.part + (long long)(g.part0 + v.x.n) * q.rows + v.row;
+                const long long plane = (long long)g.parts * q.rows;
+                p[0] = st.ref;
+                p[plane] = st.sum;
+                if (g.entropy) p[2 * plane] = st.elog;
             }
         }
-        e.finish(warp >> 2);
+        v = next;
     }
+    if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");       // what this warp has stored is there
 }
 
 // KIND: kHeadStats, kHeadGrad, or kHeadHidden for both products of d.
@@ -553,7 +617,7 @@ __global__ void __launch_bounds__(kHeadThreads, 1) head_kernel(const __grid_cons
         }
     }
     if (tid == 32) {
-        for (int k = 0; k < kHeadStages; ++k) {
+        for (int k = 0; k < kHeadMaxStages; ++k) {
             asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(smem_u32(&sh.full[k])) : "memory");
             asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(smem_u32(&sh.empty[k])) : "memory");
         }
@@ -568,7 +632,8 @@ __global__ void __launch_bounds__(kHeadThreads, 1) head_kernel(const __grid_cons
     __syncthreads();
     if (CG == 2) cluster_sync();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-    if (warp < kHeadEpiWarps) head_epilogue<CG, KIND, PROMOTE>(g, sh, rank, warp, lane);
+    cudaGridDependencySynchronize();                          // all before this touches nothing that an earlier launch has
+    if (warp < kHeadEpiWarps) head_epilogue<CG, KIND, PROMOTE>(g, sh, smem + kHeadRing, rank, warp, lane);
     else if (tid == 32 * kHeadEpiWarps) head_copies<CG>(g, smem, sh, rank);
     else if (tid == 32 * (kHeadEpiWarps + 1) && rank == 0) head_products<CG>(g, smem, sh);
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -593,6 +658,7 @@ template <typename T>
 __global__ void __launch_bounds__(256) head_pack_kernel(const T* x, long long rows, int dim, long long ld, unsigned short* out, int ldp, long long plane) {
     const int pairs = ldp / 2;
     const long long n = rows * pairs;
+    cudaGridDependencySynchronize();
     for (long long i = blockIdx.x * 256LL + threadIdx.x; i < n; i += gridDim.x * 256LL) {
         const long long r = i / pairs;
         const int c = (int)(i - r * pairs) * 2;
@@ -616,48 +682,55 @@ __global__ void __launch_bounds__(256) head_pack_kernel(const T* x, long long ro
     }
 }
 
-// Row values from the parts' statistics: kHeadRowThreads threads for `width` rows, the others share a row's parts.
+// Row values from the parts' statistics: kHeadRowThreads threads for `width` rows, which share a row's parts.  The largest reference is
+// found first, so that the terms of the sums do not wait for one another.
 constexpr int kHeadRowThreads = 512;
 __global__ void __launch_bounds__(kHeadRowThreads) head_rows_kernel(const float* part, int parts, int rows, int width, const float* ztok, const void* tokens,
-                                                                    int token_bytes, long long vocab, float c, float* logp, float* entropy, float* lse,
+                                                                    int token_bytes, long long vocab, float c, int with_entropy, float* logp, float* entropy, float* lse,
                                                                     int* status) {
-    __shared__ float sm[3][kHeadRowThreads];
+    __shared__ float sm[2][kHeadRowThreads];
     const int tid = threadIdx.x, lane = tid % width, share = tid / width, shares = kHeadRowThreads / width;
     const int r = blockIdx.x * width + lane;
-    float ref = -INFINITY, sum = 0.f, elog = 0.f;
-    auto join = [&](float m, float s, float e) {
-        if (s == 0.f) return;                                 // nothing that can occur; a NaN goes on
-        const float now = fmaxf(ref, m);
-        const float f = ref == -INFINITY ? 0.f : exp2f(ref - now), h = exp2f(m - now);
-        elog = (f > 0.f ? f * fmaf(ref - now, sum, elog) : 0.f) + h * fmaf(m - now, s, e);
-        sum = f * sum + h * s;
-        ref = now;
-    };
+    const long long plane = (long long)parts * rows;
+    cudaGridDependencySynchronize();
+    float ref = -INFINITY;
     if (r < rows) {
-        const long long plane = (long long)parts * rows;
-#pragma unroll 4
-        for (int k = share; k < parts; k += shares) {
-            const float* p = part + (long long)k * rows + r;
-            join(p[0], p[plane], p[2 * plane]);
-        }
+#pragma unroll 8
+        for (int k = share; k < parts; k += shares) ref = fmaxf(ref, part[(long long)k * rows + r]);
     }
-    sm[0][tid] = ref; sm[1][tid] = sum; sm[2][tid] = elog;
+    sm[0][tid] = ref;
     for (int n = shares / 2; n; n /= 2) {
         __syncthreads();
-        if (share < n) {
-            const int o = tid + n * width;
-            join(sm[0][o], sm[1][o], sm[2][o]);
-            sm[0][tid] = ref; sm[1][tid] = sum; sm[2][tid] = elog;
+        if (share < n) sm[0][tid] = fmaxf(sm[0][tid], sm[0][tid + n * width]);
+    }
+    __syncthreads();
+    ref = sm[0][lane];
+    const float base = ref == -INFINITY ? 0.f : ref;
+    float sum = 0.f, elog = 0.f;
+    if (r < rows) {
+#pragma unroll 8
+        for (int k = share; k < parts; k += shares) {
+            const float* p = part + (long long)k * rows + r;
+            const float m = p[0], s = p[plane], e = with_entropy ? p[2 * plane] : 0.f, d = m - base, f = exp2f(d);
+            sum = fmaf(f, s, sum);
+            elog += f != 0.f ? f * fmaf(d, s, e) : 0.f;       // a part that cannot occur is -inf away; a NaN goes on by the sum
         }
     }
+    __syncthreads();
+    sm[0][tid] = sum; sm[1][tid] = elog;
+    for (int n = shares / 2; n; n /= 2) {
+        __syncthreads();
+        if (share < n) { sm[0][tid] += sm[0][tid + n * width]; sm[1][tid] += sm[1][tid + n * width]; }
+    }
     if (share != 0 || r >= rows) return;
+    sum = sm[0][tid]; elog = sm[1][tid];
     const double ln2 = 0.69314718055994530942, ls = log((double)sum);
-    if (lse) lse[r] = sum == 0.f ? -INFINITY : (float)((double)ref * ln2 + ls);
+    if (lse) lse[r] = sum == 0.f ? -INFINITY : (float)((double)base * ln2 + ls);
     if (entropy) entropy[r] = sum == 0.f ? 0.f : (float)(ls - ln2 * (double)elog / (double)sum);
     if (logp) {
         const long long id = token_bytes == 8 ? token_id((const long long*)tokens, r, vocab, status) : token_id((const int*)tokens, r, vocab, status);
         // the token's logit against the reference as the sum has it, so that a sure token's value keeps its digits
-        logp[r] = id < 0 ? (sum == sum ? 0.f : sum) : sum == 0.f ? -INFINITY : (float)(ln2 * ((double)ztok[r] * (double)c - (double)ref) - ls);
+        logp[r] = id < 0 ? (sum == sum ? 0.f : sum) : sum == 0.f ? -INFINITY : (float)(ln2 * ((double)ztok[r] * (double)c - (double)base) - ls);
     }
 }
 
@@ -667,6 +740,7 @@ __global__ void __launch_bounds__(1024) head_coef_kernel(int rows, long long voc
                                                          HeadRow* coef, int* row_token, float* unscale, int* status) {
     __shared__ float most[32];
     const int tid = threadIdx.x;
+    cudaGridDependencySynchronize();
     auto row = [&](int r, HeadRow& h) {
         long long id = -1;
         if (tokens) id = token_bytes == 8 ? token_id((const long long*)tokens, r, vocab, status) : token_id((const int*)tokens, r, vocab, status);
@@ -711,6 +785,7 @@ template <typename T>
 __global__ void __launch_bounds__(256) head_sum_kernel(const float* plane, long long plane_size, int planes, int ldp, int rows, int dim, const float* unscale,
                                                        T* out, long long ldo) {
     const int groups = ldp / 8;
+    cudaGridDependencySynchronize();
     const float f = *unscale;
     for (long long i = blockIdx.x * 256LL + threadIdx.x; i < (long long)rows * groups; i += gridDim.x * 256LL) {
         const long long r = i / groups;

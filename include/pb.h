@@ -428,7 +428,8 @@ int pb_dropout(const void* dev_x, int dtype, int64_t rows, int64_t dim, int64_t 
  * y and x are the stream, of stream_dtype (float32, or dtype); u, h and gate are of dtype; the norms' weights
  * are float32 or of dtype.  Row r takes row r / rows_per_gate of the gate: 1 is a gate per row, a sequence's length one
  * per sequence, rows one for all.  Sums are float32, y enters the norm before it is rounded.  The rstds
- * (float32, [rows], may be NULL) are for the backward.  y may be the very buffer of x, h that of u.  dim is at most 16384. */
+ * (float32, [rows], may be NULL) are for the backward.  y may be the very buffer of x, h that of u.  rows is at most 2^30, dim
+ * 16384. */
 typedef struct {
     int64_t rows, dim;
     int32_t dtype, stream_dtype, weight_dtype;

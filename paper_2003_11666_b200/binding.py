@@ -138,10 +138,10 @@ def load_library():
     lib.pb_head_logprob_backward.argtypes = [vp, vp, i32, i64, i64, i64, i64, i64, vp, i32, C.c_double, vp, vp, vp, vp, vp, vp, i64, vp, i32, i64, i32,
                                              vp, C.c_size_t, vp, vp]
     lib.pb_dropout.argtypes = [vp, i32, i64, i64, i64, C.c_double, C.c_uint64, i64, vp, vp, i64, vp]
-    lib.pb_join_forward.argtypes = [C.POINTER(pb_join_args), vp]
+    lib.pb_join_forward.argtypes = [vp, vp]                   # a pb_join_args, by reference or as its bytes
     lib.pb_join_scratch_bytes.argtypes = [i64, i64, i64]
     lib.pb_join_scratch_bytes.restype = C.c_size_t
-    lib.pb_join_backward.argtypes = [C.POINTER(pb_join_args), C.POINTER(pb_join_grads), vp, C.c_size_t, vp]
+    lib.pb_join_backward.argtypes = [vp, vp, vp, C.c_size_t, vp]
     _lib = lib
     return lib
 

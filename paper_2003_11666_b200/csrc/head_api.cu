@@ -122,12 +122,6 @@ bool map_of_out(CUtensorMap* map, const void* p, int64_t rows, int64_t cols, int
     return tensor_map(map, p, 3, dims, strides, box, false, elem == 4);
 }
 
-HeadDiv div_by(int64_t d) {
-    int l = 0;
-    while (((int64_t)1 << l) < d) ++l;
-    return HeadDiv{(unsigned)(((uint64_t)1 << (31 + l)) / (uint64_t)d + 1), 31 + l};
-}
-
 // D[m, n] = sum over k of a[m, k] b[n, k]; an MN-major operand lies as [k, m] or [k, n].
 bool job_of(HeadJob& j, int kind, int cg, const HeadMatrix& a, bool a_mn, const HeadMatrix& b, bool b_mn, int64_t chunks_per_split = 0) {
     const int64_t tile = 128 * cg, m = a_mn ? a.cols : a.rows, n = b_mn ? b.cols : b.rows, k = a_mn ? a.rows : a.cols;
@@ -147,10 +141,10 @@ bool job_of(HeadJob& j, int kind, int cg, const HeadMatrix& a, bool a_mn, const 
     j.cols = (int)n;
     j.tiles = j.tiles_m * j.tiles_n * j.splits;
     j.groups = (j.tiles_m + j.group_m - 1) / j.group_m;
-    j.by_split = div_by((int64_t)j.tiles_m * j.tiles_n);
-    j.by_group = div_by((int64_t)j.group_m * j.tiles_n);
-    j.by_height = div_by(j.group_m);
-    j.by_last = div_by(j.tiles_m - (j.groups - 1) * j.group_m);
+    j.by_split = Quotient((int64_t)j.tiles_m * j.tiles_n);
+    j.by_group = Quotient((int64_t)j.group_m * j.tiles_n);
+    j.by_height = Quotient(j.group_m);
+    j.by_last = Quotient(j.tiles_m - (j.groups - 1) * j.group_m);
     return true;
 }
 

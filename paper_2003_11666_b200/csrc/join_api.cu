@@ -11,8 +11,7 @@ using namespace pb;
 
 namespace {
 
-constexpr int64_t kMaxJoinDim = 16384;
-constexpr int kJoinBlocks = 2 * kSms;           // of the backward: each ends in a partial sum of the weights' gradients
+constexpr int64_t kMaxJoinDim = 16384, kMaxJoinRows = 1 << 30;
 constexpr int kJoinTurns = 2;                   // chunks per worker of the backward, where gates are long enough
 
 int refuse(const char* who, const char* what) {
@@ -21,32 +20,34 @@ int refuse(const char* who, const char* what) {
     return fail_text(PB_E_ARG, text);
 }
 
-// Threads of a row, eight columns each as long as that takes no more than 512.
-int join_lanes(int64_t dim, int& units) {
-    units = dim > 4096 ? 2 : 1;
-    int lanes = 1;
-    while ((int64_t)lanes * 8 * units < dim) lanes *= 2;
-    return lanes;
+// Threads of a row: eight columns each, or 16 in rows of more than `wide` columns.
+int join_lanes_log(int64_t dim, int64_t wide, int& units) {
+    units = dim > wide ? 2 : 1;
+    int l = 0;
+    while (((int64_t)8 * units << l) < dim) ++l;
+    return l;
 }
 
 struct JoinPlan {
-    int lanes, units, threads, blocks;
-    int64_t chunk_rows, chunks_per_gate, chunks;
+    int lanes_log, units, threads, slots, blocks;
+    int64_t rows_per_gate, chunk_rows, chunks_per_gate, chunks;
     float *pre, *post, *gate;
     size_t bytes;
 };
 JoinPlan join_plan(int64_t rows, int64_t dim, int64_t rows_per_gate, char* scratch) {
     JoinPlan e{};
-    e.lanes = join_lanes(dim, e.units);
-    e.threads = std::max(kJoinThreads, e.lanes);
-    const int64_t slots = e.threads / e.lanes, gate = rows_per_gate > 0 ? std::min(rows_per_gate, rows) : rows;
-    const int64_t want = std::max<int64_t>(1, (rows + kJoinBlocks * slots * kJoinTurns - 1) / (kJoinBlocks * slots * kJoinTurns));
+    e.lanes_log = join_lanes_log(dim, 4096, e.units);
+    e.threads = std::max(kJoinThreads, 1 << e.lanes_log);
+    e.slots = e.threads >> e.lanes_log;
+    e.rows_per_gate = rows_per_gate > 0 ? std::min(rows_per_gate, rows) : rows;
+    const int64_t gate = e.rows_per_gate, most = kSms * std::max<int64_t>(1, 512 / e.threads), workers = most * e.slots;      // what is resident at 128 registers
+    const int64_t want = std::max<int64_t>(1, (rows + workers * kJoinTurns - 1) / (workers * kJoinTurns));
     e.chunks_per_gate = gate > want ? (gate + want - 1) / want : 1;
     e.chunk_rows = (gate + e.chunks_per_gate - 1) / e.chunks_per_gate;
     e.chunks_per_gate = (gate + e.chunk_rows - 1) / e.chunk_rows;                  // none is empty
     const int64_t whole = rows / gate, rest = rows - whole * gate;
     e.chunks = whole * e.chunks_per_gate + (rest + e.chunk_rows - 1) / e.chunk_rows;
-    e.blocks = (int)std::min<int64_t>(kJoinBlocks, (e.chunks + slots - 1) / slots);
+    e.blocks = (int)std::min<int64_t>(most, (e.chunks + e.slots - 1) / e.slots);
     size_t at = 0;
     auto take = [&](int64_t floats) {
         float* p = scratch ? (float*)(scratch + at) : nullptr;
@@ -67,7 +68,7 @@ bool share_of(double p, unsigned& drop) {
     return drop < 65536;
 }
 Keep keep_of(unsigned drop, uint64_t seed, int64_t offset, const int64_t* dev_offset) {
-    return Keep{seed, offset, (const long long*)dev_offset, drop, (float)(65536.0 / (65536.0 - drop))};
+    return Keep{seed, offset, (const long long*)dev_offset, drop << 16, (float)(65536.0 / (65536.0 - drop))};
 }
 
 template <typename F> auto by_types(int dtype, int stream_dtype, F f) {
@@ -83,7 +84,7 @@ const char* bad_join(const pb_join_args& a) {
     if (!dtype_ok(a.dtype) || !dtype_ok(a.stream_dtype) || !dtype_ok(a.weight_dtype)) return "unknown element type";
     if (a.stream_dtype != PB_F32 && a.stream_dtype != a.dtype) return "the residual stream is float32 or of the block's type";
     if (a.weight_dtype != PB_F32 && a.weight_dtype != a.dtype) return "the norms' weights are float32 or of the block's type";
-    if (a.rows < 0 || a.rows > kMaxCount) return "rows out of range";
+    if (a.rows < 0 || a.rows > kMaxJoinRows) return "rows must be between 0 and 2^30";
     if (a.dim < 1 || a.dim > kMaxJoinDim) return "dim must be between 1 and 16384";
     if (a.gate && (a.rows_per_gate < 1 || a.rows_per_gate > kMaxCount)) return "rows_per_gate must be at least 1";
     if (a.gate && a.ld_gate < a.dim) return "a row stride is smaller than dim";
@@ -95,12 +96,12 @@ const char* bad_join(const pb_join_args& a) {
     return nullptr;
 }
 
-JoinParams params_of(const pb_join_args& a, int lanes) {
+JoinParams params_of(const pb_join_args& a, int lanes_log) {
     JoinParams p{};
-    p.rows = a.rows; p.dim = (int)a.dim; p.lanes = lanes;
+    p.rows = a.rows; p.dim = (int)a.dim; p.lanes_log = lanes_log;
     p.u = a.u; p.ld_u = a.ld_u;
     p.gate = a.gate; p.ld_gate = a.ld_gate;
-    p.rows_per_gate = a.gate ? a.rows_per_gate : std::max<int64_t>(a.rows, 1);
+    p.by_gate = Quotient(a.gate ? a.rows_per_gate : std::max<int64_t>(a.rows, 1));
     p.post = a.post_weight; p.pre = a.pre_weight;
     p.weights_f32 = a.weight_dtype == PB_F32;
     p.rstd_post = a.rstd_post; p.rstd_pre = a.rstd_pre;
@@ -159,7 +160,7 @@ int pb_dropout(const void* dev_x, int dtype, int64_t rows, int64_t dim, int64_t 
 }
 
 size_t pb_join_scratch_bytes(int64_t rows, int64_t dim, int64_t rows_per_gate) {
-    if (rows < 0 || rows > kMaxCount || dim < 1 || dim > kMaxJoinDim || rows_per_gate < 0) return 0;
+    if (rows < 0 || rows > kMaxJoinRows || dim < 1 || dim > kMaxJoinDim || rows_per_gate < 0) return 0;
     return join_plan(std::max<int64_t>(rows, 1), dim, rows_per_gate, nullptr).bytes;
 }
 
@@ -189,15 +190,17 @@ int pb_join_forward(const pb_join_args* args, void* stream) {
             if (meet(out[k], out[l])) return refuse(who, "two outputs overlap");
     }
     int units;
-    const int lanes = join_lanes(a.dim, units), threads = std::max(kJoinThreads, lanes);
-    JoinParams p = params_of(a, lanes);
+    // 16 columns per thread where that leaves every SM as many threads as it holds: half the instructions that a row's sums take.
+    const int lanes_log = join_lanes_log(a.dim, a.rows * a.dim >= (int64_t)kSms * 1024 * 16 && a.dim >= 512 ? 511 : 8192, units);
+    const int threads = std::max(kJoinThreads, 1 << lanes_log);
+    JoinParams p = params_of(a, lanes_log);
     p.x = a.x; p.ld_x = a.ld_x;
     p.y = a.y; p.ld_y = a.ld_y;
     p.h = a.h; p.ld_h = a.ld_h;
     const bool pieces = a.dim % 8 == 0 && piece_ok(a.x, a.ld_x, a.rows, a.stream_dtype) && piece_ok(a.u, a.ld_u, a.rows, a.dtype) &&
                         piece_ok(a.y, a.ld_y, a.rows, a.stream_dtype) && piece_ok(a.h, a.ld_h, a.rows, a.dtype) && piece_ok(a.gate, a.ld_gate, gates, a.dtype) &&
                         piece_ok(a.post_weight, 0, 1, a.weight_dtype) && piece_ok(a.pre_weight, 0, 1, a.weight_dtype);
-    const int64_t slots = threads / lanes;
+    const int64_t slots = threads >> lanes_log;
     const dim3 grid((unsigned)((a.rows + slots - 1) / slots));
     return launched(who, by_types(a.dtype, a.stream_dtype, [&](auto t, auto st) {
         using T = decltype(t);
@@ -255,14 +258,15 @@ int pb_join_backward(const pb_join_args* args, const pb_join_grads* grads, void*
         for (int l = 0; l < k; ++l)
             if (meet(out[k], out[l])) return refuse(who, "two outputs overlap");
     }
-    JoinParams p = params_of(a, e.lanes);
+    JoinParams p = params_of(a, e.lanes_log);
     p.yin = a.y; p.ld_y = a.ld_y;
     p.dy = d.dy; p.ld_dy = d.ld_dy;
     p.dh = d.dh; p.ld_dh = d.ld_dh;
     p.dx = d.dx; p.ld_dx = d.ld_dx;
     p.du = d.du; p.ld_du = d.ld_du;
-    p.chunk_rows = e.chunk_rows; p.chunks_per_gate = e.chunks_per_gate; p.chunks = e.chunks;
-    p.rows_per_gate = a.gate ? std::min(a.rows_per_gate, a.rows) : a.rows;
+    p.rows_per_gate = (int)e.rows_per_gate;
+    p.chunk_rows = (int)e.chunk_rows; p.chunks_per_gate = (int)e.chunks_per_gate; p.chunks = (int)e.chunks;
+    p.by_chunks = Quotient(e.chunks_per_gate);
     p.dgate = d.dgate; p.ld_dgate = d.ld_dgate;
     p.dgate_f32 = d.dgate_dtype == PB_F32;
     p.gate_part = e.gate;
@@ -273,15 +277,17 @@ int pb_join_backward(const pb_join_args* args, const pb_join_grads* grads, void*
                         piece_ok(d.dx, d.ld_dx, a.rows, a.stream_dtype) && piece_ok(d.du, d.ld_du, a.rows, a.dtype) &&
                         piece_ok(a.gate, a.ld_gate, gates, a.dtype) && piece_ok(d.dgate, d.ld_dgate, gates, d.dgate_dtype) &&
                         piece_ok(a.post_weight, 0, 1, a.weight_dtype) && piece_ok(a.pre_weight, 0, 1, a.weight_dtype);
-    const int slots = e.threads / e.lanes;
-    const size_t shared = slots > 1 ? (size_t)e.threads * 8 * e.units * 4 : 0;
+    const size_t shared = e.slots > 1 ? (size_t)e.threads * 8 * e.units * 4 : 0;
     return launched(who, by_types(a.dtype, a.stream_dtype, [&](auto t, auto st) {
         using T = decltype(t);
         using S = decltype(st);
-        auto kernel = pieces ? (e.units == 1 ? join_backward_kernel<T, S, true, 1, 512> : e.lanes <= 512 ? join_backward_kernel<T, S, true, 2, 512>
-                                                                                                        : join_backward_kernel<T, S, true, 2, 1024>)
-                             : (e.units == 1 ? join_backward_kernel<T, S, false, 1, 512> : e.lanes <= 512 ? join_backward_kernel<T, S, false, 2, 512>
-                                                                                                         : join_backward_kernel<T, S, false, 2, 1024>);
+        auto by_pieces = [&](auto pc) {
+            constexpr bool P = decltype(pc)::value;
+            if (e.threads <= 256) return join_backward_kernel<T, S, P, 1, 256, true>;
+            if (e.units == 1) return join_backward_kernel<T, S, P, 1, 512, true>;
+            return e.threads <= 512 ? join_backward_kernel<T, S, P, 2, 512, false> : join_backward_kernel<T, S, P, 2, 1024, false>;
+        };
+        auto kernel = pieces ? by_pieces(std::true_type()) : by_pieces(std::false_type());
         cudaLaunchConfig_t c{};
         c.gridDim = dim3((unsigned)e.blocks);
         c.blockDim = dim3((unsigned)e.threads);

@@ -93,6 +93,18 @@ struct Pair {
 __device__ __forceinline__ Pair operator*(Pair a, Pair b) { Pair r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.x) : "l"(a.x), "l"(b.x)); return r; }
 __device__ __forceinline__ Pair operator+(Pair a, Pair b) { Pair r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.x) : "l"(a.x), "l"(b.x)); return r; }
 __device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) { Pair r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.x) : "l"(a.x), "l"(b.x), "l"(c.x)); return r; }
+// Quotient of a number below 2^31 by d >= 1: n m >> s with m = floor(2^s / d) + 1, s = 31 + ceil(log2 d).
+struct Quotient {
+    unsigned m;
+    int s;
+    Quotient() = default;
+    __host__ explicit Quotient(long long d) : m(0), s(31) {
+        while ((1ll << (s - 31)) < d) ++s;
+        m = (unsigned)((1ull << s) / (unsigned long long)d + 1);
+    }
+    __device__ __forceinline__ int operator()(int n) const { return (int)((unsigned long long)(unsigned)n * m >> s); }
+};
+
 // SplitMix64 finaliser (Steele, Lea & Flood 2014) of a counter on a stream that starts at `base`.
 __host__ __device__ __forceinline__ unsigned long long splitmix64(unsigned long long base, unsigned long long counter) {
     unsigned long long z = base + (counter + 1ull) * 0x9E3779B97F4A7C15ull;

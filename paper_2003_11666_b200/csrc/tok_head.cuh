@@ -43,13 +43,6 @@ constexpr int kHeadPlanes = 3;                // bfloat16 planes of a float32 op
 
 enum HeadKind { kHeadStats = 0, kHeadGrad = 1, kHeadHidden = 2, kHeadWeight = 3 };
 
-// Quotient of a number below 2^31 by d >= 1: n m >> s with m = floor(2^s / d) + 1, s = 31 + ceil(log2 d).
-struct HeadDiv {
-    unsigned m;
-    int s;
-    __device__ __forceinline__ int operator()(int n) const { return (int)((unsigned long long)(unsigned)n * m >> s); }
-};
-
 // One product: tiles_m x tiles_n tiles, K split `splits` ways.
 struct alignas(64) HeadJob {
     CUtensorMap a, b;            // K-major: (k, row, plane); MN-major: (row, k, plane)
@@ -61,7 +54,7 @@ struct alignas(64) HeadJob {
     int chunks, chunks_per_split;
     int rows, cols;              // of D
     int tiles;                   // tiles_m * tiles_n * splits
-    HeadDiv by_split, by_group, by_height, by_last;      // tiles of a split, of a group; row tiles of a group, of the last one
+    Quotient by_split, by_group, by_height, by_last;      // tiles of a split, of a group; row tiles of a group, of the last one
     int groups;
     int a_bytes;                 // bytes of A that a stage receives per block
 };

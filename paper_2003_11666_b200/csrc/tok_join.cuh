@@ -18,6 +18,59 @@
 
 namespace pb {
 
+// ------------------------------------------------------------------ eight columns
+// Eight numbers of a thread as four pairs, on which one instruction works at a time: these kernels run out of instructions before they run out of
+// memory bandwidth (16384 x 4096 with a gate and dropout: 242 us one by one).
+struct Eight {
+    Pair p[4];
+    __device__ __forceinline__ void fill(float a) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) p[k] = Pair(a);
+    }
+    __device__ __forceinline__ void from(const float (&v)[8]) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) p[k] = Pair(v[2 * k], v[2 * k + 1]);
+    }
+    __device__ __forceinline__ void to(float (&v)[8]) const {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) p[k].split(v[2 * k], v[2 * k + 1]);
+    }
+};
+__device__ __forceinline__ Eight operator*(const Eight& a, const Eight& b) {
+    Eight r;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) r.p[k] = a.p[k] * b.p[k];
+    return r;
+}
+__device__ __forceinline__ Eight operator*(const Eight& a, float s) {
+    const Pair f(s);
+    Eight r;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) r.p[k] = a.p[k] * f;
+    return r;
+}
+__device__ __forceinline__ Eight fma8(const Eight& a, const Eight& b, const Eight& c) {
+    Eight r;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) r.p[k] = fma2(a.p[k], b.p[k], c.p[k]);
+    return r;
+}
+__device__ __forceinline__ Eight fma8(float s, const Eight& b, const Eight& c) {
+    const Pair f(s);
+    Eight r;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) r.p[k] = fma2(f, b.p[k], c.p[k]);
+    return r;
+}
+__device__ __forceinline__ float dot8(const Eight& a, const Eight& b) {
+    Pair s = a.p[0] * b.p[0], t = a.p[1] * b.p[1];
+    s = fma2(a.p[2], b.p[2], s);
+    t = fma2(a.p[3], b.p[3], t);
+    float x, y;
+    (s + t).split(x, y);
+    return x + y;
+}
+
 // ------------------------------------------------------------------ which elements are kept
 // Element i of a call's [rows, dim] values (i = row * dim + column) has bits 16 (i mod 4) .. + 15 of the hash of counter i / 4 on the
 // stream that (seed, offset) name; it is kept where they are at least `drop`.
@@ -25,64 +78,96 @@ struct Keep {
     unsigned long long seed;
     long long offset;
     const long long* dev_offset;
-    unsigned drop;               // of 65536
+    unsigned drop;               // of 65536, in the upper half of the word
     float scale;                 // 65536 / (65536 - drop)
 };
 __device__ __forceinline__ unsigned long long keep_base(const Keep& k) {
     return splitmix64(k.seed, (unsigned long long)(k.dev_offset ? *k.dev_offset : k.offset));
 }
-__device__ __forceinline__ void keep4(float (&f)[4], unsigned long long base, unsigned long long quad, const Keep& k) {
-    const unsigned long long z = splitmix64(base, quad);
-    const unsigned lo = (unsigned)z, hi = (unsigned)(z >> 32);
-    f[0] = (lo & 0xffffu) >= k.drop ? k.scale : 0.f;
-    f[1] = (lo >> 16) >= k.drop ? k.scale : 0.f;
-    f[2] = (hi & 0xffffu) >= k.drop ? k.scale : 0.f;
-    f[3] = (hi >> 16) >= k.drop ? k.scale : 0.f;
+// Zero where the half word is below `drop`, whatever was there; the low half is moved up, the upper one is compared with what is below it.
+__device__ __forceinline__ Pair keep2(Pair v, unsigned bits, unsigned drop) {
+    float a, b;
+    v.split(a, b);
+    return Pair((bits << 16) >= drop ? a : 0.f, bits >= drop ? b : 0.f);
+}
+// Elements 4 quad .. + 7, not scaled yet.
+__device__ __forceinline__ Eight keep8(const Eight& v, unsigned long long base, unsigned long long quad, unsigned drop) {
+    const unsigned long long y = splitmix64(base, quad), z = splitmix64(base, quad + 1);
+    Eight r;
+    r.p[0] = keep2(v.p[0], (unsigned)y, drop);
+    r.p[1] = keep2(v.p[1], (unsigned)(y >> 32), drop);
+    r.p[2] = keep2(v.p[2], (unsigned)z, drop);
+    r.p[3] = keep2(v.p[3], (unsigned)(z >> 32), drop);
+    return r;
+}
+__device__ __forceinline__ bool kept(unsigned long long base, unsigned long long i, unsigned drop) {
+    return ((unsigned)(splitmix64(base, i / 4) >> (16 * (i % 4))) << 16) >= drop;
 }
 
-__device__ __forceinline__ void load_piece(float (&x)[8], const float* p) { load8_wide(x, p); }
-template <typename T> __device__ __forceinline__ void load_piece(float (&x)[8], const T* p) { load8(x, p); }
-__device__ __forceinline__ void store_piece(float* p, const float (&x)[8]) { store8_wide(p, x); }
-template <typename T> __device__ __forceinline__ void store_piece(T* p, const float (&x)[8]) { store8(p, x); }
-
-// What is dropped is zero, whatever it was.
-__device__ __forceinline__ float kept(float f, float x) { return f != 0.f ? f * x : 0.f; }
+// Eight consecutive elements as they lie in memory.
+template <typename T> struct RawEight {
+    uint4 q;
+    __device__ __forceinline__ void load(const T* p) { q = *reinterpret_cast<const uint4*>(p); }
+    __device__ __forceinline__ void zero() { q = make_uint4(0, 0, 0, 0); }
+    __device__ __forceinline__ Eight get() const {
+        float v[8];
+        unpack8(v, q, T());
+        Eight r;
+        r.from(v);
+        return r;
+    }
+};
+template <> struct RawEight<float> {
+    float v[8];
+    __device__ __forceinline__ void load(const float* p) { load8_wide(v, p); }
+    __device__ __forceinline__ void zero() {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = 0.f;
+    }
+    __device__ __forceinline__ Eight get() const {
+        Eight r;
+        r.from(v);
+        return r;
+    }
+};
+__device__ __forceinline__ void store_eight(float* p, const Eight& x) {
+    float v[8];
+    x.to(v);
+    store8_wide(p, v);
+}
+template <typename T> __device__ __forceinline__ void store_eight(T* p, const Eight& x) {
+    float v[8];
+    x.to(v);
+    store8(p, v);
+}
 
 constexpr int kDropThreads = 256;
 
-// kDense: the rows follow each other without a gap, the whole is one row.  kPieces: eight elements at a time.
+// kPieces: eight elements at a time; dense: the rows follow each other without a gap, the whole is one row.
 template <typename T, bool kPieces>
 __global__ void __launch_bounds__(kDropThreads) dropout_kernel(const T* x, T* out, long long n, long long cols, long long ld_x, long long ld_out, bool dense, Keep k) {
     const unsigned long long base = keep_base(k);
-    const long long step = (long long)gridDim.x * kDropThreads;
-    if (kPieces) {
-        for (long long i = blockIdx.x * (long long)kDropThreads + threadIdx.x; i < n / 8; i += step) {
+    const long long step = (long long)gridDim.x * kDropThreads, first = blockIdx.x * (long long)kDropThreads + threadIdx.x;
+    if constexpr (kPieces) {
+        for (long long i = first; i < n / 8; i += step) {
             const long long r = dense ? 0 : i * 8 / cols, c = i * 8 - r * cols;
-            float v[8], f[4], g[4];
-            load_piece(v, x + r * ld_x + c);
-            keep4(f, base, 2 * i, k);
-            keep4(g, base, 2 * i + 1, k);
-#pragma unroll
-            for (int u = 0; u < 4; ++u) { v[u] = kept(f[u], v[u]); v[u + 4] = kept(g[u], v[u + 4]); }
-            store_piece(out + r * ld_out + c, v);
+            RawEight<T> v;
+            v.load(x + r * ld_x + c);
+            store_eight(out + r * ld_out + c, keep8(v.get() * k.scale, base, 2 * i, k.drop));
         }
         if (blockIdx.x == 0 && threadIdx.x < n % 8) {         // dense only
             const long long i = n / 8 * 8 + threadIdx.x;
-            float f[4];
-            keep4(f, base, i / 4, k);
-            out[i] = from_f32<T>(kept(i % 4 == 0 ? f[0] : i % 4 == 1 ? f[1] : i % 4 == 2 ? f[2] : f[3], to_f32(x[i])));
+            out[i] = from_f32<T>(kept(base, i, k.drop) ? to_f32(x[i]) * k.scale : 0.f);
         }
-        return;
-    }
-    for (long long q = blockIdx.x * (long long)kDropThreads + threadIdx.x; q < (n + 3) / 4; q += step) {
-        float f[4];
-        keep4(f, base, q, k);
-        long long r = dense ? 0 : q * 4 / cols, c = q * 4 - r * cols;
+    } else {
+        for (long long q = first; q < (n + 3) / 4; q += step) {
+            const unsigned long long z = splitmix64(base, q);
+            long long r = dense ? 0 : q * 4 / cols, c = q * 4 - r * cols;
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            if (q * 4 + u < n) out[r * ld_out + c] = from_f32<T>(kept(f[u], to_f32(x[r * ld_x + c])));
-            if (!dense && ++c == cols) { c = 0; ++r; }
-            else if (dense) ++c;
+            for (int u = 0; u < 4; ++u) {
+                if (q * 4 + u < n) out[r * ld_out + c] = from_f32<T>(((unsigned)(z >> (16 * u)) << 16) >= k.drop ? to_f32(x[r * ld_x + c]) * k.scale : 0.f);
+                if (++c == cols && !dense) { c = 0; ++r; }
+            }
         }
     }
 }
@@ -90,17 +175,18 @@ __global__ void __launch_bounds__(kDropThreads) dropout_kernel(const T* x, T* ou
 // ------------------------------------------------------------------ join
 struct JoinParams {
     long long rows;
-    int dim, lanes;              // threads of a row: a power of two
+    int dim, lanes_log;          // log2 of the threads of a row
     const void *x, *u, *gate, *post, *pre, *yin, *dy, *dh;
     void *y, *h, *dx, *du;
     long long ld_x, ld_u, ld_y, ld_h, ld_gate, ld_dy, ld_dh, ld_dx, ld_du, ld_dgate;
     float *rstd_post, *rstd_pre;
     bool weights_f32;            // else of u's type
-    long long rows_per_gate;
+    Quotient by_gate;            // rows that share a row of the gate
     float rs, eps, inv_dim;
     Keep keep;                   // drop == 0: everything is kept
     // backward: chunks of rows that share a gate
-    long long chunk_rows, chunks_per_gate, chunks;
+    int rows_per_gate, chunk_rows, chunks_per_gate, chunks;
+    Quotient by_chunks;
     float* gate_part;            // [chunks][dim], or NULL: a chunk is all rows of its gate, and written to dgate
     void* dgate;
     bool dgate_f32;
@@ -111,251 +197,267 @@ constexpr int kJoinThreads = 256;             // of a block, or the threads of a
 constexpr int kJoinMaxLanes = 1024;
 
 // Sum over the threads of a row.  Rows of more than a warp meet in shared memory: all threads of the block call this.
-__device__ __forceinline__ float row_sum(float v, int lanes, float* sm) {
-    for (int k = min(lanes, 32) / 2; k; k /= 2) v += __shfl_xor_sync(0xffffffffu, v, k);
-    if (lanes <= 32) return v;
-    const int warp = threadIdx.x / 32, n = lanes / 32, first = warp / n * n;
-    if (threadIdx.x % 32 == 0) sm[warp] = v;
-    __syncthreads();
-    const int l = threadIdx.x % 32;
-    v = l < n ? sm[first + l] : 0.f;
+__device__ __forceinline__ float row_sum(float v, int lanes_log, float* sm) {
+    if (lanes_log < 5) {
+        for (int k = (1 << lanes_log) / 2; k; k /= 2) v += __shfl_xor_sync(0xffffffffu, v, k);
+        return v;
+    }
 #pragma unroll
     for (int k = 16; k; k /= 2) v += __shfl_xor_sync(0xffffffffu, v, k);
+    if (lanes_log == 5) return v;
+    const int warp = threadIdx.x / 32, l = threadIdx.x % 32, n = 1 << (lanes_log - 5);
+    if (l == 0) sm[warp] = v;
+    __syncthreads();
+    v = sm[(warp & ~(n - 1)) + (l & (n - 1))];               // as often as the warp has room for it
+    for (int k = n / 2; k; k /= 2) v += __shfl_xor_sync(0xffffffffu, v, k);
     return v;
 }
 
+// 1 / sqrt(x) to 2^-23: the approximation, and one step of Newton's method where that is finite.
+__device__ __forceinline__ float root_of(float x) {
+    const float r = rsqrtf(x);
+    return r > 0.f && r < INFINITY ? r * fmaf(-0.5f * x * r, r, 1.5f) : r;
+}
+
 // Eight columns of a row: in pieces consecutive ones, else `lanes` apart, so that neighbours read neighbours.
+template <typename T, bool kPieces> struct RawColumns : RawEight<T> {};
+template <typename T> struct RawColumns<T, false> {
+    T v[8];
+    __device__ __forceinline__ Eight get() const {
+        Eight r;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) r.p[k] = Pair(to_f32(v[2 * k]), to_f32(v[2 * k + 1]));
+        return r;
+    }
+};
 template <bool kPieces>
 struct Columns {
     int first, step, n;          // n: how many exist
-    __device__ __forceinline__ Columns(int lane, int unit, int lanes, int dim) {
-        first = kPieces ? (unit * lanes + lane) * 8 : unit * 8 * lanes + lane;
-        step = kPieces ? 1 : lanes;
-        n = first >= dim ? 0 : min(8, (dim - first + step - 1) / step);
+    __device__ __forceinline__ Columns(int lane, int unit, int lanes_log, int dim) {
+        first = kPieces ? ((unit << lanes_log) + lane) * 8 : (unit * 8 << lanes_log) + lane;
+        step = kPieces ? 1 : 1 << lanes_log;
+        n = first >= dim ? 0 : kPieces ? 8 : min(8, (dim - first + step - 1) >> lanes_log);
     }
-    template <typename T> __device__ __forceinline__ void load(float (&v)[8], const T* row) const {
-        if (kPieces) {
-            if (n) load_piece(v, row + first);
-            else
-#pragma unroll
-                for (int k = 0; k < 8; ++k) v[k] = 0.f;
+    template <typename T> __device__ __forceinline__ void load(RawColumns<T, kPieces>& v, const T* row) const {
+        if constexpr (kPieces) {
+            if (n) v.load(row + first); else v.zero();
         } else {
 #pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] = k < n ? to_f32(row[first + k * step]) : 0.f;
+            for (int k = 0; k < 8; ++k) v.v[k] = k < n ? row[first + k * step] : from_f32<T>(0.f);
         }
     }
-    template <typename T> __device__ __forceinline__ void store(T* row, const float (&v)[8]) const {
-        if (kPieces) {
-            if (n) store_piece(row + first, v);
+    template <typename T> __device__ __forceinline__ Eight get(const T* row) const {
+        RawColumns<T, kPieces> v;
+        load(v, row);
+        return v.get();
+    }
+    template <typename T> __device__ __forceinline__ Eight weight(const void* w, bool f32) const {
+        return f32 ? get((const float*)w) : get((const T*)w);
+    }
+    template <typename T> __device__ __forceinline__ void put(T* row, const Eight& x) const {
+        if constexpr (kPieces) {
+            if (n) store_eight(row + first, x);
         } else {
+            float v[8];
+            x.to(v);
 #pragma unroll
             for (int k = 0; k < 8; ++k)
                 if (k < n) row[first + k * step] = from_f32<T>(v[k]);
         }
     }
-    __device__ __forceinline__ void keep(float (&f)[8], unsigned long long base, long long row, int dim, const Keep& k) const {
-        if (kPieces) {                                       // dim is a multiple of 8
-            const unsigned long long q = ((unsigned long long)row * dim + first) / 4;
-            float a[4], b[4];
-            keep4(a, base, q, k);
-            keep4(b, base, q + 1, k);
+    // What dropout leaves of a row's columns.
+    __device__ __forceinline__ Eight drop(const Eight& x, unsigned long long base, long long row, int dim, const Keep& k) const {
+        const unsigned long long i = (unsigned long long)row * dim + first;
+        if constexpr (kPieces) return keep8(x * k.scale, base, i / 4, k.drop);       // dim is a multiple of 8
+        float v[8];
+        (x * k.scale).to(v);
 #pragma unroll
-            for (int u = 0; u < 4; ++u) { f[u] = a[u]; f[u + 4] = b[u]; }
-        } else {
-#pragma unroll
-            for (int u = 0; u < 8; ++u) {
-                const unsigned long long i = (unsigned long long)row * dim + first + u * step;
-                const unsigned long long z = splitmix64(base, i / 4);
-                f[u] = (unsigned)(z >> (16 * (i % 4)) & 0xffffu) >= k.drop ? k.scale : 0.f;
-            }
-        }
+        for (int u = 0; u < 8; ++u) v[u] = kept(base, i + u * step, k.drop) ? v[u] : 0.f;
+        Eight r;
+        r.from(v);
+        return r;
     }
 };
-
-template <bool kPieces, typename T>
-__device__ __forceinline__ void load_weight(float (&v)[8], const Columns<kPieces>& c, const void* w, bool f32) {
-    if (f32) c.load(v, (const float*)w); else c.load(v, (const T*)w);
-}
 
 template <typename T, typename S, bool kPieces, int kUnits>
 __global__ void __launch_bounds__(kJoinMaxLanes) join_forward_kernel(const JoinParams p) {
     __shared__ float sm[2][32];
-    const int lane = threadIdx.x % p.lanes, slot = threadIdx.x / p.lanes, slots = blockDim.x / p.lanes;
+    const int lane = threadIdx.x & ((1 << p.lanes_log) - 1), slot = threadIdx.x >> p.lanes_log, slots = blockDim.x >> p.lanes_log;
     const unsigned long long base = p.keep.drop ? keep_base(p.keep) : 0;
     const long long r = (long long)blockIdx.x * slots + slot;
     const bool live = r < p.rows;
-    float y[kUnits][8], b[kUnits][8];
+    Eight y[kUnits], b[kUnits];
     float sum = 0.f;
 #pragma unroll
     for (int k = 0; k < kUnits; ++k) {
-        Columns<kPieces> c(lane, k, p.lanes, p.dim);
+        Columns<kPieces> c(lane, k, p.lanes_log, p.dim);
         if (!live) c.n = 0;
-        c.load(y[k], (const S*)p.x + r * p.ld_x);
-        c.load(b[k], (const T*)p.u + r * p.ld_u);
-#pragma unroll
-        for (int u = 0; u < 8; ++u) sum = fmaf(b[k][u], b[k][u], sum);
+        b[k] = c.get((const T*)p.u + r * p.ld_u);
+        y[k] = c.get((const S*)p.x + r * p.ld_x);
     }
     float rstd = 1.f;
     if (p.post) {
-        rstd = 1.f / sqrtf(fmaf(row_sum(sum, p.lanes, sm[0]), p.inv_dim, p.eps));
+#pragma unroll
+        for (int k = 0; k < kUnits; ++k) sum += dot8(b[k], b[k]);
+        rstd = root_of(fmaf(row_sum(sum, p.lanes_log, sm[0]), p.inv_dim, p.eps));
         if (live && lane == 0 && p.rstd_post) p.rstd_post[r] = rstd;
     }
     sum = 0.f;
 #pragma unroll
     for (int k = 0; k < kUnits; ++k) {
-        Columns<kPieces> c(lane, k, p.lanes, p.dim);
+        Columns<kPieces> c(lane, k, p.lanes_log, p.dim);
         if (!live) c.n = 0;
-        float v[8];
-        if (p.post) {
-            load_weight<kPieces, T>(v, c, p.post, p.weights_f32);
-#pragma unroll
-            for (int u = 0; u < 8; ++u) b[k][u] = b[k][u] * rstd * v[u];
-        }
-        if (p.gate) {
-            c.load(v, (const T*)p.gate + (live ? r / p.rows_per_gate : 0) * p.ld_gate);
-#pragma unroll
-            for (int u = 0; u < 8; ++u) b[k][u] *= v[u];
-        }
-        if (p.keep.drop) {
-            c.keep(v, base, r, p.dim, p.keep);
-#pragma unroll
-            for (int u = 0; u < 8; ++u) b[k][u] = kept(v[u], b[k][u]);
-        }
-#pragma unroll
-        for (int u = 0; u < 8; ++u) {
-            y[k][u] = fmaf(p.rs, y[k][u], b[k][u]);
-            sum = fmaf(y[k][u], y[k][u], sum);               // columns that do not exist are zero
-        }
-        c.store((S*)p.y + r * p.ld_y, y[k]);
+        if (p.post) b[k] = b[k] * rstd * c.template weight<T>(p.post, p.weights_f32);
+        if (p.gate) b[k] = b[k] * c.get((const T*)p.gate + (live ? p.by_gate((int)r) : 0) * p.ld_gate);
+        if (p.keep.drop) b[k] = c.drop(b[k], base, r, p.dim, p.keep);
+        y[k] = fma8(p.rs, y[k], b[k]);                       // columns that do not exist are zero
+        c.put((S*)p.y + r * p.ld_y, y[k]);
+        sum += dot8(y[k], y[k]);
     }
     if (!p.h) return;
-    rstd = 1.f / sqrtf(fmaf(row_sum(sum, p.lanes, sm[1]), p.inv_dim, p.eps));
+    rstd = root_of(fmaf(row_sum(sum, p.lanes_log, sm[1]), p.inv_dim, p.eps));
     if (!live) return;
     if (lane == 0 && p.rstd_pre) p.rstd_pre[r] = rstd;
 #pragma unroll
     for (int k = 0; k < kUnits; ++k) {
-        const Columns<kPieces> c(lane, k, p.lanes, p.dim);
-        float v[8];
-        load_weight<kPieces, T>(v, c, p.pre, p.weights_f32);
-#pragma unroll
-        for (int u = 0; u < 8; ++u) v[u] *= y[k][u] * rstd;
-        c.store((T*)p.h + r * p.ld_h, v);
+        const Columns<kPieces> c(lane, k, p.lanes_log, p.dim);
+        c.put((T*)p.h + r * p.ld_h, y[k] * rstd * c.template weight<T>(p.pre, p.weights_f32));
     }
 }
 
-template <typename T, typename S, bool kPieces, int kUnits, int kThreads>
-__global__ void __launch_bounds__(kThreads) join_backward_kernel(const JoinParams p) {
+// What the backward reads of a row.
+template <typename T, typename S, bool kPieces>
+struct JoinRow {
+    RawColumns<T, kPieces> u, dh, gate;
+    RawColumns<S, kPieces> y, dy;
+    float rp, rr;
+};
+
+// kAhead: a row is read while the one before it is worked on, and the weights stay in registers.
+template <typename T, typename S, bool kPieces, int kUnits, int kThreads, bool kAhead>
+__global__ void __launch_bounds__(kThreads, 512 / kThreads > 0 ? 512 / kThreads : 1) join_backward_kernel(const JoinParams p) {
     extern __shared__ float cross[];             // [slots][lanes * 8 * kUnits]
     __shared__ float sm[2][2][32];
-    const int lane = threadIdx.x % p.lanes, slot = threadIdx.x / p.lanes, slots = blockDim.x / p.lanes;
+    const int lane = threadIdx.x & ((1 << p.lanes_log) - 1), slot = threadIdx.x >> p.lanes_log, slots = blockDim.x >> p.lanes_log;
     const unsigned long long base = p.keep.drop ? keep_base(p.keep) : 0;
-    const long long workers = (long long)gridDim.x * slots;
-    float dpre[kUnits][8] = {}, dpost[kUnits][8] = {}, dgate[kUnits][8] = {};
-    int turn = 0;
-    // every worker takes as many turns, so that the threads of a block meet in row_sum
-    for (long long k0 = 0; k0 < p.chunks; k0 += workers) {
-        const long long chunk = k0 + (long long)blockIdx.x * slots + slot;
-        const long long group = chunk / p.chunks_per_gate;
-        const long long first = group * p.rows_per_gate + (chunk - group * p.chunks_per_gate) * p.chunk_rows;
-        const long long last = chunk < p.chunks ? min(min(first + p.chunk_rows, (group + 1) * p.rows_per_gate), p.rows) : first;
-        for (long long q = 0; q < p.chunk_rows; ++q, turn ^= 1) {
-            const long long r = first + q;
-            const bool live = r < last;
-            const float rp = live && p.post ? p.rstd_post[r] : 1.f, rr = live && p.dh ? p.rstd_pre[r] : 0.f;
-            float g[kUnits][8], un[kUnits][8], yn[kUnits][8], w[kUnits][8];
-            float sum = 0.f;
+    const int workers = (int)gridDim.x * slots;
+    Eight dpre[kUnits], dpost[kUnits], dgate[kUnits], post[kUnits], pre[kUnits];
 #pragma unroll
-            for (int k = 0; k < kUnits; ++k) {
-                Columns<kPieces> c(lane, k, p.lanes, p.dim);
-                if (!live) c.n = 0;
-                c.load(un[k], (const T*)p.u + r * p.ld_u);
-                if (p.dy) c.load(g[k], (const S*)p.dy + r * p.ld_dy);
-                else
+    for (int k = 0; k < kUnits; ++k) {
+        dpre[k].fill(0.f); dpost[k].fill(0.f); dgate[k].fill(0.f);
+        if (kAhead) {
+            const Columns<kPieces> c(lane, k, p.lanes_log, p.dim);
+            if (p.post) post[k] = c.template weight<T>(p.post, p.weights_f32);
+            if (p.dh) pre[k] = c.template weight<T>(p.pre, p.weights_f32);
+        }
+    }
+    // The rows of a worker: chunk by chunk, every worker as many turns (so that the threads of a block meet in row_sum), some of them idle.
+    struct Place {
+        int chunk, q, group;
+        long long r;
+        bool live;
+    };
+    auto place = [&](int chunk, int q) {
+        Place a;
+        a.chunk = chunk; a.q = q;
+        a.group = p.by_chunks(chunk);
+        const int within = (chunk - a.group * p.chunks_per_gate) * p.chunk_rows + q;
+        a.r = (long long)a.group * p.rows_per_gate + within;
+        a.live = chunk < p.chunks && within < p.rows_per_gate && a.r < p.rows;
+        return a;
+    };
+    auto read = [&](JoinRow<T, S, kPieces> (&v)[kUnits], const Place& a) {
 #pragma unroll
-                    for (int u = 0; u < 8; ++u) g[k][u] = 0.f;
-                if (p.dh) {
-                    float v[8];
-                    c.load(yn[k], (const S*)p.yin + r * p.ld_y);
-                    c.load(w[k], (const T*)p.dh + r * p.ld_dh);
-                    load_weight<kPieces, T>(v, c, p.pre, p.weights_f32);
-#pragma unroll
-                    for (int u = 0; u < 8; ++u) {
-                        yn[k][u] *= rr;
-                        dpre[k][u] = fmaf(w[k][u], yn[k][u], dpre[k][u]);
-                        w[k][u] *= v[u];
-                        sum = fmaf(w[k][u], yn[k][u], sum);
-                    }
-                }
-            }
+        for (int k = 0; k < kUnits; ++k) {
+            Columns<kPieces> c(lane, k, p.lanes_log, p.dim);
+            if (!a.live) c.n = 0;
+            c.load(v[k].u, (const T*)p.u + a.r * p.ld_u);
+            if (p.dy) c.load(v[k].dy, (const S*)p.dy + a.r * p.ld_dy);
             if (p.dh) {
-                const float m = row_sum(sum, p.lanes, sm[turn][0]) * p.inv_dim;
-#pragma unroll
-                for (int k = 0; k < kUnits; ++k)
-#pragma unroll
-                    for (int u = 0; u < 8; ++u) g[k][u] = fmaf(rr, fmaf(-m, yn[k][u], w[k][u]), g[k][u]);
+                c.load(v[k].y, (const S*)p.yin + a.r * p.ld_y);
+                c.load(v[k].dh, (const T*)p.dh + a.r * p.ld_dh);
             }
-            sum = 0.f;
+            if (p.gate) c.load(v[k].gate, (const T*)p.gate + a.group * p.ld_gate);
+        }
+        v[0].rp = a.live && p.post ? p.rstd_post[a.r] : 1.f;
+        v[0].rr = a.live && p.dh ? p.rstd_pre[a.r] : 0.f;
+    };
+    const int mine = (int)blockIdx.x * slots + slot, rounds = (p.chunks + workers - 1) / workers;
+    JoinRow<T, S, kPieces> row[kUnits];
+    Place at = place(mine, 0);
+    if (kAhead) read(row, at);
+    for (int round = 0, q = 0, turn = 0; round < rounds; turn ^= 1) {
+        if (!kAhead) read(row, at);
+        Eight g[kUnits], un[kUnits], yn[kUnits], gate[kUnits];
+        float sum = 0.f;
+        const float rp = row[0].rp, rr = row[0].rr;
+        const Place now = at;
 #pragma unroll
-            for (int k = 0; k < kUnits; ++k) {
-                Columns<kPieces> c(lane, k, p.lanes, p.dim);
-                if (!live) c.n = 0;
-                float v[8];
-                if (p.dx) {
-#pragma unroll
-                    for (int u = 0; u < 8; ++u) v[u] = p.rs * g[k][u];
-                    c.store((S*)p.dx + r * p.ld_dx, v);
-                }
-                if (p.keep.drop) {
-                    c.keep(v, base, r, p.dim, p.keep);
-#pragma unroll
-                    for (int u = 0; u < 8; ++u) g[k][u] = kept(v[u], g[k][u]);
-                }
-                float post[8];
-                if (p.post) {
-                    load_weight<kPieces, T>(post, c, p.post, p.weights_f32);
-#pragma unroll
-                    for (int u = 0; u < 8; ++u) un[k][u] *= rp;
-                }
-                if (p.gate) {
-                    c.load(v, (const T*)p.gate + (live ? group : 0) * p.ld_gate);
-#pragma unroll
-                    for (int u = 0; u < 8; ++u) {
-                        dgate[k][u] = fmaf(g[k][u], p.post ? un[k][u] * post[u] : un[k][u], dgate[k][u]);
-                        g[k][u] *= v[u];
-                    }
-                }
-                if (p.post) {
-#pragma unroll
-                    for (int u = 0; u < 8; ++u) {
-                        dpost[k][u] = fmaf(g[k][u], un[k][u], dpost[k][u]);
-                        g[k][u] *= post[u];
-                        sum = fmaf(g[k][u], un[k][u], sum);
-                    }
-                }
-            }
-            float m = 0.f;
-            if (p.post) m = row_sum(sum, p.lanes, sm[turn][1]) * p.inv_dim;
-            if (live) {
-#pragma unroll
-                for (int k = 0; k < kUnits; ++k) {
-                    const Columns<kPieces> c(lane, k, p.lanes, p.dim);
-                    if (p.post) {
-#pragma unroll
-                        for (int u = 0; u < 8; ++u) g[k][u] = rp * fmaf(-m, un[k][u], g[k][u]);
-                    }
-                    c.store((T*)p.du + r * p.ld_du, g[k]);
-                }
+        for (int k = 0; k < kUnits; ++k) {
+            const Columns<kPieces> c(lane, k, p.lanes_log, p.dim);
+            un[k] = row[k].u.get();
+            if (p.gate) gate[k] = row[k].gate.get();
+            if (p.dy) g[k] = row[k].dy.get(); else g[k].fill(0.f);
+            if (p.dh) {
+                const Eight w = kAhead ? pre[k] : c.template weight<T>(p.pre, p.weights_f32), dh = row[k].dh.get();
+                yn[k] = row[k].y.get() * rr;
+                dpre[k] = fma8(dh, yn[k], dpre[k]);
+                const Eight wd = dh * w;
+                sum += dot8(wd, yn[k]);
+                g[k] = fma8(rr, wd, g[k]);
             }
         }
-        if (p.dgate && chunk < p.chunks) {
+        const bool ends = ++q == p.chunk_rows;                // of the chunk
+        if (ends) { q = 0; ++round; }
+        at = place(mine + round * workers, q);
+        if (kAhead && round < rounds) read(row, at);
+        if (p.dh) {
+            const float m = -rr * p.inv_dim * row_sum(sum, p.lanes_log, sm[turn][0]);
+#pragma unroll
+            for (int k = 0; k < kUnits; ++k) g[k] = fma8(m, yn[k], g[k]);
+        }
+        sum = 0.f;
+#pragma unroll
+        for (int k = 0; k < kUnits; ++k) {
+            Columns<kPieces> c(lane, k, p.lanes_log, p.dim);
+            if (!now.live) c.n = 0;
+            if (p.dx) c.put((S*)p.dx + now.r * p.ld_dx, g[k] * p.rs);
+            if (p.keep.drop) g[k] = c.drop(g[k], base, now.r, p.dim, p.keep);
+            if (!p.post) {
+                if (p.gate) {
+                    dgate[k] = fma8(g[k], un[k], dgate[k]);
+                    g[k] = g[k] * gate[k];
+                }
+                c.put((T*)p.du + now.r * p.ld_du, g[k]);
+            } else {
+                const Eight w = kAhead ? post[k] : c.template weight<T>(p.post, p.weights_f32);
+                un[k] = un[k] * rp;
+                if (p.gate) {
+                    dgate[k] = fma8(g[k], un[k] * w, dgate[k]);
+                    g[k] = g[k] * gate[k];
+                }
+                dpost[k] = fma8(g[k], un[k], dpost[k]);
+                g[k] = g[k] * w;
+                sum += dot8(g[k], un[k]);
+            }
+        }
+        if (p.post) {
+            const float m = -rp * p.inv_dim * row_sum(sum, p.lanes_log, sm[turn][1]);
 #pragma unroll
             for (int k = 0; k < kUnits; ++k) {
-                const Columns<kPieces> c(lane, k, p.lanes, p.dim);
-                if (p.gate_part) c.store(p.gate_part + chunk * p.dim, dgate[k]);
-                else if (p.dgate_f32) c.store((float*)p.dgate + group * p.ld_dgate, dgate[k]);
-                else c.store((T*)p.dgate + group * p.ld_dgate, dgate[k]);
+                Columns<kPieces> c(lane, k, p.lanes_log, p.dim);
+                if (!now.live) c.n = 0;
+                c.put((T*)p.du + now.r * p.ld_du, fma8(m, un[k], g[k] * rp));
+            }
+        }
+        if (ends && p.dgate && now.chunk < p.chunks) {
 #pragma unroll
-                for (int u = 0; u < 8; ++u) dgate[k][u] = 0.f;
+            for (int k = 0; k < kUnits; ++k) {
+                const Columns<kPieces> c(lane, k, p.lanes_log, p.dim);
+                if (p.gate_part) c.put(p.gate_part + (long long)now.chunk * p.dim, dgate[k]);
+                else if (p.dgate_f32) c.put((float*)p.dgate + now.group * p.ld_dgate, dgate[k]);
+                else c.put((T*)p.dgate + now.group * p.ld_dgate, dgate[k]);
+                dgate[k].fill(0.f);
             }
         }
     }
@@ -364,16 +466,19 @@ __global__ void __launch_bounds__(kThreads) join_backward_kernel(const JoinParam
         float* part = which ? p.part_post : p.part_pre;
         if (!part) continue;
         part += (long long)blockIdx.x * p.dim;
-        const int width = p.lanes * 8 * kUnits;
+        const int width = 8 * kUnits << p.lanes_log;
         if (slots > 1) {
             __syncthreads();
 #pragma unroll
-            for (int k = 0; k < kUnits; ++k)
+            for (int k = 0; k < kUnits; ++k) {
+                float v[8];
+                (which ? dpost[k] : dpre[k]).to(v);
 #pragma unroll
                 for (int u = 0; u < 8; ++u) {
-                    const int column = kPieces ? (k * p.lanes + lane) * 8 + u : (k * 8 + u) * p.lanes + lane;
-                    cross[slot * width + column] = which ? dpost[k][u] : dpre[k][u];
+                    const int column = kPieces ? ((k << p.lanes_log) + lane) * 8 + u : ((k * 8 + u) << p.lanes_log) + lane;
+                    cross[slot * width + column] = v[u];
                 }
+            }
             __syncthreads();
             for (int c = threadIdx.x; c < p.dim; c += blockDim.x) {
                 float s = 0.f;
@@ -382,7 +487,7 @@ __global__ void __launch_bounds__(kThreads) join_backward_kernel(const JoinParam
             }
         } else {
 #pragma unroll
-            for (int k = 0; k < kUnits; ++k) Columns<kPieces>(lane, k, p.lanes, p.dim).store(part, which ? dpost[k] : dpre[k]);
+            for (int k = 0; k < kUnits; ++k) Columns<kPieces>(lane, k, p.lanes_log, p.dim).put(part, which ? dpost[k] : dpre[k]);
         }
     }
 }

@@ -8,10 +8,11 @@ an integer (0: the legacy default stream), names another one.  Arguments that do
 PBError with code -1 before anything is launched.
 """
 import ctypes as C
+import struct
 
 import torch
 
-from .binding import PBError, load_library, pb_adamw_args, pb_adamw_tensor, pb_join_args, pb_join_grads
+from .binding import PBError, load_library, pb_adamw_args, pb_adamw_tensor
 
 _DTYPE = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 _ID_BYTES = {torch.int64: 8, torch.int32: 4}
@@ -271,43 +272,49 @@ def dropout(x, out, p, seed, offset=0, dev_offset=None, stream=None):
                            out.data_ptr(), ld_out, _current(d) if stream is None else stream))
 
 
-def _join_weights(who, dim, post_weight, pre_weight):
-    """Type of the norms' weights, which have one."""
-    given = [w for w in (post_weight, pre_weight) if w is not None]
-    if not given:
-        return torch.float32
-    if any(w.dtype not in _DTYPE or w.dtype is not given[0].dtype for w in given):
-        _refuse(who, "the norms' weights must be of one type")
-    return given[0].dtype
+# pb_join_args and pb_join_grads in their own order: one call lays all fields out, where setting them one by one takes as long as the launch.
+_JOIN_ARGS, _JOIN_GRADS = struct.Struct("@qqiiiffdQqPPqPqPqqPPPqPqPP"), struct.Struct("@PqPqPqPqPqPPii")
 
 
-def _join_like(who, name, t, rows, dim, dtype):
-    """Address and row stride of a [rows, dim] matrix that may be absent."""
+def _plane(who, name, t, shape, dtype, device):
+    """Address and row stride of a matrix with dense rows that may be absent."""
     if t is None:
-        return None, dim
-    r, c, ld = _rows(who, name, t)
-    if (r, c) != (rows, dim) or t.dtype is not dtype:
-        _refuse(who, "%s must be [rows, dim] of type %s" % (name, dtype))
-    return t.data_ptr(), ld
+        return 0, shape[1]
+    if t.shape != shape or t.dtype is not dtype:
+        _refuse(who, "%s must be a matrix of %d x %d of type %s" % (name, *shape, dtype))
+    if t.get_device() != device:
+        _refuse(who, _OFF_DEVICE)
+    ld, step = t.stride()
+    if step != 1 and shape[1] > 1:
+        _refuse(who, "%s must have dense rows" % name)
+    return t.data_ptr(), ld if shape[0] > 1 else shape[1]
 
 
-def _join_args(who, u, stream_dtype, gate, rows_per_gate, post_weight, pre_weight, rstd_post, rstd_pre, residual_scale, eps, p, seed, offset, dev_offset):
-    rows, dim, ld = _rows(who, "u", u)
-    a = pb_join_args()
-    a.rows, a.dim, a.u, a.ld_u = rows, dim, u.data_ptr(), ld
-    weights = _join_weights(who, dim, post_weight, pre_weight)
-    a.dtype, a.stream_dtype, a.weight_dtype = _DTYPE[u.dtype], _DTYPE[stream_dtype], _DTYPE[weights]
-    a.residual_scale, a.eps, a.p, a.seed, a.offset = residual_scale, eps, p, seed & 0xFFFFFFFFFFFFFFFF, offset
-    a.dev_offset = _vector(who, "dev_offset", dev_offset, 1, torch.int64)
-    if gate is not None:
-        per = rows if rows_per_gate is None else rows_per_gate
-        if rows and per < 1:
-            _refuse(who, "rows_per_gate must be at least 1")
-        a.gate, a.ld_gate = _join_like(who, "gate", gate, -(-rows // max(per, 1)), dim, u.dtype)
-        a.rows_per_gate = max(per, 1)
-    a.post_weight, a.pre_weight = _vector(who, "post_weight", post_weight, dim, weights), _vector(who, "pre_weight", pre_weight, dim, weights)
-    a.rstd_post, a.rstd_pre = _vector(who, "rstd_post", rstd_post, rows), _vector(who, "rstd_pre", rstd_pre, rows)
-    return a
+def _line(who, name, t, n, dtype, device):
+    """Address of a dense vector that may be absent."""
+    if t is None:
+        return 0
+    if t.get_device() != device:
+        _refuse(who, _OFF_DEVICE)
+    return _vector(who, name, t, n, dtype)
+
+
+def _one_type(who, a, b):
+    """Type of two vectors that have one, if they are there."""
+    dtype = (a if a is not None else b).dtype if a is not None or b is not None else torch.float32
+    if dtype not in _DTYPE or (a is not None and b is not None and b.dtype is not dtype):
+        _refuse(who, "the norms' weights, and their gradients, must be of one type")
+    return dtype
+
+
+def _join_gate(who, gate, rows_per_gate, rows, dim, dtype, device):
+    """Address, row stride and rows per row of the gate."""
+    if gate is None:
+        return 0, dim, 1
+    per = rows_per_gate or rows or 1
+    if per < 1:
+        _refuse(who, "rows_per_gate must be at least 1")
+    return *_plane(who, "gate", gate, (-(-rows // per), dim), dtype, device), per
 
 
 def join_forward(x, u, y, h=None, pre_weight=None, post_weight=None, gate=None, rows_per_gate=None, rstd_pre=None, rstd_post=None, residual_scale=1.0,
@@ -316,14 +323,23 @@ def join_forward(x, u, y, h=None, pre_weight=None, post_weight=None, gate=None, 
     [ceil(rows / rows_per_gate), dim] (rows_per_gate None: one row for all)."""
     who = "join_forward"
     d = _device(who, x)
-    _on_device(who, d, u, y, h, pre_weight, post_weight, gate, rstd_pre, rstd_post, dev_offset)
-    if u is None or y is None or x.dtype not in _DTYPE:
-        _refuse(who, "x, u and y are needed, of float32, bfloat16 or float16")
-    a = _join_args(who, u, x.dtype, gate, rows_per_gate, post_weight, pre_weight, rstd_post, rstd_pre, residual_scale, eps, p, seed, offset, dev_offset)
-    a.x, a.ld_x = _join_like(who, "x", x, a.rows, a.dim, x.dtype)
-    a.y, a.ld_y = _join_like(who, "y", y, a.rows, a.dim, x.dtype)
-    a.h, a.ld_h = _join_like(who, "h", h, a.rows, a.dim, u.dtype)
-    _check(_lib.pb_join_forward(C.byref(a), _current(d) if stream is None else stream))
+    if u is None or y is None:
+        _refuse(who, "u and y are needed")
+    try:
+        shape, stream_dtype, dtype = u.shape, x.dtype, u.dtype
+        if len(shape) != 2 or stream_dtype not in _DTYPE or dtype not in _DTYPE:
+            _refuse(who, "x and u must be matrices of float32, bfloat16 or float16")
+        rows, dim = shape
+        weights = _one_type(who, post_weight, pre_weight)
+        args = _JOIN_ARGS.pack(
+            rows, dim, _DTYPE[dtype], _DTYPE[stream_dtype], _DTYPE[weights], residual_scale, eps, p, seed & 0xFFFFFFFFFFFFFFFF, offset,
+            _line(who, "dev_offset", dev_offset, 1, torch.int64, d), *_plane(who, "x", x, shape, stream_dtype, d), *_plane(who, "u", u, shape, dtype, d),
+            *_join_gate(who, gate, rows_per_gate, rows, dim, dtype, d), _line(who, "post_weight", post_weight, dim, weights, d),
+            _line(who, "pre_weight", pre_weight, dim, weights, d), *_plane(who, "y", y, shape, stream_dtype, d), *_plane(who, "h", h, shape, dtype, d),
+            _line(who, "rstd_post", rstd_post, rows, torch.float32, d), _line(who, "rstd_pre", rstd_pre, rows, torch.float32, d))
+    except (AttributeError, TypeError, struct.error):
+        _refuse(who, "an argument is not what it has to be: tensors on the current device, and numbers")
+    _check(_lib.pb_join_forward(args, _current(d) if stream is None else stream))
 
 
 def join_scratch_bytes(rows, dim, rows_per_gate=0):
@@ -340,26 +356,34 @@ def join_backward(y, u, dx, du, scratch, dy=None, dh=None, pre_weight=None, post
     join_scratch_bytes(...) bytes; y may be None without dh, dx if it is not wanted."""
     who = "join_backward"
     d = _device(who, u)
-    _on_device(who, d, y, dx, du, scratch, dy, dh, pre_weight, post_weight, gate, rstd_pre, rstd_post, dpre_weight, dpost_weight, dgate, dev_offset)
-    stream_dtype = next((t.dtype for t in (y, dy, dx) if t is not None), u.dtype)
-    if du is None or stream_dtype not in _DTYPE:
-        _refuse(who, "du is needed, and the stream of float32, bfloat16 or float16")
-    a = _join_args(who, u, stream_dtype, gate, rows_per_gate, post_weight, pre_weight, rstd_post, rstd_pre, residual_scale, 0.0, p, seed, offset, dev_offset)
-    g = pb_join_grads()
-    a.y, a.ld_y = _join_like(who, "y", y, a.rows, a.dim, stream_dtype)
-    g.dy, g.ld_dy = _join_like(who, "dy", dy, a.rows, a.dim, stream_dtype)
-    g.dh, g.ld_dh = _join_like(who, "dh", dh, a.rows, a.dim, u.dtype)
-    g.dx, g.ld_dx = _join_like(who, "dx", dx, a.rows, a.dim, stream_dtype)
-    g.du, g.ld_du = _join_like(who, "du", du, a.rows, a.dim, u.dtype)
-    if dgate is not None:
-        if gate is None or dgate.dtype not in _DTYPE:
+    if du is None or scratch is None:
+        _refuse(who, "du and scratch are needed")
+    try:
+        shape, dtype = u.shape, u.dtype
+        stream_dtype = dy.dtype if dy is not None else y.dtype if y is not None else dx.dtype if dx is not None else dtype
+        if len(shape) != 2 or stream_dtype not in _DTYPE or dtype not in _DTYPE:
+            _refuse(who, "u must be a matrix of float32, bfloat16 or float16, and so the residual stream")
+        rows, dim = shape
+        weights, grads = _one_type(who, post_weight, pre_weight), _one_type(who, dpost_weight, dpre_weight)
+        gate_type = dtype if dgate is None else dgate.dtype
+        if gate_type not in _DTYPE or (dgate is not None and gate is None):
             _refuse(who, "dgate goes with a gate, and is of float32 or of its type")
-        g.dgate, g.ld_dgate = _join_like(who, "dgate", dgate, gate.shape[0], a.dim, dgate.dtype)
-        g.dgate_dtype = _DTYPE[dgate.dtype]
-    weights = _join_weights(who, a.dim, dpost_weight, dpre_weight)
-    g.dweight_dtype = _DTYPE[weights]
-    g.dpost_weight, g.dpre_weight = _vector(who, "dpost_weight", dpost_weight, a.dim, weights), _vector(who, "dpre_weight", dpre_weight, a.dim, weights)
-    _check(_lib.pb_join_backward(C.byref(a), C.byref(g), *_scratch(who, scratch), _current(d) if stream is None else stream))
+        args = _JOIN_ARGS.pack(
+            rows, dim, _DTYPE[dtype], _DTYPE[stream_dtype], _DTYPE[weights], residual_scale, 0.0, p, seed & 0xFFFFFFFFFFFFFFFF, offset,
+            _line(who, "dev_offset", dev_offset, 1, torch.int64, d), 0, dim, *_plane(who, "u", u, shape, dtype, d),
+            *_join_gate(who, gate, rows_per_gate, rows, dim, dtype, d), _line(who, "post_weight", post_weight, dim, weights, d),
+            _line(who, "pre_weight", pre_weight, dim, weights, d), *_plane(who, "y", y, shape, stream_dtype, d), 0, dim,
+            _line(who, "rstd_post", rstd_post, rows, torch.float32, d), _line(who, "rstd_pre", rstd_pre, rows, torch.float32, d))
+        out = _JOIN_GRADS.pack(
+            *_plane(who, "dy", dy, shape, stream_dtype, d), *_plane(who, "dh", dh, shape, dtype, d), *_plane(who, "dx", dx, shape, stream_dtype, d),
+            *_plane(who, "du", du, shape, dtype, d), *((0, dim) if dgate is None else _plane(who, "dgate", dgate, gate.shape, gate_type, d)),
+            _line(who, "dpost_weight", dpost_weight, dim, grads, d), _line(who, "dpre_weight", dpre_weight, dim, grads, d), _DTYPE[gate_type], _DTYPE[grads])
+        if scratch.get_device() != d:
+            _refuse(who, _OFF_DEVICE)
+        room = _scratch(who, scratch)
+    except (AttributeError, TypeError, struct.error):
+        _refuse(who, "an argument is not what it has to be: tensors on the current device, and numbers")
+    _check(_lib.pb_join_backward(args, out, *room, _current(d) if stream is None else stream))
 
 
 def adamw_moments(m, m_scale, v, v_scale, m_out=None, v_out=None, stream=None):

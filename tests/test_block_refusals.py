@@ -96,7 +96,7 @@ def _join(lib, backward=False, args=True, grads=True, scratch=1 << 50, nscratch=
     return lib.pb_join_forward(C.byref(x) if args else None, None)
 
 
-BOTH = [dict(args=False), dict(dtype=4), dict(stream_dtype=2), dict(weight_dtype=2), dict(stream_dtype=7), dict(rows=-1), dict(rows=1 << 31), dict(dim=0),
+BOTH = [dict(args=False), dict(dtype=4), dict(stream_dtype=2), dict(weight_dtype=2), dict(stream_dtype=7), dict(rows=-1), dict(rows=(1 << 30) + 1), dict(dim=0),
         dict(dim=16385), dict(rows_per_gate=0), dict(ld_gate=63), dict(residual_scale=float("inf")), dict(eps=-1.0), dict(eps=float("nan")), dict(p=1.0),
         dict(p=-1.0), dict(ld_u=63), dict(u=None), dict(u=(1 << 31) + 1), dict(gate=(1 << 32) + 1), dict(post_weight=(1 << 33) + 2), dict(rstd_pre=2),
         dict(dev_offset=4)]

@@ -20,25 +20,29 @@ int refuse(const char* who, const char* what) {
     return fail_text(PB_E_ARG, text);
 }
 
-// Threads of a row: eight columns each, or 16 in rows of more than `wide` columns.
-int join_lanes_log(int64_t dim, int64_t wide, int& units) {
+// Threads of a row, eight columns each, or 16 in rows of more than `wide` columns: a power of two up to a warp, else whole warps.
+int join_lanes(int64_t dim, int64_t wide, int& units) {
     units = dim > wide ? 2 : 1;
-    int l = 0;
-    while (((int64_t)8 * units << l) < dim) ++l;
-    return l;
+    const int64_t n = (dim + 8 * units - 1) / (8 * units);
+    if (n > 32) return (int)((n + 31) / 32 * 32);
+    int lanes = 1;
+    while (lanes < n) lanes *= 2;
+    return lanes;
 }
+// A block: rows of a warp or less share one.
+int join_threads(int lanes) { return lanes > 32 ? lanes : kJoinThreads; }
 
 struct JoinPlan {
-    int lanes_log, units, threads, slots, blocks;
+    int lanes, units, threads, slots, blocks;
     int64_t rows_per_gate, chunk_rows, chunks_per_gate, chunks;
     float *pre, *post, *gate;
     size_t bytes;
 };
 JoinPlan join_plan(int64_t rows, int64_t dim, int64_t rows_per_gate, char* scratch) {
     JoinPlan e{};
-    e.lanes_log = join_lanes_log(dim, 4096, e.units);
-    e.threads = std::max(kJoinThreads, 1 << e.lanes_log);
-    e.slots = e.threads >> e.lanes_log;
+    e.lanes = join_lanes(dim, 4096, e.units);
+    e.threads = join_threads(e.lanes);
+    e.slots = e.threads / e.lanes;
     e.rows_per_gate = rows_per_gate > 0 ? std::min(rows_per_gate, rows) : rows;
     const int64_t gate = e.rows_per_gate, most = kSms * std::max<int64_t>(1, 512 / e.threads), workers = most * e.slots;      // what is resident at 128 registers
     const int64_t want = std::max<int64_t>(1, (rows + workers * kJoinTurns - 1) / (workers * kJoinTurns));
@@ -71,6 +75,7 @@ Keep keep_of(unsigned drop, uint64_t seed, int64_t offset, const int64_t* dev_of
     return Keep{seed, offset, (const long long*)dev_offset, drop << 16, (float)(65536.0 / (65536.0 - drop))};
 }
 
+template <int L> using Layout = std::integral_constant<int, L>;
 template <typename F> auto by_types(int dtype, int stream_dtype, F f) {
     using B = __nv_bfloat16;
     using H = __half;
@@ -96,9 +101,9 @@ const char* bad_join(const pb_join_args& a) {
     return nullptr;
 }
 
-JoinParams params_of(const pb_join_args& a, int lanes_log) {
+JoinParams params_of(const pb_join_args& a, int lanes) {
     JoinParams p{};
-    p.rows = a.rows; p.dim = (int)a.dim; p.lanes_log = lanes_log;
+    p.rows = a.rows; p.dim = (int)a.dim; p.lanes = lanes;
     p.u = a.u; p.ld_u = a.ld_u;
     p.gate = a.gate; p.ld_gate = a.ld_gate;
     p.by_gate = Quotient(a.gate ? a.rows_per_gate : std::max<int64_t>(a.rows, 1));
@@ -191,22 +196,25 @@ int pb_join_forward(const pb_join_args* args, void* stream) {
     }
     int units;
     // 16 columns per thread where that leaves every SM as many threads as it holds: half the instructions that a row's sums take.
-    const int lanes_log = join_lanes_log(a.dim, a.rows * a.dim >= (int64_t)kSms * 1024 * 16 && a.dim >= 512 ? 511 : 8192, units);
-    const int threads = std::max(kJoinThreads, 1 << lanes_log);
-    JoinParams p = params_of(a, lanes_log);
+    const int lanes = join_lanes(a.dim, a.rows * a.dim >= (int64_t)kSms * 1024 * 16 && a.dim >= 512 ? 511 : 8192, units);
+    const int threads = join_threads(lanes);
+    JoinParams p = params_of(a, lanes);
     p.x = a.x; p.ld_x = a.ld_x;
     p.y = a.y; p.ld_y = a.ld_y;
     p.h = a.h; p.ld_h = a.ld_h;
     const bool pieces = a.dim % 8 == 0 && piece_ok(a.x, a.ld_x, a.rows, a.stream_dtype) && piece_ok(a.u, a.ld_u, a.rows, a.dtype) &&
                         piece_ok(a.y, a.ld_y, a.rows, a.stream_dtype) && piece_ok(a.h, a.ld_h, a.rows, a.dtype) && piece_ok(a.gate, a.ld_gate, gates, a.dtype) &&
                         piece_ok(a.post_weight, 0, 1, a.weight_dtype) && piece_ok(a.pre_weight, 0, 1, a.weight_dtype);
-    const int64_t slots = threads >> lanes_log;
+    const int64_t slots = threads / lanes;
     const dim3 grid((unsigned)((a.rows + slots - 1) / slots));
     return launched(who, by_types(a.dtype, a.stream_dtype, [&](auto t, auto st) {
         using T = decltype(t);
         using S = decltype(st);
-        auto kernel = pieces ? (units == 1 ? join_forward_kernel<T, S, true, 1> : join_forward_kernel<T, S, true, 2>)
-                             : (units == 1 ? join_forward_kernel<T, S, false, 1> : join_forward_kernel<T, S, false, 2>);
+        auto by_layout = [&](auto l) {
+            constexpr int L = decltype(l)::value;
+            return units == 1 ? join_forward_kernel<T, S, L, 1> : join_forward_kernel<T, S, L, 2>;
+        };
+        auto kernel = !pieces ? by_layout(Layout<kOdd>()) : slots == 1 && a.dim == 8 * units * lanes ? by_layout(Layout<kFull>()) : by_layout(Layout<kEven>());
         return launch(kernel, grid, threads, (cudaStream_t)stream, p);
     }));
 }
@@ -258,7 +266,7 @@ int pb_join_backward(const pb_join_args* args, const pb_join_grads* grads, void*
         for (int l = 0; l < k; ++l)
             if (meet(out[k], out[l])) return refuse(who, "two outputs overlap");
     }
-    JoinParams p = params_of(a, e.lanes_log);
+    JoinParams p = params_of(a, e.lanes);
     p.yin = a.y; p.ld_y = a.ld_y;
     p.dy = d.dy; p.ld_dy = d.ld_dy;
     p.dh = d.dh; p.ld_dh = d.ld_dh;
@@ -281,13 +289,13 @@ int pb_join_backward(const pb_join_args* args, const pb_join_grads* grads, void*
     return launched(who, by_types(a.dtype, a.stream_dtype, [&](auto t, auto st) {
         using T = decltype(t);
         using S = decltype(st);
-        auto by_pieces = [&](auto pc) {
-            constexpr bool P = decltype(pc)::value;
-            if (e.threads <= 256) return join_backward_kernel<T, S, P, 1, 256, true>;
-            if (e.units == 1) return join_backward_kernel<T, S, P, 1, 512, true>;
-            return e.threads <= 512 ? join_backward_kernel<T, S, P, 2, 512, false> : join_backward_kernel<T, S, P, 2, 1024, false>;
+        auto by_layout = [&](auto l) {
+            constexpr int L = decltype(l)::value;
+            if (e.threads <= 256) return join_backward_kernel<T, S, L, 1, 256, true>;
+            if (e.units == 1) return join_backward_kernel<T, S, L, 1, 512, true>;
+            return e.threads <= 512 ? join_backward_kernel<T, S, L, 2, 512, false> : join_backward_kernel<T, S, L, 2, 1024, false>;
         };
-        auto kernel = pieces ? by_pieces(std::true_type()) : by_pieces(std::false_type());
+        auto kernel = !pieces ? by_layout(Layout<kOdd>()) : e.slots == 1 && a.dim == 8 * e.units * e.lanes ? by_layout(Layout<kFull>()) : by_layout(Layout<kEven>());
         cudaLaunchConfig_t c{};
         c.gridDim = dim3((unsigned)e.blocks);
         c.blockDim = dim3((unsigned)e.threads);

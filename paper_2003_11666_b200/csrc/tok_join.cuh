@@ -175,7 +175,7 @@ __global__ void __launch_bounds__(kDropThreads) dropout_kernel(const T* x, T* ou
 // ------------------------------------------------------------------ join
 struct JoinParams {
     long long rows;
-    int dim, lanes_log;          // log2 of the threads of a row
+    int dim, lanes;              // threads of a row: up to a warp a power of two, else the whole block
     const void *x, *u, *gate, *post, *pre, *yin, *dy, *dh;
     void *y, *h, *dx, *du;
     long long ld_x, ld_u, ld_y, ld_h, ld_gate, ld_dy, ld_dh, ld_dx, ld_du, ld_dgate;
@@ -197,19 +197,20 @@ constexpr int kJoinThreads = 256;             // of a block, or the threads of a
 constexpr int kJoinMaxLanes = 1024;
 
 // Sum over the threads of a row.  Rows of more than a warp meet in shared memory: all threads of the block call this.
-__device__ __forceinline__ float row_sum(float v, int lanes_log, float* sm) {
-    if (lanes_log < 5) {
-        for (int k = (1 << lanes_log) / 2; k; k /= 2) v += __shfl_xor_sync(0xffffffffu, v, k);
+__device__ __forceinline__ float row_sum(float v, int lanes, float* sm) {
+    if (lanes < 32) {
+        for (int k = lanes / 2; k; k /= 2) v += __shfl_xor_sync(0xffffffffu, v, k);
         return v;
     }
 #pragma unroll
     for (int k = 16; k; k /= 2) v += __shfl_xor_sync(0xffffffffu, v, k);
-    if (lanes_log == 5) return v;
-    const int warp = threadIdx.x / 32, l = threadIdx.x % 32, n = 1 << (lanes_log - 5);
-    if (l == 0) sm[warp] = v;
+    if (lanes == 32) return v;
+    const int l = threadIdx.x % 32;
+    if (l == 0) sm[threadIdx.x / 32] = v;
     __syncthreads();
-    v = sm[(warp & ~(n - 1)) + (l & (n - 1))];               // as often as the warp has room for it
-    for (int k = n / 2; k; k /= 2) v += __shfl_xor_sync(0xffffffffu, v, k);
+    v = l * 32 < lanes ? sm[l] : 0.f;
+#pragma unroll
+    for (int k = 16; k; k /= 2) v += __shfl_xor_sync(0xffffffffu, v, k);
     return v;
 }
 
@@ -219,7 +220,9 @@ __device__ __forceinline__ float root_of(float x) {
     return r > 0.f && r < INFINITY ? r * fmaf(-0.5f * x * r, r, 1.5f) : r;
 }
 
-// Eight columns of a row: in pieces consecutive ones, else `lanes` apart, so that neighbours read neighbours.
+// How a thread's eight columns lie: kOdd: `lanes` apart, so that neighbours read neighbours; kEven: consecutive; kFull: consecutive, and every
+// thread has all of its own, in rows of a block each.
+enum JoinLayout { kOdd = 0, kEven = 1, kFull = 2 };
 template <typename T, bool kPieces> struct RawColumns : RawEight<T> {};
 template <typename T> struct RawColumns<T, false> {
     T v[8];
@@ -230,16 +233,19 @@ template <typename T> struct RawColumns<T, false> {
         return r;
     }
 };
-template <bool kPieces>
+template <int kLayout>
 struct Columns {
+    static constexpr bool kPieces = kLayout != kOdd;
     int first, step, n;          // n: how many exist
-    __device__ __forceinline__ Columns(int lane, int unit, int lanes_log, int dim) {
-        first = kPieces ? ((unit << lanes_log) + lane) * 8 : (unit * 8 << lanes_log) + lane;
-        step = kPieces ? 1 : 1 << lanes_log;
-        n = first >= dim ? 0 : kPieces ? 8 : min(8, (dim - first + step - 1) >> lanes_log);
+    __device__ __forceinline__ Columns(int lane, int unit, int lanes, int dim, bool live = true) {
+        first = kPieces ? (unit * lanes + lane) * 8 : unit * 8 * lanes + lane;
+        step = kPieces ? 1 : lanes;
+        n = kLayout == kFull ? 8 : first >= dim || !live ? 0 : kPieces ? 8 : min(8, (dim - first + step - 1) / step);
     }
     template <typename T> __device__ __forceinline__ void load(RawColumns<T, kPieces>& v, const T* row) const {
-        if constexpr (kPieces) {
+        if constexpr (kLayout == kFull) {
+            v.load(row + first);
+        } else if constexpr (kPieces) {
             if (n) v.load(row + first); else v.zero();
         } else {
 #pragma unroll
@@ -256,7 +262,7 @@ struct Columns {
     }
     template <typename T> __device__ __forceinline__ void put(T* row, const Eight& x) const {
         if constexpr (kPieces) {
-            if (n) store_eight(row + first, x);
+            if (kLayout == kFull || n) store_eight(row + first, x);
         } else {
             float v[8];
             x.to(v);
@@ -268,30 +274,34 @@ struct Columns {
     // What dropout leaves of a row's columns.
     __device__ __forceinline__ Eight drop(const Eight& x, unsigned long long base, long long row, int dim, const Keep& k) const {
         const unsigned long long i = (unsigned long long)row * dim + first;
-        if constexpr (kPieces) return keep8(x * k.scale, base, i / 4, k.drop);       // dim is a multiple of 8
-        float v[8];
-        (x * k.scale).to(v);
+        if constexpr (kPieces) {
+            return keep8(x * k.scale, base, i / 4, k.drop);  // dim is a multiple of 8
+        } else {
+            float v[8];
+            (x * k.scale).to(v);
 #pragma unroll
-        for (int u = 0; u < 8; ++u) v[u] = kept(base, i + u * step, k.drop) ? v[u] : 0.f;
-        Eight r;
-        r.from(v);
-        return r;
+            for (int u = 0; u < 8; ++u) v[u] = kept(base, i + u * step, k.drop) ? v[u] : 0.f;
+            Eight r;
+            r.from(v);
+            return r;
+        }
     }
 };
 
-template <typename T, typename S, bool kPieces, int kUnits>
+template <typename T, typename S, int kLayout, int kUnits>
 __global__ void __launch_bounds__(kJoinMaxLanes) join_forward_kernel(const JoinParams p) {
     __shared__ float sm[2][32];
-    const int lane = threadIdx.x & ((1 << p.lanes_log) - 1), slot = threadIdx.x >> p.lanes_log, slots = blockDim.x >> p.lanes_log;
+    constexpr bool kAll = kLayout == kFull;
+    const int lane = kAll || p.lanes > 32 ? threadIdx.x : threadIdx.x & (p.lanes - 1), slot = kAll || p.lanes > 32 ? 0 : threadIdx.x / p.lanes,
+              slots = kAll || p.lanes > 32 ? 1 : blockDim.x / p.lanes;
     const unsigned long long base = p.keep.drop ? keep_base(p.keep) : 0;
     const long long r = (long long)blockIdx.x * slots + slot;
-    const bool live = r < p.rows;
+    const bool live = kAll || r < p.rows;
     Eight y[kUnits], b[kUnits];
     float sum = 0.f;
 #pragma unroll
     for (int k = 0; k < kUnits; ++k) {
-        Columns<kPieces> c(lane, k, p.lanes_log, p.dim);
-        if (!live) c.n = 0;
+        const Columns<kLayout> c(lane, k, p.lanes, p.dim, live);
         b[k] = c.get((const T*)p.u + r * p.ld_u);
         y[k] = c.get((const S*)p.x + r * p.ld_x);
     }
@@ -299,14 +309,13 @@ __global__ void __launch_bounds__(kJoinMaxLanes) join_forward_kernel(const JoinP
     if (p.post) {
 #pragma unroll
         for (int k = 0; k < kUnits; ++k) sum += dot8(b[k], b[k]);
-        rstd = root_of(fmaf(row_sum(sum, p.lanes_log, sm[0]), p.inv_dim, p.eps));
+        rstd = root_of(fmaf(row_sum(sum, p.lanes, sm[0]), p.inv_dim, p.eps));
         if (live && lane == 0 && p.rstd_post) p.rstd_post[r] = rstd;
     }
     sum = 0.f;
 #pragma unroll
     for (int k = 0; k < kUnits; ++k) {
-        Columns<kPieces> c(lane, k, p.lanes_log, p.dim);
-        if (!live) c.n = 0;
+        const Columns<kLayout> c(lane, k, p.lanes, p.dim, live);
         if (p.post) b[k] = b[k] * rstd * c.template weight<T>(p.post, p.weights_f32);
         if (p.gate) b[k] = b[k] * c.get((const T*)p.gate + (live ? p.by_gate((int)r) : 0) * p.ld_gate);
         if (p.keep.drop) b[k] = c.drop(b[k], base, r, p.dim, p.keep);
@@ -315,12 +324,12 @@ __global__ void __launch_bounds__(kJoinMaxLanes) join_forward_kernel(const JoinP
         sum += dot8(y[k], y[k]);
     }
     if (!p.h) return;
-    rstd = root_of(fmaf(row_sum(sum, p.lanes_log, sm[1]), p.inv_dim, p.eps));
+    rstd = root_of(fmaf(row_sum(sum, p.lanes, sm[1]), p.inv_dim, p.eps));
     if (!live) return;
     if (lane == 0 && p.rstd_pre) p.rstd_pre[r] = rstd;
 #pragma unroll
     for (int k = 0; k < kUnits; ++k) {
-        const Columns<kPieces> c(lane, k, p.lanes_log, p.dim);
+        const Columns<kLayout> c(lane, k, p.lanes, p.dim);
         c.put((T*)p.h + r * p.ld_h, y[k] * rstd * c.template weight<T>(p.pre, p.weights_f32));
     }
 }
@@ -334,11 +343,13 @@ struct JoinRow {
 };
 
 // kAhead: a row is read while the one before it is worked on, and the weights stay in registers.
-template <typename T, typename S, bool kPieces, int kUnits, int kThreads, bool kAhead>
+template <typename T, typename S, int kLayout, int kUnits, int kThreads, bool kAhead>
 __global__ void __launch_bounds__(kThreads, 512 / kThreads > 0 ? 512 / kThreads : 1) join_backward_kernel(const JoinParams p) {
     extern __shared__ float cross[];             // [slots][lanes * 8 * kUnits]
     __shared__ float sm[2][2][32];
-    const int lane = threadIdx.x & ((1 << p.lanes_log) - 1), slot = threadIdx.x >> p.lanes_log, slots = blockDim.x >> p.lanes_log;
+    constexpr bool kAll = kLayout == kFull;
+    const int lane = kAll || p.lanes > 32 ? threadIdx.x : threadIdx.x & (p.lanes - 1), slot = kAll || p.lanes > 32 ? 0 : threadIdx.x / p.lanes,
+              slots = kAll || p.lanes > 32 ? 1 : blockDim.x / p.lanes;
     const unsigned long long base = p.keep.drop ? keep_base(p.keep) : 0;
     const int workers = (int)gridDim.x * slots;
     Eight dpre[kUnits], dpost[kUnits], dgate[kUnits], post[kUnits], pre[kUnits];
@@ -346,12 +357,12 @@ __global__ void __launch_bounds__(kThreads, 512 / kThreads > 0 ? 512 / kThreads 
     for (int k = 0; k < kUnits; ++k) {
         dpre[k].fill(0.f); dpost[k].fill(0.f); dgate[k].fill(0.f);
         if (kAhead) {
-            const Columns<kPieces> c(lane, k, p.lanes_log, p.dim);
+            const Columns<kLayout> c(lane, k, p.lanes, p.dim);
             if (p.post) post[k] = c.template weight<T>(p.post, p.weights_f32);
             if (p.dh) pre[k] = c.template weight<T>(p.pre, p.weights_f32);
         }
     }
-    // The rows of a worker: chunk by chunk, every worker as many turns (so that the threads of a block meet in row_sum), some of them idle.
+    // The rows of a worker: chunk by chunk, every worker as many turns, since the workers of a warp move together; some are idle.
     struct Place {
         int chunk, q, group;
         long long r;
@@ -366,11 +377,11 @@ __global__ void __launch_bounds__(kThreads, 512 / kThreads > 0 ? 512 / kThreads 
         a.live = chunk < p.chunks && within < p.rows_per_gate && a.r < p.rows;
         return a;
     };
-    auto read = [&](JoinRow<T, S, kPieces> (&v)[kUnits], const Place& a) {
+    auto read = [&](JoinRow<T, S, kLayout != kOdd> (&v)[kUnits], const Place& a) {
 #pragma unroll
         for (int k = 0; k < kUnits; ++k) {
-            Columns<kPieces> c(lane, k, p.lanes_log, p.dim);
-            if (!a.live) c.n = 0;
+            const Columns<kLayout> c(lane, k, p.lanes, p.dim, a.live);
+            if (kAll && !a.live) continue;                    // nothing of an idle turn is written
             c.load(v[k].u, (const T*)p.u + a.r * p.ld_u);
             if (p.dy) c.load(v[k].dy, (const S*)p.dy + a.r * p.ld_dy);
             if (p.dh) {
@@ -383,7 +394,7 @@ __global__ void __launch_bounds__(kThreads, 512 / kThreads > 0 ? 512 / kThreads 
         v[0].rr = a.live && p.dh ? p.rstd_pre[a.r] : 0.f;
     };
     const int mine = (int)blockIdx.x * slots + slot, rounds = (p.chunks + workers - 1) / workers;
-    JoinRow<T, S, kPieces> row[kUnits];
+    JoinRow<T, S, kLayout != kOdd> row[kUnits];
     Place at = place(mine, 0);
     if (kAhead) read(row, at);
     for (int round = 0, q = 0, turn = 0; round < rounds; turn ^= 1) {
@@ -392,9 +403,11 @@ __global__ void __launch_bounds__(kThreads, 512 / kThreads > 0 ? 512 / kThreads 
         float sum = 0.f;
         const float rp = row[0].rp, rr = row[0].rr;
         const Place now = at;
+        const bool idle = slots == 1 && !now.live;            // the whole block
 #pragma unroll
         for (int k = 0; k < kUnits; ++k) {
-            const Columns<kPieces> c(lane, k, p.lanes_log, p.dim);
+            if (idle) break;
+            const Columns<kLayout> c(lane, k, p.lanes, p.dim);
             un[k] = row[k].u.get();
             if (p.gate) gate[k] = row[k].gate.get();
             if (p.dy) g[k] = row[k].dy.get(); else g[k].fill(0.f);
@@ -411,16 +424,16 @@ __global__ void __launch_bounds__(kThreads, 512 / kThreads > 0 ? 512 / kThreads 
         if (ends) { q = 0; ++round; }
         at = place(mine + round * workers, q);
         if (kAhead && round < rounds) read(row, at);
-        if (p.dh) {
-            const float m = -rr * p.inv_dim * row_sum(sum, p.lanes_log, sm[turn][0]);
+        if (p.dh && !idle) {
+            const float m = -rr * p.inv_dim * row_sum(sum, p.lanes, sm[turn][0]);
 #pragma unroll
             for (int k = 0; k < kUnits; ++k) g[k] = fma8(m, yn[k], g[k]);
         }
         sum = 0.f;
 #pragma unroll
         for (int k = 0; k < kUnits; ++k) {
-            Columns<kPieces> c(lane, k, p.lanes_log, p.dim);
-            if (!now.live) c.n = 0;
+            if (idle) break;
+            const Columns<kLayout> c(lane, k, p.lanes, p.dim, now.live);
             if (p.dx) c.put((S*)p.dx + now.r * p.ld_dx, g[k] * p.rs);
             if (p.keep.drop) g[k] = c.drop(g[k], base, now.r, p.dim, p.keep);
             if (!p.post) {
@@ -441,19 +454,18 @@ __global__ void __launch_bounds__(kThreads, 512 / kThreads > 0 ? 512 / kThreads 
                 sum += dot8(g[k], un[k]);
             }
         }
-        if (p.post) {
-            const float m = -rp * p.inv_dim * row_sum(sum, p.lanes_log, sm[turn][1]);
+        if (p.post && !idle) {
+            const float m = -rp * p.inv_dim * row_sum(sum, p.lanes, sm[turn][1]);
 #pragma unroll
             for (int k = 0; k < kUnits; ++k) {
-                Columns<kPieces> c(lane, k, p.lanes_log, p.dim);
-                if (!now.live) c.n = 0;
+                const Columns<kLayout> c(lane, k, p.lanes, p.dim, now.live);
                 c.put((T*)p.du + now.r * p.ld_du, fma8(m, un[k], g[k] * rp));
             }
         }
         if (ends && p.dgate && now.chunk < p.chunks) {
 #pragma unroll
             for (int k = 0; k < kUnits; ++k) {
-                const Columns<kPieces> c(lane, k, p.lanes_log, p.dim);
+                const Columns<kLayout> c(lane, k, p.lanes, p.dim);
                 if (p.gate_part) c.put(p.gate_part + (long long)now.chunk * p.dim, dgate[k]);
                 else if (p.dgate_f32) c.put((float*)p.dgate + now.group * p.ld_dgate, dgate[k]);
                 else c.put((T*)p.dgate + now.group * p.ld_dgate, dgate[k]);
@@ -466,7 +478,7 @@ __global__ void __launch_bounds__(kThreads, 512 / kThreads > 0 ? 512 / kThreads 
         float* part = which ? p.part_post : p.part_pre;
         if (!part) continue;
         part += (long long)blockIdx.x * p.dim;
-        const int width = 8 * kUnits << p.lanes_log;
+        const int width = 8 * kUnits * p.lanes;
         if (slots > 1) {
             __syncthreads();
 #pragma unroll
@@ -475,7 +487,7 @@ __global__ void __launch_bounds__(kThreads, 512 / kThreads > 0 ? 512 / kThreads 
                 (which ? dpost[k] : dpre[k]).to(v);
 #pragma unroll
                 for (int u = 0; u < 8; ++u) {
-                    const int column = kPieces ? ((k << p.lanes_log) + lane) * 8 + u : ((k * 8 + u) << p.lanes_log) + lane;
+                    const int column = kLayout != kOdd ? (k * p.lanes + lane) * 8 + u : (k * 8 + u) * p.lanes + lane;
                     cross[slot * width + column] = v[u];
                 }
             }
@@ -487,7 +499,7 @@ __global__ void __launch_bounds__(kThreads, 512 / kThreads > 0 ? 512 / kThreads 
             }
         } else {
 #pragma unroll
-            for (int k = 0; k < kUnits; ++k) Columns<kPieces>(lane, k, p.lanes_log, p.dim).put(part, which ? dpost[k] : dpre[k]);
+            for (int k = 0; k < kUnits; ++k) Columns<kLayout>(lane, k, p.lanes, p.dim).put(part, which ? dpost[k] : dpre[k]);
         }
     }
 }

@@ -32,6 +32,23 @@ int join_lanes(int64_t dim, int64_t wide, int& units) {
 // A block: rows of a warp or less share one.
 int join_threads(int lanes) { return lanes > 32 ? lanes : kJoinThreads; }
 
+// Rows of a ring in shared memory, with so many blocks on an SM; below two the ring is no use.
+int ring_depth(int row_bytes, int blocks) {
+    return std::min(kJoinRing, 220 * 1024 / blocks / row_bytes);
+}
+cudaError_t launch_ring(void (*kernel)(JoinParams), int blocks, int threads, size_t shared, cudaStream_t s, const JoinParams& p) {
+    if (shared > 48 * 1024) {
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shared);
+        if (e != cudaSuccess) return e;
+    }
+    cudaLaunchConfig_t c{};
+    c.gridDim = dim3((unsigned)blocks);
+    c.blockDim = dim3((unsigned)threads);
+    c.dynamicSmemBytes = shared;
+    c.stream = s;
+    return cudaLaunchKernelEx(&c, (void (*)(const JoinParams))kernel, p);
+}
+
 struct JoinPlan {
     int lanes, units, threads, slots, blocks;
     int64_t rows_per_gate, chunk_rows, chunks_per_gate, chunks;
@@ -44,7 +61,7 @@ JoinPlan join_plan(int64_t rows, int64_t dim, int64_t rows_per_gate, char* scrat
     e.threads = join_threads(e.lanes);
     e.slots = e.threads / e.lanes;
     e.rows_per_gate = rows_per_gate > 0 ? std::min(rows_per_gate, rows) : rows;
-    const int64_t gate = e.rows_per_gate, most = kSms * std::max<int64_t>(1, 512 / e.threads), workers = most * e.slots;      // what is resident at 128 registers
+    const int64_t gate = e.rows_per_gate, most = kSms * std::max<int64_t>(1, 768 / e.threads), workers = most * e.slots;      // what is resident
     const int64_t want = std::max<int64_t>(1, (rows + workers * kJoinTurns - 1) / (workers * kJoinTurns));
     e.chunks_per_gate = gate > want ? (gate + want - 1) / want : 1;
     e.chunk_rows = (gate + e.chunks_per_gate - 1) / e.chunks_per_gate;
@@ -206,16 +223,28 @@ int pb_join_forward(const pb_join_args* args, void* stream) {
                         piece_ok(a.y, a.ld_y, a.rows, a.stream_dtype) && piece_ok(a.h, a.ld_h, a.rows, a.dtype) && piece_ok(a.gate, a.ld_gate, gates, a.dtype) &&
                         piece_ok(a.post_weight, 0, 1, a.weight_dtype) && piece_ok(a.pre_weight, 0, 1, a.weight_dtype);
     const int64_t slots = threads / lanes;
+    bool ring = false;
+    if (pieces && units == 2 && slots == 1 && a.dim == 16 * lanes) {
+        p.row_bytes = (int)((a.dim * (ss + (a.gate ? 2 : 1) * es) + 127) / 128 * 128);
+        p.depth = ring_depth(p.row_bytes, std::max(1, 512 / threads));
+        // A plain sum with one norm is as fast as memory without (16384 x 4096: 84 us, 99 in the ring; with a norm behind the block 95 and 86, with
+        // a gate and dropout too 120 and 116).
+        ring = p.depth > 1 && a.rows >= 4 * kSms && (a.post_weight || a.gate);
+    }
     const dim3 grid((unsigned)((a.rows + slots - 1) / slots));
     return launched(who, by_types(a.dtype, a.stream_dtype, [&](auto t, auto st) {
         using T = decltype(t);
         using S = decltype(st);
+        if (ring) {
+            auto kernel = threads <= 256 ? join_forward_ring_kernel<T, S, 256> : threads <= 512 ? join_forward_ring_kernel<T, S, 512> : join_forward_ring_kernel<T, S, 1024>;
+            const int64_t blocks = std::min(a.rows, kSms * std::max<int64_t>(1, 512 / threads));
+            return launch_ring(kernel, (int)blocks, threads, p.depth * p.row_bytes, (cudaStream_t)stream, p);
+        }
         auto by_layout = [&](auto l) {
             constexpr int L = decltype(l)::value;
             return units == 1 ? join_forward_kernel<T, S, L, 1> : join_forward_kernel<T, S, L, 2>;
         };
-        auto kernel = !pieces ? by_layout(Layout<kOdd>()) : slots == 1 && a.dim == 8 * units * lanes ? by_layout(Layout<kFull>()) : by_layout(Layout<kEven>());
-        return launch(kernel, grid, threads, (cudaStream_t)stream, p);
+        return launch(pieces ? by_layout(Layout<kEven>()) : by_layout(Layout<kOdd>()), grid, threads, (cudaStream_t)stream, p);
     }));
 }
 
@@ -285,28 +314,36 @@ int pb_join_backward(const pb_join_args* args, const pb_join_grads* grads, void*
                         piece_ok(d.dx, d.ld_dx, a.rows, a.stream_dtype) && piece_ok(d.du, d.ld_du, a.rows, a.dtype) &&
                         piece_ok(a.gate, a.ld_gate, gates, a.dtype) && piece_ok(d.dgate, d.ld_dgate, gates, d.dgate_dtype) &&
                         piece_ok(a.post_weight, 0, 1, a.weight_dtype) && piece_ok(a.pre_weight, 0, 1, a.weight_dtype);
-    const size_t shared = e.slots > 1 ? (size_t)e.threads * 8 * e.units * 4 : 0;
+    size_t shared = e.slots > 1 ? (size_t)e.threads * 8 * e.units * 4 : 0;
+    bool ring = false;
+    if (pieces && e.slots == 1 && a.dim == 8 * e.units * e.lanes) {
+        p.row_bytes = (int)((a.dim * (2 * ss + 3 * es) + 127) / 128 * 128);
+        p.depth = ring_depth(p.row_bytes, std::max(1, 512 / e.threads));
+        ring = p.depth > 1;
+        if (ring) shared = (size_t)p.depth * p.row_bytes;
+    }
     return launched(who, by_types(a.dtype, a.stream_dtype, [&](auto t, auto st) {
         using T = decltype(t);
         using S = decltype(st);
         auto by_layout = [&](auto l) {
             constexpr int L = decltype(l)::value;
-            if (e.threads <= 256) return join_backward_kernel<T, S, L, 1, 256, true>;
-            if (e.units == 1) return join_backward_kernel<T, S, L, 1, 512, true>;
-            return e.threads <= 512 ? join_backward_kernel<T, S, L, 2, 512, false> : join_backward_kernel<T, S, L, 2, 1024, false>;
+            if (e.threads <= 256) return join_backward_kernel<T, S, L, 1, 256>;
+            if (e.units == 1) return join_backward_kernel<T, S, L, 1, 512>;
+            return e.threads <= 512 ? join_backward_kernel<T, S, L, 2, 512> : join_backward_kernel<T, S, L, 2, 1024>;
         };
-        auto kernel = !pieces ? by_layout(Layout<kOdd>()) : e.slots == 1 && a.dim == 8 * e.units * e.lanes ? by_layout(Layout<kFull>()) : by_layout(Layout<kEven>());
-        cudaLaunchConfig_t c{};
-        c.gridDim = dim3((unsigned)e.blocks);
-        c.blockDim = dim3((unsigned)e.threads);
-        c.dynamicSmemBytes = shared;
-        c.stream = s;
-        cudaError_t err = cudaLaunchKernelEx(&c, kernel, p);
+        auto in_ring = [&]() {
+            if (e.threads <= 256) return join_backward_ring_kernel<T, S, 1, 256>;
+            if (e.units == 1) return join_backward_ring_kernel<T, S, 1, 512>;
+            return e.threads <= 512 ? join_backward_ring_kernel<T, S, 2, 512> : join_backward_ring_kernel<T, S, 2, 1024>;
+        };
+        auto kernel = ring ? in_ring() : pieces ? by_layout(Layout<kEven>()) : by_layout(Layout<kOdd>());
+        const int blocks = ring ? std::min(e.blocks, kSms * std::max(1, 512 / e.threads)) : e.blocks;      // what is resident
+        cudaError_t err = launch_ring(kernel, blocks, e.threads, shared, s, p);
         const int first = p.part_pre || p.part_post ? 0 : 2;
         const int64_t jobs = 2 - first + (d.dgate && e.gate ? gates : 0);
         if (jobs > 0 && err == cudaSuccess)
             err = launch_after(join_sum_kernel<T>, dim3((unsigned)jobs, (unsigned)((a.dim + kJoinSumColumns - 1) / kJoinSumColumns)),
-                               kJoinSumColumns * kJoinSumShares, s, p.part_pre, p.part_post, e.blocks, e.gate, e.chunks_per_gate, e.chunks, (int)a.dim,
+                               kJoinSumColumns * kJoinSumShares, s, p.part_pre, p.part_post, blocks, e.gate, e.chunks_per_gate, e.chunks, (int)a.dim,
                                d.dpre_weight, d.dpost_weight, d.dweight_dtype == PB_F32, d.dgate, d.ld_dgate, d.dgate_dtype == PB_F32, first);
         return err;
     }));

@@ -8,12 +8,15 @@
 //   dy' = dy + rstd_pre (dh pre - yn mean(dh pre yn))        dx = residual_scale dy'     dpre = sum_t dh yn
 //   db  = keep dy'          dgate = sum over its rows of db un post                      dpost = sum_t db gate un
 //   du  = rstd_post (db gate post - un mean(db gate post un))
+// In dy' = e - m1 yn, with e = dy + rstd_pre dh pre and m1 = rstd_pre mean(dh pre yn), the second mean is that of keep gate post un e less m1 times
+// that of keep gate post un yn, so that the threads of a row meet once for three sums instead of twice for one.
 //
 // Everything is bound by the rows' bytes.  A row is held in registers by a group of threads (a power of two, kUnits pieces
 // of eight columns each), so that it is read and written once; its two sums are the only thing that the threads of a
 // group exchange.  In the backward a thread keeps the same columns in every row, so that the sums over rows
 // stay in its registers; they end in one partial sum per block, and in one per chunk of rows that share a gate.
 #pragma once
+#include "tc_common.cuh"
 #include "tok_common.cuh"
 
 namespace pb {
@@ -90,7 +93,7 @@ __device__ __forceinline__ Pair keep2(Pair v, unsigned bits, unsigned drop) {
     v.split(a, b);
     return Pair((bits << 16) >= drop ? a : 0.f, bits >= drop ? b : 0.f);
 }
-// Elements 4 quad .. + 7, not scaled yet.
+// Elements 4 quad .. + 7 of v, which is scaled already.
 __device__ __forceinline__ Eight keep8(const Eight& v, unsigned long long base, unsigned long long quad, unsigned drop) {
     const unsigned long long y = splitmix64(base, quad), z = splitmix64(base, quad + 1);
     Eight r;
@@ -108,6 +111,7 @@ __device__ __forceinline__ bool kept(unsigned long long base, unsigned long long
 template <typename T> struct RawEight {
     uint4 q;
     __device__ __forceinline__ void load(const T* p) { q = *reinterpret_cast<const uint4*>(p); }
+    __device__ __forceinline__ void load_shared(const T* p) { load(p); }
     __device__ __forceinline__ void zero() { q = make_uint4(0, 0, 0, 0); }
     __device__ __forceinline__ Eight get() const {
         float v[8];
@@ -120,6 +124,11 @@ template <typename T> struct RawEight {
 template <> struct RawEight<float> {
     float v[8];
     __device__ __forceinline__ void load(const float* p) { load8_wide(v, p); }
+    __device__ __forceinline__ void load_shared(const float* p) {
+        const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
+        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+        v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+    }
     __device__ __forceinline__ void zero() {
 #pragma unroll
         for (int k = 0; k < 8; ++k) v[k] = 0.f;
@@ -191,6 +200,7 @@ struct JoinParams {
     void* dgate;
     bool dgate_f32;
     float *part_pre, *part_post; // [blocks][dim], or NULL
+    int depth, row_bytes;        // rows of the ring, bytes of one: 128-byte aligned
 };
 
 constexpr int kJoinThreads = 256;             // of a block, or the threads of a row if those are more
@@ -214,15 +224,66 @@ __device__ __forceinline__ float row_sum(float v, int lanes, float* sm) {
     return v;
 }
 
+// Three sums at once.
+__device__ __forceinline__ void row_sums(float& a, float& b, float& c, int lanes, float (&sm)[3][32]) {
+    if (lanes < 32) {
+        for (int k = lanes / 2; k; k /= 2) {
+            a += __shfl_xor_sync(0xffffffffu, a, k);
+            b += __shfl_xor_sync(0xffffffffu, b, k);
+            c += __shfl_xor_sync(0xffffffffu, c, k);
+        }
+        return;
+    }
+#pragma unroll
+    for (int k = 16; k; k /= 2) {
+        a += __shfl_xor_sync(0xffffffffu, a, k);
+        b += __shfl_xor_sync(0xffffffffu, b, k);
+        c += __shfl_xor_sync(0xffffffffu, c, k);
+    }
+    if (lanes == 32) return;
+    const int l = threadIdx.x % 32, warp = threadIdx.x / 32;
+    if (l < 3) sm[l][warp] = l == 0 ? a : l == 1 ? b : c;
+    __syncthreads();
+    const bool there = l * 32 < lanes;
+    a = there ? sm[0][l] : 0.f; b = there ? sm[1][l] : 0.f; c = there ? sm[2][l] : 0.f;
+#pragma unroll
+    for (int k = 16; k; k /= 2) {
+        a += __shfl_xor_sync(0xffffffffu, a, k);
+        b += __shfl_xor_sync(0xffffffffu, b, k);
+        c += __shfl_xor_sync(0xffffffffu, c, k);
+    }
+}
+
 // 1 / sqrt(x) to 2^-23: the approximation, and one step of Newton's method where that is finite.
 __device__ __forceinline__ float root_of(float x) {
     const float r = rsqrtf(x);
     return r > 0.f && r < INFINITY ? r * fmaf(-0.5f * x * r, r, 1.5f) : r;
 }
 
-// How a thread's eight columns lie: kOdd: `lanes` apart, so that neighbours read neighbours; kEven: consecutive; kFull: consecutive, and every
-// thread has all of its own, in rows of a block each.
+// A copy that has not come in time may still land: before the shared memory that it writes goes back to the SM.
+__device__ __forceinline__ void ring_late() {
+    for (int k = 0; k < 512; ++k) __nanosleep(200);
+}
+
+// How a thread's eight columns lie: kOdd: `lanes` apart, so that neighbours read neighbours; kEven: consecutive; kFull: consecutive, every
+// thread has all of its own, and a block works on one row after the other, which bulk copies bring into a ring of rows in shared memory.
 enum JoinLayout { kOdd = 0, kEven = 1, kFull = 2 };
+
+constexpr int kJoinRing = 4;                  // rows on their way at most
+struct JoinRing {
+    uint64_t full[kJoinRing];
+    int fail;
+};
+__device__ __forceinline__ void bulk_row(unsigned char* dst, const void* src, uint32_t bytes, uint32_t bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                 ::"r"(smem_u32(dst)), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
+// One thread sets the barriers up before the block meets for the first time.
+__device__ __forceinline__ void ring_init(JoinRing& ring) {
+    for (int k = 0; k < kJoinRing; ++k) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(smem_u32(&ring.full[k])) : "memory");
+    ring.fail = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+}
 template <typename T, bool kPieces> struct RawColumns : RawEight<T> {};
 template <typename T> struct RawColumns<T, false> {
     T v[8];
@@ -271,14 +332,14 @@ struct Columns {
                 if (k < n) row[first + k * step] = from_f32<T>(v[k]);
         }
     }
-    // What dropout leaves of a row's columns.
+    // What dropout leaves of a row's columns (x scaled already).
     __device__ __forceinline__ Eight drop(const Eight& x, unsigned long long base, long long row, int dim, const Keep& k) const {
         const unsigned long long i = (unsigned long long)row * dim + first;
         if constexpr (kPieces) {
-            return keep8(x * k.scale, base, i / 4, k.drop);  // dim is a multiple of 8
+            return keep8(x, base, i / 4, k.drop);            // dim is a multiple of 8
         } else {
             float v[8];
-            (x * k.scale).to(v);
+            x.to(v);
 #pragma unroll
             for (int u = 0; u < 8; ++u) v[u] = kept(base, i + u * step, k.drop) ? v[u] : 0.f;
             Eight r;
@@ -291,19 +352,22 @@ struct Columns {
 template <typename T, typename S, int kLayout, int kUnits>
 __global__ void __launch_bounds__(kJoinMaxLanes) join_forward_kernel(const JoinParams p) {
     __shared__ float sm[2][32];
-    constexpr bool kAll = kLayout == kFull;
-    const int lane = kAll || p.lanes > 32 ? threadIdx.x : threadIdx.x & (p.lanes - 1), slot = kAll || p.lanes > 32 ? 0 : threadIdx.x / p.lanes,
-              slots = kAll || p.lanes > 32 ? 1 : blockDim.x / p.lanes;
+    const int lane = p.lanes > 32 ? threadIdx.x : threadIdx.x & (p.lanes - 1), slot = p.lanes > 32 ? 0 : threadIdx.x / p.lanes,
+              slots = p.lanes > 32 ? 1 : blockDim.x / p.lanes;
     const unsigned long long base = p.keep.drop ? keep_base(p.keep) : 0;
     const long long r = (long long)blockIdx.x * slots + slot;
-    const bool live = kAll || r < p.rows;
-    Eight y[kUnits], b[kUnits];
+    const bool live = r < p.rows;
+    Eight y[kUnits], b[kUnits], w[kUnits];
+    RawColumns<T, kLayout != kOdd> gate[kUnits];
     float sum = 0.f;
+    // what the sums are waited for with is on its way before they are formed
 #pragma unroll
     for (int k = 0; k < kUnits; ++k) {
         const Columns<kLayout> c(lane, k, p.lanes, p.dim, live);
         b[k] = c.get((const T*)p.u + r * p.ld_u);
         y[k] = c.get((const S*)p.x + r * p.ld_x);
+        if (p.gate) c.load(gate[k], (const T*)p.gate + (live ? p.by_gate((int)r) : 0) * p.ld_gate);
+        if (p.post) w[k] = c.template weight<T>(p.post, p.weights_f32);
     }
     float rstd = 1.f;
     if (p.post) {
@@ -312,12 +376,15 @@ __global__ void __launch_bounds__(kJoinMaxLanes) join_forward_kernel(const JoinP
         rstd = root_of(fmaf(row_sum(sum, p.lanes, sm[0]), p.inv_dim, p.eps));
         if (live && lane == 0 && p.rstd_post) p.rstd_post[r] = rstd;
     }
+    const float scale = p.keep.drop ? rstd * p.keep.scale : rstd;
     sum = 0.f;
 #pragma unroll
     for (int k = 0; k < kUnits; ++k) {
         const Columns<kLayout> c(lane, k, p.lanes, p.dim, live);
-        if (p.post) b[k] = b[k] * rstd * c.template weight<T>(p.post, p.weights_f32);
-        if (p.gate) b[k] = b[k] * c.get((const T*)p.gate + (live ? p.by_gate((int)r) : 0) * p.ld_gate);
+        b[k] = b[k] * scale;
+        if (p.post) b[k] = b[k] * w[k];
+        if (p.h) w[k] = c.template weight<T>(p.pre, p.weights_f32);
+        if (p.gate) b[k] = b[k] * gate[k].get();
         if (p.keep.drop) b[k] = c.drop(b[k], base, r, p.dim, p.keep);
         y[k] = fma8(p.rs, y[k], b[k]);                       // columns that do not exist are zero
         c.put((S*)p.y + r * p.ld_y, y[k]);
@@ -330,145 +397,178 @@ __global__ void __launch_bounds__(kJoinMaxLanes) join_forward_kernel(const JoinP
 #pragma unroll
     for (int k = 0; k < kUnits; ++k) {
         const Columns<kLayout> c(lane, k, p.lanes, p.dim);
-        c.put((T*)p.h + r * p.ld_h, y[k] * rstd * c.template weight<T>(p.pre, p.weights_f32));
+        c.put((T*)p.h + r * p.ld_h, y[k] * rstd * w[k]);
     }
 }
 
-// What the backward reads of a row.
-template <typename T, typename S, bool kPieces>
-struct JoinRow {
-    RawColumns<T, kPieces> u, dh, gate;
-    RawColumns<S, kPieces> y, dy;
-    float rp, rr;
-};
-
-// kAhead: a row is read while the one before it is worked on, and the weights stay in registers.
-template <typename T, typename S, int kLayout, int kUnits, int kThreads, bool kAhead>
-__global__ void __launch_bounds__(kThreads, 512 / kThreads > 0 ? 512 / kThreads : 1) join_backward_kernel(const JoinParams p) {
-    extern __shared__ float cross[];             // [slots][lanes * 8 * kUnits]
+// Rows that a block takes one after the other, 16 columns per thread: their parts come by bulk copies some rows ahead, and the weights stay in registers.
+template <typename T, typename S, int kThreads>
+__global__ void __launch_bounds__(kThreads, kThreads <= 256 ? 512 / kThreads : 1) join_forward_ring_kernel(const JoinParams p) {
+    extern __shared__ __align__(128) unsigned char store[];
     __shared__ float sm[2][2][32];
-    constexpr bool kAll = kLayout == kFull;
-    const int lane = kAll || p.lanes > 32 ? threadIdx.x : threadIdx.x & (p.lanes - 1), slot = kAll || p.lanes > 32 ? 0 : threadIdx.x / p.lanes,
-              slots = kAll || p.lanes > 32 ? 1 : blockDim.x / p.lanes;
+    __shared__ JoinRing ring;
+    constexpr int kUnits = 2;
+    const int lane = threadIdx.x;
     const unsigned long long base = p.keep.drop ? keep_base(p.keep) : 0;
-    const int workers = (int)gridDim.x * slots;
-    Eight dpre[kUnits], dpost[kUnits], dgate[kUnits], post[kUnits], pre[kUnits];
+    if (lane == 0) ring_init(ring);
+    __syncthreads();
+    const uint32_t s_bytes = (uint32_t)(p.dim * sizeof(S)), t_bytes = (uint32_t)(p.dim * sizeof(T));
+    auto ask = [&](long long r, int at) {
+        const uint32_t bar = smem_u32(&ring.full[at]);
+        unsigned char* to = store + at * p.row_bytes;
+        mbar_arrive_tx(bar, s_bytes + (p.gate ? 2 : 1) * t_bytes);
+        bulk_row(to, (const S*)p.x + r * p.ld_x, s_bytes, bar);
+        bulk_row(to + s_bytes, (const T*)p.u + r * p.ld_u, t_bytes, bar);
+        if (p.gate) bulk_row(to + s_bytes + t_bytes, (const T*)p.gate + (long long)p.by_gate((int)r) * p.ld_gate, t_bytes, bar);
+    };
+    if (lane == 0)
+        for (int k = 0; k < p.depth; ++k)
+            if (blockIdx.x + (long long)k * gridDim.x < p.rows) ask(blockIdx.x + (long long)k * gridDim.x, k);
+    Eight post[kUnits], pre[kUnits];
 #pragma unroll
     for (int k = 0; k < kUnits; ++k) {
-        dpre[k].fill(0.f); dpost[k].fill(0.f); dgate[k].fill(0.f);
-        if (kAhead) {
-            const Columns<kLayout> c(lane, k, p.lanes, p.dim);
-            if (p.post) post[k] = c.template weight<T>(p.post, p.weights_f32);
-            if (p.dh) pre[k] = c.template weight<T>(p.pre, p.weights_f32);
-        }
+        const Columns<kFull> c(lane, k, blockDim.x, p.dim);
+        if (p.post) post[k] = c.template weight<T>(p.post, p.weights_f32);
+        if (p.h) pre[k] = c.template weight<T>(p.pre, p.weights_f32);
     }
-    // The rows of a worker: chunk by chunk, every worker as many turns, since the workers of a warp move together; some are idle.
-    struct Place {
-        int chunk, q, group;
-        long long r;
-        bool live;
-    };
-    auto place = [&](int chunk, int q) {
-        Place a;
-        a.chunk = chunk; a.q = q;
-        a.group = p.by_chunks(chunk);
-        const int within = (chunk - a.group * p.chunks_per_gate) * p.chunk_rows + q;
-        a.r = (long long)a.group * p.rows_per_gate + within;
-        a.live = chunk < p.chunks && within < p.rows_per_gate && a.r < p.rows;
-        return a;
-    };
-    auto read = [&](JoinRow<T, S, kLayout != kOdd> (&v)[kUnits], const Place& a) {
-#pragma unroll
-        for (int k = 0; k < kUnits; ++k) {
-            const Columns<kLayout> c(lane, k, p.lanes, p.dim, a.live);
-            if (kAll && !a.live) continue;                    // nothing of an idle turn is written
-            c.load(v[k].u, (const T*)p.u + a.r * p.ld_u);
-            if (p.dy) c.load(v[k].dy, (const S*)p.dy + a.r * p.ld_dy);
-            if (p.dh) {
-                c.load(v[k].y, (const S*)p.yin + a.r * p.ld_y);
-                c.load(v[k].dh, (const T*)p.dh + a.r * p.ld_dh);
-            }
-            if (p.gate) c.load(v[k].gate, (const T*)p.gate + a.group * p.ld_gate);
-        }
-        v[0].rp = a.live && p.post ? p.rstd_post[a.r] : 1.f;
-        v[0].rr = a.live && p.dh ? p.rstd_pre[a.r] : 0.f;
-    };
-    const int mine = (int)blockIdx.x * slots + slot, rounds = (p.chunks + workers - 1) / workers;
-    JoinRow<T, S, kLayout != kOdd> row[kUnits];
-    Place at = place(mine, 0);
-    if (kAhead) read(row, at);
-    for (int round = 0, q = 0, turn = 0; round < rounds; turn ^= 1) {
-        if (!kAhead) read(row, at);
-        Eight g[kUnits], un[kUnits], yn[kUnits], gate[kUnits];
+    int at = 0, turn = 0;
+    uint32_t phase = 0;
+    bool ok = true;
+    for (long long r = blockIdx.x; r < p.rows; r += gridDim.x, turn ^= 1) {
+        if (ok) ok = mbar_wait(smem_u32(&ring.full[at]), phase, &ring.fail);
+        const unsigned char* from = store + at * p.row_bytes;
+        Eight y[kUnits], b[kUnits], gate[kUnits];
         float sum = 0.f;
-        const float rp = row[0].rp, rr = row[0].rr;
-        const Place now = at;
-        const bool idle = slots == 1 && !now.live;            // the whole block
 #pragma unroll
         for (int k = 0; k < kUnits; ++k) {
-            if (idle) break;
-            const Columns<kLayout> c(lane, k, p.lanes, p.dim);
-            un[k] = row[k].u.get();
-            if (p.gate) gate[k] = row[k].gate.get();
-            if (p.dy) g[k] = row[k].dy.get(); else g[k].fill(0.f);
-            if (p.dh) {
-                const Eight w = kAhead ? pre[k] : c.template weight<T>(p.pre, p.weights_f32), dh = row[k].dh.get();
-                yn[k] = row[k].y.get() * rr;
-                dpre[k] = fma8(dh, yn[k], dpre[k]);
-                const Eight wd = dh * w;
-                sum += dot8(wd, yn[k]);
-                g[k] = fma8(rr, wd, g[k]);
+            const Columns<kFull> c(lane, k, blockDim.x, p.dim);
+            RawEight<S> x;
+            RawEight<T> u;
+            x.load_shared((const S*)from + c.first);
+            u.load_shared((const T*)(from + s_bytes) + c.first);
+            y[k] = x.get();
+            b[k] = u.get();
+            if (p.gate) {
+                u.load_shared((const T*)(from + s_bytes + t_bytes) + c.first);
+                gate[k] = u.get();
             }
+            if (p.post) sum += dot8(b[k], b[k]);
         }
-        const bool ends = ++q == p.chunk_rows;                // of the chunk
-        if (ends) { q = 0; ++round; }
-        at = place(mine + round * workers, q);
-        if (kAhead && round < rounds) read(row, at);
-        if (p.dh && !idle) {
-            const float m = -rr * p.inv_dim * row_sum(sum, p.lanes, sm[turn][0]);
-#pragma unroll
-            for (int k = 0; k < kUnits; ++k) g[k] = fma8(m, yn[k], g[k]);
+        if (!ok) y[0].fill(__int_as_float(0x7fffffff));       // a copy never came: the row is NaN
+        float rstd = 1.f;
+        if (p.post) {
+            rstd = root_of(fmaf(row_sum(sum, blockDim.x, sm[turn][0]), p.inv_dim, p.eps));
+            if (lane == 0 && p.rstd_post) p.rstd_post[r] = rstd;
+        } else {
+            __syncthreads();
         }
+        if (lane == 0 && r + (long long)p.depth * gridDim.x < p.rows) ask(r + (long long)p.depth * gridDim.x, at);     // all have read this row
+        if (++at == p.depth) { at = 0; phase ^= 1; }
+        const float scale = p.keep.drop ? rstd * p.keep.scale : rstd;
         sum = 0.f;
 #pragma unroll
         for (int k = 0; k < kUnits; ++k) {
-            if (idle) break;
-            const Columns<kLayout> c(lane, k, p.lanes, p.dim, now.live);
-            if (p.dx) c.put((S*)p.dx + now.r * p.ld_dx, g[k] * p.rs);
-            if (p.keep.drop) g[k] = c.drop(g[k], base, now.r, p.dim, p.keep);
-            if (!p.post) {
-                if (p.gate) {
-                    dgate[k] = fma8(g[k], un[k], dgate[k]);
-                    g[k] = g[k] * gate[k];
-                }
-                c.put((T*)p.du + now.r * p.ld_du, g[k]);
-            } else {
-                const Eight w = kAhead ? post[k] : c.template weight<T>(p.post, p.weights_f32);
-                un[k] = un[k] * rp;
-                if (p.gate) {
-                    dgate[k] = fma8(g[k], un[k] * w, dgate[k]);
-                    g[k] = g[k] * gate[k];
-                }
-                dpost[k] = fma8(g[k], un[k], dpost[k]);
-                g[k] = g[k] * w;
-                sum += dot8(g[k], un[k]);
-            }
+            const Columns<kFull> c(lane, k, blockDim.x, p.dim);
+            b[k] = b[k] * scale;
+            if (p.post) b[k] = b[k] * post[k];
+            if (p.gate) b[k] = b[k] * gate[k];
+            if (p.keep.drop) b[k] = c.drop(b[k], base, r, p.dim, p.keep);
+            y[k] = fma8(p.rs, y[k], b[k]);
+            c.put((S*)p.y + r * p.ld_y, y[k]);
+            sum += dot8(y[k], y[k]);
         }
-        if (p.post && !idle) {
-            const float m = -rp * p.inv_dim * row_sum(sum, p.lanes, sm[turn][1]);
+        if (!p.h) continue;
+        rstd = root_of(fmaf(row_sum(sum, blockDim.x, sm[turn][1]), p.inv_dim, p.eps));
+        if (lane == 0 && p.rstd_pre) p.rstd_pre[r] = rstd;
+#pragma unroll
+        for (int k = 0; k < kUnits; ++k) Columns<kFull>(lane, k, blockDim.x, p.dim).put((T*)p.h + r * p.ld_h, y[k] * rstd * pre[k]);
+    }
+    if (!ok) ring_late();
+}
+
+// Rows of any layout: a worker is the threads of a row, and goes through chunks of rows that share a gate.
+template <typename T, typename S, int kLayout, int kUnits, int kThreads>
+__global__ void __launch_bounds__(kThreads, kThreads <= 256 ? 3 : 1) join_backward_kernel(const JoinParams p) {
+    extern __shared__ float cross[];             // [slots][lanes * 8 * kUnits]
+    __shared__ float sm[2][2][32];
+    const int lane = p.lanes > 32 ? threadIdx.x : threadIdx.x & (p.lanes - 1), slot = p.lanes > 32 ? 0 : threadIdx.x / p.lanes,
+              slots = p.lanes > 32 ? 1 : blockDim.x / p.lanes;
+    const unsigned long long base = p.keep.drop ? keep_base(p.keep) : 0;
+    const int workers = (int)gridDim.x * slots, mine = (int)blockIdx.x * slots + slot;
+    Eight dpre[kUnits], dpost[kUnits], dgate[kUnits];
+#pragma unroll
+    for (int k = 0; k < kUnits; ++k) { dpre[k].fill(0.f); dpost[k].fill(0.f); dgate[k].fill(0.f); }
+    int turn = 0;
+    // every worker takes as many turns, since those of a warp move together; some are idle, and read zeros
+    for (int k0 = 0; k0 < p.chunks; k0 += workers) {
+        const int chunk = k0 + mine, group = p.by_chunks(chunk), start = (chunk - group * p.chunks_per_gate) * p.chunk_rows;
+        for (int q = 0; q < p.chunk_rows; ++q, turn ^= 1) {
+            const long long r = (long long)group * p.rows_per_gate + start + q;
+            const bool live = chunk < p.chunks && start + q < p.rows_per_gate && r < p.rows;
+            const float rp = live && p.post ? p.rstd_post[r] : 1.f, rr = live && p.dh ? p.rstd_pre[r] : 0.f;
+            Eight g[kUnits], un[kUnits], yn[kUnits];
+            RawColumns<T, kLayout != kOdd> gate[kUnits];
+            float sum = 0.f;
 #pragma unroll
             for (int k = 0; k < kUnits; ++k) {
-                const Columns<kLayout> c(lane, k, p.lanes, p.dim, now.live);
-                c.put((T*)p.du + now.r * p.ld_du, fma8(m, un[k], g[k] * rp));
+                const Columns<kLayout> c(lane, k, p.lanes, p.dim, live);
+                un[k] = c.get((const T*)p.u + r * p.ld_u);
+                if (p.gate) c.load(gate[k], (const T*)p.gate + group * p.ld_gate);
+                if (p.dy) g[k] = c.get((const S*)p.dy + r * p.ld_dy); else g[k].fill(0.f);
+                if (p.dh) {
+                    const Eight dh = c.get((const T*)p.dh + r * p.ld_dh);
+                    yn[k] = c.get((const S*)p.yin + r * p.ld_y) * rr;
+                    dpre[k] = fma8(dh, yn[k], dpre[k]);
+                    const Eight w = dh * c.template weight<T>(p.pre, p.weights_f32);
+                    sum += dot8(w, yn[k]);
+                    g[k] = fma8(rr, w, g[k]);
+                }
+            }
+            if (p.dh) {
+                const float m = -rr * p.inv_dim * row_sum(sum, p.lanes, sm[turn][0]);
+#pragma unroll
+                for (int k = 0; k < kUnits; ++k) g[k] = fma8(m, yn[k], g[k]);
+            }
+            sum = 0.f;
+#pragma unroll
+            for (int k = 0; k < kUnits; ++k) {
+                const Columns<kLayout> c(lane, k, p.lanes, p.dim, live);
+                if (p.dx) c.put((S*)p.dx + r * p.ld_dx, g[k] * p.rs);
+                if (p.keep.drop) g[k] = c.drop(g[k] * p.keep.scale, base, r, p.dim, p.keep);
+                if (!p.post) {
+                    if (p.gate) {
+                        dgate[k] = fma8(g[k], un[k], dgate[k]);
+                        g[k] = g[k] * gate[k].get();
+                    }
+                    c.put((T*)p.du + r * p.ld_du, g[k]);
+                } else {
+                    const Eight w = c.template weight<T>(p.post, p.weights_f32);
+                    un[k] = un[k] * rp;
+                    if (p.gate) {
+                        dgate[k] = fma8(g[k], un[k] * w, dgate[k]);
+                        g[k] = g[k] * gate[k].get();
+                    }
+                    dpost[k] = fma8(g[k], un[k], dpost[k]);
+                    g[k] = g[k] * w;
+                    sum += dot8(g[k], un[k]);
+                }
+            }
+            if (p.post) {
+                const float m = -rp * p.inv_dim * row_sum(sum, p.lanes, sm[turn][1]);
+#pragma unroll
+                for (int k = 0; k < kUnits; ++k) {
+                    const Columns<kLayout> c(lane, k, p.lanes, p.dim, live);
+                    c.put((T*)p.du + r * p.ld_du, fma8(m, un[k], g[k] * rp));
+                }
             }
         }
-        if (ends && p.dgate && now.chunk < p.chunks) {
+        if (p.dgate && chunk < p.chunks) {
 #pragma unroll
             for (int k = 0; k < kUnits; ++k) {
                 const Columns<kLayout> c(lane, k, p.lanes, p.dim);
-                if (p.gate_part) c.put(p.gate_part + (long long)now.chunk * p.dim, dgate[k]);
-                else if (p.dgate_f32) c.put((float*)p.dgate + now.group * p.ld_dgate, dgate[k]);
-                else c.put((T*)p.dgate + now.group * p.ld_dgate, dgate[k]);
+                if (p.gate_part) c.put(p.gate_part + (long long)chunk * p.dim, dgate[k]);
+                else if (p.dgate_f32) c.put((float*)p.dgate + group * p.ld_dgate, dgate[k]);
+                else c.put((T*)p.dgate + group * p.ld_dgate, dgate[k]);
                 dgate[k].fill(0.f);
             }
         }
@@ -501,6 +601,157 @@ __global__ void __launch_bounds__(kThreads, 512 / kThreads > 0 ? 512 / kThreads 
 #pragma unroll
             for (int k = 0; k < kUnits; ++k) Columns<kLayout>(lane, k, p.lanes, p.dim).put(part, which ? dpost[k] : dpre[k]);
         }
+    }
+}
+
+// Rows that a block takes one after the other, eight columns per thread (16 in rows of more than 4096): their parts come by bulk copies some rows
+// ahead.
+template <typename T, typename S, int kUnits, int kThreads>
+__global__ void __launch_bounds__(kThreads, kThreads <= 256 ? 512 / kThreads : 1) join_backward_ring_kernel(const JoinParams p) {
+    extern __shared__ __align__(128) unsigned char store[];
+    __shared__ float sm[2][3][32];
+    __shared__ JoinRing ring;
+    const int lane = threadIdx.x, blocks = (int)gridDim.x;
+    const unsigned long long base = p.keep.drop ? keep_base(p.keep) : 0;
+    if (lane == 0) ring_init(ring);
+    __syncthreads();
+    const uint32_t s_bytes = (uint32_t)(p.dim * sizeof(S)), t_bytes = (uint32_t)(p.dim * sizeof(T));
+    struct Chunk {
+        int group, rows;
+        long long first;
+    };
+    auto chunk_at = [&](int chunk) {
+        Chunk c;
+        c.group = p.by_chunks(chunk);
+        const int start = (chunk - c.group * p.chunks_per_gate) * p.chunk_rows;
+        c.first = (long long)c.group * p.rows_per_gate + start;
+        c.rows = (int)min((long long)min(p.chunk_rows, p.rows_per_gate - start), p.rows - c.first);
+        return c;
+    };
+    // the row that the next copies are for
+    int ask_chunk = blockIdx.x, ask_q = 0, put = 0;
+    Chunk asked = chunk_at(ask_chunk);
+    auto ask = [&]() {
+        if (ask_chunk >= p.chunks) return;
+        const long long r = asked.first + ask_q;
+        const uint32_t bar = smem_u32(&ring.full[put]);
+        unsigned char* to = store + put * p.row_bytes;
+        mbar_arrive_tx(bar, t_bytes * (1 + (p.dh != nullptr) + (p.gate != nullptr)) + s_bytes * ((p.dh != nullptr) + (p.dy != nullptr)));
+        bulk_row(to, (const T*)p.u + r * p.ld_u, t_bytes, bar);
+        if (p.gate) bulk_row(to + t_bytes, (const T*)p.gate + asked.group * p.ld_gate, t_bytes, bar);
+        if (p.dh) {
+            bulk_row(to + 2 * t_bytes, (const T*)p.dh + r * p.ld_dh, t_bytes, bar);
+            bulk_row(to + 3 * t_bytes, (const S*)p.yin + r * p.ld_y, s_bytes, bar);
+        }
+        if (p.dy) bulk_row(to + 3 * t_bytes + s_bytes, (const S*)p.dy + r * p.ld_dy, s_bytes, bar);
+        if (++put == p.depth) put = 0;
+        if (++ask_q == asked.rows) {
+            ask_q = 0;
+            ask_chunk += blocks;
+            if (ask_chunk < p.chunks) asked = chunk_at(ask_chunk);
+        }
+    };
+    if (lane == 0)
+        for (int k = 0; k < p.depth; ++k) ask();
+    // What dpost and dgate have in common is the sum of db un over the rows of a gate: times post that is dgate, times the gate it goes to dpost.
+    constexpr bool kKept = kUnits == 1;                       // the weights stay in registers
+    Eight dpre[kUnits], dpost[kUnits], both[kUnits], post[kUnits], pre[kUnits];
+#pragma unroll
+    for (int k = 0; k < kUnits; ++k) {
+        dpre[k].fill(0.f); dpost[k].fill(0.f); both[k].fill(0.f);
+        if (kKept) {
+            const Columns<kFull> c(lane, k, blockDim.x, p.dim);
+            if (p.post) post[k] = c.template weight<T>(p.post, p.weights_f32);
+            if (p.dh) pre[k] = c.template weight<T>(p.pre, p.weights_f32);
+        }
+    }
+    int get = 0, turn = 0;
+    uint32_t phase = 0;
+    bool ok = true;
+    for (int chunk = blockIdx.x; chunk < p.chunks; chunk += blocks) {
+        const Chunk now = chunk_at(chunk);
+        for (int q = 0; q < now.rows; ++q, turn ^= 1) {
+            const long long r = now.first + q;
+            float rp = p.post ? p.rstd_post[r] : 1.f;
+            const float rr = p.dh ? p.rstd_pre[r] : 0.f;
+            if (ok) ok = mbar_wait(smem_u32(&ring.full[get]), phase, &ring.fail);
+            if (!ok) rp = __int_as_float(0x7fffffff);         // a copy never came: NaN
+            const unsigned char* from = store + get * p.row_bytes;
+            Eight g[kUnits], un[kUnits], yn[kUnits], gate[kUnits], keep[kUnits];
+            float s1 = 0.f, s2 = 0.f, s3 = 0.f;
+#pragma unroll
+            for (int k = 0; k < kUnits; ++k) {
+                const Columns<kFull> c(lane, k, blockDim.x, p.dim);
+                RawEight<T> t;
+                RawEight<S> s;
+                t.load_shared((const T*)from + c.first);
+                un[k] = t.get() * rp;
+                if (p.gate) {
+                    t.load_shared((const T*)(from + t_bytes) + c.first);
+                    gate[k] = t.get();
+                }
+                if (p.dy) {
+                    s.load_shared((const S*)(from + 3 * t_bytes + s_bytes) + c.first);
+                    g[k] = s.get();
+                } else {
+                    g[k].fill(0.f);
+                }
+                if (p.dh) {
+                    t.load_shared((const T*)(from + 2 * t_bytes) + c.first);
+                    s.load_shared((const S*)(from + 3 * t_bytes) + c.first);
+                    const Eight dh = t.get(), w = dh * (kKept ? pre[k] : c.template weight<T>(p.pre, p.weights_f32));
+                    yn[k] = s.get() * rr;
+                    dpre[k] = fma8(dh, yn[k], dpre[k]);
+                    s1 += dot8(w, yn[k]);
+                    g[k] = fma8(rr, w, g[k]);
+                }
+                keep[k].fill(p.keep.scale);
+                if (p.keep.drop) keep[k] = c.drop(keep[k], base, r, p.dim, p.keep);
+                if (p.post) {
+                    Eight f = keep[k] * un[k] * (kKept ? post[k] : c.template weight<T>(p.post, p.weights_f32));
+                    if (p.gate) f = f * gate[k];
+                    s2 += dot8(f, g[k]);
+                    if (p.dh) s3 += dot8(f, yn[k]);
+                }
+            }
+            if (p.dh || p.post) row_sums(s1, s2, s3, blockDim.x, sm[turn]);
+            const float m1 = -rr * p.inv_dim * s1, m2 = -rp * p.inv_dim * fmaf(m1, s3, s2);
+            if (!(p.dh || p.post) || blockDim.x == 32) __syncthreads();
+            if (lane == 0) ask();                             // all have read this row: another may have its place
+            if (++get == p.depth) { get = 0; phase ^= 1; }
+#pragma unroll
+            for (int k = 0; k < kUnits; ++k) {
+                const Columns<kFull> c(lane, k, blockDim.x, p.dim);
+                if (p.dh) g[k] = fma8(m1, yn[k], g[k]);
+                if (p.dx) c.put((S*)p.dx + r * p.ld_dx, g[k] * p.rs);
+                if (p.keep.drop) g[k] = g[k] * keep[k];
+                both[k] = fma8(g[k], un[k], both[k]);
+                if (p.gate) g[k] = g[k] * gate[k];
+                if (p.post) g[k] = fma8(m2, un[k], g[k] * (kKept ? post[k] : c.template weight<T>(p.post, p.weights_f32)) * rp);
+                c.put((T*)p.du + r * p.ld_du, g[k]);
+            }
+        }
+        if (p.gate) {
+#pragma unroll
+            for (int k = 0; k < kUnits; ++k) {
+                const Columns<kFull> c(lane, k, blockDim.x, p.dim);
+                if (p.post) dpost[k] = fma8(c.get((const T*)p.gate + now.group * p.ld_gate), both[k], dpost[k]);
+                if (p.dgate) {
+                    const Eight d = p.post ? both[k] * (kKept ? post[k] : c.template weight<T>(p.post, p.weights_f32)) : both[k];
+                    if (p.gate_part) c.put(p.gate_part + (long long)chunk * p.dim, d);
+                    else if (p.dgate_f32) c.put((float*)p.dgate + now.group * p.ld_dgate, d);
+                    else c.put((T*)p.dgate + now.group * p.ld_dgate, d);
+                }
+                both[k].fill(0.f);
+            }
+        }
+    }
+    if (!ok) ring_late();
+#pragma unroll
+    for (int k = 0; k < kUnits; ++k) {
+        const Columns<kFull> c(lane, k, blockDim.x, p.dim);
+        if (p.part_pre) c.put(p.part_pre + (long long)blockIdx.x * p.dim, dpre[k]);
+        if (p.part_post) c.put(p.part_post + (long long)blockIdx.x * p.dim, p.gate ? dpost[k] : both[k]);
     }
 }
 

@@ -259,31 +259,16 @@ def head_logprob_backward(hidden, weight, scratch, tokens, lse, dhidden=None, dw
         ld_dw, 1 if accumulate else 0, *_scratch(who, scratch), _status(who, status), _current(d) if stream is None else stream))
 
 
-def dropout(x, out, p, seed, offset=0, dev_offset=None, stream=None):
-    """pb_dropout: out = x / (1 - p) where kept, else 0; of matrices [rows, dim].  The gradient is the same call on out's gradient."""
-    who = "dropout"
-    d = _device(who, x)
-    _on_device(who, d, out, dev_offset)
-    rows, dim, ld = _rows(who, "x", x)
-    orows, odim, ld_out = _rows(who, "out", out)
-    if (orows, odim) != (rows, dim) or out.dtype is not x.dtype:
-        _refuse(who, "out must have x's shape and type")
-    _check(_lib.pb_dropout(x.data_ptr(), _DTYPE[x.dtype], rows, dim, ld, p, seed & 0xFFFFFFFFFFFFFFFF, offset, _vector(who, "dev_offset", dev_offset, 1, torch.int64),
-                           out.data_ptr(), ld_out, _current(d) if stream is None else stream))
-
-
 # pb_join_args and pb_join_grads in their own order: one call lays all fields out, where setting them one by one takes as long as the launch.
 _JOIN_ARGS, _JOIN_GRADS = struct.Struct("@qqiiiffdQqPPqPqPqqPPPqPqPP"), struct.Struct("@PqPqPqPqPqPPii")
 
 
 def _plane(who, name, t, shape, dtype, device):
-    """Address and row stride of a matrix with dense rows that may be absent."""
-    if t is None:
-        return 0, shape[1]
-    if t.shape != shape or t.dtype is not dtype:
+    """Address and row stride of a matrix with dense rows."""
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != device:
+        if t.get_device() != device:
+            _refuse(who, _OFF_DEVICE)
         _refuse(who, "%s must be a matrix of %d x %d of type %s" % (name, *shape, dtype))
-    if t.get_device() != device:
-        _refuse(who, _OFF_DEVICE)
     ld, step = t.stride()
     if step != 1 and shape[1] > 1:
         _refuse(who, "%s must have dense rows" % name)
@@ -296,12 +281,14 @@ def _line(who, name, t, n, dtype, device):
         return 0
     if t.get_device() != device:
         _refuse(who, _OFF_DEVICE)
-    return _vector(who, name, t, n, dtype)
+    if t.dtype is not dtype or t.numel() != n or not t.is_contiguous():
+        _refuse(who, "%s must be a dense %s tensor of %d elements" % (name, dtype, n))
+    return t.data_ptr()
 
 
 def _one_type(who, a, b):
     """Type of two vectors that have one, if they are there."""
-    dtype = (a if a is not None else b).dtype if a is not None or b is not None else torch.float32
+    dtype = a.dtype if a is not None else b.dtype if b is not None else torch.float32
     if dtype not in _DTYPE or (a is not None and b is not None and b.dtype is not dtype):
         _refuse(who, "the norms' weights, and their gradients, must be of one type")
     return dtype
@@ -309,12 +296,31 @@ def _one_type(who, a, b):
 
 def _join_gate(who, gate, rows_per_gate, rows, dim, dtype, device):
     """Address, row stride and rows per row of the gate."""
-    if gate is None:
-        return 0, dim, 1
     per = rows_per_gate or rows or 1
     if per < 1:
         _refuse(who, "rows_per_gate must be at least 1")
     return *_plane(who, "gate", gate, (-(-rows // per), dim), dtype, device), per
+
+
+_NOT_THAT = "an argument is not what it has to be: tensors on the current device, and numbers"
+
+
+def dropout(x, out, p, seed, offset=0, dev_offset=None, stream=None):
+    """pb_dropout: out = x / (1 - p) where kept, else 0; of matrices [rows, dim].  The gradient is the same call on out's gradient."""
+    who = "dropout"
+    d = _device(who, x)
+    try:
+        shape, dtype = x.shape, x.dtype
+        if len(shape) != 2 or dtype not in _DTYPE:
+            _refuse(who, "x must be a matrix of float32, bfloat16 or float16")
+        px, ld = _plane(who, "x", x, shape, dtype, d)
+        po, ld_out = _plane(who, "out", out, shape, dtype, d)
+        at = None if dev_offset is None else _line(who, "dev_offset", dev_offset, 1, torch.int64, d)
+        rc = _lib.pb_dropout(px, _DTYPE[dtype], shape[0], shape[1], ld, p, seed & 0xFFFFFFFFFFFFFFFF, offset, at, po, ld_out,
+                             _current(d) if stream is None else stream)
+    except (AttributeError, TypeError, C.ArgumentError):
+        _refuse(who, _NOT_THAT)
+    _check(rc)
 
 
 def join_forward(x, u, y, h=None, pre_weight=None, post_weight=None, gate=None, rows_per_gate=None, rstd_pre=None, rstd_post=None, residual_scale=1.0,
@@ -323,22 +329,24 @@ def join_forward(x, u, y, h=None, pre_weight=None, post_weight=None, gate=None, 
     [ceil(rows / rows_per_gate), dim] (rows_per_gate None: one row for all)."""
     who = "join_forward"
     d = _device(who, x)
-    if u is None or y is None:
-        _refuse(who, "u and y are needed")
     try:
-        shape, stream_dtype, dtype = u.shape, x.dtype, u.dtype
-        if len(shape) != 2 or stream_dtype not in _DTYPE or dtype not in _DTYPE:
+        shape, of_stream, dtype, f32 = u.shape, x.dtype, u.dtype, torch.float32
+        if len(shape) != 2 or of_stream not in _DTYPE or dtype not in _DTYPE:
             _refuse(who, "x and u must be matrices of float32, bfloat16 or float16")
         rows, dim = shape
         weights = _one_type(who, post_weight, pre_weight)
+        px, ld_x = _plane(who, "x", x, shape, of_stream, d)
+        pu, ld_u = _plane(who, "u", u, shape, dtype, d)
+        py, ld_y = _plane(who, "y", y, shape, of_stream, d)
+        ph, ld_h = (0, dim) if h is None else _plane(who, "h", h, shape, dtype, d)
+        pg, ld_g, per = (0, dim, 1) if gate is None else _join_gate(who, gate, rows_per_gate, rows, dim, dtype, d)
         args = _JOIN_ARGS.pack(
-            rows, dim, _DTYPE[dtype], _DTYPE[stream_dtype], _DTYPE[weights], residual_scale, eps, p, seed & 0xFFFFFFFFFFFFFFFF, offset,
-            _line(who, "dev_offset", dev_offset, 1, torch.int64, d), *_plane(who, "x", x, shape, stream_dtype, d), *_plane(who, "u", u, shape, dtype, d),
-            *_join_gate(who, gate, rows_per_gate, rows, dim, dtype, d), _line(who, "post_weight", post_weight, dim, weights, d),
-            _line(who, "pre_weight", pre_weight, dim, weights, d), *_plane(who, "y", y, shape, stream_dtype, d), *_plane(who, "h", h, shape, dtype, d),
-            _line(who, "rstd_post", rstd_post, rows, torch.float32, d), _line(who, "rstd_pre", rstd_pre, rows, torch.float32, d))
+            rows, dim, _DTYPE[dtype], _DTYPE[of_stream], _DTYPE[weights], residual_scale, eps, p, seed & 0xFFFFFFFFFFFFFFFF, offset,
+            0 if dev_offset is None else _line(who, "dev_offset", dev_offset, 1, torch.int64, d), px, ld_x, pu, ld_u, pg, ld_g, per,
+            _line(who, "post_weight", post_weight, dim, weights, d), _line(who, "pre_weight", pre_weight, dim, weights, d), py, ld_y, ph, ld_h,
+            _line(who, "rstd_post", rstd_post, rows, f32, d), _line(who, "rstd_pre", rstd_pre, rows, f32, d))
     except (AttributeError, TypeError, struct.error):
-        _refuse(who, "an argument is not what it has to be: tensors on the current device, and numbers")
+        _refuse(who, _NOT_THAT)
     _check(_lib.pb_join_forward(args, _current(d) if stream is None else stream))
 
 
@@ -356,34 +364,39 @@ def join_backward(y, u, dx, du, scratch, dy=None, dh=None, pre_weight=None, post
     join_scratch_bytes(...) bytes; y may be None without dh, dx if it is not wanted."""
     who = "join_backward"
     d = _device(who, u)
-    if du is None or scratch is None:
-        _refuse(who, "du and scratch are needed")
     try:
-        shape, dtype = u.shape, u.dtype
-        stream_dtype = dy.dtype if dy is not None else y.dtype if y is not None else dx.dtype if dx is not None else dtype
-        if len(shape) != 2 or stream_dtype not in _DTYPE or dtype not in _DTYPE:
+        shape, dtype, f32 = u.shape, u.dtype, torch.float32
+        of_stream = dy.dtype if dy is not None else y.dtype if y is not None else dx.dtype if dx is not None else dtype
+        if len(shape) != 2 or of_stream not in _DTYPE or dtype not in _DTYPE:
             _refuse(who, "u must be a matrix of float32, bfloat16 or float16, and so the residual stream")
         rows, dim = shape
         weights, grads = _one_type(who, post_weight, pre_weight), _one_type(who, dpost_weight, dpre_weight)
-        gate_type = dtype if dgate is None else dgate.dtype
-        if gate_type not in _DTYPE or (dgate is not None and gate is None):
-            _refuse(who, "dgate goes with a gate, and is of float32 or of its type")
+        pu, ld_u = _plane(who, "u", u, shape, dtype, d)
+        py, ld_y = (0, dim) if y is None else _plane(who, "y", y, shape, of_stream, d)
+        pg, ld_g, per = (0, dim, 1) if gate is None else _join_gate(who, gate, rows_per_gate, rows, dim, dtype, d)
         args = _JOIN_ARGS.pack(
-            rows, dim, _DTYPE[dtype], _DTYPE[stream_dtype], _DTYPE[weights], residual_scale, 0.0, p, seed & 0xFFFFFFFFFFFFFFFF, offset,
-            _line(who, "dev_offset", dev_offset, 1, torch.int64, d), 0, dim, *_plane(who, "u", u, shape, dtype, d),
-            *_join_gate(who, gate, rows_per_gate, rows, dim, dtype, d), _line(who, "post_weight", post_weight, dim, weights, d),
-            _line(who, "pre_weight", pre_weight, dim, weights, d), *_plane(who, "y", y, shape, stream_dtype, d), 0, dim,
-            _line(who, "rstd_post", rstd_post, rows, torch.float32, d), _line(who, "rstd_pre", rstd_pre, rows, torch.float32, d))
-        out = _JOIN_GRADS.pack(
-            *_plane(who, "dy", dy, shape, stream_dtype, d), *_plane(who, "dh", dh, shape, dtype, d), *_plane(who, "dx", dx, shape, stream_dtype, d),
-            *_plane(who, "du", du, shape, dtype, d), *((0, dim) if dgate is None else _plane(who, "dgate", dgate, gate.shape, gate_type, d)),
-            _line(who, "dpost_weight", dpost_weight, dim, grads, d), _line(who, "dpre_weight", dpre_weight, dim, grads, d), _DTYPE[gate_type], _DTYPE[grads])
+            rows, dim, _DTYPE[dtype], _DTYPE[of_stream], _DTYPE[weights], residual_scale, 0.0, p, seed & 0xFFFFFFFFFFFFFFFF, offset,
+            0 if dev_offset is None else _line(who, "dev_offset", dev_offset, 1, torch.int64, d), 0, dim, pu, ld_u, pg, ld_g, per,
+            _line(who, "post_weight", post_weight, dim, weights, d), _line(who, "pre_weight", pre_weight, dim, weights, d), py, ld_y, 0, dim,
+            _line(who, "rstd_post", rstd_post, rows, f32, d), _line(who, "rstd_pre", rstd_pre, rows, f32, d))
+        pdy, ld_dy = (0, dim) if dy is None else _plane(who, "dy", dy, shape, of_stream, d)
+        pdh, ld_dh = (0, dim) if dh is None else _plane(who, "dh", dh, shape, dtype, d)
+        pdx, ld_dx = (0, dim) if dx is None else _plane(who, "dx", dx, shape, of_stream, d)
+        pdu, ld_du = _plane(who, "du", du, shape, dtype, d)
+        of_gate, pdg, ld_dg = dtype, 0, dim
+        if dgate is not None:
+            of_gate = dgate.dtype
+            if gate is None or of_gate not in _DTYPE:
+                _refuse(who, "dgate goes with a gate, and is of float32 or of its type")
+            pdg, ld_dg = _plane(who, "dgate", dgate, gate.shape, of_gate, d)
+        out = _JOIN_GRADS.pack(pdy, ld_dy, pdh, ld_dh, pdx, ld_dx, pdu, ld_du, pdg, ld_dg, _line(who, "dpost_weight", dpost_weight, dim, grads, d),
+                               _line(who, "dpre_weight", dpre_weight, dim, grads, d), _DTYPE[of_gate], _DTYPE[grads])
         if scratch.get_device() != d:
             _refuse(who, _OFF_DEVICE)
-        room = _scratch(who, scratch)
+        room, size = _scratch(who, scratch)
     except (AttributeError, TypeError, struct.error):
-        _refuse(who, "an argument is not what it has to be: tensors on the current device, and numbers")
-    _check(_lib.pb_join_backward(args, out, *room, _current(d) if stream is None else stream))
+        _refuse(who, _NOT_THAT)
+    _check(_lib.pb_join_backward(args, out, room, size, _current(d) if stream is None else stream))
 
 
 def adamw_moments(m, m_scale, v, v_scale, m_out=None, v_out=None, stream=None):

@@ -23,9 +23,10 @@ constexpr int64_t kHeadFewRows = 128;           // rows that one block's tile ho
 constexpr int64_t kHeadPieceBytes = 256 << 20;  // of d, or of packed weights, held at a time
 constexpr int64_t kHeadPieceMin = 8192;         // tokens of a piece at least: dhidden's partial sums are read and written once for each
 constexpr int64_t kHeadStatRows = 8192;         // rows whose statistics are held at a time
-// Chunks of K that the tensor core adds up by itself.  It does not round to nearest, so its sums drift towards zero: log probabilities
-// of normal logits are off by 2e-7 of themselves after 1024 columns, 8e-7 after 4096, 1.7e-6 after 8192.
-constexpr int kHeadPromote = 4;                 // float32 operands: 6e-8
+// Chunks of K that the tensor core adds up by itself.  It does not round to nearest, so its sums drift towards zero, with every step that it adds at full
+// size (four of a chunk; of float32 operands twelve or 24): log probabilities of normal logits are off by 6e-8 of themselves after 16 steps, 2e-7 after 64, 8e-7
+// after 256, 1.7e-6 after 512.
+constexpr int kHeadPromoteNear = 2, kHeadPromoteWide = 1;       // float32 operands: 24 steps
 constexpr int kHeadPromoteLong = 32;            // 16-bit ones of more than kHeadLong chunks in the forward: 4096 x 131072 x 4096 takes 3.40 ms
 constexpr int kHeadLong = 64;                   // without, 3.51 with 16 chunks, 4.10 with 4
 constexpr int kHeadNever = 1 << 28;
@@ -34,17 +35,18 @@ constexpr int kHeadTileCost = 2;                // what a tile costs beside its 
 int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 
 struct HeadPlan {
-    int cg, planes, terms;
-    bool packed;
+    int cg;
+    bool f32, packed;            // packed: 16-bit operands are copied
     int64_t dp;                  // row stride of packed operands
-    int64_t piece;               // tokens of a piece of the vocabulary
+    int64_t piece, pieces;       // tokens of a piece of the vocabulary
     int64_t stat_rows, parts;
     int64_t ldd, ldp;
     int splits;
     int64_t split_chunks;
-    // scratch
-    unsigned short *hidden, *weight, *d;
-    float *part, *ztok, *plane, *unscale;
+    // scratch; `near` and `wide`: float16 and bfloat16 planes of float32 operands
+    unsigned short *hidden, *hidden_wide, *weight, *d, *d_wide;
+    float *part, *ztok, *plane, *unscale, *row_scale, *col_scale, *d_scale;
+    int* col_most;               // of each piece
     HeadRow* coef;
     int* row_token;
     size_t bytes;
@@ -53,26 +55,30 @@ struct HeadPlan {
 HeadPlan head_plan(int dtype, int64_t rows, int64_t vocab, int64_t dim, bool direct, bool backward, char* scratch) {
     HeadPlan e{};
     e.cg = rows <= kHeadFewRows ? 1 : 2;
-    e.planes = dtype == PB_F32 ? kHeadPlanes : 1;
-    e.terms = dtype == PB_F32 ? 6 : 1;
-    e.packed = dtype == PB_F32 || !direct;
+    e.f32 = dtype == PB_F32;
+    e.packed = !e.f32 && !direct;
     e.dp = up(dim, 8);
-    const int64_t tile = 128 * e.cg;
+    const int64_t tile = 128 * e.cg, operand = e.f32 ? kHeadNear : 1, planes = e.f32 ? kHeadNear + kHeadWide : 1;
     int64_t most = vocab;
-    if (e.packed) most = std::min(most, kHeadPieceBytes / (e.planes * e.dp * 2));
-    if (backward) most = std::min(most, kHeadPieceBytes / (e.planes * rows * 2));
+    if (e.f32 || e.packed) most = std::min(most, kHeadPieceBytes / (operand * e.dp * 2));
+    if (backward) most = std::min(most, kHeadPieceBytes / (planes * rows * 2));
     e.piece = most >= vocab ? vocab : std::min(vocab, up(std::max(most, kHeadPieceMin), 256));
-    const int64_t pieces = (vocab + e.piece - 1) / e.piece;
-    if (pieces > 1) e.piece = up((vocab + pieces - 1) / pieces, 256);          // of one size, but for the last
+    e.pieces = (vocab + e.piece - 1) / e.piece;
+    if (e.pieces > 1) e.piece = up((vocab + e.pieces - 1) / e.pieces, 256);    // of one size, but for the last
+    e.pieces = (vocab + e.piece - 1) / e.piece;
     size_t at = 0;
     auto take = [&](int64_t bytes) {
         char* p = scratch ? scratch + at : nullptr;
         at += (size_t)up(bytes, 256);
         return p;
     };
-    if (e.packed) {
-        e.hidden = (unsigned short*)take(e.planes * rows * e.dp * 2);
-        e.weight = (unsigned short*)take(e.planes * e.piece * e.dp * 2);
+    if (e.f32 || e.packed) {
+        e.hidden = (unsigned short*)take(operand * rows * e.dp * 2);
+        e.weight = (unsigned short*)take(operand * e.piece * e.dp * 2);
+    }
+    if (e.f32) {
+        e.row_scale = (float*)take(rows * 4);
+        e.col_scale = (float*)take((e.piece + kHeadGroup - 1) / kHeadGroup * 4);
     }
     if (!backward) {
         e.stat_rows = std::min(rows, kHeadStatRows);
@@ -82,7 +88,13 @@ HeadPlan head_plan(int dtype, int64_t rows, int64_t vocab, int64_t dim, bool dir
     } else {
         e.ldd = up(e.piece, 64);
         e.ldp = up(dim, 8);
-        e.d = (unsigned short*)take(e.planes * rows * e.ldd * 2);
+        e.d = (unsigned short*)take(operand * rows * e.ldd * 2);
+        if (e.f32) {
+            e.d_wide = (unsigned short*)take(kHeadWide * rows * e.ldd * 2);
+            e.hidden_wide = (unsigned short*)take(kHeadWide * rows * e.dp * 2);
+            e.d_scale = (float*)take(rows * 4);
+            e.col_most = (int*)take(e.pieces * 4);
+        }
         // Enough splits of K for every block where dhidden has few tiles, but no shorter than 16 chunks.
         const int64_t tiles = ((rows + tile - 1) / tile) * ((dim + tile - 1) / tile), chunks = (e.piece + kHeadChunk - 1) / kHeadChunk;
         const int64_t splits = std::max<int64_t>(1, std::min((kSms / e.cg) / tiles, chunks / 16));
@@ -123,12 +135,16 @@ bool map_of_out(CUtensorMap* map, const void* p, int64_t rows, int64_t cols, int
 }
 
 // D[m, n] = sum over k of a[m, k] b[n, k]; an MN-major operand lies as [k, m] or [k, n].
-bool job_of(HeadJob& j, int kind, int cg, const HeadMatrix& a, bool a_mn, const HeadMatrix& b, bool b_mn, int64_t chunks_per_split = 0) {
+bool job_of(HeadJob& j, int kind, int cg, int dtype, const HeadMatrix& a, bool a_mn, const HeadMatrix& b, bool b_mn, int promote,
+            int64_t chunks_per_split = 0) {
     const int64_t tile = 128 * cg, m = a_mn ? a.cols : a.rows, n = b_mn ? b.cols : b.rows, k = a_mn ? a.rows : a.cols;
     const int box = a_mn || m >= 128 ? 128 : (int)up(m, 8);
     if (!map_of(&j.a, a, a_mn, box) || !map_of(&j.b, b, b_mn, 128)) return false;
     j.kind = kind;
     j.a_mn = a_mn; j.b_mn = b_mn;
+    j.half = dtype == PB_F16 || a.planes == kHeadNear;
+    j.planes = a.planes;
+    j.promote = promote;
     j.a_bytes = a_mn ? kHeadOperand : box * 128;
     j.tiles_m = (int)((m + tile - 1) / tile);
     j.tiles_n = (int)((n + tile - 1) / tile);
@@ -155,8 +171,10 @@ cudaError_t head_launch(HeadArgs& g, cudaStream_t s) {
     if (e != cudaSuccess) return e;
     int64_t tiles = 0;
     g.a_slot = 1024;
+    int planes = 1;
     for (int j = 0; j < g.jobs; ++j) {
         tiles += g.job[j].tiles;
+        planes = std::max(planes, g.job[j].planes);
         g.a_slot = std::max(g.a_slot, g.job[j].a_bytes);
     }
     const int clusters = (int)std::min<int64_t>(tiles, kSms / CG);
@@ -168,8 +186,9 @@ cudaError_t head_launch(HeadArgs& g, cudaStream_t s) {
         const int64_t ratio = (g.job[0].chunks_per_split + kHeadTileCost) / (g.job[1].chunks_per_split + kHeadTileCost);
         if (g.late) g.extra = (int)std::min(ratio, g.job[1].tiles / early);
     }
-    // A whole A tile is read from the last slot too.
-    g.stages = std::min(kHeadMaxStages, (kHeadRing + g.a_slot - kHeadOperand) / (kHeadOperand + g.a_slot));
+    // The tensor core reads whole A tiles: behind the last one's rows it finds the epilogue's buffers.
+    g.stage_bytes = planes * (kHeadOperand + g.a_slot);
+    g.stages = std::min(kHeadMaxStages, kHeadRing / g.stage_bytes);
     cudaLaunchAttribute attr[2] = {};
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;      // barriers and tensor memory are set up while the launch before ends
     attr[0].val.programmaticStreamSerializationAllowed = 1;
@@ -192,11 +211,32 @@ cudaError_t head_launch(HeadArgs& g, int cg, bool promote, cudaStream_t s) {
     return promote ? head_launch<1, KIND, true>(g, s) : head_launch<1, KIND, false>(g, s);
 }
 
+// 16-bit rows copied, or the wide planes of float32 ones.
 cudaError_t pack(int dtype, const void* x, int64_t rows, int64_t dim, int64_t ld, unsigned short* out, int64_t ldp, cudaStream_t s) {
     const int64_t pairs = rows * (ldp / 2);
     const dim3 grid((unsigned)std::min<int64_t>((pairs + 255) / 256, kSms * 16));
     if (dtype == PB_F32) return launch_after(head_pack_kernel<float>, grid, 256, s, (const float*)x, rows, (int)dim, ld, out, (int)ldp, rows * ldp);
     return launch_after(head_pack_kernel<__half>, grid, 256, s, (const __half*)x, rows, (int)dim, ld, out, (int)ldp, rows * ldp);
+}
+// The near planes of float32 rows.
+template <int kGroup>
+cudaError_t pack_near(const float* x, int64_t rows, int64_t dim, int64_t ld, unsigned short* out, int64_t ldp, float* scale, int* most, cudaStream_t s) {
+    auto kernel = aligned(x, 16) && (ld % 4 == 0 || rows == 1) && dim % 4 == 0 ? head_near_kernel<kGroup, true> : head_near_kernel<kGroup, false>;
+    return launch_after(kernel, dim3((unsigned)((rows + kGroup - 1) / kGroup)), kNearThreads, s, x, (long long)rows, (int)dim, (long long)ld, out, (int)ldp,
+                        (long long)(rows * ldp), scale, most);
+}
+// What a call's products read of the hidden states and of a piece of the weights, packed where it has to be.
+cudaError_t hidden_of(HeadMatrix& m, const HeadPlan& e, int dtype, const void* x, int64_t rows, int64_t dim, int64_t ld, cudaStream_t s) {
+    m = HeadMatrix{x, rows, dim, ld, 0, 1};
+    if (!e.f32 && !e.packed) return cudaSuccess;
+    m = HeadMatrix{e.hidden, rows, dim, e.dp, rows * e.dp, e.f32 ? kHeadNear : 1};
+    return e.f32 ? pack_near<1>((const float*)x, rows, dim, ld, e.hidden, e.dp, e.row_scale, nullptr, s) : pack(dtype, x, rows, dim, ld, e.hidden, e.dp, s);
+}
+cudaError_t weight_of(HeadMatrix& m, const HeadPlan& e, int dtype, const void* x, int64_t rows, int64_t dim, int64_t ld, int* most, cudaStream_t s) {
+    m = HeadMatrix{x, rows, dim, ld, 0, 1};
+    if (!e.f32 && !e.packed) return cudaSuccess;
+    m = HeadMatrix{e.weight, rows, dim, e.dp, rows * e.dp, e.f32 ? kHeadNear : 1};
+    return e.f32 ? pack_near<kHeadGroup>((const float*)x, rows, dim, ld, e.weight, e.dp, e.col_scale, most, s) : pack(dtype, x, rows, dim, ld, e.weight, e.dp, s);
 }
 
 // Rows that a bulk copy can start on.
@@ -256,11 +296,8 @@ int pb_head_logprob_forward(const void* dev_hidden, const void* dev_weight, int 
     if (in_scratch(dev_hidden, n_h) || in_scratch(dev_weight, n_w) || in_scratch(dev_tokens, n_t) || in_scratch(dev_status, n_st) ||
         in_scratch(dev_logp, rows * 4) || in_scratch(dev_entropy, rows * 4) || in_scratch(dev_lse, rows * 4)) return refuse(who, "buffers overlap");
     const cudaStream_t s = (cudaStream_t)stream;
-    const bool half = dtype == PB_F16;
-    const HeadMatrix hidden = e.packed ? HeadMatrix{e.hidden, rows, dim, e.dp, rows * e.dp, e.planes}
-                                       : HeadMatrix{dev_hidden, rows, dim, ld_hidden, 0, 1};
-    cudaError_t err = cudaSuccess;
-    if (e.packed) err = pack(dtype, dev_hidden, rows, dim, ld_hidden, e.hidden, e.dp, s);
+    HeadMatrix hidden, b;
+    cudaError_t err = hidden_of(hidden, e, dtype, dev_hidden, rows, dim, ld_hidden, s);
     for (int64_t r0 = 0; r0 < rows && err == cudaSuccess; r0 += e.stat_rows) {
         const int64_t nr = std::min(e.stat_rows, rows - r0);
         HeadMatrix a = hidden;
@@ -268,10 +305,9 @@ int pb_head_logprob_forward(const void* dev_hidden, const void* dev_weight, int 
         a.rows = nr;
         HeadArgs g{};
         g.jobs = 1;
-        g.half = half;
-        g.terms = e.terms;
-        const bool promote = dtype == PB_F32 || dim > kHeadLong * kHeadChunk;
-        g.promote = dtype == PB_F32 ? kHeadPromote : promote ? kHeadPromoteLong : kHeadNever;
+        if (e.f32) { g.row_scale = e.row_scale + r0; g.col_scale = e.col_scale; }
+        const bool promote = e.f32 || dim > kHeadLong * kHeadChunk;
+        const int chunks = e.f32 ? kHeadPromoteNear : promote ? kHeadPromoteLong : kHeadNever;
         g.c = (float)(inv_temperature * 1.4426950408889634074);
         g.status = dev_status;
         g.part = e.part;
@@ -283,13 +319,9 @@ int pb_head_logprob_forward(const void* dev_hidden, const void* dev_weight, int 
         g.vocab = vocab;
         for (int64_t v0 = 0; v0 < vocab && err == cudaSuccess; v0 += e.piece) {
             const int64_t nv = std::min(e.piece, vocab - v0);
-            const char* w0 = (const char*)dev_weight + v0 * ld_weight * (int64_t)es;
-            HeadMatrix b{w0, nv, dim, ld_weight, 0, 1};
-            if (e.packed) {
-                if (r0 == 0 || e.piece < vocab) err = pack(dtype, w0, nv, dim, ld_weight, e.weight, e.dp, s);
-                b = HeadMatrix{e.weight, nv, dim, e.dp, nv * e.dp, e.planes};
-            }
-            if (!job_of(g.job[0], kHeadStats, e.cg, a, false, b, false)) return no_map(who);
+            // a single piece stays packed for the next rows
+            if (r0 == 0 || e.pieces > 1) err = weight_of(b, e, dtype, (const char*)dev_weight + v0 * ld_weight * (int64_t)es, nv, dim, ld_weight, nullptr, s);
+            if (!job_of(g.job[0], kHeadStats, e.cg, dtype, a, false, b, false, chunks)) return no_map(who);
             g.col0 = (int)v0;
             if (err == cudaSuccess) err = head_launch<kHeadStats>(g, e.cg, promote, s);
             g.part0 += g.job[0].tiles_n;
@@ -351,16 +383,24 @@ int pb_head_logprob_backward(const void* dev_hidden, const void* dev_weight, int
         for (int l = 0; l < k; ++l)
             if (written[l].p && overlap(written[k].p, written[k].n, written[l].p, written[l].n)) return refuse(who, "buffers overlap");
     }
-    const bool half = dtype == PB_F16, promote = dtype == PB_F32;
     cudaError_t err = launch_after(head_coef_kernel, dim3(1), 1024, s, (int)rows, (long long)vocab, dev_tokens, token_bytes, inv_temperature, dev_lse, dev_entropy,
-                             dev_g_logp, dev_g_entropy, dev_g_lse, half ? 16384.f : 1.f, e.coef, e.row_token, e.unscale, dev_status);
-    if (e.packed && err == cudaSuccess) err = pack(dtype, dev_hidden, rows, dim, ld_hidden, e.hidden, e.dp, s);
-    const HeadMatrix hidden = e.packed ? HeadMatrix{e.hidden, rows, dim, e.dp, rows * e.dp, e.planes}
-                                       : HeadMatrix{dev_hidden, rows, dim, ld_hidden, 0, 1};
+                                   dev_g_logp, dev_g_entropy, dev_g_lse, dtype == PB_F16 ? 16384.f : 1.f, e.coef, e.row_token, e.unscale, e.d_scale, e.col_most,
+                                   (int)(e.f32 ? e.pieces : 0), dev_status);
+    HeadMatrix hidden, w;
+    if (err == cudaSuccess) err = hidden_of(hidden, e, dtype, dev_hidden, rows, dim, ld_hidden, s);
+    // dweight's own
+    HeadMatrix hidden_wide = hidden;
+    if (e.f32 && dev_dweight) {
+        if (err == cudaSuccess) err = pack(dtype, dev_hidden, rows, dim, ld_hidden, e.hidden_wide, e.dp, s);
+        hidden_wide = HeadMatrix{e.hidden_wide, rows, dim, e.dp, rows * e.dp, kHeadWide};
+    }
     HeadArgs g{};
-    g.half = half;
-    g.terms = e.terms;
-    g.promote = promote ? kHeadPromote : kHeadNever;
+    const int near = e.f32 ? kHeadPromoteNear : kHeadNever, wide = e.f32 ? kHeadPromoteWide : kHeadNever;
+    g.row_scale = e.row_scale;
+    g.col_scale = e.col_scale;
+    g.d_scale = e.d_scale;
+    g.store_near = dev_dhidden != nullptr;
+    g.store_wide = dev_dweight != nullptr;
     g.c = (float)(inv_temperature * 1.4426950408889634074);
     g.status = dev_status;
     g.coef = e.coef;
@@ -377,42 +417,45 @@ int pb_head_logprob_backward(const void* dev_hidden, const void* dev_weight, int
     int planes = 0;
     for (int64_t v0 = 0; v0 < vocab && err == cudaSuccess; v0 += e.piece) {
         const int64_t nv = std::min(e.piece, vocab - v0);
-        const char* w0 = (const char*)dev_weight + v0 * ld_weight * (int64_t)es;
-        HeadMatrix w{w0, nv, dim, ld_weight, 0, 1};
-        if (e.packed) {
-            err = pack(dtype, w0, nv, dim, ld_weight, e.weight, e.dp, s);
-            w = HeadMatrix{e.weight, nv, dim, e.dp, nv * e.dp, e.planes};
-        }
-        const HeadMatrix d{e.d, rows, nv, e.ldd, d_plane, e.planes};
+        int* const most = e.f32 ? e.col_most + v0 / e.piece : nullptr;
+        if (err == cudaSuccess) err = weight_of(w, e, dtype, (const char*)dev_weight + v0 * ld_weight * (int64_t)es, nv, dim, ld_weight, most, s);
+        g.col_most = (const float*)most;
+        const HeadMatrix d{e.d, rows, nv, e.ldd, d_plane, e.f32 ? kHeadNear : 1}, d_wide = e.f32 ? HeadMatrix{e.d_wide, rows, nv, e.ldd, d_plane, kHeadWide} : d;
         g.col0 = (int)v0;
         g.jobs = 1;
-        if (!job_of(g.job[0], kHeadGrad, e.cg, hidden, false, w, false) || !map_of_out(&g.job[0].out, e.d, rows, nv, e.ldd, d_plane, e.planes, 2))
-            return no_map(who);
-        if (err == cudaSuccess) err = head_launch<kHeadGrad>(g, e.cg, promote, s);
+        if (!job_of(g.job[0], kHeadGrad, e.cg, dtype, hidden, false, w, false, near) ||
+            !map_of_out(&g.job[0].out, d_wide.p, rows, nv, e.ldd, d_plane, d_wide.planes, 2) ||
+            !map_of_out(&g.job[1].out, d.p, rows, nv, e.ldd, d_plane, d.planes, 2)) return no_map(who);
+        if (err == cudaSuccess) err = head_launch<kHeadGrad>(g, e.cg, e.f32, s);
         g.jobs = 0;
         g.add = v0 > 0;
         if (dev_dhidden) {
             // as many chunks in each split of every piece, so that the first piece has the most splits
             HeadJob& j = g.job[g.jobs++];
-            if (!job_of(j, kHeadHidden, e.cg, d, false, w, true, e.split_chunks) || !map_of_out(&j.out, e.plane, rows, dim, e.ldp, plane_size, e.splits, 4))
+            if (!job_of(j, kHeadHidden, e.cg, dtype, d, false, w, true, near, e.split_chunks) || !map_of_out(&j.out, e.plane, rows, dim, e.ldp, plane_size, e.splits, 4))
                 return no_map(who);
             planes = std::max(planes, j.splits);
         }
         if (dev_dweight) {
             g.out = (char*)dev_dweight + v0 * ld_dweight * (int64_t)gs;
             HeadJob& j = g.job[g.jobs++];
-            if (!job_of(j, kHeadWeight, e.cg, d, true, hidden, true) || (g.bulk && !map_of_out(&j.out, g.out, nv, dim, ld_dweight, 0, 1, (int)gs))) return no_map(who);
+            if (!job_of(j, kHeadWeight, e.cg, dtype, d_wide, true, hidden_wide, true, wide) || (g.bulk && !map_of_out(&j.out, g.out, nv, dim, ld_dweight, 0, 1, (int)gs))) return no_map(who);
+        }
+        if (e.f32 && g.jobs == 2) {              // stages of another size each: two launches
+            g.jobs = 1;
+            if (err == cudaSuccess) err = head_launch<kHeadHidden>(g, e.cg, e.f32, s);
+            std::swap(g.job[0], g.job[1]);
         }
         // the longer product's tiles first
         if (g.jobs == 2 && g.job[1].chunks_per_split > g.job[0].chunks_per_split) std::swap(g.job[0], g.job[1]);
-        if (err == cudaSuccess) err = head_launch<kHeadHidden>(g, e.cg, promote, s);
+        if (err == cudaSuccess) err = head_launch<kHeadHidden>(g, e.cg, e.f32, s);
     }
     if (dev_dhidden && err == cudaSuccess) {
         const int64_t n = rows * (e.ldp / 8);
         const dim3 grid((unsigned)std::min<int64_t>((n + 255) / 256, kSms * 16));
         auto go = [&](auto t) {
             using T = decltype(t);
-            return launch_after(head_sum_kernel<T>, grid, 256, s, e.plane, plane_size, planes, (int)e.ldp, (int)rows, (int)dim, e.unscale, (T*)dev_dhidden, (long long)ld_dhidden);
+            return launch_after(head_sum_kernel<T>, grid, 256, s, e.plane, plane_size, planes, (int)e.ldp, (int)rows, (int)dim, e.unscale, e.d_scale, (T*)dev_dhidden, (long long)ld_dhidden);
         };
         err = dtype == PB_F32 ? go(float()) : dtype == PB_BF16 ? go(__nv_bfloat16()) : go(__half());
     }

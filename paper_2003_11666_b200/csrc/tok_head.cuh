@@ -19,10 +19,13 @@
 //   logits   A = hidden (K-major)        B = weight (K-major)      the row statistics, or d, are computed from the tile
 //   hidden   A = d (K-major)             B = weight (MN-major)     float32 partial sums, one plane per split of K
 //   weight   A = d, read transposed (MN-major)  B = hidden (MN-major)
-// float32 operands are held as three bfloat16 planes (x = x0 + x1 + x2 to 2^-25 of x), and a product is
-// the six terms x_i y_j with i + j <= 2; what is left out is below 2^-25.
+// float32 operands are held in planes of 16 bits, and a product is a sum of products of planes.  Where the absolute size of an error
+// counts (the logits; dhidden, a sum over tokens), two float16 planes do: x = 2^k (x0 + x1) to 2^-24 of x or 2^-39 of the largest number
+// that shares k (a row of hidden states, 32 rows of the weights, a row of d), and x0 y0 + x0 y1 + x1 y0 leaves out 2^-24.  A row of
+// dweight is a token's own, however improbable, so its product keeps float32's range: three bfloat16 planes (x0 + x1 + x2 to 2^-25)
+// and the six terms x_i y_j with i + j <= 2.  (Six terms everywhere: 509 x 50021 x 1001 forward 360 us, and backward 1000.)
 // The tensor core adds to its float32 accumulator without rounding to nearest, so a long K drifts:
-// float32 products, and the logits of the forward, leave the tensor core every kHeadPromote chunks and are
+// float32 products, and the logits of the forward, leave the tensor core every few chunks and are
 // added up in registers.
 // Every wait is bounded (see mbar_wait); a block whose wait runs out reports it and gives NaN for its tiles.
 #pragma once
@@ -34,12 +37,14 @@ namespace pb {
 constexpr int kHeadChunk = 64;                // K elements per stage: one 128-byte swizzled row
 constexpr int kHeadOperand = 128 * 128;       // bytes of an operand's 128 x 64 tile
 constexpr int kHeadMaxStages = 12;
-constexpr int kHeadEpiWarps = 8;              // quarter w % 4 of the tensor-memory lanes, half w / 4 of the columns
 constexpr int kHeadBuf = 32 * 128;            // bytes of an epilogue warp's buffer: 128 of each of its rows
-constexpr int kHeadRing = 196608;             // bytes for the stages: six of 32 KB, or twelve with A tiles of up to eight rows
-constexpr int kHeadSmem = 1024 + kHeadRing + kHeadEpiWarps * kHeadBuf;
-constexpr int kHeadThreads = 32 * (kHeadEpiWarps + 2);
-constexpr int kHeadPlanes = 3;                // bfloat16 planes of a float32 operand
+constexpr int kHeadEpi = 8;                   // epilogue warps: quarter w % 4 of the tensor-memory lanes, half w / 4 of the columns
+constexpr int kHeadThreads = 32 * (kHeadEpi + 2);
+constexpr int kHeadRing = 196608;             // bytes for the stages: six of 32 KB; three with two planes of each operand, two with three; twelve with A
+                                              // tiles of up to eight rows
+constexpr int kHeadSmem = 1024 + kHeadRing + kHeadEpi * kHeadBuf;
+constexpr int kHeadWide = 3, kHeadNear = 2;  // bfloat16 and float16 planes of a float32 operand
+constexpr int kHeadGroup = 32;                // rows of the weights that share a power of two
 
 enum HeadKind { kHeadStats = 0, kHeadGrad = 1, kHeadHidden = 2, kHeadWeight = 3 };
 
@@ -49,6 +54,8 @@ struct alignas(64) HeadJob {
     CUtensorMap out;             // (column, row, plane) of what is stored by bulk copies: boxes of 128 bytes by 32 rows
     int kind;
     int a_mn, b_mn;              // operand is MN-major
+    int half, planes;            // operands are float16; planes of each: 1, 2 or 3, of which 1, 3 or 6 products are taken
+    int promote;                 // chunks of K that the tensor core adds up by itself
     int tiles_m, tiles_n, splits;
     int group_m;                 // row tiles that are walked through together, for one column tile after the other
     int chunks, chunks_per_split;
@@ -68,11 +75,9 @@ struct HeadRow {
 
 struct alignas(64) HeadArgs {
     HeadJob job[2];
-    int jobs, half;              // half: operands are float16
+    int jobs;
     int extra, late, rounds;     // see head_tile
-    int stages, a_slot;          // of the ring; bytes between two stages' A tiles, which lie behind the B tiles
-    int terms;                   // 1, or 6 products of planes
-    int promote;                 // chunks of K that the tensor core adds up by itself
+    int stages, stage_bytes, a_slot;     // of the ring: a stage has the B tiles of a chunk's planes, then its A tiles, a_slot bytes each
     float c;                     // inv_temperature * log2(e)
     int col0;                    // first column (token) of this piece of the vocabulary
     int* status;
@@ -83,6 +88,9 @@ struct alignas(64) HeadArgs {
     const void* tokens;
     int token_bytes;
     long long vocab;
+    // float32: the powers of two of the float16 planes (NULL: none), of hidden rows, of groups of the weights' rows, the largest of those; of d's rows
+    const float *row_scale, *col_scale, *col_most, *d_scale;
+    int store_near, store_wide;  // planes of d that are wanted: for dhidden (map job[1].out), for dweight (map job[0].out)
     // d
     const HeadRow* coef;
     const int* row_token;        // index of the token, or -1
@@ -186,114 +194,120 @@ __device__ __forceinline__ bool head_tile(const HeadArgs& g, int i, int& j, Head
     return true;
 }
 
-// Planes of the terms of a float32 product, the smallest first: what is added to a small sum loses less.
-__device__ __forceinline__ void head_term(int terms, int k, int& pa, int& pb) {
-    if (terms == 1) { pa = pb = 0; return; }
-    pa = k == 0 ? 2 : k == 2 || k == 3 ? 1 : 0;              // (2,0) (0,2) (1,1) (1,0) (0,1) (0,0)
-    pb = k == 1 ? 2 : k == 2 || k == 4 ? 1 : 0;
-}
-
 // ------------------------------------------------------------------ copies (one thread of each block)
 template <int CG>
 __device__ void head_copies(const HeadArgs& g, unsigned char* smem, HeadShared& sh, int rank) {
-    int stg = 0, j;
-    uint32_t phase = 1;                                       // every stage is free at first
-    HeadTile x;
     constexpr int kRows = 128 * CG;
-    const uint32_t b_tiles = smem_u32(smem), a_tiles = b_tiles + g.stages * kHeadOperand;
+    const uint32_t ring = smem_u32(smem), full0 = smem_u32(&sh.full[0]), empty0 = smem_u32(&sh.empty[0]), lead0 = CG == 2 ? of_leader(full0) : full0;
+    const int stages = g.stages, stage = g.stage_bytes, slot = g.a_slot;
+    int stg = 0, j;
+    uint32_t phase = 1, off = 0;                              // every stage is free at first
+    HeadTile x;
     for (int i = 0; head_tile(g, i, j, x); ++i) {
         const HeadJob& q = g.job[j];
-        const int m0 = x.m * kRows + rank * 128, n0 = x.n * kRows + rank * 128;
-        const uint32_t bytes = (uint32_t)(q.a_bytes + kHeadOperand) * CG;
-        for (int c0 = x.chunk0; c0 < x.chunk1; c0 += g.promote) {
-            const int c1 = min(x.chunk1, c0 + g.promote);
-            for (int term = 0; term < g.terms; ++term) {
-                int pa, pb;
-                head_term(g.terms, term, pa, pb);
-                for (int c = c0; c < c1; ++c) {
-                    const uint32_t empty = smem_u32(&sh.empty[stg]);
-                    if (!(CG == 2 ? mbar_wait_pair(empty, phase, &sh.fail) : mbar_wait(empty, phase, &sh.fail))) { sh.fail = 1; return; }
-                    const uint32_t sa = a_tiles + stg * g.a_slot, sb = b_tiles + stg * kHeadOperand;
-                    const uint32_t own = smem_u32(&sh.full[stg]), full = CG == 2 ? of_leader(own) : own;
-                    if (rank == 0) mbar_arrive_tx(own, bytes);
-                    auto copy = [&](uint32_t dst, const CUtensorMap* tm, int u, int v, int w) {
-                        if (CG == 2) tma_3d_pair(dst, tm, u, v, w, full); else tma_3d(dst, tm, u, v, w, full);
-                    };
-                    const int k = c * kHeadChunk;
-                    if (q.a_mn) {
-                        copy(sa, &q.a, m0, k, pa);
-                        copy(sa + kHeadOperand / 2, &q.a, m0 + 64, k, pa);
-                    } else {
-                        copy(sa, &q.a, k, m0, pa);
-                    }
-                    if (q.b_mn) {
-                        copy(sb, &q.b, n0, k, pb);
-                        copy(sb + kHeadOperand / 2, &q.b, n0 + 64, k, pb);
-                    } else {
-                        copy(sb, &q.b, k, n0, pb);
-                    }
-                    if (++stg == g.stages) { stg = 0; phase ^= 1; }
+        const int m0 = x.m * kRows + rank * 128, n0 = x.n * kRows + rank * 128, planes = q.planes;
+        const bool a_mn = q.a_mn, b_mn = q.b_mn;
+        const uint32_t bytes = (uint32_t)(planes * (q.a_bytes + kHeadOperand)) * CG;
+        for (int c = x.chunk0; c < x.chunk1; ++c) {
+            const uint32_t empty = empty0 + stg * 8, full = lead0 + stg * 8;
+            if (!(CG == 2 ? mbar_wait_pair(empty, phase, &sh.fail) : mbar_wait(empty, phase, &sh.fail))) { sh.fail = 1; return; }
+            if (rank == 0) mbar_arrive_tx(full0 + stg * 8, bytes);
+            uint32_t sb = ring + off, sa = sb + planes * kHeadOperand;
+            auto copy = [&](uint32_t dst, const CUtensorMap* tm, int u, int v, int w) {
+                if (CG == 2) tma_3d_pair(dst, tm, u, v, w, full); else tma_3d(dst, tm, u, v, w, full);
+            };
+            const int k = c * kHeadChunk;
+            for (int plane = 0; plane < planes; ++plane, sa += slot, sb += kHeadOperand) {
+                if (a_mn) {
+                    copy(sa, &q.a, m0, k, plane);
+                    copy(sa + kHeadOperand / 2, &q.a, m0 + 64, k, plane);
+                } else {
+                    copy(sa, &q.a, k, m0, plane);
+                }
+                if (b_mn) {
+                    copy(sb, &q.b, n0, k, plane);
+                    copy(sb + kHeadOperand / 2, &q.b, n0 + 64, k, plane);
+                } else {
+                    copy(sb, &q.b, k, n0, plane);
                 }
             }
+            off += stage;
+            if (++stg == stages) { stg = 0; off = 0; phase ^= 1; }
         }
     }
 }
 
 // ------------------------------------------------------------------ products (one thread of a block or pair)
+// One product of 16 columns of K; the low words of the operands' descriptors, of which the high word is the same.
+template <int CG>
+__device__ __forceinline__ void head_mma(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t acc) {
+    constexpr uint64_t kHigh = (uint64_t)((1024 >> 4) | (1u << 14) | (2u << 29)) << 32;      // tc_desc's: 8 rows are 1024 bytes, version 1, 128-byte swizzle
+    if (CG == 2)
+        asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}"
+                     ::"r"(d), "l"(kHigh | a), "l"(kHigh | b), "r"(idesc), "r"(acc) : "memory");
+    else
+        asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}"
+                     ::"r"(d), "l"(kHigh | a), "l"(kHigh | b), "r"(idesc), "r"(acc) : "memory");
+}
+
+// One thread issues everything, and a chunk of a pair's tile takes the tensor cores 512 cycles: what it does per chunk has to be short (with the descriptors
+// put together for each product, and loops over the planes, 4096 x 131072 x 4096 took 3.29 ms where 2.94 are possible).
 template <int CG>
 __device__ void head_products(const HeadArgs& g, unsigned char* smem, HeadShared& sh) {
-    int stg = 0, at = 0, j;
-    uint32_t phase = 0;
-    HeadTile x;
     constexpr int kCols = 128 * CG;
-    const uint32_t b_tiles = smem_u32(smem), a_tiles = b_tiles + g.stages * kHeadOperand;
+    const uint32_t ring = smem_u32(smem) >> 4, stage = (uint32_t)g.stage_bytes >> 4, slot = (uint32_t)g.a_slot >> 4, tmem = sh.tmem_base;
+    const uint32_t full0 = smem_u32(&sh.full[0]), empty0 = smem_u32(&sh.empty[0]);
+    const int stages = g.stages;
+    int stg = 0, at = 0, j;
+    uint32_t phase = 0, off = 0;
+    HeadTile x;
+    auto wait = [&](uint32_t bar, uint32_t parity) { return CG == 2 ? mbar_wait_pair(bar, parity, &sh.fail) : mbar_wait(bar, parity, &sh.fail); };
+    auto commit = [&](uint32_t bar) {
+        if (CG == 2)
+            asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+                         ::"r"(bar), "h"((unsigned short)3) : "memory");
+        else
+            asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+    };
     for (int i = 0; head_tile(g, i, j, x); ++i) {
         const HeadJob& q = g.job[j];
-        const uint32_t type = g.half ? 0u : (1u << 7) | (1u << 10);
+        const uint32_t type = q.half ? 0u : (1u << 7) | (1u << 10);
         const uint32_t idesc = (1u << 4) | type | ((uint32_t)q.a_mn << 15) | ((uint32_t)q.b_mn << 16) | ((uint32_t)(kCols >> 3) << 17) |
                                ((uint32_t)(128 * CG >> 4) << 24);
-        const uint32_t step_a = q.a_mn ? 2048 : 32, step_b = q.b_mn ? 2048 : 32;
-        const uint32_t lead_a = q.a_mn ? kHeadOperand / 2 : 16, lead_b = q.b_mn ? kHeadOperand / 2 : 16;
-        for (int c0 = x.chunk0; c0 < x.chunk1; c0 += g.promote, ++at) {
-            const int n = (min(x.chunk1, c0 + g.promote) - c0) * g.terms, buf = at & 1;
-            if (at >= 2) {
-                const uint32_t bar = smem_u32(&sh.acc_empty[buf]), parity = (uint32_t)(((at >> 1) & 1) ^ 1);
-                if (!(CG == 2 ? mbar_wait_pair(bar, parity, &sh.fail) : mbar_wait(bar, parity, &sh.fail))) { sh.fail = 1; return; }
-            }
+        // in units of 16 bytes: 16 columns of K further; the distance of an MN-major tile's halves, in the upper half of the word
+        const uint32_t step_a = q.a_mn ? 128 : 2, step_b = q.b_mn ? 128 : 2;
+        const uint32_t a0 = (ring + (uint32_t)q.planes * (kHeadOperand >> 4)) | (q.a_mn ? (uint32_t)kHeadOperand / 2 >> 4 : 1u) << 16;
+        const uint32_t b0 = ring | (q.b_mn ? (uint32_t)kHeadOperand / 2 >> 4 : 1u) << 16;
+        const int planes = q.planes, promote = q.promote;
+        for (int c0 = x.chunk0; c0 < x.chunk1; c0 += promote, ++at) {
+            const int n = min(x.chunk1 - c0, promote), buf = at & 1;
+            if (at >= 2 && !wait(smem_u32(&sh.acc_empty[buf]), (uint32_t)(((at >> 1) & 1) ^ 1))) { sh.fail = 1; return; }
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            const uint32_t dcol = sh.tmem_base + (uint32_t)(buf * kCols);
+            const uint32_t dcol = tmem + (uint32_t)(buf * kCols);
             for (int k = 0; k < n; ++k) {
-                const uint32_t full = smem_u32(&sh.full[stg]);
-                if (!(CG == 2 ? mbar_wait_pair(full, phase, &sh.fail) : mbar_wait(full, phase, &sh.fail))) { sh.fail = 1; return; }
+                if (!wait(full0 + stg * 8, phase)) { sh.fail = 1; return; }
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                const uint32_t sa = a_tiles + stg * g.a_slot, sb = b_tiles + stg * kHeadOperand;
+                const uint32_t a = a0 + off, b = b0 + off;
+                uint32_t acc = k > 0;
+                auto term = [&](int pa, int pb) {
 #pragma unroll
-                for (int u = 0; u < kHeadChunk / 16; ++u) {
-                    const uint64_t da = tc_desc(sa + u * step_a, lead_a, 1024), db = tc_desc(sb + u * step_b, lead_b, 1024);
-                    const uint32_t acc = k > 0 || u > 0;
-                    if (CG == 2)
-                        asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}"
-                                     ::"r"(dcol), "l"(da), "l"(db), "r"(idesc), "r"(acc) : "memory");
-                    else
-                        asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}"
-                                     ::"r"(dcol), "l"(da), "l"(db), "r"(idesc), "r"(acc) : "memory");
-                }
-                auto commit = [&](uint64_t* bar) {
-                    if (CG == 2)
-                        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
-                                     ::"r"(smem_u32(bar)), "h"((unsigned short)3) : "memory");
-                    else
-                        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+                    for (int u = 0; u < kHeadChunk / 16; ++u, acc = 1)
+                        head_mma<CG>(dcol, a + pa * slot + u * step_a, b + pb * (kHeadOperand >> 4) + u * step_b, idesc, acc);
                 };
-                commit(&sh.empty[stg]);
-                if (k == n - 1) commit(&sh.acc_full[buf]);
-                if (++stg == g.stages) { stg = 0; phase ^= 1; }
+                // the products of planes, the smallest first: what is added to a small sum loses less
+                if (planes == 3) { term(2, 0); term(0, 2); term(1, 1); }
+                if (planes > 1) { term(1, 0); term(0, 1); }
+                term(0, 0);
+                commit(empty0 + stg * 8);
+                if (k == n - 1) commit(smem_u32(&sh.acc_full[buf]));
+                off += stage;
+                if (++stg == stages) { stg = 0; off = 0; phase ^= 1; }
             }
         }
     }
 }
 
-// ------------------------------------------------------------------ what becomes of a tile (eight warps of each block)
+// ------------------------------------------------------------------ what becomes of a tile (the epilogue warps)
 // A thread holds a row, 32 threads of a warp 32 rows: stored as they are, an instruction would send 32 sectors of 32 rows one by one (2 us for
 // a tile of 128 x 128, whatever its K).  Instead 128 bytes of each row go to a buffer of the warp, 16-byte piece k of row r at k ^ (r mod 8) as the
 // 128-byte swizzle of the bulk copy that stores them.
@@ -301,10 +315,16 @@ __device__ __forceinline__ void buf_free(int lane) {           // the copy befor
     if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
     __syncwarp();
 }
-__device__ __forceinline__ void buf_put(unsigned char* buf, int lane, const unsigned* w) {
+__device__ __forceinline__ void buf_put(unsigned char* buf, int lane, int k, uint4 w) {
+    *reinterpret_cast<uint4*>(buf + lane * 128 + ((k ^ (lane & 7)) << 4)) = w;
+}
+// 64 columns in a 16-bit type, eight at a time: nothing is held beside the columns themselves, which fill the registers where parts of K are added up.
+template <typename T>
+__device__ __forceinline__ void buf_halves(unsigned char* buf, int lane, const float (&z)[64]) {
 #pragma unroll
     for (int k = 0; k < 8; ++k)
-        *reinterpret_cast<uint4*>(buf + lane * 128 + ((k ^ (lane & 7)) << 4)) = make_uint4(w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]);
+        buf_put(buf, lane, k, make_uint4(pack2(z[8 * k], z[8 * k + 1], T()), pack2(z[8 * k + 2], z[8 * k + 3], T()), pack2(z[8 * k + 4], z[8 * k + 5], T()),
+                                         pack2(z[8 * k + 6], z[8 * k + 7], T())));
 }
 template <bool kAdd>
 __device__ __forceinline__ void buf_store(unsigned char* buf, int lane, const CUtensorMap* map, int c, int r, int plane) {
@@ -323,13 +343,21 @@ __device__ __forceinline__ void buf_floats(const HeadJob& q, unsigned char* buf,
 #pragma unroll
     for (int h = 0; h < 64; h += 32) {
         if (c0 + h >= q.cols) break;
-        unsigned w[32];
-#pragma unroll
-        for (int k = 0; k < 32; ++k) w[k] = __float_as_uint(z[h + k]);
         buf_free(lane);
-        buf_put(buf, lane, w);
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            buf_put(buf, lane, k, make_uint4(__float_as_uint(z[h + 4 * k]), __float_as_uint(z[h + 4 * k + 1]), __float_as_uint(z[h + 4 * k + 2]),
+                                             __float_as_uint(z[h + 4 * k + 3])));
         if (add) buf_store<true>(buf, lane, &q.out, c0 + h, r, plane); else buf_store<false>(buf, lane, &q.out, c0 + h, r, plane);
     }
+}
+
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+                   "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+                 : "r"(taddr) : "memory");
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 }
 
 // Exponents from here down give zero; a finite one, so that zero times it is zero too.  A NaN stays.
@@ -389,6 +417,7 @@ struct HeadView {
     bool live;
     HeadRow hr;
     int tok;                      // column of the row's token in the piece, or out of it
+    float row_scale, d_scale;
 };
 
 template <int CG, int KIND>
@@ -399,6 +428,9 @@ __device__ __forceinline__ HeadView head_view(const HeadArgs& g, int i, int rank
     const HeadJob& q = g.job[v.j];
     v.row = v.x.m * 128 * CG + rank * 128 + (warp & 3) * 32 + lane;
     v.tok = -1;
+    v.row_scale = v.d_scale = 1.f;
+    if ((KIND == kHeadStats || KIND == kHeadGrad) && g.row_scale && v.row < q.rows) v.row_scale = g.row_scale[v.row];
+    if (KIND == kHeadGrad && g.d_scale && v.row < q.rows) v.d_scale = g.d_scale[v.row];
     if (KIND == kHeadStats && v.row < q.rows && g.tokens) {
         const long long id = g.token_bytes == 8 ? ((const long long*)g.tokens)[v.row] : (long long)((const int*)g.tokens)[v.row];
         if (id >= g.col0 && id < (long long)g.col0 + q.cols) v.tok = (int)(id - g.col0);
@@ -435,20 +467,55 @@ __device__ __forceinline__ void head_gradient(const HeadArgs& g, const HeadJob& 
 #pragma unroll
         for (int u = 0; u < 64; ++u) z[u] = v.tok == c0 + u ? own : z[u];
     }
-    for (int plane = 0;; ++plane) {
-        unsigned w[32];
+    if (kF32 && g.store_near) {
+        // two float16 planes, each column times its weights' power of two over the largest: those weights are smaller by as much
+        const float most = v.d_scale / *g.col_most, f0 = g.col_scale[c0 / kHeadGroup] * most,
+                    f1 = c0 + kHeadGroup < q.cols ? g.col_scale[c0 / kHeadGroup + 1] * most : 0.f;
 #pragma unroll
-        for (int u = 0; u < 32; ++u)
-            w[u] = !kF32 && g.half ? pack2(z[2 * u], z[2 * u + 1], __half()) : pack2(z[2 * u], z[2 * u + 1], __nv_bfloat16());
-        buf_free(lane);
-        buf_put(buf, lane, w);
-        buf_store<false>(buf, lane, &q.out, c0, v.row - lane, plane);
-        if (!kF32 || plane == kHeadPlanes - 1) break;
+        for (int plane = 0; plane < kHeadNear; ++plane) {
+            buf_free(lane);
 #pragma unroll
-        for (int u = 0; u < 32; ++u) {                       // what the plane has left over; exact
-            z[2 * u] -= __uint_as_float(w[u] << 16);
-            z[2 * u + 1] -= __uint_as_float(w[u] & 0xffff0000u);
+            for (int k = 0; k < 8; ++k) {
+                const Pair f(k < 4 ? f0 : f1);
+                unsigned w[4];
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    float a, b;
+                    (Pair(z[8 * k + 2 * u], z[8 * k + 2 * u + 1]) * f).split(a, b);
+                    w[u] = pack2(a, b, __half());
+                    if (plane) {
+                        const float2 h = __half22float2(*reinterpret_cast<const __half2*>(&w[u]));
+                        w[u] = pack2(a - h.x, b - h.y, __half());
+                    }
+                }
+                buf_put(buf, lane, k, make_uint4(w[0], w[1], w[2], w[3]));
+            }
+            buf_store<false>(buf, lane, &g.job[1].out, c0, v.row - lane, plane);
         }
+    }
+    if (kF32) {
+        if (!g.store_wide) return;
+#pragma unroll
+        for (int plane = 0; plane < kHeadWide; ++plane) {
+            buf_free(lane);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                unsigned w[4];
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    float &a = z[8 * k + 2 * u], &b = z[8 * k + 2 * u + 1];
+                    w[u] = pack2(a, b, __nv_bfloat16());
+                    a -= __uint_as_float(w[u] << 16);        // what the plane has left over; exact
+                    b -= __uint_as_float(w[u] & 0xffff0000u);
+                }
+                buf_put(buf, lane, k, make_uint4(w[0], w[1], w[2], w[3]));
+            }
+            buf_store<false>(buf, lane, &q.out, c0, v.row - lane, plane);
+        }
+    } else {
+        buf_free(lane);
+        if (q.half) buf_halves<__half>(buf, lane, z); else buf_halves<__nv_bfloat16>(buf, lane, z);
+        buf_store<false>(buf, lane, &q.out, c0, v.row - lane, 0);
     }
 }
 
@@ -459,11 +526,8 @@ __device__ __forceinline__ void head_weight(const HeadArgs& g, const HeadJob& q,
         if constexpr (sizeof(T) == 4) {
             buf_floats(q, buf, lane, z, c0, v.row - lane, 0, g.accumulate);
         } else {
-            unsigned w[32];
-#pragma unroll
-            for (int k = 0; k < 32; ++k) w[k] = pack2(z[2 * k], z[2 * k + 1], T());
             buf_free(lane);
-            buf_put(buf, lane, w);
+            buf_halves<T>(buf, lane, z);
             buf_store<false>(buf, lane, &q.out, c0, v.row - lane, 0);
         }
         return;
@@ -495,6 +559,11 @@ template <int KIND, bool kF32>
 __device__ __forceinline__ void head_take(const HeadArgs& g, const HeadJob& q, const HeadView& v, HeadStat& st, float (&z)[64], int c0, float unscale,
                                           unsigned char* buf, int lane) {
     if (c0 >= q.cols || v.row - lane >= q.rows) return;       // the same for all
+    if ((KIND == kHeadStats || KIND == kHeadGrad) && kF32 && g.row_scale) {
+        const float f0 = v.row_scale * g.col_scale[c0 / kHeadGroup], f1 = c0 + kHeadGroup < q.cols ? v.row_scale * g.col_scale[c0 / kHeadGroup + 1] : 0.f;
+#pragma unroll
+        for (int k = 0; k < 64; ++k) z[k] *= k < kHeadGroup ? f0 : f1;
+    }
     if (KIND == kHeadStats) {
         if (c0 + 64 > q.cols) {
 #pragma unroll
@@ -510,6 +579,11 @@ __device__ __forceinline__ void head_take(const HeadArgs& g, const HeadJob& q, c
     } else if (KIND == kHeadGrad) {
         if (g.entropy) head_gradient<true, kF32>(g, q, v, z, c0, buf, lane); else head_gradient<false, kF32>(g, q, v, z, c0, buf, lane);
     } else if (q.kind == kHeadHidden) {
+        if (kF32) {
+            const float f = *g.col_most;
+#pragma unroll
+            for (int k = 0; k < 64; ++k) z[k] *= f;
+        }
         buf_floats(q, buf, lane, z, c0, v.row - lane, v.x.split, g.add);
     } else {
 #pragma unroll
@@ -522,8 +596,8 @@ __device__ __forceinline__ void head_take(const HeadArgs& g, const HeadJob& q, c
 
 template <int CG, int KIND, bool PROMOTE>
 __device__ void head_epilogue(const HeadArgs& g, HeadShared& sh, unsigned char* area, int rank, int warp, int lane) {
-    constexpr int kCols = 64 * CG;                            // columns of a thread
-    const int right = warp >> 2;
+    constexpr int kParts = kHeadEpi / 4, kCols = 128 * CG / kParts, kTakes = kCols / 64;       // columns of a thread
+    const int part = warp >> 2;
     const float unscale = KIND == kHeadHidden && g.unscale ? *g.unscale : 1.f;
     unsigned char* buf = area + warp * kHeadBuf;
     int at = 0;
@@ -532,28 +606,38 @@ __device__ void head_epilogue(const HeadArgs& g, HeadShared& sh, unsigned char* 
     for (int i = 1; v.live; ++i) {
         const HeadView next = head_view<CG, KIND>(g, i, rank, warp, lane);        // its reads are under way meanwhile
         const HeadJob& q = g.job[v.j];
-        const int col = v.x.n * 128 * CG + right * kCols;
+        const int col = v.x.n * 128 * CG + part * kCols;
         HeadStat st;
         st.start();
-        float sum[PROMOTE ? CG : 1][64];                      // 64 columns of the tile each, where the parts of K are added up here
-        for (int c0 = v.x.chunk0; c0 < v.x.chunk1; c0 += g.promote, ++at) {
+        float sum[PROMOTE ? kTakes : 1][64];                      // 64 columns of the tile each, where the parts of K are added up here
+        for (int c0 = v.x.chunk0; c0 < v.x.chunk1; c0 += q.promote, ++at) {
             const int half = at & 1;
             const uint32_t bar = smem_u32(&sh.acc_full[half]), parity = (uint32_t)((at >> 1) & 1);
             if (ok) ok = __all_sync(0xffffffffu, CG == 2 ? mbar_wait_pair(bar, parity, &sh.fail) : mbar_wait(bar, parity, &sh.fail));
             if (!ok) sh.fail = 1;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            const uint32_t from = sh.tmem_base + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)(half * 128 * CG + right * kCols);
+            const uint32_t from = sh.tmem_base + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)(half * 128 * CG + part * kCols);
 #pragma unroll
-            for (int u = 0; u < CG; ++u) {
+            for (int u = 0; u < kTakes; ++u) {
                 float (&z)[64] = sum[PROMOTE ? u : 0];
+                if (PROMOTE) {
 #pragma unroll
-                for (int h = 0; h < 64; h += 32) {
-                    uint32_t r[32];
-                    tmem_ld32(from + u * 64 + h, r);
+                    for (int h = 0; h < 64; h += 16) {
+                        uint32_t r[16];
+                        tmem_ld16(from + u * 64 + h, r);
 #pragma unroll
-                    for (int k = 0; k < 32; ++k) z[h + k] = PROMOTE && c0 > v.x.chunk0 ? z[h + k] + __uint_as_float(r[k]) : __uint_as_float(r[k]);
+                        for (int k = 0; k < 16; ++k) z[h + k] = c0 > v.x.chunk0 ? z[h + k] + __uint_as_float(r[k]) : __uint_as_float(r[k]);
+                    }
+                } else {
+#pragma unroll
+                    for (int h = 0; h < 64; h += 32) {
+                        uint32_t r[32];
+                        tmem_ld32(from + u * 64 + h, r);
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) z[h + k] = __uint_as_float(r[k]);
+                    }
                 }
-                if (u + 1 == CG) {                            // all of it is in registers: the next product may have the accumulator
+                if (u + 1 == kTakes) {                            // all of it is in registers: the next product may have the accumulator
                     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                     __syncwarp();
                     if (lane == 0) {
@@ -570,15 +654,19 @@ __device__ void head_epilogue(const HeadArgs& g, HeadShared& sh, unsigned char* 
         }
         if (PROMOTE) {
 #pragma unroll
-            for (int u = 0; u < CG; ++u) head_take<KIND, PROMOTE>(g, q, v, st, sum[u], col + u * 64, unscale, buf, lane);
+            for (int u = 0; u < kTakes; ++u) head_take<KIND, PROMOTE>(g, q, v, st, sum[u], col + u * 64, unscale, buf, lane);
         }
         if (KIND == kHeadStats) {
-            // the two halves of the columns meet in shared memory, in one of two places by turns
-            float* meet = (float*)area + (i & 1) * 384 + (warp & 3) * 32 + lane;
-            if (right) { meet[0] = st.ref; meet[128] = st.sum; meet[256] = st.elog; }
-            asm volatile("bar.sync 1, %0;" ::"n"(32 * kHeadEpiWarps) : "memory");
-            if (!right && v.row < q.rows) {
-                st.join(meet[0], meet[128], meet[256]);
+            // the parts of the columns meet in shared memory, in one of two places by turns
+            float* meet = (float*)area + (i & 1) * (kParts - 1) * 384 + (warp & 3) * 32 + lane;
+            if (part) {
+                float* m = meet + (part - 1) * 384;
+                m[0] = st.ref; m[128] = st.sum; m[256] = st.elog;
+            }
+            asm volatile("bar.sync 1, %0;" ::"n"(128 * kParts) : "memory");
+            if (!part && v.row < q.rows) {
+#pragma unroll
+                for (int k = 0; k < kParts - 1; ++k) st.join(meet[k * 384], meet[k * 384 + 128], meet[k * 384 + 256]);
                 float* p = g.part + (long long)(g.part0 + v.x.n) * q.rows + v.row;
                 const long long plane = (long long)g.parts * q.rows;
                 p[0] = st.ref;
@@ -616,7 +704,7 @@ __global__ void __launch_bounds__(kHeadThreads, 1) head_kernel(const __grid_cons
         }
         for (int k = 0; k < 2; ++k) {
             asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(smem_u32(&sh.acc_full[k])) : "memory");
-            asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(&sh.acc_empty[k])), "r"(kHeadEpiWarps * CG) : "memory");
+            asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(&sh.acc_empty[k])), "r"(kHeadEpi * CG) : "memory");
         }
         sh.fail = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -626,9 +714,9 @@ __global__ void __launch_bounds__(kHeadThreads, 1) head_kernel(const __grid_cons
     if (CG == 2) cluster_sync();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     cudaGridDependencySynchronize();                          // all before this touches nothing that an earlier launch has
-    if (warp < kHeadEpiWarps) head_epilogue<CG, KIND, PROMOTE>(g, sh, smem + kHeadRing, rank, warp, lane);
-    else if (tid == 32 * kHeadEpiWarps) head_copies<CG>(g, smem, sh, rank);
-    else if (tid == 32 * (kHeadEpiWarps + 1) && rank == 0) head_products<CG>(g, smem, sh);
+    if (warp < kHeadEpi) head_epilogue<CG, KIND, PROMOTE>(g, sh, smem + kHeadRing, rank, warp, lane);
+    else if (tid == 32 * kHeadEpi) head_copies<CG>(g, smem, sh, rank);
+    else if (tid == 32 * (kHeadEpi + 1) && rank == 0) head_products<CG>(g, smem, sh);
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
     if (sh.fail) {
@@ -645,8 +733,8 @@ __global__ void __launch_bounds__(kHeadThreads, 1) head_kernel(const __grid_cons
 }
 
 // ------------------------------------------------------------------ around the products
-// Planes of a matrix whose rows the bulk copies cannot take as they are: three bfloat16 planes of float32, or a copy of 16-bit
-// rows at a stride of 16 bytes.  Columns behind dim are zero.  A value that bfloat16 has no finite number for stays in plane 0.
+// A copy of 16-bit rows at a stride of 16 bytes, where bulk copies cannot start on them; or three bfloat16 planes of float32 rows.  Columns behind dim
+// are zero.  A value that bfloat16 has no finite number for stays in plane 0.
 template <typename T>
 __global__ void __launch_bounds__(256) head_pack_kernel(const T* x, long long rows, int dim, long long ld, unsigned short* out, int ldp, long long plane) {
     const int pairs = ldp / 2;
@@ -661,9 +749,9 @@ __global__ void __launch_bounds__(256) head_pack_kernel(const T* x, long long ro
             const unsigned short* q = (const unsigned short*)p;
             *to = (c < dim ? (unsigned)q[0] : 0u) | (c + 1 < dim ? (unsigned)q[1] << 16 : 0u);
         } else {
-            float a = c < dim ? to_f32(p[0]) : 0.f, b = c + 1 < dim ? to_f32(p[1]) : 0.f;
+            float a = c < dim ? p[0] : 0.f, b = c + 1 < dim ? p[1] : 0.f;
 #pragma unroll
-            for (int k = 0; k < kHeadPlanes; ++k) {
+            for (int k = 0; k < kHeadWide; ++k) {
                 const unsigned w = pack2(a, b, __nv_bfloat16());
                 to[k * (plane / 2)] = w;
                 a -= __uint_as_float(w << 16);
@@ -673,6 +761,80 @@ __global__ void __launch_bounds__(256) head_pack_kernel(const T* x, long long ro
             }
         }
     }
+}
+
+// Two float16 planes of float32 rows, kGroup of them (a block) times a power of two that brings their largest finite number to between 2^14 and 2^15;
+// scale[block] takes that back, and the largest scale goes to *most.  A group of 32 rows has a warp for each, a row by itself all of them.  What the
+// first look has read stays in registers as far as they go (1024 columns of 32 rows; with every row read twice by eight warps 50021 x 1001 took 130 us,
+// since the blocks at work together held more than L2).
+constexpr int kNearThreads = 1024;
+template <int kGroup, bool kVector>
+__global__ void __launch_bounds__(kNearThreads) head_near_kernel(const float* x, long long rows, int dim, long long ld, unsigned short* out, int ldp,
+                                                                 long long plane, float* scale, int* most) {
+    __shared__ float tops[32];
+    constexpr int kHeld = 8, kStep = kGroup > 1 ? 128 : 4 * kNearThreads;
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, start = (kGroup > 1 ? lane : (int)threadIdx.x) * 4;
+    const long long r = (long long)blockIdx.x * kGroup + (kGroup > 1 ? warp : 0);
+    const bool live = r < rows;
+    const float* row = x + r * ld;
+    cudaGridDependencySynchronize();
+    auto four = [&](int c) {
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (!live) return v;
+        if (kVector) {
+            if (c < dim) v = *reinterpret_cast<const float4*>(row + c);
+        } else {
+            if (c < dim) v.x = row[c];
+            if (c + 1 < dim) v.y = row[c + 1];
+            if (c + 2 < dim) v.z = row[c + 2];
+            if (c + 3 < dim) v.w = row[c + 3];
+        }
+        return v;
+    };
+    float top = 0.f;
+    auto see = [&](const float4& v) {
+        if (fabsf(v.x) < INFINITY) top = fmaxf(top, fabsf(v.x));
+        if (fabsf(v.y) < INFINITY) top = fmaxf(top, fabsf(v.y));
+        if (fabsf(v.z) < INFINITY) top = fmaxf(top, fabsf(v.z));
+        if (fabsf(v.w) < INFINITY) top = fmaxf(top, fabsf(v.w));
+    };
+    float4 held[kHeld];
+#pragma unroll
+    for (int k = 0; k < kHeld; ++k) held[k] = four(start + k * kStep);
+#pragma unroll
+    for (int k = 0; k < kHeld; ++k) see(held[k]);
+    for (int c = start + kHeld * kStep; c < dim; c += kStep) see(four(c));
+#pragma unroll
+    for (int k = 16; k; k /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, k));
+    if (lane == 0) tops[warp] = top;
+    __syncthreads();
+    top = tops[lane];
+#pragma unroll
+    for (int k = 16; k; k /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, k));
+    int e = 15;
+    if (top > 0.f) frexpf(top, &e);
+    e = min(max(15 - e, -120), 120);
+    const float f = ldexpf(1.f, e);
+    if (threadIdx.x == 0) {
+        scale[blockIdx.x] = ldexpf(1.f, -e);
+        if (most) atomicMax(most, __float_as_int(ldexpf(1.f, -e)));     // of positive numbers
+    }
+    if (!live) return;
+    auto split = [&](int c, const float4& v) {
+        if (c >= ldp) return;                                // ldp is a multiple of 8
+        float a[4] = {v.x * f, v.y * f, v.z * f, v.w * f};
+        const uint2 w = make_uint2(pack2(a[0], a[1], __half()), pack2(a[2], a[3], __half()));
+        *reinterpret_cast<uint2*>(out + r * ldp + c) = w;
+        const float2 h = __half22float2(*reinterpret_cast<const __half2*>(&w.x)), i = __half22float2(*reinterpret_cast<const __half2*>(&w.y));
+        a[0] -= h.x; a[1] -= h.y; a[2] -= i.x; a[3] -= i.y;
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (!isfinite(a[k])) a[k] = 0.f;                 // what is not finite is in the first plane
+        *reinterpret_cast<uint2*>(out + plane + r * ldp + c) = make_uint2(pack2(a[0], a[1], __half()), pack2(a[2], a[3], __half()));
+    };
+#pragma unroll
+    for (int k = 0; k < kHeld; ++k) split(start + k * kStep, held[k]);
+    for (int c = start + kHeld * kStep; c < ldp; c += kStep) split(c, four(c));
 }
 
 // Row values from the parts' statistics: kHeadRowThreads threads for `width` rows, which share a row's parts.  The largest reference is
@@ -730,7 +892,8 @@ __global__ void __launch_bounds__(kHeadRowThreads) head_rows_kernel(const float*
 // Coefficients of d for every row, and the power of two that brings the largest to `top`: one block.
 __global__ void __launch_bounds__(1024) head_coef_kernel(int rows, long long vocab, const void* tokens, int token_bytes, double it, const float* lse,
                                                          const float* entropy, const float* g_logp, const float* g_entropy, const float* g_lse, float top,
-                                                         HeadRow* coef, int* row_token, float* unscale, int* status) {
+                                                         HeadRow* coef, int* row_token, float* unscale, float* d_scale, int* col_most,
+                                                         int pieces, int* status) {
     __shared__ float most[32];
     const int tid = threadIdx.x;
     cudaGridDependencySynchronize();
@@ -768,15 +931,24 @@ __global__ void __launch_bounds__(1024) head_coef_kernel(int rows, long long voc
     e = min(max(e - 1, -120), 120);
     const float f = ldexpf(1.f, e);
     for (int r = tid; r < rows; r += 1024) {
-        coef[r].a *= f; coef[r].c0 *= f; coef[r].c1 *= f;
+        HeadRow h = coef[r];
+        h.a *= f; h.c0 *= f; h.c1 *= f;
+        coef[r] = h;
+        if (d_scale) {                                        // brings the row's own largest to between 2^13 and 2^14
+            const float s = fabsf(h.a) + fabsf(h.c0) + fabsf(h.c1);
+            int own = 14;
+            if (s > 0.f && isfinite(s)) frexpf(s, &own);
+            d_scale[r] = ldexpf(1.f, min(max(14 - own, -100), 100));
+        }
     }
     if (tid == 0) *unscale = ldexpf(1.f, -e);
+    for (int k = tid; k < pieces; k += 1024) col_most[k] = 0;
 }
 
 // dhidden from the planes of partial sums, in the order of the planes.
 template <typename T>
 __global__ void __launch_bounds__(256) head_sum_kernel(const float* plane, long long plane_size, int planes, int ldp, int rows, int dim, const float* unscale,
-                                                       T* out, long long ldo) {
+                                                       const float* d_scale, T* out, long long ldo) {
     const int groups = ldp / 8;
     cudaGridDependencySynchronize();
     const float f = *unscale;
@@ -790,9 +962,10 @@ __global__ void __launch_bounds__(256) head_sum_kernel(const float* plane, long 
 #pragma unroll
             for (int u = 0; u < 8; ++u) s[u] += v[u];
         }
+        const float own = d_scale ? f / d_scale[r] : f;
 #pragma unroll
         for (int u = 0; u < 8; ++u)
-            if (c + u < dim) out[r * ldo + c + u] = from_f32<T>(s[u] * f);
+            if (c + u < dim) out[r * ldo + c + u] = from_f32<T>(s[u] * own);
     }
 }
 

@@ -45,13 +45,18 @@ def head_forward(hidden, weight, tokens, it):
 
 def head_logit_error(hidden, weight, it):
     """Bound on a logit's error, [rows, vocab].  With S the sum of the magnitudes of its terms: the tensor core adds 16 products
-    at a time to its accumulator, at most 96 times (six terms of a float32 product, 256 columns) before float32
-    registers take over, and each time drops less than 2^-22 of what it holds (bits behind the float32 accumulator's last, and of aligned
-    products); the small terms of a float32 product are 2^-8 of S or less, so that only 16 of the 96 count in full.
-    Adding the parts costs U of each, splitting a float32 operand in three 2^-25 and leaving out terms 3 * 2^-27; the scale
-    by a float32 inv_temperature 2 U."""
-    s = hidden.double().abs() @ weight.double().abs().T * it
-    return s * (20 * 2.0 ** -22 + (-(-hidden.shape[1] // 256) + 5) * U)
+    at a time to its accumulator and each time drops less than 2^-22 of what it holds (bits behind the float32 accumulator's last,
+    and of aligned products).  A float32 product is at most 48 such steps (three terms, 256 columns; the two small terms are 2^-10 of
+    S, so that 16 count in full) before float32 registers take over; 16-bit ones are summed through up to 4096 columns, 256
+    steps, or 2048: what it holds grows with the steps, so that half of them count.  Adding the parts costs U of each, a float32 operand in two
+    planes U of it, or 2^-39 of the largest among the 32 rows that share a scale (for hidden rows, of their own), the term left out U, the scale by a float32 inv_temperature 2 U."""
+    f32, n = hidden.dtype is torch.float32, hidden.shape[1]
+    h, w = hidden.double().abs(), weight.double().abs()
+    s = h @ w.T * it
+    if not f32:
+        return s * ((min(n, 4096) / 32 + 4) * 2.0 ** -22 + (-(-n // 2048) + 5) * U)
+    floor = 2.0 ** -38 * it * (h.amax(1)[:, None] * w.sum(1)[None] + h.sum(1)[:, None] * w.max())
+    return s * (20 * 2.0 ** -22 + (-(-n // 256) + 5) * U) + floor
 
 
 def head_forward_error(hidden, weight, tokens, it):
@@ -85,7 +90,7 @@ def head_backward(hidden, weight, tokens, it, lse, entropy=None, g_logp=None, g_
 
 def head_backward_error(hidden, weight, tokens, it, lse, entropy, g_logp, g_entropy, g_lse, half, store):
     """Bounds for dhidden and dweight (before what an accumulated dweight adds).  `half`: the relative rounding of d, which is held
-    in the operands' type (0 stands for float32's three planes, 2^-25); float16 also has a smallest number, 2^-25 of a scale at which
+    in the operands' type (0 stands for float32's planes, 2^-24); float16 also has a smallest number, 2^-25 of a scale at which
     the largest coefficient of d is 2^13 or more.  `store`: the rounding of the outputs."""
     d, dh, dw, lp = head_backward(hidden, weight, tokens, it, lse, entropy, g_logp, g_entropy, g_lse)
     zero = torch.zeros_like(lse, dtype=torch.float64)
@@ -94,13 +99,15 @@ def head_backward_error(hidden, weight, tokens, it, lse, entropy, g_logp, g_entr
     h = zero if entropy is None else entropy.double().abs()
     size = (a + gz + ge * h)[:, None] + ge[:, None] * lp.abs()      # |d| / p, and what its sum is made of
     off = head_logit_error(hidden, weight, it) + 4 * U * (lp.abs() + (lp + lse.double()[:, None]).abs() + lse.double().abs()[:, None]) + 2.0 ** -21
-    ed = d.abs() * (half or 2.0 ** -25) + lp.exp() * (size + ge[:, None]) * off + 8 * U * lp.exp() * size
+    ed = d.abs() * (half or U) + lp.exp() * (size + ge[:, None]) * off + 8 * U * lp.exp() * size
     if half == 2.0 ** -11:
         ed += 2.0 ** -38 * 2 * (a * 2 + gz + ge * h + ge).max()
     w, x = weight.double().abs(), hidden.double().abs()
     # the products' own sums: 16 products at a time, over the whole length for 16-bit operands
     long = lambda n: (n / 16 + 1) * 2.0 ** -22 if half else 20 * 2.0 ** -22 + (n / 256 + 5) * U      # noqa: E731
-    eh = ed @ w + (d.abs() @ w) * (long(weight.shape[0]) + 8 * U) + store * dh.abs()
+    # float32: dhidden's planes of d hold 2^-25 of a scale at which the row's largest coefficient is 2^13 or more, and the largest weight 2^14
+    floor = 0 if half else 2.0 ** -37 * weight.shape[0] * w.max() * (2 * a + gz + ge * h + ge)[:, None]
+    eh = floor + ed @ w + (d.abs() @ w) * (long(weight.shape[0]) + 8 * U) + store * dh.abs()
     ew = ed.T @ x + (d.abs().T @ x) * (long(hidden.shape[0]) + 4 * U) + store * dw.abs()
     return eh, ew
 

@@ -26,7 +26,7 @@ constexpr int64_t kHeadStatRows = 8192;         // rows whose statistics are hel
 // Chunks of K that the tensor core adds up by itself.  It does not round to nearest, so its sums drift towards zero, with every step that it adds at full
 // size (four of a chunk; of float32 operands twelve or 24): log probabilities of normal logits are off by 6e-8 of themselves after 16 steps, 2e-7 after 64, 8e-7
 // after 256, 1.7e-6 after 512.
-constexpr int kHeadPromoteNear = 2, kHeadPromoteWide = 1;       // float32 operands: 24 steps
+constexpr int kHeadPromoteNear = 4, kHeadPromoteWide = 2;       // float32 operands: 48 steps
 constexpr int kHeadPromoteLong = 32;            // 16-bit ones of more than kHeadLong chunks in the forward: 4096 x 131072 x 4096 takes 3.40 ms
 constexpr int kHeadLong = 64;                   // without, 3.51 with 16 chunks, 4.10 with 4
 constexpr int kHeadNever = 1 << 28;
@@ -222,7 +222,7 @@ cudaError_t pack(int dtype, const void* x, int64_t rows, int64_t dim, int64_t ld
 template <int kGroup>
 cudaError_t pack_near(const float* x, int64_t rows, int64_t dim, int64_t ld, unsigned short* out, int64_t ldp, float* scale, int* most, cudaStream_t s) {
     auto kernel = aligned(x, 16) && (ld % 4 == 0 || rows == 1) && dim % 4 == 0 ? head_near_kernel<kGroup, true> : head_near_kernel<kGroup, false>;
-    return launch_after(kernel, dim3((unsigned)((rows + kGroup - 1) / kGroup)), kNearThreads, s, x, (long long)rows, (int)dim, (long long)ld, out, (int)ldp,
+    return launch_after(kernel, dim3((unsigned)((rows + kGroup - 1) / kGroup)), kNearThreads<kGroup>, s, x, (long long)rows, (int)dim, (long long)ld, out, (int)ldp,
                         (long long)(rows * ldp), scale, most);
 }
 // What a call's products read of the hidden states and of a piece of the weights, packed where it has to be.

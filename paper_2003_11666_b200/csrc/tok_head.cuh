@@ -23,9 +23,10 @@
 // counts (the logits; dhidden, a sum over tokens), two float16 planes do: x = 2^k (x0 + x1) to 2^-24 of x or 2^-39 of the largest number
 // that shares k (a row of hidden states, 32 rows of the weights, a row of d), and x0 y0 + x0 y1 + x1 y0 leaves out 2^-24.  A row of
 // dweight is a token's own, however improbable, so its product keeps float32's range: three bfloat16 planes (x0 + x1 + x2 to 2^-25)
-// and the six terms x_i y_j with i + j <= 2.  (Six terms everywhere: 509 x 50021 x 1001 forward 360 us, and backward 1000.)
+// and the six terms x_i y_j with i + j <= 2.  (Six terms everywhere: 509 x 50021 x 1001
+// forward 360 us, and x 1000 backward 1000.)
 // The tensor core adds to its float32 accumulator without rounding to nearest, so a long K drifts:
-// float32 products, and the logits of the forward, leave the tensor core every few chunks and are
+// float32 products, and long rows' logits in the forward, leave the tensor core every few chunks and are
 // added up in registers.
 // Every wait is bounded (see mbar_wait); a block whose wait runs out reports it and gives NaN for its tiles.
 #pragma once
@@ -604,12 +605,19 @@ __device__ void head_epilogue(const HeadArgs& g, HeadShared& sh, unsigned char* 
     bool ok = true;
     HeadView v = head_view<CG, KIND>(g, 0, rank, warp, lane);
     for (int i = 1; v.live; ++i) {
-        const HeadView next = head_view<CG, KIND>(g, i, rank, warp, lane);        // its reads are under way meanwhile
+        HeadView next;
+        if (!PROMOTE) next = head_view<CG, KIND>(g, i, rank, warp, lane);         // its reads are under way meanwhile
         const HeadJob& q = g.job[v.j];
         const int col = v.x.n * 128 * CG + part * kCols;
         HeadStat st;
         st.start();
-        float sum[PROMOTE ? kTakes : 1][64];                      // 64 columns of the tile each, where the parts of K are added up here
+        float sum[PROMOTE ? kTakes : 1][64];                  // 64 columns of the tile each, where the parts of K are added up here
+        if (PROMOTE) {
+#pragma unroll
+            for (int u = 0; u < kTakes; ++u)
+#pragma unroll
+                for (int k = 0; k < 64; ++k) sum[u][k] = 0.f;
+        }
         for (int c0 = v.x.chunk0; c0 < v.x.chunk1; c0 += q.promote, ++at) {
             const int half = at & 1;
             const uint32_t bar = smem_u32(&sh.acc_full[half]), parity = (uint32_t)((at >> 1) & 1);
@@ -626,7 +634,7 @@ __device__ void head_epilogue(const HeadArgs& g, HeadShared& sh, unsigned char* 
                         uint32_t r[16];
                         tmem_ld16(from + u * 64 + h, r);
 #pragma unroll
-                        for (int k = 0; k < 16; ++k) z[h + k] = c0 > v.x.chunk0 ? z[h + k] + __uint_as_float(r[k]) : __uint_as_float(r[k]);
+                        for (int k = 0; k < 16; ++k) z[h + k] += __uint_as_float(r[k]);
                     }
                 } else {
 #pragma unroll
@@ -674,7 +682,7 @@ __device__ void head_epilogue(const HeadArgs& g, HeadShared& sh, unsigned char* 
                 if (g.entropy) p[2 * plane] = st.elog;
             }
         }
-        v = next;
+        v = PROMOTE ? head_view<CG, KIND>(g, i, rank, warp, lane) : next;         // the sums leave no registers for it any earlier
     }
     if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");       // what this warp has stored is there
 }
@@ -767,12 +775,12 @@ __global__ void __launch_bounds__(256) head_pack_kernel(const T* x, long long ro
 // scale[block] takes that back, and the largest scale goes to *most.  A group of 32 rows has a warp for each, a row by itself all of them.  What the
 // first look has read stays in registers as far as they go (1024 columns of 32 rows; with every row read twice by eight warps 50021 x 1001 took 130 us,
 // since the blocks at work together held more than L2).
-constexpr int kNearThreads = 1024;
+template <int kGroup> constexpr int kNearThreads = kGroup > 1 ? 32 * kGroup : 256;
 template <int kGroup, bool kVector>
-__global__ void __launch_bounds__(kNearThreads) head_near_kernel(const float* x, long long rows, int dim, long long ld, unsigned short* out, int ldp,
+__global__ void __launch_bounds__(kNearThreads<kGroup>) head_near_kernel(const float* x, long long rows, int dim, long long ld, unsigned short* out, int ldp,
                                                                  long long plane, float* scale, int* most) {
     __shared__ float tops[32];
-    constexpr int kHeld = 8, kStep = kGroup > 1 ? 128 : 4 * kNearThreads;
+    constexpr int kHeld = 8, kWarps = kNearThreads<kGroup> / 32, kStep = kGroup > 1 ? 128 : 128 * kWarps;
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, start = (kGroup > 1 ? lane : (int)threadIdx.x) * 4;
     const long long r = (long long)blockIdx.x * kGroup + (kGroup > 1 ? warp : 0);
     const bool live = r < rows;
@@ -808,9 +816,9 @@ __global__ void __launch_bounds__(kNearThreads) head_near_kernel(const float* x,
     for (int k = 16; k; k /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, k));
     if (lane == 0) tops[warp] = top;
     __syncthreads();
-    top = tops[lane];
+    top = tops[lane % kWarps];
 #pragma unroll
-    for (int k = 16; k; k /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, k));
+    for (int k = kWarps / 2; k; k /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, k));
     int e = 15;
     if (top > 0.f) frexpf(top, &e);
     e = min(max(15 - e, -120), 120);

@@ -46,9 +46,9 @@ def head_forward(hidden, weight, tokens, it):
 def head_logit_error(hidden, weight, it):
     """Bound on a logit's error, [rows, vocab].  With S the sum of the magnitudes of its terms: the tensor core adds 16 products
     at a time to its accumulator and each time drops less than 2^-22 of what it holds (bits behind the float32 accumulator's last,
-    and of aligned products).  A float32 product is at most 48 such steps (three terms, 256 columns; the two small terms are 2^-10 of
-    S, so that 16 count in full) before float32 registers take over; 16-bit ones are summed through up to 4096 columns, 256
-    steps, or 2048: what it holds grows with the steps, so that half of them count.  Adding the parts costs U of each, a float32 operand in two
+    and of aligned products).  A float32 product is at most 48 such steps (three terms of 256 columns, or six of 128) before float32
+    registers take over; 16-bit ones are summed through up to 4096 columns, 256 steps, or 2048.  What it holds grows with the steps, so
+    that half of them count, and four more for the products' own alignment.  Adding the parts costs U of each, a float32 operand in two
     planes U of it, or 2^-39 of the largest among the 32 rows that share a scale (for hidden rows, of their own), the term left out U, the scale by a float32 inv_temperature 2 U."""
     f32, n = hidden.dtype is torch.float32, hidden.shape[1]
     h, w = hidden.double().abs(), weight.double().abs()
@@ -56,7 +56,7 @@ def head_logit_error(hidden, weight, it):
     if not f32:
         return s * ((min(n, 4096) / 32 + 4) * 2.0 ** -22 + (-(-n // 2048) + 5) * U)
     floor = 2.0 ** -38 * it * (h.amax(1)[:, None] * w.sum(1)[None] + h.sum(1)[:, None] * w.max())
-    return s * (20 * 2.0 ** -22 + (-(-n // 256) + 5) * U) + floor
+    return s * (28 * 2.0 ** -22 + (-(-n // 256) + 5) * U) + floor
 
 
 def head_forward_error(hidden, weight, tokens, it):
@@ -104,7 +104,7 @@ def head_backward_error(hidden, weight, tokens, it, lse, entropy, g_logp, g_entr
         ed += 2.0 ** -38 * 2 * (a * 2 + gz + ge * h + ge).max()
     w, x = weight.double().abs(), hidden.double().abs()
     # the products' own sums: 16 products at a time, over the whole length for 16-bit operands
-    long = lambda n: (n / 16 + 1) * 2.0 ** -22 if half else 20 * 2.0 ** -22 + (n / 256 + 5) * U      # noqa: E731
+    long = lambda n: (n / 16 + 1) * 2.0 ** -22 if half else 28 * 2.0 ** -22 + (n / 128 + 5) * U      # noqa: E731
     # float32: dhidden's planes of d hold 2^-25 of a scale at which the row's largest coefficient is 2^13 or more, and the largest weight 2^14
     floor = 0 if half else 2.0 ** -37 * weight.shape[0] * w.max() * (2 * a + gz + ge * h + ge)[:, None]
     eh = floor + ed @ w + (d.abs() @ w) * (long(weight.shape[0]) + 8 * U) + store * dh.abs()

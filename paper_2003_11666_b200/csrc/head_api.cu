@@ -27,8 +27,8 @@ constexpr int64_t kHeadStatRows = 8192;         // rows whose statistics are hel
 // size (four of a chunk; of float32 operands twelve or 24): log probabilities of normal logits are off by 6e-8 of themselves after 16 steps, 2e-7 after 64, 8e-7
 // after 256, 1.7e-6 after 512.
 constexpr int kHeadPromoteNear = 4, kHeadPromoteWide = 2;       // float32 operands: 48 steps
-constexpr int kHeadPromoteLong = 32;            // 16-bit ones of more than kHeadLong chunks in the forward: 4096 x 131072 x 4096 takes 3.40 ms
-constexpr int kHeadLong = 64;                   // without, 3.51 with 16 chunks, 4.10 with 4
+constexpr int kHeadPromoteLong = 16;            // 16-bit ones of more than kHeadLong chunks in the forward: 4096 x 131072 x 4096 takes 3.50 ms, as it
+constexpr int kHeadLong = 16;                   // does without
 constexpr int kHeadNever = 1 << 28;
 constexpr int kHeadTileCost = 2;                // what a tile costs beside its chunks, in chunks
 

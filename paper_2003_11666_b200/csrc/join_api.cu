@@ -57,7 +57,7 @@ struct JoinPlan {
 };
 JoinPlan join_plan(int64_t rows, int64_t dim, int64_t rows_per_gate, char* scratch) {
     JoinPlan e{};
-    e.lanes = join_lanes(dim, 4096, e.units);
+    e.lanes = join_lanes(dim, 8192, e.units);
     e.threads = join_threads(e.lanes);
     e.slots = e.threads / e.lanes;
     e.rows_per_gate = rows_per_gate > 0 ? std::min(rows_per_gate, rows) : rows;
@@ -224,7 +224,7 @@ int pb_join_forward(const pb_join_args* args, void* stream) {
                         piece_ok(a.post_weight, 0, 1, a.weight_dtype) && piece_ok(a.pre_weight, 0, 1, a.weight_dtype);
     const int64_t slots = threads / lanes;
     bool ring = false;
-    if (pieces && units == 2 && slots == 1 && a.dim == 16 * lanes) {
+    if (pieces && units == 2 && slots == 1) {
         p.row_bytes = (int)((a.dim * (ss + (a.gate ? 2 : 1) * es) + 127) / 128 * 128);
         p.depth = ring_depth(p.row_bytes, std::max(1, 512 / threads));
         // A plain sum with one norm is as fast as memory without (16384 x 4096: 84 us, 99 in the ring; with a norm behind the block 95 and 86, with
@@ -236,7 +236,11 @@ int pb_join_forward(const pb_join_args* args, void* stream) {
         using T = decltype(t);
         using S = decltype(st);
         if (ring) {
-            auto kernel = threads <= 256 ? join_forward_ring_kernel<T, S, 256> : threads <= 512 ? join_forward_ring_kernel<T, S, 512> : join_forward_ring_kernel<T, S, 1024>;
+            auto in_ring = [&](auto l) {
+                constexpr int L = decltype(l)::value;
+                return threads <= 256 ? join_forward_ring_kernel<T, S, L, 256> : threads <= 512 ? join_forward_ring_kernel<T, S, L, 512> : join_forward_ring_kernel<T, S, L, 1024>;
+            };
+            auto kernel = a.dim == 16 * lanes ? in_ring(Layout<kFull>()) : in_ring(Layout<kEven>());
             const int64_t blocks = std::min(a.rows, kSms * std::max<int64_t>(1, 512 / threads));
             return launch_ring(kernel, (int)blocks, threads, p.depth * p.row_bytes, (cudaStream_t)stream, p);
         }
@@ -316,7 +320,7 @@ int pb_join_backward(const pb_join_args* args, const pb_join_grads* grads, void*
                         piece_ok(a.post_weight, 0, 1, a.weight_dtype) && piece_ok(a.pre_weight, 0, 1, a.weight_dtype);
     size_t shared = e.slots > 1 ? (size_t)e.threads * 8 * e.units * 4 : 0;
     bool ring = false;
-    if (pieces && e.slots == 1 && a.dim == 8 * e.units * e.lanes) {
+    if (pieces && e.slots == 1) {
         p.row_bytes = (int)((a.dim * (2 * ss + 3 * es) + 127) / 128 * 128);
         p.depth = ring_depth(p.row_bytes, std::max(1, 512 / e.threads));
         ring = p.depth > 1;
@@ -328,15 +332,17 @@ int pb_join_backward(const pb_join_args* args, const pb_join_grads* grads, void*
         auto by_layout = [&](auto l) {
             constexpr int L = decltype(l)::value;
             if (e.threads <= 256) return join_backward_kernel<T, S, L, 1, 256>;
-            if (e.units == 1) return join_backward_kernel<T, S, L, 1, 512>;
-            return e.threads <= 512 ? join_backward_kernel<T, S, L, 2, 512> : join_backward_kernel<T, S, L, 2, 1024>;
+            if (e.threads <= 512) return join_backward_kernel<T, S, L, 1, 512>;
+            return e.units == 1 ? join_backward_kernel<T, S, L, 1, 1024> : join_backward_kernel<T, S, L, 2, 1024>;
         };
-        auto in_ring = [&]() {
-            if (e.threads <= 256) return join_backward_ring_kernel<T, S, 1, 256>;
-            if (e.units == 1) return join_backward_ring_kernel<T, S, 1, 512>;
-            return e.threads <= 512 ? join_backward_ring_kernel<T, S, 2, 512> : join_backward_ring_kernel<T, S, 2, 1024>;
+        auto in_ring = [&](auto l) {
+            constexpr int L = decltype(l)::value;
+            if (e.threads <= 256) return join_backward_ring_kernel<T, S, L, 1, 256>;
+            if (e.threads <= 512) return join_backward_ring_kernel<T, S, L, 1, 512>;
+            return e.units == 1 ? join_backward_ring_kernel<T, S, L, 1, 1024> : join_backward_ring_kernel<T, S, L, 2, 1024>;
         };
-        auto kernel = ring ? in_ring() : pieces ? by_layout(Layout<kEven>()) : by_layout(Layout<kOdd>());
+        auto kernel = ring ? (a.dim == 8 * e.units * e.lanes ? in_ring(Layout<kFull>()) : in_ring(Layout<kEven>())) : pieces ? by_layout(Layout<kEven>())
+                                                                                                                       : by_layout(Layout<kOdd>());
         const int blocks = ring ? std::min(e.blocks, kSms * std::max(1, 512 / e.threads)) : e.blocks;      // what is resident
         cudaError_t err = launch_ring(kernel, blocks, e.threads, shared, s, p);
         const int first = p.part_pre || p.part_post ? 0 : 2;

@@ -546,10 +546,17 @@ __device__ __forceinline__ void head_weight(const HeadArgs& g, const HeadJob& q,
         __syncwarp();
         if (c0 + h + lane < q.cols) {
             T* p = to + h;
-#pragma unroll 8
-            for (int r = 0; r < rows; ++r, p += g.ldo) {
-                const float s = f[r * 32 + (lane ^ r)];
-                *p = from_f32<T>(g.accumulate ? s + to_f32(*p) : s);
+            for (int r = 0; r < rows; r += 8, p += 8 * g.ldo) {
+                T old[8];                                    // all of them under way before the first is written
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (g.accumulate && r + k < rows) old[k] = p[k * g.ldo];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    if (r + k >= rows) break;
+                    const float s = f[(r + k) * 32 + (lane ^ (r + k))];
+                    p[k * g.ldo] = from_f32<T>(g.accumulate ? s + to_f32(old[k]) : s);
+                }
             }
         }
     }
@@ -811,6 +818,7 @@ __global__ void __launch_bounds__(kNearThreads<kGroup>) head_near_kernel(const f
     for (int k = 0; k < kHeld; ++k) held[k] = four(start + k * kStep);
 #pragma unroll
     for (int k = 0; k < kHeld; ++k) see(held[k]);
+#pragma unroll 8
     for (int c = start + kHeld * kStep; c < dim; c += kStep) see(four(c));
 #pragma unroll
     for (int k = 16; k; k /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, k));
@@ -842,6 +850,7 @@ __global__ void __launch_bounds__(kNearThreads<kGroup>) head_near_kernel(const f
     };
 #pragma unroll
     for (int k = 0; k < kHeld; ++k) split(start + k * kStep, held[k]);
+#pragma unroll 8
     for (int c = start + kHeld * kStep; c < ldp; c += kStep) split(c, four(c));
 }
 

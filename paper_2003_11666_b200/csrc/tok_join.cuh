@@ -265,10 +265,11 @@ __device__ __forceinline__ void ring_late() {
     for (int k = 0; k < 512; ++k) __nanosleep(200);
 }
 
-// How a thread's eight columns lie: kOdd: `lanes` apart, so that neighbours read neighbours; kEven: consecutive; kFull: consecutive, every
-// thread has all of its own, and a block works on one row after the other, which bulk copies bring into a ring of rows in shared memory.
+// How a thread's eight columns lie: kOdd: `lanes` apart, so that neighbours read neighbours; kEven: consecutive; kFull: consecutive, and every thread has
+// all of its own (what else asks at each access whether they exist: 7 % of the time of 8192 rows of 4096).
 enum JoinLayout { kOdd = 0, kEven = 1, kFull = 2 };
 
+// Rows that a block takes one after the other come by bulk copies into a ring in shared memory.
 constexpr int kJoinRing = 4;                  // rows on their way at most
 struct JoinRing {
     uint64_t full[kJoinRing];
@@ -304,10 +305,8 @@ struct Columns {
         n = kLayout == kFull ? 8 : first >= dim || !live ? 0 : kPieces ? 8 : min(8, (dim - first + step - 1) / step);
     }
     template <typename T> __device__ __forceinline__ void load(RawColumns<T, kPieces>& v, const T* row) const {
-        if constexpr (kLayout == kFull) {
-            v.load(row + first);
-        } else if constexpr (kPieces) {
-            if (n) v.load(row + first); else v.zero();
+        if constexpr (kPieces) {
+            if (kLayout == kFull || n) v.load(row + first); else v.zero();
         } else {
 #pragma unroll
             for (int k = 0; k < 8; ++k) v.v[k] = k < n ? row[first + k * step] : from_f32<T>(0.f);
@@ -316,6 +315,11 @@ struct Columns {
     template <typename T> __device__ __forceinline__ Eight get(const T* row) const {
         RawColumns<T, kPieces> v;
         load(v, row);
+        return v.get();
+    }
+    template <typename T> __device__ __forceinline__ Eight get_shared(const void* row) const {
+        RawEight<T> v;
+        if (kLayout == kFull || n) v.load_shared((const T*)row + first); else v.zero();
         return v.get();
     }
     template <typename T> __device__ __forceinline__ Eight weight(const void* w, bool f32) const {
@@ -402,7 +406,7 @@ __global__ void __launch_bounds__(kJoinMaxLanes) join_forward_kernel(const JoinP
 }
 
 // Rows that a block takes one after the other, 16 columns per thread: their parts come by bulk copies some rows ahead, and the weights stay in registers.
-template <typename T, typename S, int kThreads>
+template <typename T, typename S, int kLayout, int kThreads>
 __global__ void __launch_bounds__(kThreads, kThreads <= 256 ? 512 / kThreads : 1) join_forward_ring_kernel(const JoinParams p) {
     extern __shared__ __align__(128) unsigned char store[];
     __shared__ float sm[2][2][32];
@@ -427,7 +431,7 @@ __global__ void __launch_bounds__(kThreads, kThreads <= 256 ? 512 / kThreads : 1
     Eight post[kUnits], pre[kUnits];
 #pragma unroll
     for (int k = 0; k < kUnits; ++k) {
-        const Columns<kFull> c(lane, k, blockDim.x, p.dim);
+        const Columns<kLayout> c(lane, k, blockDim.x, p.dim);
         if (p.post) post[k] = c.template weight<T>(p.post, p.weights_f32);
         if (p.h) pre[k] = c.template weight<T>(p.pre, p.weights_f32);
     }
@@ -441,17 +445,10 @@ __global__ void __launch_bounds__(kThreads, kThreads <= 256 ? 512 / kThreads : 1
         float sum = 0.f;
 #pragma unroll
         for (int k = 0; k < kUnits; ++k) {
-            const Columns<kFull> c(lane, k, blockDim.x, p.dim);
-            RawEight<S> x;
-            RawEight<T> u;
-            x.load_shared((const S*)from + c.first);
-            u.load_shared((const T*)(from + s_bytes) + c.first);
-            y[k] = x.get();
-            b[k] = u.get();
-            if (p.gate) {
-                u.load_shared((const T*)(from + s_bytes + t_bytes) + c.first);
-                gate[k] = u.get();
-            }
+            const Columns<kLayout> c(lane, k, blockDim.x, p.dim);
+            y[k] = c.template get_shared<S>(from);
+            b[k] = c.template get_shared<T>(from + s_bytes);
+            if (p.gate) gate[k] = c.template get_shared<T>(from + s_bytes + t_bytes);
             if (p.post) sum += dot8(b[k], b[k]);
         }
         if (!ok) y[0].fill(__int_as_float(0x7fffffff));       // a copy never came: the row is NaN
@@ -468,7 +465,7 @@ __global__ void __launch_bounds__(kThreads, kThreads <= 256 ? 512 / kThreads : 1
         sum = 0.f;
 #pragma unroll
         for (int k = 0; k < kUnits; ++k) {
-            const Columns<kFull> c(lane, k, blockDim.x, p.dim);
+            const Columns<kLayout> c(lane, k, blockDim.x, p.dim);
             b[k] = b[k] * scale;
             if (p.post) b[k] = b[k] * post[k];
             if (p.gate) b[k] = b[k] * gate[k];
@@ -481,7 +478,7 @@ __global__ void __launch_bounds__(kThreads, kThreads <= 256 ? 512 / kThreads : 1
         rstd = root_of(fmaf(row_sum(sum, blockDim.x, sm[turn][1]), p.inv_dim, p.eps));
         if (lane == 0 && p.rstd_pre) p.rstd_pre[r] = rstd;
 #pragma unroll
-        for (int k = 0; k < kUnits; ++k) Columns<kFull>(lane, k, blockDim.x, p.dim).put((T*)p.h + r * p.ld_h, y[k] * rstd * pre[k]);
+        for (int k = 0; k < kUnits; ++k) Columns<kLayout>(lane, k, blockDim.x, p.dim).put((T*)p.h + r * p.ld_h, y[k] * rstd * pre[k]);
     }
     if (!ok) ring_late();
 }
@@ -604,9 +601,9 @@ __global__ void __launch_bounds__(kThreads, kThreads <= 256 ? 3 : 1) join_backwa
     }
 }
 
-// Rows that a block takes one after the other, eight columns per thread (16 in rows of more than 4096): their parts come by bulk copies some rows
+// Rows that a block takes one after the other, eight columns per thread (16 in rows of more than 8192): their parts come by bulk copies some rows
 // ahead.
-template <typename T, typename S, int kUnits, int kThreads>
+template <typename T, typename S, int kLayout, int kUnits, int kThreads>
 __global__ void __launch_bounds__(kThreads, kThreads <= 256 ? 512 / kThreads : 1) join_backward_ring_kernel(const JoinParams p) {
     extern __shared__ __align__(128) unsigned char store[];
     __shared__ float sm[2][3][32];
@@ -660,7 +657,7 @@ __global__ void __launch_bounds__(kThreads, kThreads <= 256 ? 512 / kThreads : 1
     for (int k = 0; k < kUnits; ++k) {
         dpre[k].fill(0.f); dpost[k].fill(0.f); both[k].fill(0.f);
         if (kKept) {
-            const Columns<kFull> c(lane, k, blockDim.x, p.dim);
+            const Columns<kLayout> c(lane, k, blockDim.x, p.dim);
             if (p.post) post[k] = c.template weight<T>(p.post, p.weights_f32);
             if (p.dh) pre[k] = c.template weight<T>(p.pre, p.weights_f32);
         }
@@ -681,26 +678,13 @@ __global__ void __launch_bounds__(kThreads, kThreads <= 256 ? 512 / kThreads : 1
             float s1 = 0.f, s2 = 0.f, s3 = 0.f;
 #pragma unroll
             for (int k = 0; k < kUnits; ++k) {
-                const Columns<kFull> c(lane, k, blockDim.x, p.dim);
-                RawEight<T> t;
-                RawEight<S> s;
-                t.load_shared((const T*)from + c.first);
-                un[k] = t.get() * rp;
-                if (p.gate) {
-                    t.load_shared((const T*)(from + t_bytes) + c.first);
-                    gate[k] = t.get();
-                }
-                if (p.dy) {
-                    s.load_shared((const S*)(from + 3 * t_bytes + s_bytes) + c.first);
-                    g[k] = s.get();
-                } else {
-                    g[k].fill(0.f);
-                }
+                const Columns<kLayout> c(lane, k, blockDim.x, p.dim);
+                un[k] = c.template get_shared<T>(from) * rp;
+                if (p.gate) gate[k] = c.template get_shared<T>(from + t_bytes);
+                if (p.dy) g[k] = c.template get_shared<S>(from + 3 * t_bytes + s_bytes); else g[k].fill(0.f);
                 if (p.dh) {
-                    t.load_shared((const T*)(from + 2 * t_bytes) + c.first);
-                    s.load_shared((const S*)(from + 3 * t_bytes) + c.first);
-                    const Eight dh = t.get(), w = dh * (kKept ? pre[k] : c.template weight<T>(p.pre, p.weights_f32));
-                    yn[k] = s.get() * rr;
+                    const Eight dh = c.template get_shared<T>(from + 2 * t_bytes), w = dh * (kKept ? pre[k] : c.template weight<T>(p.pre, p.weights_f32));
+                    yn[k] = c.template get_shared<S>(from + 3 * t_bytes) * rr;
                     dpre[k] = fma8(dh, yn[k], dpre[k]);
                     s1 += dot8(w, yn[k]);
                     g[k] = fma8(rr, w, g[k]);
@@ -721,7 +705,7 @@ __global__ void __launch_bounds__(kThreads, kThreads <= 256 ? 512 / kThreads : 1
             if (++get == p.depth) { get = 0; phase ^= 1; }
 #pragma unroll
             for (int k = 0; k < kUnits; ++k) {
-                const Columns<kFull> c(lane, k, blockDim.x, p.dim);
+                const Columns<kLayout> c(lane, k, blockDim.x, p.dim);
                 if (p.dh) g[k] = fma8(m1, yn[k], g[k]);
                 if (p.dx) c.put((S*)p.dx + r * p.ld_dx, g[k] * p.rs);
                 if (p.keep.drop) g[k] = g[k] * keep[k];
@@ -734,7 +718,7 @@ __global__ void __launch_bounds__(kThreads, kThreads <= 256 ? 512 / kThreads : 1
         if (p.gate) {
 #pragma unroll
             for (int k = 0; k < kUnits; ++k) {
-                const Columns<kFull> c(lane, k, blockDim.x, p.dim);
+                const Columns<kLayout> c(lane, k, blockDim.x, p.dim);
                 if (p.post) dpost[k] = fma8(c.get((const T*)p.gate + now.group * p.ld_gate), both[k], dpost[k]);
                 if (p.dgate) {
                     const Eight d = p.post ? both[k] * (kKept ? post[k] : c.template weight<T>(p.post, p.weights_f32)) : both[k];
@@ -749,7 +733,7 @@ __global__ void __launch_bounds__(kThreads, kThreads <= 256 ? 512 / kThreads : 1
     if (!ok) ring_late();
 #pragma unroll
     for (int k = 0; k < kUnits; ++k) {
-        const Columns<kFull> c(lane, k, blockDim.x, p.dim);
+        const Columns<kLayout> c(lane, k, blockDim.x, p.dim);
         if (p.part_pre) c.put(p.part_pre + (long long)blockIdx.x * p.dim, dpre[k]);
         if (p.part_post) c.put(p.part_post + (long long)blockIdx.x * p.dim, p.gate ? dpost[k] : both[k]);
     }

@@ -382,9 +382,10 @@ int pb_logprob_backward(const void* dev_logits, int dtype, int64_t rows, int64_t
  * of logits: logits[r, v] = hidden[r, :] . weight[v, :], hidden: [rows, dim] with row stride
  * ld_hidden, weight: [vocab, dim] (an embedding table will do) with row stride ld_weight, both of
  * `dtype`.  logp, entropy, lse are those of pb_logprob_forward (the cross entropy is -logp); each
- * may be NULL, logp and tokens are given together.  Products are summed in float32; float32
- * operands are multiplied to 2^-23 of their products.  A row that meets a value that is not finite has NaN, or for
- * infinite logits what pb_logprob_forward says.  rows and vocab are at most 2^24, dim 2^20.
+ * may be NULL, logp and tokens are given together.  Products are summed in float32.  float32 operands
+ * are multiplied in 16-bit parts: an element counts to 2^-24 of itself, or to 2^-39 of the largest finite one of its
+ * row (hidden) or of the 32 rows it is among (weight).  A row that meets a value that is not finite, or
+ * logits beyond float32, has NaN or an infinity; the other rows do not notice.  rows and vocab are at most 2^24, dim 2^20.
  * dev_scratch: pb_head_scratch_bytes(...) bytes, 256-byte aligned, not used by another call that may run
  * at the same time (two captured graphs included); aligned_rows says that every row of a 16-bit hidden and
  * weight starts on 16 bytes (rows that do not are copied through the scratch).  Should a kernel give up
@@ -402,7 +403,8 @@ int pb_head_logprob_forward(const void* dev_hidden, const void* dev_weight, int 
  * there (several batches; a table that is also the embedding, see pb_embed_backward).  Either
  * gradient may be NULL, not both.  d is formed for a piece of the vocabulary at a time and held in
  * the operands' type, scaled by a power of two so that it does not underflow: 16-bit operands give gradients whose terms are
- * off by up to 2^-9 (bfloat16) or 2^-12 (float16) of themselves, whatever the type of dweight.  rows == 0 clears dweight,
+ * off by up to 2^-8 (bfloat16) or 2^-11 (float16) of themselves, whatever the type of dweight; of float32 ones 2^-24, in dhidden also
+ * 2^-37 of the row's largest coefficient times the largest weight.  rows == 0 clears dweight,
  * or leaves it if accumulate.  PB_E_ARG if a buffer that is written overlaps another. */
 int pb_head_logprob_backward(const void* dev_hidden, const void* dev_weight, int dtype, int64_t rows, int64_t vocab, int64_t dim,
                              int64_t ld_hidden, int64_t ld_weight, const void* dev_tokens, int token_bytes, double inv_temperature,

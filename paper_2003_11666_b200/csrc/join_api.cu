@@ -262,9 +262,9 @@ int pb_join_backward(const pb_join_args* args, const pb_join_grads* grads, void*
         (d.dgate_dtype != PB_F32 && d.dgate_dtype != a.dtype)) return refuse(who, "gradients of weights and gates are float32 or of the block's type");
     if (a.ld_u < a.dim || d.ld_du < a.dim || (d.dx && d.ld_dx < a.dim) || (d.dy && d.ld_dy < a.dim) || (d.dh && (d.ld_dh < a.dim || a.ld_y < a.dim)) ||
         (d.dgate && d.ld_dgate < a.dim)) return refuse(who, "a row stride is smaller than dim");
-    if ((d.dgate && !a.gate) || (d.dpost_weight && !a.post_weight) || (d.dpre_weight && !d.dh))
-        return refuse(who, "a gradient is asked for of what the join does not have");
-    if (a.rows > 0) {
+    if (a.rows > 0) {                           // no rows may have no addresses
+        if ((d.dgate && !a.gate) || (d.dpost_weight && !a.post_weight) || (d.dpre_weight && !d.dh))
+            return refuse(who, "a gradient is asked for of what the join does not have");
         if (!a.u || !d.du || !dev_scratch) return refuse(who, "NULL pointer");
         if (!d.dy && !d.dh) return refuse(who, "neither dy nor dh is given");
         if (d.dh && (!a.y || !a.pre_weight || !a.rstd_pre)) return refuse(who, "dh needs y, pre_weight and rstd_pre");

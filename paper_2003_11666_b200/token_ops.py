@@ -296,7 +296,7 @@ def _one_type(who, a, b):
 
 def _join_gate(who, gate, rows_per_gate, rows, dim, dtype, device):
     """Address, row stride and rows per row of the gate."""
-    per = rows_per_gate or rows or 1
+    per = (rows or 1) if rows_per_gate is None else rows_per_gate
     if per < 1:
         _refuse(who, "rows_per_gate must be at least 1")
     return *_plane(who, "gate", gate, (-(-rows // per), dim), dtype, device), per

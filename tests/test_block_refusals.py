@@ -131,6 +131,7 @@ def test_calls_without_work_touch_nothing(lib):   # noqa: F811
     assert _dropout(lib, rows=0, x=None, out=None) == 0 and _dropout(lib, dim=0, x=None, out=None) == 0
     assert _join(lib, rows=0, x=None, u=None, y=None, h=None) == 0
     assert _join(lib, backward=True, rows=0, u=None, scratch=None, dpre_weight=None, dpost_weight=None) == 0
+    assert _join(lib, backward=True, rows=0, u=None, scratch=None, dy=None, dh=None, gate=None, dpre_weight=None, dpost_weight=None) == 0
     assert lib.pb_join_scratch_bytes(-1, 10, 0) == 0 and lib.pb_join_scratch_bytes(10, 0, 0) == 0 and lib.pb_join_scratch_bytes(10, 16385, 0) == 0
     assert lib.pb_join_scratch_bytes(0, 10, 0) > 0
 

@@ -138,6 +138,14 @@ def test_many_rows(rows, dim, per):
     _run(rows, dim, TYPES[0], per=per)
 
 
+# rows in the ring: every thread with all its columns, and not; a gate for each row, for some, for all; 1024 threads; two rows in flight, or none
+@pytest.mark.parametrize("types", TYPES, ids=str)
+@pytest.mark.parametrize("rows,dim,per", [(1500, 1024, 700), (700, 1032, 1), (2000, 528, 3), (640, 4096, 640), (600, 5120, 5), (601, 8192, 300), (600, 8200, 600)])
+def test_rows_in_the_ring(rows, dim, per, types):
+    _run(rows, dim, types, per=per, p=0.2)
+    _run(rows, dim, types, per=None, post=True)
+
+
 def test_more_gates_of_several_chunks_than_a_grid_has_in_one_direction():
     rows, dim, per = 2_500_000, 16, 36                            # 69445 gates; 33 rows per chunk
     _run(rows, dim, (torch.float32, torch.float32), per=per, post=False, pre=False)
@@ -300,3 +308,41 @@ def _last_factors(seed, offset, first, n):
     base = hashed(seed, offset)
     quads = [hashed(base, q) for q in range(first // 4, (first + n) // 4)]
     return torch.tensor([2.0 if (q >> (16 * k)) & 0xFFFF >= 32768 else 0.0 for q in quads for k in range(4)], dtype=torch.float64)
+
+
+def test_no_rows():
+    pb = _p()
+    e = lambda *n: torch.empty(*n, device="cuda")                 # noqa: E731
+    w, none, no_row = torch.ones(64, device="cuda"), e(0, 64), e(0)
+    scratch = torch.empty(pb.join_scratch_bytes(0, 64, 3), device="cuda", dtype=torch.uint8)
+    pb.dropout(none, none, 0.5, 1)
+    pb.join_forward(none, none, none.clone(), h=none.clone(), pre_weight=w, post_weight=w, gate=none, rows_per_gate=3, rstd_pre=no_row, rstd_post=no_row)
+    d = [torch.full((64,), 3.0, device="cuda") for _ in range(2)]
+    pb.join_backward(none, none, none.clone(), none.clone(), scratch, dy=none, dh=none, pre_weight=w, post_weight=w, gate=none, rows_per_gate=3, rstd_pre=no_row,
+                     rstd_post=no_row, dpre_weight=d[0], dpost_weight=d[1], dgate=none.clone())
+    assert not d[0].any() and not d[1].any()                       # sums over nothing
+
+
+def test_calls_follow_the_current_stream():
+    pb = _p()
+    x, u, w = torch.randn(1200, 512, device="cuda"), torch.randn(1200, 512, device="cuda"), torch.rand(512, device="cuda")
+    scratch = torch.empty(pb.join_scratch_bytes(1200, 512), device="cuda", dtype=torch.uint8)
+
+    def run(x, out):
+        pb.dropout(x, out[0], 0.2, 3)
+        pb.join_forward(out[0], u, out[1], h=out[2], pre_weight=w, post_weight=w, rstd_pre=out[3], rstd_post=out[4])
+        pb.join_backward(out[1], u, out[5], out[6], scratch, dh=out[2], pre_weight=w, post_weight=w, rstd_pre=out[3], rstd_post=out[4], dpre_weight=out[7],
+                         dpost_weight=out[8])
+    new = lambda: [torch.zeros_like(x) for _ in range(3)] + [torch.zeros(1200, device="cuda") for _ in range(2)] + [torch.zeros_like(x) for _ in range(2)] + \
+        [torch.zeros(512, device="cuda") for _ in range(2)]                    # noqa: E731
+    ref, got, late = new(), new(), torch.zeros_like(x)
+    run(x, ref)
+    torch.cuda.synchronize()
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        torch.cuda._sleep(20_000_000)
+        late.copy_(x)
+        run(late, got)
+    stream.synchronize()
+    for a, b in zip(ref, got):
+        assert torch.equal(a, b)

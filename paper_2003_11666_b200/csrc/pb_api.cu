@@ -56,7 +56,7 @@ int fail_text(int code, const char* text) {
     return code;
 }
 
-// Map of a matrix of 16-bit (or float32) elements for bulk tensor copies: up to three dimensions, innermost first, strides in bytes,
+// Map of a matrix of 16-bit (or float32) elements for bulk tensor copies: up to four dimensions, innermost first, strides in bytes,
 // 128-byte swizzle, zero fill outside the matrix.  ahead: L2 fetches the next 128 bytes of a row too (131072 rows of 4 KB, read by all
 // SMs in boxes of 128 bytes by 128 rows: 1 % faster).
 bool tensor_map(CUtensorMap* map, const void* base, int rank, const unsigned long long* dims, const unsigned long long* strides, const unsigned* box,
@@ -69,8 +69,10 @@ bool tensor_map(CUtensorMap* map, const void* base, int rank, const unsigned lon
         const bool found = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &qr) == cudaSuccess && qr == cudaDriverEntryPointSuccess;
         return found ? reinterpret_cast<Encode>(p) : nullptr;
     }();
-    cuuint64_t gd[3] = {1, 1, 1}, gs[2] = {0, 0};
-    cuuint32_t bx[3] = {1, 1, 1}, es[3] = {1, 1, 1};
+    constexpr int kMost = 4;                 // dimensions
+    if (rank < 1 || rank > kMost) return false;
+    cuuint64_t gd[kMost] = {1, 1, 1, 1}, gs[kMost - 1] = {0, 0, 0};
+    cuuint32_t bx[kMost] = {1, 1, 1, 1}, es[kMost] = {1, 1, 1, 1};
     for (int q = 0; q < rank; ++q) { gd[q] = dims[q]; bx[q] = box[q]; }
     for (int q = 0; q + 1 < rank; ++q) gs[q] = strides[q];
     return encode && encode(map, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)rank, const_cast<void*>(base), gd, gs, bx, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
@@ -436,7 +438,7 @@ void add_tiles(std::vector<GemmTile>& tiles, int gemm, int M, int N, int nsplit,
             for (int n0 = 0; n0 < N; n0 += bn) tiles.push_back(GemmTile{gemm, m0, n0, q});
 }
 
-// Tensor map (descriptor of a bulk tensor copy) of a bfloat16 matrix with up to three
+// Tensor map (descriptor of a bulk tensor copy) of a bfloat16 matrix with up to four
 // dimensions, innermost first; strides in bytes for dimensions 1.., 128-byte swizzle, zero
 // fill outside the matrix.  With a null base (the sizing pass before the arena exists) an
 // empty placeholder is filed so that table sizes do not change between the passes.

@@ -382,8 +382,8 @@ int pb_logprob_backward(const void* dev_logits, int dtype, int64_t rows, int64_t
  * of logits: logits[r, v] = hidden[r, :] . weight[v, :], hidden: [rows, dim] with row stride
  * ld_hidden, weight: [vocab, dim] (an embedding table will do) with row stride ld_weight, both of
  * `dtype`.  logp, entropy, lse are those of pb_logprob_forward (the cross entropy is -logp); each
- * may be NULL, logp and tokens are given together.  Products are summed in float32.  float32 operands
- * are multiplied in 16-bit parts: an element counts to 2^-24 of itself, or to 2^-39 of the largest finite one of its
+ * may be NULL, logp and tokens are given together.  Products are summed in float32.  More than four
+ * rows of float32 operands, or rows off 16 bytes, are multiplied in 16-bit parts: an element counts to 2^-24 of itself, or to 2^-39 of the largest finite one of its
  * row (hidden) or of the 32 rows it is among (weight).  A row that meets a value that is not finite, or
  * logits beyond float32, has NaN or an infinity; the other rows do not notice.  rows and vocab are at most 2^24, dim 2^20.
  * dev_scratch: pb_head_scratch_bytes(...) bytes, 256-byte aligned, not used by another call that may run

@@ -20,6 +20,11 @@ namespace {
 
 constexpr int64_t kMaxHeadRows = 1 << 24, kMaxHeadVocab = 1 << 24, kMaxHeadDim = 1 << 20;
 constexpr int64_t kHeadFewRows = 128;           // rows that one block's tile holds; more run in pairs of blocks
+// Forwards that read the weights without the tensor cores, where their rows start on 16 bytes.  us among others, that way / by the tensor cores:
+// bf16, 131072 tokens, 1 row: 23.8 / 18.9 (64 columns), 23.9 / 24.7 (256), 43.9 / 58.6 (1024), 80.2 / 95.5 (2048); 2 rows: 29.2 / 23.7 (256),
+// 49.3 / 54.8 (1024), 86.7 / 96.6 (2048); 3 and 4 rows: 78 / 55 (1024).  f32, 131072 tokens, 1 row: 24 / 91 (64), 164 / 656 (2048); 4 rows: 40 / 93, 219 / 658;
+// 1000 tokens, 1 row: 5.6 / 12.7 (64), 8.5 / 38.9 (2048).  Beside the time, these sums round to nearest (2e-8 of a logsumexp; 2e-6 there).
+constexpr int64_t kHeadFewFloat = 4, kHeadFewHalf = 2, kHeadFewDim = 256;      // 16-bit rows: as many as dim has of kHeadFewDim
 constexpr int64_t kHeadPieceBytes = 256 << 20;  // of d, or of packed weights, held at a time
 constexpr int64_t kHeadPieceMin = 8192;         // tokens of a piece at least: dhidden's partial sums are read and written once for each
 constexpr int64_t kHeadStatRows = 8192;         // rows whose statistics are held at a time
@@ -37,6 +42,7 @@ int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 struct HeadPlan {
     int cg;
     bool f32, packed;            // packed: 16-bit operands are copied
+    bool few;                    // a forward without the tensor cores
     int64_t dp;                  // row stride of packed operands
     int64_t piece, pieces;       // tokens of a piece of the vocabulary
     int64_t stat_rows, parts;
@@ -57,7 +63,18 @@ HeadPlan head_plan(int dtype, int64_t rows, int64_t vocab, int64_t dim, bool dir
     e.cg = rows <= kHeadFewRows ? 1 : 2;
     e.f32 = dtype == PB_F32;
     e.packed = !e.f32 && !direct;
+    e.few = !backward && direct && rows <= (e.f32 ? kHeadFewFloat : std::min(kHeadFewHalf, dim / kHeadFewDim));
     e.dp = up(dim, 8);
+    if (e.few) {
+        const int64_t groups = (vocab + kHeadFewCols - 1) / kHeadFewCols;
+        e.stat_rows = rows;
+        e.parts = std::min<int64_t>(groups, kSms * kHeadFewBlocks);
+        e.part = (float*)scratch;
+        e.ztok = e.part + 3 * e.parts * rows;
+        e.bytes = (size_t)((3 * e.parts + 1) * rows * 4);
+        if (e.f32) e.bytes = std::max(e.bytes, head_plan(dtype, rows, vocab, dim, false, false, nullptr).bytes);      // a size for any rows
+        return e;
+    }
     const int64_t tile = 128 * e.cg, operand = e.f32 ? kHeadNear : 1, planes = e.f32 ? kHeadNear + kHeadWide : 1;
     int64_t most = vocab;
     if (e.f32 || e.packed) most = std::min(most, kHeadPieceBytes / (operand * e.dp * 2));
@@ -239,6 +256,18 @@ cudaError_t weight_of(HeadMatrix& m, const HeadPlan& e, int dtype, const void* x
     return e.f32 ? pack_near<kHeadGroup>((const float*)x, rows, dim, ld, e.weight, e.dp, e.col_scale, most, s) : pack(dtype, x, rows, dim, ld, e.weight, e.dp, s);
 }
 
+// Statistics of a few rows.
+template <typename T>
+cudaError_t few_rows(const HeadPlan& e, const void* hidden, const void* weight, int64_t rows, int64_t vocab, int64_t dim, int64_t ldh, int64_t ldw,
+                     const void* tokens, int token_bytes, float c, cudaStream_t s) {
+    auto kernel = rows == 1 ? head_few_kernel<T, 1> : head_few_kernel<T, 2>;
+    if constexpr (sizeof(T) == 4) {
+        if (rows > 2) kernel = head_few_kernel<T, 4>;
+    }
+    return launch_after(kernel, dim3((unsigned)e.parts), 32 * kHeadFewWarps, s, (const T*)hidden, (const T*)weight, (int)rows, (int)vocab, (int)dim, (long long)ldh,
+                        (long long)ldw, tokens, token_bytes, c, e.part, e.ztok);
+}
+
 // Rows that a bulk copy can start on.
 bool direct_rows(const void* p, int64_t rows, int64_t ld) { return aligned(p, 16) && (ld % 8 == 0 || rows == 1); }
 
@@ -296,6 +325,15 @@ int pb_head_logprob_forward(const void* dev_hidden, const void* dev_weight, int 
     if (in_scratch(dev_hidden, n_h) || in_scratch(dev_weight, n_w) || in_scratch(dev_tokens, n_t) || in_scratch(dev_status, n_st) ||
         in_scratch(dev_logp, rows * 4) || in_scratch(dev_entropy, rows * 4) || in_scratch(dev_lse, rows * 4)) return refuse(who, "buffers overlap");
     const cudaStream_t s = (cudaStream_t)stream;
+    if (e.few) {
+        const float c = (float)(inv_temperature * 1.4426950408889634074);
+        auto few = dtype == PB_F32 ? few_rows<float> : dtype == PB_BF16 ? few_rows<__nv_bfloat16> : few_rows<__half>;
+        cudaError_t err = few(e, dev_hidden, dev_weight, rows, vocab, dim, ld_hidden, ld_weight, dev_tokens, token_bytes, c, s);
+        if (err == cudaSuccess)
+            err = launch_after(head_rows_kernel, dim3((unsigned)rows), kHeadRowThreads, s, e.part, (int)e.parts, (int)rows, 1, e.ztok, dev_tokens, token_bytes,
+                               (long long)vocab, c, (int)(dev_entropy != nullptr), dev_logp, dev_entropy, dev_lse, dev_status);
+        return launched(who, err);
+    }
     HeadMatrix hidden, b;
     cudaError_t err = hidden_of(hidden, e, dtype, dev_hidden, rows, dim, ld_hidden, s);
     for (int64_t r0 = 0; r0 < rows && err == cudaSuccess; r0 += e.stat_rows) {

@@ -29,7 +29,7 @@
 // added up in registers.
 // What bounds it: 16-bit products wait for L2 (a pair reads 64 KB for 512 cycles of its tensor cores; 42 to 46 bytes per cycle reach an SM,
 // the tensor cores are 70 to 75 % busy: 1340 TFLOP/s in the forward of 4096 x 131072 x 4096, and the power limit in long runs), float32 ones
-// for the tensor cores (98 % busy, since a chunk's planes are read once for all terms), a single row for memory (5.7 TB/s).
+// for the tensor cores (98 % busy, since a chunk's planes are read once for all terms).  One or two rows (four of float32) have a kernel without them.
 // Every wait is bounded (see mbar_wait); a block whose wait runs out reports it and gives NaN for its tiles.
 #pragma once
 #include "tc_common.cuh"
@@ -854,6 +854,137 @@ __global__ void __launch_bounds__(kNearThreads<kGroup>) head_near_kernel(const f
     for (int k = 0; k < kHeld; ++k) split(start + k * kStep, held[k]);
 #pragma unroll 8
     for (int c = start + kHeld * kStep; c < ldp; c += kStep) split(c, four(c));
+}
+
+// ------------------------------------------------------------------ a few rows
+// Statistics of kRows rows without the tensor cores, whose tiles of 128 rows would be all but empty: a warp reads kHeadFewCols rows of the weights at a
+// time, 256 elements of each per step, and multiplies them in float32 with the hidden rows, which stay in L1.  Its groups of columns are
+// `gridDim * kHeadFewWarps` apart, neighbours in neighbouring blocks, so that a short vocabulary reaches every SM.  Bound by the weights' one pass: a row on
+// 131072 x 2048 bf16 takes 80 us, 6.7 TB/s; four columns of a warp's took 83.
+constexpr int kHeadFewWarps = 8, kHeadFewBlocks = 4, kHeadFewCols = 2;
+struct HeadEight { uint4 q[2]; };            // eight elements; 16-bit ones take the first half
+
+template <typename T, bool kStream> __device__ __forceinline__ HeadEight eight_of(const T* p) {
+    HeadEight e;
+#pragma unroll
+    for (int k = 0; k < (int)sizeof(T) / 2; ++k) {
+        uint4& q = e.q[k];
+        if (kStream) asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(q.x), "=r"(q.y), "=r"(q.z), "=r"(q.w) : "l"((const uint4*)p + k));
+        else q = __ldg((const uint4*)p + k);
+    }
+    return e;
+}
+template <typename T> __device__ __forceinline__ void floats_of(Pair (&f)[4], const HeadEight& e, T) {
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            f[2 * k] = Pair(__uint_as_float(e.q[k].x), __uint_as_float(e.q[k].y));
+            f[2 * k + 1] = Pair(__uint_as_float(e.q[k].z), __uint_as_float(e.q[k].w));
+        }
+    } else {
+        float x[8];
+        unpack8(x, e.q[0], T());
+#pragma unroll
+        for (int k = 0; k < 4; ++k) f[k] = Pair(x[2 * k], x[2 * k + 1]);
+    }
+}
+
+template <typename T, int kRows>
+__global__ void __launch_bounds__(32 * kHeadFewWarps, kRows == 4 ? 2 : kHeadFewBlocks) head_few_kernel(const T* hidden, const T* weight, int rows, int vocab, int dim,
+                                                                                      long long ldh, long long ldw, const void* tokens, int token_bytes, float c,
+                                                                                      float* part, float* ztok) {
+    __shared__ HeadStat all[kHeadFewWarps][kRows];
+    constexpr int kCols = kHeadFewCols;
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, mine = lane % kRows, whole = dim & ~7;
+    cudaGridDependencySynchronize();
+    long long token = -1;                                    // of the lane's row
+    if (tokens && mine < rows) token = token_bytes == 8 ? ((const long long*)tokens)[mine] : (long long)((const int*)tokens)[mine];
+    HeadStat st;
+    st.start();
+    for (int c0 = (warp * gridDim.x + blockIdx.x) * kCols; c0 < vocab; c0 += gridDim.x * kHeadFewWarps * kCols) {
+        const T* w[kCols];
+#pragma unroll
+        for (int u = 0; u < kCols; ++u) w[u] = weight + min(c0 + u, vocab - 1) * ldw;       // behind the last column: the last one again
+        Pair sum[kRows][kCols];
+#pragma unroll
+        for (int r = 0; r < kRows; ++r)
+#pragma unroll
+            for (int u = 0; u < kCols; ++u) sum[r][u] = Pair(0.f);
+        auto step = [&](const HeadEight (&e)[kCols], int k) {
+            Pair f[kCols][4];
+#pragma unroll
+            for (int u = 0; u < kCols; ++u) floats_of(f[u], e[u], T());
+#pragma unroll
+            for (int r = 0; r < kRows; ++r) {
+                Pair h[4];
+                floats_of(h, eight_of<T, false>(hidden + (r < rows ? r : 0) * ldh + k), T());
+#pragma unroll
+                for (int u = 0; u < kCols; ++u)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) sum[r][u] = fma2(f[u][i], h[i], sum[r][u]);
+            }
+        };
+        constexpr int kAhead = sizeof(T) == 4 ? 2 : 4;       // steps whose weights are under way, as registers go
+        int k = lane * 8;
+        for (; k + (kAhead - 1) * 256 < whole; k += kAhead * 256) {
+            HeadEight e[kAhead][kCols];
+#pragma unroll
+            for (int a = 0; a < kAhead; ++a)
+#pragma unroll
+                for (int u = 0; u < kCols; ++u) e[a][u] = eight_of<T, true>(w[u] + k + a * 256);
+#pragma unroll
+            for (int a = 0; a < kAhead; ++a) step(e[a], k + a * 256);
+        }
+        for (; k < whole; k += 256) {
+            HeadEight e[kCols];
+#pragma unroll
+            for (int u = 0; u < kCols; ++u) e[u] = eight_of<T, true>(w[u] + k);
+            step(e, k);
+        }
+        float z[kCols];
+#pragma unroll
+        for (int r = 0; r < kRows; ++r)
+#pragma unroll
+            for (int u = 0; u < kCols; ++u) {
+                float a, b;
+                sum[r][u].split(a, b);
+                a += b;
+                if (whole + lane < dim) a = fmaf(to_f32(w[u][whole + lane]), to_f32(hidden[(r < rows ? r : 0) * ldh + whole + lane]), a);
+#pragma unroll
+                for (int n = 16; n; n /= 2) a += __shfl_xor_sync(0xffffffffu, a, n);
+                if (r == mine) z[u] = a;
+            }
+        float top = -INFINITY;
+#pragma unroll
+        for (int u = 0; u < kCols; ++u) {
+            if (token == c0 + u && c0 + u < vocab && lane < rows) ztok[lane] = z[u];
+            if (c0 + u >= vocab) z[u] = -INFINITY;
+            top = fmaxf(top, z[u]);
+        }
+        const float now = fmaxf(st.ref, top * c), base = now == -INFINITY ? 0.f : now;      // c > 0
+        if (now > st.ref && st.ref != -INFINITY) {
+            const float shift = st.ref - now, f = exp2f(shift);
+            st.elog = f * fmaf(shift, st.sum, st.elog);
+            st.sum *= f;
+        }
+        st.ref = now;
+#pragma unroll
+        for (int u = 0; u < kCols; ++u) {
+            const float t = head_floor(fmaf(z[u], c, -base)), e = exp2f(t);
+            st.sum += e;
+            st.elog = fmaf(e, t, st.elog);
+        }
+    }
+    if (lane < kRows) all[warp][lane] = st;
+    __syncthreads();
+    if (threadIdx.x < rows) {
+        st = all[0][threadIdx.x];
+        for (int k = 1; k < kHeadFewWarps; ++k) st.join(all[k][threadIdx.x].ref, all[k][threadIdx.x].sum, all[k][threadIdx.x].elog);
+        const long long at = (long long)blockIdx.x * rows + threadIdx.x, plane = (long long)gridDim.x * rows;
+        part[at] = st.ref;
+        part[plane + at] = st.sum;
+        part[2 * plane + at] = st.elog;
+    }
 }
 
 // Row values from the parts' statistics: kHeadRowThreads threads for `width` rows, which share a row's parts.  The largest reference is

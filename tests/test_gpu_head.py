@@ -325,3 +325,27 @@ def test_offsets_pass_32_bits():
     d[tok] += 1
     _within(dw[[0, 5, vocab - 2, vocab - 1], 3], 0.5 * d[[0, 5, vocab - 2, vocab - 1]], 0.5 * (3 * 2.0 ** -8 + 2.0 ** -18) * (3 * ref.exp() + (d > 0))[[0, 5, vocab - 2, vocab - 1]])
     assert bool((dw[:, 64:] == 0).all())
+
+
+# rows that run without the tensor cores: odd widths at strides of 16 bytes, vocabularies shorter than a block and longer than a round of all of them
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("rows", [1, 2, 3, 4, 5])
+@pytest.mark.parametrize("vocab,dim,pad", [(1, 512, 0), (7, 1021, 3), (9475, 513, 7), (50021, 776, 8), (300, 9000, 0)])
+def test_a_few_rows(rows, vocab, dim, pad, dtype):
+    h, w, tok, rand = _case(rows, vocab, dim, dtype, pad)
+    _check_forward(h, w, tok, 0.8)
+    logp, entropy, lse = _forward(h, w, tok, 0.8)
+    again = _forward(h, w, tok, 0.8)
+    assert all(torch.equal(a, b) for a, b in zip((logp, entropy, lse), again))
+    lse_only = torch.full((rows,), 9.0, device="cuda")
+    _p().head_logprob_forward(h, w, _scratch(h, w), lse=lse_only, inv_temperature=0.8)
+    assert torch.equal(lse_only, lse)
+    h[0, dim - 1] = float("nan")
+    bad = _forward(h, w, tok, 0.8)
+    assert all(bool(b[0].isnan()) and torch.equal(b[1:], a[1:]) for a, b in zip((logp, entropy, lse), bad))
+
+
+def test_a_float32_scratch_serves_any_rows():
+    lib = __import__("paper_2003_11666_b200.binding", fromlist=["load_library"]).load_library()
+    for rows, vocab, dim in ((1, 1, 1), (1, 1000, 1), (4, 100, 3), (4, 100000, 64)):
+        assert lib.pb_head_scratch_bytes(0, rows, vocab, dim, 1, 0) == lib.pb_head_scratch_bytes(0, rows, vocab, dim, 0, 0)

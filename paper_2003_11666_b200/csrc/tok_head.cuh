@@ -472,8 +472,9 @@ __device__ __forceinline__ void head_gradient(const HeadArgs& g, const HeadJob& 
     }
     if (kF32 && g.store_near) {
         // two float16 planes, each column times its weights' power of two over the largest: those weights are smaller by as much
-        const float most = v.d_scale / *g.col_most, f0 = g.col_scale[c0 / kHeadGroup] * most,
-                    f1 = c0 + kHeadGroup < q.cols ? g.col_scale[c0 / kHeadGroup + 1] * most : 0.f;
+        // (the scales' quotient first: it is at most 1, where d_scale over a small scale may be beyond float32)
+        const float most = 1.f / *g.col_most, f0 = g.col_scale[c0 / kHeadGroup] * most * v.d_scale,
+                    f1 = c0 + kHeadGroup < q.cols ? g.col_scale[c0 / kHeadGroup + 1] * most * v.d_scale : 0.f;
 #pragma unroll
         for (int plane = 0; plane < kHeadNear; ++plane) {
             buf_free(lane);

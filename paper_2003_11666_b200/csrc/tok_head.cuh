@@ -830,7 +830,9 @@ __global__ void __launch_bounds__(kNearThreads<kGroup>) head_near_kernel(const f
     top = tops[lane % kWarps];
 #pragma unroll
     for (int k = kWarps / 2; k; k /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, k));
-    int e = 15;
+    // Weights of nothing but zeros (a padded vocabulary) take the smallest scale there is, so that the largest one, which d is formed for, is that of numbers
+    // that count: with a scale of 1, 16 or more of d's digits went to a product with zero.
+    int e = kGroup > 1 ? 15 - 120 : 15;
     if (top > 0.f) frexpf(top, &e);
     e = min(max(15 - e, -120), 120);
     const float f = ldexpf(1.f, e);

@@ -431,7 +431,8 @@ int pb_dropout(const void* dev_x, int dtype, int64_t rows, int64_t dim, int64_t 
  * are float32 or of dtype.  Row r takes row r / rows_per_gate of the gate: 1 is a gate per row, a sequence's length one
  * per sequence, rows one for all.  Sums are float32, y enters the norm before it is rounded.  The rstds
  * (float32, [rows], may be NULL) are for the backward.  y may be the very buffer of x, h that of u.  rows is at most 2^30, dim
- * 16384. */
+ * 16384.  Should a kernel give up waiting for copies of its own (after 0.2 s), the rows that it then has not done, and the sums
+ * over rows that they belong to, are NaN; so in the gradient. */
 typedef struct {
     int64_t rows, dim;
     int32_t dtype, stream_dtype, weight_dtype;

@@ -131,6 +131,7 @@ JoinParams params_of(const pb_join_args& a, int lanes) {
     unsigned drop = 0;
     share_of(a.p, drop);
     p.keep = keep_of(drop, a.seed, a.offset, a.dev_offset);
+    p.wait_ns = kTcWaitNs;
     return p;
 }
 

@@ -28,7 +28,8 @@ __device__ __forceinline__ long long global_ns() {
     asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
     return t;
 }
-__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, const volatile int* fail) {
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, const volatile int* fail, long long limit = kTcWaitNs) {
+    if (limit <= 0) return false;                        // none at all
     uint32_t done = 0;
     long long t0 = 0;
     for (int it = 0; !done; ++it) {
@@ -38,7 +39,7 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, const v
             if (*fail) return false;
             const long long now = global_ns();
             if (t0 == 0) t0 = now;
-            else if (now - t0 > kTcWaitNs) return false;
+            else if (now - t0 > limit) return false;
         }
     }
     return true;

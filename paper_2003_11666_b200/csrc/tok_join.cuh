@@ -201,6 +201,7 @@ struct JoinParams {
     bool dgate_f32;
     float *part_pre, *part_post; // [blocks][dim], or NULL
     int depth, row_bytes;        // rows of the ring, bytes of one: 128-byte aligned
+    long long wait_ns;           // that a row's copies are waited for
 };
 
 constexpr int kJoinThreads = 256;             // of a block, or the threads of a row if those are more
@@ -260,20 +261,17 @@ __device__ __forceinline__ float root_of(float x) {
     return r > 0.f && r < INFINITY ? r * fmaf(-0.5f * x * r, r, 1.5f) : r;
 }
 
-// A copy that has not come in time may still land: before the shared memory that it writes goes back to the SM.
-__device__ __forceinline__ void ring_late() {
-    for (int k = 0; k < 512; ++k) __nanosleep(200);
-}
-
 // How a thread's eight columns lie: kOdd: `lanes` apart, so that neighbours read neighbours; kEven: consecutive; kFull: consecutive, and every thread has
 // all of its own (what else asks at each access whether they exist: 7 % of the time of 8192 rows of 4096).
 enum JoinLayout { kOdd = 0, kEven = 1, kFull = 2 };
 
-// Rows that a block takes one after the other come by bulk copies into a ring in shared memory.
+// Rows that a block takes one after the other come by bulk copies into a ring in shared memory.  Should a row's copies not come in time, the block asks for
+// no more of them, and what it would have written from that row on is NaN.
 constexpr int kJoinRing = 4;                  // rows on their way at most
 struct JoinRing {
     uint64_t full[kJoinRing];
-    int fail;
+    int fail[2];                              // a wait for this row has run out; rows take turns, so that all threads see the same after they have met
+    int calm;                                 // always 0
 };
 __device__ __forceinline__ void bulk_row(unsigned char* dst, const void* src, uint32_t bytes, uint32_t bar) {
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
@@ -282,8 +280,19 @@ __device__ __forceinline__ void bulk_row(unsigned char* dst, const void* src, ui
 // One thread sets the barriers up before the block meets for the first time.
 __device__ __forceinline__ void ring_init(JoinRing& ring) {
     for (int k = 0; k < kJoinRing; ++k) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(smem_u32(&ring.full[k])) : "memory");
-    ring.fail = 0;
+    ring.fail[0] = ring.fail[1] = ring.calm = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+}
+// The threads have met after a wait has run out.  The n rows that are under way, from place `at` on, land before the shared memory that they write goes back to
+// the SM, or have had their time once more.
+__device__ __forceinline__ void ring_lost(JoinRing& ring, int at, uint32_t phase, int depth, int n) {
+    if (threadIdx.x == 0) {
+        for (; n > 0; --n) {
+            mbar_wait(smem_u32(&ring.full[at]), phase, &ring.calm);
+            if (++at == depth) { at = 0; phase ^= 1; }
+        }
+    }
+    __syncthreads();
 }
 template <typename T, bool kPieces> struct RawColumns : RawEight<T> {};
 template <typename T> struct RawColumns<T, false> {
@@ -437,9 +446,9 @@ __global__ void __launch_bounds__(kThreads, kThreads <= 256 ? 512 / kThreads : 1
     }
     int at = 0, turn = 0;
     uint32_t phase = 0;
-    bool ok = true;
-    for (long long r = blockIdx.x; r < p.rows; r += gridDim.x, turn ^= 1) {
-        if (ok) ok = mbar_wait(smem_u32(&ring.full[at]), phase, &ring.fail);
+    long long r = blockIdx.x;
+    for (; r < p.rows; r += gridDim.x, turn ^= 1) {
+        if (!mbar_wait(smem_u32(&ring.full[at]), phase, &ring.fail[turn], p.wait_ns)) ring.fail[turn] = 1;
         const unsigned char* from = store + at * p.row_bytes;
         Eight y[kUnits], b[kUnits], gate[kUnits];
         float sum = 0.f;
@@ -451,7 +460,6 @@ __global__ void __launch_bounds__(kThreads, kThreads <= 256 ? 512 / kThreads : 1
             if (p.gate) gate[k] = c.template get_shared<T>(from + s_bytes + t_bytes);
             if (p.post) sum += dot8(b[k], b[k]);
         }
-        if (!ok) y[0].fill(__int_as_float(0x7fffffff));       // a copy never came: the row is NaN
         float rstd = 1.f;
         if (p.post) {
             rstd = root_of(fmaf(row_sum(sum, blockDim.x, sm[turn][0]), p.inv_dim, p.eps));
@@ -459,6 +467,7 @@ __global__ void __launch_bounds__(kThreads, kThreads <= 256 ? 512 / kThreads : 1
         } else {
             __syncthreads();
         }
+        if (ring.fail[turn]) break;
         if (lane == 0 && r + (long long)p.depth * gridDim.x < p.rows) ask(r + (long long)p.depth * gridDim.x, at);     // all have read this row
         if (++at == p.depth) { at = 0; phase ^= 1; }
         const float scale = p.keep.drop ? rstd * p.keep.scale : rstd;
@@ -480,7 +489,20 @@ __global__ void __launch_bounds__(kThreads, kThreads <= 256 ? 512 / kThreads : 1
 #pragma unroll
         for (int k = 0; k < kUnits; ++k) Columns<kLayout>(lane, k, blockDim.x, p.dim).put((T*)p.h + r * p.ld_h, y[k] * rstd * pre[k]);
     }
-    if (!ok) ring_late();
+    if (r >= p.rows) return;
+    ring_lost(ring, at, phase, p.depth, (int)min((long long)p.depth, (p.rows - 1 - r) / gridDim.x + 1));
+    Eight none;
+    none.fill(__int_as_float(0x7fffffff));
+    for (; r < p.rows; r += gridDim.x) {
+#pragma unroll
+        for (int k = 0; k < kUnits; ++k) {
+            const Columns<kLayout> c(lane, k, blockDim.x, p.dim);
+            c.put((S*)p.y + r * p.ld_y, none);
+            if (p.h) c.put((T*)p.h + r * p.ld_h, none);
+        }
+        if (lane == 0 && p.post && p.rstd_post) p.rstd_post[r] = __int_as_float(0x7fffffff);
+        if (lane == 0 && p.h && p.rstd_pre) p.rstd_pre[r] = __int_as_float(0x7fffffff);
+    }
 }
 
 // Rows of any layout: a worker is the threads of a row, and goes through chunks of rows that share a gate.
@@ -664,15 +686,13 @@ __global__ void __launch_bounds__(kThreads, kThreads <= 256 ? 512 / kThreads : 1
     }
     int get = 0, turn = 0;
     uint32_t phase = 0;
-    bool ok = true;
-    for (int chunk = blockIdx.x; chunk < p.chunks; chunk += blocks) {
+    int chunk = blockIdx.x, q = 0;
+    for (; chunk < p.chunks; chunk += blocks) {
         const Chunk now = chunk_at(chunk);
-        for (int q = 0; q < now.rows; ++q, turn ^= 1) {
+        for (q = 0; q < now.rows; ++q, turn ^= 1) {
             const long long r = now.first + q;
-            float rp = p.post ? p.rstd_post[r] : 1.f;
-            const float rr = p.dh ? p.rstd_pre[r] : 0.f;
-            if (ok) ok = mbar_wait(smem_u32(&ring.full[get]), phase, &ring.fail);
-            if (!ok) rp = __int_as_float(0x7fffffff);         // a copy never came: NaN
+            const float rp = p.post ? p.rstd_post[r] : 1.f, rr = p.dh ? p.rstd_pre[r] : 0.f;
+            if (!mbar_wait(smem_u32(&ring.full[get]), phase, &ring.fail[turn], p.wait_ns)) ring.fail[turn] = 1;
             const unsigned char* from = store + get * p.row_bytes;
             Eight g[kUnits], un[kUnits], yn[kUnits], gate[kUnits], keep[kUnits];
             float s1 = 0.f, s2 = 0.f, s3 = 0.f;
@@ -701,6 +721,7 @@ __global__ void __launch_bounds__(kThreads, kThreads <= 256 ? 512 / kThreads : 1
             if (p.dh || p.post) row_sums(s1, s2, s3, blockDim.x, sm[turn]);
             const float m1 = -rr * p.inv_dim * s1, m2 = -rp * p.inv_dim * fmaf(m1, s3, s2);
             if (!(p.dh || p.post) || blockDim.x == 32) __syncthreads();
+            if (ring.fail[turn]) break;
             if (lane == 0) ask();                             // all have read this row: another may have its place
             if (++get == p.depth) { get = 0; phase ^= 1; }
 #pragma unroll
@@ -715,6 +736,7 @@ __global__ void __launch_bounds__(kThreads, kThreads <= 256 ? 512 / kThreads : 1
                 c.put((T*)p.du + r * p.ld_du, g[k]);
             }
         }
+        if (q < now.rows) break;
         if (p.gate) {
 #pragma unroll
             for (int k = 0; k < kUnits; ++k) {
@@ -730,7 +752,29 @@ __global__ void __launch_bounds__(kThreads, kThreads <= 256 ? 512 / kThreads : 1
             }
         }
     }
-    if (!ok) ring_late();
+    if (chunk < p.chunks) {
+        ring_lost(ring, get, phase, p.depth, (put - get + p.depth - 1) % p.depth + 1);       // of the first thread, which has asked: all places, but for the last rows
+        Eight none;
+        none.fill(__int_as_float(0x7fffffff));
+        for (; chunk < p.chunks; chunk += blocks, q = 0) {
+            const Chunk now = chunk_at(chunk);
+#pragma unroll
+            for (int k = 0; k < kUnits; ++k) {
+                const Columns<kLayout> c(lane, k, blockDim.x, p.dim);
+                for (int i = q; i < now.rows; ++i) {
+                    if (p.dx) c.put((S*)p.dx + (now.first + i) * p.ld_dx, none);
+                    c.put((T*)p.du + (now.first + i) * p.ld_du, none);
+                }
+                if (p.gate && p.dgate) {
+                    if (p.gate_part) c.put(p.gate_part + (long long)chunk * p.dim, none);
+                    else if (p.dgate_f32) c.put((float*)p.dgate + now.group * p.ld_dgate, none);
+                    else c.put((T*)p.dgate + now.group * p.ld_dgate, none);
+                }
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < kUnits; ++k) dpre[k] = dpost[k] = both[k] = none;
+    }
 #pragma unroll
     for (int k = 0; k < kUnits; ++k) {
         const Columns<kLayout> c(lane, k, blockDim.x, p.dim);

@@ -32,13 +32,16 @@ int join_lanes(int64_t dim, int64_t wide, int& units) {
 // A block: rows of a warp or less share one.
 int join_threads(int lanes) { return lanes > 32 ? lanes : kJoinThreads; }
 
+constexpr int kRingBytes = 220 * 1024;          // of an SM, for the rings of all of its blocks
 // Rows of a ring in shared memory, with so many blocks on an SM; below two the ring is no use.
 int ring_depth(int row_bytes, int blocks) {
-    return std::min(kJoinRing, 220 * 1024 / blocks / row_bytes);
+    return std::min(kJoinRing, kRingBytes / blocks / row_bytes);
 }
+// The limit of a kernel's shared memory is the same in every call: it belongs to the kernel, and another thread's call may come between this one's and its
+// launch.
 cudaError_t launch_ring(void (*kernel)(JoinParams), int blocks, int threads, size_t shared, cudaStream_t s, const JoinParams& p) {
     if (shared > 48 * 1024) {
-        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shared);
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kRingBytes);
         if (e != cudaSuccess) return e;
     }
     cudaLaunchConfig_t c{};

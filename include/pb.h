@@ -388,7 +388,8 @@ int pb_logprob_backward(const void* dev_logits, int dtype, int64_t rows, int64_t
  * logits beyond float32, has NaN or an infinity; the other rows do not notice.  rows and vocab are at most 2^24, dim 2^20.
  * dev_scratch: pb_head_scratch_bytes(...) bytes, 256-byte aligned, not used by another call that may run
  * at the same time (two captured graphs included); aligned_rows says that every row of a 16-bit hidden and
- * weight starts on 16 bytes (rows that do not are copied through the scratch).  Should a kernel give up
+ * weight starts on 16 bytes (rows that do not are copied through the scratch).  A size serves fewer rows too, and one
+ * for rows that do not start on 16 bytes also those that do.  Should a kernel give up
  * waiting for its own copies, *dev_status is 2 and values that depend on them are NaN. */
 size_t pb_head_scratch_bytes(int dtype, int64_t rows, int64_t vocab, int64_t dim, int aligned_rows, int backward);
 int pb_head_logprob_forward(const void* dev_hidden, const void* dev_weight, int dtype, int64_t rows, int64_t vocab, int64_t dim,

@@ -126,6 +126,52 @@ HeadPlan head_plan(int dtype, int64_t rows, int64_t vocab, int64_t dim, bool dir
     return e;
 }
 
+// Scratch for `rows` rows or fewer.  Fewer can need more: one or two rows have a kernel with parts of its own, up to 128 rows tiles of half the size and more splits,
+// and the pieces of the vocabulary grow as the rows become fewer.
+size_t head_bytes(int dtype, int64_t rows, int64_t vocab, int64_t dim, bool direct, bool backward) {
+    const bool f32 = dtype == PB_F32;
+    if (!backward) {
+        size_t most = 0;
+        for (int64_t r : {rows, std::min(rows, kHeadFewRows), std::min(rows, kHeadFewFloat), std::min(rows, kHeadFewHalf), int64_t(1)})
+            for (bool d : {direct, true}) most = std::max(most, head_plan(dtype, r, vocab, dim, d, false, nullptr).bytes);     // a row alone may start on 16 bytes
+        return most;
+    }
+    const HeadPlan one = head_plan(dtype, 1, vocab, dim, direct, true, nullptr);         // the longest piece
+    const int64_t operand = f32 ? kHeadNear : 1, planes = f32 ? kHeadNear + kHeadWide : 1, held = kHeadPieceBytes / (planes * 2);
+    // Numbers of d in a plane: of the whole vocabulary, or as many as the pieces are cut for (to a multiple of 256 tokens), or the shortest pieces of every row.
+    const int64_t d = std::min(rows * up(vocab, 64), std::max(held + 256 * rows, kHeadPieceMin * rows));
+    // Rows of partial sums: a plane for each split.
+    int64_t sums = 0;
+    for (int cg : {1, 2})
+        for (int64_t tiles_m = 1;; ++tiles_m) {
+            const int64_t tile = 128 * cg, tiles = tiles_m * ((dim + tile - 1) / tile);
+            const int64_t splits = std::max<int64_t>(1, std::min((kSms / cg) / tiles, up(vocab, kHeadChunk) / kHeadChunk / 16));
+            const bool last = (cg == 1 && tiles_m * tile >= kHeadFewRows) || tiles_m * tile >= rows || splits == 1;
+            sums = std::max(sums, splits * (splits == 1 && cg == 2 ? rows : std::min(rows, tiles_m * tile)));
+            if (last) break;
+        }
+    size_t at = 0;
+    auto take = [&](int64_t bytes) { at += (size_t)up(bytes, 256); };
+    if (f32 || !direct) {
+        take(operand * rows * one.dp * 2);
+        take(operand * one.piece * one.dp * 2);
+    }
+    take(operand * d * 2);
+    take(sums * up(dim, 8) * 4);
+    take(rows * (int64_t)sizeof(HeadRow));
+    take(rows * 4);
+    take(4);
+    if (f32) {
+        take(rows * 4);
+        take((one.piece + kHeadGroup - 1) / kHeadGroup * 4);
+        take(kHeadWide * d * 2);
+        take(kHeadWide * rows * one.dp * 2);
+        take(rows * 4);
+        take((vocab + kHeadPieceMin - 1) / kHeadPieceMin * 4);
+    }
+    return at;
+}
+
 // A matrix that a product reads: 16-bit elements, planes of [rows, cols] with row stride ld.
 struct HeadMatrix {
     const void* p;
@@ -299,7 +345,7 @@ extern "C" {
 
 size_t pb_head_scratch_bytes(int dtype, int64_t rows, int64_t vocab, int64_t dim, int aligned_rows, int backward) {
     if (bad_sizes(dtype, rows, vocab, dim, dim, dim)) return 0;
-    return std::max<size_t>(256, head_plan(dtype, std::max<int64_t>(rows, 1), vocab, dim, aligned_rows != 0, backward != 0, nullptr).bytes);
+    return std::max<size_t>(256, head_bytes(dtype, std::max<int64_t>(rows, 1), vocab, dim, aligned_rows != 0, backward != 0));
 }
 
 int pb_head_logprob_forward(const void* dev_hidden, const void* dev_weight, int dtype, int64_t rows, int64_t vocab, int64_t dim, int64_t ld_hidden,
@@ -318,7 +364,7 @@ int pb_head_logprob_forward(const void* dev_hidden, const void* dev_weight, int 
     if (!aligned(dev_scratch, 256)) return refuse(who, "scratch must be 256-byte aligned");
     const bool direct = direct_rows(dev_hidden, rows, ld_hidden) && direct_rows(dev_weight, vocab, ld_weight);
     const HeadPlan e = head_plan(dtype, rows, vocab, dim, direct, false, (char*)dev_scratch);
-    if (scratch_bytes < e.bytes) return refuse(who, "scratch is smaller than pb_head_scratch_bytes");
+    if (scratch_bytes < std::max(e.bytes, head_bytes(dtype, rows, vocab, dim, direct, false))) return refuse(who, "scratch is smaller than pb_head_scratch_bytes");
     const size_t n_h = extent(rows, dim, ld_hidden, es), n_w = extent(vocab, dim, ld_weight, es), n_t = dev_tokens ? (size_t)rows * token_bytes : 0,
                  n_st = dev_status ? 4 : 0;
     auto in_scratch = [&](const void* p, size_t n) { return overlap(p, p ? n : 0, dev_scratch, scratch_bytes); };
@@ -406,7 +452,7 @@ int pb_head_logprob_backward(const void* dev_hidden, const void* dev_weight, int
     if (!aligned(dev_scratch, 256)) return refuse(who, "scratch must be 256-byte aligned");
     const bool direct = direct_rows(dev_hidden, rows, ld_hidden) && direct_rows(dev_weight, vocab, ld_weight);
     const HeadPlan e = head_plan(dtype, rows, vocab, dim, direct, true, (char*)dev_scratch);
-    if (scratch_bytes < e.bytes) return refuse(who, "scratch is smaller than pb_head_scratch_bytes");
+    if (scratch_bytes < std::max(e.bytes, head_bytes(dtype, rows, vocab, dim, direct, true))) return refuse(who, "scratch is smaller than pb_head_scratch_bytes");
     struct Span { const void* p; size_t n; };
     const size_t nr4 = (size_t)rows * 4;
     const Span read[] = {{dev_hidden, extent(rows, dim, ld_hidden, es)}, {dev_weight, extent(vocab, dim, ld_weight, es)},

@@ -461,7 +461,7 @@ int pb_join_forward(const pb_join_args* args, void* stream);
  * They are written, not added to.  Sums over rows are float32, in an order that depends on the sizes alone.  dx may
  * be the very buffer of dy, du that of dh.  dev_scratch: pb_join_scratch_bytes(rows, dim, rows_per_gate, or 0 without a
  * gate) bytes, 256-byte aligned, not used by another call that may run at the same time (two captured
- * graphs included).  Buffers that overlap otherwise are PB_E_ARG. */
+ * graphs included); a size serves fewer rows too.  Buffers that overlap otherwise are PB_E_ARG. */
 typedef struct {
     const void* dy; int64_t ld_dy;
     const void* dh; int64_t ld_dh;

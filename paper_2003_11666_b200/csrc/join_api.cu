@@ -85,6 +85,17 @@ JoinPlan join_plan(int64_t rows, int64_t dim, int64_t rows_per_gate, char* scrat
     return e;
 }
 
+// Scratch of a gradient of `rows` rows or fewer, which can need more: their chunks are shorter.
+size_t join_bytes(int64_t rows, int64_t dim, int64_t rows_per_gate) {
+    const JoinPlan e = join_plan(rows, dim, rows_per_gate, nullptr);
+    const int64_t most = kSms * std::max<int64_t>(1, 768 / e.threads), blocks = std::min(most, (rows + e.slots - 1) / e.slots);
+    const int64_t turns = most * e.slots * kJoinTurns;
+    // Rows of n times `turns` come in chunks of n: as many as turns and one for each gate, no more than rows; none where a gate has no more than n.
+    const int64_t split = rows_per_gate > 1 ? std::min(rows, std::min(rows_per_gate, rows) * turns) : 0;
+    const int64_t chunks = split > 1 ? std::min(split, turns + (split + rows_per_gate - 1) / rows_per_gate) : 0;
+    return (size_t)(2 * ((blocks * dim * 4 + 255) / 256 * 256) + (chunks * dim * 4 + 255) / 256 * 256);
+}
+
 // Share of the elements that is dropped, in units of 2^-16; false if p is no such share.
 bool share_of(double p, unsigned& drop) {
     if (!(p >= 0.0) || !(p < 1.0)) return false;
@@ -187,7 +198,7 @@ int pb_dropout(const void* dev_x, int dtype, int64_t rows, int64_t dim, int64_t 
 
 size_t pb_join_scratch_bytes(int64_t rows, int64_t dim, int64_t rows_per_gate) {
     if (rows < 0 || rows > kMaxJoinRows || dim < 1 || dim > kMaxJoinDim || rows_per_gate < 0) return 0;
-    return join_plan(std::max<int64_t>(rows, 1), dim, rows_per_gate, nullptr).bytes;
+    return join_bytes(std::max<int64_t>(rows, 1), dim, rows_per_gate);
 }
 
 int pb_join_forward(const pb_join_args* args, void* stream) {
@@ -287,7 +298,7 @@ int pb_join_backward(const pb_join_args* args, const pb_join_grads* grads, void*
     }
     if (!aligned(dev_scratch, 256)) return refuse(who, "scratch must be 256-byte aligned");
     const JoinPlan e = join_plan(a.rows, a.dim, a.gate ? a.rows_per_gate : 0, (char*)dev_scratch);
-    if (scratch_bytes < e.bytes) return refuse(who, "scratch is smaller than pb_join_scratch_bytes");
+    if (scratch_bytes < std::max(e.bytes, join_bytes(a.rows, a.dim, a.gate ? a.rows_per_gate : 0))) return refuse(who, "scratch is smaller than pb_join_scratch_bytes");
     const int64_t gates = a.gate ? (a.rows + a.rows_per_gate - 1) / a.rows_per_gate : 0;
     const size_t nr = (size_t)a.rows * 4, nw = (size_t)a.dim * ws;
     const Span in[] = {{d.dy, extent(a.rows, a.dim, d.ld_dy, ss), d.ld_dy, a.stream_dtype}, {d.dh, extent(a.rows, a.dim, d.ld_dh, es), d.ld_dh, a.dtype},

@@ -314,8 +314,8 @@ cudaError_t few_rows(const HeadPlan& e, const void* hidden, const void* weight, 
                         (long long)ldw, tokens, token_bytes, c, e.part, e.ztok);
 }
 
-// Rows that a bulk copy can start on.
-bool direct_rows(const void* p, int64_t rows, int64_t ld) { return aligned(p, 16) && (ld % 8 == 0 || rows == 1); }
+// Rows that start on 16 bytes: a bulk copy can start on them, and a load of 16 bytes.
+bool direct_rows(const void* p, int64_t rows, int64_t ld, size_t es) { return aligned(p, 16) && (ld * (int64_t)es % 16 == 0 || rows == 1); }
 
 int no_map(const char* who) {
     char text[128];
@@ -362,7 +362,7 @@ int pb_head_logprob_forward(const void* dev_hidden, const void* dev_weight, int 
     if (!aligned(dev_hidden, es) || !aligned(dev_weight, es) || (dev_tokens && !aligned(dev_tokens, token_bytes)) || !aligned(dev_logp, 4) ||
         !aligned(dev_entropy, 4) || !aligned(dev_lse, 4) || !aligned(dev_status, 4)) return refuse(who, "a pointer is not aligned to its element");
     if (!aligned(dev_scratch, 256)) return refuse(who, "scratch must be 256-byte aligned");
-    const bool direct = direct_rows(dev_hidden, rows, ld_hidden) && direct_rows(dev_weight, vocab, ld_weight);
+    const bool direct = direct_rows(dev_hidden, rows, ld_hidden, es) && direct_rows(dev_weight, vocab, ld_weight, es);
     const HeadPlan e = head_plan(dtype, rows, vocab, dim, direct, false, (char*)dev_scratch);
     if (scratch_bytes < std::max(e.bytes, head_bytes(dtype, rows, vocab, dim, direct, false))) return refuse(who, "scratch is smaller than pb_head_scratch_bytes");
     const size_t n_h = extent(rows, dim, ld_hidden, es), n_w = extent(vocab, dim, ld_weight, es), n_t = dev_tokens ? (size_t)rows * token_bytes : 0,
@@ -450,7 +450,7 @@ int pb_head_logprob_backward(const void* dev_hidden, const void* dev_weight, int
         !aligned(dev_entropy, 4) || !aligned(dev_g_logp, 4) || !aligned(dev_g_entropy, 4) || !aligned(dev_g_lse, 4) || !aligned(dev_dhidden, es) ||
         !aligned(dev_dweight, gs) || !aligned(dev_status, 4)) return refuse(who, "a pointer is not aligned to its element");
     if (!aligned(dev_scratch, 256)) return refuse(who, "scratch must be 256-byte aligned");
-    const bool direct = direct_rows(dev_hidden, rows, ld_hidden) && direct_rows(dev_weight, vocab, ld_weight);
+    const bool direct = direct_rows(dev_hidden, rows, ld_hidden, es) && direct_rows(dev_weight, vocab, ld_weight, es);
     const HeadPlan e = head_plan(dtype, rows, vocab, dim, direct, true, (char*)dev_scratch);
     if (scratch_bytes < std::max(e.bytes, head_bytes(dtype, rows, vocab, dim, direct, true))) return refuse(who, "scratch is smaller than pb_head_scratch_bytes");
     struct Span { const void* p; size_t n; };

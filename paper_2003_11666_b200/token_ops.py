@@ -201,7 +201,7 @@ def head_scratch_bytes(hidden, weight, backward=False):
     if not isinstance(hidden, torch.Tensor) or not isinstance(weight, torch.Tensor):
         _refuse(who, "hidden and weight must be tensors")
     rows, vocab, dim, ldh, ldw, dtype = _head(who, hidden, weight)
-    whole = all(t.data_ptr() % 16 == 0 and (n <= 1 or ld % 8 == 0) for t, n, ld in ((hidden, rows, ldh), (weight, vocab, ldw)))
+    whole = all(t.data_ptr() % 16 == 0 and (n <= 1 or ld * t.element_size() % 16 == 0) for t, n, ld in ((hidden, rows, ldh), (weight, vocab, ldw)))
     n = _lib.pb_head_scratch_bytes(dtype, rows, vocab, dim, int(whole), int(bool(backward)))
     if n == 0:
         _refuse(who, "sizes out of range")

@@ -377,7 +377,7 @@ int pb_head_logprob_forward(const void* dev_hidden, const void* dev_weight, int 
         cudaError_t err = few(e, dev_hidden, dev_weight, rows, vocab, dim, ld_hidden, ld_weight, dev_tokens, token_bytes, c, s);
         if (err == cudaSuccess)
             err = launch_after(head_rows_kernel, dim3((unsigned)rows), kHeadRowThreads, s, e.part, (int)e.parts, (int)rows, 1, e.ztok, dev_tokens, token_bytes,
-                               (long long)vocab, c, (int)(dev_entropy != nullptr), dev_logp, dev_entropy, dev_lse, dev_status);
+                               (long long)vocab, c, inv_temperature / c, (int)(dev_entropy != nullptr), dev_logp, dev_entropy, dev_lse, dev_status);
         return launched(who, err);
     }
     HeadMatrix hidden, b;
@@ -415,7 +415,7 @@ int pb_head_logprob_forward(const void* dev_hidden, const void* dev_weight, int 
         auto at = [&](float* p) { return p ? p + r0 : nullptr; };
         if (err == cudaSuccess)
             err = launch_after(head_rows_kernel, dim3((unsigned)((nr + width - 1) / width)), kHeadRowThreads, s, e.part, (int)e.parts, (int)nr, width, e.ztok, g.tokens,
-                         token_bytes, (long long)vocab, g.c, g.entropy, at(dev_logp), at(dev_entropy), at(dev_lse), dev_status);
+                         token_bytes, (long long)vocab, g.c, inv_temperature / g.c, g.entropy, at(dev_logp), at(dev_entropy), at(dev_lse), dev_status);
     }
     return launched(who, err);
 }
@@ -467,7 +467,8 @@ int pb_head_logprob_backward(const void* dev_hidden, const void* dev_weight, int
         for (int l = 0; l < k; ++l)
             if (written[l].p && overlap(written[k].p, written[k].n, written[l].p, written[l].n)) return refuse(who, "buffers overlap");
     }
-    cudaError_t err = launch_after(head_coef_kernel, dim3(1), 1024, s, (int)rows, (long long)vocab, dev_tokens, token_bytes, inv_temperature, dev_lse, dev_entropy,
+    const float c2 = (float)(inv_temperature * 1.4426950408889634074);         // of logits, in units of log 2
+    cudaError_t err = launch_after(head_coef_kernel, dim3(1), 1024, s, (int)rows, (long long)vocab, dev_tokens, token_bytes, inv_temperature, c2, dev_lse, dev_entropy,
                                    dev_g_logp, dev_g_entropy, dev_g_lse, dtype == PB_F16 ? 16384.f : 1.f, e.coef, e.row_token, e.unscale, e.d_scale, e.col_most,
                                    (int)(e.f32 ? e.pieces : 0), dev_status);
     HeadMatrix hidden, w;
@@ -485,7 +486,7 @@ int pb_head_logprob_backward(const void* dev_hidden, const void* dev_weight, int
     g.d_scale = e.d_scale;
     g.store_near = dev_dhidden != nullptr;
     g.store_wide = dev_dweight != nullptr;
-    g.c = (float)(inv_temperature * 1.4426950408889634074);
+    g.c = c2;
     g.status = dev_status;
     g.coef = e.coef;
     g.row_token = e.row_token;

@@ -990,11 +990,11 @@ __global__ void __launch_bounds__(32 * kHeadFewWarps, kRows == 4 ? 2 : kHeadFewB
     }
 }
 
-// Row values from the parts' statistics: kHeadRowThreads threads for `width` rows, which share a row's parts.  The largest reference is
+// Row values from the parts' statistics (logits times c; unit: inv_temperature / c): kHeadRowThreads threads for `width` rows, which share a row's parts.  The largest reference is
 // found first, so that the terms of the sums do not wait for one another.
 constexpr int kHeadRowThreads = 512;
 __global__ void __launch_bounds__(kHeadRowThreads) head_rows_kernel(const float* part, int parts, int rows, int width, const float* ztok, const void* tokens,
-                                                                    int token_bytes, long long vocab, float c, int with_entropy, float* logp, float* entropy, float* lse,
+                                                                    int token_bytes, long long vocab, float c, double unit, int with_entropy, float* logp, float* entropy, float* lse,
                                                                     int* status) {
     __shared__ float sm[2][kHeadRowThreads];
     const int tid = threadIdx.x, lane = tid % width, share = tid / width, shares = kHeadRowThreads / width;
@@ -1033,7 +1033,8 @@ __global__ void __launch_bounds__(kHeadRowThreads) head_rows_kernel(const float*
     if (share != 0 || r >= rows) return;
     sum = sm[0][tid]; elog = sm[1][tid];
     const double ln2 = 0.69314718055994530942, ls = log((double)sum);
-    if (lse) lse[r] = sum == 0.f ? -INFINITY : (float)((double)base * ln2 + ls);
+    // The reference goes back to the logit that it is of by what that has been multiplied with, a float32 (logits of 4000 would be off by 5e-5 otherwise).
+    if (lse) lse[r] = sum == 0.f ? -INFINITY : (float)((double)base * unit + ls);
     if (entropy) entropy[r] = sum == 0.f ? 0.f : (float)(ls - ln2 * (double)elog / (double)sum);
     if (logp) {
         const long long id = token_bytes == 8 ? token_id((const long long*)tokens, r, vocab, status) : token_id((const int*)tokens, r, vocab, status);
@@ -1043,7 +1044,7 @@ __global__ void __launch_bounds__(kHeadRowThreads) head_rows_kernel(const float*
 }
 
 // Coefficients of d for every row, and the power of two that brings the largest to `top`: one block.
-__global__ void __launch_bounds__(1024) head_coef_kernel(int rows, long long vocab, const void* tokens, int token_bytes, double it, const float* lse,
+__global__ void __launch_bounds__(1024) head_coef_kernel(int rows, long long vocab, const void* tokens, int token_bytes, double it, float c, const float* lse,
                                                          const float* entropy, const float* g_logp, const float* g_entropy, const float* g_lse, float top,
                                                          HeadRow* coef, int* row_token, float* unscale, float* d_scale, int* col_most,
                                                          int pieces, int* status) {
@@ -1059,9 +1060,14 @@ __global__ void __launch_bounds__(1024) head_coef_kernel(int rows, long long voc
         const float ge = g_entropy && !none ? (float)(it * g_entropy[r]) : 0.f;
         const float gz = g_lse && !none ? (float)(it * g_lse[r]) : 0.f;
         h.a = a;
-        h.c0 = gz - a - (ge != 0.f ? ge * entropy[r] : 0.f);
+        // Logits are multiplied by a float32 c, so lse is by the same number over it: what c is off by then counts for their difference alone.  What lse2 leaves of
+        // it goes into the factors of p and p log2 p (logits near 130: 5e-6 of p without).
+        const double l = (double)z * ((double)c / it);
+        h.lse2 = none ? INFINITY : (float)l;
+        const float rest = fabsf(h.lse2) < 0x1p30f ? (float)((double)h.lse2 - l) : 0.f, f = exp2f(rest);      // (beyond that no difference is left)
         h.c1 = -ge * 0.69314718055994531f;
-        h.lse2 = none ? INFINITY : (float)((double)z * 1.4426950408889634074);
+        h.c0 = f * fmaf(h.c1, rest, gz - a - (ge != 0.f ? ge * entropy[r] : 0.f));
+        h.c1 *= f;
         return (int)id;
     };
     float m = 0.f;

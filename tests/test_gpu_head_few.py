@@ -4,6 +4,7 @@ import torch
 
 pytestmark = pytest.mark.gpu
 
+
 def _values(h, w, tok):
     import paper_2003_11666_b200 as p
     out = [torch.empty(h.shape[0], device="cuda") for _ in range(3)]

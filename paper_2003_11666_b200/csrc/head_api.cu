@@ -469,7 +469,7 @@ int pb_head_logprob_backward(const void* dev_hidden, const void* dev_weight, int
     }
     const float c2 = (float)(inv_temperature * 1.4426950408889634074);         // of logits, in units of log 2
     cudaError_t err = launch_after(head_coef_kernel, dim3(1), 1024, s, (int)rows, (long long)vocab, dev_tokens, token_bytes, inv_temperature, c2, dev_lse, dev_entropy,
-                                   dev_g_logp, dev_g_entropy, dev_g_lse, dtype == PB_F16 ? 16384.f : 1.f, e.coef, e.row_token, e.unscale, e.d_scale, e.col_most,
+                                   dev_g_logp, dev_g_entropy, dev_g_lse, dtype == PB_F16 ? 14 : 0, e.coef, e.row_token, e.unscale, e.d_scale, e.col_most,
                                    (int)(e.f32 ? e.pieces : 0), dev_status);
     HeadMatrix hidden, w;
     if (err == cudaSuccess) err = hidden_of(hidden, e, dtype, dev_hidden, rows, dim, ld_hidden, s);

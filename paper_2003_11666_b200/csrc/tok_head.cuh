@@ -1043,9 +1043,10 @@ __global__ void __launch_bounds__(kHeadRowThreads) head_rows_kernel(const float*
     }
 }
 
-// Coefficients of d for every row, and the power of two that brings the largest to `top`: one block.
+// Coefficients of d for every row, and the power of two that brings the largest to 2^top: one block.  Powers up to 149, what float32's smallest numbers ask for
+// at a top of 0, whose inverse float32 still holds.
 __global__ void __launch_bounds__(1024) head_coef_kernel(int rows, long long vocab, const void* tokens, int token_bytes, double it, float c, const float* lse,
-                                                         const float* entropy, const float* g_logp, const float* g_entropy, const float* g_lse, float top,
+                                                         const float* entropy, const float* g_logp, const float* g_entropy, const float* g_lse, int top,
                                                          HeadRow* coef, int* row_token, float* unscale, float* d_scale, int* col_most,
                                                          int pieces, int* status) {
     __shared__ float most[32];
@@ -1085,13 +1086,15 @@ __global__ void __launch_bounds__(1024) head_coef_kernel(int rows, long long voc
     m = most[tid & 31];
 #pragma unroll
     for (int k = 16; k; k >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, k));
-    int e = 0;
-    if (m > 0.f) frexpf(top / m, &e);                         // 2^(e - 1) <= top / m
-    e = min(max(e - 1, -120), 120);
-    const float f = ldexpf(1.f, e);
+    int e = top;
+    if (m > 0.f) {
+        const bool power = frexpf(m, &e) == 0.5f;             // m < 2^e, or 2^(e - 1)
+        e = top - e + power;
+    }
+    e = min(max(e, -120), 149);
     for (int r = tid; r < rows; r += 1024) {
         HeadRow h = coef[r];
-        h.a *= f; h.c0 *= f; h.c1 *= f;
+        h.a = ldexpf(h.a, e); h.c0 = ldexpf(h.c0, e); h.c1 = ldexpf(h.c1, e);
         coef[r] = h;
         if (d_scale) {                                        // brings the row's own largest to between 2^13 and 2^14
             const float s = fabsf(h.a) + fabsf(h.c0) + fabsf(h.c1);
@@ -1121,10 +1124,10 @@ __global__ void __launch_bounds__(256) head_sum_kernel(const float* plane, long 
 #pragma unroll
             for (int u = 0; u < 8; ++u) s[u] += v[u];
         }
-        const float own = d_scale ? f / d_scale[r] : f;
+        const float own = d_scale ? 1.f / d_scale[r] : 1.f;      // (its product with f may be below float32's numbers)
 #pragma unroll
         for (int u = 0; u < 8; ++u)
-            if (c + u < dim) out[r * ldo + c + u] = from_f32<T>(s[u] * own);
+            if (c + u < dim) out[r * ldo + c + u] = from_f32<T>(s[u] * own * f);
     }
 }
 

@@ -38,6 +38,8 @@ _current_device, _current = torch._C._cuda_getDevice, torch._C._cuda_getCurrentR
 _address, _numel, _get_device, _is_contiguous = torch.Tensor.data_ptr, torch.Tensor.numel, torch.Tensor.get_device, torch.Tensor.is_contiguous
 
 _OFF_DEVICE = "every tensor must be a CUDA tensor on the current device"
+_NOT_THAT = "an argument is not what it has to be: tensors on the current device, and numbers"
+_MISFITS = (AttributeError, TypeError, OverflowError, struct.error, C.ArgumentError)      # what such an argument raises on its way to the C call
 
 
 def _on_device(who, device, *tensors):
@@ -222,10 +224,14 @@ def head_logprob_forward(hidden, weight, scratch, tokens=None, logp=None, entrop
             _refuse(who, "tokens must hold one id per row")
     if (tokens is None) != (logp is None):
         _refuse(who, "logp and tokens go together")
-    _check(_lib.pb_head_logprob_forward(
-        hidden.data_ptr(), weight.data_ptr(), dtype, rows, vocab, dim, ldh, ldw, p, size, inv_temperature, _vector(who, "logp", logp, rows),
-        _vector(who, "entropy", entropy, rows), _vector(who, "lse", lse, rows), *_scratch(who, scratch), _status(who, status),
-        _current(d) if stream is None else stream))
+    try:
+        rc = _lib.pb_head_logprob_forward(
+            hidden.data_ptr(), weight.data_ptr(), dtype, rows, vocab, dim, ldh, ldw, p, size, inv_temperature, _vector(who, "logp", logp, rows),
+            _vector(who, "entropy", entropy, rows), _vector(who, "lse", lse, rows), *_scratch(who, scratch), _status(who, status),
+            _current(d) if stream is None else stream)
+    except _MISFITS:
+        _refuse(who, _NOT_THAT)
+    _check(rc)
 
 
 def head_logprob_backward(hidden, weight, scratch, tokens, lse, dhidden=None, dweight=None, g_logp=None, g_entropy=None, entropy=None, g_lse=None,
@@ -252,11 +258,15 @@ def head_logprob_backward(hidden, weight, scratch, tokens, lse, dhidden=None, dw
         if (r, c) != (vocab, dim):
             _refuse(who, "dweight must have the weight's shape")
         dw_type = _DTYPE[dweight.dtype]
-    _check(_lib.pb_head_logprob_backward(
-        hidden.data_ptr(), weight.data_ptr(), dtype, rows, vocab, dim, ldh, ldw, p, size, inv_temperature, _vector(who, "lse", lse, rows),
-        _vector(who, "entropy", entropy, rows), _vector(who, "g_logp", g_logp, rows), _vector(who, "g_entropy", g_entropy, rows),
-        _vector(who, "g_lse", g_lse, rows), None if dhidden is None else dhidden.data_ptr(), ld_dh, None if dweight is None else dweight.data_ptr(), dw_type,
-        ld_dw, 1 if accumulate else 0, *_scratch(who, scratch), _status(who, status), _current(d) if stream is None else stream))
+    try:
+        rc = _lib.pb_head_logprob_backward(
+            hidden.data_ptr(), weight.data_ptr(), dtype, rows, vocab, dim, ldh, ldw, p, size, inv_temperature, _vector(who, "lse", lse, rows),
+            _vector(who, "entropy", entropy, rows), _vector(who, "g_logp", g_logp, rows), _vector(who, "g_entropy", g_entropy, rows),
+            _vector(who, "g_lse", g_lse, rows), None if dhidden is None else dhidden.data_ptr(), ld_dh, None if dweight is None else dweight.data_ptr(), dw_type,
+            ld_dw, 1 if accumulate else 0, *_scratch(who, scratch), _status(who, status), _current(d) if stream is None else stream)
+    except _MISFITS:
+        _refuse(who, _NOT_THAT)
+    _check(rc)
 
 
 # pb_join_args and pb_join_grads in their own order: one call lays all fields out, where setting them one by one takes as long as the launch.
@@ -302,9 +312,6 @@ def _join_gate(who, gate, rows_per_gate, rows, dim, dtype, device):
     return *_plane(who, "gate", gate, (-(-rows // per), dim), dtype, device), per
 
 
-_NOT_THAT = "an argument is not what it has to be: tensors on the current device, and numbers"
-
-
 def dropout(x, out, p, seed, offset=0, dev_offset=None, stream=None):
     """pb_dropout: out = x / (1 - p) where kept, else 0; of matrices [rows, dim].  The gradient is the same call on out's gradient."""
     who = "dropout"
@@ -316,9 +323,11 @@ def dropout(x, out, p, seed, offset=0, dev_offset=None, stream=None):
         px, ld = _plane(who, "x", x, shape, dtype, d)
         po, ld_out = _plane(who, "out", out, shape, dtype, d)
         at = None if dev_offset is None else _line(who, "dev_offset", dev_offset, 1, torch.int64, d)
+        if not -1 << 63 <= offset < 1 << 63:                     # ctypes would drop the bits above
+            _refuse(who, "offset must be a 64-bit integer")
         rc = _lib.pb_dropout(px, _DTYPE[dtype], shape[0], shape[1], ld, p, seed & 0xFFFFFFFFFFFFFFFF, offset, at, po, ld_out,
                              _current(d) if stream is None else stream)
-    except (AttributeError, TypeError, C.ArgumentError):
+    except _MISFITS:
         _refuse(who, _NOT_THAT)
     _check(rc)
 
@@ -345,9 +354,10 @@ def join_forward(x, u, y, h=None, pre_weight=None, post_weight=None, gate=None, 
             0 if dev_offset is None else _line(who, "dev_offset", dev_offset, 1, torch.int64, d), px, ld_x, pu, ld_u, pg, ld_g, per,
             _line(who, "post_weight", post_weight, dim, weights, d), _line(who, "pre_weight", pre_weight, dim, weights, d), py, ld_y, ph, ld_h,
             _line(who, "rstd_post", rstd_post, rows, f32, d), _line(who, "rstd_pre", rstd_pre, rows, f32, d))
-    except (AttributeError, TypeError, struct.error):
+        rc = _lib.pb_join_forward(args, _current(d) if stream is None else stream)
+    except _MISFITS:
         _refuse(who, _NOT_THAT)
-    _check(_lib.pb_join_forward(args, _current(d) if stream is None else stream))
+    _check(rc)
 
 
 def join_scratch_bytes(rows, dim, rows_per_gate=0):
@@ -394,9 +404,10 @@ def join_backward(y, u, dx, du, scratch, dy=None, dh=None, pre_weight=None, post
         if scratch.get_device() != d:
             _refuse(who, _OFF_DEVICE)
         room, size = _scratch(who, scratch)
-    except (AttributeError, TypeError, struct.error):
+        rc = _lib.pb_join_backward(args, out, room, size, _current(d) if stream is None else stream)
+    except _MISFITS:
         _refuse(who, _NOT_THAT)
-    _check(_lib.pb_join_backward(args, out, room, size, _current(d) if stream is None else stream))
+    _check(rc)
 
 
 def adamw_moments(m, m_scale, v, v_scale, m_out=None, v_out=None, stream=None):

@@ -39,11 +39,11 @@ namespace pb {
 
 constexpr int kHeadChunk = 64;                // K elements per stage: one 128-byte swizzled row
 constexpr int kHeadOperand = 128 * 128;       // bytes of an operand's 128 x 64 tile
-constexpr int kHeadMaxStages = 12;
+constexpr int kHeadMaxStages = 11;
 constexpr int kHeadBuf = 32 * 128;            // bytes of an epilogue warp's buffer: 128 of each of its rows
 constexpr int kHeadEpi = 8;                   // epilogue warps: quarter w % 4 of the tensor-memory lanes, half w / 4 of the columns
 constexpr int kHeadThreads = 32 * (kHeadEpi + 2);
-constexpr int kHeadRing = 196608;             // bytes for the stages: six of 32 KB; three with two planes of each operand, two with three; twelve with A
+constexpr int kHeadRing = 196608;             // bytes for the stages: six of 32 KB; three with two planes of each operand, two with three; eleven with A
                                               // tiles of up to eight rows
 constexpr int kHeadSmem = 1024 + kHeadRing + kHeadEpi * kHeadBuf;
 constexpr int kHeadWide = 3, kHeadNear = 2;  // bfloat16 and float16 planes of a float32 operand

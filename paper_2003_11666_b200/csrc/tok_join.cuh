@@ -11,8 +11,8 @@
 // In dy' = e - m1 yn, with e = dy + rstd_pre dh pre and m1 = rstd_pre mean(dh pre yn), the second mean is that of keep gate post un e less m1 times
 // that of keep gate post un yn, so that the threads of a row meet once for three sums instead of twice for one.
 //
-// Everything is bound by the rows' bytes.  A row is held in registers by a group of threads (a power of two, kUnits pieces
-// of eight columns each), so that it is read and written once; its two sums are the only thing that the threads of a
+// Everything is bound by the rows' bytes.  A row is held in registers by a group of threads (up to a warp a power of two, else whole warps; kUnits
+// pieces of eight columns each), so that it is read and written once; its two sums are the only thing that the threads of a
 // group exchange.  In the backward a thread keeps the same columns in every row, so that the sums over rows
 // stay in its registers; they end in one partial sum per block, and in one per chunk of rows that share a gate.
 #pragma once
@@ -720,7 +720,7 @@ __global__ void __launch_bounds__(kThreads, kThreads <= 256 ? 512 / kThreads : 1
             }
             if (p.dh || p.post) row_sums(s1, s2, s3, blockDim.x, sm[turn]);
             const float m1 = -rr * p.inv_dim * s1, m2 = -rp * p.inv_dim * fmaf(m1, s3, s2);
-            if (!(p.dh || p.post) || blockDim.x == 32) __syncthreads();
+            if (!(p.dh || p.post)) __syncthreads();               // (a row in the ring has more threads than a warp)
             if (ring.fail[turn]) break;
             if (lane == 0) ask();                             // all have read this row: another may have its place
             if (++get == p.depth) { get = 0; phase ^= 1; }

@@ -1038,7 +1038,7 @@ __global__ void __launch_bounds__(kHeadRowThreads) head_rows_kernel(const float*
     if (entropy) entropy[r] = sum == 0.f ? 0.f : (float)(ls - ln2 * (double)elog / (double)sum);
     if (logp) {
         const long long id = token_bytes == 8 ? token_id((const long long*)tokens, r, vocab, status) : token_id((const int*)tokens, r, vocab, status);
-        // the token's logit against the reference as the sum has it, so that a sure token's value keeps its digits
+        // the token's logit against the reference as the sum has it, so that a sure token's value is off by the last digit of a sum near 1 at most
         logp[r] = id < 0 ? (sum == sum ? 0.f : sum) : sum == 0.f ? -INFINITY : (float)(ln2 * ((double)ztok[r] * (double)c - (double)base) - ls);
     }
 }

@@ -60,3 +60,25 @@ def test_sums_of_a_few_rows_round_to_nearest(dim, rows, dtype):
     tol = 6 * spread + U * ref + 2.0 ** -22 + 2 * U * 32 + 10 * U
     err = (lse.double() - ref).abs()
     assert bool((err <= tol).all()), (err / tol).tolist()
+
+
+# float32 operands that run on the tensor cores: single blocks and pairs
+@pytest.mark.parametrize("rows", [5, 150])
+@pytest.mark.parametrize("dim", [256, 1024, 2048])
+def test_float32_sums_drift_by_no_more_than_a_few_steps(dim, rows):
+    # terms of one sign again.  What a step of the tensor core's sum drops is half of the sum's last place on average, and a sum leaves it after 24 steps at most:
+    # it grows by a 24th of itself with each
+    part = torch.arange(1, 25, dtype=torch.float64) / 24
+    g = torch.Generator(device="cuda").manual_seed(dim + rows)
+    h, w = ((torch.rand(n, dim, generator=g, device="cuda") + 0.5) for n in (rows, 4096))
+    scale = 102.4 / dim
+    z = h.double() @ w.double().T * scale
+    tok = torch.randint(0, 4096, (rows,), generator=g, device="cuda")
+    _, _, lse = _values(h, w, tok, scale)
+    ref = z.logsumexp(1)
+    per_part = 128.0                                                # a part is the sum of 128 columns of numbers near 1, of any binade's place
+    drift = 0.5 * 2.0 ** -23 * float((2.0 ** torch.floor(torch.log2(part * per_part))).sum()) / per_part
+    # 1.6 times that for logits that differ from the mean, and lse's own: see above
+    tol = 1.6 * drift * z.mean(1) + U * ref + 2.0 ** -22 + 2 * U * 32 + 10 * U
+    err = (lse.double() - ref).abs()
+    assert bool((err <= tol).all()), ((err / tol).max(), drift)

@@ -380,7 +380,7 @@ int pb_head_logprob_forward(const void* dev_hidden, const void* dev_weight, int 
         cudaError_t err = few(e, dev_hidden, dev_weight, rows, vocab, dim, ld_hidden, ld_weight, dev_tokens, token_bytes, c, s);
         if (err == cudaSuccess)
             err = launch_after(head_rows_kernel, dim3((unsigned)rows), kHeadRowThreads, s, e.part, (int)e.parts, (int)rows, 1, e.ztok, dev_tokens, token_bytes,
-                               (long long)vocab, c, inv_temperature / c, (int)(dev_entropy != nullptr), dev_logp, dev_entropy, dev_lse, dev_status);
+                               (long long)vocab, c, inv_temperature, (int)(dev_entropy != nullptr), dev_logp, dev_entropy, dev_lse, dev_status);
         return launched(who, err);
     }
     HeadMatrix hidden, b;
@@ -418,7 +418,7 @@ int pb_head_logprob_forward(const void* dev_hidden, const void* dev_weight, int 
         auto at = [&](float* p) { return p ? p + r0 : nullptr; };
         if (err == cudaSuccess)
             err = launch_after(head_rows_kernel, dim3((unsigned)((nr + width - 1) / width)), kHeadRowThreads, s, e.part, (int)e.parts, (int)nr, width, e.ztok, g.tokens,
-                         token_bytes, (long long)vocab, g.c, inv_temperature / g.c, g.entropy, at(dev_logp), at(dev_entropy), at(dev_lse), dev_status);
+                         token_bytes, (long long)vocab, g.c, inv_temperature, g.entropy, at(dev_logp), at(dev_entropy), at(dev_lse), dev_status);
     }
     return launched(who, err);
 }

@@ -85,7 +85,7 @@ struct alignas(64) HeadArgs {
     int col0;                    // first column (token) of this piece of the vocabulary
     int* status;
     // row statistics
-    float* part;                 // [3][parts][rows]: reference (log2), sum, sum of e log2 e
+    float* part;                 // [3][parts][rows]: HeadStat's
     int part0, parts, entropy;   // entropy: its sum is wanted, or its gradient given
     float* ztok;                 // the token's logit of each row
     const void* tokens;
@@ -366,10 +366,11 @@ __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
 // Exponents from here down give zero; a finite one, so that zero times it is zero too.  A NaN stays.
 __device__ __forceinline__ float head_floor(float t) { return max_nan(t, -1000.f); }
 
-// Statistics of one row's logits, in units of log 2 around a reference.
+// Statistics of one row's logits z: the largest, top; the sum of e = 2^(c (z - top)) less 1, over, so that where one token is all but sure what is left for the others
+// keeps its digits; and the sum of e log2 e.  Without a logit above -inf over is -1.
 struct HeadStat {
-    float ref, sum, elog;
-    __device__ __forceinline__ void start() { ref = -INFINITY; sum = elog = 0.f; }
+    float top, over, elog;
+    __device__ __forceinline__ void start() { top = -INFINITY; over = -1.f; elog = 0.f; }
     template <bool kEntropy> __device__ __forceinline__ void add(const float (&z)[64], float c) {
         float m0 = fmaxf(z[0], z[1]), m1 = fmaxf(z[2], z[3]);
 #pragma unroll
@@ -377,39 +378,54 @@ struct HeadStat {
             m0 = fmaxf(m0, fmaxf(z[u], z[u + 1]));
             m1 = fmaxf(m1, fmaxf(z[u + 2], z[u + 3]));
         }
-        const float now = fmaxf(ref, fmaxf(m0, m1) * c);     // c > 0
-        const float base = now == -INFINITY ? 0.f : now;
-        if (now > ref && ref != -INFINITY) {
-            const float shift = ref - now, f = exp2_near(shift);
-            if (kEntropy) elog = f * fmaf(shift, sum, elog);
-            sum *= f;
-        }
-        ref = now;
+        const float now = fmaxf(top, fmaxf(m0, m1)), base = now == -INFINITY ? 0.f : now;
         const Pair scale(c), from(-base);
         Pair s[2] = {Pair(0.f), Pair(0.f)}, l[2] = {Pair(0.f), Pair(0.f)};
 #pragma unroll
         for (int u = 0; u < 64; u += 2) {
             float a, b;
-            fma2(Pair(z[u], z[u + 1]), scale, from).split(a, b);
+            ((Pair(z[u], z[u + 1]) + from) * scale).split(a, b);
             if (kEntropy) { a = head_floor(a); b = head_floor(b); }
             const Pair e(exp2_near(a), exp2_near(b));
             s[u / 2 & 1] = s[u / 2 & 1] + e;
             if (kEntropy) l[u / 2 & 1] = fma2(e, Pair(a, b), l[u / 2 & 1]);
         }
-        float a, b;
+        float a, b, sum, log = 0.f;
         (s[0] + s[1]).split(a, b);
-        sum += a + b;
+        sum = a + b;
         if (kEntropy) {
-            (l[0] + l[1]).split(a, b);
-            elog += a + b;
+            (l[0] + l[1]).split(a, b);                        // the largest has no part in it: its log2 e is 0
+            log = a + b;
+        }
+        if (now > top) {
+            if (sum < 1.0625f) {                             // the others by themselves: the largest is alone
+                s[0] = s[1] = Pair(0.f);
+#pragma unroll
+                for (int u = 0; u < 64; u += 2) {
+                    ((Pair(z[u], z[u + 1]) + from) * scale).split(a, b);
+                    s[u / 2 & 1] = s[u / 2 & 1] + Pair(a == 0.f ? 0.f : exp2_near(a), b == 0.f ? 0.f : exp2_near(b));
+                }
+                (s[0] + s[1]).split(a, b);
+                sum = a + b;
+            } else {
+                sum -= 1.f;
+            }
+            const float d = fmaxf((top - now) * c, -1000.f), f = exp2_near(d), all = 1.f + over;
+            over = fmaf(f, all, sum);
+            if (kEntropy) elog = fmaf(f, fmaf(d, all, elog), log);
+            top = now;
+        } else {
+            over += sum;
+            elog += log;
         }
     }
-    __device__ __forceinline__ void join(float m, float s, float e) {
-        const float now = fmaxf(ref, m), base = now == -INFINITY ? 0.f : now;
-        const float d0 = fmaxf(ref - base, -1000.f), d1 = fmaxf(m - base, -1000.f), f = exp2_near(d0), h = exp2_near(d1);
-        elog = f * fmaf(d0, sum, elog) + h * fmaf(d1, s, e);
-        sum = fmaf(f, sum, h * s);
-        ref = now;
+    // Joins another's.
+    __device__ __forceinline__ void join(float m, float x, float l, float c) {
+        const bool first = top >= m;
+        const float d = fmaxf((first ? m - top : top - m) * c, -1000.f), f = exp2_near(d), all = 1.f + (first ? x : over);
+        elog = fmaf(f, fmaf(d, all, first ? l : elog), first ? elog : l);
+        over = fmaf(f, all, first ? over : x);
+        top = fmaxf(top, m);
     }
 };
 
@@ -679,16 +695,16 @@ __device__ void head_epilogue(const HeadArgs& g, HeadShared& sh, unsigned char* 
             float* meet = (float*)area + (i & 1) * (kParts - 1) * 384 + (warp & 3) * 32 + lane;
             if (part) {
                 float* m = meet + (part - 1) * 384;
-                m[0] = st.ref; m[128] = st.sum; m[256] = st.elog;
+                m[0] = st.top; m[128] = st.over; m[256] = st.elog;
             }
             asm volatile("bar.sync 1, %0;" ::"n"(128 * kParts) : "memory");
             if (!part && v.row < q.rows) {
 #pragma unroll
-                for (int k = 0; k < kParts - 1; ++k) st.join(meet[k * 384], meet[k * 384 + 128], meet[k * 384 + 256]);
+                for (int k = 0; k < kParts - 1; ++k) st.join(meet[k * 384], meet[k * 384 + 128], meet[k * 384 + 256], g.c);
                 float* p = g.part + (long long)(g.part0 + v.x.n) * q.rows + v.row;
                 const long long plane = (long long)g.parts * q.rows;
-                p[0] = st.ref;
-                p[plane] = st.sum;
+                p[0] = st.top;
+                p[plane] = st.over;
                 if (g.entropy) p[2 * plane] = st.elog;
             }
         }
@@ -957,89 +973,89 @@ __global__ void __launch_bounds__(32 * kHeadFewWarps, kRows == 4 ? 2 : kHeadFewB
                 for (int n = 16; n; n /= 2) a += __shfl_xor_sync(0xffffffffu, a, n);
                 if (r == mine) z[u] = a;
             }
-        float top = -INFINITY;
 #pragma unroll
         for (int u = 0; u < kCols; ++u) {
-            if (token == c0 + u && c0 + u < vocab && lane < rows) ztok[lane] = z[u];
-            if (c0 + u >= vocab) z[u] = -INFINITY;
-            top = fmaxf(top, z[u]);
-        }
-        const float now = fmaxf(st.ref, top * c), base = now == -INFINITY ? 0.f : now;      // c > 0
-        if (now > st.ref && st.ref != -INFINITY) {
-            const float shift = st.ref - now, f = exp2f(shift);
-            st.elog = f * fmaf(shift, st.sum, st.elog);
-            st.sum *= f;
-        }
-        st.ref = now;
-#pragma unroll
-        for (int u = 0; u < kCols; ++u) {
-            const float t = head_floor(fmaf(z[u], c, -base)), e = exp2f(t);
-            st.sum += e;
-            st.elog = fmaf(e, t, st.elog);
+            if (c0 + u >= vocab) break;
+            if (token == c0 + u && lane < rows) ztok[lane] = z[u];
+            const float total = 1.f + st.over;
+            if (z[u] > st.top) {
+                const float d = fmaxf((st.top - z[u]) * c, -1000.f), f = exp2f(d);
+                st.elog = f * fmaf(d, total, st.elog);
+                st.over = f * total;
+                st.top = z[u];
+            } else {
+                const float d = head_floor((z[u] - (st.top == -INFINITY ? 0.f : st.top)) * c), e = exp2f(d);
+                st.over += e;
+                st.elog = fmaf(e, d, st.elog);
+            }
         }
     }
     if (lane < kRows) all[warp][lane] = st;
     __syncthreads();
     if (threadIdx.x < rows) {
         st = all[0][threadIdx.x];
-        for (int k = 1; k < kHeadFewWarps; ++k) st.join(all[k][threadIdx.x].ref, all[k][threadIdx.x].sum, all[k][threadIdx.x].elog);
+        for (int k = 1; k < kHeadFewWarps; ++k) st.join(all[k][threadIdx.x].top, all[k][threadIdx.x].over, all[k][threadIdx.x].elog, c);
         const long long at = (long long)blockIdx.x * rows + threadIdx.x, plane = (long long)gridDim.x * rows;
-        part[at] = st.ref;
-        part[plane + at] = st.sum;
+        part[at] = st.top;
+        part[plane + at] = st.over;
         part[2 * plane + at] = st.elog;
     }
 }
 
-// Row values from the parts' statistics (logits times c; unit: inv_temperature / c): kHeadRowThreads threads for `width` rows, which share a row's parts.  The largest reference is
+// Row values from the parts' statistics (it: inv_temperature, c: over log 2): kHeadRowThreads threads for `width` rows, which share a row's parts.  The largest logit is
 // found first, so that the terms of the sums do not wait for one another.
 constexpr int kHeadRowThreads = 512;
 __global__ void __launch_bounds__(kHeadRowThreads) head_rows_kernel(const float* part, int parts, int rows, int width, const float* ztok, const void* tokens,
-                                                                    int token_bytes, long long vocab, float c, double unit, int with_entropy, float* logp, float* entropy, float* lse,
+                                                                    int token_bytes, long long vocab, float c, double it, int with_entropy, float* logp, float* entropy, float* lse,
                                                                     int* status) {
-    __shared__ float sm[2][kHeadRowThreads];
+    __shared__ float sm[3][kHeadRowThreads];
     const int tid = threadIdx.x, lane = tid % width, share = tid / width, shares = kHeadRowThreads / width;
     const int r = blockIdx.x * width + lane;
     const long long plane = (long long)parts * rows;
     cudaGridDependencySynchronize();
-    float ref = -INFINITY;
+    float top = -INFINITY;
     if (r < rows) {
 #pragma unroll 8
-        for (int k = share; k < parts; k += shares) ref = fmaxf(ref, part[(long long)k * rows + r]);
+        for (int k = share; k < parts; k += shares) top = fmaxf(top, part[(long long)k * rows + r]);
     }
-    sm[0][tid] = ref;
+    sm[0][tid] = top;
     for (int n = shares / 2; n; n /= 2) {
         __syncthreads();
         if (share < n) sm[0][tid] = fmaxf(sm[0][tid], sm[0][tid + n * width]);
     }
     __syncthreads();
-    ref = sm[0][lane];
-    const float base = ref == -INFINITY ? 0.f : ref;
-    float sum = 0.f, elog = 0.f;
+    top = sm[0][lane];
+    float at_top = 0.f, over = 0.f, elog = 0.f;              // parts that have the largest logit; the rest of their sums, and the others'
     if (r < rows) {
 #pragma unroll 8
         for (int k = share; k < parts; k += shares) {
             const float* p = part + (long long)k * rows + r;
-            const float m = p[0], s = p[plane], e = with_entropy ? p[2 * plane] : 0.f, d = m - base, f = exp2f(d);
-            sum = fmaf(f, s, sum);
-            elog += f != 0.f ? f * fmaf(d, s, e) : 0.f;       // a part that cannot occur is -inf away; a NaN goes on by the sum
+            const float m = p[0], x = p[plane], e = with_entropy ? p[2 * plane] : 0.f, d = fmaxf((m - top) * c, -1000.f), f = exp2f(d), all = 1.f + x;
+            const bool has = m == top;
+            at_top += has ? 1.f : 0.f;
+            over += has ? x : f * all;
+            elog += has ? e : f * fmaf(d, all, e);
         }
     }
     __syncthreads();
-    sm[0][tid] = sum; sm[1][tid] = elog;
+    sm[0][tid] = at_top; sm[1][tid] = over; sm[2][tid] = elog;
     for (int n = shares / 2; n; n /= 2) {
         __syncthreads();
-        if (share < n) { sm[0][tid] += sm[0][tid + n * width]; sm[1][tid] += sm[1][tid + n * width]; }
+        if (share < n) {
+#pragma unroll
+            for (int k = 0; k < 3; ++k) sm[k][tid] += sm[k][tid + n * width];
+        }
     }
     if (share != 0 || r >= rows) return;
-    sum = sm[0][tid]; elog = sm[1][tid];
-    const double ln2 = 0.69314718055994530942, ls = log((double)sum);
-    // The reference goes back to the logit that it is of by what that has been multiplied with, a float32 (logits of 4000 would be off by 5e-5 otherwise).
-    if (lse) lse[r] = sum == 0.f ? -INFINITY : (float)((double)base * unit + ls);
-    if (entropy) entropy[r] = sum == 0.f ? 0.f : (float)(ls - ln2 * (double)elog / (double)sum);
+    over = top == INFINITY ? __int_as_float(0x7fffffff) : sm[1][tid];
+    elog = sm[2][tid];
+    const double rest = (double)sm[0][tid] - 1.0 + (double)over, ls = log1p(rest);
+    const bool none = rest == -1.0;                          // no logit is above -inf
+    if (lse) lse[r] = none ? -INFINITY : (float)((double)top * it + ls);
+    if (entropy) entropy[r] = none ? 0.f : (float)(ls - 0.69314718055994530942 * (double)elog / (1.0 + rest));
     if (logp) {
         const long long id = token_bytes == 8 ? token_id((const long long*)tokens, r, vocab, status) : token_id((const int*)tokens, r, vocab, status);
-        // the token's logit against the reference as the sum has it, so that a sure token's value is off by the last digit of a sum near 1 at most
-        logp[r] = id < 0 ? (sum == sum ? 0.f : sum) : sum == 0.f ? -INFINITY : (float)(ln2 * ((double)ztok[r] * (double)c - (double)base) - ls);
+        logp[r] = id < 0 ? (rest == rest ? 0.f : (float)rest) : none ? -INFINITY : (float)(((double)ztok[r] - (double)top) * it - ls);
     }
 }
 

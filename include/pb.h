@@ -403,9 +403,11 @@ int pb_head_logprob_forward(const void* dev_hidden, const void* dev_weight, int 
  * dweight = d^T hidden (float32 or of `dtype`, row stride ld_dweight).  accumulate = 1 adds to the dweight that is
  * there (several batches; a table that is also the embedding, see pb_embed_backward).  Either
  * gradient may be NULL, not both.  d is formed for a piece of the vocabulary at a time and held in
- * the operands' type, scaled by a power of two so that it does not underflow: 16-bit operands give gradients whose terms are
- * off by up to 2^-8 (bfloat16) or 2^-11 (float16) of themselves, whatever the type of dweight; of float32 ones 2^-24, in dhidden also
- * 2^-37 of the row's largest coefficient times the largest weight.  rows == 0 clears dweight,
+ * the operands' type, scaled by one power of two for the call, which brings its largest coefficient near float16's largest number.  So
+ * 16-bit operands give gradients whose terms are off by up to 2^-8 (bfloat16) or 2^-11 (float16) of themselves, whatever the type of dweight, float16
+ * ones also by 2^-38 of the call's largest coefficient (a very improbable token, or a quiet row beside a loud one); of float32 ones
+ * 2^-24, in dhidden also 2^-37 of the row's largest coefficient times the largest weight.  The probabilities themselves are exp(z - lse) of the
+ * lse given, to 2^-21 and 2^-23 of z - lse, where the logits z are exact.  rows == 0 clears dweight,
  * or leaves it if accumulate.  PB_E_ARG if a buffer that is written overlaps another. */
 int pb_head_logprob_backward(const void* dev_hidden, const void* dev_weight, int dtype, int64_t rows, int64_t vocab, int64_t dim,
                              int64_t ld_hidden, int64_t ld_weight, const void* dev_tokens, int token_bytes, double inv_temperature,

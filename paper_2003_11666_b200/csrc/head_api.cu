@@ -31,8 +31,8 @@ constexpr int64_t kHeadStatRows = 8192;         // rows whose statistics are hel
 // Chunks of K that the tensor core adds up by itself.  It does not round to nearest, so its sums drift towards zero, with every step that it adds at full
 // size (four of a chunk; of float32 operands twelve or 24): log probabilities of normal logits are off by 6e-8 of themselves after 16 steps, 2e-7 after 64, 8e-7
 // after 256, 1.7e-6 after 512.
-// float32 operands: 24 steps (three terms) for logits and dhidden, 48 (six terms) for dweight, whose errors are those of d.  With 48, 24 or 12 for the logits the
-// forward of 509 x 50021 x 1001 takes 201, 219 or 268 us, and logits whose terms have one sign are off by 1.3e-6, 6e-7 or 3e-7 of themselves.  With 48 the
+// float32 operands: 24 steps (three terms) for logits and dhidden, 48 (six terms) for dweight, whose errors are those of d.  With 24 or 12 for the logits the
+// forward of 509 x 50021 x 1001 takes 9 or 34 % longer than with 48, and logits whose terms have one sign are off by 6e-7 or 3e-7 of themselves instead of 1.3e-6.  With 48 the
 // gradients at low temperatures were several times as far off as those of float32 products; with 24 they are about as far.
 constexpr int kHeadPromoteNear = 2, kHeadPromoteWide = 2;
 constexpr int kHeadPromoteLong = 16;            // 16-bit ones of more than kHeadLong chunks in the forward: 4096 x 131072 x 4096 takes 3.50 ms, as it

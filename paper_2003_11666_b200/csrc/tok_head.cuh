@@ -23,13 +23,13 @@
 // counts (the logits; dhidden, a sum over tokens), two float16 planes do: x = 2^k (x0 + x1) to 2^-24 of x or 2^-39 of the largest number
 // that shares k (a row of hidden states, 32 rows of the weights, a row of d), and x0 y0 + x0 y1 + x1 y0 leaves out 2^-24.  A row of
 // dweight is a token's own, however improbable, so its product keeps float32's range: three bfloat16 planes (x0 + x1 + x2 to 2^-25)
-// and the six terms x_i y_j with i + j <= 2.  (Six terms everywhere: 509 x 50021 x 1001 forward 360 us, 229 so.)
+// and the six terms x_i y_j with i + j <= 2.  (Six terms everywhere took the forward of 509 x 50021 x 1001 1.6 times as long.)
 // The tensor core adds to its float32 accumulator without rounding to nearest, so a long K drifts:
 // float32 products, and long rows' logits in the forward, leave the tensor core every few chunks and are
 // added up in registers.
 // What bounds it: 16-bit products wait for L2 (a pair reads 64 KB for 512 cycles of its tensor cores; 42 to 46 bytes per cycle reach an SM,
-// the tensor cores are 70 to 75 % busy: 1340 TFLOP/s in the forward of 4096 x 131072 x 4096, and the power limit in long runs), float32 ones
-// for the tensor cores (98 % busy, since a chunk's planes are read once for all terms).  One or two rows (four of float32) have a kernel without them.
+// the tensor cores are 68 to 75 % busy: 1340 TFLOP/s in the forward of 4096 x 131072 x 4096, and the power limit in long runs), float32 ones
+// for the tensor cores (82 to 94 % busy, since a chunk's planes are read once for all terms) and their sums' way out of them.  One or two rows (four of float32) have a kernel without them.
 // Every wait is bounded (see mbar_wait); a block whose wait runs out reports it and gives NaN for its tiles.
 #pragma once
 #include "tc_common.cuh"

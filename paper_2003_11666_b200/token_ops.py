@@ -198,7 +198,7 @@ def _scratch(who, t):
 
 
 def head_scratch_bytes(hidden, weight, backward=False):
-    """pb_head_scratch_bytes: bytes of scratch that head_logprob_forward (or _backward) needs for these tensors."""
+    """pb_head_scratch_bytes: bytes of scratch that head_logprob_forward (or _backward) needs for these tensors, and for fewer rows of hidden states."""
     who = "head_scratch_bytes"
     if not isinstance(hidden, torch.Tensor) or not isinstance(weight, torch.Tensor):
         _refuse(who, "hidden and weight must be tensors")
@@ -361,7 +361,7 @@ def join_forward(x, u, y, h=None, pre_weight=None, post_weight=None, gate=None, 
 
 
 def join_scratch_bytes(rows, dim, rows_per_gate=0):
-    """pb_join_scratch_bytes: bytes of scratch that join_backward needs for these sizes (rows_per_gate 0: no gate)."""
+    """pb_join_scratch_bytes: bytes of scratch that join_backward needs for these sizes, and for fewer rows (rows_per_gate 0: no gate)."""
     n = _lib.pb_join_scratch_bytes(int(rows), int(dim), int(rows_per_gate))
     if n == 0:
         _refuse("join_scratch_bytes", "sizes out of range")
